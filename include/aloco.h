@@ -513,6 +513,156 @@ int aloco_adamw_step_normed(void *const *params, const void *const *grads,
                             aloco_adamw_stats_t *stats_out);
 
 /* ------------------------------------------------------------------------
+ * Post-training losses.  The paper tunes a language model between its
+ * synchronisations (UltraChat SFT, Tab. training settings) and takes the
+ * gradients as given; these entry points are the losses of preference and
+ * policy tuning, with their gradients by the logits, and the log-probabilities
+ * of given tokens that both losses compare with.
+ *
+ * For a row x[0..V) of logits with its token a and the temperature tau:
+ *   y = x / tau,   logp = y[a] - log sum_j exp(y_j),   p_j = exp(y_j) / sum
+ * in fp32 with the row's maximum taken out first.  Logits of -inf (tokens that
+ * may not be drawn) have probability 0; a row of nothing else, and one that
+ * holds NaN or +inf, has logp NaN, as has a token >= V.  A row that takes no
+ * part (a negative token, or a weight of 0 in the policy loss) is never read:
+ * its logp is 0 and its gradient row is zeros.
+ *
+ * Every buffer is device memory of the current device.  The calls only
+ * enqueue on opts->stream (the other options do not apply) and allocate
+ * nothing; sums are taken in a fixed order, so that results are bit-identical
+ * from call to call.  Scratch is the caller's: calls that may overlap on the
+ * GPU need their own.  Gradients have the logits' dtype and may be written
+ * over the logits themselves (same address and strides); otherwise no output
+ * may overlap an input or another output.
+ * ---------------------------------------------------------------------- */
+
+#define ALOCO_MAX_VOCAB 262144
+
+/* Logits and their tokens: batch sequences of `rows` positions, V = vocab
+ * logits each.  Row (b, r) starts batch_stride * b + row_stride * r elements
+ * after `logits` (so that a view without each sequence's last position, or one
+ * of logits that lie position by position, is taken as it is); rows may not
+ * overlap.  targets is [batch * rows] int32 or int64, contiguous, as is
+ * every other array of one value per row.  Any alignment to the element size
+ * is accepted. */
+typedef struct aloco_tokens {
+    const void *logits;
+    const void *targets;
+    int64_t batch, rows, vocab;         /* vocab in [1, ALOCO_MAX_VOCAB]   */
+    int64_t batch_stride, row_stride;   /* elements                        */
+    double temperature;                 /* tau, in [1e-6, 1e6]             */
+    int32_t dtype;                      /* aloco_dtype of the logits       */
+    int32_t target_bytes;               /* 4 or 8                          */
+} aloco_tokens_t;
+
+/* A gradient by the logits, in the logits' dtype: row (b, r) starts
+ * batch_stride * b + row_stride * r elements after `data`; strides as
+ * aloco_tokens_t. */
+typedef struct aloco_logits_grad {
+    void *data;
+    int64_t batch_stride, row_stride;
+} aloco_logits_grad_t;
+
+/* logp[batch * rows] of the tokens. */
+int aloco_token_logprobs(const aloco_tokens_t *tokens, float *logp,
+                         const aloco_opts_t *opts);
+
+/* Bytes of scratch for a loss over that many rows (batch * rows). */
+size_t aloco_loss_scratch_bytes(int64_t rows);
+
+typedef struct aloco_policy_cfg {
+    double clip_low;    /* the ratio is clipped to [1 - clip_low,           */
+    double clip_high;   /*   1 + clip_high]; finite, >= 0                   */
+    double kl_coef;     /* weight of the KL term, finite, >= 0              */
+} aloco_policy_cfg_t;
+
+/* Clipped policy loss with a KL term.  With r = exp(logp - old_logp),
+ * d = ref_logp - logp and the rows' advantages A and weights w (a mask
+ * divided by its sum gives the mean over tokens):
+ *   L = sum w [ -min(r A, clip(r) A) + kl_coef (exp(d) - d - 1) ]
+ *   dL/dlogp = w [ -A r [r A <= clip(r) A] + kl_coef (1 - exp(d)) ]
+ *   dL/dx_j  = dL/dlogp / tau ([j = a] - p_j)
+ * terms[4]: L, sum w (-min(..)), sum w (exp(d) - d - 1) and the weight of the
+ * rows whose ratio was clipped.  ref_logp may be NULL with kl_coef = 0 (the
+ * KL sum is then 0).  grad may be NULL (terms and logp only).  scratch: at
+ * least aloco_loss_scratch_bytes(batch * rows), 16-byte aligned. */
+int aloco_policy_loss(const aloco_tokens_t *tokens, const float *advantages,
+                      const float *old_logp, const float *ref_logp,
+                      const float *weights, const aloco_policy_cfg_t *cfg,
+                      float *terms, float *logp,
+                      const aloco_logits_grad_t *grad, void *scratch,
+                      size_t scratch_bytes, const aloco_opts_t *opts);
+
+typedef struct aloco_preference_cfg {
+    double beta;             /* scale of the log ratios, finite, > 0        */
+    double label_smoothing;  /* share eps of flipped labels, in [0, 1)      */
+} aloco_preference_cfg_t;
+
+/* Preference loss of paired log ratios.  Sequence i covers the rows
+ * [cu_seqlens[i], cu_seqlens[i + 1]) of the batch * rows rows taken in order;
+ * sequences 2k and 2k + 1 are pair k's chosen and rejected answers:
+ *   R_i = sum over the sequence's rows that take part of logp - ref_logp
+ *   z_k = beta (R_2k - R_2k+1)
+ *   L   = mean_k [ -(1 - eps) log sigmoid(z_k) - eps log sigmoid(-z_k) ]
+ *   dL/dlogp = +-(beta / pairs) (sigmoid(z_k) - 1 + eps)
+ *                                     (+ in the chosen, - in the rejected)
+ * cu_seqlens is a device array [2 pairs + 1] of cu_bytes (4 or 8) byte
+ * integers, non-decreasing (values outside [0, batch * rows] are taken as the
+ * nearer end); rows of no sequence have zero gradients.  ref_logp may be NULL
+ * (no reference: 0).  Outputs: loss[1], log_ratios[2 pairs] = R, logp and
+ * grad as aloco_policy_loss.  pairs = 0 is allowed (L = 0). */
+int aloco_preference_loss(const aloco_tokens_t *tokens, const float *ref_logp,
+                          const void *cu_seqlens, int32_t cu_bytes,
+                          int64_t pairs, const aloco_preference_cfg_t *cfg,
+                          float *loss, float *log_ratios, float *logp,
+                          const aloco_logits_grad_t *grad, void *scratch,
+                          size_t scratch_bytes, const aloco_opts_t *opts);
+
+/* ------------------------------------------------------------------------
+ * Global gradient norm over many tensors, and clipping (Tab. training
+ * settings: gradient-norm clipping 1.0).  aloco_adamw_step clips one flat
+ * gradient per replica; these take the gradients where a backward pass leaves
+ * them, in tensors of their own, and can put them, clipped, into the flat
+ * vector the step takes.
+ * ---------------------------------------------------------------------- */
+
+/* The gradient tensors of one model: a handle that keeps their addresses on
+ * the device.  The tensors stay the caller's and must stay where they are. */
+typedef struct aloco_grads aloco_grads_t;
+
+/* n >= 0 tensors: grads[i] has sizes[i] >= 0 contiguous elements of dtypes[i]
+ * (aloco_dtype).  Allocates device memory (the handle's table and partial
+ * sums) on the current device and waits for its upload. */
+int aloco_grads_create(const void *const *grads, const int64_t *sizes,
+                       const int32_t *dtypes, int64_t n,
+                       aloco_grads_t **out);
+
+/* Free a handle (NULL: nothing) after the work enqueued with it is done. */
+void aloco_grads_destroy(aloco_grads_t *grads);
+
+/* norm[1] (device fp32) = sqrt(sum of all g^2).  Squares are added in fp32
+ * over at most 32 elements and then in fp64, in a fixed order; values whose
+ * squares leave fp32's range are squared in fp64.  NaN or inf where a
+ * gradient is.  Enqueues one kernel on opts->stream.  Calls with one handle
+ * share its partial sums: calls that overlap on the GPU race. */
+int aloco_grad_norm(aloco_grads_t *grads, float *norm,
+                    const aloco_opts_t *opts);
+
+/* Clip: c = min(1, max_norm / (norm + 1e-6)), as aloco_adamw_step forms it
+ * (a norm of inf gives c = 0, and inf * 0 = NaN where the inf was; NaN gives
+ * NaN everywhere), and every g becomes c g, rounded once.
+ *   out = NULL: in place (nothing is written where c = 1); the tensors may
+ *     not overlap one another;
+ *   else out is a flat vector of out_dtype that receives tensor after tensor
+ *     in the handle's order, and the tensors are only read.  It may overlap
+ *     none of them.
+ * max_norm is finite and > 0.  norm[1] receives the norm before clipping.
+ * Enqueues two kernels. */
+int aloco_clip_grads(aloco_grads_t *grads, double max_norm, void *out,
+                     aloco_dtype out_dtype, float *norm,
+                     const aloco_opts_t *opts);
+
+/* ------------------------------------------------------------------------
  * Interval controller (Sec. 3.1; App. A).  Host-only and scalar: after each
  * completed interval it takes that interval's D_t, C_t, accumulated inner
  * learning rate and token count, assesses them against the accepted-horizon

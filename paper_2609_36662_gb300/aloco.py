@@ -11,9 +11,10 @@ import ctypes
 import os
 import struct
 from dataclasses import dataclass
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence
 
 MAX_WORKERS = 32
+MAX_VOCAB = 262144
 
 F32, BF16 = 0, 1
 SCHED_COSINE, SCHED_CONSTANT, SCHED_LINEAR = 0, 1, 2
@@ -40,6 +41,9 @@ EXPORTS = ("aloco_default_opts", "aloco_inner_lr_accum", "aloco_correction",
            "aloco_sync_int8", "aloco_int8_num_blocks", "aloco_int8_encode",
            "aloco_int8_decode", "aloco_adamw_default_cfg", "aloco_adamw_step",
            "aloco_adamw_step_normed",
+           "aloco_token_logprobs", "aloco_loss_scratch_bytes", "aloco_policy_loss",
+           "aloco_preference_loss", "aloco_grads_create", "aloco_grads_destroy",
+           "aloco_grad_norm", "aloco_clip_grads",
            "aloco_ctrl_default_cfg", "aloco_ctrl_init", "aloco_select_interval",
            "aloco_ctrl_state_bytes", "aloco_ctrl_save", "aloco_ctrl_load",
            "aloco_test_stall_tile", "aloco_last_error", "aloco_shutdown",
@@ -91,6 +95,29 @@ class AdamwStats(ctypes.Structure):
         return {"grad_norm": list(self.grad_norm[:self.M]),
                 "clip": list(self.clip[:self.M]), "M": self.M,
                 "grid": self.grid, "kernel_ms": self.kernel_ms}
+
+
+class Tokens(ctypes.Structure):
+    """aloco_tokens_t: logits and their tokens."""
+    _fields_ = [("logits", ctypes.c_void_p), ("targets", ctypes.c_void_p),
+                ("batch", ctypes.c_int64), ("rows", ctypes.c_int64),
+                ("vocab", ctypes.c_int64), ("batch_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64), ("temperature", ctypes.c_double),
+                ("dtype", ctypes.c_int32), ("target_bytes", ctypes.c_int32)]
+
+
+class LogitsGrad(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64)]
+
+
+class PolicyCfg(ctypes.Structure):
+    _fields_ = [("clip_low", ctypes.c_double), ("clip_high", ctypes.c_double),
+                ("kl_coef", ctypes.c_double)]
+
+
+class PreferenceCfg(ctypes.Structure):
+    _fields_ = [("beta", ctypes.c_double), ("label_smoothing", ctypes.c_double)]
 
 
 class Correction(ctypes.Structure):
@@ -249,6 +276,25 @@ def load():
                                             i32, i32, P(AdamwCfg), vp, P(Opts),
                                             P(AdamwStats)]
     lib.aloco_adamw_step_normed.restype = i32
+    lib.aloco_token_logprobs.argtypes = [P(Tokens), vp, P(Opts)]
+    lib.aloco_token_logprobs.restype = i32
+    lib.aloco_loss_scratch_bytes.argtypes = [i64]
+    lib.aloco_loss_scratch_bytes.restype = ctypes.c_size_t
+    lib.aloco_policy_loss.argtypes = [P(Tokens), vp, vp, vp, vp, P(PolicyCfg), vp, vp,
+                                      P(LogitsGrad), vp, ctypes.c_size_t, P(Opts)]
+    lib.aloco_policy_loss.restype = i32
+    lib.aloco_preference_loss.argtypes = [P(Tokens), vp, vp, ctypes.c_int32, i64,
+                                          P(PreferenceCfg), vp, vp, vp, P(LogitsGrad), vp,
+                                          ctypes.c_size_t, P(Opts)]
+    lib.aloco_preference_loss.restype = i32
+    lib.aloco_grads_create.argtypes = [vp, vp, vp, i64, P(vp)]
+    lib.aloco_grads_create.restype = i32
+    lib.aloco_grads_destroy.argtypes = [vp]
+    lib.aloco_grads_destroy.restype = None
+    lib.aloco_grad_norm.argtypes = [vp, vp, P(Opts)]
+    lib.aloco_grad_norm.restype = i32
+    lib.aloco_clip_grads.argtypes = [vp, dbl, vp, i32, vp, P(Opts)]
+    lib.aloco_clip_grads.restype = i32
     lib.aloco_sync_host.argtypes = sync_args + [ctypes.c_size_t, P(Opts), P(Stats)]
     lib.aloco_sync_host.restype = i32
     lib.aloco_sync_shard.argtypes = sync_args + [P(Opts), P(Partials)]
@@ -718,3 +764,304 @@ def test_stall_tile(tile: int):
     """Testing only: the next bulk-copy round on this thread skips the copies
     of one tile, so that its bounded wait runs out (aloco_test_stall_tile)."""
     load().aloco_test_stall_tile(int(tile))
+
+
+# -------------------------------------------- post-training losses and gradients
+
+class PolicyLoss(NamedTuple):
+    """terms: float32 [4] (the loss, its policy term, its KL term before the
+    coefficient, the weight of the clipped rows); logp: float32, the tokens'
+    log-probabilities; grad: the gradient by the logits, or None."""
+    terms: object
+    logp: object
+    grad: object
+
+
+class PreferenceLoss(NamedTuple):
+    """loss: float32 scalar; log_ratios: float32 [2 pairs], the sequences' sums
+    of logp - ref_logp; logp: float32, the tokens' log-probabilities; grad: the
+    gradient by the logits, or None."""
+    loss: object
+    log_ratios: object
+    logp: object
+    grad: object
+
+
+class _OtherStream:
+    """The context of a call on a stream that is not the current one: what the
+    call allocates belongs to that stream, and the memory of what it is given
+    or returns is not handed out again before both are past it."""
+
+    def __init__(self, stream, current, inputs):
+        import torch
+        self.current = current
+        self.stream = stream
+        self.inner = torch.cuda.stream(stream)
+        self.inputs = inputs
+
+    def __enter__(self):
+        self.inner.__enter__()
+
+    def __exit__(self, *exc):
+        self.inner.__exit__(*exc)
+        for t in self.inputs:
+            if t is not None:
+                t.record_stream(self.stream)
+        return False
+
+
+def _on_stream(stream, device, inputs):
+    """(context, raw stream handle) of a call."""
+    if stream is not None:
+        import torch
+        current = torch.cuda.current_stream(device)
+        if stream != current:
+            return _OtherStream(stream, current, inputs), stream.cuda_stream
+    return _on_device(device), _stream_of(None, device)
+
+
+def _finish(rc, ctx, *outputs):
+    """Raise what a call reported; hand its outputs to the current stream."""
+    if rc != OK:
+        raise AlocoError(rc, last_error())
+    if isinstance(ctx, _OtherStream):
+        for t in outputs:
+            if t is not None:
+                t.record_stream(ctx.current)
+
+
+def _tokens(logits, targets, temperature) -> Tokens:
+    """The descriptor of [rows, V] or [batch, rows, V] logits and their targets."""
+    import torch
+    dtype = logits.dtype
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
+        raise TypeError(f"logits must be float32 or bfloat16, not {dtype}")
+    shape, strides = logits.shape, logits.stride()
+    if len(shape) == 3:
+        batch, rows, vocab = shape
+        batch_stride, row_stride, last = strides
+    elif len(shape) == 2:
+        (rows, vocab), batch = shape, 1
+        batch_stride, (row_stride, last) = 0, strides
+    else:
+        raise ValueError("logits must be [rows, vocab] or [batch, rows, vocab]")
+    if last != 1 and vocab > 1:
+        raise ValueError("the logits of a row must be contiguous")
+    if targets.dtype is torch.int64:
+        size = 8
+    elif targets.dtype is torch.int32:
+        size = 4
+    else:
+        raise TypeError(f"targets must be int32 or int64, not {targets.dtype}")
+    if targets.shape != shape[:-1] or not targets.is_contiguous():
+        raise ValueError(f"targets must be contiguous of shape {tuple(shape[:-1])}")
+    if not logits.is_cuda or targets.device != logits.device:
+        raise ValueError("logits and targets must be CUDA tensors of one device")
+    return Tokens(logits.data_ptr(), targets.data_ptr(), batch, rows, vocab, batch_stride,
+                  row_stride, temperature, F32 if dtype is torch.float32 else BF16, size)
+
+
+def _per_row(name, t, logits) -> int:
+    """The address of a float32 tensor of one value per row."""
+    import torch
+    if t.dtype is not torch.float32 or not t.is_contiguous() or t.device != logits.device \
+            or t.shape != logits.shape[:-1]:
+        raise ValueError(f"{name} must be a contiguous float32 tensor of shape "
+                         f"{tuple(logits.shape[:-1])} on the logits' device")
+    return t.data_ptr()
+
+
+def _logits_grad(logits, grad, want_grad):
+    """(gradient tensor, its descriptor): `grad`, or a new one."""
+    import torch
+    if grad is None:
+        if not want_grad:
+            return None, None
+        grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    elif grad.dtype != logits.dtype or grad.shape != logits.shape or \
+            grad.device != logits.device or (grad.stride(-1) != 1 and grad.shape[-1] > 1):
+        raise ValueError("grad must have the logits' shape, dtype and device, with "
+                         "contiguous rows")
+    st = grad.stride()
+    return grad, LogitsGrad(grad.data_ptr(), st[0] if len(st) == 3 else 0, st[-2])
+
+
+def token_logprobs(logits, targets, *, temperature: float = 1.0, stream=None):
+    """Log-probabilities of the tokens `targets` (int32 or int64, [rows] or
+    [batch, rows]) under logits [..., V] / temperature (float32 or bfloat16 CUDA
+    tensor with contiguous rows and any strides between them); 0 where a
+    target is negative.  float32, in targets' shape."""
+    import torch
+    tok = _tokens(logits, targets, temperature)
+    device = logits.device
+    ctx, handle = _on_stream(stream, device, (logits, targets))
+    opts = Opts(stream=handle)
+    with ctx:
+        logp = torch.empty(targets.shape, dtype=torch.float32, device=device)
+        rc = load().aloco_token_logprobs(ctypes.byref(tok), logp.data_ptr(),
+                                         ctypes.byref(opts))
+    _finish(rc, ctx, logp)
+    return logp
+
+
+def policy_loss(logits, targets, advantages, old_logp, weights, *, ref_logp=None,
+                clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0,
+                temperature: float = 1.0, grad=None, want_grad: bool = True,
+                stream=None) -> PolicyLoss:
+    """Clipped policy loss with a KL term over the rows of `logits`, and its
+    gradient by them (aloco_policy_loss).  advantages, old_logp, weights and
+    ref_logp are float32 of targets' shape; rows of weight 0 or a negative
+    target take no part.  grad (optional) receives the gradient and may be
+    `logits` itself; without it a new tensor does, unless want_grad is False.
+    Enqueues only."""
+    import torch
+    tok = _tokens(logits, targets, temperature)
+    device = logits.device
+    adv, old, w = (_per_row("advantages", advantages, logits),
+                   _per_row("old_logp", old_logp, logits), _per_row("weights", weights, logits))
+    ref = _per_row("ref_logp", ref_logp, logits) if ref_logp is not None else None
+    cfg = PolicyCfg(clip_low, clip_high, kl_coef)
+    ctx, handle = _on_stream(stream, device, (logits, targets, advantages, old_logp, weights,
+                                              ref_logp, grad))
+    opts = Opts(stream=handle)
+    lib = load()
+    with ctx:
+        out, desc = _logits_grad(logits, grad, want_grad)
+        n = targets.numel()
+        terms = torch.empty(4, dtype=torch.float32, device=device)
+        logp = torch.empty(targets.shape, dtype=torch.float32, device=device)
+        need = lib.aloco_loss_scratch_bytes(n)
+        scratch = torch.empty(need, dtype=torch.uint8, device=device)
+        rc = lib.aloco_policy_loss(ctypes.byref(tok), adv, old, ref, w, ctypes.byref(cfg),
+                                   terms.data_ptr(), logp.data_ptr(),
+                                   ctypes.byref(desc) if desc is not None else None,
+                                   scratch.data_ptr(), need, ctypes.byref(opts))
+    _finish(rc, ctx, terms, logp, out)
+    return PolicyLoss(terms, logp, out)
+
+
+def preference_loss(logits, targets, cu_seqlens, ref_logp=None, *, beta: float = 0.1,
+                    label_smoothing: float = 0.0, temperature: float = 1.0, grad=None,
+                    want_grad: bool = True, stream=None) -> PreferenceLoss:
+    """Preference loss of paired log ratios, and its gradient by the logits
+    (aloco_preference_loss).  cu_seqlens (int32 or int64 CUDA tensor [2 pairs +
+    1]) bounds the sequences among the rows taken in order, chosen and rejected
+    answers in turn; rows with a negative target (prompts, padding) take no
+    part.  ref_logp is float32 of targets' shape (None: no reference).  grad
+    and want_grad as policy_loss.  Enqueues only."""
+    import torch
+    tok = _tokens(logits, targets, temperature)
+    device = logits.device
+    ref = _per_row("ref_logp", ref_logp, logits) if ref_logp is not None else None
+    if cu_seqlens.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"cu_seqlens must be int32 or int64, not {cu_seqlens.dtype}")
+    if cu_seqlens.dim() != 1 or cu_seqlens.numel() % 2 == 0 or \
+            not cu_seqlens.is_contiguous() or cu_seqlens.device != device:
+        raise ValueError("cu_seqlens must be a contiguous vector of 2 pairs + 1 bounds on the "
+                         "logits' device")
+    pairs = cu_seqlens.numel() // 2
+    cfg = PreferenceCfg(beta, label_smoothing)
+    ctx, handle = _on_stream(stream, device, (logits, targets, cu_seqlens, ref_logp, grad))
+    opts = Opts(stream=handle)
+    lib = load()
+    with ctx:
+        out, desc = _logits_grad(logits, grad, want_grad)
+        n = targets.numel()
+        loss = torch.empty((), dtype=torch.float32, device=device)
+        ratios = torch.empty(2 * pairs, dtype=torch.float32, device=device)
+        logp = torch.empty(targets.shape, dtype=torch.float32, device=device)
+        need = lib.aloco_loss_scratch_bytes(n)
+        scratch = torch.empty(need, dtype=torch.uint8, device=device)
+        rc = lib.aloco_preference_loss(
+            ctypes.byref(tok), ref, cu_seqlens.data_ptr(), cu_seqlens.element_size(), pairs,
+            ctypes.byref(cfg), loss.data_ptr(), ratios.data_ptr(), logp.data_ptr(),
+            ctypes.byref(desc) if desc is not None else None, scratch.data_ptr(), need,
+            ctypes.byref(opts))
+    _finish(rc, ctx, loss, ratios, logp, out)
+    return PreferenceLoss(loss, ratios, logp, out)
+
+
+class GradList:
+    """The gradient tensors of one model (contiguous float32 or bfloat16 CUDA
+    tensors of one device, in the order of the flat vector), kept for
+    grad_norm and clip_grads step after step.  It holds the tensors; one whose
+    memory has moved since is refused."""
+
+    def __init__(self, tensors):
+        import torch
+        self._handle = None
+        self.tensors = list(tensors)
+        if not self.tensors:
+            raise ValueError("need at least one gradient")
+        self.device = self.tensors[0].device
+        for t in self.tensors:
+            if t.dtype not in (torch.float32, torch.bfloat16):
+                raise TypeError(f"unsupported gradient dtype {t.dtype}")
+            if not t.is_cuda or t.device != self.device or not t.is_contiguous():
+                raise ValueError("gradients must be contiguous CUDA tensors of one device")
+        n = len(self.tensors)
+        self._at = [t.data_ptr() for t in self.tensors]
+        sizes = [t.numel() for t in self.tensors]
+        self.numel = sum(sizes)
+        handle = ctypes.c_void_p()
+        with _on_device(self.device):
+            rc = load().aloco_grads_create(
+                (ctypes.c_void_p * n)(*self._at), (ctypes.c_int64 * n)(*sizes),
+                (ctypes.c_int32 * n)(*[_replica_dtype_code(t) for t in self.tensors]), n,
+                ctypes.byref(handle))
+        if rc != OK:
+            raise AlocoError(rc, last_error())
+        self._handle = handle
+
+    def _check(self):
+        if [t.data_ptr() for t in self.tensors] != self._at:
+            raise ValueError("a gradient's memory has moved since the GradList was made")
+
+    def __del__(self):
+        if getattr(self, "_handle", None) is not None and _lib is not None:
+            _lib.aloco_grads_destroy(self._handle)
+            self._handle = None
+
+
+def _grad_list(grads) -> GradList:
+    if not isinstance(grads, GradList):
+        return GradList(grads)
+    grads._check()
+    return grads
+
+
+def grad_norm(grads, *, stream=None):
+    """Global norm of a GradList (or of a sequence of tensors, which costs a new
+    list each time): a float32 scalar tensor.  Enqueues only."""
+    import torch
+    g = _grad_list(grads)
+    ctx, handle = _on_stream(stream, g.device, g.tensors)
+    opts = Opts(stream=handle)
+    with ctx:
+        norm = torch.empty((), dtype=torch.float32, device=g.device)
+        rc = load().aloco_grad_norm(g._handle, norm.data_ptr(), ctypes.byref(opts))
+    _finish(rc, ctx, norm)
+    return norm
+
+
+def clip_grads(grads, max_norm: float, *, out=None, stream=None):
+    """Scale the gradients by min(1, max_norm / (norm + 1e-6)): in place, or,
+    with `out` (a contiguous float32 or bfloat16 vector of all their elements),
+    into it, tensor after tensor, as adamw_step takes them.  Returns the norm
+    before clipping, a float32 scalar tensor.  Enqueues only."""
+    import torch
+    g = _grad_list(grads)
+    if out is not None and (out.numel() != g.numel or not out.is_contiguous() or
+                            out.device != g.device):
+        raise ValueError(f"out must be a contiguous vector of {g.numel} elements on the "
+                         "gradients' device")
+    dtype = _replica_dtype_code(out) if out is not None else F32
+    ctx, handle = _on_stream(stream, g.device, g.tensors if out is None else [*g.tensors, out])
+    opts = Opts(stream=handle)
+    with ctx:
+        norm = torch.empty((), dtype=torch.float32, device=g.device)
+        rc = load().aloco_clip_grads(g._handle, max_norm,
+                                     out.data_ptr() if out is not None else None, dtype,
+                                     norm.data_ptr(), ctypes.byref(opts))
+    _finish(rc, ctx, norm)
+    return norm

@@ -1,0 +1,36 @@
+// Internal interface of the gradient-list operators (norm, clipping).
+#pragma once
+
+#include "aloco_internal.h"
+
+namespace aloco {
+
+// A stretch of one tensor: at most kGradChunk elements, from a place that
+// lies to the 16-byte boundaries as the tensor's start does.
+struct GradChunk {
+    void *p;
+    int64_t at;     // its first element's place in the flat vector
+    int32_t n;
+    int32_t bf16;
+};
+
+constexpr int kGradBlock = 256;
+
+struct GradArgs {
+    const GradChunk *chunks;
+    int n_chunks;
+    double *partials;       // [grid]
+    unsigned int *ticket;   // 0 between launches
+    double *factor;         // clipping factor
+    float *norm;
+    double max_norm;        // <= 0: no factor
+    void *out;              // null: in place
+    int out_bf16;
+};
+
+// Blocks of the norm pass on a device of that many SMs (partials' length).
+int grad_norm_blocks(int sm_count, int n_chunks);
+cudaError_t launch_grad_norm(const GradArgs &a, int sm_count, cudaStream_t stream);
+cudaError_t launch_grad_scale(const GradArgs &a, int sm_count, cudaStream_t stream);
+
+}  // namespace aloco

@@ -1,0 +1,50 @@
+// Internal interface of the post-training losses: what aloco_losses.cpp checks
+// and fills in, and what the kernels of aloco_logits.cu take by value.
+#pragma once
+
+#include "aloco_internal.h"
+
+namespace aloco {
+
+// Rows of a [batch, rows, vocab] array with strides (elements).
+struct Rows {
+    char *data;
+    int64_t per_batch;               // rows of one sequence
+    int64_t batch_stride, row_stride;
+};
+
+// Per-row terms of the policy loss, summed by its last kernel: one float each
+// for L's three sums.
+constexpr int kTerms = 3;
+
+struct LogitsArgs {
+    Rows x, g;                       // logits; gradient (g.data null: none)
+    int64_t n;                       // rows
+    int vocab;
+    const void *target;
+    int target_bytes, cu_bytes;
+    float inv_temp;                  // 1 / tau
+    float scale, scale_lo;           // log2(e) / tau as a sum, scale_lo > 0
+    float *logp;                     // [n]
+    // policy loss
+    const float *adv, *old, *ref, *w;
+    float lo, hi, kl;                // 1 - clip_low, 1 + clip_high, kl_coef
+    float *terms;                    // [n][kTerms] per row (scratch)
+    float *terms_out;                // [kTerms + 1]
+    // preference loss (ref as above)
+    const void *cu;
+    int64_t pairs;
+    double beta, eps;
+    float2 *stats;                   // [n] row maximum and 1 / sum (scratch)
+    float *coef;                     // [n] dL/dlogp (scratch)
+    float *loss, *ratios;
+};
+
+cudaError_t launch_token_logprobs(const LogitsArgs &a, aloco_dtype dtype, int sm_count,
+                                  cudaStream_t stream);
+cudaError_t launch_policy_loss(const LogitsArgs &a, aloco_dtype dtype, int sm_count,
+                               cudaStream_t stream);
+cudaError_t launch_preference_loss(const LogitsArgs &a, aloco_dtype dtype, int sm_count,
+                                   cudaStream_t stream);
+
+}  // namespace aloco
