@@ -6,21 +6,28 @@
 //   logp = (x_a - m) / tau - log z,   p_j = exp((x_j - m) / tau) / z
 //   dL/dx_j = k ([j = a] - p_j),  k = dL/dlogp / tau.
 //
-// Row kernel: a cluster of C CTAs holds a row in its registers, 16-byte units
-// of it in a fixed pattern per thread.  Every thread turns its elements into
-// exp((x - own maximum) / tau) once; one reduction over (maximum, sum) pairs
-// (warp, CTA, and through distributed shared memory the cluster) gives m and
-// z, and the gradient is each kept value times one factor per thread.  The
-// logits are thus read once and the gradient written once.
+// Row kernel: persistent clusters take the rows in turn.  Each CTA has a
+// producer warp that copies its part of the rows ahead into a ring in shared
+// memory (cp.async.bulk), so that HBM is read while the consumers compute,
+// reduce and store; the consumers take a row's part into registers, turn it
+// into exp((x - own maximum) / tau) once, and reduce (maximum, sum) pairs over
+// warp, CTA and, through distributed shared memory, the cluster.  The gradient
+// is each kept value times one factor per thread: the logits are read once and
+// the gradient is written once.
 // The preference loss needs every row of a pair before any of its gradients:
 // its first kernel leaves m and 1/z of every row, its second adds the log
 // ratios, and its third reads the logits again.
 //
 // A row may start off a 16-byte boundary (odd vocabularies): the units are
-// those of the aligned window around it, and the two at its ends are read and
-// written element by element.
+// those of the aligned window around it; whole ones are copied, and the two at
+// its ends are read and written element by element.
+#include <limits.h>
+
+#include <type_traits>
+
 #include <cooperative_groups.h>
 
+#include "aloco_bulk.cuh"
 #include "aloco_logits.h"
 #include "aloco_sync_kernel.cuh"
 
@@ -30,7 +37,17 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kFwd = 0, kPolicy = 1, kPref = 2;  // what a row kernel leaves
+// Wait until the kernel before this one in the stream has completed (at once
+// where this launch is not serialised programmatically).
+__device__ __forceinline__ void wait_for_previous() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
+// What a row kernel leaves: log-probabilities, also a gradient, the same where
+// the gradient's rows may lie otherwise to the 16-byte boundaries than the
+// logits' do, or what the preference loss needs of a row.
+constexpr int kFwd = 0, kPolicy = 1, kPolicyShifted = 2, kPref = 3;
+constexpr bool has_grad(int mode) { return mode == kPolicy || mode == kPolicyShifted; }
 
 template <bool BF16>
 struct Unit {
@@ -47,17 +64,17 @@ struct Window {
 };
 
 template <bool BF16>
+__device__ __forceinline__ Window window_at(char *base, int head, int vocab) {
+    const int end = head + vocab;
+    return {base, head, end, (end + Unit<BF16>::kElems - 1) / Unit<BF16>::kElems};
+}
+template <bool BF16>
 __device__ __forceinline__ Window window_of(const Rows &r, int64_t row, int vocab) {
-    const int64_t b = row / r.per_batch;
-    char *p = r.data + (b * r.batch_stride + (row - b * r.per_batch) * r.row_stride) *
-                           Unit<BF16>::kSize;
-    Window w;
+    const uint32_t per = (uint32_t)r.per_batch, b = (uint32_t)row / per;  // rows < 2^31
+    char *p = r.data + ((int64_t)b * r.batch_stride +
+                        (int64_t)((uint32_t)row - b * per) * r.row_stride) * Unit<BF16>::kSize;
     const int off = (int)((uintptr_t)p & 15);
-    w.base = p - off;
-    w.head = off / Unit<BF16>::kSize;
-    w.end = w.head + vocab;
-    w.units = (w.end + Unit<BF16>::kElems - 1) / Unit<BF16>::kElems;
-    return w;
+    return window_at<BF16>(p - off, off / Unit<BF16>::kSize, vocab);
 }
 
 template <bool BF16>
@@ -75,64 +92,83 @@ __device__ __forceinline__ void store1(char *base, int e, float v) {
         reinterpret_cast<float *>(base)[e] = v;
 }
 
-// Unit u as floats; places outside the row hold -inf.
+// Unit u of a row; places outside the row hold -inf.
 template <bool BF16>
-__device__ __forceinline__ void load_unit(const Window &w, int u,
-                                          float (&o)[Unit<BF16>::kElems]) {
+__device__ __forceinline__ uint4 load_unit(const Window &w, int u) {
     constexpr int E = Unit<BF16>::kElems;
     const int e0 = u * E;
-    if (e0 >= w.head && e0 + E <= w.end) {
-        const uint4 q = __ldcs(reinterpret_cast<const uint4 *>(w.base) + u);
-        const uint32_t r[4] = {q.x, q.y, q.z, q.w};
+    if (e0 >= w.head && e0 + E <= w.end) return __ldcs(reinterpret_cast<const uint4 *>(w.base) + u);
+    uint32_t r[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if constexpr (BF16) {
-                o[2 * j] = bf16_lo(r[j]);
-                o[2 * j + 1] = bf16_hi(r[j]);
-            } else {
-                o[j] = __uint_as_float(r[j]);
-            }
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (BF16) {
+            const int e = e0 + 2 * j;
+            const uint16_t *p = reinterpret_cast<const uint16_t *>(w.base);
+            const uint32_t a = e >= w.head && e < w.end ? p[e] : 0xff80u;
+            const uint32_t b = e + 1 >= w.head && e + 1 < w.end ? p[e + 1] : 0xff80u;
+            r[j] = a | b << 16;
+        } else {
+            const int e = e0 + j;
+            r[j] = e >= w.head && e < w.end ? reinterpret_cast<const uint32_t *>(w.base)[e]
+                                            : 0xff800000u;
         }
-    } else {
-#pragma unroll
-        for (int j = 0; j < E; ++j)
-            o[j] = e0 + j >= w.head && e0 + j < w.end ? load1<BF16>(w.base, e0 + j) : -INFINITY;
     }
+    return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
-// The unit of elements that is u in the source's window, into a row that may
-// lie otherwise to the 16-byte boundaries (shift: destination head - source
-// head).
+// One 16-byte unit of a row's elements, unit u of the source's window, element
+// by element into a row that may lie otherwise to the 16-byte boundaries.
 template <bool BF16>
-__device__ __forceinline__ void store_unit(const Window &src, const Window &dst, int u,
-                                           const float (&v)[Unit<BF16>::kElems]) {
+__device__ __forceinline__ void store_elems(const Window &src, const Window &dst, int u, uint4 q) {
     constexpr int E = Unit<BF16>::kElems;
     const int e0 = u * E;
-    if (src.head == dst.head && e0 >= src.head && e0 + E <= src.end) {
-        uint4 q;
-        if constexpr (BF16)
-            q = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
-                           pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-        else
-            q = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
-                           __float_as_uint(v[3]));
-        __stcs(reinterpret_cast<uint4 *>(dst.base) + u, q);
-        return;
-    }
-    const int shift = dst.head - src.head;
+    const uint32_t r[4] = {q.x, q.y, q.z, q.w};
+    const int to = e0 + dst.head - src.head;
 #pragma unroll
     for (int j = 0; j < E; ++j)
-        if (e0 + j >= src.head && e0 + j < src.end) store1<BF16>(dst.base, e0 + j + shift, v[j]);
+        if (e0 + j >= src.head && e0 + j < src.end) {
+            if constexpr (BF16)
+                reinterpret_cast<uint16_t *>(dst.base)[to + j] =
+                    (uint16_t)(j & 1 ? r[j / 2] >> 16 : r[j / 2]);
+            else
+                reinterpret_cast<uint32_t *>(dst.base)[to + j] = r[j];
+        }
 }
 
-// Zeros in the units [u0, u1) of a row, by `threads` threads.
+// The elements [lo, hi) of a unit that starts at element e0 of g's window, as
+// far as they lie in the row.
+template <bool BF16>
+__device__ __forceinline__ void store_some(const Window &g, int e0, int lo, int hi,
+                                           const uint4 &q) {
+    constexpr int E = Unit<BF16>::kElems;
+    const uint32_t r[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+        if (j >= lo && j < hi && e0 + j >= g.head && e0 + j < g.end) {
+            if constexpr (BF16)
+                reinterpret_cast<uint16_t *>(g.base)[e0 + j] =
+                    (uint16_t)(j & 1 ? r[j / 2] >> 16 : r[j / 2]);
+            else
+                reinterpret_cast<uint32_t *>(g.base)[e0 + j] = r[j];
+        }
+}
+
+// The same, in one piece where the unit is whole and both rows lie alike.
+template <bool BF16>
+__device__ __forceinline__ void store_unit(const Window &src, const Window &dst, int u,
+                                           const uint4 &q) {
+    constexpr int E = Unit<BF16>::kElems;
+    if (src.head == dst.head && u * E >= src.head && u * E + E <= src.end)
+        __stcs(reinterpret_cast<uint4 *>(dst.base) + u, q);
+    else
+        store_elems<BF16>(src, dst, u, q);
+}
+
+// Zeros in a row's units first, first + step, ...
 template <bool BF16>
 __device__ __forceinline__ void zero_units(const Window &w, int first, int step) {
-    constexpr int E = Unit<BF16>::kElems;
-    float z[E];
-#pragma unroll
-    for (int j = 0; j < E; ++j) z[j] = 0.f;
-    for (int u = first; u < w.units; u += step) store_unit<BF16>(w, w, u, z);
+    for (int u = first; u < w.units; u += step)
+        store_unit<BF16>(w, w, u, make_uint4(0, 0, 0, 0));
 }
 
 __device__ __forceinline__ int64_t load_index(const void *p, int64_t i, int bytes) {
@@ -147,157 +183,741 @@ __device__ __forceinline__ int64_t load_index(const void *p, int64_t i, int byte
 struct Scale {
     float hi, lo;
 };
+constexpr float kLog2e = 1.44269490f, kLog2eLo = 1.3846892e-07f;  // their sum: log2(e)
+
+// Pairs of floats in one 64-bit register: the packed fp32 instructions of
+// sm_100 and later do two per lane.
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 pair(float a, float b) {
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void split(f2 p, float &a, float &b) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p));
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+// 2^x; results below 2^-126 of the row's (or thread's) largest term are 0.
+__device__ __forceinline__ float pow2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float warp_max(float v) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+    return v;
+}
 
 // exp((x - m) / tau).  The difference comes first: a product of the type's
 // lowest value and the scale would leave the range.
 __device__ __forceinline__ float exp_of(float x, float m, Scale s) {
     const float d = x - m;
-    return exp2f(fmaf(d, s.hi, d * s.lo));
+    return pow2(fmaf(d, s.hi, d * s.lo));
+}
+__device__ __forceinline__ f2 exp_of2(f2 x, f2 neg_m, f2 hi, f2 lo) {
+    const f2 d = add2(x, neg_m);
+    float a, b;
+    split(fma2(d, hi, mul2(d, lo)), a, b);
+    return pair(pow2(a), pow2(b));
 }
 
-// (m, s) = the pair of both parts of a row: s counts exp((x - m) / tau).  An
-// empty part has m = -inf and s = 0.
-__device__ __forceinline__ float2 join(float2 a, float2 b, Scale scale) {
-    const float m = fmaxf(a.x, b.x);
-    const float base = m == -INFINITY ? 0.f : m;
-    return make_float2(m, a.y * exp_of(a.x, base, scale) + b.y * exp_of(b.x, base, scale));
+// A 16-byte unit of pairs, rounded to the type.
+template <bool BF16>
+__device__ __forceinline__ uint4 narrow(const f2 (&v)[Unit<BF16>::kElems / 2]) {
+    uint32_t r[4];
+#pragma unroll
+    for (int j = 0; j < Unit<BF16>::kElems / 2; ++j) {
+        float a, b;
+        split(v[j], a, b);
+        if constexpr (BF16) {
+            r[j] = pack_bf16x2(a, b);
+        } else {
+            r[2 * j] = __float_as_uint(a);
+            r[2 * j + 1] = __float_as_uint(b);
+        }
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
-// Row kernel: cluster of C CTAs per row; thread t of CTA c holds the units
-// (c * UPT + k) * THREADS + t, k < UPT.
-template <bool BF16, int THREADS, int UPT, int MODE>
-__global__ void __launch_bounds__(THREADS)
-    row_kernel(const __grid_constant__ LogitsArgs a) {
+// The pairs of a 16-byte unit.
+template <bool BF16>
+__device__ __forceinline__ void widen(const uint4 &q, f2 (&o)[Unit<BF16>::kElems / 2]) {
+    if constexpr (BF16) {
+        o[0] = pair(bf16_lo(q.x), bf16_hi(q.x));
+        o[1] = pair(bf16_lo(q.y), bf16_hi(q.y));
+        o[2] = pair(bf16_lo(q.z), bf16_hi(q.z));
+        o[3] = pair(bf16_lo(q.w), bf16_hi(q.w));
+    } else {
+        o[0] = pair(__uint_as_float(q.x), __uint_as_float(q.y));
+        o[1] = pair(__uint_as_float(q.z), __uint_as_float(q.w));
+    }
+}
+
+// The maximum of N units.  NaN is left to the exponentials, which keep it.
+template <bool BF16, int N>
+__device__ __forceinline__ float max_of(const uint4 *q) {
+    if constexpr (BF16) {
+        __nv_bfloat162 m2 = __floats2bfloat162_rn(-INFINITY, -INFINITY);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const uint32_t w[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                m2 = __hmax2(m2, *reinterpret_cast<const __nv_bfloat162 *>(&w[j]));
+        }
+        return fmaxf(__low2float(m2), __high2float(m2));
+    } else {
+        float m = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            m = fmaxf(fmaxf(m, fmaxf(__uint_as_float(q[k].x), __uint_as_float(q[k].y))),
+                      fmaxf(__uint_as_float(q[k].z), __uint_as_float(q[k].w)));
+        return m;
+    }
+}
+
+// The sum of exp((x - base) / tau) over N units, and with HOLD the terms.
+template <bool BF16, int N, bool HOLD>
+__device__ __forceinline__ float exps_of(const uint4 *q, f2 (*v)[Unit<BF16>::kElems / 2],
+                                         float base, f2 hi, f2 lo) {
+    constexpr int P = Unit<BF16>::kElems / 2;
+    const f2 neg = pair(-base, -base);
+    f2 sums[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        f2 e[P];
+        widen<BF16>(q[k], e);
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            e[j] = exp_of2(e[j], neg, hi, lo);
+            f2 &to = sums[(k * P + j) & 3];
+            to = add2(to, e[j]);
+            if constexpr (HOLD) v[k][j] = e[j];
+        }
+    }
+    float a, b;
+    split(add2(add2(sums[0], sums[1]), add2(sums[2], sums[3])), a, b);
+    return a + b;
+}
+
+// Base of the exponentials of a part whose maximum is m (a part of nothing but
+// -inf, or of nothing, has the sum 0 whatever the base).
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
+
+// The maximum and the sum of n <= 32 parts in shared memory: (m, s) with s
+// counting exp((x - m) / tau); a part of nothing is (-inf, 0).
+__device__ __forceinline__ float2 join_parts(const float2 *parts, int n, int lane, Scale scale) {
+    const float2 mine = lane < n ? parts[lane] : make_float2(-INFINITY, 0.f);
+    const float m = warp_max(mine.x);
+    return make_float2(m, warp_sum(mine.y * exp_of(mine.x, base_of(m), scale)));
+}
+
+// -------------------------------------------------------------- row kernel
+
+// The part of a row's units that CTA `rank` of 2^log_c holds.
+struct Part {
+    int first, count;
+};
+__device__ __forceinline__ Part part_of(int units, int rank, int log_c) {
+    const int per = (units + (1 << log_c) - 1) >> log_c;
+    const int first = min(rank * per, units);
+    return {first, min(per, units - first)};
+}
+
+// The units at a row's ends that are not whole: lanes 0..E-1 of a warp stand
+// for the first unit's places, E..2E-1 for the last's.
+template <bool BF16>
+struct Ends {
+    static constexpr int E = Unit<BF16>::kElems;
+    bool cut_first, cut_last;
+    bool mine, inside;    // this lane's place is in such a unit; and in the row
+    int unit, element;    // its unit and place in the window
+    __device__ __forceinline__ Ends(const Window &w, int lane) {
+        cut_first = w.head > 0 || w.end < E;
+        cut_last = w.end < w.units * E && w.units > 1;
+        mine = lane < 2 * E && (lane < E ? cut_first : cut_last);
+        unit = lane < E ? 0 : w.units - 1;
+        element = unit * E + (lane & (E - 1));
+        inside = element >= w.head && element < w.end;
+    }
+};
+
+// Zeros in a part of a gradient row, by one warp: whole units as bulk copies of
+// `bytes` zeros in shared memory, the ends element by element.
+template <bool BF16>
+__device__ __forceinline__ void zero_part(const Window &w, const Part &p, int lane,
+                                          const unsigned char *zeros, int bytes) {
     constexpr int E = Unit<BF16>::kElems;
-    constexpr int WARPS = THREADS / 32;
-    const Scale scale = {a.scale, a.scale_lo};
-    __shared__ float2 s_warp[WARPS];
-    __shared__ float2 s_cta[16];
-    const cg::cluster_group cluster = cg::this_cluster();
-    const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const int64_t row = blockIdx.x / C;
-    if (C > 1) cluster.barrier_arrive();  // every CTA runs before its memory is written
+    const int lo = max(p.first, (w.head + E - 1) / E), hi = min(p.first + p.count, w.end / E);
+    if (lane == 0) {
+        for (int64_t at = (int64_t)lo * 16; at < (int64_t)hi * 16; at += bytes)
+            bulk_store(w.base + at, smem_addr(zeros),
+                       (uint32_t)min((int64_t)bytes, (int64_t)hi * 16 - at));
+        bulk_commit();
+    }
+    const Ends<BF16> ends(w, lane);
+    if (ends.mine && ends.inside && ends.unit >= p.first && ends.unit < p.first + p.count)
+        store1<BF16>(w.base, ends.element, 0.f);
+}
 
-    const int64_t target = load_index(a.target, row, a.target_bytes);
-    float weight = 1.f;
-    if constexpr (MODE == kPolicy) weight = a.w[row];
-    const bool live = target >= 0 && weight != 0.f;
-    const Window g = a.g.data ? window_of<BF16>(a.g, row, a.vocab) : Window{};
-    const bool first = rank == 0 && threadIdx.x == 0;
-    if (!live) {
-        if (C > 1) cluster.barrier_wait();
-        if (MODE == kPolicy && a.g.data)
-            zero_units<BF16>(g, rank * THREADS + threadIdx.x, C * THREADS);
-        if (first) {
-            a.logp[row] = 0.f;
-            if constexpr (MODE == kPolicy)
-                for (int j = 0; j < kTerms; ++j) a.terms[row * kTerms + j] = 0.f;
-            if constexpr (MODE == kPref) a.coef[row] = 0.f;
+constexpr int kMaxStages = 16;   // slots of a ring
+constexpr int kMaxCluster = 8;
+constexpr int kBatch = 32;       // rows whose scalars are fetched together
+
+// A place in a ring of `n` slots whose mbarriers change phase with every turn.
+struct Place {
+    int i = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next(int n) {
+        if (++i == n) {
+            i = 0;
+            phase ^= 1;
+        }
+    }
+};
+
+// What the consumers take of a row besides its logits: the producer's lanes
+// work it out, each for a row of its own.
+struct __align__(16) RowInfo {
+    float4 f;      // weight, old, ref, advantage
+    char *g;       // the gradient's window
+    int head;      // elements before the row in the logits' window
+    int g_head;    // and in the gradient's
+    int target;    // < 0: the row takes no part
+    float xt;      // the token's logit; NaN for a token beyond the vocabulary
+};
+
+// A sum in fp32 and what its additions rounded away (an fp64 sum in a thread
+// that all the others wait for costs more).
+struct Sum {
+    float s, rest;
+    __device__ __forceinline__ void add(float x) {
+        const float t = s + x, b = t - s;
+        rest += (s - (t - b)) + (x - b);
+        s = t;
+    }
+};
+
+__device__ __forceinline__ int clamp_count(int n, int most) { return max(0, min(n, most)); }
+
+// The units first, first + step, ... below end that a thread holds of `count`
+// consecutive ones: the block's threads in turn, or, where the gradient's row
+// lies otherwise to the 16-byte boundaries, a stretch of consecutive ones for
+// each warp, so that a unit's neighbour is in the next lane.
+struct Units {
+    int first, step, end;
+};
+template <int THREADS>
+__device__ __forceinline__ Units units_of(int count, int tid, bool shifted) {
+    if (!shifted) return {tid, THREADS, count};
+    const int per = (count + THREADS - 1) / THREADS * 32, from = (tid >> 5) * per;
+    return {from + (tid & 31), 32, min(count, from + per)};
+}
+
+// A unit's gradient entries from its exponentials: each times f, and k more at
+// place `at` (outside [0, E): not here).
+template <bool BF16>
+__device__ __forceinline__ void entries(f2 (&v)[Unit<BF16>::kElems / 2], float k, f2 f, int at) {
+    constexpr int E = Unit<BF16>::kElems;
+#pragma unroll
+    for (int h = 0; h < E / 2; ++h) v[h] = mul2(v[h], f);
+    if ((unsigned)at < E) {
+#pragma unroll
+        for (int h = 0; h < E / 2; ++h)
+            v[h] = add2(v[h], pair(at == 2 * h ? k : 0.f, at == 2 * h + 1 ? k : 0.f));
+    }
+}
+
+// Store the gradient entries of a thread's units, of a part of `count` that
+// starts at the window's unit u0 (k, f, at: see entries(); at counts from the
+// part's start), into a row that lies to the 16-byte boundaries as its source does: whole units in
+// one piece, those at the row's ends element by element.
+template <bool BF16, int N, int THREADS>
+__device__ __forceinline__ void store_alike(f2 (*v)[Unit<BF16>::kElems / 2], const Window &x,
+                                            char *base, int u0, int count, int tid, float k, f2 f,
+                                            int at) {
+    constexpr int E = Unit<BF16>::kElems;
+    const int left = count - tid;
+    uint4 *const to = reinterpret_cast<uint4 *>(base) + u0 + tid;
+    const int own = at - tid * E;
+    if (x.head == 0 && (x.end & (E - 1)) == 0) {  // nothing but whole units
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            entries<BF16>(v[j], k, f, own - j * THREADS * E);
+            if (j * THREADS < left) __stcs(to + j * THREADS, narrow<BF16>(v[j]));
         }
         return;
     }
-    const Window x = window_of<BF16>(a.x, row, a.vocab);
-    float v[UPT][E];
-    const int u0 = rank * UPT * THREADS + threadIdx.x;
+    const Window dst = {base, x.head, x.end, x.units};
+    const int lo = max((x.head + E - 1) / E - u0, 0) - tid;
+    const unsigned whole = max(min(x.end / E - u0, count) - tid - lo, 0);
 #pragma unroll
-    for (int k = 0; k < UPT; ++k) {
-        const int u = u0 + k * THREADS;
-        if (u < x.units) {
-            load_unit<BF16>(x, u, v[k]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < E; ++j) v[k][j] = -INFINITY;
-        }
+    for (int j = 0; j < N; ++j) {
+        entries<BF16>(v[j], k, f, own - j * THREADS * E);
+        const uint4 q = narrow<BF16>(v[j]);
+        if ((unsigned)(j * THREADS - lo) < whole)
+            __stcs(to + j * THREADS, q);
+        else if (j * THREADS < left)
+            store_elems<BF16>(x, dst, u0 + j * THREADS + tid, q);
     }
-    const float xt = target < a.vocab ? load1<BF16>(x.base, x.head + (int)target) : NAN;
-    float old = 0.f, ref = 0.f, adv = 0.f;
-    if constexpr (MODE == kPolicy) {
-        old = a.old[row];
-        adv = a.adv[row];
-        if (a.ref) ref = a.ref[row];
-    }
+}
 
-    float mt = -INFINITY;
+// The 16 bytes that end `bytes` (2..14, even; whole words for fp32) into cur,
+// with prev before it: what prev and cur make of a unit that lies `bytes`
+// further on.
+__device__ __forceinline__ uint4 join_units(const uint4 &prev, const uint4 &cur, int bytes) {
+    const uint32_t c[8] = {prev.x, prev.y, prev.z, prev.w, cur.x, cur.y, cur.z, cur.w};
+    const int words = bytes >> 2;
+    uint32_t t[5];  // words 3 - words and on
 #pragma unroll
-    for (int k = 0; k < UPT; ++k)
-#pragma unroll
-        for (int j = 0; j < E; ++j) mt = fmaxf(mt, v[k][j]);
-    const float base = mt == -INFINITY ? 0.f : mt;
-    float st = 0.f;
-#pragma unroll
-    for (int k = 0; k < UPT; ++k)
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-            v[k][j] = exp_of(v[k][j], base, scale);
-            st += v[k][j];
-        }
+    for (int i = 0; i < 5; ++i)
+        t[i] = words & 2 ? (words & 1 ? c[i] : c[i + 1]) : (words & 1 ? c[i + 2] : c[i + 3]);
+    const uint32_t pick = bytes & 2 ? 0x5432u : 0x7654u;
+    return make_uint4(__byte_perm(t[0], t[1], pick), __byte_perm(t[1], t[2], pick),
+                      __byte_perm(t[2], t[3], pick), __byte_perm(t[3], t[4], pick));
+}
 
-    // the row's maximum and sum, in an order that depends on the grid alone
-    float2 q = make_float2(mt, st);
+// Store a stretch of n consecutive units, the window's unit u0 and on, lane i
+// holding i, i + 32, ..., into a row g that lies otherwise to the boundaries: a
+// unit of g is the end of one unit of the source and the start of the next,
+// which the neighbouring lane holds.  What the stretch has only a part of goes
+// out element by element.
+template <bool BF16, int N>
+__device__ __forceinline__ void store_shifted(f2 (*v)[Unit<BF16>::kElems / 2],
+                                              const Window &x, const Window &g, int u0, int n,
+                                              int lane, float k, f2 f, int at) {
+    constexpr int E = Unit<BF16>::kElems;
+    const int by = g.head - x.head, shift = by < 0 ? by + E : by;  // 1..E - 1 elements
+    uint4 last = make_uint4(0, 0, 0, 0);
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        float2 o;
-        o.x = __shfl_xor_sync(0xffffffffu, q.x, off);
-        o.y = __shfl_xor_sync(0xffffffffu, q.y, off);
-        q = join(q, o, scale);
+    for (int j = 0; j < N; ++j) {
+        if (j * 32 >= n) break;
+        const int i = j * 32 + lane;
+        entries<BF16>(v[j], k, f, at - i * E);
+        const uint4 cur = narrow<BF16>(v[j]);
+        uint4 prev = lane == 31 ? last : cur;
+        prev.x = __shfl_sync(0xffffffffu, prev.x, (lane + 31) & 31);
+        prev.y = __shfl_sync(0xffffffffu, prev.y, (lane + 31) & 31);
+        prev.z = __shfl_sync(0xffffffffu, prev.z, (lane + 31) & 31);
+        prev.w = __shfl_sync(0xffffffffu, prev.w, (lane + 31) & 31);
+        last = cur;
+        if (i >= n) continue;
+        const int e0 = (u0 + i - (by < 0)) * E;  // of the unit in g that cur starts in
+        if (i > 0 && e0 >= g.head && e0 + E <= g.end)
+            __stcs(reinterpret_cast<uint4 *>(g.base) + e0 / E,
+                   join_units(prev, cur, shift * Unit<BF16>::kSize));
+        else
+            store_some<BF16>(g, e0, i > 0 ? 0 : shift,
+                             E, join_units(prev, cur, shift * Unit<BF16>::kSize));
+        if (i == n - 1)
+            store_some<BF16>(g, e0 + E, 0, shift,
+                             join_units(cur, cur, shift * Unit<BF16>::kSize));
     }
-    if ((threadIdx.x & 31) == 0) s_warp[threadIdx.x >> 5] = q;
-    __syncthreads();
-    q = s_warp[0];
-#pragma unroll
-    for (int i = 1; i < WARPS; ++i) q = join(q, s_warp[i], scale);
-    if (C > 1) {
-        cluster.barrier_wait();
-        if (threadIdx.x < C) *cluster.map_shared_rank(&s_cta[rank], threadIdx.x) = q;
+}
+
+// Whether every consumer (barrier 1) says yes.
+template <int THREADS>
+__device__ __forceinline__ bool all_of(bool yes) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %1, 0;\n\t"
+        "barrier.cta.red.and.pred q, 1, %2, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"((uint32_t)yes), "n"(THREADS)
+        : "memory");
+    return r != 0;
+}
+
+// NaN in a row that the block has given up.
+template <int MODE>
+__device__ __forceinline__ void give_up(const LogitsArgs &a, int64_t row) {
+    a.logp[row] = NAN;
+    if constexpr (MODE == kPref) {
+        a.stats[row] = make_float2(NAN, NAN);
+        a.coef[row] = 0.f;
+    }
+}
+
+// THREADS consumers and one producer warp.  CTA c of a cluster holds its part
+// of a row in the registers of its consumers: thread t the units k * THREADS +
+// t of the part, k < UPT.  A slot of the ring is DEPTH units of every thread.
+template <bool BF16, int THREADS, int UPT, int DEPTH, int CTAS, int MODE>
+__global__ void __launch_bounds__(THREADS + 32, CTAS)
+    row_kernel(const __grid_constant__ LogitsArgs a) {
+    constexpr int E = Unit<BF16>::kElems, P = E / 2;
+    constexpr int WARPS = THREADS / 32;
+    constexpr int SLOT = DEPTH * THREADS;          // units of a slot
+    constexpr int ZEROS = SLOT * 16 / 4 < 8192 ? SLOT * 16 / 4 : 8192;  // bytes
+    extern __shared__ __align__(128) unsigned char ring[];
+    __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_joined[2];
+    __shared__ __align__(8) uint64_t s_rows_full[2], s_rows_empty[2];
+    __shared__ RowInfo s_rows[2][kBatch];
+    __shared__ float2 s_warp[2][WARPS];
+    __shared__ __align__(8) float2 s_cta[2][kMaxCluster];
+    __shared__ volatile int s_abort;
+
+    const cg::cluster_group cluster = cg::this_cluster();
+    const int log_c = a.log_c, C = 1 << log_c, rank = (int)blockIdx.x & (C - 1);
+    const int64_t step = gridDim.x >> log_c;
+    const int64_t row0 = blockIdx.x >> log_c;
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int stages = a.stages;
+    const volatile int *const aborted = &s_abort;
+    if (tid == 0) {
+        for (int i = 0; i < stages; ++i) {
+            mbar_init(smem_addr(&s_full[i]), 1);
+            mbar_init(smem_addr(&s_empty[i]), WARPS);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_addr(&s_joined[i]), 1);
+            mbar_init(smem_addr(&s_rows_full[i]), 1);
+            mbar_init(smem_addr(&s_rows_empty[i]), WARPS);
+        }
+        s_abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (C > 1)
         cluster.sync();
-        q = s_cta[0];
-        for (int i = 1; i < C; ++i) q = join(q, s_cta[i], scale);
-    }
-    const float m = q.x, z = q.y;
-    // a row without a finite logit leaves z = 0: -inf - -inf
-    const float logp = z > 0.f ? (xt - m) * a.inv_temp - logf(z) : NAN;
+    else
+        __syncthreads();
 
-    if constexpr (MODE == kPolicy) {
-        const float r = expf(logp - old);
-        const float free = r * adv;
-        const float bound = fminf(fmaxf(r, a.lo), a.hi) * adv;
-        const bool act = free <= bound;
-        const float d = ref - logp;
-        const float back = a.kl != 0.f ? expf(d) : 1.f;
-        if (first) {
-            a.logp[row] = logp;
-            float *t = a.terms + row * kTerms;
-            t[0] = -weight * (act || free != free ? free : bound);
-            t[1] = a.ref ? weight * (expf(d) - d - 1.f) : 0.f;
-            t[2] = act ? 0.f : weight;
+    if (tid >= THREADS) {
+        // Producer: the rows' scalars, kBatch rows at a time, and their parts,
+        // slot after slot, as far ahead as the ring is free.  Whole units come
+        // as bulk copies; the elements of a unit at a row's end that is not
+        // whole come one by one, with -inf beside them.
+        Place place, batch;
+        unsigned filled = 0;
+        bool ok = true, mixed = false, again = false;
+        unsigned char *const zeros = ring + (size_t)stages * SLOT * 16;
+        if (has_grad(MODE) && a.g.data) {
+            for (int i = lane; i < ZEROS / 16; i += 32)
+                reinterpret_cast<uint4 *>(zeros)[i] = make_uint4(0, 0, 0, 0);
+            fence_proxy_async_smem();
+            __syncwarp();
         }
-        if (!a.g.data) return;
-        const float k = weight * (a.kl * (1.f - back) - (act || free != free ? free : 0.f)) *
-                        a.inv_temp;
-        // this thread's values are exp((x - base) / tau), all 0 where it has no
-        // finite logit
-        const float f = -k * (z > 0.f ? (mt == -INFINITY ? 0.f : exp_of(base, m, scale) / z) : NAN);
-        const int ut = (x.head + (int)target) / E;
-#pragma unroll
-        for (int i = 0; i < UPT; ++i) {
-            const int u = u0 + i * THREADS;
-            if (u >= x.units) break;
-#pragma unroll
-            for (int j = 0; j < E; ++j) v[i][j] *= f;
-            if (u == ut) {
-#pragma unroll
-                for (int j = 0; j < E; ++j)
-                    if (ut * E + j == x.head + (int)target) v[i][j] += k;
+        for (int64_t base = row0; base < a.n && ok; base += kBatch * step, batch.next(2)) {
+            const int64_t my_row = base + lane * step;
+            RowInfo mine = {make_float4(1.f, 0.f, 0.f, 0.f), nullptr, 0, 0, -1, NAN};
+            Window my_x = {};
+            int64_t t = -1;
+            if (my_row < a.n) {
+                t = load_index(a.target, my_row, a.target_bytes);
+                if constexpr (has_grad(MODE)) {
+                    mine.f = make_float4(a.w[my_row], a.old[my_row], a.ref ? a.ref[my_row] : 0.f,
+                                         a.adv[my_row]);
+                    if (mine.f.x == 0.f) t = -1;
+                    if (a.g.data) {
+                        const Window g = window_of<BF16>(a.g, my_row, a.vocab);
+                        mine.g = g.base;
+                        mine.g_head = g.head;
+                    }
+                }
+                my_x = window_of<BF16>(a.x, my_row, a.vocab);
+                mine.head = my_x.head;
             }
-            store_unit<BF16>(x, g, u, v[i]);
+            // read here, and so before this CTA lets the row's gradient be
+            // written, which may lie over the logits
+            if (t >= 0 && t < a.vocab) mine.xt = load1<BF16>(my_x.base, my_x.head + (int)t);
+            mine.target = t < 0 ? -1 : t >= a.vocab ? a.vocab : (int)t;
+            unsigned todo = __ballot_sync(0xffffffffu, t >= 0);
+            // rows without a part to play: this CTA's part of their zeros
+            unsigned idle = has_grad(MODE) && a.g.data
+                                ? __ballot_sync(0xffffffffu, my_row < a.n && t < 0) : 0u;
+            // The window of the next row and the elements at its ends are
+            // fetched a row ahead.
+            Window ahead_x = {};
+            float ahead_edge = 0.f;
+            const auto look_ahead = [&](int from) {
+                ahead_x = window_at<BF16>(
+                    reinterpret_cast<char *>(__shfl_sync(
+                        0xffffffffu, reinterpret_cast<uint64_t>(my_x.base), from)),
+                    __shfl_sync(0xffffffffu, my_x.head, from), a.vocab);
+                const Ends<BF16> ends(ahead_x, lane);
+                ahead_edge = ends.mine && ends.inside ? load1<BF16>(ahead_x.base, ends.element)
+                                                      : -INFINITY;
+            };
+            if (todo) look_ahead(__ffs(todo) - 1);
+            // The scalars go out behind the first row's copies, which then do
+            // not wait for them; ahead of them where a part may be longer than
+            // the ring, which only consumers that know the row make room in.
+            bool told = false;
+            const auto tell = [&] {
+                told = true;
+                if (again)
+                    ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&s_rows_empty[batch.i]),
+                                                           batch.phase ^ 1, aborted));
+                if (!ok) return;
+                s_rows[batch.i][lane] = mine;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_addr(&s_rows_full[batch.i]));
+            };
+            if (!has_grad(MODE)) tell();
+            while (ok && (!told || todo || idle)) {
+                if (idle && (!todo || (told && __ffs(idle) < __ffs(todo)))) {
+                    const int from = __ffs(idle) - 1;
+                    idle &= idle - 1;
+                    const Window g = window_at<BF16>(
+                        reinterpret_cast<char *>(__shfl_sync(
+                            0xffffffffu, reinterpret_cast<uint64_t>(mine.g), from)),
+                        __shfl_sync(0xffffffffu, mine.g_head, from), a.vocab);
+                    zero_part<BF16>(g, part_of(g.units, rank, log_c), lane, zeros, ZEROS);
+                } else if (todo) {
+                    todo &= todo - 1;
+                    const Window x = ahead_x;
+                    const float edge = ahead_edge;
+                    if (todo) look_ahead(__ffs(todo) - 1);
+                    const Part p = part_of(x.units, rank, log_c);
+                    const Ends<BF16> ends(x, lane);
+                    mixed = mixed || ends.cut_first || ends.cut_last;
+                    for (int s = 0; s < p.count; s += SLOT) {
+                        const uint32_t full = smem_addr(&s_full[place.i]);
+                        unsigned char *at = ring + (size_t)place.i * SLOT * 16;
+                        if (filled >= (unsigned)stages)
+                            ok = __all_sync(0xffffffffu,
+                                            mbar_wait(smem_addr(&s_empty[place.i]),
+                                                      place.phase ^ 1, aborted));
+                        if (!ok) break;
+                        // earlier stores to this slot come before its next copy
+                        if (mixed) fence_proxy_async_smem();
+                        int lo = p.first + s, hi = p.first + min(s + SLOT, p.count);
+                        const int u0 = lo;
+                        if (ends.mine && ends.unit >= lo && ends.unit < hi)
+                            store1<BF16>((char *)at, ends.element - u0 * E, edge);
+                        if (ends.cut_first && lo == 0) ++lo;
+                        if (ends.cut_last && hi == x.units) --hi;
+                        __syncwarp();
+                        if (lane == 0) {
+                            const uint32_t bytes = hi > lo ? (uint32_t)(hi - lo) * 16 : 0;
+                            mbar_arrive_expect_tx(full, bytes);
+                            if (bytes)
+                                bulk_load(smem_addr(at + (size_t)(lo - u0) * 16),
+                                          x.base + (size_t)lo * 16, bytes, full);
+                        }
+                        place.next(stages);
+                        ++filled;
+                    }
+                }
+                if (!told && ok) tell();
+            }
+            again = again || batch.i == 1;
         }
-    } else if (first) {
-        a.logp[row] = logp;
-        if constexpr (MODE == kPref) {
-            a.stats[row] = make_float2(m, z > 0.f ? 1.f / z : NAN);
-            a.coef[row] = 0.f;
+        // the zeros' source stays until their copies have read it
+        if (has_grad(MODE) && lane == 0) bulk_wait_all();
+        if (!ok) {  // given up: no copy may land after the block has ended
+            s_abort = 1;
+            for (unsigned k = 0; k < (unsigned)stages && k < filled; ++k) {
+                if (place.i == 0) {
+                    place.i = stages;
+                    place.phase ^= 1;
+                }
+                --place.i;
+                mbar_wait(smem_addr(&s_full[place.i]), place.phase, nullptr);
+            }
         }
+    } else {
+        const Scale scale = {a.scale, a.scale_lo};
+        const f2 hi2 = pair(scale.hi, scale.hi), lo2 = pair(scale.lo, scale.lo);
+        Place place, batch;
+        unsigned rows = 0;  // rows taken
+        bool ok = true;
+        int next = 0;       // the row's place in its batch
+        Sum terms[kTerms] = {};
+        // This thread's units of the next slot, which holds `count` (none: 0),
+        // -inf where it has none.
+        const auto take_slot = [&](uint4 *q, int count, bool shifted) {
+            const Units w = units_of<THREADS>(count, tid, MODE == kPolicyShifted && shifted);
+            const int left = w.end - w.first;
+            if (count > 0) ok = mbar_wait(smem_addr(&s_full[place.i]), place.phase, aborted) && ok;
+            const uint4 *slot = reinterpret_cast<const uint4 *>(ring) + (size_t)place.i * SLOT + w.first;
+#pragma unroll
+            for (int j = 0; j < DEPTH; ++j) {
+                const uint32_t none = BF16 ? 0xff80ff80u : 0xff800000u;  // -inf
+                q[j] = make_uint4(none, none, none, none);
+                if (j * w.step < left) q[j] = slot[j * w.step];
+            }
+            if (count > 0) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_addr(&s_empty[place.i]));
+                place.next(stages);
+            }
+        };
+        for (int64_t row = row0; row < a.n; row += step) {
+            if (next == kBatch) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_addr(&s_rows_empty[batch.i]));
+                batch.next(2);
+                next = 0;
+            }
+            if (next == 0 && !all_of<THREADS>(mbar_wait(smem_addr(&s_rows_full[batch.i]),
+                                                        batch.phase, aborted))) {
+                // without the rows' scalars nothing can be said of them
+                s_abort = 1;
+                for (; row < a.n; row += step)
+                    if (rank == 0 && tid == 0) give_up<MODE>(a, row);
+                terms[0].s = terms[1].s = NAN;
+                break;
+            }
+            const RowInfo r = s_rows[batch.i][next++];
+            const bool first = rank == 0 && tid == 0;
+            if (r.target < 0) {  // the producer writes its zeros
+                if (first) {
+                    a.logp[row] = 0.f;
+                    if constexpr (MODE == kPref) a.coef[row] = 0.f;
+                }
+                continue;
+            }
+            const Window x = window_at<BF16>(nullptr, r.head, a.vocab);
+            const Part p = part_of(x.units, rank, log_c);
+            // this thread's maximum, and the sum of its exp((x - maximum) /
+            // tau): all of them at once where they are kept for the gradient,
+            // slot by slot otherwise
+            constexpr bool kHold = has_grad(MODE);
+            const bool shifted = kHold && r.g && r.g_head != r.head;
+            f2 v[kHold ? UPT : 1][P];
+            float mt = -INFINITY, st = 0.f;
+            if constexpr (kHold) {
+                uint4 q[UPT];
+#pragma unroll
+                for (int k = 0; k < UPT; k += DEPTH)
+                    take_slot(q + k, clamp_count(p.count - k * THREADS, SLOT), shifted);
+                mt = max_of<BF16, UPT>(q);
+                st = exps_of<BF16, UPT, true>(q, v, base_of(mt), hi2, lo2);
+            } else {
+                for (int u = 0; u < p.count; u += SLOT) {
+                    uint4 q[DEPTH];
+                    take_slot(q, clamp_count(p.count - u, SLOT), false);
+                    const float before = mt;
+                    mt = fmaxf(mt, max_of<BF16, DEPTH>(q));
+                    st = st * exp_of(before, base_of(mt), scale) +
+                         exps_of<BF16, DEPTH, false>(q, v, base_of(mt), hi2, lo2);
+                }
+            }
+
+            // the row's maximum and sum: warps, CTA, cluster, each in a fixed
+            // order.  Two sets of shared places take turns, so that one
+            // barrier a row is enough: a CTA sends row i + 1's pair only when
+            // all its warps have read row i's.  (Every warp's pair sent to
+            // every CTA, without the barrier, took longer: 704 against 665 us
+            // at 8000 rows of 128256 bf16.)
+            const unsigned turn = rows & 1, phase = (rows >> 1) & 1;
+            ++rows;
+            const float mw = warp_max(mt);
+            const float sw = warp_sum(st * exp_of(mt, base_of(mw), scale));
+            if (lane == 0) s_warp[turn][tid >> 5] = make_float2(mw, sw);
+            asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+            float2 part;
+            if (C == 1 || tid < 32) part = join_parts(s_warp[turn], WARPS, lane, scale);
+            if (C > 1) {
+                // every CTA sends its pair to all CTAs of the cluster, and
+                // waits for theirs
+                const uint32_t bar = smem_addr(&s_joined[turn]);
+                if (tid == 0) mbar_arrive_expect_tx(bar, C * 8);
+                if (tid < C) {
+                    uint32_t to, there;
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                                 : "=r"(to) : "r"(smem_addr(&s_cta[turn][rank])), "r"(tid));
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                                 : "=r"(there) : "r"(bar), "r"(tid));
+                    asm volatile(
+                        "st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 "
+                        "[%0], {%1, %2}, [%3];" ::"r"(to), "f"(part.x), "f"(part.y), "r"(there)
+                        : "memory");
+                }
+                ok = mbar_wait(bar, phase, aborted) && ok;
+                part = join_parts(s_cta[turn], C, lane, scale);
+            }
+            // A wait that ran out leaves NaN in this row and the block's later
+            // ones, whose waits see s_abort and return at once.
+            if (!ok) {
+                s_abort = 1;
+                part.y = NAN;
+            }
+            const float m = part.x, z = part.y;
+            // a row without a finite logit leaves z = 0: -inf - -inf
+            const float logp = z > 0.f ? fmaf(r.xt - m, a.inv_temp, -logf(z)) : NAN;
+
+            if constexpr (has_grad(MODE)) {
+                const float weight = r.f.x;
+                const Scale unit = {kLog2e, kLog2eLo};
+                const float ratio = exp_of(logp, r.f.y, unit);
+                const float free = ratio * r.f.w;
+                const float bound = fminf(fmaxf(ratio, a.lo), a.hi) * r.f.w;
+                const bool act = free <= bound;
+                const float d = r.f.z - logp;
+                const float back = exp_of(r.f.z, logp, unit);
+                if (first) {
+                    a.logp[row] = logp;
+                    terms[0].add(-weight * (act || free != free ? free : bound));
+                    if (a.ref) terms[1].add(weight * (expm1f(d) - d));
+                    if (!act) terms[2].add(weight);
+                }
+                if (!r.g) continue;
+                const float k =
+                    weight * ((a.kl != 0.f ? a.kl * (1.f - back) : 0.f) -
+                              (act || free != free ? free : 0.f)) * a.inv_temp;
+                // this thread's values are exp((x - base) / tau), all 0 where
+                // it has no finite logit
+                const float f = -k * (z > 0.f ? (mt == -INFINITY ? 0.f
+                                                 : exp_of(mt, m, scale) * __fdividef(1.f, z))
+                                              : NAN);
+                const f2 ff = pair(f, f);
+                // the token's own entry (none within reach where it is beyond
+                // the vocabulary, whose rows are NaN)
+                const int at = r.target < a.vocab ? x.head + r.target : INT_MIN / 2;
+#pragma unroll
+                for (int i = 0; i < UPT; i += DEPTH) {
+                    const int count = clamp_count(p.count - i * THREADS, SLOT);
+                    const int u0 = p.first + i * THREADS;
+                    if (MODE == kPolicyShifted && shifted) {
+                        const Units w = units_of<THREADS>(count, tid, true);
+                        const int from = u0 + w.first - lane;
+                        store_shifted<BF16, DEPTH>(v + i, x, window_at<BF16>(r.g, r.g_head, a.vocab),
+                                                   from, max(w.end - w.first + lane, 0), lane, k, ff,
+                                                   at - from * E);
+                    } else {
+                        store_alike<BF16, DEPTH, THREADS>(v + i, x, r.g, u0, count, tid, k, ff,
+                                                          at - u0 * E);
+                    }
+                }
+            } else if (first) {
+                a.logp[row] = logp;
+                if constexpr (MODE == kPref) {
+                    a.stats[row] = make_float2(m, z > 0.f ? 1.f / z : NAN);
+                    a.coef[row] = 0.f;
+                }
+            }
+        }
+        if (has_grad(MODE) && rank == 0 && tid == 0)
+            for (int j = 0; j < kTerms; ++j) a.terms[row0 * kTerms + j] = (double)terms[j].s + (double)terms[j].rest;
     }
+    // no CTA leaves while another may still write to its memory
+    if (C > 1)
+        cluster.sync();
+    else
+        __syncthreads();
 }
 
 // Sum over the block in a fixed order (fp64); valid in every thread.
@@ -313,12 +933,18 @@ __device__ __forceinline__ double block_total(double v, double *sh) {
     return s;
 }
 
-__global__ void __launch_bounds__(1024) policy_terms_kernel(const __grid_constant__ LogitsArgs a) {
-    __shared__ double sh[32];
+// The policy loss's sums over the clusters of its row kernel.  One warp: fp64
+// additions are rare units here, and the kernel waits for little else.
+__global__ void __launch_bounds__(32)
+    policy_terms_kernel(const __grid_constant__ LogitsArgs a, int clusters) {
+    wait_for_previous();
     double s[kTerms] = {};
-    for (int64_t r = threadIdx.x; r < a.n; r += 1024)
-        for (int j = 0; j < kTerms; ++j) s[j] += (double)a.terms[r * kTerms + j];
-    for (int j = 0; j < kTerms; ++j) s[j] = block_total<1024>(s[j], sh);
+    for (int c = threadIdx.x; c < clusters; c += 32)
+        for (int j = 0; j < kTerms; ++j) s[j] += a.terms[c * kTerms + j];
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+        for (int j = 0; j < kTerms; ++j) s[j] += __shfl_xor_sync(0xffffffffu, s[j], off);
     if (threadIdx.x == 0) {
         a.terms_out[0] = (float)(s[0] + (double)a.kl * s[1]);
         for (int j = 0; j < kTerms; ++j) a.terms_out[1 + j] = (float)s[j];
@@ -331,6 +957,7 @@ __global__ void __launch_bounds__(1024) pairs_kernel(const __grid_constant__ Log
     __shared__ double sh[32];
     const int lane = threadIdx.x & 31;
     double sum = 0.0;
+    wait_for_previous();
     for (int64_t k = threadIdx.x >> 5; k < a.pairs; k += 32) {
         int64_t lo[2], hi[2];
         double R[2];
@@ -371,6 +998,7 @@ __global__ void __launch_bounds__(512) grad_kernel(const __grid_constant__ Logit
     constexpr int E = Unit<BF16>::kElems;
     const int64_t row = blockIdx.x;
     const Window g = window_of<BF16>(a.g, row, a.vocab);
+    wait_for_previous();
     const int64_t target = load_index(a.target, row, a.target_bytes);
     const float k = a.coef[row] * a.inv_temp;
     if (target < 0 || k == 0.f) {
@@ -379,80 +1007,155 @@ __global__ void __launch_bounds__(512) grad_kernel(const __grid_constant__ Logit
     }
     const Window x = window_of<BF16>(a.x, row, a.vocab);
     const float2 q = a.stats[row];
-    const Scale scale = {a.scale, a.scale_lo};
     const float f = -k * q.y;
+    const float base = base_of(q.x);
+    const f2 hi2 = pair(a.scale, a.scale), lo2 = pair(a.scale_lo, a.scale_lo);
+    const f2 neg = pair(-base, -base), ff = pair(f, f);
     const int at = target < a.vocab ? x.head + (int)target : -1;
     for (int u = threadIdx.x; u < x.units; u += 512) {
-        float v[E];
-        load_unit<BF16>(x, u, v);
+        f2 v[E / 2];
+        widen<BF16>(load_unit<BF16>(x, u), v);
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            v[j] = exp_of(v[j], q.x, scale) * f;
-            if (u * E + j == at) v[j] += k;
+        for (int j = 0; j < E / 2; ++j) {
+            v[j] = mul2(exp_of2(v[j], neg, hi2, lo2), ff);
+            if (u == at / E)
+                v[j] = add2(v[j], pair(u * E + 2 * j == at ? k : 0.f,
+                                       u * E + 2 * j + 1 == at ? k : 0.f));
         }
-        store_unit<BF16>(x, g, u, v);
+        store_unit<BF16>(x, g, u, narrow<BF16>(v));
     }
 }
 
-// Launch a row kernel: THREADS * UPT units a CTA, as many CTAs as the row's
-// window takes, and more where there are too few rows for the SMs.
-template <bool BF16, int THREADS, int EPT, int MODE>
-cudaError_t launch_rows_as(const LogitsArgs &a, int sm_count, cudaStream_t stream) {
+// Launch of a row kernel of THREADS consumers with EPT elements each: a
+// cluster of as many CTAs as a row takes (more where there are too few rows for
+// the SMs), and as many clusters as the device holds at once, which take the
+// rows in turn.
+template <bool BF16, int THREADS, int EPT, int DEPTH, int STAGES, int CTAS, int MODE>
+cudaError_t launch_rows_as(const LogitsArgs &in, int sm_count, cudaStream_t stream, int *used) {
     constexpr int E = Unit<BF16>::kElems, UPT = EPT / E;
-    const int units = (a.vocab + 2 * (E - 1)) / E;
-    int C = (units + THREADS * UPT - 1) / (THREADS * UPT);
-    if (C > 8) return cudaErrorInvalidValue;
+    constexpr int kSlot = DEPTH * THREADS * 16;
+    constexpr int kSmem = STAGES * kSlot + (!has_grad(MODE) ? 0 : kSlot / 4 < 8192 ? kSlot / 4 : 8192);
+    static_assert(STAGES <= kMaxStages && UPT % DEPTH == 0, "ring");
+    static PerDevice ready, most[kMaxCluster + 1];
+    const auto kernel = row_kernel<BF16, THREADS, UPT, DEPTH, CTAS, MODE>;
+    const int units = (in.vocab + 2 * (E - 1)) / E;
+    int log_c = 0;
+    // (the forward kernels take a part of any length, slot by slot)
+    const auto fits = [&](int c) {
+        return !has_grad(MODE) || (units + (1 << c) - 1) >> c <= THREADS * UPT;
+    };
+    while (!fits(log_c))
+        if ((1 << ++log_c) > kMaxCluster) return cudaErrorInvalidValue;
+    while (2 << log_c <= kMaxCluster && in.n * (2 << log_c) <= sm_count &&
+           units >= (2 << log_c) * THREADS)
+        ++log_c;
+    const int C = 1 << log_c;
+
+    const int dev = PerDevice::device();
+    if (!ready.get(dev)) {
+        const cudaError_t e = cudaFuncSetAttribute(
+            kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (e != cudaSuccess) return e;
+        ready.set(dev, 1);
+    }
     cudaLaunchAttribute attr = {};
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = (unsigned)C;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(a.n * C));
-    cfg.blockDim = dim3(THREADS);
+    cfg.gridDim = dim3((unsigned)C);
+    cfg.blockDim = dim3(THREADS + 32);
+    cfg.dynamicSmemBytes = kSmem;
     cfg.stream = stream;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, row_kernel<BF16, THREADS, UPT, MODE>, a);
+    int clusters = most[C].get(dev);
+    if (!clusters) {
+        const cudaError_t e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg);
+        if (e != cudaSuccess) return e;
+        if (clusters < 1) return cudaErrorInvalidConfiguration;
+        most[C].set(dev, clusters);
+    }
+    LogitsArgs a = in;
+    a.stages = STAGES;
+    a.log_c = log_c;
+    *used = (int)(in.n < clusters ? in.n : clusters);
+    cfg.gridDim = dim3((unsigned)(*used * C));
+    return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 template <bool BF16, int MODE>
-cudaError_t launch_rows(const LogitsArgs &a, int sm_count, cudaStream_t stream) {
+cudaError_t launch_rows(const LogitsArgs &a, int sm_count, cudaStream_t stream, int *used) {
+    *used = 0;
     if (a.n == 0) return cudaSuccess;
-    if (a.vocab <= 4096 - 8) return launch_rows_as<BF16, 128, 32, MODE>(a, sm_count, stream);
-    if (a.vocab <= 131072 - 8) return launch_rows_as<BF16, 512, 32, MODE>(a, sm_count, stream);
-    return launch_rows_as<BF16, 512, 72, MODE>(a, sm_count, stream);
+    if (a.vocab <= 32 * 72 - 14)
+        return launch_rows_as<BF16, 32, 72, 9, 3, 8, MODE>(a, sm_count, stream, used);
+    if (a.vocab <= 64 * 72 - 14)
+        return launch_rows_as<BF16, 64, 72, 9, 3, 5, MODE>(a, sm_count, stream, used);
+    if constexpr (!has_grad(MODE))
+        return launch_rows_as<BF16, 224, 72, 3, 5, 4, MODE>(a, sm_count, stream, used);
+    if (a.vocab <= 128 * 72 - 14)
+        return launch_rows_as<BF16, 128, 72, 9, 3, 3, MODE>(a, sm_count, stream, used);
+    if (a.vocab <= 224 * 72 - 14 ||
+        (a.vocab > 480 * 72 - 14 && a.vocab <= kMaxCluster * 224 * 72 - 14))
+        return launch_rows_as<BF16, 224, 72, 9, 3, 2, MODE>(a, sm_count, stream, used);
+    return launch_rows_as<BF16, 480, 72, 9, 3, 1, MODE>(a, sm_count, stream, used);
+}
+
+// A launch that may begin before the kernel ahead of it in the stream has
+// ended: it waits for that kernel itself.
+template <typename... Params, typename... Args>
+cudaError_t launch_behind(void (*kernel)(Params...), unsigned grid, unsigned block,
+                          cudaStream_t stream, Args... args) {
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 }  // namespace
 
 cudaError_t launch_token_logprobs(const LogitsArgs &a, aloco_dtype dtype, int sm_count,
                                   cudaStream_t stream) {
-    return dtype == ALOCO_BF16 ? launch_rows<true, kFwd>(a, sm_count, stream)
-                               : launch_rows<false, kFwd>(a, sm_count, stream);
+    int used;
+    return dtype == ALOCO_BF16 ? launch_rows<true, kFwd>(a, sm_count, stream, &used)
+                               : launch_rows<false, kFwd>(a, sm_count, stream, &used);
 }
 
 cudaError_t launch_policy_loss(const LogitsArgs &a, aloco_dtype dtype, int sm_count,
                                cudaStream_t stream) {
-    const cudaError_t e = dtype == ALOCO_BF16 ? launch_rows<true, kPolicy>(a, sm_count, stream)
-                                              : launch_rows<false, kPolicy>(a, sm_count, stream);
+    int used;
+    // do all rows of the gradient lie to the 16-byte boundaries as the logits'?
+    const int64_t size = dtype == ALOCO_BF16 ? 2 : 4, per = a.x.per_batch;
+    const bool alike = !a.g.data ||
+                       ((((int64_t)((uintptr_t)a.x.data - (uintptr_t)a.g.data)) | (per > 1 ? (a.x.row_stride - a.g.row_stride) * size : 0) |
+                         (a.n > per ? (a.x.batch_stride - a.g.batch_stride) * size : 0)) & 15) == 0;
+    const auto rows = [&](auto bf16) {
+        constexpr bool B = decltype(bf16)::value;
+        return alike ? launch_rows<B, kPolicy>(a, sm_count, stream, &used)
+                     : launch_rows<B, kPolicyShifted>(a, sm_count, stream, &used);
+    };
+    const cudaError_t e = dtype == ALOCO_BF16 ? rows(std::true_type{}) : rows(std::false_type{});
     if (e != cudaSuccess) return e;
-    policy_terms_kernel<<<1, 1024, 0, stream>>>(a);
-    return cudaGetLastError();
+    return launch_behind(policy_terms_kernel, 1, 32, stream, a, used);
 }
 
 cudaError_t launch_preference_loss(const LogitsArgs &a, aloco_dtype dtype, int sm_count,
                                    cudaStream_t stream) {
-    const cudaError_t e = dtype == ALOCO_BF16 ? launch_rows<true, kPref>(a, sm_count, stream)
-                                              : launch_rows<false, kPref>(a, sm_count, stream);
-    if (e != cudaSuccess) return e;
-    pairs_kernel<<<1, 1024, 0, stream>>>(a);
-    if (a.g.data && a.n) {
-        if (dtype == ALOCO_BF16)
-            grad_kernel<true><<<(unsigned)a.n, 512, 0, stream>>>(a);
-        else
-            grad_kernel<false><<<(unsigned)a.n, 512, 0, stream>>>(a);
-    }
-    return cudaGetLastError();
+    int used;
+    cudaError_t e = dtype == ALOCO_BF16 ? launch_rows<true, kPref>(a, sm_count, stream, &used)
+                                        : launch_rows<false, kPref>(a, sm_count, stream, &used);
+    if (e == cudaSuccess) e = launch_behind(pairs_kernel, 1, 1024, stream, a);
+    if (e == cudaSuccess && a.g.data && a.n)
+        e = launch_behind(dtype == ALOCO_BF16 ? grad_kernel<true> : grad_kernel<false>,
+                          (unsigned)a.n, 512, stream, a);
+    return e;
 }
 
 }  // namespace aloco

@@ -13,8 +13,7 @@ struct Rows {
     int64_t batch_stride, row_stride;
 };
 
-// Per-row terms of the policy loss, summed by its last kernel: one float each
-// for L's three sums.
+// Sums of the policy loss besides L itself.
 constexpr int kTerms = 3;
 
 struct LogitsArgs {
@@ -29,7 +28,8 @@ struct LogitsArgs {
     // policy loss
     const float *adv, *old, *ref, *w;
     float lo, hi, kl;                // 1 - clip_low, 1 + clip_high, kl_coef
-    float *terms;                    // [n][kTerms] per row (scratch)
+    double *terms;                   // [clusters][kTerms], one of each at most
+                                     // n clusters of the row kernel (scratch)
     float *terms_out;                // [kTerms + 1]
     // preference loss (ref as above)
     const void *cu;
@@ -38,6 +38,7 @@ struct LogitsArgs {
     float2 *stats;                   // [n] row maximum and 1 / sum (scratch)
     float *coef;                     // [n] dL/dlogp (scratch)
     float *loss, *ratios;
+    int stages, log_c;               // the row kernel's ring slots and cluster
 };
 
 cudaError_t launch_token_logprobs(const LogitsArgs &a, aloco_dtype dtype, int sm_count,

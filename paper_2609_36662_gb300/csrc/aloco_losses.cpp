@@ -187,7 +187,7 @@ cudaStream_t stream_of(const aloco_opts_t *o) {
 
 extern "C" {
 
-size_t aloco_loss_scratch_bytes(int64_t rows) { return rows > 0 ? (size_t)rows * 16 : 0; }
+size_t aloco_loss_scratch_bytes(int64_t rows) { return rows > 0 ? (size_t)rows * 24 : 0; }
 
 int aloco_token_logprobs(const aloco_tokens_t *tokens, float *logp, const aloco_opts_t *opts) {
     aloco::LogitsArgs a;
@@ -241,7 +241,7 @@ int aloco_policy_loss(const aloco_tokens_t *tokens, const float *advantages,
     a.kl = (float)cfg->kl_coef;
     a.logp = logp;
     a.terms_out = terms;
-    a.terms = static_cast<float *>(scratch);
+    a.terms = static_cast<double *>(scratch);
     int sms;
     if ((rc = check_buffers(s, over, &sms)) != ALOCO_OK) return rc;
     const cudaError_t e =

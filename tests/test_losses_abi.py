@@ -71,7 +71,7 @@ def test_policy_arguments(lib):
     assert _policy(lib, cfg=A.PolicyCfg(0.2, 0.2, 0.1), ref=None) == A.ERR_ARG
     for name in ("adv", "old", "w", "terms", "logp", "scratch"):
         assert _policy(lib, **{name: None}) == A.ERR_ARG and name[:3] in A.last_error()
-    assert _policy(lib, bytes=6 * 16 - 1) == A.ERR_ARG and "scratch" in A.last_error()
+    assert _policy(lib, bytes=lib.aloco_loss_scratch_bytes(6) - 1) == A.ERR_ARG and "scratch" in A.last_error()
     assert _policy(lib, scratch=BASE + (9 << 24) + 8) == A.ERR_ARG
     assert _policy(lib, logp=BASE) == A.ERR_ALIAS
     assert _policy(lib, terms=BASE + (7 << 24)) == A.ERR_ALIAS  # over logp
