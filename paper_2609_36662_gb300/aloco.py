@@ -812,29 +812,49 @@ class _OtherStream:
 
 def _on_stream(stream, device, inputs):
     """(context, raw stream handle) of a call."""
+    torch = _torch_module()
     if stream is not None:
-        import torch
         current = torch.cuda.current_stream(device)
         if stream != current:
             return _OtherStream(stream, current, inputs), stream.cuda_stream
-    return _on_device(device), _stream_of(None, device)
+    handle = torch._C._cuda_getCurrentRawStream(device.index)
+    if torch.cuda.current_device() == device.index:
+        return _NO_SWITCH, handle
+    return torch.cuda.device(device), handle
 
 
 def _finish(rc, ctx, *outputs):
     """Raise what a call reported; hand its outputs to the current stream."""
     if rc != OK:
         raise AlocoError(rc, last_error())
-    if isinstance(ctx, _OtherStream):
+    if ctx.__class__ is _OtherStream:
         for t in outputs:
             if t is not None:
                 t.record_stream(ctx.current)
 
 
+_torch = None
+
+
+def _torch_module():
+    """torch, imported on first use (an import statement in every call costs
+    more than the lookup)."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
 def _tokens(logits, targets, temperature) -> Tokens:
     """The descriptor of [rows, V] or [batch, rows, V] logits and their targets."""
-    import torch
+    torch = _torch_module()
     dtype = logits.dtype
-    if dtype is not torch.bfloat16 and dtype is not torch.float32:
+    if dtype is torch.bfloat16:
+        code = BF16
+    elif dtype is torch.float32:
+        code = F32
+    else:
         raise TypeError(f"logits must be float32 or bfloat16, not {dtype}")
     shape, strides = logits.shape, logits.stride()
     if len(shape) == 3:
@@ -858,32 +878,30 @@ def _tokens(logits, targets, temperature) -> Tokens:
     if not logits.is_cuda or targets.device != logits.device:
         raise ValueError("logits and targets must be CUDA tensors of one device")
     return Tokens(logits.data_ptr(), targets.data_ptr(), batch, rows, vocab, batch_stride,
-                  row_stride, temperature, F32 if dtype is torch.float32 else BF16, size)
+                  row_stride, temperature, code, size)
 
 
-def _per_row(name, t, logits) -> int:
+def _per_row(name, t, targets, device) -> int:
     """The address of a float32 tensor of one value per row."""
-    import torch
-    if t.dtype is not torch.float32 or not t.is_contiguous() or t.device != logits.device \
-            or t.shape != logits.shape[:-1]:
+    if t.dtype is not _torch.float32 or t.shape != targets.shape or t.device != device or \
+            not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous float32 tensor of shape "
-                         f"{tuple(logits.shape[:-1])} on the logits' device")
+                         f"{tuple(targets.shape)} on the logits' device")
     return t.data_ptr()
 
 
 def _logits_grad(logits, grad, want_grad):
     """(gradient tensor, its descriptor): `grad`, or a new one."""
-    import torch
     if grad is None:
         if not want_grad:
             return None, None
-        grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        grad = _torch.empty_like(logits)
     elif grad.dtype != logits.dtype or grad.shape != logits.shape or \
             grad.device != logits.device or (grad.stride(-1) != 1 and grad.shape[-1] > 1):
         raise ValueError("grad must have the logits' shape, dtype and device, with "
                          "contiguous rows")
     st = grad.stride()
-    return grad, LogitsGrad(grad.data_ptr(), st[0] if len(st) == 3 else 0, st[-2])
+    return grad, ctypes.byref(LogitsGrad(grad.data_ptr(), st[0] if len(st) == 3 else 0, st[-2]))
 
 
 def token_logprobs(logits, targets, *, temperature: float = 1.0, stream=None):
@@ -891,15 +909,13 @@ def token_logprobs(logits, targets, *, temperature: float = 1.0, stream=None):
     [batch, rows]) under logits [..., V] / temperature (float32 or bfloat16 CUDA
     tensor with contiguous rows and any strides between them); 0 where a
     target is negative.  float32, in targets' shape."""
-    import torch
     tok = _tokens(logits, targets, temperature)
     device = logits.device
     ctx, handle = _on_stream(stream, device, (logits, targets))
-    opts = Opts(stream=handle)
     with ctx:
-        logp = torch.empty(targets.shape, dtype=torch.float32, device=device)
+        logp = _torch.empty(targets.shape, dtype=_torch.float32, device=device)
         rc = load().aloco_token_logprobs(ctypes.byref(tok), logp.data_ptr(),
-                                         ctypes.byref(opts))
+                                         ctypes.byref(Opts(stream=handle)))
     _finish(rc, ctx, logp)
     return logp
 
@@ -914,28 +930,25 @@ def policy_loss(logits, targets, advantages, old_logp, weights, *, ref_logp=None
     target take no part.  grad (optional) receives the gradient and may be
     `logits` itself; without it a new tensor does, unless want_grad is False.
     Enqueues only."""
-    import torch
     tok = _tokens(logits, targets, temperature)
     device = logits.device
-    adv, old, w = (_per_row("advantages", advantages, logits),
-                   _per_row("old_logp", old_logp, logits), _per_row("weights", weights, logits))
-    ref = _per_row("ref_logp", ref_logp, logits) if ref_logp is not None else None
+    adv = _per_row("advantages", advantages, targets, device)
+    old = _per_row("old_logp", old_logp, targets, device)
+    w = _per_row("weights", weights, targets, device)
+    ref = _per_row("ref_logp", ref_logp, targets, device) if ref_logp is not None else None
     cfg = PolicyCfg(clip_low, clip_high, kl_coef)
     ctx, handle = _on_stream(stream, device, (logits, targets, advantages, old_logp, weights,
                                               ref_logp, grad))
-    opts = Opts(stream=handle)
     lib = load()
     with ctx:
         out, desc = _logits_grad(logits, grad, want_grad)
-        n = targets.numel()
-        terms = torch.empty(4, dtype=torch.float32, device=device)
-        logp = torch.empty(targets.shape, dtype=torch.float32, device=device)
-        need = lib.aloco_loss_scratch_bytes(n)
-        scratch = torch.empty(need, dtype=torch.uint8, device=device)
+        logp = _torch.empty_like(old_logp)
+        terms = _torch.empty(4, dtype=_torch.float32, device=device)
+        need = lib.aloco_loss_scratch_bytes(tok.batch * tok.rows)
+        scratch = _torch.empty(need, dtype=_torch.uint8, device=device)
         rc = lib.aloco_policy_loss(ctypes.byref(tok), adv, old, ref, w, ctypes.byref(cfg),
-                                   terms.data_ptr(), logp.data_ptr(),
-                                   ctypes.byref(desc) if desc is not None else None,
-                                   scratch.data_ptr(), need, ctypes.byref(opts))
+                                   terms.data_ptr(), logp.data_ptr(), desc, scratch.data_ptr(),
+                                   need, ctypes.byref(Opts(stream=handle)))
     _finish(rc, ctx, terms, logp, out)
     return PolicyLoss(terms, logp, out)
 
@@ -949,11 +962,14 @@ def preference_loss(logits, targets, cu_seqlens, ref_logp=None, *, beta: float =
     answers in turn; rows with a negative target (prompts, padding) take no
     part.  ref_logp is float32 of targets' shape (None: no reference).  grad
     and want_grad as policy_loss.  Enqueues only."""
-    import torch
     tok = _tokens(logits, targets, temperature)
     device = logits.device
-    ref = _per_row("ref_logp", ref_logp, logits) if ref_logp is not None else None
-    if cu_seqlens.dtype not in (torch.int32, torch.int64):
+    ref = _per_row("ref_logp", ref_logp, targets, device) if ref_logp is not None else None
+    if cu_seqlens.dtype is _torch.int32:
+        cu_bytes = 4
+    elif cu_seqlens.dtype is _torch.int64:
+        cu_bytes = 8
+    else:
         raise TypeError(f"cu_seqlens must be int32 or int64, not {cu_seqlens.dtype}")
     if cu_seqlens.dim() != 1 or cu_seqlens.numel() % 2 == 0 or \
             not cu_seqlens.is_contiguous() or cu_seqlens.device != device:
@@ -962,21 +978,19 @@ def preference_loss(logits, targets, cu_seqlens, ref_logp=None, *, beta: float =
     pairs = cu_seqlens.numel() // 2
     cfg = PreferenceCfg(beta, label_smoothing)
     ctx, handle = _on_stream(stream, device, (logits, targets, cu_seqlens, ref_logp, grad))
-    opts = Opts(stream=handle)
     lib = load()
     with ctx:
+        f32 = {"dtype": _torch.float32, "device": device}
         out, desc = _logits_grad(logits, grad, want_grad)
-        n = targets.numel()
-        loss = torch.empty((), dtype=torch.float32, device=device)
-        ratios = torch.empty(2 * pairs, dtype=torch.float32, device=device)
-        logp = torch.empty(targets.shape, dtype=torch.float32, device=device)
-        need = lib.aloco_loss_scratch_bytes(n)
-        scratch = torch.empty(need, dtype=torch.uint8, device=device)
+        loss = _torch.empty((), **f32)
+        ratios = _torch.empty(2 * pairs, **f32)
+        logp = _torch.empty(targets.shape, **f32)
+        need = lib.aloco_loss_scratch_bytes(tok.batch * tok.rows)
+        scratch = _torch.empty(need, dtype=_torch.uint8, device=device)
         rc = lib.aloco_preference_loss(
-            ctypes.byref(tok), ref, cu_seqlens.data_ptr(), cu_seqlens.element_size(), pairs,
-            ctypes.byref(cfg), loss.data_ptr(), ratios.data_ptr(), logp.data_ptr(),
-            ctypes.byref(desc) if desc is not None else None, scratch.data_ptr(), need,
-            ctypes.byref(opts))
+            ctypes.byref(tok), ref, cu_seqlens.data_ptr(), cu_bytes, pairs, ctypes.byref(cfg),
+            loss.data_ptr(), ratios.data_ptr(), logp.data_ptr(), desc, scratch.data_ptr(), need,
+            ctypes.byref(Opts(stream=handle)))
     _finish(rc, ctx, loss, ratios, logp, out)
     return PreferenceLoss(loss, ratios, logp, out)
 
@@ -1000,7 +1014,8 @@ class GradList:
             if not t.is_cuda or t.device != self.device or not t.is_contiguous():
                 raise ValueError("gradients must be contiguous CUDA tensors of one device")
         n = len(self.tensors)
-        self._at = [t.data_ptr() for t in self.tensors]
+        self._pointers = [t.data_ptr for t in self.tensors]
+        self._at = [p() for p in self._pointers]
         sizes = [t.numel() for t in self.tensors]
         self.numel = sum(sizes)
         handle = ctypes.c_void_p()
@@ -1014,7 +1029,7 @@ class GradList:
         self._handle = handle
 
     def _check(self):
-        if [t.data_ptr() for t in self.tensors] != self._at:
+        if [p() for p in self._pointers] != self._at:
             raise ValueError("a gradient's memory has moved since the GradList was made")
 
     def __del__(self):
@@ -1033,13 +1048,11 @@ def _grad_list(grads) -> GradList:
 def grad_norm(grads, *, stream=None):
     """Global norm of a GradList (or of a sequence of tensors, which costs a new
     list each time): a float32 scalar tensor.  Enqueues only."""
-    import torch
     g = _grad_list(grads)
     ctx, handle = _on_stream(stream, g.device, g.tensors)
-    opts = Opts(stream=handle)
     with ctx:
-        norm = torch.empty((), dtype=torch.float32, device=g.device)
-        rc = load().aloco_grad_norm(g._handle, norm.data_ptr(), ctypes.byref(opts))
+        norm = _torch.empty((), dtype=_torch.float32, device=g.device)
+        rc = load().aloco_grad_norm(g._handle, norm.data_ptr(), ctypes.byref(Opts(stream=handle)))
     _finish(rc, ctx, norm)
     return norm
 
@@ -1049,7 +1062,6 @@ def clip_grads(grads, max_norm: float, *, out=None, stream=None):
     with `out` (a contiguous float32 or bfloat16 vector of all their elements),
     into it, tensor after tensor, as adamw_step takes them.  Returns the norm
     before clipping, a float32 scalar tensor.  Enqueues only."""
-    import torch
     g = _grad_list(grads)
     if out is not None and (out.numel() != g.numel or not out.is_contiguous() or
                             out.device != g.device):
@@ -1057,11 +1069,10 @@ def clip_grads(grads, max_norm: float, *, out=None, stream=None):
                          "gradients' device")
     dtype = _replica_dtype_code(out) if out is not None else F32
     ctx, handle = _on_stream(stream, g.device, g.tensors if out is None else [*g.tensors, out])
-    opts = Opts(stream=handle)
     with ctx:
-        norm = torch.empty((), dtype=torch.float32, device=g.device)
+        norm = _torch.empty((), dtype=_torch.float32, device=g.device)
         rc = load().aloco_clip_grads(g._handle, max_norm,
                                      out.data_ptr() if out is not None else None, dtype,
-                                     norm.data_ptr(), ctypes.byref(opts))
+                                     norm.data_ptr(), ctypes.byref(Opts(stream=handle)))
     _finish(rc, ctx, norm)
     return norm

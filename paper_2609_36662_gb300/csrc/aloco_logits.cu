@@ -45,9 +45,12 @@ __device__ __forceinline__ void wait_for_previous() {
 
 // What a row kernel leaves: log-probabilities, also a gradient, the same where
 // the gradient's rows may lie otherwise to the 16-byte boundaries than the
-// logits' do, or what the preference loss needs of a row.
-constexpr int kFwd = 0, kPolicy = 1, kPolicyShifted = 2, kPref = 3;
-constexpr bool has_grad(int mode) { return mode == kPolicy || mode == kPolicyShifted; }
+// logits' do, what the preference loss needs of a row, or its gradient.
+constexpr int kFwd = 0, kPolicy = 1, kPolicyShifted = 2, kPref = 3, kGrad = 4, kGradShifted = 5;
+constexpr bool is_policy(int mode) { return mode == kPolicy || mode == kPolicyShifted; }
+constexpr bool is_grad(int mode) { return mode == kGrad || mode == kGradShifted; }
+constexpr bool writes_grad(int mode) { return is_policy(mode) || is_grad(mode); }
+constexpr bool may_shift(int mode) { return mode == kPolicyShifted || mode == kGradShifted; }
 
 template <bool BF16>
 struct Unit {
@@ -92,30 +95,6 @@ __device__ __forceinline__ void store1(char *base, int e, float v) {
         reinterpret_cast<float *>(base)[e] = v;
 }
 
-// Unit u of a row; places outside the row hold -inf.
-template <bool BF16>
-__device__ __forceinline__ uint4 load_unit(const Window &w, int u) {
-    constexpr int E = Unit<BF16>::kElems;
-    const int e0 = u * E;
-    if (e0 >= w.head && e0 + E <= w.end) return __ldcs(reinterpret_cast<const uint4 *>(w.base) + u);
-    uint32_t r[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if constexpr (BF16) {
-            const int e = e0 + 2 * j;
-            const uint16_t *p = reinterpret_cast<const uint16_t *>(w.base);
-            const uint32_t a = e >= w.head && e < w.end ? p[e] : 0xff80u;
-            const uint32_t b = e + 1 >= w.head && e + 1 < w.end ? p[e + 1] : 0xff80u;
-            r[j] = a | b << 16;
-        } else {
-            const int e = e0 + j;
-            r[j] = e >= w.head && e < w.end ? reinterpret_cast<const uint32_t *>(w.base)[e]
-                                            : 0xff800000u;
-        }
-    }
-    return make_uint4(r[0], r[1], r[2], r[3]);
-}
-
 // One 16-byte unit of a row's elements, unit u of the source's window, element
 // by element into a row that may lie otherwise to the 16-byte boundaries.
 template <bool BF16>
@@ -151,24 +130,6 @@ __device__ __forceinline__ void store_some(const Window &g, int e0, int lo, int 
             else
                 reinterpret_cast<uint32_t *>(g.base)[e0 + j] = r[j];
         }
-}
-
-// The same, in one piece where the unit is whole and both rows lie alike.
-template <bool BF16>
-__device__ __forceinline__ void store_unit(const Window &src, const Window &dst, int u,
-                                           const uint4 &q) {
-    constexpr int E = Unit<BF16>::kElems;
-    if (src.head == dst.head && u * E >= src.head && u * E + E <= src.end)
-        __stcs(reinterpret_cast<uint4 *>(dst.base) + u, q);
-    else
-        store_elems<BF16>(src, dst, u, q);
-}
-
-// Zeros in a row's units first, first + step, ...
-template <bool BF16>
-__device__ __forceinline__ void zero_units(const Window &w, int first, int step) {
-    for (int u = first; u < w.units; u += step)
-        store_unit<BF16>(w, w, u, make_uint4(0, 0, 0, 0));
 }
 
 __device__ __forceinline__ int64_t load_index(const void *p, int64_t i, int bytes) {
@@ -427,6 +388,8 @@ struct Sum {
         rest += (s - (t - b)) + (x - b);
         s = t;
     }
+    // (an infinite sum has no rest)
+    __device__ __forceinline__ float value() const { return fabsf(s) <= FLT_MAX ? s + rest : s; }
 };
 
 __device__ __forceinline__ int clamp_count(int n, int most) { return max(0, min(n, most)); }
@@ -561,10 +524,18 @@ __device__ __forceinline__ bool all_of(bool yes) {
     return r != 0;
 }
 
+// The row at a place of the kernel's order.  The gradients of the preference
+// loss go from the last row to the first, so that they meet the logits that L2
+// still holds of the pass before.
+template <int MODE>
+__device__ __forceinline__ int64_t row_at(const LogitsArgs &a, int64_t place) {
+    return is_grad(MODE) ? a.n - 1 - place : place;
+}
+
 // NaN in a row that the block has given up.
 template <int MODE>
 __device__ __forceinline__ void give_up(const LogitsArgs &a, int64_t row) {
-    a.logp[row] = NAN;
+    a.logp[row_at<MODE>(a, row)] = NAN;
     if constexpr (MODE == kPref) {
         a.stats[row] = make_float2(NAN, NAN);
         a.coef[row] = 0.f;
@@ -613,6 +584,8 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
         cluster.sync();
     else
         __syncthreads();
+    wait_for_previous();
+    if (MODE == kPref && blockIdx.x == 0 && tid == 0) *a.ticket = 0;
 
     if (tid >= THREADS) {
         // Producer: the rows' scalars, kBatch rows at a time, and their parts,
@@ -623,40 +596,47 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
         unsigned filled = 0;
         bool ok = true, mixed = false, again = false;
         unsigned char *const zeros = ring + (size_t)stages * SLOT * 16;
-        if (has_grad(MODE) && a.g.data) {
+        if (writes_grad(MODE) && a.g.data) {
             for (int i = lane; i < ZEROS / 16; i += 32)
                 reinterpret_cast<uint4 *>(zeros)[i] = make_uint4(0, 0, 0, 0);
             fence_proxy_async_smem();
             __syncwarp();
         }
         for (int64_t base = row0; base < a.n && ok; base += kBatch * step, batch.next(2)) {
-            const int64_t my_row = base + lane * step;
+            const int64_t my_place = base + lane * step;
+            const int64_t my_row = row_at<MODE>(a, my_place);
             RowInfo mine = {make_float4(1.f, 0.f, 0.f, 0.f), nullptr, 0, 0, -1, NAN};
             Window my_x = {};
             int64_t t = -1;
-            if (my_row < a.n) {
+            if (my_place < a.n) {
                 t = load_index(a.target, my_row, a.target_bytes);
-                if constexpr (has_grad(MODE)) {
+                if constexpr (is_policy(MODE)) {
                     mine.f = make_float4(a.w[my_row], a.old[my_row], a.ref ? a.ref[my_row] : 0.f,
                                          a.adv[my_row]);
                     if (mine.f.x == 0.f) t = -1;
-                    if (a.g.data) {
-                        const Window g = window_of<BF16>(a.g, my_row, a.vocab);
-                        mine.g = g.base;
-                        mine.g_head = g.head;
-                    }
+                }
+                if constexpr (is_grad(MODE)) {
+                    const float k = a.coef[my_row] * a.inv_temp;
+                    const float2 q = a.stats[my_row];
+                    mine.f = make_float4(k, -k * q.y, base_of(q.x), 0.f);
+                    if (k == 0.f) t = -1;
+                }
+                if (writes_grad(MODE) && a.g.data) {
+                    const Window g = window_of<BF16>(a.g, my_row, a.vocab);
+                    mine.g = g.base;
+                    mine.g_head = g.head;
                 }
                 my_x = window_of<BF16>(a.x, my_row, a.vocab);
                 mine.head = my_x.head;
             }
             // read here, and so before this CTA lets the row's gradient be
             // written, which may lie over the logits
-            if (t >= 0 && t < a.vocab) mine.xt = load1<BF16>(my_x.base, my_x.head + (int)t);
+            if (!is_grad(MODE) && t >= 0 && t < a.vocab) mine.xt = load1<BF16>(my_x.base, my_x.head + (int)t);
             mine.target = t < 0 ? -1 : t >= a.vocab ? a.vocab : (int)t;
             unsigned todo = __ballot_sync(0xffffffffu, t >= 0);
             // rows without a part to play: this CTA's part of their zeros
-            unsigned idle = has_grad(MODE) && a.g.data
-                                ? __ballot_sync(0xffffffffu, my_row < a.n && t < 0) : 0u;
+            unsigned idle = writes_grad(MODE) && a.g.data
+                                ? __ballot_sync(0xffffffffu, my_place < a.n && t < 0) : 0u;
             // The window of the next row and the elements at its ends are
             // fetched a row ahead.
             Window ahead_x = {};
@@ -685,7 +665,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&s_rows_full[batch.i]));
             };
-            if (!has_grad(MODE)) tell();
+            if (!is_policy(MODE)) tell();
             while (ok && (!told || todo || idle)) {
                 if (idle && (!todo || (told && __ffs(idle) < __ffs(todo)))) {
                     const int from = __ffs(idle) - 1;
@@ -736,7 +716,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
             again = again || batch.i == 1;
         }
         // the zeros' source stays until their copies have read it
-        if (has_grad(MODE) && lane == 0) bulk_wait_all();
+        if (writes_grad(MODE) && lane == 0) bulk_wait_all();
         if (!ok) {  // given up: no copy may land after the block has ended
             s_abort = 1;
             for (unsigned k = 0; k < (unsigned)stages && k < filled; ++k) {
@@ -759,7 +739,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
         // This thread's units of the next slot, which holds `count` (none: 0),
         // -inf where it has none.
         const auto take_slot = [&](uint4 *q, int count, bool shifted) {
-            const Units w = units_of<THREADS>(count, tid, MODE == kPolicyShifted && shifted);
+            const Units w = units_of<THREADS>(count, tid, may_shift(MODE) && shifted);
             const int left = w.end - w.first;
             if (count > 0) ok = mbar_wait(smem_addr(&s_full[place.i]), place.phase, aborted) && ok;
             const uint4 *slot = reinterpret_cast<const uint4 *>(ring) + (size_t)place.i * SLOT + w.first;
@@ -794,7 +774,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
             const RowInfo r = s_rows[batch.i][next++];
             const bool first = rank == 0 && tid == 0;
             if (r.target < 0) {  // the producer writes its zeros
-                if (first) {
+                if (!is_grad(MODE) && first) {
                     a.logp[row] = 0.f;
                     if constexpr (MODE == kPref) a.coef[row] = 0.f;
                 }
@@ -802,11 +782,45 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
             }
             const Window x = window_at<BF16>(nullptr, r.head, a.vocab);
             const Part p = part_of(x.units, rank, log_c);
+            if constexpr (is_grad(MODE)) {
+                // the preference loss's gradient, slot by slot
+                const f2 neg = pair(-r.f.z, -r.f.z);
+                const int at = r.target < a.vocab ? x.head + r.target : INT_MIN / 2;
+                const bool shifted = r.g_head != r.head;
+                for (int u = 0; u < p.count; u += SLOT) {
+                    const int count = clamp_count(p.count - u, SLOT), u0 = p.first + u;
+                    uint4 q[DEPTH];
+                    take_slot(q, count, shifted);
+                    if (!ok) {
+                        s_abort = 1;
+                        if (first) give_up<MODE>(a, row);
+                    }
+                    const float f = ok ? r.f.y : NAN;
+                    f2 v[DEPTH][P];
+#pragma unroll
+                    for (int j = 0; j < DEPTH; ++j) {
+                        widen<BF16>(q[j], v[j]);
+#pragma unroll
+                        for (int h = 0; h < P; ++h) v[j][h] = exp_of2(v[j][h], neg, hi2, lo2);
+                    }
+                    if (may_shift(MODE) && shifted) {
+                        const Units w = units_of<THREADS>(count, tid, true);
+                        const int from = u0 + w.first - lane;
+                        store_shifted<BF16, DEPTH>(v, x, window_at<BF16>(r.g, r.g_head, a.vocab), from,
+                                                   max(w.end - w.first + lane, 0), lane, r.f.x,
+                                                   pair(f, f), at - from * E);
+                    } else {
+                        store_alike<BF16, DEPTH, THREADS>(v, x, r.g, u0, count, tid, r.f.x, pair(f, f),
+                                                          at - u0 * E);
+                    }
+                }
+                continue;
+            }
             // this thread's maximum, and the sum of its exp((x - maximum) /
             // tau): all of them at once where they are kept for the gradient,
             // slot by slot otherwise
-            constexpr bool kHold = has_grad(MODE);
-            const bool shifted = kHold && r.g && r.g_head != r.head;
+            constexpr bool kHold = is_policy(MODE);
+            const bool shifted = r.g && r.g_head != r.head;
             f2 v[kHold ? UPT : 1][P];
             float mt = -INFINITY, st = 0.f;
             if constexpr (kHold) {
@@ -870,7 +884,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
             // a row without a finite logit leaves z = 0: -inf - -inf
             const float logp = z > 0.f ? fmaf(r.xt - m, a.inv_temp, -logf(z)) : NAN;
 
-            if constexpr (has_grad(MODE)) {
+            if constexpr (is_policy(MODE)) {
                 const float weight = r.f.x;
                 const Scale unit = {kLog2e, kLog2eLo};
                 const float ratio = exp_of(logp, r.f.y, unit);
@@ -902,7 +916,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
                 for (int i = 0; i < UPT; i += DEPTH) {
                     const int count = clamp_count(p.count - i * THREADS, SLOT);
                     const int u0 = p.first + i * THREADS;
-                    if (MODE == kPolicyShifted && shifted) {
+                    if (may_shift(MODE) && shifted) {
                         const Units w = units_of<THREADS>(count, tid, true);
                         const int from = u0 + w.first - lane;
                         store_shifted<BF16, DEPTH>(v + i, x, window_at<BF16>(r.g, r.g_head, a.vocab),
@@ -921,27 +935,14 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
                 }
             }
         }
-        if (has_grad(MODE) && rank == 0 && tid == 0)
-            for (int j = 0; j < kTerms; ++j) a.terms[row0 * kTerms + j] = (double)terms[j].s + (double)terms[j].rest;
+        if (is_policy(MODE) && rank == 0 && tid == 0)
+            for (int j = 0; j < kTerms; ++j) a.terms[row0 * kTerms + j] = (double)terms[j].value();
     }
     // no CTA leaves while another may still write to its memory
     if (C > 1)
         cluster.sync();
     else
         __syncthreads();
-}
-
-// Sum over the block in a fixed order (fp64); valid in every thread.
-template <int THREADS>
-__device__ __forceinline__ double block_total(double v, double *sh) {
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
-    __syncthreads();
-    double s = 0.0;
-    for (int i = 0; i < THREADS / 32; ++i) s += sh[i];
-    __syncthreads();
-    return s;
 }
 
 // The policy loss's sums over the clusters of its row kernel.  One warp: fp64
@@ -962,79 +963,84 @@ __global__ void __launch_bounds__(32)
     }
 }
 
-// Log ratios, losses and the rows' coefficients: one warp a pair, then one
-// sum over the pairs.
-__global__ void __launch_bounds__(1024) pairs_kernel(const __grid_constant__ LogitsArgs a) {
-    __shared__ double sh[32];
-    const int lane = threadIdx.x & 31;
-    double sum = 0.0;
-    wait_for_previous();
-    for (int64_t k = threadIdx.x >> 5; k < a.pairs; k += 32) {
-        int64_t lo[2], hi[2];
-        double R[2];
-        for (int i = 0; i < 2; ++i) {
-            lo[i] = load_index(a.cu, 2 * k + i, a.cu_bytes);
-            hi[i] = load_index(a.cu, 2 * k + i + 1, a.cu_bytes);
-            lo[i] = lo[i] < 0 ? 0 : lo[i];
-            hi[i] = hi[i] > a.n ? a.n : hi[i];
-            double s = 0.0;
-            for (int64_t r = lo[i] + lane; r < hi[i]; r += 32)
-                if (load_index(a.target, r, a.target_bytes) >= 0)
-                    s += (double)a.logp[r] - (a.ref ? (double)a.ref[r] : 0.0);
+// Log ratios, losses and the rows' coefficients, a pair for each block in turn;
+// the last block to finish adds the losses.  In fp32 with the additions' rests
+// kept: fp64 units are rare here (one fp64 exp took longer than a pair's rows).
+constexpr int kPairBlock = 256;
+
+// The sum of `s` over the block in a fixed order, in every thread.
+__device__ __forceinline__ Sum block_total(Sum s, float2 *sh) {
 #pragma unroll
-            for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-            R[i] = s;
-        }
-        const double z = a.beta * (R[0] - R[1]);
-        const double t = exp(-fabs(z));
-        // -log sigmoid(z) = log(1 + exp(-|z|)) + max(-z, 0)
-        sum += log1p(t) + (z < 0.0 ? (1.0 - a.eps) * -z : a.eps * z);
-        const double sig = z >= 0.0 ? 1.0 / (1.0 + t) : t / (1.0 + t);
-        const double slope = (sig - (1.0 - a.eps)) * a.beta / (double)a.pairs;
-        if (lane < 2) a.ratios[2 * k + lane] = (float)R[lane];
-        if (a.g.data)
-            for (int i = 0; i < 2; ++i)
-                for (int64_t r = lo[i] + lane; r < hi[i]; r += 32)
-                    if (load_index(a.target, r, a.target_bytes) >= 0)
-                        a.coef[r] = (float)(i ? -slope : slope);
+    for (int off = 16; off > 0; off >>= 1) {
+        const float a = __shfl_xor_sync(0xffffffffu, s.s, off);
+        const float b = __shfl_xor_sync(0xffffffffu, s.rest, off);
+        s.add(a);
+        s.rest += b;
     }
-    if (lane) sum = 0.0;
-    sum = block_total<1024>(sum, sh);
-    if (threadIdx.x == 0) a.loss[0] = a.pairs ? (float)(sum / (double)a.pairs) : 0.f;
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = make_float2(s.s, s.rest);
+    __syncthreads();
+    s = {0.f, 0.f};
+    for (int i = 0; i < kPairBlock / 32; ++i) {
+        s.add(sh[i].x);
+        s.rest += sh[i].y;
+    }
+    return s;
 }
 
-// The preference loss's gradient: k ([j = a] - exp((x_j - m) / tau) / z).
-template <bool BF16>
-__global__ void __launch_bounds__(512) grad_kernel(const __grid_constant__ LogitsArgs a) {
-    constexpr int E = Unit<BF16>::kElems;
-    const int64_t row = blockIdx.x;
-    const Window g = window_of<BF16>(a.g, row, a.vocab);
+// -(1 - eps) log sigmoid(z) - eps log sigmoid(-z)
+__device__ __forceinline__ float pair_loss(float z, float eps) {
+    // -log sigmoid(z) = log(1 + exp(-|z|)) + max(-z, 0)
+    return log1pf(expf(-fabsf(z))) + (z < 0.f ? (1.f - eps) * -z : eps * z);
+}
+
+__global__ void __launch_bounds__(kPairBlock)
+    pairs_kernel(const __grid_constant__ LogitsArgs a) {
+    __shared__ float2 sh[kPairBlock / 32];
+    __shared__ bool last;
+    const int tid = threadIdx.x;
     wait_for_previous();
-    const int64_t target = load_index(a.target, row, a.target_bytes);
-    const float k = a.coef[row] * a.inv_temp;
-    if (target < 0 || k == 0.f) {
-        zero_units<BF16>(g, threadIdx.x, 512);
-        return;
-    }
-    const Window x = window_of<BF16>(a.x, row, a.vocab);
-    const float2 q = a.stats[row];
-    const float f = -k * q.y;
-    const float base = base_of(q.x);
-    const f2 hi2 = pair(a.scale, a.scale), lo2 = pair(a.scale_lo, a.scale_lo);
-    const f2 neg = pair(-base, -base), ff = pair(f, f);
-    const int at = target < a.vocab ? x.head + (int)target : -1;
-    for (int u = threadIdx.x; u < x.units; u += 512) {
-        f2 v[E / 2];
-        widen<BF16>(load_unit<BF16>(x, u), v);
-#pragma unroll
-        for (int j = 0; j < E / 2; ++j) {
-            v[j] = mul2(exp_of2(v[j], neg, hi2, lo2), ff);
-            if (u == at / E)
-                v[j] = add2(v[j], pair(u * E + 2 * j == at ? k : 0.f,
-                                       u * E + 2 * j + 1 == at ? k : 0.f));
+    for (int64_t k = blockIdx.x; k < a.pairs; k += gridDim.x) {
+        int64_t cu[3];
+        for (int i = 0; i < 3; ++i) {
+            cu[i] = load_index(a.cu, 2 * k + i, a.cu_bytes);
+            cu[i] = cu[i] < 0 ? 0 : cu[i] > a.n ? a.n : cu[i];
         }
-        store_unit<BF16>(x, g, u, narrow<BF16>(v));
+        float R[2];
+        for (int i = 0; i < 2; ++i) {
+            Sum s = {0.f, 0.f};
+            for (int64_t r = cu[i] + tid; r < cu[i + 1]; r += kPairBlock)
+                if (load_index(a.target, r, a.target_bytes) >= 0) {
+                    s.add(a.logp[r]);
+                    if (a.ref) s.add(-a.ref[r]);
+                }
+            s = block_total(s, sh);
+            R[i] = s.value();
+        }
+        if (tid < 2) a.ratios[2 * k + tid] = R[tid];
+        if (!a.g.data) continue;
+        const float z = a.beta * (R[0] - R[1]), t = expf(-fabsf(z));
+        // sigmoid(z) - 1 + eps, without the difference where z is large
+        const float slope = (z >= 0.f ? a.eps - t / (1.f + t) : t / (1.f + t) - (1.f - a.eps)) *
+                            a.per_pair;
+        for (int64_t r = cu[0] + tid; r < cu[2]; r += kPairBlock)
+            if (load_index(a.target, r, a.target_bytes) >= 0) a.coef[r] = r < cu[1] ? slope : -slope;
     }
+    if (gridDim.x > 1) {
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
+        __syncthreads();
+        if (!last) return;
+        __threadfence();
+    } else {
+        __syncthreads();
+    }
+    Sum s = {0.f, 0.f};
+    for (int64_t k = tid; k < a.pairs; k += kPairBlock)
+        s.add(pair_loss(a.beta * (__ldcg(a.ratios + 2 * k) - __ldcg(a.ratios + 2 * k + 1)), a.eps));
+    s = block_total(s, sh);
+    if (tid == 0) a.loss[0] = a.pairs ? s.value() / (float)a.pairs : 0.f;
 }
 
 // Launch of a row kernel of THREADS consumers with EPT elements each: a
@@ -1045,7 +1051,7 @@ template <bool BF16, int THREADS, int EPT, int DEPTH, int STAGES, int CTAS, int 
 cudaError_t launch_rows_as(const LogitsArgs &in, int sm_count, cudaStream_t stream, int *used) {
     constexpr int E = Unit<BF16>::kElems, UPT = EPT / E;
     constexpr int kSlot = DEPTH * THREADS * 16;
-    constexpr int kSmem = STAGES * kSlot + (!has_grad(MODE) ? 0 : kSlot / 4 < 8192 ? kSlot / 4 : 8192);
+    constexpr int kSmem = STAGES * kSlot + (!writes_grad(MODE) ? 0 : kSlot / 4 < 8192 ? kSlot / 4 : 8192);
     static_assert(STAGES <= kMaxStages && UPT % DEPTH == 0, "ring");
     static PerDevice ready, most[kMaxCluster + 1];
     const auto kernel = row_kernel<BF16, THREADS, UPT, DEPTH, CTAS, MODE>;
@@ -1053,7 +1059,7 @@ cudaError_t launch_rows_as(const LogitsArgs &in, int sm_count, cudaStream_t stre
     int log_c = 0;
     // (the forward kernels take a part of any length, slot by slot)
     const auto fits = [&](int c) {
-        return !has_grad(MODE) || (units + (1 << c) - 1) >> c <= THREADS * UPT;
+        return !is_policy(MODE) || (units + (1 << c) - 1) >> c <= THREADS * UPT;
     };
     while (!fits(log_c))
         if ((1 << ++log_c) > kMaxCluster) return cudaErrorInvalidValue;
@@ -1069,16 +1075,19 @@ cudaError_t launch_rows_as(const LogitsArgs &in, int sm_count, cudaStream_t stre
         if (e != cudaSuccess) return e;
         ready.set(dev, 1);
     }
-    cudaLaunchAttribute attr = {};
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = (unsigned)C;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[2] = {};
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)C;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    // the kernel sets itself up while the one before it ends
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)C);
     cfg.blockDim = dim3(THREADS + 32);
     cfg.dynamicSmemBytes = kSmem;
     cfg.stream = stream;
-    cfg.attrs = &attr;
+    cfg.attrs = attr;
     cfg.numAttrs = 1;
     int clusters = most[C].get(dev);
     if (!clusters) {
@@ -1087,6 +1096,7 @@ cudaError_t launch_rows_as(const LogitsArgs &in, int sm_count, cudaStream_t stre
         if (clusters < 1) return cudaErrorInvalidConfiguration;
         most[C].set(dev, clusters);
     }
+    cfg.numAttrs = 2;
     LogitsArgs a = in;
     a.stages = STAGES;
     a.log_c = log_c;
@@ -1103,14 +1113,16 @@ cudaError_t launch_rows(const LogitsArgs &a, int sm_count, cudaStream_t stream, 
         return launch_rows_as<BF16, 32, 72, 9, 3, 8, MODE>(a, sm_count, stream, used);
     if (a.vocab <= 64 * 72 - 14)
         return launch_rows_as<BF16, 64, 72, 9, 3, 5, MODE>(a, sm_count, stream, used);
-    if constexpr (!has_grad(MODE))
+    if constexpr (!is_policy(MODE)) {
         return launch_rows_as<BF16, 224, 72, 3, 5, 4, MODE>(a, sm_count, stream, used);
-    if (a.vocab <= 128 * 72 - 14)
-        return launch_rows_as<BF16, 128, 72, 9, 3, 3, MODE>(a, sm_count, stream, used);
-    if (a.vocab <= 224 * 72 - 14 ||
-        (a.vocab > 480 * 72 - 14 && a.vocab <= kMaxCluster * 224 * 72 - 14))
-        return launch_rows_as<BF16, 224, 72, 9, 3, 2, MODE>(a, sm_count, stream, used);
-    return launch_rows_as<BF16, 480, 72, 9, 3, 1, MODE>(a, sm_count, stream, used);
+    } else {
+        if (a.vocab <= 128 * 72 - 14)
+            return launch_rows_as<BF16, 128, 72, 9, 3, 3, MODE>(a, sm_count, stream, used);
+        if (a.vocab <= 224 * 72 - 14 ||
+            (a.vocab > 480 * 72 - 14 && a.vocab <= kMaxCluster * 224 * 72 - 14))
+            return launch_rows_as<BF16, 224, 72, 9, 3, 2, MODE>(a, sm_count, stream, used);
+        return launch_rows_as<BF16, 480, 72, 9, 3, 1, MODE>(a, sm_count, stream, used);
+    }
 }
 
 // A launch that may begin before the kernel ahead of it in the stream has
@@ -1130,6 +1142,16 @@ cudaError_t launch_behind(void (*kernel)(Params...), unsigned grid, unsigned blo
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+// Whether all rows of the gradient lie to the 16-byte boundaries as the logits'.
+bool rows_alike(const LogitsArgs &a, aloco_dtype dtype) {
+    if (!a.g.data) return true;
+    const int64_t size = dtype == ALOCO_BF16 ? 2 : 4, per = a.x.per_batch;
+    int64_t off = (int64_t)((uintptr_t)a.x.data - (uintptr_t)a.g.data);
+    if (per > 1) off |= (a.x.row_stride - a.g.row_stride) * size;
+    if (a.n > per) off |= (a.x.batch_stride - a.g.batch_stride) * size;
+    return (off & 15) == 0;
+}
+
 }  // namespace
 
 cudaError_t launch_token_logprobs(const LogitsArgs &a, aloco_dtype dtype, int sm_count,
@@ -1142,11 +1164,7 @@ cudaError_t launch_token_logprobs(const LogitsArgs &a, aloco_dtype dtype, int sm
 cudaError_t launch_policy_loss(const LogitsArgs &a, aloco_dtype dtype, int sm_count,
                                cudaStream_t stream) {
     int used;
-    // do all rows of the gradient lie to the 16-byte boundaries as the logits'?
-    const int64_t size = dtype == ALOCO_BF16 ? 2 : 4, per = a.x.per_batch;
-    const bool alike = !a.g.data ||
-                       ((((int64_t)((uintptr_t)a.x.data - (uintptr_t)a.g.data)) | (per > 1 ? (a.x.row_stride - a.g.row_stride) * size : 0) |
-                         (a.n > per ? (a.x.batch_stride - a.g.batch_stride) * size : 0)) & 15) == 0;
+    const bool alike = rows_alike(a, dtype);
     const auto rows = [&](auto bf16) {
         constexpr bool B = decltype(bf16)::value;
         return alike ? launch_rows<B, kPolicy>(a, sm_count, stream, &used)
@@ -1159,14 +1177,18 @@ cudaError_t launch_policy_loss(const LogitsArgs &a, aloco_dtype dtype, int sm_co
 
 cudaError_t launch_preference_loss(const LogitsArgs &a, aloco_dtype dtype, int sm_count,
                                    cudaStream_t stream) {
-    int used;
-    cudaError_t e = dtype == ALOCO_BF16 ? launch_rows<true, kPref>(a, sm_count, stream, &used)
-                                        : launch_rows<false, kPref>(a, sm_count, stream, &used);
-    if (e == cudaSuccess) e = launch_behind(pairs_kernel, 1, 1024, stream, a);
-    if (e == cudaSuccess && a.g.data && a.n)
-        e = launch_behind(dtype == ALOCO_BF16 ? grad_kernel<true> : grad_kernel<false>,
-                          (unsigned)a.n, 512, stream, a);
-    return e;
+    const bool alike = rows_alike(a, dtype);
+    const unsigned blocks = a.n == 0 || a.pairs < 2 ? 1u : (unsigned)(a.pairs < 1024 ? a.pairs : 1024);
+    const auto all = [&](auto bf16) {
+        constexpr bool B = decltype(bf16)::value;
+        int used;
+        cudaError_t e = launch_rows<B, kPref>(a, sm_count, stream, &used);
+        if (e == cudaSuccess) e = launch_behind(pairs_kernel, blocks, kPairBlock, stream, a);
+        if (e != cudaSuccess || !a.g.data) return e;
+        return alike ? launch_rows<B, kGrad>(a, sm_count, stream, &used)
+                     : launch_rows<B, kGradShifted>(a, sm_count, stream, &used);
+    };
+    return dtype == ALOCO_BF16 ? all(std::true_type{}) : all(std::false_type{});
 }
 
 }  // namespace aloco

@@ -34,9 +34,10 @@ struct LogitsArgs {
     // preference loss (ref as above)
     const void *cu;
     int64_t pairs;
-    double beta, eps;
+    float beta, eps, per_pair;       // per_pair: beta / pairs
     float2 *stats;                   // [n] row maximum and 1 / sum (scratch)
     float *coef;                     // [n] dL/dlogp (scratch)
+    unsigned int *ticket;            // blocks of the pairs' kernel that are done (scratch)
     float *loss, *ratios;
     int stages, log_c;               // the row kernel's ring slots and cluster
 };

@@ -187,7 +187,7 @@ cudaStream_t stream_of(const aloco_opts_t *o) {
 
 extern "C" {
 
-size_t aloco_loss_scratch_bytes(int64_t rows) { return rows > 0 ? (size_t)rows * 24 : 0; }
+size_t aloco_loss_scratch_bytes(int64_t rows) { return rows > 0 ? (size_t)rows * 24 + 16 : 0; }
 
 int aloco_token_logprobs(const aloco_tokens_t *tokens, float *logp, const aloco_opts_t *opts) {
     aloco::LogitsArgs a;
@@ -282,13 +282,15 @@ int aloco_preference_loss(const aloco_tokens_t *tokens, const float *ref_logp,
     a.cu = cu_seqlens;
     a.cu_bytes = cu_bytes;
     a.pairs = pairs;
-    a.beta = cfg->beta;
-    a.eps = cfg->label_smoothing;
+    a.beta = (float)cfg->beta;
+    a.eps = (float)cfg->label_smoothing;
+    a.per_pair = pairs ? (float)(cfg->beta / (double)pairs) : 0.f;
     a.loss = loss;
     a.ratios = log_ratios;
     a.logp = logp;
     a.stats = static_cast<float2 *>(scratch);
     a.coef = reinterpret_cast<float *>(a.stats + a.n);
+    a.ticket = reinterpret_cast<unsigned int *>(a.coef + a.n);
     int sms;
     if ((rc = check_buffers(s, over, &sms)) != ALOCO_OK) return rc;
     const cudaError_t e =
