@@ -641,9 +641,9 @@ int aloco_grads_create(const void *const *grads, const int64_t *sizes,
 void aloco_grads_destroy(aloco_grads_t *grads);
 
 /* norm[1] (device fp32) = sqrt(sum of all g^2).  Squares are added in fp32
- * over at most 32 elements and then in fp64, in a fixed order; values whose
- * squares leave fp32's range are squared in fp64.  NaN or inf where a
- * gradient is.  Enqueues one kernel on opts->stream.  Calls with one handle
+ * over at most 32 elements and then in fp32 with the additions' rounding kept,
+ * in a fixed order; values whose squares leave fp32's range are squared and
+ * added in fp64.  NaN or inf where a gradient is, or the norm leaves fp32.  Enqueues one kernel on opts->stream.  Calls with one handle
  * share its partial sums: calls that overlap on the GPU race. */
 int aloco_grad_norm(aloco_grads_t *grads, float *norm,
                     const aloco_opts_t *opts);
@@ -656,7 +656,7 @@ int aloco_grad_norm(aloco_grads_t *grads, float *norm,
  *   else out is a flat vector of out_dtype that receives tensor after tensor
  *     in the handle's order, and the tensors are only read.  It may overlap
  *     none of them.
- * max_norm is finite and > 0.  norm[1] receives the norm before clipping.
+ * max_norm is finite and > 0 in fp32.  norm[1] receives the norm before clipping.
  * Enqueues two kernels. */
 int aloco_clip_grads(aloco_grads_t *grads, double max_norm, void *out,
                      aloco_dtype out_dtype, float *norm,

@@ -7,6 +7,8 @@
 // memory; blocks take stretches in turn, so that a set of many small and few
 // large tensors spreads evenly.  Both kernels stream: the norm reads every
 // gradient once, the scaling reads it again and writes it.
+#include <algorithm>
+
 #include "aloco_grads.h"
 #include "aloco_sync_kernel.cuh"
 
@@ -52,11 +54,25 @@ __device__ __forceinline__ int head_of(const void *p, int n) {
     return h < n ? h : n;
 }
 
-// Sum of the squares of up to 32 elements that this thread holds as units.
-// In fp32; where that leaves its range (a square above 3.4e38, or all so
-// small that theirs round away), again in fp64.
+// A sum of squares: in fp32 with what its additions rounded away (fp64 units are
+// rare here: with fp64 sums the norm of 3e6 elements took 14 us, most of it in
+// the reduction), and in fp64 what fp32 cannot hold.
+struct Squares {
+    float s = 0.f, rest = 0.f;
+    double wide = 0.0;
+    __device__ __forceinline__ void add(float x) {
+        const float t = s + x, b = t - s;
+        rest += (s - (t - b)) + (x - b);
+        s = t;
+    }
+    // x: a sum of at most 32 squares.  Below 1e25 the fp32 sum of 2^44 of them
+    // stays in range, and above 1e-30 squares that round away do not matter.
+    __device__ __forceinline__ static bool fits(float x) { return x >= 1e-30f && x <= 1e25f; }
+};
+
+// Add the squares of up to 32 elements that this thread holds as units.
 template <bool BF16>
-__device__ __forceinline__ double squares(const uint4 (&q)[kUnits]) {
+__device__ __forceinline__ void add_squares(Squares &acc, const uint4 (&q)[kUnits]) {
     constexpr int E = BF16 ? 8 : 4;
     float s = 0.f;
 #pragma unroll
@@ -66,22 +82,22 @@ __device__ __forceinline__ double squares(const uint4 (&q)[kUnits]) {
 #pragma unroll
         for (int j = 0; j < E; ++j) s = fmaf(v[j], v[j], s);
     }
-    if (s >= 1e-30f && s <= FLT_MAX) return (double)s;
-    double d = 0.0;
+    if (Squares::fits(s)) {
+        acc.add(s);
+        return;
+    }
     for (int k = 0; k < kUnits; ++k) {
         const uint32_t any = (q[k].x | q[k].y | q[k].z | q[k].w) &
                              (BF16 ? 0x7fff7fffu : 0x7fffffffu);
         if (!any) continue;
         float v[E];
         widen<BF16>(q[k], v);
-        for (int j = 0; j < E; ++j) d += (double)v[j] * (double)v[j];
+        for (int j = 0; j < E; ++j) acc.wide += (double)v[j] * (double)v[j];
     }
-    return d;
 }
 
 template <bool BF16>
-__device__ __forceinline__ double chunk_squares(const void *p, int n) {
-    double acc = 0.0;
+__device__ __forceinline__ void add_chunk(Squares &acc, const void *p, int n) {
     const int h = head_of<BF16>(p, n);
     constexpr int E = BF16 ? 8 : 4;
     const int units = (n - h) / E;
@@ -94,142 +110,200 @@ __device__ __forceinline__ double chunk_squares(const void *p, int n) {
             const int j = i + k * kGradBlock;
             q[k] = j < units ? __ldg(u + j) : make_uint4(0, 0, 0, 0);
         }
-        acc += squares<BF16>(q);
+        add_squares<BF16>(acc, q);
     }
     const int tail = h + units * E;
     for (int e = threadIdx.x; e < h + n - tail; e += kGradBlock) {
-        const double x = (double)grad1<BF16>(p, e < h ? e : tail + e - h);
-        acc += x * x;
+        const float x = grad1<BF16>(p, e < h ? e : tail + e - h);
+        if (Squares::fits(x * x))
+            acc.add(x * x);
+        else
+            acc.wide += (double)x * (double)x;
     }
-    return acc;
 }
 
-__device__ __forceinline__ double block_sum(double v) {
-    __shared__ double sh[kGradBlock / 32];
+// The block's sum in a fixed order, in thread 0.  fp64 only where some thread
+// has a part of its own there.
+__device__ __forceinline__ Squares block_sum(Squares v) {
+    __shared__ float2 sh[kGradBlock / 32];
+    __shared__ double sh_wide[kGradBlock / 32];
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) v += __shfl_down_sync(0xffffffffu, v, off);
-    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
+    for (int off = 16; off > 0; off >>= 1) {
+        const float s = __shfl_down_sync(0xffffffffu, v.s, off);
+        const float r = __shfl_down_sync(0xffffffffu, v.rest, off);
+        v.add(s);
+        v.rest += r;
+    }
+    const bool wide = __syncthreads_or(v.wide != 0.0);  // (NaN is not 0)
+    if (wide)
+        for (int off = 16; off > 0; off >>= 1)
+            v.wide += __shfl_down_sync(0xffffffffu, v.wide, off);
+    if ((threadIdx.x & 31) == 0) {
+        sh[threadIdx.x >> 5] = make_float2(v.s, v.rest);
+        sh_wide[threadIdx.x >> 5] = v.wide;
+    }
     __syncthreads();
-    double s = 0.0;
     if (threadIdx.x == 0)
-        for (int w = 0; w < kGradBlock / 32; ++w) s += sh[w];
-    return s;
+        for (int w = 1; w < kGradBlock / 32; ++w) {
+            v.add(sh[w].x);
+            v.rest += sh[w].y;
+            if (wide) v.wide += sh_wide[w];
+        }
+    return v;
 }
 
 __global__ void __launch_bounds__(kGradBlock) grad_norm_kernel(const __grid_constant__ GradArgs a) {
-    double acc = 0.0;
+    Squares acc;
     for (int c = blockIdx.x; c < a.n_chunks; c += gridDim.x) {
         const GradChunk k = a.chunks[c];
-        acc += k.bf16 ? chunk_squares<true>(k.p, k.n) : chunk_squares<false>(k.p, k.n);
+        if (k.bf16)
+            add_chunk<true>(acc, k.p, k.n);
+        else
+            add_chunk<false>(acc, k.p, k.n);
     }
-    double s = block_sum(acc);
+    acc = block_sum(acc);
     __shared__ bool last;
     if (threadIdx.x == 0) {
-        a.partials[blockIdx.x] = s;
+        a.partials[blockIdx.x] = {acc.s, acc.rest, acc.wide};
         __threadfence();
         last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
     }
     __syncthreads();
     if (!last) return;
     __threadfence();
-    s = 0.0;
-    for (int b = threadIdx.x; b < (int)gridDim.x; b += kGradBlock) s += __ldcg(a.partials + b);
-    __syncthreads();
-    s = block_sum(s);
+    acc = Squares();
+    for (int b = threadIdx.x; b < (int)gridDim.x; b += kGradBlock) {
+        const float4 p = __ldcg(reinterpret_cast<const float4 *>(a.partials + b));
+        acc.add(p.x);
+        acc.rest += p.y;
+        const double w = __hiloint2double(__float_as_int(p.w), __float_as_int(p.z));
+        if (w != 0.0) acc.wide += w;
+    }
+    acc = block_sum(acc);
     if (threadIdx.x == 0) {
-        const double norm = sqrt(s);
-        a.norm[0] = (float)norm;
-        double c = a.max_norm / (norm + 1e-6);
-        if (c > 1.0) c = 1.0;
-        *a.factor = c;
+        const float norm = acc.wide == 0.0 ? sqrtf(acc.s + acc.rest)
+                                           : (float)sqrt((double)acc.s + (double)acc.rest + acc.wide);
+        a.norm[0] = norm;
+        // (a norm beyond fp32 is inf, whose factor is 0)
+        const float c = a.max_norm / (norm + 1e-6f);
+        *a.factor = c > 1.f ? 1.f : c;
         *a.ticket = 0;
     }
 }
 
-// c g of one stretch, rounded once to the destination's type.
+// E elements, scaled and rounded, as 16 or 32 bytes (OBF16: 8 or 16) at o.
+template <bool OBF16, int E>
+__device__ __forceinline__ void put_unit(char *o, const float (&v)[E]) {
+    if constexpr (OBF16) {
+        uint32_t r[E / 2];
+#pragma unroll
+        for (int e = 0; e < E / 2; ++e) r[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+        if constexpr (E == 8)
+            __stcs(reinterpret_cast<uint4 *>(o), make_uint4(r[0], r[1], r[2], r[3]));
+        else
+            __stcs(reinterpret_cast<uint2 *>(o), make_uint2(r[0], r[1]));
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; e += 4)
+            __stcs(reinterpret_cast<float4 *>(o) + e / 4,
+                   make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]));
+    }
+}
+
+// N units of the source, kGradBlock apart, scaled into o.
+template <bool BF16, bool OBF16, int N>
+__device__ __forceinline__ void scale_units(const uint4 *u, char *o, float c) {
+    constexpr int E = BF16 ? 8 : 4, OB = E * (OBF16 ? 2 : 4);
+    uint4 q[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) q[k] = __ldcs(u + k * kGradBlock);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        float v[E];
+        widen<BF16>(q[k], v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] *= c;
+        put_unit<OBF16>(o + k * kGradBlock * OB, v);
+    }
+}
+
+// N 16-byte units of the destination, kGradBlock apart, from elements at src.
+template <bool BF16, bool OBF16, int N>
+__device__ __forceinline__ void gather_units(const char *src, char *o, float c) {
+    constexpr int E = OBF16 ? 8 : 4, IS = BF16 ? 2 : 4;
+    float v[N][E];
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[k][e] = grad1<BF16>(src + k * kGradBlock * E * IS, e);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[k][e] *= c;
+        put_unit<OBF16>(o + k * kGradBlock * 16, v[k]);
+    }
+}
+
+// c g of one stretch, rounded once to the destination's type, in 16-byte units
+// of the source where those lie on a boundary of the destination too.  Else (a
+// tensor's place in the flat vector is the sum of the sizes before it) units
+// are the destination's, and the source's elements come one by one: neighbours
+// share their lines in L1, while stores of single elements would each go to L2.
 template <bool BF16, bool OBF16>
 __device__ __forceinline__ void scale_chunk(const void *p, void *out, int n, float c) {
-    constexpr int E = BF16 ? 8 : 4;
-    const int h = head_of<BF16>(p, n);
-    const int units = (n - h) / E;
-    const uint4 *u = reinterpret_cast<const uint4 *>(static_cast<const char *>(p) +
-                                                     (size_t)h * (BF16 ? 2 : 4));
-    constexpr int OB = E * (OBF16 ? 2 : 4);  // bytes of a unit's elements in out
-    char *o = static_cast<char *>(out) + (size_t)h * (OBF16 ? 2 : 4);
-    const bool whole = ((uintptr_t)o & ((OB < 16 ? OB : 16) - 1)) == 0;
-    for (int i = threadIdx.x; i < units; i += kUnits * kGradBlock) {
-        uint4 q[kUnits];
-#pragma unroll
-        for (int k = 0; k < kUnits; ++k) {
-            const int j = i + k * kGradBlock;
-            if (j < units) q[k] = __ldcs(u + j);
-        }
-#pragma unroll
-        for (int k = 0; k < kUnits; ++k) {
-            const int j = i + k * kGradBlock;
-            if (j >= units) break;
-            float v[E];
-            widen<BF16>(q[k], v);
-#pragma unroll
-            for (int e = 0; e < E; ++e) v[e] *= c;
-            if (!whole) {
-#pragma unroll
-                for (int e = 0; e < E; ++e) put1<OBF16>(o, (int64_t)j * E + e, v[e]);
-            } else if constexpr (OBF16) {
-                uint32_t r[E / 2];
-#pragma unroll
-                for (int e = 0; e < E / 2; ++e) r[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
-                if constexpr (BF16)
-                    __stcs(reinterpret_cast<uint4 *>(o) + j, make_uint4(r[0], r[1], r[2], r[3]));
-                else
-                    __stcs(reinterpret_cast<uint2 *>(o) + j, make_uint2(r[0], r[1]));
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; e += 4)
-                    __stcs(reinterpret_cast<float4 *>(o) + (int64_t)j * (E / 4) + e / 4,
-                           make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]));
-            }
-        }
+    constexpr int IS = BF16 ? 2 : 4, OS = OBF16 ? 2 : 4, OB = 16 / IS * OS;
+    const char *src = static_cast<const char *>(p);
+    char *dst = static_cast<char *>(out);
+    int h = head_of<BF16>(p, n), end;
+    if (((uintptr_t)(dst + h * OS) & ((OB < 16 ? OB : 16) - 1)) == 0) {
+        const int units = (n - h) / (16 / IS);
+        const uint4 *u = reinterpret_cast<const uint4 *>(src + h * IS);
+        char *o = dst + h * OS;
+        int i = threadIdx.x;
+        for (; i + (kUnits - 1) * kGradBlock < units; i += kUnits * kGradBlock)
+            scale_units<BF16, OBF16, kUnits>(u + i, o + (size_t)i * OB, c);
+        for (; i < units; i += kGradBlock)
+            scale_units<BF16, OBF16, 1>(u + i, o + (size_t)i * OB, c);
+        end = h + units * (16 / IS);
+    } else {
+        h = head_of<OBF16>(out, n);
+        const int units = (n - h) / (16 / OS);
+        src += h * IS;
+        char *o = dst + h * OS;
+        int i = threadIdx.x;
+        for (; i + kGradBlock < units; i += 2 * kGradBlock)
+            gather_units<BF16, OBF16, 2>(src + (size_t)i * (16 / OS) * IS, o + (size_t)i * 16, c);
+        for (; i < units; i += kGradBlock)
+            gather_units<BF16, OBF16, 1>(src + (size_t)i * (16 / OS) * IS, o + (size_t)i * 16, c);
+        end = h + units * (16 / OS);
     }
-    const int tail = h + units * E;
-    for (int e = threadIdx.x; e < h + n - tail; e += kGradBlock) {
-        const int at = e < h ? e : tail + e - h;
+    for (int e = threadIdx.x; e < h + n - end; e += kGradBlock) {
+        const int at = e < h ? e : end + e - h;
         put1<OBF16>(out, at, c * grad1<BF16>(p, at));
     }
 }
 
-__global__ void __launch_bounds__(kGradBlock) grad_scale_kernel(const __grid_constant__ GradArgs a) {
-    const double cd = __ldcg(a.factor);
-    if (!a.out && cd == 1.0) return;
-    const float c = (float)cd;
+// OUT: 0 in place, 1 into an fp32 vector, 2 into a bf16 one.
+template <int OUT>
+__global__ void __launch_bounds__(kGradBlock, 4)
+    grad_scale_kernel(const __grid_constant__ GradArgs a) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // for the norm
+    const float c = __ldcg(a.factor);
+    if (OUT == 0 && c == 1.f) return;
     for (int i = blockIdx.x; i < a.n_chunks; i += gridDim.x) {
         const GradChunk k = a.chunks[a.n_chunks - 1 - i];  // the end first: L2 still has it
-        if (!a.out) {
-            if (k.bf16)
-                scale_chunk<true, true>(k.p, k.p, k.n, c);
-            else
-                scale_chunk<false, false>(k.p, k.p, k.n, c);
-            continue;
-        }
-        char *o = static_cast<char *>(a.out) + (size_t)k.at * (a.out_bf16 ? 2 : 4);
-        if (k.bf16) {
-            if (a.out_bf16)
-                scale_chunk<true, true>(k.p, o, k.n, c);
-            else
-                scale_chunk<true, false>(k.p, o, k.n, c);
-        } else {
-            if (a.out_bf16)
-                scale_chunk<false, true>(k.p, o, k.n, c);
-            else
-                scale_chunk<false, false>(k.p, o, k.n, c);
-        }
+        void *o = OUT == 0 ? k.p : static_cast<char *>(a.out) + (size_t)k.at * (OUT == 2 ? 2 : 4);
+        if (k.bf16)
+            scale_chunk<true, OUT != 1>(k.p, o, k.n, c);
+        else
+            scale_chunk<false, OUT == 2>(k.p, o, k.n, c);
     }
 }
 
 }  // namespace
 
 int grad_norm_blocks(int sm_count, int n_chunks) {
-    const int most = sm_count * 8;
+    const int most = sm_count * 4;  // as many as are resident at once
     return n_chunks < 1 ? 1 : n_chunks < most ? n_chunks : most;
 }
 
@@ -240,8 +314,17 @@ cudaError_t launch_grad_norm(const GradArgs &a, int sm_count, cudaStream_t strea
 
 cudaError_t launch_grad_scale(const GradArgs &a, int sm_count, cudaStream_t stream) {
     if (a.n_chunks == 0) return cudaSuccess;
-    grad_scale_kernel<<<grad_norm_blocks(sm_count, a.n_chunks), kGradBlock, 0, stream>>>(a);
-    return cudaGetLastError();
+    cudaLaunchAttribute attr = {};  // its blocks come while the norm's last ones end
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)std::min(a.n_chunks, sm_count * 32));
+    cfg.blockDim = dim3(kGradBlock);
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, !a.out ? grad_scale_kernel<0>
+                                    : a.out_bf16 ? grad_scale_kernel<2> : grad_scale_kernel<1>, a);
 }
 
 }  // namespace aloco

@@ -16,14 +16,21 @@ struct GradChunk {
 
 constexpr int kGradBlock = 256;
 
+// A block's sum of squares: fp32, what its additions rounded away, and what
+// only fp64 holds.
+struct __align__(16) GradPartial {
+    float s, rest;
+    double wide;
+};
+
 struct GradArgs {
     const GradChunk *chunks;
     int n_chunks;
-    double *partials;       // [grid]
+    GradPartial *partials;  // [grid]
     unsigned int *ticket;   // 0 between launches
-    double *factor;         // clipping factor
+    float *factor;          // clipping factor
     float *norm;
-    double max_norm;        // <= 0: no factor
+    float max_norm;         // 0 where only the norm is wanted
     void *out;              // null: in place
     int out_bf16;
 };

@@ -966,26 +966,34 @@ __global__ void __launch_bounds__(32)
 // Log ratios, losses and the rows' coefficients, a pair for each block in turn;
 // the last block to finish adds the losses.  In fp32 with the additions' rests
 // kept: fp64 units are rare here (one fp64 exp took longer than a pair's rows).
-constexpr int kPairBlock = 256;
+constexpr int kPairBlock = 512;
 
-// The sum of `s` over the block in a fixed order, in every thread.
-__device__ __forceinline__ Sum block_total(Sum s, float2 *sh) {
+// The sums of N values over the block in a fixed order, in every thread.
+template <int N>
+__device__ __forceinline__ void block_totals(Sum (&v)[N], float2 (*sh)[kPairBlock / 32]) {
+    const int lane = threadIdx.x & 31;
+    const auto over_warp = [](Sum &s, int from) {
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        const float a = __shfl_xor_sync(0xffffffffu, s.s, off);
-        const float b = __shfl_xor_sync(0xffffffffu, s.rest, off);
-        s.add(a);
-        s.rest += b;
+        for (int off = from; off > 0; off >>= 1) {
+            const float a = __shfl_xor_sync(0xffffffffu, s.s, off);
+            const float b = __shfl_xor_sync(0xffffffffu, s.rest, off);
+            s.add(a);
+            s.rest += b;
+        }
+    };
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        over_warp(v[i], 16);
+        if (lane == 0) sh[i][threadIdx.x >> 5] = make_float2(v[i].s, v[i].rest);
     }
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = make_float2(s.s, s.rest);
-    __syncthreads();
-    s = {0.f, 0.f};
-    for (int i = 0; i < kPairBlock / 32; ++i) {
-        s.add(sh[i].x);
-        s.rest += sh[i].y;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float2 p = sh[i][lane & (kPairBlock / 32 - 1)];
+        v[i] = {p.x, p.y};
+        over_warp(v[i], kPairBlock / 64);
     }
-    return s;
 }
 
 // -(1 - eps) log sigmoid(z) - eps log sigmoid(-z)
@@ -996,7 +1004,7 @@ __device__ __forceinline__ float pair_loss(float z, float eps) {
 
 __global__ void __launch_bounds__(kPairBlock)
     pairs_kernel(const __grid_constant__ LogitsArgs a) {
-    __shared__ float2 sh[kPairBlock / 32];
+    __shared__ float2 sh[2][kPairBlock / 32];
     __shared__ bool last;
     const int tid = threadIdx.x;
     wait_for_previous();
@@ -1006,20 +1014,27 @@ __global__ void __launch_bounds__(kPairBlock)
             cu[i] = load_index(a.cu, 2 * k + i, a.cu_bytes);
             cu[i] = cu[i] < 0 ? 0 : cu[i] > a.n ? a.n : cu[i];
         }
-        float R[2];
-        for (int i = 0; i < 2; ++i) {
-            Sum s = {0.f, 0.f};
-            for (int64_t r = cu[i] + tid; r < cu[i + 1]; r += kPairBlock)
-                if (load_index(a.target, r, a.target_bytes) >= 0) {
-                    s.add(a.logp[r]);
-                    if (a.ref) s.add(-a.ref[r]);
-                }
-            s = block_total(s, sh);
-            R[i] = s.value();
+        Sum s[2] = {};
+#pragma unroll 2
+        for (int64_t r = cu[0] + tid; r < cu[2]; r += kPairBlock) {
+            const bool live = load_index(a.target, r, a.target_bytes) >= 0;
+            const float lp = a.logp[r], ref = a.ref ? a.ref[r] : 0.f;
+            if (live && r < cu[1]) {
+                s[0].add(lp);
+                s[0].add(-ref);
+            } else if (live) {
+                s[1].add(lp);
+                s[1].add(-ref);
+            }
         }
-        if (tid < 2) a.ratios[2 * k + tid] = R[tid];
+        block_totals(s, sh);
+        const float chosen = s[0].value(), rejected = s[1].value();
+        if (tid == 0) {
+            a.ratios[2 * k] = chosen;
+            a.ratios[2 * k + 1] = rejected;
+        }
         if (!a.g.data) continue;
-        const float z = a.beta * (R[0] - R[1]), t = expf(-fabsf(z));
+        const float z = a.beta * (chosen - rejected), t = expf(-fabsf(z));
         // sigmoid(z) - 1 + eps, without the difference where z is large
         const float slope = (z >= 0.f ? a.eps - t / (1.f + t) : t / (1.f + t) - (1.f - a.eps)) *
                             a.per_pair;
@@ -1036,11 +1051,11 @@ __global__ void __launch_bounds__(kPairBlock)
     } else {
         __syncthreads();
     }
-    Sum s = {0.f, 0.f};
+    Sum s[1] = {};
     for (int64_t k = tid; k < a.pairs; k += kPairBlock)
-        s.add(pair_loss(a.beta * (__ldcg(a.ratios + 2 * k) - __ldcg(a.ratios + 2 * k + 1)), a.eps));
-    s = block_total(s, sh);
-    if (tid == 0) a.loss[0] = a.pairs ? s.value() / (float)a.pairs : 0.f;
+        s[0].add(pair_loss(a.beta * (__ldcg(a.ratios + 2 * k) - __ldcg(a.ratios + 2 * k + 1)), a.eps));
+    block_totals(s, sh);
+    if (tid == 0) a.loss[0] = a.pairs ? s[0].value() / (float)a.pairs : 0.f;
 }
 
 // Launch of a row kernel of THREADS consumers with EPT elements each: a
@@ -1114,7 +1129,7 @@ cudaError_t launch_rows(const LogitsArgs &a, int sm_count, cudaStream_t stream, 
     if (a.vocab <= 64 * 72 - 14)
         return launch_rows_as<BF16, 64, 72, 9, 3, 5, MODE>(a, sm_count, stream, used);
     if constexpr (!is_policy(MODE)) {
-        return launch_rows_as<BF16, 224, 72, 3, 5, 4, MODE>(a, sm_count, stream, used);
+        return launch_rows_as<BF16, 224, 72, 3, 4, 4, MODE>(a, sm_count, stream, used);
     } else {
         if (a.vocab <= 128 * 72 - 14)
             return launch_rows_as<BF16, 128, 72, 9, 3, 3, MODE>(a, sm_count, stream, used);

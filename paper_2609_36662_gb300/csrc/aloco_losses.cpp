@@ -1,6 +1,7 @@
 // Entry points of the post-training operators: argument checks and launches of
 // the losses (aloco_logits.cu) and of the gradient-list operators
 // (aloco_grads.cu).
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -49,6 +50,66 @@ int current_device(int *device, int *sm_count) {
     return ALOCO_OK;
 }
 
+// An allocation on the current device that a buffer of this call lies in.
+struct Range {
+    uintptr_t begin = 0, end = 0;
+    bool holds(const void *p, size_t bytes) const {
+        return (uintptr_t)p >= begin && (uintptr_t)p < end && bytes <= end - (uintptr_t)p;
+    }
+};
+
+// Device memory of `device`, and its allocation's extent; false where the
+// driver says otherwise or cannot say.
+bool device_range(const void *p, int device, Range *r) {
+    typedef CUresult (*Fn)(unsigned, CUpointer_attribute *, void **, CUdeviceptr);
+    static const Fn fn = [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuPointerGetAttributes", &f, 12000,
+                                             cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            f = nullptr;
+        }
+        return (Fn)f;
+    }();
+    if (!fn) return false;
+    unsigned type = 0;
+    int ordinal = -1;
+    CUdeviceptr start = 0;
+    size_t size = 0;
+    CUpointer_attribute what[] = {CU_POINTER_ATTRIBUTE_MEMORY_TYPE,
+                                  CU_POINTER_ATTRIBUTE_DEVICE_ORDINAL,
+                                  CU_POINTER_ATTRIBUTE_RANGE_START_ADDR,
+                                  CU_POINTER_ATTRIBUTE_RANGE_SIZE};
+    void *out[] = {&type, &ordinal, &start, &size};
+    if (fn(4, what, out, (CUdeviceptr)p) != CUDA_SUCCESS || type != CU_MEMORYTYPE_DEVICE ||
+        ordinal != device || size == 0)
+        return false;
+    r->begin = (uintptr_t)start;
+    r->end = (uintptr_t)start + size;
+    return true;
+}
+
+// check_buffer for the buffers of one call.  Small ones mostly share an
+// allocation (a framework's pool): one question to the driver serves all that
+// lie in the same; what it does not settle goes to check_buffer.
+struct RangeCheck {
+    static constexpr int kKept = 4;
+    Range seen[kKept];
+    int n = 0;
+    int operator()(const void *p, size_t bytes, int device, const char *name, int index = -1) {
+        for (int i = 0; i < n; ++i)
+            if (seen[i].holds(p, bytes)) return ALOCO_OK;
+        Range r;
+        if (device_range(p, device, &r) && r.holds(p, bytes)) {
+            seen[n < kKept ? n++ : kKept - 1] = r;
+            return ALOCO_OK;
+        }
+        return aloco::check_buffer(p, bytes, device, name, index);
+    }
+};
+
 // ----------------------------------------------------------------- losses
 
 // A buffer of a call: [p, p + bytes), written or read.
@@ -88,8 +149,9 @@ int check_buffers(const Buffers &s, bool grad_over_logits, int *sm_count) {
             return fail(ALOCO_ERR_ALIAS, "%s and %s overlap", x.name, y.name);
         }
     int device, rc = current_device(&device, sm_count);
+    RangeCheck check;
     for (int i = 0; i < s.n && rc == ALOCO_OK; ++i)
-        rc = aloco::check_buffer(s.b[i].p, s.b[i].bytes, device, s.b[i].name);
+        rc = check(s.b[i].p, s.b[i].bytes, device, s.b[i].name);
     return rc;
 }
 
@@ -322,10 +384,11 @@ int grads_create(const void *const *grads, const int64_t *sizes, const int32_t *
     if ((rc = current_device(&device, &sms)) != ALOCO_OK) return rc;
     int64_t total = 0;
     std::vector<std::pair<uintptr_t, uintptr_t>> ranges;
+    RangeCheck check;
     for (int64_t i = 0; i < n; ++i) {
         const size_t size = dtypes[i] == ALOCO_F32 ? 4 : 2;
         if (sizes[i] == 0) continue;
-        if ((rc = aloco::check_buffer(grads[i], (size_t)sizes[i] * size, device, "grads",
+        if ((rc = check(grads[i], (size_t)sizes[i] * size, device, "grads",
                                       (int)std::min<int64_t>(i, INT32_MAX))) != ALOCO_OK)
             return rc;
         ranges.push_back({(uintptr_t)grads[i], (uintptr_t)grads[i] + (size_t)sizes[i] * size});
@@ -354,7 +417,7 @@ int grads_create(const void *const *grads, const int64_t *sizes, const int32_t *
 
     const size_t table = (chunks.size() * sizeof(aloco::GradChunk) + 255) / 256 * 256;
     const int blocks = aloco::grad_norm_blocks(sms, (int)chunks.size());
-    const size_t bytes = table + (size_t)blocks * sizeof(double) + 256;
+    const size_t bytes = table + (size_t)blocks * sizeof(aloco::GradPartial) + 256;
     char *dev = nullptr;
     cudaError_t e = cudaMalloc((void **)&dev, bytes);
     if (e != cudaSuccess) {
@@ -384,8 +447,8 @@ int grads_create(const void *const *grads, const int64_t *sizes, const int32_t *
     std::memset(&h->args, 0, sizeof h->args);
     h->args.chunks = reinterpret_cast<const aloco::GradChunk *>(dev);
     h->args.n_chunks = h->n_chunks;
-    h->args.partials = reinterpret_cast<double *>(dev + table);
-    h->args.factor = h->args.partials + blocks;
+    h->args.partials = reinterpret_cast<aloco::GradPartial *>(dev + table);
+    h->args.factor = reinterpret_cast<float *>(h->args.partials + blocks);
     h->args.ticket = reinterpret_cast<unsigned int *>(h->args.factor + 1);
     *out = h;
     return done();
@@ -465,8 +528,8 @@ int aloco_clip_grads(aloco_grads_t *g, double max_norm, void *out, aloco_dtype o
                      float *norm, const aloco_opts_t *opts) {
     int rc = check_list(g, norm);
     if (rc != ALOCO_OK) return rc;
-    if (!(std::isfinite(max_norm) && max_norm > 0.0))
-        return fail(ALOCO_ERR_ARG, "max_norm = %g must be finite and > 0", max_norm);
+    if (!(std::isfinite((float)max_norm) && (float)max_norm > 0.f))
+        return fail(ALOCO_ERR_ARG, "max_norm = %g must be finite and > 0 in fp32", max_norm);
     if (hits(g, norm, 4)) return fail(ALOCO_ERR_ALIAS, "norm overlaps a gradient");
     if (!out && g->overlap)
         return fail(ALOCO_ERR_ALIAS, "gradients overlap one another: they cannot be clipped "
@@ -484,7 +547,7 @@ int aloco_clip_grads(aloco_grads_t *g, double max_norm, void *out, aloco_dtype o
     }
     aloco::GradArgs a = g->args;
     a.norm = norm;
-    a.max_norm = max_norm;
+    a.max_norm = (float)max_norm;
     a.out = out;
     a.out_bf16 = out_dtype == ALOCO_BF16;
     cudaError_t e = aloco::launch_grad_norm(a, g->sm_count, stream_of(opts));
