@@ -306,12 +306,11 @@ __device__ __forceinline__ float2 join_parts(const float2 *parts, int n, int lan
 
 // -------------------------------------------------------------- row kernel
 
-// The part of a row's units that CTA `rank` of 2^log_c holds.
+// The part of a row's units that CTA `rank` of a cluster holds, `per` at most.
 struct Part {
     int first, count;
 };
-__device__ __forceinline__ Part part_of(int units, int rank, int log_c) {
-    const int per = (units + (1 << log_c) - 1) >> log_c;
+__device__ __forceinline__ Part part_of(int units, int rank, int per) {
     const int first = min(rank * per, units);
     return {first, min(per, units - first)};
 }
@@ -561,9 +560,9 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
     __shared__ volatile int s_abort;
 
     const cg::cluster_group cluster = cg::this_cluster();
-    const int log_c = a.log_c, C = 1 << log_c, rank = (int)blockIdx.x & (C - 1);
-    const int64_t step = gridDim.x >> log_c;
-    const int64_t row0 = blockIdx.x >> log_c;
+    const int C = a.cluster, rank = (int)(blockIdx.x % (unsigned)C);
+    const int64_t step = gridDim.x / (unsigned)C;
+    const int64_t row0 = blockIdx.x / (unsigned)C;
     const int tid = threadIdx.x, lane = tid & 31;
     const int stages = a.stages;
     const volatile int *const aborted = &s_abort;
@@ -594,7 +593,8 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
         // whole come one by one, with -inf beside them.
         Place place, batch;
         unsigned filled = 0;
-        bool ok = true, mixed = false, again = false;
+        bool ok = true, again = false;
+        unsigned mixed = 0;  // slots that hold stores of this warp's
         unsigned char *const zeros = ring + (size_t)stages * SLOT * 16;
         if (writes_grad(MODE) && a.g.data) {
             for (int i = lane; i < ZEROS / 16; i += 32)
@@ -674,15 +674,14 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
                         reinterpret_cast<char *>(__shfl_sync(
                             0xffffffffu, reinterpret_cast<uint64_t>(mine.g), from)),
                         __shfl_sync(0xffffffffu, mine.g_head, from), a.vocab);
-                    zero_part<BF16>(g, part_of(g.units, rank, log_c), lane, zeros, ZEROS);
+                    zero_part<BF16>(g, part_of(g.units, rank, a.per), lane, zeros, ZEROS);
                 } else if (todo) {
                     todo &= todo - 1;
                     const Window x = ahead_x;
                     const float edge = ahead_edge;
                     if (todo) look_ahead(__ffs(todo) - 1);
-                    const Part p = part_of(x.units, rank, log_c);
+                    const Part p = part_of(x.units, rank, a.per);
                     const Ends<BF16> ends(x, lane);
-                    mixed = mixed || ends.cut_first || ends.cut_last;
                     for (int s = 0; s < p.count; s += SLOT) {
                         const uint32_t full = smem_addr(&s_full[place.i]);
                         unsigned char *at = ring + (size_t)place.i * SLOT * 16;
@@ -692,13 +691,19 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
                                                       place.phase ^ 1, aborted));
                         if (!ok) break;
                         // earlier stores to this slot come before its next copy
-                        if (mixed) fence_proxy_async_smem();
+                        if (mixed >> place.i & 1) {
+                            fence_proxy_async_smem();
+                            mixed &= ~(1u << place.i);
+                        }
                         int lo = p.first + s, hi = p.first + min(s + SLOT, p.count);
                         const int u0 = lo;
                         if (ends.mine && ends.unit >= lo && ends.unit < hi)
                             store1<BF16>((char *)at, ends.element - u0 * E, edge);
-                        if (ends.cut_first && lo == 0) ++lo;
-                        if (ends.cut_last && hi == x.units) --hi;
+                        const bool cut_lo = ends.cut_first && lo == 0;
+                        const bool cut_hi = ends.cut_last && hi == x.units;
+                        if (cut_lo || cut_hi) mixed |= 1u << place.i;
+                        lo += cut_lo;
+                        hi -= cut_hi;
                         __syncwarp();
                         if (lane == 0) {
                             const uint32_t bytes = hi > lo ? (uint32_t)(hi - lo) * 16 : 0;
@@ -781,7 +786,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
                 continue;
             }
             const Window x = window_at<BF16>(nullptr, r.head, a.vocab);
-            const Part p = part_of(x.units, rank, log_c);
+            const Part p = part_of(x.units, rank, a.per);
             if constexpr (is_grad(MODE)) {
                 // the preference loss's gradient, slot by slot
                 const f2 neg = pair(-r.f.z, -r.f.z);
@@ -1071,17 +1076,10 @@ cudaError_t launch_rows_as(const LogitsArgs &in, int sm_count, cudaStream_t stre
     static PerDevice ready, most[kMaxCluster + 1];
     const auto kernel = row_kernel<BF16, THREADS, UPT, DEPTH, CTAS, MODE>;
     const int units = (in.vocab + 2 * (E - 1)) / E;
-    int log_c = 0;
-    // (the forward kernels take a part of any length, slot by slot)
-    const auto fits = [&](int c) {
-        return !is_policy(MODE) || (units + (1 << c) - 1) >> c <= THREADS * UPT;
-    };
-    while (!fits(log_c))
-        if ((1 << ++log_c) > kMaxCluster) return cudaErrorInvalidValue;
-    while (2 << log_c <= kMaxCluster && in.n * (2 << log_c) <= sm_count &&
-           units >= (2 << log_c) * THREADS)
-        ++log_c;
-    const int C = 1 << log_c;
+    // (the kernels that do not hold a row take a part of any length)
+    int C = is_policy(MODE) ? (units + THREADS * UPT - 1) / (THREADS * UPT) : 1;
+    if (C > kMaxCluster) return cudaErrorInvalidValue;
+    while (C < kMaxCluster && in.n * (C + 1) <= sm_count && units >= (C + 1) * THREADS) ++C;
 
     const int dev = PerDevice::device();
     if (!ready.get(dev)) {
@@ -1114,7 +1112,8 @@ cudaError_t launch_rows_as(const LogitsArgs &in, int sm_count, cudaStream_t stre
     cfg.numAttrs = 2;
     LogitsArgs a = in;
     a.stages = STAGES;
-    a.log_c = log_c;
+    a.cluster = C;
+    a.per = (units + C - 1) / C;
     *used = (int)(in.n < clusters ? in.n : clusters);
     cfg.gridDim = dim3((unsigned)(*used * C));
     return cudaLaunchKernelEx(&cfg, kernel, a);
@@ -1124,6 +1123,9 @@ template <bool BF16, int MODE>
 cudaError_t launch_rows(const LogitsArgs &a, int sm_count, cudaStream_t stream, int *used) {
     *used = 0;
     if (a.n == 0) return cudaSuccess;
+    // units of a thread in a slot of the ring: a whole part in bf16, a sixth of
+    // it in fp32, whose parts are twice as long
+    constexpr int kDeep = BF16 ? 9 : 3;
     if (a.vocab <= 32 * 72 - 14)
         return launch_rows_as<BF16, 32, 72, 9, 3, 8, MODE>(a, sm_count, stream, used);
     if (a.vocab <= 64 * 72 - 14)
@@ -1133,10 +1135,18 @@ cudaError_t launch_rows(const LogitsArgs &a, int sm_count, cudaStream_t stream, 
     } else {
         if (a.vocab <= 128 * 72 - 14)
             return launch_rows_as<BF16, 128, 72, 9, 3, 3, MODE>(a, sm_count, stream, used);
-        if (a.vocab <= 224 * 72 - 14 ||
-            (a.vocab > 480 * 72 - 14 && a.vocab <= kMaxCluster * 224 * 72 - 14))
-            return launch_rows_as<BF16, 224, 72, 9, 3, 2, MODE>(a, sm_count, stream, used);
-        return launch_rows_as<BF16, 480, 72, 9, 3, 1, MODE>(a, sm_count, stream, used);
+        // Two CTAs an SM or one of twice the size: the one of 480 where it
+        // holds the row alone (8 x 1023 x 32000 bf16: 162 us, as a cluster of
+        // two of 224 198), else the one whose cluster the row fills better
+        // (128256 bf16, 8 x 1000: 632 us at 0.99 of eight, 662 at 0.93 of four;
+        // 100000, 8 x 1023: 642 us at 0.89 of seven, 577 at 0.96 of three).
+        const int units = (a.vocab + 2 * (16 / (BF16 ? 2 : 4) - 1)) / (16 / (BF16 ? 2 : 4));
+        constexpr int kOne = 480 * (BF16 ? 9 : 18), kTwo = 224 * (BF16 ? 9 : 18);
+        const int one = (units + kOne - 1) / kOne, two = (units + kTwo - 1) / kTwo;
+        if (two == 1 || (one > 1 && two <= kMaxCluster && two * kTwo < one * kOne))
+            return launch_rows_as<BF16, 224, 72, kDeep, 27 / kDeep, 2, MODE>(a, sm_count, stream,
+                                                                             used);
+        return launch_rows_as<BF16, 480, 72, kDeep, 27 / kDeep, 1, MODE>(a, sm_count, stream, used);
     }
 }
 

@@ -39,7 +39,8 @@ struct LogitsArgs {
     float *coef;                     // [n] dL/dlogp (scratch)
     unsigned int *ticket;            // blocks of the pairs' kernel that are done (scratch)
     float *loss, *ratios;
-    int stages, log_c;               // the row kernel's ring slots and cluster
+    int stages, cluster, per;        // the row kernel: ring slots, CTAs of a
+                                     // cluster, units of a CTA's part at most
 };
 
 cudaError_t launch_token_logprobs(const LogitsArgs &a, aloco_dtype dtype, int sm_count,
