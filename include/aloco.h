@@ -527,6 +527,8 @@ int aloco_adamw_step_normed(void *const *params, const void *const *grads,
  * part (a negative token, or a weight of 0 in the policy loss) is never read:
  * its logp is 0 and its gradient row is zeros.
  *
+ * Every wait inside the kernels is bounded (about 2 s); one that runs out leaves
+ * NaN in the loss and in the log-probabilities of the rows that it concerns.
  * Every buffer is device memory of the current device.  The calls only
  * enqueue on opts->stream (the other options do not apply) and allocate
  * nothing; sums are taken in a fixed order, so that results are bit-identical
@@ -885,7 +887,11 @@ int aloco_sync_noalloc(float *global, float *momentum, void *const *locals,
  * mbarrier then never completes, so the bounded waits on it (about 2 s) run
  * out: the block aborts, lets its copies in flight land, and the round
  * returns ALOCO_ERR_CUDA with every kernel finished and the device usable.
- * The hook is consumed by that round; no other call reads it. */
+ * aloco_token_logprobs, aloco_policy_loss and aloco_preference_loss read it
+ * too: block 0 of their row kernel leaves out the copy of its slot `tile`, and
+ * what waits for it leaves NaN in the log-probabilities of that row and of the
+ * block's later ones, and so in the loss.  The hook is consumed by that round
+ * or call; no other reads it. */
 void aloco_test_stall_tile(int64_t tile);
 
 /* Message of the last failure on the calling thread ("" if none).  The

@@ -761,8 +761,9 @@ def adamw_step(params, grads, exp_avg, exp_avg_sq, cfg: AdamwCfg,
 
 
 def test_stall_tile(tile: int):
-    """Testing only: the next bulk-copy round on this thread skips the copies
-    of one tile, so that its bounded wait runs out (aloco_test_stall_tile)."""
+    """Testing only: the next bulk-copy round (or post-training loss) on this
+    thread skips the copies of one tile, so that its bounded wait runs out
+    (aloco_test_stall_tile)."""
     load().aloco_test_stall_tile(int(tile))
 
 
@@ -793,10 +794,9 @@ class _OtherStream:
     or returns is not handed out again before both are past it."""
 
     def __init__(self, stream, current, inputs):
-        import torch
         self.current = current
         self.stream = stream
-        self.inner = torch.cuda.stream(stream)
+        self.inner = _torch.cuda.stream(stream)
         self.inputs = inputs
 
     def __enter__(self):
@@ -1046,8 +1046,9 @@ def _grad_list(grads) -> GradList:
 
 
 def grad_norm(grads, *, stream=None):
-    """Global norm of a GradList (or of a sequence of tensors, which costs a new
-    list each time): a float32 scalar tensor.  Enqueues only."""
+    """Global norm of a GradList: a float32 scalar tensor.  Enqueues only.  (A
+    sequence of tensors does too, at the price of a list made for the call,
+    which also waits for the GPU.)"""
     g = _grad_list(grads)
     ctx, handle = _on_stream(stream, g.device, g.tensors)
     with ctx:
@@ -1061,7 +1062,8 @@ def clip_grads(grads, max_norm: float, *, out=None, stream=None):
     """Scale the gradients by min(1, max_norm / (norm + 1e-6)): in place, or,
     with `out` (a contiguous float32 or bfloat16 vector of all their elements),
     into it, tensor after tensor, as adamw_step takes them.  Returns the norm
-    before clipping, a float32 scalar tensor.  Enqueues only."""
+    before clipping, a float32 scalar tensor.  Enqueues only (grads as
+    grad_norm takes them)."""
     g = _grad_list(grads)
     if out is not None and (out.numel() != g.numel or not out.is_contiguous() or
                             out.device != g.device):

@@ -557,7 +557,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
     __shared__ RowInfo s_rows[2][kBatch];
     __shared__ float2 s_warp[2][WARPS];
     __shared__ __align__(8) float2 s_cta[2][kMaxCluster];
-    __shared__ volatile int s_abort;
+    __shared__ volatile int s_abort, s_bad[2];
 
     const cg::cluster_group cluster = cg::this_cluster();
     const int C = a.cluster, rank = (int)(blockIdx.x % (unsigned)C);
@@ -576,7 +576,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
             mbar_init(smem_addr(&s_rows_full[i]), 1);
             mbar_init(smem_addr(&s_rows_empty[i]), WARPS);
         }
-        s_abort = 0;
+        s_abort = s_bad[0] = s_bad[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (C > 1)
@@ -708,7 +708,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
                         if (lane == 0) {
                             const uint32_t bytes = hi > lo ? (uint32_t)(hi - lo) * 16 : 0;
                             mbar_arrive_expect_tx(full, bytes);
-                            if (bytes)
+                            if (bytes && (blockIdx.x || filled + 1 != a.test_stall1))
                                 bulk_load(smem_addr(at + (size_t)(lo - u0) * 16),
                                           x.base + (size_t)lo * 16, bytes, full);
                         }
@@ -741,12 +741,23 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
         bool ok = true;
         int next = 0;       // the row's place in its batch
         Sum terms[kTerms] = {};
+        // All consumers leave together where a wait of one of them ran out: NaN
+        // in this row and the block's later ones, and no barrier armed again.
+        const auto leave = [&](int64_t row) {
+            s_abort = 1;
+            for (; row < a.n; row += step)
+                if (rank == 0 && tid == 0) give_up<MODE>(a, row);
+            terms[0].s = terms[1].s = NAN;
+        };
         // This thread's units of the next slot, which holds `count` (none: 0),
         // -inf where it has none.
         const auto take_slot = [&](uint4 *q, int count, bool shifted) {
             const Units w = units_of<THREADS>(count, tid, may_shift(MODE) && shifted);
             const int left = w.end - w.first;
-            if (count > 0) ok = mbar_wait(smem_addr(&s_full[place.i]), place.phase, aborted) && ok;
+            bool here = true;
+            if (count > 0)
+                here = __all_sync(0xffffffffu, mbar_wait(smem_addr(&s_full[place.i]), place.phase,
+                                                         aborted));
             const uint4 *slot = reinterpret_cast<const uint4 *>(ring) + (size_t)place.i * SLOT + w.first;
 #pragma unroll
             for (int j = 0; j < DEPTH; ++j) {
@@ -756,7 +767,16 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
             }
             if (count > 0) {
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_addr(&s_empty[place.i]));
+                // A slot whose wait ran out is never given back: the producer
+                // may not arm its barrier again before the copy has landed.
+                // Nor is a later one, whose wait may succeed on an older phase
+                // (a row that is held takes no place of the ring twice, and the
+                // block leaves at its barrier).
+                if constexpr (!is_policy(MODE)) here = ok = ok && here;
+                if (!here)
+                    s_abort = s_bad[rows & 1] = 1;
+                else if (lane == 0)
+                    mbar_arrive(smem_addr(&s_empty[place.i]));
                 place.next(stages);
             }
         };
@@ -770,10 +790,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
             if (next == 0 && !all_of<THREADS>(mbar_wait(smem_addr(&s_rows_full[batch.i]),
                                                         batch.phase, aborted))) {
                 // without the rows' scalars nothing can be said of them
-                s_abort = 1;
-                for (; row < a.n; row += step)
-                    if (rank == 0 && tid == 0) give_up<MODE>(a, row);
-                terms[0].s = terms[1].s = NAN;
+                leave(row);
                 break;
             }
             const RowInfo r = s_rows[batch.i][next++];
@@ -796,10 +813,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
                     const int count = clamp_count(p.count - u, SLOT), u0 = p.first + u;
                     uint4 q[DEPTH];
                     take_slot(q, count, shifted);
-                    if (!ok) {
-                        s_abort = 1;
-                        if (first) give_up<MODE>(a, row);
-                    }
+                    if (!ok && first) give_up<MODE>(a, row);
                     const float f = ok ? r.f.y : NAN;
                     f2 v[DEPTH][P];
 #pragma unroll
@@ -858,6 +872,10 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
             const float sw = warp_sum(raised(st) * factor_of(mt, base_of(mw), scale));
             if (lane == 0) s_warp[turn][tid >> 5] = make_float2(mw, sw);
             asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+            if (s_bad[turn]) {  // written before this barrier only: the same for all
+                leave(row);
+                break;
+            }
             float2 part;
             if (C == 1 || tid < 32) part = join_parts(s_warp[turn], WARPS, lane, scale);
             if (C > 1) {
@@ -876,14 +894,14 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
                         "[%0], {%1, %2}, [%3];" ::"r"(to), "f"(part.x), "f"(part.y), "r"(there)
                         : "memory");
                 }
-                ok = mbar_wait(bar, phase, aborted) && ok;
+                // (where that runs out, this row is NaN and the next one's
+                // barrier is where the block leaves)
+                const bool here = __all_sync(0xffffffffu, mbar_wait(bar, phase, aborted));
                 part = join_parts(s_cta[turn], C, lane, scale);
-            }
-            // A wait that ran out leaves NaN in this row and the block's later
-            // ones, whose waits see s_abort and return at once.
-            if (!ok) {
-                s_abort = 1;
-                part.y = NAN;
+                if (!here) {
+                    s_abort = s_bad[turn ^ 1] = 1;
+                    part.y = NAN;
+                }
             }
             const float m = part.x, z = part.y;
             // a row without a finite logit leaves z = 0: -inf - -inf
@@ -995,8 +1013,8 @@ __device__ __forceinline__ void block_totals(Sum (&v)[N], float2 (*sh)[kPairBloc
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const float2 p = sh[i][lane & (kPairBlock / 32 - 1)];
-        v[i] = {p.x, p.y};
+        v[i].s = sh[i][lane & (kPairBlock / 32 - 1)].x;
+        v[i].rest = sh[i][lane & (kPairBlock / 32 - 1)].y;
         over_warp(v[i], kPairBlock / 64);
     }
 }
@@ -1123,9 +1141,11 @@ template <bool BF16, int MODE>
 cudaError_t launch_rows(const LogitsArgs &a, int sm_count, cudaStream_t stream, int *used) {
     *used = 0;
     if (a.n == 0) return cudaSuccess;
-    // units of a thread in a slot of the ring: a whole part in bf16, a sixth of
-    // it in fp32, whose parts are twice as long
-    constexpr int kDeep = BF16 ? 9 : 3;
+    // units of a thread in a slot of the ring: a whole part in bf16; in fp32,
+    // whose parts are twice as long, a sixth of it (1380 live rows of 32000: 67
+    // against 73 us with half a part), but half of it where rows lie askew (3 x
+    // 511 x 50257 shifted: 137 against 166 us)
+    constexpr int kDeep = BF16 || MODE == kPolicyShifted ? 9 : 3;
     if (a.vocab <= 32 * 72 - 14)
         return launch_rows_as<BF16, 32, 72, 9, 3, 8, MODE>(a, sm_count, stream, used);
     if (a.vocab <= 64 * 72 - 14)
@@ -1135,15 +1155,16 @@ cudaError_t launch_rows(const LogitsArgs &a, int sm_count, cudaStream_t stream, 
     } else {
         if (a.vocab <= 128 * 72 - 14)
             return launch_rows_as<BF16, 128, 72, 9, 3, 3, MODE>(a, sm_count, stream, used);
-        // Two CTAs an SM or one of twice the size: the one of 480 where it
-        // holds the row alone (8 x 1023 x 32000 bf16: 162 us, as a cluster of
-        // two of 224 198), else the one whose cluster the row fills better
-        // (128256 bf16, 8 x 1000: 632 us at 0.99 of eight, 662 at 0.93 of four;
-        // 100000, 8 x 1023: 642 us at 0.89 of seven, 577 at 0.96 of three).
+        // Two CTAs an SM or one of twice the size: the large one where it holds
+        // the row alone or in two (8 x 1023 x 32000 bf16: 162 us, 198 as a
+        // cluster of two small ones; x 50304: 328 as two, 335 as four), else
+        // the one whose cluster the row fills better (8 x 1000 x 128256: 640
+        // us at 0.99 of eight small ones, 674 at 0.93 of four; 8 x 1023 x
+        // 100000: 642 us at 0.89 of seven, 574 at 0.96 of three).
         const int units = (a.vocab + 2 * (16 / (BF16 ? 2 : 4) - 1)) / (16 / (BF16 ? 2 : 4));
         constexpr int kOne = 480 * (BF16 ? 9 : 18), kTwo = 224 * (BF16 ? 9 : 18);
         const int one = (units + kOne - 1) / kOne, two = (units + kTwo - 1) / kTwo;
-        if (two == 1 || (one > 1 && two <= kMaxCluster && two * kTwo < one * kOne))
+        if (two == 1 || (one > 2 && two <= kMaxCluster && two * kTwo < one * kOne))
             return launch_rows_as<BF16, 224, 72, kDeep, 27 / kDeep, 2, MODE>(a, sm_count, stream,
                                                                              used);
         return launch_rows_as<BF16, 480, 72, kDeep, 27 / kDeep, 1, MODE>(a, sm_count, stream, used);
@@ -1210,8 +1231,10 @@ cudaError_t launch_preference_loss(const LogitsArgs &a, aloco_dtype dtype, int s
         cudaError_t e = launch_rows<B, kPref>(a, sm_count, stream, &used);
         if (e == cudaSuccess) e = launch_behind(pairs_kernel, blocks, kPairBlock, stream, a);
         if (e != cudaSuccess || !a.g.data) return e;
-        return alike ? launch_rows<B, kGrad>(a, sm_count, stream, &used)
-                     : launch_rows<B, kGradShifted>(a, sm_count, stream, &used);
+        LogitsArgs b = a;
+        b.test_stall1 = 0;
+        return alike ? launch_rows<B, kGrad>(b, sm_count, stream, &used)
+                     : launch_rows<B, kGradShifted>(b, sm_count, stream, &used);
     };
     return dtype == ALOCO_BF16 ? all(std::true_type{}) : all(std::false_type{});
 }

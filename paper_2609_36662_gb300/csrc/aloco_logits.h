@@ -41,6 +41,8 @@ struct LogitsArgs {
     float *loss, *ratios;
     int stages, cluster, per;        // the row kernel: ring slots, CTAs of a
                                      // cluster, units of a CTA's part at most
+    int64_t test_stall1;             // testing only: 1 + the number of the slot
+                                     // whose copy block 0 leaves out (0: none)
 };
 
 cudaError_t launch_token_logprobs(const LogitsArgs &a, aloco_dtype dtype, int sm_count,

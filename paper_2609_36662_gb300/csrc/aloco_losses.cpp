@@ -17,6 +17,9 @@
 #include "aloco_grads.h"
 #include "aloco_logits.h"
 
+// The testing hook of aloco_test_stall_tile (aloco_host.cpp).
+extern thread_local int64_t t_test_stall_tile1;
+
 namespace {
 
 int fail(int code, const char *fmt, ...) {
@@ -241,6 +244,11 @@ int take_scratch(void *scratch, size_t bytes, aloco::LogitsArgs *a, Buffers *s) 
     return ALOCO_OK;
 }
 
+void take_stall(aloco::LogitsArgs *a) {
+    a->test_stall1 = t_test_stall_tile1;
+    t_test_stall_tile1 = 0;
+}
+
 cudaStream_t stream_of(const aloco_opts_t *o) {
     return o ? (cudaStream_t)o->stream : (cudaStream_t) nullptr;
 }
@@ -261,6 +269,7 @@ int aloco_token_logprobs(const aloco_tokens_t *tokens, float *logp, const aloco_
     a.logp = logp;
     int sms;
     if ((rc = check_buffers(s, false, &sms)) != ALOCO_OK) return rc;
+    take_stall(&a);
     const cudaError_t e =
         aloco::launch_token_logprobs(a, (aloco_dtype)tokens->dtype, sms, stream_of(opts));
     return e == cudaSuccess ? done() : cuda_fail(e, "token log-probabilities");
@@ -306,6 +315,7 @@ int aloco_policy_loss(const aloco_tokens_t *tokens, const float *advantages,
     a.terms = static_cast<double *>(scratch);
     int sms;
     if ((rc = check_buffers(s, over, &sms)) != ALOCO_OK) return rc;
+    take_stall(&a);
     const cudaError_t e =
         aloco::launch_policy_loss(a, (aloco_dtype)tokens->dtype, sms, stream_of(opts));
     return e == cudaSuccess ? done() : cuda_fail(e, "policy loss");
@@ -355,6 +365,7 @@ int aloco_preference_loss(const aloco_tokens_t *tokens, const float *ref_logp,
     a.ticket = reinterpret_cast<unsigned int *>(a.coef + a.n);
     int sms;
     if ((rc = check_buffers(s, over, &sms)) != ALOCO_OK) return rc;
+    take_stall(&a);
     const cudaError_t e =
         aloco::launch_preference_loss(a, (aloco_dtype)tokens->dtype, sms, stream_of(opts));
     return e == cudaSuccess ? done() : cuda_fail(e, "preference loss");
