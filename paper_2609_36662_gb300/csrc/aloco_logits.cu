@@ -541,6 +541,82 @@ __device__ __forceinline__ void give_up(const LogitsArgs &a, int64_t row) {
     }
 }
 
+// A cluster's sums of the policy loss, and behind them the call's mark.  In a
+// small call block 0 waits for all marks and adds the sums: a second kernel for
+// that takes 3 us of the host's time, which such calls are made of (48 rows of
+// 32000: 29 -> 24 us).  (No block waits for block 0, so that all end whatever is
+// resident.)  A large call has the second kernel, which the next call overlaps,
+// where block 0 would be the last to end (8 x 1023 x 32000 bf16: 162 us, 167 in
+// one kernel).
+__device__ __forceinline__ void hand_in(PolicyPart *p, unsigned long long mark, float gain,
+                                        float kl, float cut) {
+    p->term[0] = gain;
+    p->term[1] = kl;
+    p->term[2] = cut;
+    asm volatile("st.release.gpu.global.u64 [%0], %1;" ::"l"(&p->mark), "l"(mark) : "memory");
+}
+
+// About a minute: every block hands in, also one that has given up, but blocks
+// may wait for SMs that another stream's kernels hold.
+constexpr long long kMarkWaitCycles = 30 * kTmaWaitCycles;
+
+// Sums of up to 32 lanes, in every lane.
+__device__ __forceinline__ void sum_over_warp(Sum &s) {
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+        const float x = __shfl_xor_sync(0xffffffffu, s.s, off);
+        const float y = __shfl_xor_sync(0xffffffffu, s.rest, off);
+        s.add(x);
+        s.rest += y;
+    }
+}
+
+// By the consumers of a block (barrier 1), in a fixed order.  The marks are
+// taken away, so that a captured call finds none of its own when it runs again.
+template <int THREADS>
+__device__ __forceinline__ void add_parts(const LogitsArgs &a, int clusters, int tid,
+                                          float2 (*sh)[THREADS / 32]) {
+    constexpr int WARPS = THREADS / 32;
+    Sum s[kTerms] = {};
+    const long long t0 = clock64();
+    for (int c = tid; c < clusters; c += THREADS) {
+        PolicyPart *p = a.parts + c;
+        unsigned long long mark;
+        bool here = true;
+        do {
+            asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(mark) : "l"(&p->mark) : "memory");
+            here = mark == a.mark;
+        } while (!here && clock64() - t0 < kMarkWaitCycles);
+        const float t[kTerms] = {__ldcg(&p->term[0]), __ldcg(&p->term[1]), __ldcg(&p->term[2])};
+        p->mark = 0;
+        for (int j = 0; j < kTerms; ++j) s[j].add(here ? t[j] : NAN);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < kTerms; ++j) {
+        sum_over_warp(s[j]);
+        if ((tid & 31) == 0) sh[j][tid >> 5] = make_float2(s[j].s, s[j].rest);
+    }
+    asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+    if (tid >= 32) return;
+#pragma unroll
+    for (int j = 0; j < kTerms; ++j) {
+        s[j] = {0.f, 0.f};
+        if (tid < WARPS) {
+            s[j].s = sh[j][tid].x;
+            s[j].rest = sh[j][tid].y;
+        }
+        sum_over_warp(s[j]);
+    }
+    if (tid == 0) {
+        const float gain = s[0].value(), kl = s[1].value();
+        a.terms_out[0] = fmaf(a.kl, kl, gain);
+        a.terms_out[1] = gain;
+        a.terms_out[2] = kl;
+        a.terms_out[3] = s[2].value();
+    }
+}
+
 // THREADS consumers and one producer warp.  CTA c of a cluster holds its part
 // of a row in the registers of its consumers: thread t the units k * THREADS +
 // t of the part, k < UPT.  A slot of the ring is DEPTH units of every thread.
@@ -556,6 +632,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
     __shared__ __align__(8) uint64_t s_rows_full[2], s_rows_empty[2];
     __shared__ RowInfo s_rows[2][kBatch];
     __shared__ float2 s_warp[2][WARPS];
+    __shared__ float2 s_sums[is_policy(MODE) ? kTerms : 1][WARPS];
     __shared__ __align__(8) float2 s_cta[2][kMaxCluster];
     __shared__ volatile int s_abort, s_bad[2];
 
@@ -958,8 +1035,11 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
                 }
             }
         }
-        if (is_policy(MODE) && rank == 0 && tid == 0)
-            for (int j = 0; j < kTerms; ++j) a.terms[row0 * kTerms + j] = (double)terms[j].value();
+        if constexpr (is_policy(MODE)) {
+            if (rank == 0 && tid == 0)
+                hand_in(a.parts + row0, a.mark, terms[0].value(), terms[1].value(), terms[2].value());
+            if (a.finish && blockIdx.x == 0) add_parts<THREADS>(a, (int)step, tid, s_sums);
+        }
     }
     // no CTA leaves while another may still write to its memory
     if (C > 1)
@@ -968,22 +1048,12 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
         __syncthreads();
 }
 
-// The policy loss's sums over the clusters of its row kernel.  One warp: fp64
-// additions are rare units here, and the kernel waits for little else.
-__global__ void __launch_bounds__(32)
-    policy_terms_kernel(const __grid_constant__ LogitsArgs a, int clusters) {
+constexpr int kSumBlock = 256;
+__global__ void __launch_bounds__(kSumBlock)
+    policy_sums_kernel(const __grid_constant__ LogitsArgs a, int clusters) {
+    __shared__ float2 sh[kTerms][kSumBlock / 32];
     wait_for_previous();
-    double s[kTerms] = {};
-    for (int c = threadIdx.x; c < clusters; c += 32)
-        for (int j = 0; j < kTerms; ++j) s[j] += a.terms[c * kTerms + j];
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1)
-#pragma unroll
-        for (int j = 0; j < kTerms; ++j) s[j] += __shfl_xor_sync(0xffffffffu, s[j], off);
-    if (threadIdx.x == 0) {
-        a.terms_out[0] = (float)(s[0] + (double)a.kl * s[1]);
-        for (int j = 0; j < kTerms; ++j) a.terms_out[1 + j] = (float)s[j];
-    }
+    add_parts<kSumBlock>(a, clusters, threadIdx.x, sh);
 }
 
 // Log ratios, losses and the rows' coefficients, a pair for each block in turn;
@@ -995,27 +1065,21 @@ constexpr int kPairBlock = 512;
 template <int N>
 __device__ __forceinline__ void block_totals(Sum (&v)[N], float2 (*sh)[kPairBlock / 32]) {
     const int lane = threadIdx.x & 31;
-    const auto over_warp = [](Sum &s, int from) {
-#pragma unroll
-        for (int off = from; off > 0; off >>= 1) {
-            const float a = __shfl_xor_sync(0xffffffffu, s.s, off);
-            const float b = __shfl_xor_sync(0xffffffffu, s.rest, off);
-            s.add(a);
-            s.rest += b;
-        }
-    };
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        over_warp(v[i], 16);
+        sum_over_warp(v[i]);
         if (lane == 0) sh[i][threadIdx.x >> 5] = make_float2(v[i].s, v[i].rest);
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        v[i].s = sh[i][lane & (kPairBlock / 32 - 1)].x;
-        v[i].rest = sh[i][lane & (kPairBlock / 32 - 1)].y;
-        over_warp(v[i], kPairBlock / 64);
+        v[i] = {0.f, 0.f};
+        if (lane < kPairBlock / 32) {
+            v[i].s = sh[i][lane].x;
+            v[i].rest = sh[i][lane].y;
+        }
+        sum_over_warp(v[i]);
     }
 }
 
@@ -1207,8 +1271,9 @@ cudaError_t launch_token_logprobs(const LogitsArgs &a, aloco_dtype dtype, int sm
                                : launch_rows<false, kFwd>(a, sm_count, stream, &used);
 }
 
-cudaError_t launch_policy_loss(const LogitsArgs &a, aloco_dtype dtype, int sm_count,
+cudaError_t launch_policy_loss(const LogitsArgs &in, aloco_dtype dtype, int sm_count,
                                cudaStream_t stream) {
+    LogitsArgs a = in;
     int used;
     const bool alike = rows_alike(a, dtype);
     const auto rows = [&](auto bf16) {
@@ -1216,9 +1281,12 @@ cudaError_t launch_policy_loss(const LogitsArgs &a, aloco_dtype dtype, int sm_co
         return alike ? launch_rows<B, kPolicy>(a, sm_count, stream, &used)
                      : launch_rows<B, kPolicyShifted>(a, sm_count, stream, &used);
     };
+    if (a.n == 0) return cudaMemsetAsync(a.terms_out, 0, (kTerms + 1) * sizeof(float), stream);
+    // about where the GPU's time passes the host's
+    a.finish = a.n * a.vocab * (dtype == ALOCO_BF16 ? 2 : 4) < ((int64_t)80 << 20);
     const cudaError_t e = dtype == ALOCO_BF16 ? rows(std::true_type{}) : rows(std::false_type{});
-    if (e != cudaSuccess) return e;
-    return launch_behind(policy_terms_kernel, 1, 32, stream, a, used);
+    if (e != cudaSuccess || a.finish) return e;
+    return launch_behind(policy_sums_kernel, 1, kSumBlock, stream, a, used);
 }
 
 cudaError_t launch_preference_loss(const LogitsArgs &a, aloco_dtype dtype, int sm_count,

@@ -16,6 +16,13 @@ struct Rows {
 // Sums of the policy loss besides L itself.
 constexpr int kTerms = 3;
 
+// One cluster's share of them (scratch), and a mark that says it is there.
+struct PolicyPart {
+    float term[kTerms];
+    float unused;
+    unsigned long long mark;
+};
+
 struct LogitsArgs {
     Rows x, g;                       // logits; gradient (g.data null: none)
     int64_t n;                       // rows
@@ -28,8 +35,9 @@ struct LogitsArgs {
     // policy loss
     const float *adv, *old, *ref, *w;
     float lo, hi, kl;                // 1 - clip_low, 1 + clip_high, kl_coef
-    double *terms;                   // [clusters][kTerms], one of each at most
-                                     // n clusters of the row kernel (scratch)
+    PolicyPart *parts;               // [at most n clusters of the row kernel]
+    unsigned long long mark;         // this call's, never 0
+    int finish;                      // 1: block 0 of the row kernel adds them
     float *terms_out;                // [kTerms + 1]
     // preference loss (ref as above)
     const void *cu;

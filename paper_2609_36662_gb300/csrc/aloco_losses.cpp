@@ -5,6 +5,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -312,7 +313,10 @@ int aloco_policy_loss(const aloco_tokens_t *tokens, const float *advantages,
     a.kl = (float)cfg->kl_coef;
     a.logp = logp;
     a.terms_out = terms;
-    a.terms = static_cast<double *>(scratch);
+    a.parts = static_cast<aloco::PolicyPart *>(scratch);
+    static std::atomic<unsigned long long> calls{0};
+    // odd times odd, so never 0, and a value that memory hardly holds by chance
+    a.mark = (2 * calls.fetch_add(1, std::memory_order_relaxed) + 1) * 0x9e3779b97f4a7c15ull;
     int sms;
     if ((rc = check_buffers(s, over, &sms)) != ALOCO_OK) return rc;
     take_stall(&a);
