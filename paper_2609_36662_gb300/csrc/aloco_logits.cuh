@@ -21,9 +21,9 @@
 // A row may start off a 16-byte boundary (odd vocabularies): the units are
 // those of the aligned window around it; whole ones are copied, and the two at
 // its ends are read and written element by element.
-#include <limits.h>
+#pragma once
 
-#include <type_traits>
+#include <limits.h>
 
 #include <cooperative_groups.h>
 
@@ -46,8 +46,12 @@ __device__ __forceinline__ void wait_for_previous() {
 // What a row kernel leaves: log-probabilities, also a gradient, the same where
 // the gradient's rows may lie otherwise to the 16-byte boundaries than the
 // logits' do, what the preference loss needs of a row, or its gradient.
-constexpr int kFwd = 0, kPolicy = 1, kPolicyShifted = 2, kPref = 3, kGrad = 4, kGradShifted = 5;
-constexpr bool is_policy(int mode) { return mode == kPolicy || mode == kPolicyShifted; }
+// (kPolicySmall: see hand_in.)
+constexpr int kFwd = 0, kPolicy = 1, kPolicyShifted = 2, kPref = 3, kGrad = 4, kGradShifted = 5,
+              kPolicySmall = 6;
+constexpr bool is_policy(int mode) {
+    return mode == kPolicy || mode == kPolicyShifted || mode == kPolicySmall;
+}
 constexpr bool is_grad(int mode) { return mode == kGrad || mode == kGradShifted; }
 constexpr bool writes_grad(int mode) { return is_policy(mode) || is_grad(mode); }
 constexpr bool may_shift(int mode) { return mode == kPolicyShifted || mode == kGradShifted; }
@@ -571,10 +575,12 @@ __device__ __forceinline__ void sum_over_warp(Sum &s) {
     }
 }
 
-// By the consumers of a block (barrier 1), in a fixed order.  The marks are
+// By the consumers of a block (barrier 1), in a fixed order; WAIT: while others
+// may still be at their rows.  The marks are
 // taken away, so that a captured call finds none of its own when it runs again.
-template <int THREADS>
-__device__ __forceinline__ void add_parts(const LogitsArgs &a, int clusters, int tid,
+// (Not inlined: the row kernel's registers are the rows'.)
+template <int THREADS, bool WAIT>
+__device__ __noinline__ void add_parts(const LogitsArgs &a, int clusters, int tid,
                                           float2 (*sh)[THREADS / 32]) {
     constexpr int WARPS = THREADS / 32;
     Sum s[kTerms] = {};
@@ -582,13 +588,14 @@ __device__ __forceinline__ void add_parts(const LogitsArgs &a, int clusters, int
     for (int c = tid; c < clusters; c += THREADS) {
         PolicyPart *p = a.parts + c;
         unsigned long long mark;
-        bool here = true;
-        do {
+        bool here = !WAIT;
+        while (!here) {
             asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(mark) : "l"(&p->mark) : "memory");
             here = mark == a.mark;
-        } while (!here && clock64() - t0 < kMarkWaitCycles);
+            if (!here && clock64() - t0 > kMarkWaitCycles) break;
+        }
         const float t[kTerms] = {__ldcg(&p->term[0]), __ldcg(&p->term[1]), __ldcg(&p->term[2])};
-        p->mark = 0;
+        if (WAIT) p->mark = 0;
         for (int j = 0; j < kTerms; ++j) s[j].add(here ? t[j] : NAN);
     }
     __syncwarp();
@@ -617,6 +624,112 @@ __device__ __forceinline__ void add_parts(const LogitsArgs &a, int clusters, int
     }
 }
 
+// ---------------------------------------------------- pairs of log ratios
+
+// In fp32 with the additions' rests kept: fp64 units are rare here (one fp64 exp
+// took longer than a pair's rows).  THREADS threads, which barrier 1 counts.
+constexpr int kPairBlock = 512;
+
+template <int THREADS>
+__device__ __forceinline__ void sync_threads() {
+    asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+}
+
+// The sums of N values over the threads in a fixed order, in every thread.
+template <int THREADS, int N>
+__device__ __forceinline__ void block_totals(Sum (&v)[N], int tid, float2 (*sh)[THREADS / 32]) {
+    const int lane = tid & 31;
+    sync_threads<THREADS>();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        sum_over_warp(v[i]);
+        if (lane == 0) sh[i][tid >> 5] = make_float2(v[i].s, v[i].rest);
+    }
+    sync_threads<THREADS>();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        v[i] = {0.f, 0.f};
+        if (lane < THREADS / 32) {
+            v[i].s = sh[i][lane].x;
+            v[i].rest = sh[i][lane].y;
+        }
+        sum_over_warp(v[i]);
+    }
+}
+
+// -(1 - eps) log sigmoid(z) - eps log sigmoid(-z)
+__device__ __forceinline__ float pair_loss(float z, float eps) {
+    // -log sigmoid(z) = log(1 + exp(-|z|)) + max(-z, 0)
+    return log1pf(expf(-fabsf(z))) + (z < 0.f ? (1.f - eps) * -z : eps * z);
+}
+
+// Log ratios of pair k and the coefficients of its rows.
+template <int THREADS>
+__device__ __forceinline__ void one_pair(const LogitsArgs &a, int64_t k, int tid,
+                                         float2 (*sh)[THREADS / 32]) {
+    int64_t cu[3];
+    for (int i = 0; i < 3; ++i) {
+        cu[i] = load_index(a.cu, 2 * k + i, a.cu_bytes);
+        cu[i] = cu[i] < 0 ? 0 : cu[i] > a.n ? a.n : cu[i];
+    }
+    Sum s[2] = {};
+#pragma unroll 2
+    for (int64_t r = cu[0] + tid; r < cu[2]; r += THREADS) {
+        const bool live = load_index(a.target, r, a.target_bytes) >= 0;
+        const float lp = __ldcg(a.logp + r), ref = a.ref ? a.ref[r] : 0.f;
+        if (live && r < cu[1]) {
+            s[0].add(lp);
+            s[0].add(-ref);
+        } else if (live) {
+            s[1].add(lp);
+            s[1].add(-ref);
+        }
+    }
+    block_totals<THREADS>(s, tid, sh);
+    const float chosen = s[0].value(), rejected = s[1].value();
+    if (tid == 0) {
+        a.ratios[2 * k] = chosen;
+        a.ratios[2 * k + 1] = rejected;
+    }
+    if (!a.g.data) return;
+    const float z = a.beta * (chosen - rejected), t = expf(-fabsf(z));
+    // sigmoid(z) - 1 + eps, without the difference where z is large
+    const float slope =
+        (z >= 0.f ? a.eps - t / (1.f + t) : t / (1.f + t) - (1.f - a.eps)) * a.per_pair;
+    for (int64_t r = cu[0] + tid; r < cu[2]; r += THREADS)
+        if (load_index(a.target, r, a.target_bytes) >= 0) a.coef[r] = r < cu[1] ? slope : -slope;
+}
+
+// The loss, from the ratios that are in memory.
+template <int THREADS>
+__device__ __forceinline__ void mean_of_pairs(const LogitsArgs &a, int tid,
+                                              float2 (*sh)[THREADS / 32]) {
+    sync_threads<THREADS>();
+    Sum s[1] = {};
+    for (int64_t k = tid; k < a.pairs; k += THREADS)
+        s[0].add(pair_loss(a.beta * (__ldcg(a.ratios + 2 * k) - __ldcg(a.ratios + 2 * k + 1)), a.eps));
+    block_totals<THREADS>(s, tid, sh);
+    if (tid == 0) a.loss[0] = a.pairs ? s[0].value() / (float)a.pairs : 0.f;
+}
+
+// All pairs, by the consumers of one block, when every block has handed in.
+template <int THREADS>
+__device__ __noinline__ void all_pairs(const LogitsArgs &a, int blocks, int tid,
+                                       float2 (*sh)[THREADS / 32]) {
+    const long long t0 = clock64();
+    for (int c = tid; c < blocks; c += THREADS) {
+        unsigned long long mark;
+        do {
+            asm volatile("ld.acquire.gpu.global.u64 %0, [%1];"
+                         : "=l"(mark) : "l"(&a.parts[c].mark) : "memory");
+        } while (mark != a.mark && clock64() - t0 < kMarkWaitCycles);
+        a.parts[c].mark = 0;
+    }
+    sync_threads<THREADS>();
+    for (int64_t k = 0; k < a.pairs; ++k) one_pair<THREADS>(a, k, tid, sh);
+    mean_of_pairs<THREADS>(a, tid, sh);
+}
+
 // THREADS consumers and one producer warp.  CTA c of a cluster holds its part
 // of a row in the registers of its consumers: thread t the units k * THREADS +
 // t of the part, k < UPT.  A slot of the ring is DEPTH units of every thread.
@@ -632,7 +745,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
     __shared__ __align__(8) uint64_t s_rows_full[2], s_rows_empty[2];
     __shared__ RowInfo s_rows[2][kBatch];
     __shared__ float2 s_warp[2][WARPS];
-    __shared__ float2 s_sums[is_policy(MODE) ? kTerms : 1][WARPS];
+    __shared__ float2 s_sums[is_policy(MODE) ? kTerms : MODE == kPref ? 2 : 1][WARPS];
     __shared__ __align__(8) float2 s_cta[2][kMaxCluster];
     __shared__ volatile int s_abort, s_bad[2];
 
@@ -661,7 +774,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
     else
         __syncthreads();
     wait_for_previous();
-    if (MODE == kPref && blockIdx.x == 0 && tid == 0) *a.ticket = 0;
+    if (MODE == kPref && !a.finish && blockIdx.x == 0 && tid == 0) *a.ticket = 0;
 
     if (tid >= THREADS) {
         // Producer: the rows' scalars, kBatch rows at a time, and their parts,
@@ -1038,7 +1151,13 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
         if constexpr (is_policy(MODE)) {
             if (rank == 0 && tid == 0)
                 hand_in(a.parts + row0, a.mark, terms[0].value(), terms[1].value(), terms[2].value());
-            if (a.finish && blockIdx.x == 0) add_parts<THREADS>(a, (int)step, tid, s_sums);
+            if (MODE != kPolicy && a.finish && blockIdx.x == 0)
+                add_parts<THREADS, true>(a, (int)step, tid, s_sums);
+        }
+        if (MODE == kPref && a.finish) {
+            // (the first CTA of a cluster writes what its rows leave)
+            if (rank == 0 && tid == 0) hand_in(a.parts + row0, a.mark, 0.f, 0.f, 0.f);
+            if (blockIdx.x == 0) all_pairs<THREADS>(a, (int)step, tid, s_sums);
         }
     }
     // no CTA leaves while another may still write to its memory
@@ -1053,40 +1172,7 @@ __global__ void __launch_bounds__(kSumBlock)
     policy_sums_kernel(const __grid_constant__ LogitsArgs a, int clusters) {
     __shared__ float2 sh[kTerms][kSumBlock / 32];
     wait_for_previous();
-    add_parts<kSumBlock>(a, clusters, threadIdx.x, sh);
-}
-
-// Log ratios, losses and the rows' coefficients, a pair for each block in turn;
-// the last block to finish adds the losses.  In fp32 with the additions' rests
-// kept: fp64 units are rare here (one fp64 exp took longer than a pair's rows).
-constexpr int kPairBlock = 512;
-
-// The sums of N values over the block in a fixed order, in every thread.
-template <int N>
-__device__ __forceinline__ void block_totals(Sum (&v)[N], float2 (*sh)[kPairBlock / 32]) {
-    const int lane = threadIdx.x & 31;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        sum_over_warp(v[i]);
-        if (lane == 0) sh[i][threadIdx.x >> 5] = make_float2(v[i].s, v[i].rest);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        v[i] = {0.f, 0.f};
-        if (lane < kPairBlock / 32) {
-            v[i].s = sh[i][lane].x;
-            v[i].rest = sh[i][lane].y;
-        }
-        sum_over_warp(v[i]);
-    }
-}
-
-// -(1 - eps) log sigmoid(z) - eps log sigmoid(-z)
-__device__ __forceinline__ float pair_loss(float z, float eps) {
-    // -log sigmoid(z) = log(1 + exp(-|z|)) + max(-z, 0)
-    return log1pf(expf(-fabsf(z))) + (z < 0.f ? (1.f - eps) * -z : eps * z);
+    add_parts<kSumBlock, false>(a, clusters, threadIdx.x, sh);
 }
 
 __global__ void __launch_bounds__(kPairBlock)
@@ -1095,39 +1181,7 @@ __global__ void __launch_bounds__(kPairBlock)
     __shared__ bool last;
     const int tid = threadIdx.x;
     wait_for_previous();
-    for (int64_t k = blockIdx.x; k < a.pairs; k += gridDim.x) {
-        int64_t cu[3];
-        for (int i = 0; i < 3; ++i) {
-            cu[i] = load_index(a.cu, 2 * k + i, a.cu_bytes);
-            cu[i] = cu[i] < 0 ? 0 : cu[i] > a.n ? a.n : cu[i];
-        }
-        Sum s[2] = {};
-#pragma unroll 2
-        for (int64_t r = cu[0] + tid; r < cu[2]; r += kPairBlock) {
-            const bool live = load_index(a.target, r, a.target_bytes) >= 0;
-            const float lp = a.logp[r], ref = a.ref ? a.ref[r] : 0.f;
-            if (live && r < cu[1]) {
-                s[0].add(lp);
-                s[0].add(-ref);
-            } else if (live) {
-                s[1].add(lp);
-                s[1].add(-ref);
-            }
-        }
-        block_totals(s, sh);
-        const float chosen = s[0].value(), rejected = s[1].value();
-        if (tid == 0) {
-            a.ratios[2 * k] = chosen;
-            a.ratios[2 * k + 1] = rejected;
-        }
-        if (!a.g.data) continue;
-        const float z = a.beta * (chosen - rejected), t = expf(-fabsf(z));
-        // sigmoid(z) - 1 + eps, without the difference where z is large
-        const float slope = (z >= 0.f ? a.eps - t / (1.f + t) : t / (1.f + t) - (1.f - a.eps)) *
-                            a.per_pair;
-        for (int64_t r = cu[0] + tid; r < cu[2]; r += kPairBlock)
-            if (load_index(a.target, r, a.target_bytes) >= 0) a.coef[r] = r < cu[1] ? slope : -slope;
-    }
+    for (int64_t k = blockIdx.x; k < a.pairs; k += gridDim.x) one_pair<kPairBlock>(a, k, tid, sh);
     if (gridDim.x > 1) {
         __threadfence();
         __syncthreads();
@@ -1135,14 +1189,8 @@ __global__ void __launch_bounds__(kPairBlock)
         __syncthreads();
         if (!last) return;
         __threadfence();
-    } else {
-        __syncthreads();
     }
-    Sum s[1] = {};
-    for (int64_t k = tid; k < a.pairs; k += kPairBlock)
-        s[0].add(pair_loss(a.beta * (__ldcg(a.ratios + 2 * k) - __ldcg(a.ratios + 2 * k + 1)), a.eps));
-    block_totals(s, sh);
-    if (tid == 0) a.loss[0] = a.pairs ? s[0].value() / (float)a.pairs : 0.f;
+    mean_of_pairs<kPairBlock>(a, tid, sh);
 }
 
 // Launch of a row kernel of THREADS consumers with EPT elements each: a
@@ -1253,58 +1301,50 @@ cudaError_t launch_behind(void (*kernel)(Params...), unsigned grid, unsigned blo
 }
 
 // Whether all rows of the gradient lie to the 16-byte boundaries as the logits'.
-bool rows_alike(const LogitsArgs &a, aloco_dtype dtype) {
+template <bool BF16>
+bool rows_alike(const LogitsArgs &a) {
     if (!a.g.data) return true;
-    const int64_t size = dtype == ALOCO_BF16 ? 2 : 4, per = a.x.per_batch;
+    const int64_t size = Unit<BF16>::kSize, per = a.x.per_batch;
     int64_t off = (int64_t)((uintptr_t)a.x.data - (uintptr_t)a.g.data);
     if (per > 1) off |= (a.x.row_stride - a.g.row_stride) * size;
     if (a.n > per) off |= (a.x.batch_stride - a.g.batch_stride) * size;
     return (off & 15) == 0;
 }
 
-}  // namespace
-
-cudaError_t launch_token_logprobs(const LogitsArgs &a, aloco_dtype dtype, int sm_count,
-                                  cudaStream_t stream) {
-    int used;
-    return dtype == ALOCO_BF16 ? launch_rows<true, kFwd>(a, sm_count, stream, &used)
-                               : launch_rows<false, kFwd>(a, sm_count, stream, &used);
-}
-
-cudaError_t launch_policy_loss(const LogitsArgs &in, aloco_dtype dtype, int sm_count,
-                               cudaStream_t stream) {
+template <bool BF16>
+cudaError_t launch_policy_rows(const LogitsArgs &in, int sm_count, cudaStream_t stream) {
     LogitsArgs a = in;
     int used;
-    const bool alike = rows_alike(a, dtype);
-    const auto rows = [&](auto bf16) {
-        constexpr bool B = decltype(bf16)::value;
-        return alike ? launch_rows<B, kPolicy>(a, sm_count, stream, &used)
-                     : launch_rows<B, kPolicyShifted>(a, sm_count, stream, &used);
-    };
     if (a.n == 0) return cudaMemsetAsync(a.terms_out, 0, (kTerms + 1) * sizeof(float), stream);
     // about where the GPU's time passes the host's
-    a.finish = a.n * a.vocab * (dtype == ALOCO_BF16 ? 2 : 4) < ((int64_t)80 << 20);
-    const cudaError_t e = dtype == ALOCO_BF16 ? rows(std::true_type{}) : rows(std::false_type{});
+    a.finish = a.n * a.vocab * Unit<BF16>::kSize < ((int64_t)80 << 20);
+    const cudaError_t e =
+        !rows_alike<BF16>(a) ? launch_rows<BF16, kPolicyShifted>(a, sm_count, stream, &used)
+        : a.finish           ? launch_rows<BF16, kPolicySmall>(a, sm_count, stream, &used)
+                             : launch_rows<BF16, kPolicy>(a, sm_count, stream, &used);
     if (e != cudaSuccess || a.finish) return e;
     return launch_behind(policy_sums_kernel, 1, kSumBlock, stream, a, used);
 }
 
-cudaError_t launch_preference_loss(const LogitsArgs &a, aloco_dtype dtype, int sm_count,
-                                   cudaStream_t stream) {
-    const bool alike = rows_alike(a, dtype);
-    const unsigned blocks = a.n == 0 || a.pairs < 2 ? 1u : (unsigned)(a.pairs < 1024 ? a.pairs : 1024);
-    const auto all = [&](auto bf16) {
-        constexpr bool B = decltype(bf16)::value;
-        int used;
-        cudaError_t e = launch_rows<B, kPref>(a, sm_count, stream, &used);
-        if (e == cudaSuccess) e = launch_behind(pairs_kernel, blocks, kPairBlock, stream, a);
-        if (e != cudaSuccess || !a.g.data) return e;
-        LogitsArgs b = a;
-        b.test_stall1 = 0;
-        return alike ? launch_rows<B, kGrad>(b, sm_count, stream, &used)
-                     : launch_rows<B, kGradShifted>(b, sm_count, stream, &used);
-    };
-    return dtype == ALOCO_BF16 ? all(std::true_type{}) : all(std::false_type{});
+template <bool BF16>
+cudaError_t launch_preference_rows(const LogitsArgs &in, int sm_count, cudaStream_t stream) {
+    LogitsArgs a = in;
+    int used;
+    // few rows: block 0 of the row kernel is done with the pairs sooner than
+    // another kernel is launched
+    a.finish = a.n > 0 && a.n <= 2048 && a.pairs <= 16;
+    cudaError_t e = launch_rows<BF16, kPref>(a, sm_count, stream, &used);
+    if (e == cudaSuccess && !a.finish) {
+        const unsigned blocks =
+            a.n == 0 || a.pairs < 2 ? 1u : (unsigned)(a.pairs < 1024 ? a.pairs : 1024);
+        e = launch_behind(pairs_kernel, blocks, kPairBlock, stream, a);
+    }
+    if (e != cudaSuccess || !a.g.data) return e;
+    a.test_stall1 = 0;
+    return rows_alike<BF16>(a) ? launch_rows<BF16, kGrad>(a, sm_count, stream, &used)
+                               : launch_rows<BF16, kGradShifted>(a, sm_count, stream, &used);
 }
+
+}  // namespace
 
 }  // namespace aloco

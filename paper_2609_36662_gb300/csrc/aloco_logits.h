@@ -1,5 +1,5 @@
 // Internal interface of the post-training losses: what aloco_losses.cpp checks
-// and fills in, and what the kernels of aloco_logits.cu take by value.
+// and fills in, and what the kernels of aloco_logits.cuh take by value.
 #pragma once
 
 #include "aloco_internal.h"
@@ -38,6 +38,7 @@ struct LogitsArgs {
     PolicyPart *parts;               // [at most n clusters of the row kernel]
     unsigned long long mark;         // this call's, never 0
     int finish;                      // 1: block 0 of the row kernel adds them
+                                     // (preference loss: works out the pairs)
     float *terms_out;                // [kTerms + 1]
     // preference loss (ref as above)
     const void *cu;
@@ -53,11 +54,11 @@ struct LogitsArgs {
                                      // whose copy block 0 leaves out (0: none)
 };
 
-cudaError_t launch_token_logprobs(const LogitsArgs &a, aloco_dtype dtype, int sm_count,
-                                  cudaStream_t stream);
-cudaError_t launch_policy_loss(const LogitsArgs &a, aloco_dtype dtype, int sm_count,
-                               cudaStream_t stream);
-cudaError_t launch_preference_loss(const LogitsArgs &a, aloco_dtype dtype, int sm_count,
-                                   cudaStream_t stream);
+cudaError_t token_logprobs_f32(const LogitsArgs &a, int sm_count, cudaStream_t stream);
+cudaError_t token_logprobs_bf16(const LogitsArgs &a, int sm_count, cudaStream_t stream);
+cudaError_t policy_loss_f32(const LogitsArgs &a, int sm_count, cudaStream_t stream);
+cudaError_t policy_loss_bf16(const LogitsArgs &a, int sm_count, cudaStream_t stream);
+cudaError_t preference_loss_f32(const LogitsArgs &a, int sm_count, cudaStream_t stream);
+cudaError_t preference_loss_bf16(const LogitsArgs &a, int sm_count, cudaStream_t stream);
 
 }  // namespace aloco

@@ -1,5 +1,5 @@
 // Entry points of the post-training operators: argument checks and launches of
-// the losses (aloco_logits.cu) and of the gradient-list operators
+// the losses (aloco_logits.cuh) and of the gradient-list operators
 // (aloco_grads.cu).
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -245,6 +245,13 @@ int take_scratch(void *scratch, size_t bytes, aloco::LogitsArgs *a, Buffers *s) 
     return ALOCO_OK;
 }
 
+// Another value for every call: odd times odd, so never 0, and one that memory
+// hardly holds by chance.
+unsigned long long new_mark() {
+    static std::atomic<unsigned long long> calls{0};
+    return (2 * calls.fetch_add(1, std::memory_order_relaxed) + 1) * 0x9e3779b97f4a7c15ull;
+}
+
 void take_stall(aloco::LogitsArgs *a) {
     a->test_stall1 = t_test_stall_tile1;
     t_test_stall_tile1 = 0;
@@ -258,7 +265,11 @@ cudaStream_t stream_of(const aloco_opts_t *o) {
 
 extern "C" {
 
-size_t aloco_loss_scratch_bytes(int64_t rows) { return rows > 0 ? (size_t)rows * 24 + 16 : 0; }
+size_t aloco_loss_scratch_bytes(int64_t rows) {
+    if (rows <= 0) return 0;
+    // a cluster's part, a row's maximum and sum, its coefficient; a ticket
+    return (size_t)rows * (sizeof(aloco::PolicyPart) + sizeof(float2) + sizeof(float)) + 16;
+}
 
 int aloco_token_logprobs(const aloco_tokens_t *tokens, float *logp, const aloco_opts_t *opts) {
     aloco::LogitsArgs a;
@@ -272,7 +283,7 @@ int aloco_token_logprobs(const aloco_tokens_t *tokens, float *logp, const aloco_
     if ((rc = check_buffers(s, false, &sms)) != ALOCO_OK) return rc;
     take_stall(&a);
     const cudaError_t e =
-        aloco::launch_token_logprobs(a, (aloco_dtype)tokens->dtype, sms, stream_of(opts));
+        (tokens->dtype == ALOCO_BF16 ? aloco::token_logprobs_bf16 : aloco::token_logprobs_f32)(a, sms, stream_of(opts));
     return e == cudaSuccess ? done() : cuda_fail(e, "token log-probabilities");
 }
 
@@ -314,14 +325,12 @@ int aloco_policy_loss(const aloco_tokens_t *tokens, const float *advantages,
     a.logp = logp;
     a.terms_out = terms;
     a.parts = static_cast<aloco::PolicyPart *>(scratch);
-    static std::atomic<unsigned long long> calls{0};
-    // odd times odd, so never 0, and a value that memory hardly holds by chance
-    a.mark = (2 * calls.fetch_add(1, std::memory_order_relaxed) + 1) * 0x9e3779b97f4a7c15ull;
+    a.mark = new_mark();
     int sms;
     if ((rc = check_buffers(s, over, &sms)) != ALOCO_OK) return rc;
     take_stall(&a);
     const cudaError_t e =
-        aloco::launch_policy_loss(a, (aloco_dtype)tokens->dtype, sms, stream_of(opts));
+        (tokens->dtype == ALOCO_BF16 ? aloco::policy_loss_bf16 : aloco::policy_loss_f32)(a, sms, stream_of(opts));
     return e == cudaSuccess ? done() : cuda_fail(e, "policy loss");
 }
 
@@ -364,14 +373,16 @@ int aloco_preference_loss(const aloco_tokens_t *tokens, const float *ref_logp,
     a.loss = loss;
     a.ratios = log_ratios;
     a.logp = logp;
-    a.stats = static_cast<float2 *>(scratch);
+    a.parts = static_cast<aloco::PolicyPart *>(scratch);
+    a.stats = reinterpret_cast<float2 *>(a.parts + a.n);
     a.coef = reinterpret_cast<float *>(a.stats + a.n);
     a.ticket = reinterpret_cast<unsigned int *>(a.coef + a.n);
+    a.mark = new_mark();
     int sms;
     if ((rc = check_buffers(s, over, &sms)) != ALOCO_OK) return rc;
     take_stall(&a);
     const cudaError_t e =
-        aloco::launch_preference_loss(a, (aloco_dtype)tokens->dtype, sms, stream_of(opts));
+        (tokens->dtype == ALOCO_BF16 ? aloco::preference_loss_bf16 : aloco::preference_loss_f32)(a, sms, stream_of(opts));
     return e == cudaSuccess ? done() : cuda_fail(e, "preference loss");
 }
 
