@@ -5,12 +5,16 @@
 //
 // The tensors are cut into stretches of equal length, listed in device
 // memory; blocks take stretches in turn, so that a set of many small and few
-// large tensors spreads evenly.  Both kernels stream: the norm reads every
-// gradient once, the scaling reads it again and writes it.
+// large tensors spreads evenly.  Both kernels stream, bound by HBM from some 1e7
+// elements on: the norm reads every gradient once (137.8e6 fp32 in 82.7 us, 0.98
+// of the copy rate), the scaling reads it again, what L2 has kept of it from
+// there, and writes it (1.1e9 bf16 into a bf16 vector in 961 us with the norm;
+// two reads and a write take 973 at the copy rate).
 #include <algorithm>
 
 #include "aloco_grads.h"
 #include "aloco_sync_kernel.cuh"
+#include "aloco_units.cuh"
 
 namespace aloco {
 
@@ -244,11 +248,34 @@ __device__ __forceinline__ void gather_units(const char *src, char *o, float c) 
     }
 }
 
+// N 16-byte units of the destination, kGradBlock apart, each from two
+// neighbouring ones of a source of the same type.
+template <bool BF16, int N>
+__device__ __forceinline__ void join_and_scale(const uint4 *u, char *o, int bytes, float c) {
+    constexpr int E = BF16 ? 8 : 4;
+    uint4 q[N], r[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        q[k] = __ldg(u + k * kGradBlock);
+        r[k] = __ldg(u + k * kGradBlock + 1);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        float v[E];
+        widen<BF16>(join_units(q[k], r[k], bytes), v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] *= c;
+        put_unit<BF16>(o + k * kGradBlock * 16, v);
+    }
+}
+
 // c g of one stretch, rounded once to the destination's type, in 16-byte units
 // of the source where those lie on a boundary of the destination too.  Else (a
 // tensor's place in the flat vector is the sum of the sizes before it) units
-// are the destination's, and the source's elements come one by one: neighbours
-// share their lines in L1, while stores of single elements would each go to L2.
+// are the destination's: made of two neighbouring ones where both have one type
+// (5e8 bf16 at odd places: 481 against 554 us element by element), and of the
+// source's elements one by one where not; neighbours share their lines in L1,
+// while stores of single elements would each go to L2.
 template <bool BF16, bool OBF16>
 __device__ __forceinline__ void scale_chunk(const void *p, void *out, int n, float c) {
     constexpr int IS = BF16 ? 2 : 4, OS = OBF16 ? 2 : 4, OB = 16 / IS * OS;
@@ -265,6 +292,23 @@ __device__ __forceinline__ void scale_chunk(const void *p, void *out, int n, flo
         for (; i < units; i += kGradBlock)
             scale_units<BF16, OBF16, 1>(u + i, o + (size_t)i * OB, c);
         end = h + units * (16 / IS);
+    } else if constexpr (BF16 == OBF16) {
+        constexpr int E = 16 / IS;
+        const int us = (n - h) / E;           // whole units of the source, from element h
+        const int hd = head_of<OBF16>(out, n);
+        // unit j of the destination, from element hd, begins in unit j - lower of
+        // the source, (hd - h) mod E elements on
+        const int lower = hd < h, on = hd - h + lower * E;
+        const int units = max(0, min((n - hd) / E - lower, us - 1));
+        const uint4 *u = reinterpret_cast<const uint4 *>(src + h * IS);
+        h = hd + lower * E;
+        char *o = dst + h * OS;
+        int i = threadIdx.x;
+        for (; i + kGradBlock < units; i += 2 * kGradBlock)
+            join_and_scale<BF16, 2>(u + i, o + (size_t)i * 16, 16 - on * IS, c);
+        for (; i < units; i += kGradBlock)
+            join_and_scale<BF16, 1>(u + i, o + (size_t)i * 16, 16 - on * IS, c);
+        end = h + units * E;
     } else {
         h = head_of<OBF16>(out, n);
         const int units = (n - h) / (16 / OS);

@@ -15,8 +15,15 @@
 // is each kept value times one factor per thread: the logits are read once and
 // the gradient is written once.
 // The preference loss needs every row of a pair before any of its gradients:
-// its first kernel leaves m and 1/z of every row, its second adds the log
-// ratios, and its third reads the logits again.
+// its first kernel leaves m and 1/z of every row, its second (in small calls
+// block 0 of the first) adds the log ratios, and its third reads the logits
+// again.
+//
+// What bounds them is HBM, and for vocabularies of more than one CTA the
+// exchange within the cluster.  Whole calls, of the copy rate: policy 8 x 1023 x
+// 32000 bf16 without prompt rows 162 us, 0.95; 8 x 1000 x 128256 643 us, 0.89;
+// log-probabilities 4 x 1023 x 128256 131 us, 0.89; preference 16 sequences to
+// 1024 x 32000 337 us, 0.85 of its bytes with the logits read twice.
 //
 // A row may start off a 16-byte boundary (odd vocabularies): the units are
 // those of the aligned window around it; whole ones are copied, and the two at
@@ -30,6 +37,7 @@
 #include "aloco_bulk.cuh"
 #include "aloco_logits.h"
 #include "aloco_sync_kernel.cuh"
+#include "aloco_units.cuh"
 
 namespace aloco {
 
@@ -457,21 +465,6 @@ __device__ __forceinline__ void store_alike(f2 (*v)[Unit<BF16>::kElems / 2], con
         else if (j * THREADS < left)
             store_elems<BF16>(x, dst, u0 + j * THREADS + tid, q);
     }
-}
-
-// The 16 bytes that end `bytes` (2..14, even; whole words for fp32) into cur,
-// with prev before it: what prev and cur make of a unit that lies `bytes`
-// further on.
-__device__ __forceinline__ uint4 join_units(const uint4 &prev, const uint4 &cur, int bytes) {
-    const uint32_t c[8] = {prev.x, prev.y, prev.z, prev.w, cur.x, cur.y, cur.z, cur.w};
-    const int words = bytes >> 2;
-    uint32_t t[5];  // words 3 - words and on
-#pragma unroll
-    for (int i = 0; i < 5; ++i)
-        t[i] = words & 2 ? (words & 1 ? c[i] : c[i + 1]) : (words & 1 ? c[i + 2] : c[i + 3]);
-    const uint32_t pick = bytes & 2 ? 0x5432u : 0x7654u;
-    return make_uint4(__byte_perm(t[0], t[1], pick), __byte_perm(t[1], t[2], pick),
-                      __byte_perm(t[2], t[3], pick), __byte_perm(t[3], t[4], pick));
 }
 
 // Store a stretch of n consecutive units, the window's unit u0 and on, lane i
