@@ -126,6 +126,29 @@ def test_row_counts(rows, V, dtype):
     _check_preference(x, t, cu, a["ref"], 0.7)
 
 
+@pytest.mark.parametrize("dtype,rows,V", [(torch.float32, 1400, 16000), (torch.bfloat16, 2700, 16001)],
+                         ids=IDS)
+def test_calls_whose_sums_take_a_kernel_of_their_own(dtype, rows, V):
+    """Over 80 MB of logits the policy loss's sums are a second kernel's."""
+    x, t = _logits((rows, V), dtype, 3), _targets((rows,), V, 3)
+    a = _policy_inputs(x, t, 1.0, 3)
+    _check_policy(x, t, a, 1.0, _policy(x, t, a))
+
+
+@pytest.mark.parametrize("dtype", BOTH, ids=IDS)
+@pytest.mark.parametrize("rows,pairs", [(3000, 40), (2500, 1), (60, 30), (2049, 2)])
+def test_many_rows_and_many_pairs(rows, pairs, dtype):
+    """More rows or pairs than one block of the row kernel works out by itself;
+    ragged sequences, some of them empty."""
+    x, t = _logits((rows, 257), dtype, rows), _targets((rows,), 257, rows)
+    t[::5] = -1
+    rng = np.random.default_rng(rows + pairs)
+    cu = np.sort(rng.integers(0, rows + 1, 2 * pairs + 1))
+    ref = torch.randn(rows, generator=_gen(pairs), device="cuda") - 5.0
+    _check_preference(x, t, torch.tensor(cu, device="cuda"), ref, 1.0)
+    _check_preference(x, t, torch.tensor(cu, device="cuda"), ref, 1.0, want_grad=False)
+
+
 # -------------------------------------------------------------------- layouts
 
 @pytest.mark.parametrize("dtype", BOTH, ids=IDS)
