@@ -817,8 +817,9 @@ def _on_stream(stream, device, inputs):
         current = torch.cuda.current_stream(device)
         if stream != current:
             return _OtherStream(stream, current, inputs), stream.cuda_stream
-    handle = torch._C._cuda_getCurrentRawStream(device.index)
-    if torch.cuda.current_device() == device.index:
+    index = device.index
+    handle = torch._C._cuda_getCurrentRawStream(index)
+    if torch._C._cuda_getDevice() == index:
         return _NO_SWITCH, handle
     return torch.cuda.device(device), handle
 
@@ -875,18 +876,18 @@ def _tokens(logits, targets, temperature) -> Tokens:
         raise TypeError(f"targets must be int32 or int64, not {targets.dtype}")
     if targets.shape != shape[:-1] or not targets.is_contiguous():
         raise ValueError(f"targets must be contiguous of shape {tuple(shape[:-1])}")
-    if not logits.is_cuda or targets.device != logits.device:
+    if not logits.is_cuda or targets.get_device() != logits.get_device():
         raise ValueError("logits and targets must be CUDA tensors of one device")
     return Tokens(logits.data_ptr(), targets.data_ptr(), batch, rows, vocab, batch_stride,
                   row_stride, temperature, code, size)
 
 
-def _per_row(name, t, targets, device) -> int:
-    """The address of a float32 tensor of one value per row."""
-    if t.dtype is not _torch.float32 or t.shape != targets.shape or t.device != device or \
+def _per_row(name, t, shape, index) -> int:
+    """The address of a float32 tensor of one value per row, on device `index`."""
+    if t.dtype is not _torch.float32 or t.shape != shape or t.get_device() != index or \
             not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous float32 tensor of shape "
-                         f"{tuple(targets.shape)} on the logits' device")
+                         f"{tuple(shape)} on the logits' device")
     return t.data_ptr()
 
 
@@ -897,7 +898,8 @@ def _logits_grad(logits, grad, want_grad):
             return None, None
         grad = _torch.empty_like(logits)
     elif grad.dtype != logits.dtype or grad.shape != logits.shape or \
-            grad.device != logits.device or (grad.stride(-1) != 1 and grad.shape[-1] > 1):
+            grad.get_device() != logits.get_device() or \
+            (grad.stride(-1) != 1 and grad.shape[-1] > 1):
         raise ValueError("grad must have the logits' shape, dtype and device, with "
                          "contiguous rows")
     st = grad.stride()
@@ -932,10 +934,11 @@ def policy_loss(logits, targets, advantages, old_logp, weights, *, ref_logp=None
     Enqueues only."""
     tok = _tokens(logits, targets, temperature)
     device = logits.device
-    adv = _per_row("advantages", advantages, targets, device)
-    old = _per_row("old_logp", old_logp, targets, device)
-    w = _per_row("weights", weights, targets, device)
-    ref = _per_row("ref_logp", ref_logp, targets, device) if ref_logp is not None else None
+    shape, index = targets.shape, device.index
+    adv = _per_row("advantages", advantages, shape, index)
+    old = _per_row("old_logp", old_logp, shape, index)
+    w = _per_row("weights", weights, shape, index)
+    ref = _per_row("ref_logp", ref_logp, shape, index) if ref_logp is not None else None
     cfg = PolicyCfg(clip_low, clip_high, kl_coef)
     ctx, handle = _on_stream(stream, device, (logits, targets, advantages, old_logp, weights,
                                               ref_logp, grad))
@@ -964,7 +967,8 @@ def preference_loss(logits, targets, cu_seqlens, ref_logp=None, *, beta: float =
     and want_grad as policy_loss.  Enqueues only."""
     tok = _tokens(logits, targets, temperature)
     device = logits.device
-    ref = _per_row("ref_logp", ref_logp, targets, device) if ref_logp is not None else None
+    ref = _per_row("ref_logp", ref_logp, targets.shape, device.index) \
+        if ref_logp is not None else None
     if cu_seqlens.dtype is _torch.int32:
         cu_bytes = 4
     elif cu_seqlens.dtype is _torch.int64:
@@ -972,7 +976,7 @@ def preference_loss(logits, targets, cu_seqlens, ref_logp=None, *, beta: float =
     else:
         raise TypeError(f"cu_seqlens must be int32 or int64, not {cu_seqlens.dtype}")
     if cu_seqlens.dim() != 1 or cu_seqlens.numel() % 2 == 0 or \
-            not cu_seqlens.is_contiguous() or cu_seqlens.device != device:
+            not cu_seqlens.is_contiguous() or cu_seqlens.get_device() != device.index:
         raise ValueError("cu_seqlens must be a contiguous vector of 2 pairs + 1 bounds on the "
                          "logits' device")
     pairs = cu_seqlens.numel() // 2
