@@ -652,8 +652,10 @@ __device__ __forceinline__ void block_totals(Sum (&v)[N], int tid, float2 (*sh)[
 
 // -(1 - eps) log sigmoid(z) - eps log sigmoid(-z)
 __device__ __forceinline__ float pair_loss(float z, float eps) {
-    // -log sigmoid(z) = log(1 + exp(-|z|)) + max(-z, 0)
-    return log1pf(expf(-fabsf(z))) + (z < 0.f ? (1.f - eps) * -z : eps * z);
+    // -log sigmoid(z) = log(1 + exp(-|z|)) + max(-z, 0); a margin of +inf costs
+    // nothing where no labels are flipped (0 * inf is NaN)
+    return log1pf(expf(-fabsf(z))) +
+           (z < 0.f ? (1.f - eps) * -z : eps == 0.f && z == INFINITY ? 0.f : eps * z);
 }
 
 // Log ratios of pair k and the coefficients of its rows.

@@ -1,0 +1,99 @@
+"""The post-training losses where a sum, a ratio or a margin is infinite and the
+loss is not: products of 0 and infinity have no place in it.
+
+What is expected comes in float64 from the definitions, with -log sigmoid as
+log(1 + exp(-z)), whose value at +inf is 0.  Tolerances as tests/_losses.py
+derives them, over the rows whose log-probability is finite."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import _losses as L
+from paper_2609_36662_gb300 import aloco as A
+
+pytestmark = pytest.mark.gpu
+
+BOTH = [torch.float32, torch.bfloat16]
+IDS = ["f32", "bf16"]
+
+
+def _inputs(n, V, dtype, seed):
+    g = torch.Generator("cuda").manual_seed(seed)
+    x = (torch.randn(n, V, generator=g, device="cuda") * 2).to(dtype)
+    return x, torch.randint(0, V, (n,), generator=g, device="cuda")
+
+
+def _h(t):
+    return t.detach().cpu().double().numpy()
+
+
+def _row_bound(lp, V):
+    """Bound of a finite row's log-probability and of its part in a sum."""
+    ok = np.isfinite(lp)
+    lp = np.where(ok, lp, 0.0)
+    return np.where(ok, L.tol_logp(lp, V) + 4 * L.U * np.abs(lp), 0.0)
+
+
+@pytest.mark.parametrize("dtype", BOTH, ids=IDS)
+@pytest.mark.parametrize("n,pairs,V", [(12, 3, 40), (12, 3, 9001), (90, 20, 257), (2100, 2, 33)])
+@pytest.mark.parametrize("eps", [0.0, 0.1])
+def test_a_banned_token_in_an_answer(n, pairs, V, dtype, eps):
+    """A token of logit -inf in a rejected answer: the margin is +inf, and with no
+    flipped labels that pair's loss is 0.  In small and in large calls."""
+    x, t = _inputs(n, V, dtype, V)
+    cu = np.linspace(0, n, 2 * pairs + 1).astype(np.int64)
+    at = int(cu[1])                      # the first pair's rejected answer
+    x[at, t[at]] = -math.inf
+    ref = torch.full((n,), -math.log(V) - 2.0, device="cuda")
+    beta = 0.3
+    got = A.preference_loss(x, t, torch.tensor(cu, device="cuda"), ref, beta=beta,
+                            label_smoothing=eps)
+    th = _h(t).astype(np.int64)
+    lp, p = L.logprobs(_h(x), th, 1.0)
+    assert lp[at] == -math.inf and np.isfinite(np.delete(lp, at)).all()
+    d = lp - _h(ref)
+    R = np.array([d[a:b].sum() for a, b in zip(cu[:-1], cu[1:])])
+    z = beta * (R[0::2] - R[1::2])
+    assert z[0] == math.inf and np.isfinite(z[1:]).all()
+    each = np.logaddexp(0.0, -z) * (1 - eps) + (eps * np.logaddexp(0.0, z) if eps else 0.0)
+    bound = _row_bound(lp, V)
+    assert float(got.log_ratios[1]) == -math.inf
+    if eps:
+        assert float(got.loss) == math.inf
+    else:
+        L.assert_sum(got.loss, each.mean(), beta * bound / pairs)
+    # the gradient: sigmoid(+inf) = 1 in the first pair
+    sig = np.where(z >= 0, 1 / (1 + np.exp(-np.abs(z))), 1 - 1 / (1 + np.exp(-np.abs(z))))
+    k = np.zeros(n)
+    off = np.zeros(n)
+    for i in range(2 * pairs):
+        sign, q, rows = 1 if i % 2 == 0 else -1, i // 2, slice(cu[i], cu[i + 1])
+        k[rows] = sign * (sig[q] - 1 + eps) * beta / pairs
+        # a pair's margin moves the coefficient by sigma' <= 1/4
+        pair = bound[cu[2 * q]:cu[2 * q + 2]].sum()
+        off[rows] = beta / pairs * (beta * (0.25 * pair if np.isfinite(z[q]) else 0.0) + 16 * L.U)
+    want = -p * k[:, None]
+    want[np.arange(n), th] += k
+    one = np.zeros_like(p)
+    one[np.arange(n), th] = 1.0
+    dp = p * (2 * L.tol_logp(np.log(np.maximum(p, 1e-300)), V))
+    tol = 2 * (np.abs(k)[:, None] * dp + off[:, None] * np.abs(one - p)) + \
+        (2.0 ** -8 if dtype == torch.bfloat16 else 4 * L.U) * np.abs(want) + 1e-38
+    err = np.abs(_h(got.grad) - want)
+    assert np.all(err <= tol), float(np.nanmax(err / tol))
+
+
+@pytest.mark.parametrize("dtype", BOTH, ids=IDS)
+def test_margins_of_minus_infinity_and_of_none(dtype):
+    """A banned token in a chosen answer costs infinitely much; one in both
+    answers of a pair leaves no margin."""
+    x, t = _inputs(4, 500, dtype, 3)
+    cu = torch.tensor([0, 2, 4], device="cuda")
+    x[1, t[1]] = -math.inf
+    for eps in (0.0, 0.2):
+        got = A.preference_loss(x, t, cu, label_smoothing=eps)
+        assert float(got.loss) == math.inf and not bool(torch.isnan(got.grad).any())
+    x[3, t[3]] = -math.inf
+    assert math.isnan(float(A.preference_loss(x, t, cu).loss))
