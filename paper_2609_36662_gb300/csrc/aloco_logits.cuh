@@ -610,7 +610,8 @@ __device__ __noinline__ void add_parts(const LogitsArgs &a, int clusters, int ti
     }
     if (tid == 0) {
         const float gain = s[0].value(), kl = s[1].value();
-        a.terms_out[0] = fmaf(a.kl, kl, gain);
+        // (without a coefficient the KL sum is only watched, and may be infinite)
+        a.terms_out[0] = a.kl != 0.f ? fmaf(a.kl, kl, gain) : gain;
         a.terms_out[1] = gain;
         a.terms_out[2] = kl;
         a.terms_out[3] = s[2].value();

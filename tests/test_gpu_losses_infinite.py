@@ -97,3 +97,33 @@ def test_margins_of_minus_infinity_and_of_none(dtype):
         assert float(got.loss) == math.inf and not bool(torch.isnan(got.grad).any())
     x[3, t[3]] = -math.inf
     assert math.isnan(float(A.preference_loss(x, t, cu).loss))
+
+
+@pytest.mark.parametrize("dtype", BOTH, ids=IDS)
+@pytest.mark.parametrize("n,V", [(9, 40), (9, 50001), (2700, 16001)])
+def test_a_reference_that_is_only_watched(n, V, dtype):
+    """kl_coef = 0 with a reference: the KL sum is reported, here without a finite value (the
+    reference far above, and a banned token), and the loss is the policy term
+    alone.  In small calls and where the sums take a kernel of their own."""
+    x, t = _inputs(n, V, dtype, V)
+    x[1, t[1]] = -math.inf
+    lp = A.token_logprobs(x, t)
+    assert float(lp[1]) == -math.inf
+    old = torch.where(torch.isfinite(lp), lp + 0.1, -9.0)
+    ref = old.clone()
+    ref[2] += 200.0
+    adv = torch.where(torch.arange(n, device="cuda") % 2 == 0, 1.0, 0.5)
+    w = torch.full((n,), 1.0 / n, device="cuda")
+    got = A.policy_loss(x, t, adv, old, w, ref_logp=ref, kl_coef=0.0)
+    assert not math.isfinite(float(got.terms[2]))
+    exact = L.logprobs(_h(x), _h(t).astype(np.int64), 1.0)[0]
+    r = np.exp(exact - _h(old))
+    want = (_h(w) * -np.minimum(r * _h(adv), np.clip(r, 0.8, 1.2) * _h(adv))).sum()
+    bound = _h(w) * np.abs(_h(adv)) * (r * _row_bound(exact, V) + 32 * L.U * (r + 1.2))
+    L.assert_sum(got.terms[0], want, bound)
+    assert torch.equal(got.terms[0], got.terms[1])
+    alone = A.policy_loss(x, t, adv, old, w)
+    assert torch.equal(got.grad, alone.grad) and torch.equal(got.terms[0], alone.terms[0])
+    # with a coefficient it counts
+    again = A.policy_loss(x, t, adv, old, w, ref_logp=ref, kl_coef=0.1)
+    assert not math.isfinite(float(again.terms[0]))
