@@ -1097,7 +1097,10 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
                 const float weight = r.f.x;
                 const Scale unit = {kLog2e, kLog2eLo};
                 const float ratio = exp_of(logp, r.f.y, unit);
-                const float free = ratio * r.f.w;
+                // (a ratio beyond fp32 of a finite logarithm is no infinity: without
+                // an advantage it counts 0)
+                const float free = r.f.w == 0.f && ratio == INFINITY && r.f.y >= -FLT_MAX
+                                       ? 0.f : ratio * r.f.w;
                 const float bound = fminf(fmaxf(ratio, a.lo), a.hi) * r.f.w;
                 const bool act = free <= bound;
                 const float d = r.f.z - logp;

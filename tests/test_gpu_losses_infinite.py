@@ -127,3 +127,24 @@ def test_a_reference_that_is_only_watched(n, V, dtype):
     # with a coefficient it counts
     again = A.policy_loss(x, t, adv, old, w, ref_logp=ref, kl_coef=0.1)
     assert not math.isfinite(float(again.terms[0]))
+
+
+@pytest.mark.parametrize("dtype", BOTH, ids=IDS)
+def test_ratios_beyond_fp32_without_an_advantage(dtype):
+    """r A is 0 where the advantage is, also where r = exp(logp - old) leaves
+    fp32 (an old policy that all but ruled the token out)."""
+    V = 700
+    x, t = _inputs(6, V, dtype, 4)
+    lp = A.token_logprobs(x, t)
+    old, adv = lp.clone(), torch.zeros(6, device="cuda")
+    old[:3] -= 200.0
+    adv[5] = -0.0
+    old[5] -= 150.0
+    w = torch.full((6,), 1.0 / 6, device="cuda")
+    got = A.policy_loss(x, t, adv, old, w)
+    assert not bool(got.terms[:3].any()) and not bool(torch.isnan(got.terms).any())
+    assert not bool(got.grad.any())
+    # a missing value stays one
+    lost = old.clone()
+    lost[0] = math.nan
+    assert math.isnan(float(A.policy_loss(x, t, adv, lost, w).terms[0]))
