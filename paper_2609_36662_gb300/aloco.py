@@ -999,11 +999,35 @@ def preference_loss(logits, targets, cu_seqlens, ref_logp=None, *, beta: float =
     return PreferenceLoss(loss, ratios, logp, out)
 
 
+class _Owned:
+    """Tensors that somebody holds besides Python, as a parameter holds its
+    gradient (or a view its base), and whether one has lost its last such owner
+    since the last call without having been written: its owner has another by
+    then."""
+
+    def __init__(self, tensors):
+        self._take(t for t in tensors if not t.is_inference())
+
+    def _take(self, tensors):
+        """Those that are owned now, with their versions."""
+        self.seen = [(t, t._version) for t in tensors if t._use_count() > 1]
+
+    def stale(self) -> bool:
+        if any(t._use_count() == 1 and t._version == v for t, v in self.seen):
+            return True
+        self._take([t for t, _ in self.seen])
+        return False
+
+
 class GradList:
     """The gradient tensors of one model (contiguous float32 or bfloat16 CUDA
     tensors of one device, in the order of the flat vector), kept for
-    grad_norm and clip_grads step after step.  It holds the tensors; one whose
-    memory has moved since is refused."""
+    grad_norm and clip_grads step after step.  It is a list of these tensors,
+    which it holds, not of whatever takes their place: one whose memory has
+    moved is refused, and so is one that its owner has let go of since the list
+    was made or last used, if nothing has written to it since (zero_grad() drops
+    a parameter's gradient, and the next backward pass makes another; with
+    set_to_none=False it stays)."""
 
     def __init__(self, tensors):
         import torch
@@ -1020,6 +1044,7 @@ class GradList:
         n = len(self.tensors)
         self._pointers = [t.data_ptr for t in self.tensors]
         self._at = [p() for p in self._pointers]
+        self._owned = _Owned(self.tensors)
         sizes = [t.numel() for t in self.tensors]
         self.numel = sum(sizes)
         handle = ctypes.c_void_p()
@@ -1035,6 +1060,10 @@ class GradList:
     def _check(self):
         if [p() for p in self._pointers] != self._at:
             raise ValueError("a gradient's memory has moved since the GradList was made")
+        if self._owned.stale():
+            raise ValueError("a gradient has lost its owner and was not written since the last "
+                             "call (zero_grad lets backward make gradients anew unless "
+                             "set_to_none=False): make a new GradList")
 
     def __del__(self):
         if getattr(self, "_handle", None) is not None and _lib is not None:
