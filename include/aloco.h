@@ -883,15 +883,16 @@ int aloco_sync_noalloc(float *global, float *momentum, void *const *locals,
  * thread's next round that runs the bulk-copy pass (aloco_sync /
  * aloco_sync_ex) or the fused INT8 pass (aloco_sync_int8) skips the copies
  * of tile `tile` (bulk-copy pass) or of codec block `tile` (fused INT8
- * pass, a whole aligned block); a negative value cancels.  That stage's
+ * pass, a whole aligned block); -1 cancels.  That stage's
  * mbarrier then never completes, so the bounded waits on it (about 2 s) run
  * out: the block aborts, lets its copies in flight land, and the round
  * returns ALOCO_ERR_CUDA with every kernel finished and the device usable.
  * aloco_token_logprobs, aloco_policy_loss and aloco_preference_loss read it
  * too: block 0 of their row kernel leaves out the copy of its slot `tile`, and
  * what waits for it leaves NaN in the log-probabilities of that row and of the
- * block's later ones, and so in the loss.  The hook is consumed by that round
- * or call; no other reads it. */
+ * block's later ones, and so in the loss; with a tile below -1 it issues its
+ * first copy -tile cycles late instead (at most 8e9; no other round heeds such a
+ * tile).  The hook is consumed by that round or call; no other reads it. */
 void aloco_test_stall_tile(int64_t tile);
 
 /* Message of the last failure on the calling thread ("" if none).  The

@@ -762,7 +762,8 @@ def adamw_step(params, grads, exp_avg, exp_avg_sq, cfg: AdamwCfg,
 
 def test_stall_tile(tile: int):
     """Testing only: the next bulk-copy round (or post-training loss) on this
-    thread skips the copies of one tile, so that its bounded wait runs out
+    thread skips the copies of one tile, so that its bounded wait runs out; a
+    tile below -1 makes a loss's first copy so many cycles late
     (aloco_test_stall_tile)."""
     load().aloco_test_stall_tile(int(tile))
 

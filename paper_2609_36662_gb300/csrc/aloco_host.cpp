@@ -1607,7 +1607,9 @@ static int adamw_impl(void *const *params, const void *const *grads,
     return ALOCO_OK;
 }
 
-void aloco_test_stall_tile(int64_t tile) { t_test_stall_tile1 = tile >= 0 ? tile + 1 : 0; }
+void aloco_test_stall_tile(int64_t tile) {
+    t_test_stall_tile1 = tile >= 0 ? tile + 1 : tile < -1 ? tile : 0;
+}
 
 const char *aloco_last_error(void) { return t_err.c_str(); }
 

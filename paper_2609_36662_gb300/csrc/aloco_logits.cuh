@@ -16,7 +16,7 @@
 // the gradient is written once.
 // The preference loss needs every row of a pair before any of its gradients:
 // its first kernel leaves m and 1/z of every row, its second (in small calls
-// block 0 of the first) adds the log ratios, and its third reads the logits
+// the first one's last cluster) adds the log ratios, and its third reads the logits
 // again.
 //
 // What bounds them is HBM, and for vocabularies of more than one CTA the
@@ -36,6 +36,7 @@
 
 #include "aloco_bulk.cuh"
 #include "aloco_logits.h"
+#include "aloco_marks.cuh"
 #include "aloco_sync_kernel.cuh"
 #include "aloco_units.cuh"
 
@@ -54,7 +55,7 @@ __device__ __forceinline__ void wait_for_previous() {
 // What a row kernel leaves: log-probabilities, also a gradient, the same where
 // the gradient's rows may lie otherwise to the 16-byte boundaries than the
 // logits' do, what the preference loss needs of a row, or its gradient.
-// (kPolicySmall: see hand_in.)
+// (kPolicySmall: see last_to_come.)
 constexpr int kFwd = 0, kPolicy = 1, kPolicyShifted = 2, kPref = 3, kGrad = 4, kGradShifted = 5,
               kPolicySmall = 6;
 constexpr bool is_policy(int mode) {
@@ -505,7 +506,13 @@ __device__ __forceinline__ void store_shifted(f2 (*v)[Unit<BF16>::kElems / 2],
     }
 }
 
-// Whether every consumer (barrier 1) says yes.
+// Barrier 1: the consumers.
+template <int THREADS>
+__device__ __forceinline__ void sync_threads() {
+    asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+}
+
+// Whether every consumer says yes.
 template <int THREADS>
 __device__ __forceinline__ bool all_of(bool yes) {
     uint32_t r;
@@ -538,24 +545,23 @@ __device__ __forceinline__ void give_up(const LogitsArgs &a, int64_t row) {
     }
 }
 
-// A cluster's sums of the policy loss, and behind them the call's mark.  In a
-// small call block 0 waits for all marks and adds the sums: a second kernel for
-// that takes 3 us of the host's time, which such calls are made of (48 rows of
-// 32000: 29 -> 24 us).  (No block waits for block 0, so that all end whatever is
-// resident.)  A large call has the second kernel, which the next call overlaps,
-// where block 0 would be the last to end (8 x 1023 x 32000 bf16: 162 us, 167 in
-// one kernel).
-__device__ __forceinline__ void hand_in(PolicyPart *p, unsigned long long mark, float gain,
-                                        float kl, float cut) {
-    p->term[0] = gain;
-    p->term[1] = kl;
-    p->term[2] = cut;
-    asm volatile("st.release.gpu.global.u64 [%0], %1;" ::"l"(&p->mark), "l"(mark) : "memory");
+// Whether this cluster, by the consumers of its first CTA (barrier 1), is the
+// last of the grid to come here, and so finishes the call (aloco_marks.cuh).  In
+// a small call a second kernel for that takes 3 us of the host's time, which
+// such calls are made of (48 rows of 32000: 29 -> 24 us).  A large call has the
+// second kernel, which the next call overlaps (8 x 1023 x 32000 bf16: 162 us, 167
+// in one kernel).  (Not inlined: the row kernel's registers are the rows'.)
+template <int THREADS>
+__device__ __noinline__ bool last_to_come(const LogitsArgs &a, int cluster, int clusters,
+                                          int tid) {
+    char *const marks = reinterpret_cast<char *>(&a.parts->mark);
+    if (tid == 0) leave_mark(&a.parts[cluster].mark, a.mark);
+    sync_threads<THREADS>();
+    const bool last = all_of<THREADS>(
+        marks_here<THREADS>(marks, sizeof(PolicyPart), clusters, a.mark, tid));
+    if (last) take_marks<THREADS>(marks, sizeof(PolicyPart), clusters, tid);
+    return last;
 }
-
-// About a minute: every block hands in, also one that has given up, but blocks
-// may wait for SMs that another stream's kernels hold.
-constexpr long long kMarkWaitCycles = 30 * kTmaWaitCycles;
 
 // Sums of up to 32 lanes, in every lane.
 __device__ __forceinline__ void sum_over_warp(Sum &s) {
@@ -568,28 +574,17 @@ __device__ __forceinline__ void sum_over_warp(Sum &s) {
     }
 }
 
-// By the consumers of a block (barrier 1), in a fixed order; WAIT: while others
-// may still be at their rows.  The marks are
-// taken away, so that a captured call finds none of its own when it runs again.
-// (Not inlined: the row kernel's registers are the rows'.)
-template <int THREADS, bool WAIT>
+// The policy loss's sums from the clusters' parts, by THREADS threads (barrier
+// 1), in a fixed order.
+template <int THREADS>
 __device__ __noinline__ void add_parts(const LogitsArgs &a, int clusters, int tid,
                                           float2 (*sh)[THREADS / 32]) {
     constexpr int WARPS = THREADS / 32;
     Sum s[kTerms] = {};
-    const long long t0 = clock64();
     for (int c = tid; c < clusters; c += THREADS) {
-        PolicyPart *p = a.parts + c;
-        unsigned long long mark;
-        bool here = !WAIT;
-        while (!here) {
-            asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(mark) : "l"(&p->mark) : "memory");
-            here = mark == a.mark;
-            if (!here && clock64() - t0 > kMarkWaitCycles) break;
-        }
+        const PolicyPart *p = a.parts + c;
         const float t[kTerms] = {__ldcg(&p->term[0]), __ldcg(&p->term[1]), __ldcg(&p->term[2])};
-        if (WAIT) p->mark = 0;
-        for (int j = 0; j < kTerms; ++j) s[j].add(here ? t[j] : NAN);
+        for (int j = 0; j < kTerms; ++j) s[j].add(t[j]);
     }
     __syncwarp();
 #pragma unroll
@@ -597,7 +592,7 @@ __device__ __noinline__ void add_parts(const LogitsArgs &a, int clusters, int ti
         sum_over_warp(s[j]);
         if ((tid & 31) == 0) sh[j][tid >> 5] = make_float2(s[j].s, s[j].rest);
     }
-    asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+    sync_threads<THREADS>();
     if (tid >= 32) return;
 #pragma unroll
     for (int j = 0; j < kTerms; ++j) {
@@ -623,11 +618,6 @@ __device__ __noinline__ void add_parts(const LogitsArgs &a, int clusters, int ti
 // In fp32 with the additions' rests kept: fp64 units are rare here (one fp64 exp
 // took longer than a pair's rows).  THREADS threads, which barrier 1 counts.
 constexpr int kPairBlock = 512;
-
-template <int THREADS>
-__device__ __forceinline__ void sync_threads() {
-    asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
-}
 
 // The sums of N values over the threads in a fixed order, in every thread.
 template <int THREADS, int N>
@@ -708,20 +698,9 @@ __device__ __forceinline__ void mean_of_pairs(const LogitsArgs &a, int tid,
     if (tid == 0) a.loss[0] = a.pairs ? s[0].value() / (float)a.pairs : 0.f;
 }
 
-// All pairs, by the consumers of one block, when every block has handed in.
+// All pairs, by the consumers of the last block to come.
 template <int THREADS>
-__device__ __noinline__ void all_pairs(const LogitsArgs &a, int blocks, int tid,
-                                       float2 (*sh)[THREADS / 32]) {
-    const long long t0 = clock64();
-    for (int c = tid; c < blocks; c += THREADS) {
-        unsigned long long mark;
-        do {
-            asm volatile("ld.acquire.gpu.global.u64 %0, [%1];"
-                         : "=l"(mark) : "l"(&a.parts[c].mark) : "memory");
-        } while (mark != a.mark && clock64() - t0 < kMarkWaitCycles);
-        a.parts[c].mark = 0;
-    }
-    sync_threads<THREADS>();
+__device__ __noinline__ void all_pairs(const LogitsArgs &a, int tid, float2 (*sh)[THREADS / 32]) {
     for (int64_t k = 0; k < a.pairs; ++k) one_pair<THREADS>(a, k, tid, sh);
     mean_of_pairs<THREADS>(a, tid, sh);
 }
@@ -894,6 +873,9 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
                         if (lane == 0) {
                             const uint32_t bytes = hi > lo ? (uint32_t)(hi - lo) * 16 : 0;
                             mbar_arrive_expect_tx(full, bytes);
+                            if (a.test_stall1 < 0 && !blockIdx.x && !filled)
+                                for (const long long t0 = clock64();
+                                     clock64() - t0 < -a.test_stall1;) {}
                             if (bytes && (blockIdx.x || filled + 1 != a.test_stall1))
                                 bulk_load(smem_addr(at + (size_t)(lo - u0) * 16),
                                           x.base + (size_t)lo * 16, bytes, full);
@@ -1147,17 +1129,19 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
                 }
             }
         }
+        // (the first CTA of a cluster has written what its rows leave)
         if constexpr (is_policy(MODE)) {
-            if (rank == 0 && tid == 0)
-                hand_in(a.parts + row0, a.mark, terms[0].value(), terms[1].value(), terms[2].value());
-            if (MODE != kPolicy && a.finish && blockIdx.x == 0)
-                add_parts<THREADS, true>(a, (int)step, tid, s_sums);
+            if (rank == 0 && tid == 0) {
+                PolicyPart *const p = a.parts + row0;
+                for (int j = 0; j < kTerms; ++j) p->term[j] = terms[j].value();
+            }
+            if (MODE != kPolicy && a.finish && rank == 0 &&
+                last_to_come<THREADS>(a, (int)row0, (int)step, tid))
+                add_parts<THREADS>(a, (int)step, tid, s_sums);
         }
-        if (MODE == kPref && a.finish) {
-            // (the first CTA of a cluster writes what its rows leave)
-            if (rank == 0 && tid == 0) hand_in(a.parts + row0, a.mark, 0.f, 0.f, 0.f);
-            if (blockIdx.x == 0) all_pairs<THREADS>(a, (int)step, tid, s_sums);
-        }
+        if (MODE == kPref && a.finish && rank == 0 &&
+            last_to_come<THREADS>(a, (int)row0, (int)step, tid))
+            all_pairs<THREADS>(a, tid, s_sums);
     }
     // no CTA leaves while another may still write to its memory
     if (C > 1)
@@ -1171,7 +1155,7 @@ __global__ void __launch_bounds__(kSumBlock)
     policy_sums_kernel(const __grid_constant__ LogitsArgs a, int clusters) {
     __shared__ float2 sh[kTerms][kSumBlock / 32];
     wait_for_previous();
-    add_parts<kSumBlock, false>(a, clusters, threadIdx.x, sh);
+    add_parts<kSumBlock>(a, clusters, threadIdx.x, sh);
 }
 
 __global__ void __launch_bounds__(kPairBlock)
@@ -1329,7 +1313,7 @@ template <bool BF16>
 cudaError_t launch_preference_rows(const LogitsArgs &in, int sm_count, cudaStream_t stream) {
     LogitsArgs a = in;
     int used;
-    // few rows: block 0 of the row kernel is done with the pairs sooner than
+    // few rows: the row kernel's last cluster is done with the pairs sooner than
     // another kernel is launched
     a.finish = a.n > 0 && a.n <= 2048 && a.pairs <= 16;
     cudaError_t e = launch_rows<BF16, kPref>(a, sm_count, stream, &used);

@@ -16,7 +16,7 @@ struct Rows {
 // Sums of the policy loss besides L itself.
 constexpr int kTerms = 3;
 
-// One cluster's share of them (scratch), and a mark that says it is there.
+// One cluster's share of them (scratch), and the mark that it has come.
 struct PolicyPart {
     float term[kTerms];
     float unused;
@@ -37,7 +37,7 @@ struct LogitsArgs {
     float lo, hi, kl;                // 1 - clip_low, 1 + clip_high, kl_coef
     PolicyPart *parts;               // [at most n clusters of the row kernel]
     unsigned long long mark;         // this call's, never 0
-    int finish;                      // 1: block 0 of the row kernel adds them
+    int finish;                      // 1: the row kernel's last cluster adds them
                                      // (preference loss: works out the pairs)
     float *terms_out;                // [kTerms + 1]
     // preference loss (ref as above)
@@ -51,7 +51,8 @@ struct LogitsArgs {
     int stages, cluster, per;        // the row kernel: ring slots, CTAs of a
                                      // cluster, units of a CTA's part at most
     int64_t test_stall1;             // testing only: 1 + the number of the slot
-                                     // whose copy block 0 leaves out (0: none)
+                                     // whose copy block 0 leaves out; below 0:
+                                     // its first copy comes so many cycles late
 };
 
 cudaError_t token_logprobs_f32(const LogitsArgs &a, int sm_count, cudaStream_t stream);

@@ -252,8 +252,10 @@ unsigned long long new_mark() {
     return (2 * calls.fetch_add(1, std::memory_order_relaxed) + 1) * 0x9e3779b97f4a7c15ull;
 }
 
+constexpr int64_t kMostLate = 8000000000;  // cycles, 4 s
+
 void take_stall(aloco::LogitsArgs *a) {
-    a->test_stall1 = t_test_stall_tile1;
+    a->test_stall1 = std::max<int64_t>(t_test_stall_tile1, -kMostLate);
     t_test_stall_tile1 = 0;
 }
 
