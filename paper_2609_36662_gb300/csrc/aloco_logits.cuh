@@ -890,17 +890,21 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
         }
         // the zeros' source stays until their copies have read it
         if (writes_grad(MODE) && lane == 0) bulk_wait_all();
-        if (!ok) {  // given up: no copy may land after the block has ended
-            s_abort = 1;
-            for (unsigned k = 0; k < (unsigned)stages && k < filled; ++k) {
-                if (place.i == 0) {
-                    place.i = stages;
-                    place.phase ^= 1;
-                }
-                --place.i;
-                mbar_wait(smem_addr(&s_full[place.i]), place.phase, nullptr);
+        if (!ok) s_abort = 1;
+        // No copy may land after the block has ended, whoever has given up: where
+        // all slots were free, this warp comes here without having waited, and
+        // the consumers may leave while the last copies are on their way.
+        bool landed = true;
+        for (unsigned k = 0; k < (unsigned)stages && k < filled; ++k) {
+            if (place.i == 0) {
+                place.i = stages;
+                place.phase ^= 1;
             }
+            --place.i;
+            landed &= mbar_wait(smem_addr(&s_full[place.i]), place.phase, nullptr);
         }
+        if (a.test_stall1 < 0 && !blockIdx.x && lane == 0 && !landed)  // testing only
+            a.logp[row_at<MODE>(a, row0)] = 0.f;
     } else {
         const Scale scale = {a.scale, a.scale_lo};
         const f2 hi2 = pair(scale.hi, scale.hi), lo2 = pair(scale.lo, scale.lo);

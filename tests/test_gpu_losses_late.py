@@ -76,3 +76,31 @@ def test_small_calls_many_times_over():
             want = [v.clone() for v in call()]
             for _ in range(150):
                 assert all(torch.equal(p, q) for p, q in zip(call(), want))
+
+
+TOO_LATE = 6_000_000_000   # cycles: 3 s, where a wait's limit is about 2
+
+
+@pytest.mark.parametrize("dtype", BOTH, ids=IDS)
+@pytest.mark.parametrize("n,V", [(2, 300), (20, 4000), (7, 32000), (3, 128256)])
+def test_a_copy_that_comes_too_late_lands_before_its_block_ends(n, V, dtype):
+    """The consumers have given up when the copy is issued, and the producer has no
+    slot to wait for; the block stays until the copy has landed (else the row's
+    log-probability would read 0), the row is NaN, and the next call is right."""
+    x, calls = _calls(n, V, dtype, V)
+    t = torch.randint(0, V, (n,), device="cuda")
+    for call, logp in ((calls[0], lambda r: r.logp), (calls[1], lambda r: r.logp),
+                       (lambda: A.token_logprobs(x, t), lambda r: r)):
+        want = logp(call()).clone()
+        torch.cuda.synchronize()
+        A.test_stall_tile(-TOO_LATE)
+        t0 = time.time()
+        got = call()
+        torch.cuda.synchronize()
+        assert 2.0 < time.time() - t0 < 40.0
+        assert bool(torch.isnan(logp(got)[0]))
+        if not torch.is_tensor(got):
+            assert bool(torch.isnan(got[0].reshape(-1)[0]))  # the loss
+        bad = torch.isnan(logp(got))
+        assert torch.equal(logp(got)[~bad], want[~bad])
+        assert torch.equal(logp(call()), want)
