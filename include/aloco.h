@@ -645,10 +645,20 @@ void aloco_grads_destroy(aloco_grads_t *grads);
 /* norm[1] (device fp32) = sqrt(sum of all g^2).  Squares are added in fp32
  * over at most 32 elements and then in fp32 with the additions' rounding kept,
  * in a fixed order; values whose squares leave fp32's range are squared and
- * added in fp64.  NaN or inf where a gradient is, or the norm leaves fp32.  Enqueues one kernel on opts->stream.  Calls with one handle
- * share its partial sums: calls that overlap on the GPU race. */
+ * added in fp64.  NaN or inf where a gradient is, or the norm leaves fp32.
+ * Enqueues one kernel on opts->stream.  Calls without scratch of their own share
+ * the handle's partial sums: those that may overlap on the GPU need
+ * aloco_grad_norm_in. */
 int aloco_grad_norm(aloco_grads_t *grads, float *norm,
                     const aloco_opts_t *opts);
+
+/* Bytes of scratch of a call with that handle, and the call with scratch of the
+ * caller's: device memory, 16-byte aligned, zeros before its first call (every
+ * call leaves it ready for the next); NULL: the handle's.  Calls with one handle
+ * may overlap where their scratch is not the same. */
+size_t aloco_grads_scratch_bytes(const aloco_grads_t *grads);
+int aloco_grad_norm_in(aloco_grads_t *grads, float *norm, void *scratch,
+                       size_t scratch_bytes, const aloco_opts_t *opts);
 
 /* Clip: c = min(1, max_norm / (norm + 1e-6)), as aloco_adamw_step forms it
  * (a norm of inf gives c = 0, and inf * 0 = NaN where the inf was; NaN gives
@@ -659,10 +669,14 @@ int aloco_grad_norm(aloco_grads_t *grads, float *norm,
  *     in the handle's order, and the tensors are only read.  It may overlap
  *     none of them.
  * max_norm is finite and > 0 in fp32.  norm[1] receives the norm before clipping.
- * Enqueues two kernels. */
+ * Enqueues two kernels.  Calls that may overlap on the GPU need
+ * aloco_clip_grads_in, with scratch as aloco_grad_norm_in takes it. */
 int aloco_clip_grads(aloco_grads_t *grads, double max_norm, void *out,
                      aloco_dtype out_dtype, float *norm,
                      const aloco_opts_t *opts);
+int aloco_clip_grads_in(aloco_grads_t *grads, double max_norm, void *out,
+                        aloco_dtype out_dtype, float *norm, void *scratch,
+                        size_t scratch_bytes, const aloco_opts_t *opts);
 
 /* ------------------------------------------------------------------------
  * Interval controller (Sec. 3.1; App. A).  Host-only and scalar: after each

@@ -43,7 +43,8 @@ EXPORTS = ("aloco_default_opts", "aloco_inner_lr_accum", "aloco_correction",
            "aloco_adamw_step_normed",
            "aloco_token_logprobs", "aloco_loss_scratch_bytes", "aloco_policy_loss",
            "aloco_preference_loss", "aloco_grads_create", "aloco_grads_destroy",
-           "aloco_grad_norm", "aloco_clip_grads",
+           "aloco_grad_norm", "aloco_clip_grads", "aloco_grads_scratch_bytes",
+           "aloco_grad_norm_in", "aloco_clip_grads_in",
            "aloco_ctrl_default_cfg", "aloco_ctrl_init", "aloco_select_interval",
            "aloco_ctrl_state_bytes", "aloco_ctrl_save", "aloco_ctrl_load",
            "aloco_test_stall_tile", "aloco_last_error", "aloco_shutdown",
@@ -295,6 +296,12 @@ def load():
     lib.aloco_grad_norm.restype = i32
     lib.aloco_clip_grads.argtypes = [vp, dbl, vp, i32, vp, P(Opts)]
     lib.aloco_clip_grads.restype = i32
+    lib.aloco_grads_scratch_bytes.argtypes = [vp]
+    lib.aloco_grads_scratch_bytes.restype = ctypes.c_size_t
+    lib.aloco_grad_norm_in.argtypes = [vp, vp, vp, ctypes.c_size_t, P(Opts)]
+    lib.aloco_grad_norm_in.restype = i32
+    lib.aloco_clip_grads_in.argtypes = [vp, dbl, vp, i32, vp, vp, ctypes.c_size_t, P(Opts)]
+    lib.aloco_clip_grads_in.restype = i32
     lib.aloco_sync_host.argtypes = sync_args + [ctypes.c_size_t, P(Opts), P(Stats)]
     lib.aloco_sync_host.restype = i32
     lib.aloco_sync_shard.argtypes = sync_args + [P(Opts), P(Partials)]
@@ -1023,7 +1030,7 @@ class _Owned:
 class GradList:
     """The gradient tensors of one model (contiguous float32 or bfloat16 CUDA
     tensors of one device, in the order of the flat vector), kept for
-    grad_norm and clip_grads step after step.  It is a list of these tensors,
+    grad_norm and clip_grads step after step, on any stream.  It is a list of these tensors,
     which it holds, not of whatever takes their place: one whose memory has
     moved is refused, and so is one that its owner has let go of since the list
     was made or last used, if nothing has written to it since (zero_grad() drops
@@ -1057,6 +1064,20 @@ class GradList:
         if rc != OK:
             raise AlocoError(rc, last_error())
         self._handle = handle
+        self._need = load().aloco_grads_scratch_bytes(handle)
+        self._kept = {}   # scratch by stream
+
+    def _scratch(self, stream):
+        """Scratch of a call on `stream` (a raw handle, current): one for every
+        stream, whose calls follow one another.  A captured call has its own,
+        zeroed at every replay, which may run beside any other call."""
+        if _torch.cuda.is_current_stream_capturing():
+            return _torch.zeros(self._need, dtype=_torch.uint8, device=self.device)
+        s = self._kept.get(stream)
+        if s is None:
+            s = self._kept[stream] = _torch.zeros(self._need, dtype=_torch.uint8,
+                                                  device=self.device)
+        return s
 
     def _check(self):
         if [p() for p in self._pointers] != self._at:
@@ -1087,7 +1108,8 @@ def grad_norm(grads, *, stream=None):
     ctx, handle = _on_stream(stream, g.device, g.tensors)
     with ctx:
         norm = _torch.empty((), dtype=_torch.float32, device=g.device)
-        rc = load().aloco_grad_norm(g._handle, norm.data_ptr(), ctypes.byref(Opts(stream=handle)))
+        rc = load().aloco_grad_norm_in(g._handle, norm.data_ptr(), g._scratch(handle).data_ptr(),
+                                       g._need, ctypes.byref(Opts(stream=handle)))
     _finish(rc, ctx, norm)
     return norm
 
@@ -1107,8 +1129,9 @@ def clip_grads(grads, max_norm: float, *, out=None, stream=None):
     ctx, handle = _on_stream(stream, g.device, g.tensors if out is None else [*g.tensors, out])
     with ctx:
         norm = _torch.empty((), dtype=_torch.float32, device=g.device)
-        rc = load().aloco_clip_grads(g._handle, max_norm,
-                                     out.data_ptr() if out is not None else None, dtype,
-                                     norm.data_ptr(), ctypes.byref(Opts(stream=handle)))
+        rc = load().aloco_clip_grads_in(g._handle, max_norm,
+                                        out.data_ptr() if out is not None else None, dtype,
+                                        norm.data_ptr(), g._scratch(handle).data_ptr(), g._need,
+                                        ctypes.byref(Opts(stream=handle)))
     _finish(rc, ctx, norm)
     return norm

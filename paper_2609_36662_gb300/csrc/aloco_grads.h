@@ -5,8 +5,8 @@
 
 namespace aloco {
 
-// A stretch of one tensor: at most kGradChunk elements, from a place that
-// lies to the 16-byte boundaries as the tensor's start does.
+// A stretch of one tensor, of a multiple of 4096 elements but at the tensor's
+// end: its start lies to the 16-byte boundaries as the tensor's does.
 struct GradChunk {
     void *p;
     int64_t at;     // its first element's place in the flat vector
@@ -26,7 +26,7 @@ struct __align__(16) GradPartial {
 struct GradArgs {
     const GradChunk *chunks;
     int n_chunks;
-    GradPartial *partials;  // [grid]
+    GradPartial *partials;  // [grid] (scratch, as the next two)
     unsigned int *ticket;   // 0 between launches
     float *factor;          // clipping factor
     float *norm;

@@ -396,8 +396,10 @@ struct aloco_grads {
     int device = -1;
     int sm_count = 0;
     int n_chunks = 0;
-    char *dev = nullptr;           // chunk table, partial sums, factor, ticket
-    aloco::GradArgs args;          // device pointers filled in
+    char *dev = nullptr;           // chunk table, and scratch for callers with none
+    size_t scratch_bytes = 0;      // ticket, factor and partial sums
+    void *scratch = nullptr;
+    aloco::GradArgs args;          // the table filled in
     int64_t total = 0;
     bool overlap = false;          // two tensors share memory
     std::vector<std::pair<uintptr_t, uintptr_t>> ranges;  // sorted [begin, end)
@@ -445,7 +447,8 @@ int grads_create(const void *const *grads, const int64_t *sizes, const int32_t *
 
     const size_t table = (chunks.size() * sizeof(aloco::GradChunk) + 255) / 256 * 256;
     const int blocks = aloco::grad_norm_blocks(sms, (int)chunks.size());
-    const size_t bytes = table + (size_t)blocks * sizeof(aloco::GradPartial) + 256;
+    const size_t scratch = (size_t)blocks * sizeof(aloco::GradPartial) + 16;
+    const size_t bytes = table + scratch;
     char *dev = nullptr;
     cudaError_t e = cudaMalloc((void **)&dev, bytes);
     if (e != cudaSuccess) {
@@ -475,14 +478,27 @@ int grads_create(const void *const *grads, const int64_t *sizes, const int32_t *
     std::memset(&h->args, 0, sizeof h->args);
     h->args.chunks = reinterpret_cast<const aloco::GradChunk *>(dev);
     h->args.n_chunks = h->n_chunks;
-    h->args.partials = reinterpret_cast<aloco::GradPartial *>(dev + table);
-    h->args.factor = reinterpret_cast<float *>(h->args.partials + blocks);
-    h->args.ticket = reinterpret_cast<unsigned int *>(h->args.factor + 1);
+    h->scratch_bytes = scratch;
+    h->scratch = dev + table;
     *out = h;
     return done();
 }
 
-int check_list(const aloco_grads_t *g, const float *norm) {
+bool meet(const void *p, size_t m, const void *q, size_t n) {
+    return (uintptr_t)p < (uintptr_t)q + n && (uintptr_t)q < (uintptr_t)p + m;
+}
+
+bool hits(const aloco_grads_t *g, const void *p, size_t bytes) {
+    const uintptr_t a = (uintptr_t)p, b = a + bytes;
+    for (const auto &r : g->ranges)
+        if (a < r.second && r.first < b) return true;
+    return false;
+}
+
+// What both operators check of the list, norm and scratch (null: the handle's
+// own); fills in their arguments.
+int take_list(const aloco_grads_t *g, float *norm, void *scratch, size_t scratch_bytes,
+              RangeCheck *check, aloco::GradArgs *a) {
     if (!g) return fail(ALOCO_ERR_ARG, "NULL gradient list");
     if (!norm) return fail(ALOCO_ERR_ARG, "NULL norm");
     if ((uintptr_t)norm & 3) return fail(ALOCO_ERR_ARG, "norm: not aligned to 4 bytes");
@@ -491,14 +507,39 @@ int check_list(const aloco_grads_t *g, const float *norm) {
     if (device != g->device)
         return fail(ALOCO_ERR_ARG, "the gradient list lives on device %d, current device is %d",
                     g->device, device);
-    return aloco::check_buffer(norm, 4, device, "norm");
+    if (hits(g, norm, 4)) return fail(ALOCO_ERR_ALIAS, "norm overlaps a gradient");
+    if ((rc = (*check)(norm, 4, device, "norm")) != ALOCO_OK) return rc;
+    if (scratch) {
+        if (scratch_bytes < g->scratch_bytes)
+            return fail(ALOCO_ERR_ARG, "scratch of %zu bytes, need %zu", scratch_bytes,
+                        g->scratch_bytes);
+        if ((uintptr_t)scratch & 15)
+            return fail(ALOCO_ERR_ARG, "scratch: not aligned to 16 bytes");
+        if (meet(norm, 4, scratch, g->scratch_bytes))
+            return fail(ALOCO_ERR_ALIAS, "scratch and norm overlap");
+        if (hits(g, scratch, g->scratch_bytes))
+            return fail(ALOCO_ERR_ALIAS, "scratch overlaps a gradient");
+        if ((rc = (*check)(scratch, g->scratch_bytes, device, "scratch")) != ALOCO_OK) return rc;
+    } else {
+        scratch = g->scratch;
+    }
+    *a = g->args;
+    a->norm = norm;
+    a->ticket = static_cast<unsigned int *>(scratch);
+    a->factor = static_cast<float *>(scratch) + 1;
+    a->partials = reinterpret_cast<aloco::GradPartial *>(static_cast<char *>(scratch) + 16);
+    return ALOCO_OK;
 }
 
-bool hits(const aloco_grads_t *g, const void *p, size_t bytes) {
-    const uintptr_t a = (uintptr_t)p, b = a + bytes;
-    for (const auto &r : g->ranges)
-        if (a < r.second && r.first < b) return true;
-    return false;
+// The norm's kernel.  The handle's own scratch, which calls that overlapped may
+// have left with a count, begins anew in every call.
+cudaError_t launch_norm(const aloco_grads_t *g, const aloco::GradArgs &a, bool own_scratch,
+                        cudaStream_t stream) {
+    if (own_scratch) {
+        const cudaError_t e = cudaMemsetAsync(a.ticket, 0, sizeof *a.ticket, stream);
+        if (e != cudaSuccess) return e;
+    }
+    return aloco::launch_grad_norm(a, g->sm_count, stream);
 }
 
 }  // namespace
@@ -542,23 +583,31 @@ void aloco_grads_destroy(aloco_grads_t *g) {
     delete g;
 }
 
-int aloco_grad_norm(aloco_grads_t *g, float *norm, const aloco_opts_t *opts) {
-    const int rc = check_list(g, norm);
+size_t aloco_grads_scratch_bytes(const aloco_grads_t *g) { return g ? g->scratch_bytes : 0; }
+
+int aloco_grad_norm_in(aloco_grads_t *g, float *norm, void *scratch, size_t scratch_bytes,
+                       const aloco_opts_t *opts) {
+    aloco::GradArgs a;
+    RangeCheck check;
+    const int rc = take_list(g, norm, scratch, scratch_bytes, &check, &a);
     if (rc != ALOCO_OK) return rc;
-    if (hits(g, norm, 4)) return fail(ALOCO_ERR_ALIAS, "norm overlaps a gradient");
-    aloco::GradArgs a = g->args;
-    a.norm = norm;
-    const cudaError_t e = aloco::launch_grad_norm(a, g->sm_count, stream_of(opts));
+    const cudaError_t e = launch_norm(g, a, !scratch, stream_of(opts));
     return e == cudaSuccess ? done() : cuda_fail(e, "gradient norm");
 }
 
-int aloco_clip_grads(aloco_grads_t *g, double max_norm, void *out, aloco_dtype out_dtype,
-                     float *norm, const aloco_opts_t *opts) {
-    int rc = check_list(g, norm);
+int aloco_grad_norm(aloco_grads_t *g, float *norm, const aloco_opts_t *opts) {
+    return aloco_grad_norm_in(g, norm, nullptr, 0, opts);
+}
+
+int aloco_clip_grads_in(aloco_grads_t *g, double max_norm, void *out, aloco_dtype out_dtype,
+                        float *norm, void *scratch, size_t scratch_bytes,
+                        const aloco_opts_t *opts) {
+    aloco::GradArgs a;
+    RangeCheck check;
+    int rc = take_list(g, norm, scratch, scratch_bytes, &check, &a);
     if (rc != ALOCO_OK) return rc;
     if (!(std::isfinite((float)max_norm) && (float)max_norm > 0.f))
         return fail(ALOCO_ERR_ARG, "max_norm = %g must be finite and > 0 in fp32", max_norm);
-    if (hits(g, norm, 4)) return fail(ALOCO_ERR_ALIAS, "norm overlaps a gradient");
     if (!out && g->overlap)
         return fail(ALOCO_ERR_ALIAS, "gradients overlap one another: they cannot be clipped "
                                      "in place");
@@ -568,19 +617,23 @@ int aloco_clip_grads(aloco_grads_t *g, double max_norm, void *out, aloco_dtype o
         const size_t size = out_dtype == ALOCO_F32 ? 4 : 2, bytes = (size_t)g->total * size;
         if ((uintptr_t)out & (size - 1))
             return fail(ALOCO_ERR_ARG, "out: not aligned to its element");
-        if ((uintptr_t)norm < (uintptr_t)out + bytes && (uintptr_t)out < (uintptr_t)norm + 4)
-            return fail(ALOCO_ERR_ALIAS, "out and norm overlap");
+        if (meet(norm, 4, out, bytes)) return fail(ALOCO_ERR_ALIAS, "out and norm overlap");
+        if (scratch && meet(scratch, g->scratch_bytes, out, bytes))
+            return fail(ALOCO_ERR_ALIAS, "out and scratch overlap");
         if (hits(g, out, bytes)) return fail(ALOCO_ERR_ALIAS, "out overlaps a gradient");
-        if ((rc = aloco::check_buffer(out, bytes, g->device, "out")) != ALOCO_OK) return rc;
+        if ((rc = check(out, bytes, g->device, "out")) != ALOCO_OK) return rc;
     }
-    aloco::GradArgs a = g->args;
-    a.norm = norm;
     a.max_norm = (float)max_norm;
     a.out = out;
     a.out_bf16 = out_dtype == ALOCO_BF16;
-    cudaError_t e = aloco::launch_grad_norm(a, g->sm_count, stream_of(opts));
+    cudaError_t e = launch_norm(g, a, !scratch, stream_of(opts));
     if (e == cudaSuccess) e = aloco::launch_grad_scale(a, g->sm_count, stream_of(opts));
     return e == cudaSuccess ? done() : cuda_fail(e, "gradient clipping");
+}
+
+int aloco_clip_grads(aloco_grads_t *g, double max_norm, void *out, aloco_dtype out_dtype,
+                     float *norm, const aloco_opts_t *opts) {
+    return aloco_clip_grads_in(g, max_norm, out, out_dtype, norm, nullptr, 0, opts);
 }
 
 }  // extern "C"
