@@ -1027,6 +1027,12 @@ class _Owned:
         return False
 
 
+# Handles of lists that are gone.  Freeing one waits for the device, which no
+# stream that is being captured allows, and a list may be collected at any moment;
+# they go when the next list is made, which waits for the device anyway.
+_dropped_lists = []
+
+
 class GradList:
     """The gradient tensors of one model (contiguous float32 or bfloat16 CUDA
     tensors of one device, in the order of the flat vector), kept for
@@ -1057,6 +1063,8 @@ class GradList:
         self.numel = sum(sizes)
         handle = ctypes.c_void_p()
         with _on_device(self.device):
+            while _dropped_lists:
+                load().aloco_grads_destroy(_dropped_lists.pop())
             rc = load().aloco_grads_create(
                 (ctypes.c_void_p * n)(*self._at), (ctypes.c_int64 * n)(*sizes),
                 (ctypes.c_int32 * n)(*[_replica_dtype_code(t) for t in self.tensors]), n,
@@ -1088,8 +1096,8 @@ class GradList:
                              "set_to_none=False): make a new GradList")
 
     def __del__(self):
-        if getattr(self, "_handle", None) is not None and _lib is not None:
-            _lib.aloco_grads_destroy(self._handle)
+        if getattr(self, "_handle", None) is not None and _dropped_lists is not None:
+            _dropped_lists.append(self._handle)
             self._handle = None
 
 

@@ -2,6 +2,7 @@
 GPU keep apart, as Python calls (which bring scratch of their own) and through
 the C entry points that take scratch."""
 import ctypes
+import gc
 
 import pytest
 import torch
@@ -106,3 +107,30 @@ def test_the_entry_points_with_scratch():
     host = torch.zeros(need + 16, dtype=torch.uint8)
     assert clip(out.data_ptr(), (host.data_ptr() + 15) // 16 * 16, need) != A.OK
     assert clip(out.data_ptr(), at, need) == A.OK
+
+
+def test_lists_dropped_while_a_graph_is_captured():
+    """Also one that only the collector finds: the capture goes on, the graph is
+    right, and the memory goes back when another list is made."""
+    g = A.GradList(_tensors([4000, 9], 4))
+    want = A.grad_norm(g)
+    for cycle in (False, True):
+        other = A.GradList(_tensors([500], 5))
+        A.grad_norm(other)
+        if cycle:
+            other.itself = other
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        gc.collect()
+        with torch.cuda.graph(graph):
+            norm = A.grad_norm(g)
+            del other
+            gc.collect()
+            again = A.grad_norm(g)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(norm, want) and torch.equal(again, want)
+    assert A._dropped_lists
+    assert torch.equal(A.grad_norm(A.GradList(g.tensors)), want)
+    del g
+    gc.collect()
