@@ -1046,6 +1046,7 @@ class GradList:
     def __init__(self, tensors):
         import torch
         self._handle = None
+        self._captured = False   # a graph reads the handle's table: it stays
         self.tensors = list(tensors)
         if not self.tensors:
             raise ValueError("need at least one gradient")
@@ -1080,6 +1081,7 @@ class GradList:
         stream, whose calls follow one another.  A captured call has its own,
         zeroed at every replay, which may run beside any other call."""
         if _torch.cuda.is_current_stream_capturing():
+            self._captured = True
             return _torch.zeros(self._need, dtype=_torch.uint8, device=self.device)
         s = self._kept.get(stream)
         if s is None:
@@ -1097,7 +1099,8 @@ class GradList:
 
     def __del__(self):
         if getattr(self, "_handle", None) is not None and _dropped_lists is not None:
-            _dropped_lists.append(self._handle)
+            if not self._captured:
+                _dropped_lists.append(self._handle)
             self._handle = None
 
 

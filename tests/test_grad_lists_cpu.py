@@ -79,6 +79,29 @@ def test_a_list_that_is_collected_does_not_touch_the_device(lib):
     del d
 
 
+def test_the_table_of_a_captured_call_is_never_freed(lib, monkeypatch):
+    """A graph reads it at every replay, whether or not the list is still there."""
+    import torch
+    lib.aloco_grad_norm_in = lambda *a: A.OK
+    capturing = [False]
+    monkeypatch.setattr(A, "_torch", torch)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    cpu = lambda f: lambda *a, **k: f(*a, **{**k, "device": "cpu"})
+    monkeypatch.setattr(torch, "zeros", cpu(torch.zeros))
+    monkeypatch.setattr(torch, "empty", cpu(torch.empty))
+    monkeypatch.setattr(A, "_on_stream", lambda stream, device, inputs: (A._NO_SWITCH, 0))
+    lists = []
+    for capturing[0] in (False, True):
+        lists.append(A.GradList([_Tensor()]))
+        A.grad_norm(lists[-1])
+    capturing[0] = False
+    A.grad_norm(lists[-1])
+    del lists[:]
+    gc.collect()
+    A.GradList([_Tensor()])
+    assert lib.destroyed == [1]
+
+
 def test_a_list_that_was_not_made_leaves_nothing(lib, monkeypatch):
     monkeypatch.setattr(A, "last_error", lambda: "refused")
     lib.aloco_grads_create = lambda *a: A.ERR_ARG
