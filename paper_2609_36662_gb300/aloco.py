@@ -842,6 +842,13 @@ def _finish(rc, ctx, *outputs):
                 t.record_stream(ctx.current)
 
 
+def _written(tensors):
+    """Tell autograd that a call has written into the caller's tensors (or
+    tensor): a backward pass that saved one of them is refused then, as after an
+    in-place operation of torch's own."""
+    _torch.autograd.graph.increment_version(tensors)
+
+
 _torch = None
 
 
@@ -961,6 +968,8 @@ def policy_loss(logits, targets, advantages, old_logp, weights, *, ref_logp=None
                                    terms.data_ptr(), logp.data_ptr(), desc, scratch.data_ptr(),
                                    need, ctypes.byref(Opts(stream=handle)))
     _finish(rc, ctx, terms, logp, out)
+    if grad is not None:
+        _written(grad)
     return PolicyLoss(terms, logp, out)
 
 
@@ -1004,6 +1013,8 @@ def preference_loss(logits, targets, cu_seqlens, ref_logp=None, *, beta: float =
             loss.data_ptr(), ratios.data_ptr(), logp.data_ptr(), desc, scratch.data_ptr(), need,
             ctypes.byref(Opts(stream=handle)))
     _finish(rc, ctx, loss, ratios, logp, out)
+    if grad is not None:
+        _written(grad)
     return PreferenceLoss(loss, ratios, logp, out)
 
 
@@ -1014,16 +1025,17 @@ class _Owned:
     then."""
 
     def __init__(self, tensors):
-        self._take(t for t in tensors if not t.is_inference())
+        self.seen = [(t, 0) for t in tensors if not t.is_inference()]
+        self.take()
 
-    def _take(self, tensors):
+    def take(self):
         """Those that are owned now, with their versions."""
-        self.seen = [(t, t._version) for t in tensors if t._use_count() > 1]
+        self.seen = [(t, t._version) for t, _ in self.seen if t._use_count() > 1]
 
     def stale(self) -> bool:
         if any(t._use_count() == 1 and t._version == v for t, v in self.seen):
             return True
-        self._take([t for t, _ in self.seen])
+        self.take()
         return False
 
 
@@ -1145,4 +1157,9 @@ def clip_grads(grads, max_norm: float, *, out=None, stream=None):
                                         norm.data_ptr(), g._scratch(handle).data_ptr(), g._need,
                                         ctypes.byref(Opts(stream=handle)))
     _finish(rc, ctx, norm)
+    if out is not None:
+        _written(out)
+    else:
+        _written(g.tensors)
+        g._owned.take()
     return norm

@@ -102,3 +102,72 @@ def test_tensors_that_the_caller_keeps_and_gradients_taken_over():
     lst = A.GradList(taken)
     for _ in range(2):
         assert float(A.grad_norm(lst)) == pytest.approx(want, rel=1e-5)
+
+
+@pytest.mark.parametrize("loss", ["policy", "preference"])
+def test_autograd_sees_that_the_logits_were_overwritten(loss):
+    """Where the operation before the logits saved its result, a backward pass
+    through it is refused after the gradient went over the logits."""
+    h = torch.randn(4, 300, device="cuda", requires_grad=True)
+    t = torch.randint(0, 300, (4,), device="cuda")
+    f = torch.ones(4, device="cuda")
+    cu = torch.tensor([0, 2, 4], device="cuda")
+
+    def step(over):
+        capped = torch.tanh(h)
+        kw = {"grad": capped} if over else {}
+        if loss == "policy":
+            r = A.policy_loss(capped, t, f, -5 * f, f / 4, **kw)
+        else:
+            r = A.preference_loss(capped, t, cu, **kw)
+        return capped, r.grad
+
+    capped, g = step(False)
+    capped.backward(g)
+    assert bool(h.grad.any())
+    capped, g = step(True)
+    assert g.data_ptr() == capped.data_ptr()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        capped.backward(g.detach().clone())
+
+
+def test_what_is_written_counts_as_written():
+    """Version counters move with every tensor that a call writes into, and with
+    no other."""
+    x = torch.randn(4, 300, device="cuda")
+    t = torch.randint(0, 300, (4,), device="cuda")
+    f = torch.ones(4, device="cuda")
+    cu = torch.tensor([0, 2, 4], device="cuda")
+    into = torch.empty_like(x)
+    flat = torch.empty(2400, device="cuda")
+    lst = A.GradList([x, into])
+    seen = [x, t, f, cu, into, flat]
+    for call, written in (
+            (lambda: A.token_logprobs(x, t), []),
+            (lambda: A.policy_loss(x, t, f, f, f), []),
+            (lambda: A.policy_loss(x, t, f, f, f, grad=into), [into]),
+            (lambda: A.policy_loss(x, t, f, f, f, grad=x), [x]),
+            (lambda: A.preference_loss(x, t, cu, grad=into), [into]),
+            (lambda: A.preference_loss(x, t, cu, grad=x), [x]),
+            (lambda: A.grad_norm(lst), []),
+            (lambda: A.clip_grads(lst, 1.0, out=flat), [flat]),
+            (lambda: A.clip_grads(lst, 1.0), [x, into])):
+        before = [v._version for v in seen]
+        call()
+        moved = [v for v, b in zip(seen, before) if v._version > b]
+        assert [id(v) for v in moved] == [id(v) for v in written]
+
+
+def test_inference_tensors():
+    """They have no version counter, and are taken as before."""
+    with torch.inference_mode():
+        x = torch.randn(4, 300, device="cuda")
+        t = torch.randint(0, 300, (4,), device="cuda")
+        f = torch.ones(4, device="cuda")
+        want = A.policy_loss(x, t, f, f, f).grad.clone()
+        assert torch.equal(A.policy_loss(x, t, f, f, f, grad=x).grad, want)
+        lst = A.GradList([x])
+        flat = torch.empty(1200, device="cuda")
+        A.clip_grads(lst, 1.0, out=flat)
+        A.clip_grads(lst, 1.0)
+        assert torch.equal(x.reshape(-1), flat)
