@@ -55,7 +55,7 @@ __device__ __forceinline__ void wait_for_previous() {
 // What a row kernel leaves: log-probabilities, also a gradient, the same where
 // the gradient's rows may lie otherwise to the 16-byte boundaries than the
 // logits' do, what the preference loss needs of a row, or its gradient.
-// (kPolicySmall: see last_to_come.)
+// (kPolicySmall: see finishes.)
 constexpr int kFwd = 0, kPolicy = 1, kPolicyShifted = 2, kPref = 3, kGrad = 4, kGradShifted = 5,
               kPolicySmall = 6;
 constexpr bool is_policy(int mode) {
@@ -545,22 +545,21 @@ __device__ __forceinline__ void give_up(const LogitsArgs &a, int64_t row) {
     }
 }
 
-// Whether this cluster, by the consumers of its first CTA (barrier 1), is the
-// last of the grid to come here, and so finishes the call (aloco_marks.cuh).  In
-// a small call a second kernel for that takes 3 us of the host's time, which
-// such calls are made of (48 rows of 32000: 29 -> 24 us).  A large call has the
-// second kernel, which the next call overlaps (8 x 1023 x 32000 bf16: 162 us, 167
-// in one kernel).  (Not inlined: the row kernel's registers are the rows'.)
+__device__ __forceinline__ Marks marks_of(const LogitsArgs &a, int clusters) {
+    return {reinterpret_cast<char *>(&a.parts->mark), (int)sizeof(PolicyPart), clusters, a.claim,
+            a.mark};
+}
+// Whether this cluster, by the consumers of its first CTA, is the one that
+// finishes a small call (aloco_marks.cuh).  A second kernel for that takes 3 us of
+// the host's time, which such calls are made of (48 rows of 32000: 29 -> 24 us).
+// A large call has the second kernel, which the next call overlaps (8 x 1023 x
+// 32000 bf16: 162 us, 167 in one kernel).  (Not inlined: the row kernel's
+// registers are the rows'.)
 template <int THREADS>
-__device__ __noinline__ bool last_to_come(const LogitsArgs &a, int cluster, int clusters,
-                                          int tid) {
-    char *const marks = reinterpret_cast<char *>(&a.parts->mark);
-    if (tid == 0) leave_mark(&a.parts[cluster].mark, a.mark);
-    sync_threads<THREADS>();
-    const bool last = all_of<THREADS>(
-        marks_here<THREADS>(marks, sizeof(PolicyPart), clusters, a.mark, tid));
-    if (last) take_marks<THREADS>(marks, sizeof(PolicyPart), clusters, tid);
-    return last;
+__device__ __noinline__ bool finishes(const LogitsArgs &a, int cluster, int clusters, int tid) {
+    return last_to_come<THREADS>(marks_of(a, clusters), cluster, tid,
+                                 [] { sync_threads<THREADS>(); },
+                                 [](bool b) { return all_of<THREADS>(b); });
 }
 
 // Sums of up to 32 lanes, in every lane.
@@ -1139,13 +1138,13 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
                 PolicyPart *const p = a.parts + row0;
                 for (int j = 0; j < kTerms; ++j) p->term[j] = terms[j].value();
             }
-            if (MODE != kPolicy && a.finish && rank == 0 &&
-                last_to_come<THREADS>(a, (int)row0, (int)step, tid))
-                add_parts<THREADS>(a, (int)step, tid, s_sums);
         }
-        if (MODE == kPref && a.finish && rank == 0 &&
-            last_to_come<THREADS>(a, (int)row0, (int)step, tid))
-            all_pairs<THREADS>(a, tid, s_sums);
+        if ((MODE == kPolicySmall || MODE == kPolicyShifted || MODE == kPref) && a.finish &&
+            rank == 0 && finishes<THREADS>(a, (int)row0, (int)step, tid)) {
+            if constexpr (is_policy(MODE)) add_parts<THREADS>(a, (int)step, tid, s_sums);
+            if constexpr (MODE == kPref) all_pairs<THREADS>(a, tid, s_sums);
+            if (tid == 0) give_back(marks_of(a, (int)step));
+        }
     }
     // no CTA leaves while another may still write to its memory
     if (C > 1)

@@ -47,6 +47,7 @@ struct LogitsArgs {
     float2 *stats;                   // [n] row maximum and 1 / sum (scratch)
     float *coef;                     // [n] dL/dlogp (scratch)
     unsigned int *ticket;            // blocks of the pairs' kernel that are done (scratch)
+    unsigned long long *claim;       // of the sum in a small call (scratch)
     float *loss, *ratios;
     int stages, cluster, per;        // the row kernel: ring slots, CTAs of a
                                      // cluster, units of a CTA's part at most

@@ -237,19 +237,27 @@ int take_grad(const aloco_tokens_t *t, const aloco_logits_grad_t *g, aloco::Logi
     return ALOCO_OK;
 }
 
-int take_scratch(void *scratch, size_t bytes, aloco::LogitsArgs *a, Buffers *s) {
-    const size_t need = aloco_loss_scratch_bytes(a->n);
-    if (bytes < need)
-        return fail(ALOCO_ERR_ARG, "scratch of %zu bytes, need %zu", bytes, need);
-    s->add("scratch", scratch, need, 16, true);
-    return ALOCO_OK;
-}
-
 // Another value for every call: odd times odd, so never 0, and one that memory
 // hardly holds by chance.
 unsigned long long new_mark() {
     static std::atomic<unsigned long long> calls{0};
     return (2 * calls.fetch_add(1, std::memory_order_relaxed) + 1) * 0x9e3779b97f4a7c15ull;
+}
+
+int take_scratch(void *scratch, size_t bytes, aloco::LogitsArgs *a, Buffers *s) {
+    const size_t need = aloco_loss_scratch_bytes(a->n);
+    if (bytes < need)
+        return fail(ALOCO_ERR_ARG, "scratch of %zu bytes, need %zu", bytes, need);
+    s->add("scratch", scratch, need, 16, true);
+    a->parts = static_cast<aloco::PolicyPart *>(scratch);
+    a->stats = reinterpret_cast<float2 *>(a->parts + a->n);
+    a->coef = reinterpret_cast<float *>(a->stats + a->n);
+    // (of the last 16 bytes, 8 from where 8 divides the address)
+    a->claim = reinterpret_cast<unsigned long long *>(
+        ((uintptr_t)(a->coef + a->n) + 7) & ~(uintptr_t)7);
+    a->ticket = reinterpret_cast<unsigned int *>(a->claim);
+    a->mark = new_mark();
+    return ALOCO_OK;
 }
 
 constexpr int64_t kMostLate = 8000000000;  // cycles, 4 s
@@ -269,7 +277,7 @@ extern "C" {
 
 size_t aloco_loss_scratch_bytes(int64_t rows) {
     if (rows <= 0) return 0;
-    // a cluster's part, a row's maximum and sum, its coefficient; a ticket
+    // a cluster's part, a row's maximum and sum, its coefficient; a ticket or claim
     return (size_t)rows * (sizeof(aloco::PolicyPart) + sizeof(float2) + sizeof(float)) + 16;
 }
 
@@ -326,8 +334,6 @@ int aloco_policy_loss(const aloco_tokens_t *tokens, const float *advantages,
     a.kl = (float)cfg->kl_coef;
     a.logp = logp;
     a.terms_out = terms;
-    a.parts = static_cast<aloco::PolicyPart *>(scratch);
-    a.mark = new_mark();
     int sms;
     if ((rc = check_buffers(s, over, &sms)) != ALOCO_OK) return rc;
     take_stall(&a);
@@ -375,11 +381,6 @@ int aloco_preference_loss(const aloco_tokens_t *tokens, const float *ref_logp,
     a.loss = loss;
     a.ratios = log_ratios;
     a.logp = logp;
-    a.parts = static_cast<aloco::PolicyPart *>(scratch);
-    a.stats = reinterpret_cast<float2 *>(a.parts + a.n);
-    a.coef = reinterpret_cast<float *>(a.stats + a.n);
-    a.ticket = reinterpret_cast<unsigned int *>(a.coef + a.n);
-    a.mark = new_mark();
     int sms;
     if ((rc = check_buffers(s, over, &sms)) != ALOCO_OK) return rc;
     take_stall(&a);

@@ -5,56 +5,67 @@
 // at the marks of all.  Between the two stands a sequentially consistent fence:
 // of two blocks at least one sees the other's mark, so the last one sees all of
 // them.  No block waits for another, whatever is resident and however late a
-// block comes.  Blocks that come at the same time may each see all marks; they
-// then add the same parts in the same order and write the same values.  Who has
-// seen all takes them away, so that a captured call, whose mark is the same at
-// every replay, finds none of its own.
+// block comes.  Of the blocks that see all marks (those that come at the same
+// time may), the first to claim the sum does it, and takes the marks away: a
+// captured call, whose mark is the same at every replay, finds none of its own.
+// A claim is given back at the end, for the same reason; a block that claims
+// after that adds the same parts once more and writes the same values.
+// (A policy call of 1216 rows of 40 in as many blocks: 16 us; 72 with a sum by
+// every block that sees all marks; 31 with a block that waits for the others.)
 #pragma once
 
 #include <cuda_runtime.h>
 
 namespace aloco {
 
-// By the thread that has written the block's part (or behind a barrier that
-// others of the block have written theirs before).
-__device__ __forceinline__ void leave_mark(unsigned long long *p, unsigned long long mark) {
-    __threadfence();  // the part is there before the mark is
-    asm volatile("st.relaxed.gpu.global.u64 [%0], %1;" ::"l"(p), "l"(mark) : "memory");
-    __threadfence();  // and the mark before the block looks at the others
-}
+struct Marks {
+    char *first;                 // n of them, `stride` bytes apart
+    int stride, n;
+    unsigned long long *claim;
+    unsigned long long mark;     // this call's, never 0
+};
 
-// Whether this thread's share of n marks, `stride` bytes apart, is there: tid
-// and every THREADS-th after it.  Behind a barrier after leave_mark; a block
-// may read the parts when all its threads have said yes at another barrier.
-template <int THREADS>
-__device__ __forceinline__ bool marks_here(const char *first, int stride, int n,
-                                           unsigned long long mark, int tid) {
+// Whether the block that came as `own` is the one to add the parts.  By THREADS
+// threads; the block's part is thread 0's writes.  sync() is their barrier,
+// all(b) one that says whether b holds in all of them.
+template <int THREADS, typename Sync, typename All>
+__device__ __forceinline__ bool last_to_come(const Marks &m, int own, int tid, Sync sync,
+                                             All all) {
+    if (tid == 0) {
+        asm volatile("fence.acq_rel.gpu;" ::: "memory");  // the part before the mark
+        asm volatile("st.relaxed.gpu.global.u64 [%0], %1;" ::"l"(m.first + (size_t)own * m.stride),
+                     "l"(m.mark)
+                     : "memory");
+        asm volatile("fence.sc.gpu;" ::: "memory");  // the mark before the look at the others
+    }
+    sync();
     constexpr int kAtOnce = 4;
-    for (int c = tid; c < n; c += kAtOnce * THREADS) {
-        unsigned long long m[kAtOnce];
+    bool here = true;
+    for (int c = tid; here && c < m.n; c += kAtOnce * THREADS) {
+        unsigned long long got[kAtOnce];
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k) {
-            m[k] = mark;
-            if (c + k * THREADS < n)
+            got[k] = m.mark;
+            if (c + k * THREADS < m.n)
                 asm volatile("ld.relaxed.gpu.global.u64 %0, [%1];"
-                             : "=l"(m[k])
-                             : "l"(first + (size_t)(c + k * THREADS) * stride)
+                             : "=l"(got[k])
+                             : "l"(m.first + (size_t)(c + k * THREADS) * m.stride)
                              : "memory");
         }
 #pragma unroll
-        for (int k = 0; k < kAtOnce; ++k)
-            if (m[k] != mark) return false;
+        for (int k = 0; k < kAtOnce; ++k) here = here && got[k] == m.mark;
     }
-    __threadfence();  // the marks before the parts
+    if (!all(here)) return false;
+    asm volatile("fence.acq_rel.gpu;" ::: "memory");  // the marks before the parts
+    if (!all(tid != 0 || atomicExch(m.claim, m.mark) != m.mark)) return false;
+    for (int c = tid; c < m.n; c += THREADS)
+        asm volatile("st.relaxed.gpu.global.u64 [%0], %1;" ::"l"(m.first + (size_t)c * m.stride),
+                     "l"(0ull)
+                     : "memory");
     return true;
 }
 
-template <int THREADS>
-__device__ __forceinline__ void take_marks(char *first, int stride, int n, int tid) {
-    for (int c = tid; c < n; c += THREADS)
-        asm volatile("st.relaxed.gpu.global.u64 [%0], %1;" ::"l"(first + (size_t)c * stride),
-                     "l"(0ull)
-                     : "memory");
-}
+// By one thread of that block, at the end.
+__device__ __forceinline__ void give_back(const Marks &m) { atomicExch(m.claim, 0ull); }
 
 }  // namespace aloco
