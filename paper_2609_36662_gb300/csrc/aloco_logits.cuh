@@ -704,6 +704,29 @@ __device__ __noinline__ void all_pairs(const LogitsArgs &a, int tid, float2 (*sh
     mean_of_pairs<THREADS>(a, tid, sh);
 }
 
+// Testing only: whether block 0 leaves out the copy of its slot number `slot`;
+// the first one may come late.  Where it is too late for its row, that row's
+// log-probability is 0 until the copy has landed.
+template <int MODE>
+__device__ __noinline__ bool stalls(const LogitsArgs &a, unsigned slot) {
+    if (a.test_stall1 < 0 && slot == 0) {
+        for (const long long t0 = clock64(); clock64() - t0 < -a.test_stall1;) {}
+        a.logp[row_at<MODE>(a, 0)] = 0.f;
+    }
+    return slot + 1 == a.test_stall1;
+}
+
+// Wait, by the producer's warp, for the last copies into a ring whose slots were
+// armed `filled` times.
+template <int MODE>
+__device__ __noinline__ void land(const LogitsArgs &a, const uint64_t *full, unsigned filled,
+                                  int stages) {
+    bool landed = true;
+    for (unsigned k = filled > (unsigned)stages ? filled - stages : 0; k < filled; ++k)
+        landed &= mbar_wait(smem_addr(full + k % stages), k / stages & 1, nullptr);
+    if (a.test_stall1 < 0 && !blockIdx.x && landed) a.logp[row_at<MODE>(a, 0)] = NAN;  // see stalls
+}
+
 // THREADS consumers and one producer warp.  CTA c of a cluster holds its part
 // of a row in the registers of its consumers: thread t the units k * THREADS +
 // t of the part, k < UPT.  A slot of the ring is DEPTH units of every thread.
@@ -722,6 +745,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
     __shared__ float2 s_sums[is_policy(MODE) ? kTerms : MODE == kPref ? 2 : 1][WARPS];
     __shared__ __align__(8) float2 s_cta[2][kMaxCluster];
     __shared__ volatile int s_abort, s_bad[2];
+    __shared__ unsigned s_filled;
 
     const cg::cluster_group cluster = cg::this_cluster();
     const int C = a.cluster, rank = (int)(blockIdx.x % (unsigned)C);
@@ -759,6 +783,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
         unsigned filled = 0;
         bool ok = true, again = false;
         unsigned mixed = 0;  // slots that hold stores of this warp's
+        const bool tested = a.test_stall1 != 0 && blockIdx.x == 0;
         unsigned char *const zeros = ring + (size_t)stages * SLOT * 16;
         if (writes_grad(MODE) && a.g.data) {
             for (int i = lane; i < ZEROS / 16; i += 32)
@@ -872,10 +897,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
                         if (lane == 0) {
                             const uint32_t bytes = hi > lo ? (uint32_t)(hi - lo) * 16 : 0;
                             mbar_arrive_expect_tx(full, bytes);
-                            if (a.test_stall1 < 0 && !blockIdx.x && !filled)
-                                for (const long long t0 = clock64();
-                                     clock64() - t0 < -a.test_stall1;) {}
-                            if (bytes && (blockIdx.x || filled + 1 != a.test_stall1))
+                            if (bytes && !(tested && stalls<MODE>(a, filled)))
                                 bulk_load(smem_addr(at + (size_t)(lo - u0) * 16),
                                           x.base + (size_t)lo * 16, bytes, full);
                         }
@@ -890,20 +912,7 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
         // the zeros' source stays until their copies have read it
         if (writes_grad(MODE) && lane == 0) bulk_wait_all();
         if (!ok) s_abort = 1;
-        // No copy may land after the block has ended, whoever has given up: where
-        // all slots were free, this warp comes here without having waited, and
-        // the consumers may leave while the last copies are on their way.
-        bool landed = true;
-        for (unsigned k = 0; k < (unsigned)stages && k < filled; ++k) {
-            if (place.i == 0) {
-                place.i = stages;
-                place.phase ^= 1;
-            }
-            --place.i;
-            landed &= mbar_wait(smem_addr(&s_full[place.i]), place.phase, nullptr);
-        }
-        if (a.test_stall1 < 0 && !blockIdx.x && lane == 0 && !landed)  // testing only
-            a.logp[row_at<MODE>(a, row0)] = 0.f;
+        s_filled = filled;
     } else {
         const Scale scale = {a.scale, a.scale_lo};
         const f2 hi2 = pair(scale.hi, scale.hi), lo2 = pair(scale.lo, scale.lo);
@@ -1146,6 +1155,13 @@ __global__ void __launch_bounds__(THREADS + 32, CTAS)
             if (tid == 0) give_back(marks_of(a, (int)step));
         }
     }
+    // No copy may land after the block has ended, whoever has given up: where all
+    // slots were free the producer comes here without having waited, and the
+    // consumers may leave while the last copies are on their way.  (Only then:
+    // the producer's waiting here in every block cost 164 -> 169 us at 8 x 1023 x
+    // 32000 bf16.)
+    __syncthreads();
+    if (s_abort && tid >= THREADS) land<MODE>(a, s_full, s_filled, stages);
     // no CTA leaves while another may still write to its memory
     if (C > 1)
         cluster.sync();
