@@ -585,9 +585,11 @@ typedef struct aloco_policy_cfg {
  *   dL/dlogp = w [ -A r [r A <= clip(r) A] + kl_coef (1 - exp(d)) ]
  *   dL/dx_j  = dL/dlogp / tau ([j = a] - p_j)
  * terms[4]: L, sum w (-min(..)), sum w (exp(d) - d - 1) and the weight of the
- * rows whose ratio was clipped.  ref_logp may be NULL with kl_coef = 0 (the
- * KL sum is then 0).  grad may be NULL (terms and logp only).  scratch: at
- * least aloco_loss_scratch_bytes(batch * rows), 16-byte aligned. */
+ * rows whose ratio was clipped.  With kl_coef = 0 the KL sum is only reported,
+ * and may be infinite where L is not; ref_logp may be NULL then (the sum is 0).
+ * An r beyond fp32 counts 0 where A is 0.  grad may be NULL (terms and logp
+ * only).  scratch: at least aloco_loss_scratch_bytes(batch * rows), 16-byte
+ * aligned. */
 int aloco_policy_loss(const aloco_tokens_t *tokens, const float *advantages,
                       const float *old_logp, const float *ref_logp,
                       const float *weights, const aloco_policy_cfg_t *cfg,
@@ -606,6 +608,7 @@ typedef struct aloco_preference_cfg {
  *   R_i = sum over the sequence's rows that take part of logp - ref_logp
  *   z_k = beta (R_2k - R_2k+1)
  *   L   = mean_k [ -(1 - eps) log sigmoid(z_k) - eps log sigmoid(-z_k) ]
+ *         (a term whose factor is 0 is 0, also at an infinite margin)
  *   dL/dlogp = +-(beta / pairs) (sigmoid(z_k) - 1 + eps)
  *                                     (+ in the chosen, - in the rejected)
  * cu_seqlens is a device array [2 pairs + 1] of cu_bytes (4 or 8) byte

@@ -946,7 +946,9 @@ def policy_loss(logits, targets, advantages, old_logp, weights, *, ref_logp=None
     ref_logp are float32 of targets' shape; rows of weight 0 or a negative
     target take no part.  grad (optional) receives the gradient and may be
     `logits` itself; without it a new tensor does, unless want_grad is False.
-    Enqueues only."""
+    The terms are not part of an autograd graph: logits.backward(r.grad) goes on
+    from the gradient.  (A grad that is given counts as written in place: a
+    backward pass that needs what was there before is refused.)  Enqueues only."""
     tok = _tokens(logits, targets, temperature)
     device = logits.device
     shape, index = targets.shape, device.index
@@ -981,7 +983,8 @@ def preference_loss(logits, targets, cu_seqlens, ref_logp=None, *, beta: float =
     1]) bounds the sequences among the rows taken in order, chosen and rejected
     answers in turn; rows with a negative target (prompts, padding) take no
     part.  ref_logp is float32 of targets' shape (None: no reference).  grad
-    and want_grad as policy_loss.  Enqueues only."""
+    and want_grad as policy_loss, and so is the way on into a backward pass.
+    Enqueues only."""
     tok = _tokens(logits, targets, temperature)
     device = logits.device
     ref = _per_row("ref_logp", ref_logp, targets.shape, device.index) \
@@ -1033,6 +1036,8 @@ class _Owned:
         self.seen = [(t, t._version) for t, _ in self.seen if t._use_count() > 1]
 
     def stale(self) -> bool:
+        if not self.seen:
+            return False
         if any(t._use_count() == 1 and t._version == v for t, v in self.seen):
             return True
         self.take()
@@ -1053,7 +1058,8 @@ class GradList:
     moved is refused, and so is one that its owner has let go of since the list
     was made or last used, if nothing has written to it since (zero_grad() drops
     a parameter's gradient, and the next backward pass makes another; with
-    set_to_none=False it stays)."""
+    set_to_none=False it stays).  A graph that captured a call reads the
+    tensors at every replay; they have to stay as for any captured call."""
 
     def __init__(self, tensors):
         import torch
@@ -1089,16 +1095,18 @@ class GradList:
         self._kept = {}   # scratch by stream
 
     def _scratch(self, stream):
-        """Scratch of a call on `stream` (a raw handle, current): one for every
-        stream, whose calls follow one another.  A captured call has its own,
-        zeroed at every replay, which may run beside any other call."""
-        if _torch.cuda.is_current_stream_capturing():
-            self._captured = True
-            return _torch.zeros(self._need, dtype=_torch.uint8, device=self.device)
-        s = self._kept.get(stream)
+        """(tensor, address) of a call's scratch on `stream` (a raw handle, current):
+        one for every stream, whose calls follow one another.  A captured call has
+        its own, zeroed at every replay, which may run beside any other call."""
+        capturing = _torch.cuda.is_current_stream_capturing()
+        s = None if capturing else self._kept.get(stream)
         if s is None:
-            s = self._kept[stream] = _torch.zeros(self._need, dtype=_torch.uint8,
-                                                  device=self.device)
+            t = _torch.zeros(self._need, dtype=_torch.uint8, device=self.device)
+            s = t, t.data_ptr()
+            if capturing:
+                self._captured = True
+            else:
+                self._kept[stream] = s
         return s
 
     def _check(self):
@@ -1131,8 +1139,9 @@ def grad_norm(grads, *, stream=None):
     ctx, handle = _on_stream(stream, g.device, g.tensors)
     with ctx:
         norm = _torch.empty((), dtype=_torch.float32, device=g.device)
-        rc = load().aloco_grad_norm_in(g._handle, norm.data_ptr(), g._scratch(handle).data_ptr(),
-                                       g._need, ctypes.byref(Opts(stream=handle)))
+        _scratch, at = g._scratch(handle)
+        rc = load().aloco_grad_norm_in(g._handle, norm.data_ptr(), at, g._need,
+                                       ctypes.byref(Opts(stream=handle)))
     _finish(rc, ctx, norm)
     return norm
 
@@ -1142,7 +1151,7 @@ def clip_grads(grads, max_norm: float, *, out=None, stream=None):
     with `out` (a contiguous float32 or bfloat16 vector of all their elements),
     into it, tensor after tensor, as adamw_step takes them.  Returns the norm
     before clipping, a float32 scalar tensor.  Enqueues only (grads as
-    grad_norm takes them)."""
+    grad_norm takes them); what it writes counts as written in place."""
     g = _grad_list(grads)
     if out is not None and (out.numel() != g.numel or not out.is_contiguous() or
                             out.device != g.device):
@@ -1152,9 +1161,10 @@ def clip_grads(grads, max_norm: float, *, out=None, stream=None):
     ctx, handle = _on_stream(stream, g.device, g.tensors if out is None else [*g.tensors, out])
     with ctx:
         norm = _torch.empty((), dtype=_torch.float32, device=g.device)
+        _scratch, at = g._scratch(handle)
         rc = load().aloco_clip_grads_in(g._handle, max_norm,
                                         out.data_ptr() if out is not None else None, dtype,
-                                        norm.data_ptr(), g._scratch(handle).data_ptr(), g._need,
+                                        norm.data_ptr(), at, g._need,
                                         ctypes.byref(Opts(stream=handle)))
     _finish(rc, ctx, norm)
     if out is not None:
