@@ -21,9 +21,9 @@
 //
 // What bounds them is HBM, and for vocabularies of more than one CTA the
 // exchange within the cluster.  Whole calls, of the copy rate: policy 8 x 1023 x
-// 32000 bf16 without prompt rows 162 us, 0.95; 8 x 1000 x 128256 643 us, 0.89;
+// 32000 bf16 without prompt rows 164 us, 0.94; 8 x 1000 x 128256 644 us, 0.89;
 // log-probabilities 4 x 1023 x 128256 131 us, 0.89; preference 16 sequences to
-// 1024 x 32000 337 us, 0.85 of its bytes with the logits read twice.
+// 1024 x 32000 335 us, 0.86 of its bytes with the logits read twice.
 //
 // A row may start off a 16-byte boundary (odd vocabularies): the units are
 // those of the aligned window around it; whole ones are copied, and the two at
