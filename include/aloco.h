@@ -513,6 +513,91 @@ int aloco_adamw_step_normed(void *const *params, const void *const *grads,
                             aloco_adamw_stats_t *stats_out);
 
 /* ------------------------------------------------------------------------
+ * Orthogonalised updates: the inner step of matrices along the orthogonal
+ * factor of their momentum, beside aloco_adamw_step for everything else.
+ *
+ * The factor of a matrix U comes from a few odd polynomials that push the
+ * singular values of U / (||U||_F + eps) towards 1 (Newton-Schulz products):
+ *   X_0 = U / (||U||_F + eps),   A = X X^T,   X <- (a + b A + c A A) X
+ * with X transposed where U has more rows than columns.  The products run on
+ * the tensor cores: X is held as a pair of fp16 values (22 bits), A and b A + c
+ * A A in fp16 with their diagonals in fp32, sums in fp32.  The factor's error
+ * against exact steps is 2e-4 to 1.5e-3 of its norm.  A matrix that holds NaN or
+ * inf gives NaN throughout, and no other matrix is affected; zeros give zeros.
+ *
+ * The calls only enqueue on opts->stream (the other options do not apply) and
+ * allocate nothing on the device; results are bit-identical from call to call.
+ * Scratch is the caller's device memory, 256-byte aligned and not set up in any
+ * way: calls that may overlap on the GPU need their own.  Every wait inside the
+ * kernels is bounded (about 2 s); one that runs out leaves NaN in the matrix.
+ * ---------------------------------------------------------------------- */
+
+#define ALOCO_MAX_NS_STEPS 16
+#define ALOCO_MAX_SIDE 16384          /* of a matrix's smaller side          */
+#define ALOCO_MAX_LONG_SIDE 1048576   /* of its larger one                   */
+
+/* A matrix in a replica's vector: rows * cols elements from `offset` on, row
+ * by row. */
+typedef struct aloco_matrix {
+    int64_t offset;
+    int64_t rows, cols;               /* a matrix of no elements is skipped  */
+} aloco_matrix_t;
+
+/* How far a step goes: the factor times lr times */
+enum {
+    ALOCO_MUON_ADAMW = 0,   /* 0.2 sqrt(max(rows, cols)): as far as AdamW's  */
+    ALOCO_MUON_ASPECT = 1,  /* sqrt(max(1, rows / cols))                     */
+    ALOCO_MUON_UNIT = 2     /* 1                                             */
+};
+
+typedef struct aloco_muon_cfg {
+    double lr;              /* finite, >= 0                                  */
+    double momentum;        /* mu, in [0, 1)                                 */
+    double weight_decay;    /* decoupled, finite, >= 0                       */
+    double eps;             /* beside the norm, finite, > 0                  */
+    int32_t nesterov;       /* 1: U = g + mu b', 0: U = b'                   */
+    int32_t scale;          /* ALOCO_MUON_*                                  */
+    int32_t steps;          /* of the factor, in [1, ALOCO_MAX_NS_STEPS]     */
+    int32_t reserved;
+    double coefficients[ALOCO_MAX_NS_STEPS][3];  /* a, b, c of every step,
+                                                    each at most 100 in size */
+} aloco_muon_cfg_t;
+
+/* lr 4e-4, momentum 0.95 with nesterov, weight decay 0.1, eps 1e-7, the ADAMW
+ * scale, five steps of (3.4445, -4.7750, 2.0315). */
+void aloco_muon_default_cfg(aloco_muon_cfg_t *cfg);
+
+/* Bytes of scratch of a step over these matrices on M replicas (0 where an
+ * argument is out of range). */
+size_t aloco_muon_scratch_bytes(const aloco_matrix_t *matrices, int64_t n, int M);
+
+/* One step of n matrices on M <= ALOCO_MAX_WORKERS replicas, in place:
+ *   b' = mu b + g,   U = g + mu b' (or b'),   O = factor of U
+ *   x' = x - lr weight_decay x - lr scale O
+ * params[m] (N elements of param_dtype, fp32 or bf16, rounded to nearest even),
+ * grads[m] (grad_dtype, read only) and momentum[m] (fp32, updated) as
+ * aloco_adamw_step has them; what no matrix covers is neither read nor written.
+ * Matrices may not overlap, nor may updated buffers.  Returns ALOCO_OK,
+ * ALOCO_ERR_ARG / ALOCO_ERR_ALIAS before any device work, or ALOCO_ERR_CUDA. */
+int aloco_muon_step(void *const *params, const void *const *grads,
+                    float *const *momentum, size_t N, int M,
+                    aloco_dtype param_dtype, aloco_dtype grad_dtype,
+                    const aloco_matrix_t *matrices, int64_t n,
+                    const aloco_muon_cfg_t *cfg, void *scratch,
+                    size_t scratch_bytes, const aloco_opts_t *opts);
+
+/* Orthogonal factors of `batch` matrices of rows x cols elements (dtype fp32 or
+ * bf16; rows lie row_stride >= cols elements apart, matrices batch_stride >=
+ * rows * row_stride, or any whole number of elements for a batch of 1), in bf16
+ * and contiguous in `out`, which may not overlap x.  coefficients: [steps][3]
+ * host values. */
+size_t aloco_orthogonalize_scratch_bytes(int64_t batch, int64_t rows, int64_t cols);
+int aloco_orthogonalize(const void *x, int64_t batch, int64_t rows, int64_t cols,
+                        int64_t batch_stride, int64_t row_stride, aloco_dtype dtype,
+                        void *out, const double *coefficients, int32_t steps, double eps,
+                        void *scratch, size_t scratch_bytes, const aloco_opts_t *opts);
+
+/* ------------------------------------------------------------------------
  * Post-training losses.  The paper tunes a language model between its
  * synchronisations (UltraChat SFT, Tab. training settings) and takes the
  * gradients as given; these entry points are the losses of preference and
@@ -622,6 +707,40 @@ int aloco_preference_loss(const aloco_tokens_t *tokens, const float *ref_logp,
                           float *loss, float *log_ratios, float *logp,
                           const aloco_logits_grad_t *grad, void *scratch,
                           size_t scratch_bytes, const aloco_opts_t *opts);
+
+/* Log-probabilities of given tokens with what else a row of logits says: its
+ * entropy and its best alternatives.  For a row with a token >= 0 (others take
+ * no part and are not read: 0, and -1 as ids):
+ *   logp       log p[a]
+ *   entropy    H = -sum_j p_j log p_j  (terms with p_j = 0 are 0)
+ *   top_ids    the `top` largest logits' indices, largest first, equal ones by
+ *              their index; [batch * rows, top] int32
+ *   top_logp   their log-probabilities (-inf where the logit is)
+ *   stats      (largest logit, sum_j exp(y_j - largest y)), which
+ *              aloco_token_scores_grad takes; [batch * rows, 2]
+ * A row with NaN or +inf, or without a logit above -inf, has NaN and -1
+ * throughout; a token >= V has logp NaN alone.  top in [0, min(V,
+ * ALOCO_MAX_TOP)]; with 0 top_ids and top_logp are not looked at.  entropy
+ * may be NULL, and so may stats. */
+#define ALOCO_MAX_TOP 32
+int aloco_token_scores(const aloco_tokens_t *tokens, int32_t top, float *logp,
+                       float *entropy, int32_t *top_ids, float *top_logp,
+                       float *stats, const aloco_opts_t *opts);
+
+/* Gradient by the logits of a loss over token scores, from its gradients by
+ * them (any may be NULL: 0; d_top is [batch * rows, top]):
+ *   tau dL/dx_j = d_logp ([j = a] - p_j) + sum_i d_top_i ([j = top_ids_i] - p_j)
+ *                 - d_entropy p_j (log p_j + H)
+ * stats and entropy are those of aloco_token_scores on the same logits, targets
+ * and temperature (entropy may be NULL where d_entropy is).  top_ids may hold
+ * any indices, also one twice; what lies outside [0, V) takes no part.  Rows
+ * with a negative token get zeros and are not read; a token >= V gives NaN. */
+int aloco_token_scores_grad(const aloco_tokens_t *tokens, const float *stats,
+                            const float *entropy, const float *d_logp,
+                            const float *d_entropy, int32_t top,
+                            const int32_t *top_ids, const float *d_top,
+                            const aloco_logits_grad_t *grad,
+                            const aloco_opts_t *opts);
 
 /* ------------------------------------------------------------------------
  * Global gradient norm over many tensors, and clipping (Tab. training

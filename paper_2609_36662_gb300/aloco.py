@@ -15,6 +15,9 @@ from typing import NamedTuple, Optional, Sequence
 
 MAX_WORKERS = 32
 MAX_VOCAB = 262144
+MAX_TOP = 32
+MAX_NS_STEPS = 16
+MAX_SIDE, MAX_LONG_SIDE = 16384, 1048576
 
 F32, BF16 = 0, 1
 SCHED_COSINE, SCHED_CONSTANT, SCHED_LINEAR = 0, 1, 2
@@ -23,6 +26,7 @@ PASS_AUTO, PASS_REGISTERS, PASS_BULK_COPY = 0, 1, 2
 PASS_INT8_SPLIT, PASS_INT8_FUSED = 3, 4
 PASS_TILE = 5
 WAIT_SPIN, WAIT_BLOCK = 0, 1
+MUON_ADAMW, MUON_ASPECT, MUON_UNIT = 0, 1, 2
 
 OK = 0
 ERR_ARG = -1
@@ -41,6 +45,9 @@ EXPORTS = ("aloco_default_opts", "aloco_inner_lr_accum", "aloco_correction",
            "aloco_sync_int8", "aloco_int8_num_blocks", "aloco_int8_encode",
            "aloco_int8_decode", "aloco_adamw_default_cfg", "aloco_adamw_step",
            "aloco_adamw_step_normed",
+           "aloco_muon_default_cfg", "aloco_muon_scratch_bytes", "aloco_muon_step",
+           "aloco_orthogonalize_scratch_bytes", "aloco_orthogonalize",
+           "aloco_token_scores", "aloco_token_scores_grad",
            "aloco_token_logprobs", "aloco_loss_scratch_bytes", "aloco_policy_loss",
            "aloco_preference_loss", "aloco_grads_create", "aloco_grads_destroy",
            "aloco_grad_norm", "aloco_clip_grads", "aloco_grads_scratch_bytes",
@@ -96,6 +103,18 @@ class AdamwStats(ctypes.Structure):
         return {"grad_norm": list(self.grad_norm[:self.M]),
                 "clip": list(self.clip[:self.M]), "M": self.M,
                 "grid": self.grid, "kernel_ms": self.kernel_ms}
+
+
+class Matrix(ctypes.Structure):
+    _fields_ = [("offset", ctypes.c_int64), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
+
+
+class MuonCfg(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("momentum", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("eps", ctypes.c_double),
+                ("nesterov", ctypes.c_int32), ("scale", ctypes.c_int32),
+                ("steps", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("coefficients", ctypes.c_double * 3 * MAX_NS_STEPS)]
 
 
 class Tokens(ctypes.Structure):
@@ -302,6 +321,23 @@ def load():
     lib.aloco_grad_norm_in.restype = i32
     lib.aloco_clip_grads_in.argtypes = [vp, dbl, vp, i32, vp, vp, ctypes.c_size_t, P(Opts)]
     lib.aloco_clip_grads_in.restype = i32
+    lib.aloco_token_scores.argtypes = [P(Tokens), i32, vp, vp, vp, vp, vp, P(Opts)]
+    lib.aloco_token_scores.restype = i32
+    lib.aloco_token_scores_grad.argtypes = [P(Tokens), vp, vp, vp, vp, i32, vp, vp,
+                                            P(LogitsGrad), P(Opts)]
+    lib.aloco_token_scores_grad.restype = i32
+    lib.aloco_muon_default_cfg.argtypes = [P(MuonCfg)]
+    lib.aloco_muon_default_cfg.restype = None
+    lib.aloco_muon_scratch_bytes.argtypes = [P(Matrix), i64, i32]
+    lib.aloco_muon_scratch_bytes.restype = ctypes.c_size_t
+    lib.aloco_muon_step.argtypes = [vp, vp, vp, ctypes.c_size_t, i32, i32, i32, P(Matrix), i64,
+                                    P(MuonCfg), vp, ctypes.c_size_t, P(Opts)]
+    lib.aloco_muon_step.restype = i32
+    lib.aloco_orthogonalize_scratch_bytes.argtypes = [i64, i64, i64]
+    lib.aloco_orthogonalize_scratch_bytes.restype = ctypes.c_size_t
+    lib.aloco_orthogonalize.argtypes = [vp, i64, i64, i64, i64, i64, i32, vp, vp, i32, dbl, vp,
+                                        ctypes.c_size_t, P(Opts)]
+    lib.aloco_orthogonalize.restype = i32
     lib.aloco_sync_host.argtypes = sync_args + [ctypes.c_size_t, P(Opts), P(Stats)]
     lib.aloco_sync_host.restype = i32
     lib.aloco_sync_shard.argtypes = sync_args + [P(Opts), P(Partials)]
@@ -767,6 +803,133 @@ def adamw_step(params, grads, exp_avg, exp_avg_sq, cfg: AdamwCfg,
     return st.as_dict() | {"status": rc}
 
 
+# --------------------------------------------------- orthogonalised updates
+
+# a, b, c of the steps X <- (a + b A + c A A) X, A = X X^T, that the default
+# settings take five times.
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
+
+
+def muon_cfg(**kw) -> MuonCfg:
+    """The library's default settings of muon_step with the given fields
+    replaced; `coefficients` is a sequence of (a, b, c), one for every step of
+    the orthogonal factor."""
+    c = MuonCfg()
+    load().aloco_muon_default_cfg(ctypes.byref(c))
+    if "coefficients" in kw:
+        steps = [tuple(float(x) for x in s) for s in kw.pop("coefficients")]
+        if not 1 <= len(steps) <= MAX_NS_STEPS or any(len(s) != 3 for s in steps):
+            raise ValueError(f"coefficients must be 1 to {MAX_NS_STEPS} triples")
+        c.steps = len(steps)
+        for i, s in enumerate(steps):
+            c.coefficients[i][:] = s
+    for k, v in kw.items():
+        if not hasattr(c, k):
+            raise TypeError(f"unknown muon setting {k!r}")
+        setattr(c, k, v)
+    return c
+
+
+class Matrices:
+    """The matrices of a replica's vector: (offset, rows, columns) of each, kept
+    for muon_step step after step."""
+
+    def __init__(self, parts):
+        self.parts = [tuple(int(x) for x in p) for p in parts]
+        self.array = (Matrix * len(self.parts))(*self.parts)
+        self._need = {}
+
+    def scratch_bytes(self, workers: int) -> int:
+        need = self._need.get(workers)
+        if need is None:
+            need = load().aloco_muon_scratch_bytes(self.array, len(self.parts), workers)
+            self._need[workers] = need
+        return need
+
+
+def _scratch_of(need, device):
+    """Device memory of a call, from the current stream's pool (whose blocks start
+    on 512-byte boundaries)."""
+    return _torch.empty(need, dtype=_torch.uint8, device=device)
+
+
+def muon_step(params, grads, momentum, matrices, cfg: MuonCfg, stream=None):
+    """One step of the matrices of every replica along the orthogonal factor of
+    their momentum, in place (aloco_muon_step): lists of flat contiguous CUDA
+    tensors of one device, params and grads fp32 or bf16, momentum fp32.
+    `matrices`: a Matrices, or a sequence of (offset, rows, columns); what they do
+    not cover is left alone.  Enqueues only; what it writes counts as written in
+    place."""
+    torch = _torch_module()
+    M = len(params)
+    if not M or not (len(grads) == len(momentum) == M):
+        raise ValueError("params, grads and momentum need one tensor per replica")
+    if not isinstance(matrices, Matrices):
+        matrices = Matrices(matrices)
+    device, N = params[0].device, params[0].numel()
+    for name, ts, dtypes in (("params", params, (torch.float32, torch.bfloat16)),
+                             ("grads", grads, (torch.float32, torch.bfloat16)),
+                             ("momentum", momentum, (torch.float32,))):
+        for t in ts:
+            if t.dtype not in dtypes or t.dtype is not ts[0].dtype:
+                raise TypeError(f"unsupported or mixed {name} dtype {t.dtype}")
+            if t.device != device or not t.is_cuda or t.numel() != N or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous CUDA tensors of one size and device")
+    ctx, handle = _on_stream(stream, device, (*params, *grads, *momentum))
+    lib = load()
+    with ctx:
+        need = matrices.scratch_bytes(M)
+        scratch = _scratch_of(need, device)
+        rc = lib.aloco_muon_step(
+            _pointers(params), _pointers(grads), _pointers(momentum), N, M,
+            F32 if params[0].dtype is torch.float32 else BF16,
+            F32 if grads[0].dtype is torch.float32 else BF16, matrices.array,
+            len(matrices.parts), ctypes.byref(cfg), scratch.data_ptr(), need,
+            ctypes.byref(Opts(stream=handle)))
+    _finish(rc, ctx)
+    _written([*params, *momentum])
+
+
+def orthogonalize(x, *, coefficients=(NEWTON_SCHULZ,) * 5, eps: float = 1e-7, out=None,
+                  stream=None):
+    """Orthogonal factors of matrices [rows, columns] or [batch, rows, columns]
+    (float32 or bfloat16 CUDA tensor with contiguous rows, any strides between
+    them) by Newton-Schulz steps, one for every (a, b, c) of `coefficients`
+    (aloco_orthogonalize).  Returns bfloat16 of x's shape, or fills `out`, a
+    contiguous one.  Enqueues only."""
+    torch = _torch_module()
+    if x.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"matrices must be float32 or bfloat16, not {x.dtype}")
+    if x.dim() not in (2, 3):
+        raise ValueError("need [rows, columns] or [batch, rows, columns]")
+    if not x.is_cuda or (x.stride(-1) != 1 and x.shape[-1] > 1):
+        raise ValueError("need a CUDA tensor with contiguous rows")
+    steps = [float(v) for s in coefficients for v in s]
+    if len(steps) != 3 * len(coefficients):
+        raise ValueError("coefficients must be triples")
+    if out is not None and (out.dtype is not torch.bfloat16 or out.shape != x.shape or
+                            out.device != x.device or not out.is_contiguous()):
+        raise ValueError("out must be a contiguous bfloat16 tensor of x's shape and device")
+    rows, cols = x.shape[-2:]
+    batch = x.shape[0] if x.dim() == 3 else 1
+    device = x.device
+    ctx, handle = _on_stream(stream, device, (x, out))
+    lib = load()
+    with ctx:
+        result = torch.empty(x.shape, dtype=torch.bfloat16, device=device) if out is None else out
+        need = lib.aloco_orthogonalize_scratch_bytes(batch, rows, cols)
+        scratch = _scratch_of(need, device)
+        rc = lib.aloco_orthogonalize(
+            x.data_ptr(), batch, rows, cols, x.stride(0) if x.dim() == 3 else 0, x.stride(-2),
+            F32 if x.dtype is torch.float32 else BF16, result.data_ptr(),
+            (ctypes.c_double * len(steps))(*steps), len(coefficients), eps, scratch.data_ptr(),
+            need, ctypes.byref(Opts(stream=handle)))
+    _finish(rc, ctx, result)
+    if out is not None:
+        _written(out)
+    return result
+
+
 def test_stall_tile(tile: int):
     """Testing only: the next bulk-copy round (or post-training loss) on this
     thread skips the copies of one tile, so that its bounded wait runs out; a
@@ -776,6 +939,18 @@ def test_stall_tile(tile: int):
 
 
 # -------------------------------------------- post-training losses and gradients
+
+class TokenScores(NamedTuple):
+    """logp, entropy: float32, in targets' shape; top_ids: int32, and top_logp:
+    float32, [..., top], the largest logits first and equal ones by their index
+    (None for top = 0); stats: float32 [..., 2], what token_scores_grad needs of
+    a row (its largest logit and sum)."""
+    logp: object
+    entropy: object
+    top_ids: object
+    top_logp: object
+    stats: object
+
 
 class PolicyLoss(NamedTuple):
     """terms: float32 [4] (the loss, its policy term, its KL term before the
@@ -935,6 +1110,75 @@ def token_logprobs(logits, targets, *, temperature: float = 1.0, stream=None):
                                          ctypes.byref(Opts(stream=handle)))
     _finish(rc, ctx, logp)
     return logp
+
+
+def token_scores(logits, targets, *, top: int = 0, temperature: float = 1.0,
+                 stream=None) -> TokenScores:
+    """Log-probabilities of the tokens `targets` with the entropy and the `top`
+    (at most 32) best alternatives of every row (aloco_token_scores); logits and
+    targets as token_logprobs takes them.  Enqueues only."""
+    tok = _tokens(logits, targets, temperature)
+    if not 0 <= top <= min(MAX_TOP, tok.vocab):
+        raise ValueError(f"top = {top} outside [0, min(vocab, {MAX_TOP})]")
+    device, shape = logits.device, targets.shape
+    ctx, handle = _on_stream(stream, device, (logits, targets))
+    with ctx:
+        empty = _torch.empty
+        logp = empty(shape, dtype=_torch.float32, device=device)
+        entropy = empty(shape, dtype=_torch.float32, device=device)
+        stats = empty((*shape, 2), dtype=_torch.float32, device=device)
+        ids = best = None
+        if top:
+            ids = empty((*shape, top), dtype=_torch.int32, device=device)
+            best = empty((*shape, top), dtype=_torch.float32, device=device)
+        rc = load().aloco_token_scores(
+            ctypes.byref(tok), top, logp.data_ptr(), entropy.data_ptr(),
+            ids.data_ptr() if top else None, best.data_ptr() if top else None, stats.data_ptr(),
+            ctypes.byref(Opts(stream=handle)))
+    _finish(rc, ctx, logp, entropy, stats, ids, best)
+    return TokenScores(logp, entropy, ids, best, stats)
+
+
+def token_scores_grad(logits, targets, scores: TokenScores, *, d_logp=None, d_entropy=None,
+                      d_top=None, temperature: float = 1.0, grad=None, stream=None):
+    """Gradient by the logits of a loss over `scores` (token_scores' of the same
+    logits, targets and temperature), from its gradients by their log-probabilities,
+    entropies and alternatives' log-probabilities (float32 of their shapes; at
+    least one is given).  `grad` (optional) receives it and may be `logits` itself;
+    one that is given counts as written in place.  Enqueues only."""
+    tok = _tokens(logits, targets, temperature)
+    if d_logp is None and d_entropy is None and d_top is None:
+        raise ValueError("need d_logp, d_entropy or d_top")
+    device, shape, index = logits.device, targets.shape, logits.device.index
+    stats = _per_row("scores.stats", scores.stats, (*shape, 2), index)
+    by_logp = _per_row("d_logp", d_logp, shape, index) if d_logp is not None else None
+    by_entropy = entropy = by_top = ids = None
+    if d_entropy is not None:
+        by_entropy = _per_row("d_entropy", d_entropy, shape, index)
+        entropy = _per_row("scores.entropy", scores.entropy, shape, index)
+    top = 0
+    if d_top is not None:
+        if scores.top_ids is None:
+            raise ValueError("d_top needs scores with alternatives (top > 0)")
+        top = scores.top_ids.shape[-1]
+        by_top = _per_row("d_top", d_top, (*shape, top), index)
+        t = scores.top_ids
+        if t.dtype is not _torch.int32 or t.shape != (*shape, top) or \
+                t.get_device() != index or not t.is_contiguous():
+            raise ValueError("scores.top_ids must be contiguous int32 of shape "
+                             f"{(*shape, top)} on the logits' device")
+        ids = t.data_ptr()
+    ctx, handle = _on_stream(stream, device, (logits, targets, *scores, d_logp, d_entropy, d_top,
+                                              grad))
+    with ctx:
+        out, desc = _logits_grad(logits, grad, True)
+        rc = load().aloco_token_scores_grad(
+            ctypes.byref(tok), stats, entropy, by_logp, by_entropy, top, ids, by_top, desc,
+            ctypes.byref(Opts(stream=handle)))
+    _finish(rc, ctx, out)
+    if grad is not None:
+        _written(grad)
+    return out
 
 
 def policy_loss(logits, targets, advantages, old_logp, weights, *, ref_logp=None,

@@ -7,157 +7,25 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <cstring>
 #include <limits>
 #include <new>
 #include <utility>
 #include <vector>
 
+#include "aloco_checks.h"
 #include "aloco_grads.h"
 #include "aloco_logits.h"
+#include "aloco_scores.h"
 
 // The testing hook of aloco_test_stall_tile (aloco_host.cpp).
 extern thread_local int64_t t_test_stall_tile1;
 
+using namespace aloco;  // the checks of aloco_checks.h
+
 namespace {
 
-int fail(int code, const char *fmt, ...) {
-    char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof buf, fmt, ap);
-    va_end(ap);
-    return aloco::report_error(code, buf);
-}
-
-int cuda_fail(cudaError_t e, const char *what) {
-    return fail(ALOCO_ERR_CUDA, "%s: %s (%s)", what, cudaGetErrorString(e),
-                cudaGetErrorName(e));
-}
-
-int done() { return aloco::report_error(ALOCO_OK, ""); }
-
-// The current device and its SMs.
-int current_device(int *device, int *sm_count) {
-    static aloco::PerDevice sms;
-    cudaError_t e = cudaGetDevice(device);
-    if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
-    const int slot = *device < aloco::kMaxDevices ? *device : -1;
-    *sm_count = sms.get(slot);
-    if (*sm_count == 0) {
-        e = cudaDeviceGetAttribute(sm_count, cudaDevAttrMultiProcessorCount, *device);
-        if (e != cudaSuccess) return cuda_fail(e, "cudaDeviceGetAttribute");
-        sms.set(slot, *sm_count);
-    }
-    return ALOCO_OK;
-}
-
-// An allocation on the current device that a buffer of this call lies in.
-struct Range {
-    uintptr_t begin = 0, end = 0;
-    bool holds(const void *p, size_t bytes) const {
-        return (uintptr_t)p >= begin && (uintptr_t)p < end && bytes <= end - (uintptr_t)p;
-    }
-};
-
-// Device memory of `device`, and its allocation's extent; false where the
-// driver says otherwise or cannot say.
-bool device_range(const void *p, int device, Range *r) {
-    typedef CUresult (*Fn)(unsigned, CUpointer_attribute *, void **, CUdeviceptr);
-    static const Fn fn = [] {
-        void *f = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuPointerGetAttributes", &f, 12000,
-                                             cudaEnableDefault, &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess) {
-            cudaGetLastError();
-            f = nullptr;
-        }
-        return (Fn)f;
-    }();
-    if (!fn) return false;
-    unsigned type = 0;
-    int ordinal = -1;
-    CUdeviceptr start = 0;
-    size_t size = 0;
-    CUpointer_attribute what[] = {CU_POINTER_ATTRIBUTE_MEMORY_TYPE,
-                                  CU_POINTER_ATTRIBUTE_DEVICE_ORDINAL,
-                                  CU_POINTER_ATTRIBUTE_RANGE_START_ADDR,
-                                  CU_POINTER_ATTRIBUTE_RANGE_SIZE};
-    void *out[] = {&type, &ordinal, &start, &size};
-    if (fn(4, what, out, (CUdeviceptr)p) != CUDA_SUCCESS || type != CU_MEMORYTYPE_DEVICE ||
-        ordinal != device || size == 0)
-        return false;
-    r->begin = (uintptr_t)start;
-    r->end = (uintptr_t)start + size;
-    return true;
-}
-
-// check_buffer for the buffers of one call.  Small ones mostly share an
-// allocation (a framework's pool): one question to the driver serves all that
-// lie in the same; what it does not settle goes to check_buffer.
-struct RangeCheck {
-    static constexpr int kKept = 4;
-    Range seen[kKept];
-    int n = 0;
-    int operator()(const void *p, size_t bytes, int device, const char *name, int index = -1) {
-        for (int i = 0; i < n; ++i)
-            if (seen[i].holds(p, bytes)) return ALOCO_OK;
-        Range r;
-        if (device_range(p, device, &r) && r.holds(p, bytes)) {
-            seen[n < kKept ? n++ : kKept - 1] = r;
-            return ALOCO_OK;
-        }
-        return aloco::check_buffer(p, bytes, device, name, index);
-    }
-};
-
 // ----------------------------------------------------------------- losses
-
-// A buffer of a call: [p, p + bytes), written or read.
-struct Buffer {
-    const char *name;
-    const void *p;
-    size_t bytes, align;
-    bool written;
-};
-
-// Most buffers of one call: logits, targets, advantages, old, ref, weights,
-// terms, logp, grad, scratch, cu_seqlens.
-struct Buffers {
-    Buffer b[12];
-    int n = 0;
-    void add(const char *name, const void *p, size_t bytes, size_t align, bool written) {
-        if (bytes) b[n++] = {name, p, bytes, align, written};
-    }
-};
-
-int check_buffers(const Buffers &s, bool grad_over_logits, int *sm_count) {
-    for (int i = 0; i < s.n; ++i) {
-        const Buffer &x = s.b[i];
-        if (!x.p) return fail(ALOCO_ERR_ARG, "NULL %s", x.name);
-        if ((uintptr_t)x.p & (x.align - 1))
-            return fail(ALOCO_ERR_ARG, "%s: not aligned to %zu bytes", x.name, x.align);
-    }
-    for (int i = 0; i < s.n; ++i)
-        for (int j = i + 1; j < s.n; ++j) {
-            const Buffer &x = s.b[i], &y = s.b[j];
-            if (!x.written && !y.written) continue;
-            if ((uintptr_t)x.p >= (uintptr_t)y.p + y.bytes ||
-                (uintptr_t)y.p >= (uintptr_t)x.p + x.bytes)
-                continue;
-            if (grad_over_logits && !std::strcmp(x.name, "logits") && !std::strcmp(y.name, "grad"))
-                continue;
-            return fail(ALOCO_ERR_ALIAS, "%s and %s overlap", x.name, y.name);
-        }
-    int device, rc = current_device(&device, sm_count);
-    RangeCheck check;
-    for (int i = 0; i < s.n && rc == ALOCO_OK; ++i)
-        rc = check(s.b[i].p, s.b[i].bytes, device, s.b[i].name);
-    return rc;
-}
 
 // Strides of a [batch, rows, vocab] array, whose rows may not overlap (either
 // dimension may be the outer one), and its extent in bytes.
@@ -220,6 +88,21 @@ int take_tokens(const aloco_tokens_t *t, aloco::LogitsArgs *a, Buffers *s) {
     return ALOCO_OK;
 }
 
+// The same for the scores, from what take_tokens filled in.
+void take_scores(const aloco_tokens_t *t, const LogitsArgs &a, int top, ScoresArgs *s) {
+    std::memset(s, 0, sizeof *s);
+    s->x = a.x;
+    s->g = a.g;
+    s->n = a.n;
+    s->vocab = a.vocab;
+    s->bf16 = t->dtype == ALOCO_BF16;
+    s->target = a.target;
+    s->target_bytes = a.target_bytes;
+    s->scale = (float)(1.4426950408889634 / t->temperature);
+    s->inv_temp = a.inv_temp;
+    s->top = top;
+}
+
 int take_grad(const aloco_tokens_t *t, const aloco_logits_grad_t *g, aloco::LogitsArgs *a,
               Buffers *s, bool *over) {
     *over = false;
@@ -267,10 +150,6 @@ void take_stall(aloco::LogitsArgs *a) {
     t_test_stall_tile1 = 0;
 }
 
-cudaStream_t stream_of(const aloco_opts_t *o) {
-    return o ? (cudaStream_t)o->stream : (cudaStream_t) nullptr;
-}
-
 }  // namespace
 
 extern "C" {
@@ -295,6 +174,74 @@ int aloco_token_logprobs(const aloco_tokens_t *tokens, float *logp, const aloco_
     const cudaError_t e =
         (tokens->dtype == ALOCO_BF16 ? aloco::token_logprobs_bf16 : aloco::token_logprobs_f32)(a, sms, stream_of(opts));
     return e == cudaSuccess ? done() : cuda_fail(e, "token log-probabilities");
+}
+
+int aloco_token_scores(const aloco_tokens_t *tokens, int32_t top, float *logp, float *entropy,
+                       int32_t *top_ids, float *top_logp, float *stats, const aloco_opts_t *opts) {
+    aloco::LogitsArgs a;
+    Buffers s;
+    int rc = take_tokens(tokens, &a, &s);
+    if (rc != ALOCO_OK) return rc;
+    if (top < 0 || top > ALOCO_MAX_TOP || top > tokens->vocab)
+        return fail(ALOCO_ERR_ARG, "top = %d outside [0, min(vocab, %d)]", top, ALOCO_MAX_TOP);
+    if (a.n == 0) return done();
+    const size_t each = (size_t)a.n * 4;
+    s.add("logp", logp, each, 4, true);
+    if (entropy) s.add("entropy", entropy, each, 4, true);
+    if (stats) s.add("stats", stats, 2 * each, 8, true);
+    s.add("top_ids", top_ids, each * top, 4, true);
+    s.add("top_logp", top_logp, each * top, 4, true);
+    int sms;
+    if ((rc = check_buffers(s, false, &sms)) != ALOCO_OK) return rc;
+    aloco::ScoresArgs b;
+    take_scores(tokens, a, top, &b);
+    b.logp = logp;
+    b.entropy = entropy;
+    b.stats = reinterpret_cast<float2 *>(stats);
+    b.top_ids = top_ids;
+    b.top_logp = top_logp;
+    const cudaError_t e = aloco::launch_token_scores(b, sms, stream_of(opts));
+    return e == cudaSuccess ? done() : cuda_fail(e, "token scores");
+}
+
+int aloco_token_scores_grad(const aloco_tokens_t *tokens, const float *stats, const float *entropy,
+                            const float *d_logp, const float *d_entropy, int32_t top,
+                            const int32_t *top_ids, const float *d_top,
+                            const aloco_logits_grad_t *grad, const aloco_opts_t *opts) {
+    aloco::LogitsArgs a;
+    Buffers s;
+    int rc = take_tokens(tokens, &a, &s);
+    if (rc != ALOCO_OK) return rc;
+    if (top < 0 || top > ALOCO_MAX_TOP)
+        return fail(ALOCO_ERR_ARG, "top = %d outside [0, %d]", top, ALOCO_MAX_TOP);
+    if (!grad) return fail(ALOCO_ERR_ARG, "NULL grad");
+    bool over;
+    if ((rc = take_grad(tokens, grad, &a, &s, &over)) != ALOCO_OK) return rc;
+    if (a.n == 0) return done();
+    const size_t each = (size_t)a.n * 4;
+    if (top == 0) d_top = nullptr;
+    s.add("stats", stats, 2 * each, 8, false);
+    if (d_logp) s.add("d_logp", d_logp, each, 4, false);
+    if (d_entropy) {
+        s.add("d_entropy", d_entropy, each, 4, false);
+        s.add("entropy", entropy, each, 4, false);
+    }
+    if (d_top) {
+        s.add("d_top", d_top, each * top, 4, false);
+        s.add("top_ids", top_ids, each * top, 4, false);
+    }
+    int sms;
+    if ((rc = check_buffers(s, over, &sms)) != ALOCO_OK) return rc;
+    aloco::ScoresArgs b;
+    take_scores(tokens, a, top, &b);
+    b.stats_in = reinterpret_cast<const float2 *>(stats);
+    b.entropy_in = entropy;
+    b.d_logp = d_logp;
+    b.d_entropy = d_entropy;
+    b.ids_in = top_ids;
+    b.d_top = d_top;
+    const cudaError_t e = aloco::launch_token_scores_grad(b, sms, stream_of(opts));
+    return e == cudaSuccess ? done() : cuda_fail(e, "token scores' gradient");
 }
 
 int aloco_policy_loss(const aloco_tokens_t *tokens, const float *advantages,

@@ -1,0 +1,572 @@
+// Entry points of the orthogonalised updates: argument checks, the split of
+// the matrices into passes, and the passes' launches (aloco_orthogonal.cu).
+#include <algorithm>
+#include <cmath>
+#include <limits>
+#include <new>
+#include <vector>
+
+#include "aloco_checks.h"
+#include "aloco_orthogonal.h"
+
+// The testing hook of aloco_test_stall_tile (aloco_host.cpp).
+extern thread_local int64_t t_test_stall_tile1;
+
+using namespace aloco;
+
+namespace {
+
+// Scratch that a pass may fill.  More matrices at once fill the tiles' last
+// round better; a pass of this size holds thousands of tiles.
+constexpr size_t kPassBytes = (size_t)3 << 30;
+constexpr size_t kAlign = 256;
+
+size_t up(size_t x, size_t to) { return (x + to - 1) / to * to; }
+
+// Matrices of one shape: `period` places of M workers.
+struct Shape {
+    int64_t rows, cols;
+    int first, period;               // places [first, first + period)
+    int64_t m() const { return std::min(rows, cols); }
+    int64_t n() const { return std::max(rows, cols); }
+    int64_t ldx() const { return (int64_t)up((size_t)n(), 8); }
+    int64_t lda() const { return (int64_t)up((size_t)m(), 8); }
+    // norm blocks of a matrix and the elements of each
+    int64_t chunk() const {
+        return std::max<int64_t>(16384, (int64_t)up((size_t)(rows * cols / 512), 4096));
+    }
+    int64_t chunks() const { return (rows * cols + chunk() - 1) / chunk(); }
+    // scratch of `count` matrices
+    size_t bytes(int64_t count) const {
+        return 3 * up((size_t)(count * m() * ldx()) * 2, kAlign) +
+               2 * up((size_t)(count * m() * lda()) * 2, kAlign) +
+               2 * up((size_t)(count * m()) * 4, kAlign) +
+               up((size_t)(count * chunks()) * 8, kAlign);
+    }
+};
+
+// A part of a shape's matrices: those from `skip` on.
+struct Part {
+    int shape;
+    int64_t skip, count;
+};
+struct Pass {
+    std::vector<Part> parts;
+    int places = 0;
+    size_t bytes = 0;
+};
+
+struct Plan {
+    std::vector<int64_t> place;
+    std::vector<Shape> shapes;
+    std::vector<Pass> passes;
+    size_t bytes = 0;
+};
+
+// Shapes in `p` (places set) into passes that keep within kPassBytes, kOrthoGroups
+// and kOrthoMatrices: deep products first, so that the last tiles are short.
+void split(Plan *p, int workers) {
+    std::stable_sort(p->shapes.begin(), p->shapes.end(), [](const Shape &x, const Shape &y) {
+        return x.m() != y.m() ? x.m() > y.m() : x.n() > y.n();
+    });
+    Pass pass;
+    const auto flush = [&] {
+        if (pass.parts.empty()) return;
+        p->bytes = std::max(p->bytes, pass.bytes);
+        p->passes.push_back(std::move(pass));
+        pass = Pass();
+    };
+    for (int i = 0; i < (int)p->shapes.size(); ++i) {
+        const Shape &s = p->shapes[i];
+        const int64_t total = (int64_t)s.period * workers;
+        for (int64_t at = 0; at < total;) {
+            if (pass.parts.size() == kOrthoGroups || pass.places + s.period > kOrthoMatrices)
+                flush();
+            const size_t room = kPassBytes - std::min(kPassBytes, pass.bytes);
+            int64_t fit = (int64_t)(room / s.bytes(1));
+            if (fit == 0 && !pass.parts.empty()) {
+                flush();
+                continue;
+            }
+            fit = std::max<int64_t>(fit, 1);
+            // equal parts where one does not hold all
+            const int64_t left = total - at, parts = (left + fit - 1) / fit;
+            const int64_t count = pass.parts.empty() ? (left + parts - 1) / parts
+                                                     : std::min(left, fit);
+            pass.parts.push_back({i, at, count});
+            pass.places += s.period;
+            pass.bytes += s.bytes(count);
+            at += count;
+        }
+    }
+    flush();
+}
+
+// Matrices by shape, in the order of their places.
+int plan_matrices(const aloco_matrix_t *mats, int64_t n, int workers, Plan *p) {
+    std::vector<int64_t> order;
+    for (int64_t i = 0; i < n; ++i)
+        if (mats[i].rows > 0 && mats[i].cols > 0) order.push_back(i);
+    std::stable_sort(order.begin(), order.end(), [&](int64_t a, int64_t b) {
+        const aloco_matrix_t &x = mats[a], &y = mats[b];
+        return x.rows != y.rows ? x.rows < y.rows : x.cols < y.cols;
+    });
+    for (const int64_t i : order) {
+        const aloco_matrix_t &x = mats[i];
+        if (p->shapes.empty() || p->shapes.back().rows != x.rows ||
+            p->shapes.back().cols != x.cols || p->shapes.back().period == 256)
+            p->shapes.push_back({x.rows, x.cols, (int)p->place.size(), 0});
+        ++p->shapes.back().period;
+        p->place.push_back(x.offset);
+    }
+    split(p, workers);
+    return ALOCO_OK;
+}
+
+void plan_batch(int64_t batch, int64_t rows, int64_t cols, Plan *p) {
+    for (int64_t i = 0; i < batch; ++i) {
+        if (p->shapes.empty() || p->shapes.back().period == 256)
+            p->shapes.push_back({rows, cols, (int)i, 0});
+        ++p->shapes.back().period;
+        p->place.push_back(i);
+    }
+    split(p, 1);
+}
+
+int check_side(int64_t rows, int64_t cols, const char *what, int64_t i) {
+    if (rows < 0 || cols < 0 || std::min(rows, cols) > ALOCO_MAX_SIDE ||
+        std::max(rows, cols) > ALOCO_MAX_LONG_SIDE)
+        return fail(ALOCO_ERR_ARG, "%s[%lld]: %lld x %lld out of range (sides up to %d and %d)",
+                    what, (long long)i, (long long)rows, (long long)cols, ALOCO_MAX_SIDE,
+                    ALOCO_MAX_LONG_SIDE);
+    return ALOCO_OK;
+}
+
+int check_steps(const double (*coefficients)[3], int32_t steps, double eps) {
+    if (steps < 1 || steps > ALOCO_MAX_NS_STEPS)
+        return fail(ALOCO_ERR_ARG, "steps = %d outside [1, %d]", steps, ALOCO_MAX_NS_STEPS);
+    for (int s = 0; s < steps; ++s)
+        for (int i = 0; i < 3; ++i)
+            if (!(std::fabs(coefficients[s][i]) <= 100.0))
+                return fail(ALOCO_ERR_ARG, "coefficients[%d][%d] = %g outside [-100, 100]", s, i,
+                            coefficients[s][i]);
+    if (!(std::isfinite(eps) && eps >= 1e-30))
+        return fail(ALOCO_ERR_ARG, "eps = %g must be finite and >= 1e-30", eps);
+    return ALOCO_OK;
+}
+
+// A map of `count` matrices of rows x cols fp16 values, ld elements a row, in
+// boxes of 64 x 64.
+int tensor_map(CUtensorMap *map, void *data, int64_t cols, int64_t rows, int64_t ld,
+               int64_t count) {
+    typedef CUresult (*Fn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
+                           const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                           const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                           CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static const Fn fn = [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000,
+                                             cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            f = nullptr;
+        }
+        return (Fn)f;
+    }();
+    if (!fn) return fail(ALOCO_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)count};
+    const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)(ld * rows) * 2};
+    const cuuint32_t box[3] = {64, 64, 1}, step[3] = {1, 1, 1};
+    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, data, dims, strides, box, step,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS)
+        return fail(ALOCO_ERR_CUDA, "cuTensorMapEncodeTiled: error %d (%lld x %lld x %lld)",
+                    (int)r, (long long)cols, (long long)rows, (long long)count);
+    return ALOCO_OK;
+}
+
+// The tensor maps of a pass; the products copy the ones that they take.
+struct Maps {
+    CUtensorMap x[2][kOrthoGroups], a[kOrthoGroups], p[kOrthoGroups];
+};
+
+// Tiles of all groups for products by `ctas` CTAs a tile.
+void count_tiles(OrthoArgs *a, int sym_ctas, int up_ctas) {
+    const int half = ortho_pair_tile() / 2;
+    a->sym_tiles = a->up_tiles = 0;
+    for (int i = 0; i < a->n_groups; ++i) {
+        OrthoGroup &g = a->g[i];
+        const int s = half * sym_ctas, u = half * up_ctas;
+        const int rows = (g.m + s - 1) / s;
+        g.sym_tiles = rows * (rows + 1) / 2;
+        g.up_tiles = ((g.m + u - 1) / u) * ((g.n + u - 1) / u);
+        g.sym0 = a->sym_tiles;
+        g.up0 = a->up_tiles;
+        a->sym_tiles += g.sym_tiles * g.count;
+        a->up_tiles += g.up_tiles * g.count;
+    }
+}
+
+// `base`: the caller's buffers and settings filled in.
+int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base,
+             const double (*coefficients)[3], int steps, const double *shape_step,
+             char *scratch, int sm_count, cudaStream_t stream) {
+    OrthoArgs a = base;
+    Maps maps;
+    char *at = scratch;
+    const auto take = [&](size_t bytes) {
+        char *p = at;
+        at += up(bytes, kAlign);
+        return p;
+    };
+    a.n_groups = (int)pass.parts.size();
+    int places = 0, norm = 0, prep = 0;
+    for (int i = 0; i < a.n_groups; ++i) {
+        const Part &part = pass.parts[i];
+        const Shape &s = plan.shapes[part.shape];
+        OrthoGroup &g = a.g[i];
+        const int64_t m = s.m(), n = s.n(), count = part.count;
+        g = OrthoGroup();
+        g.m = (int)m;
+        g.n = (int)n;
+        g.ldx = (int)s.ldx();
+        g.lda = (int)s.lda();
+        g.rows = (int)s.rows;
+        g.cols = (int)s.cols;
+        g.tall = s.rows > s.cols;
+        g.count = (int)count;
+        g.first = places;
+        g.period = s.period;
+        g.skip = (int)part.skip;
+        for (int k = 0; k < s.period; ++k) a.place[places++] = plan.place[s.first + k];
+        g.chunk = (int)s.chunk();
+        g.chunks = (int)s.chunks();
+        g.norm0 = norm;
+        norm += g.chunks * g.count;
+        g.prep0 = prep;
+        prep += (int)((s.rows + 63) / 64 * ((s.cols + 63) / 64)) * g.count;
+        const size_t x_bytes = (size_t)(count * m * s.ldx()) * 2;
+        const size_t a_bytes = (size_t)(count * m * s.lda()) * 2;
+        for (int k = 0; k < 2; ++k) g.x[k] = (__half *)take(x_bytes);
+        g.lo = (__half *)take(x_bytes);
+        g.a = (__half *)take(a_bytes);
+        g.p = (__half *)take(a_bytes);
+        g.diag = (float *)take((size_t)(count * m) * 4);
+        g.lead = (float *)take((size_t)(count * m) * 4);
+        g.partial = (double *)take((size_t)(count * s.chunks()) * 8);
+        a.step[i] = shape_step ? (float)shape_step[part.shape] : 0.f;
+        int rc;
+        for (int k = 0; k < 2; ++k)
+            if ((rc = tensor_map(&maps.x[k][i], g.x[k], n, m, s.ldx(), count)) != ALOCO_OK)
+                return rc;
+        if ((rc = tensor_map(&maps.a[i], g.a, m, m, s.lda(), count)) != ALOCO_OK) return rc;
+        if ((rc = tensor_map(&maps.p[i], g.p, m, m, s.lda(), count)) != ALOCO_OK) return rc;
+    }
+    a.norm_blocks = norm;
+    a.prep_blocks = prep;
+    // Pairs of CTAs where their tiles fill the GPU; single CTAs, whose tiles are
+    // a quarter, below.
+    count_tiles(&a, 2, 2);
+    const int sym_ctas = a.sym_tiles >= sm_count / 2 ? 2 : 1;
+    const int up_ctas = a.up_tiles >= sm_count / 2 ? 2 : 1;
+    count_tiles(&a, sym_ctas, up_ctas);
+
+    cudaError_t e = launch_ortho_norm(a, stream);
+    if (e == cudaSuccess) e = launch_ortho_prepare(a, stream);
+    const size_t map_bytes = sizeof(CUtensorMap) * a.n_groups;
+    for (int s = 0; s < steps && e == cudaSuccess; ++s) {
+        a.ca = (float)coefficients[s][0];
+        a.cb = (float)coefficients[s][1];
+        a.cc = (float)coefficients[s][2];
+        a.last = s + 1 == steps;
+        a.next = (s & 1) ^ 1;
+        const CUtensorMap *x = maps.x[s & 1];
+        std::memcpy(a.map_a, x, map_bytes);
+        std::memcpy(a.map_b, x, map_bytes);
+        e = launch_ortho_product(kGram, a, sym_ctas, sm_count, stream);
+        a.test_stall1 = 0;
+        if (e != cudaSuccess) break;
+        std::memcpy(a.map_a, maps.a, map_bytes);
+        std::memcpy(a.map_b, maps.a, map_bytes);
+        e = launch_ortho_product(kPoly, a, sym_ctas, sm_count, stream);
+        if (e != cudaSuccess) break;
+        std::memcpy(a.map_a, maps.p, map_bytes);
+        std::memcpy(a.map_b, x, map_bytes);
+        e = launch_ortho_product(kUpdate, a, up_ctas, sm_count, stream);
+    }
+    return e == cudaSuccess ? ALOCO_OK : cuda_fail(e, "orthogonal factor");
+}
+
+int check_scratch(const void *scratch, size_t bytes, size_t need) {
+    if (bytes < need)
+        return fail(ALOCO_ERR_ARG, "scratch of %zu bytes, need %zu", bytes, need);
+    if (!scratch) return fail(ALOCO_ERR_ARG, "NULL scratch");
+    if ((uintptr_t)scratch & (kAlign - 1))
+        return fail(ALOCO_ERR_ARG, "scratch: not aligned to %zu bytes", kAlign);
+    return ALOCO_OK;
+}
+
+bool meet(const void *p, size_t m, const void *q, size_t n) {
+    return (uintptr_t)p < (uintptr_t)q + n && (uintptr_t)q < (uintptr_t)p + m;
+}
+
+int64_t take_stall() {
+    const int64_t s = t_test_stall_tile1;
+    t_test_stall_tile1 = 0;
+    return s > 0 ? s : 0;
+}
+
+// The matrices lie in a vector of N elements (N < 0: any) and do not overlap.
+int check_matrices(const aloco_matrix_t *mats, int64_t n, int64_t N) {
+    if (n < 0 || n > (1 << 20)) return fail(ALOCO_ERR_ARG, "n = %lld out of range", (long long)n);
+    if (n > 0 && !mats) return fail(ALOCO_ERR_ARG, "NULL matrices");
+    std::vector<std::pair<int64_t, int64_t>> spans;
+    bool sorted = true;
+    for (int64_t i = 0; i < n; ++i) {
+        const aloco_matrix_t &x = mats[i];
+        const int rc = check_side(x.rows, x.cols, "matrices", i);
+        if (rc != ALOCO_OK) return rc;
+        const int64_t size = x.rows * x.cols;
+        if (x.offset < 0 || x.offset > std::numeric_limits<int64_t>::max() / 8 ||
+            (N >= 0 && (x.offset > N || size > N - x.offset)))
+            return fail(ALOCO_ERR_ARG, "matrices[%lld]: %lld x %lld from %lld does not lie in a "
+                        "vector of %lld", (long long)i, (long long)x.rows, (long long)x.cols,
+                        (long long)x.offset, (long long)N);
+        if (!size) continue;
+        sorted = sorted && (spans.empty() || spans.back().first <= x.offset);
+        spans.push_back({x.offset, x.offset + size});
+    }
+    if (!sorted) std::sort(spans.begin(), spans.end());
+    for (size_t i = 1; i < spans.size(); ++i)
+        if (spans[i].first < spans[i - 1].second)
+            return fail(ALOCO_ERR_ALIAS, "two matrices overlap at element %lld",
+                        (long long)spans[i].first);
+    return ALOCO_OK;
+}
+
+int muon_step(void *const *params, const void *const *grads, float *const *momentum, size_t N,
+              int M, aloco_dtype param_dtype, aloco_dtype grad_dtype, const aloco_matrix_t *mats,
+              int64_t n, const aloco_muon_cfg_t *cfg, void *scratch, size_t scratch_bytes,
+              const aloco_opts_t *opts) {
+    int rc;
+    if (!cfg) return fail(ALOCO_ERR_ARG, "NULL cfg");
+    if (!params || !grads || !momentum) return fail(ALOCO_ERR_ARG, "NULL buffer array");
+    if (M < 1 || M > ALOCO_MAX_WORKERS)
+        return fail(ALOCO_ERR_ARG, "M = %d outside [1, %d]", M, ALOCO_MAX_WORKERS);
+    if ((param_dtype != ALOCO_F32 && param_dtype != ALOCO_BF16) ||
+        (grad_dtype != ALOCO_F32 && grad_dtype != ALOCO_BF16))
+        return fail(ALOCO_ERR_ARG, "unknown dtype (params %d, grads %d)", (int)param_dtype,
+                    (int)grad_dtype);
+    if (N > (size_t)std::numeric_limits<int64_t>::max() / 8)
+        return fail(ALOCO_ERR_ARG, "N = %zu out of range", N);
+    if (!(std::isfinite(cfg->lr) && cfg->lr >= 0.0))
+        return fail(ALOCO_ERR_ARG, "lr = %g must be finite and >= 0", cfg->lr);
+    if (!(cfg->momentum >= 0.0 && cfg->momentum < 1.0))
+        return fail(ALOCO_ERR_ARG, "momentum = %g outside [0, 1)", cfg->momentum);
+    if (!(std::isfinite(cfg->weight_decay) && cfg->weight_decay >= 0.0))
+        return fail(ALOCO_ERR_ARG, "weight_decay = %g must be finite and >= 0", cfg->weight_decay);
+    if (cfg->nesterov != 0 && cfg->nesterov != 1)
+        return fail(ALOCO_ERR_ARG, "nesterov = %d must be 0 or 1", cfg->nesterov);
+    if (cfg->scale < ALOCO_MUON_ADAMW || cfg->scale > ALOCO_MUON_UNIT)
+        return fail(ALOCO_ERR_ARG, "unknown scale %d", cfg->scale);
+    if ((rc = check_steps(cfg->coefficients, cfg->steps, cfg->eps)) != ALOCO_OK) return rc;
+    if ((rc = check_matrices(mats, n, (int64_t)N)) != ALOCO_OK) return rc;
+    Plan plan;
+    plan_matrices(mats, n, M, &plan);
+    if (plan.passes.empty()) return done();
+    if ((rc = check_scratch(scratch, scratch_bytes, plan.bytes)) != ALOCO_OK) return rc;
+
+    const size_t px = param_dtype == ALOCO_F32 ? 4 : 2, pg = grad_dtype == ALOCO_F32 ? 4 : 2;
+    struct Buf { const void *p; size_t bytes, size; bool written; const char *name; int i; };
+    Buf bufs[3 * ALOCO_MAX_WORKERS + 1];
+    int nb = 0;
+    for (int i = 0; i < M; ++i) {
+        bufs[nb++] = {params[i], N * px, px, true, "params", i};
+        bufs[nb++] = {grads[i], N * pg, pg, false, "grads", i};
+        bufs[nb++] = {momentum[i], N * 4, 4, true, "momentum", i};
+    }
+    for (int i = 0; i < nb; ++i) {
+        if (!bufs[i].p) return fail(ALOCO_ERR_ARG, "NULL %s[%d]", bufs[i].name, bufs[i].i);
+        if ((uintptr_t)bufs[i].p & (bufs[i].size - 1))
+            return fail(ALOCO_ERR_ARG, "%s[%d]: not aligned to its element", bufs[i].name,
+                        bufs[i].i);
+    }
+    bufs[nb++] = {scratch, plan.bytes, 1, true, "scratch", 0};
+    for (int i = 0; i < nb; ++i)
+        for (int j = 0; j < i; ++j)
+            if ((bufs[i].written || bufs[j].written) &&
+                meet(bufs[i].p, bufs[i].bytes, bufs[j].p, bufs[j].bytes))
+                return fail(ALOCO_ERR_ALIAS, "%s[%d] and %s[%d] overlap", bufs[j].name, bufs[j].i,
+                            bufs[i].name, bufs[i].i);
+    int device, sms;
+    if ((rc = current_device(&device, &sms)) != ALOCO_OK) return rc;
+    RangeCheck check;
+    for (int i = 0; i < nb; ++i)
+        if ((rc = check(bufs[i].p, bufs[i].bytes, device, bufs[i].name, bufs[i].i)) != ALOCO_OK)
+            return rc;
+
+    OrthoArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.source = kSourceMuon;
+    a.in_bf16 = grad_dtype == ALOCO_BF16;
+    a.out_bf16 = param_dtype == ALOCO_BF16;
+    for (int i = 0; i < M; ++i) {
+        a.in[i] = grads[i];
+        a.momentum[i] = momentum[i];
+        a.out[i] = params[i];
+    }
+    a.mu = (float)cfg->momentum;
+    a.nesterov = cfg->nesterov;
+    a.decay = (float)(1.0 - cfg->lr * cfg->weight_decay);
+    a.eps = cfg->eps;
+    a.test_stall1 = take_stall();
+    std::vector<double> step;
+    for (const Shape &s : plan.shapes) {
+        const double by = cfg->scale == ALOCO_MUON_ADAMW ? 0.2 * std::sqrt((double)s.n())
+                          : cfg->scale == ALOCO_MUON_ASPECT
+                              ? std::sqrt(std::max(1.0, (double)s.rows / (double)s.cols))
+                              : 1.0;
+        step.push_back(-cfg->lr * by);
+    }
+    for (const Pass &pass : plan.passes) {
+        rc = run_pass(plan, pass, a, cfg->coefficients, cfg->steps, step.data(), (char *)scratch,
+                      sms, stream_of(opts));
+        if (rc != ALOCO_OK) return rc;
+        a.test_stall1 = 0;
+    }
+    return done();
+}
+
+int orthogonalize(const void *x, int64_t batch, int64_t rows, int64_t cols, int64_t batch_stride,
+                  int64_t row_stride, aloco_dtype dtype, void *out, const double *coefficients,
+                  int32_t steps, double eps, void *scratch, size_t scratch_bytes,
+                  const aloco_opts_t *opts) {
+    int rc;
+    if (dtype != ALOCO_F32 && dtype != ALOCO_BF16)
+        return fail(ALOCO_ERR_ARG, "unknown dtype %d", (int)dtype);
+    if (batch < 0 || batch > (1 << 20))
+        return fail(ALOCO_ERR_ARG, "batch = %lld out of range", (long long)batch);
+    if ((rc = check_side(rows, cols, "x", 0)) != ALOCO_OK) return rc;
+    if (!coefficients) return fail(ALOCO_ERR_ARG, "NULL coefficients");
+    double steps_of[ALOCO_MAX_NS_STEPS][3];
+    if (steps >= 1 && steps <= ALOCO_MAX_NS_STEPS)
+        std::memcpy(steps_of, coefficients, sizeof(double) * 3 * (size_t)steps);
+    if ((rc = check_steps(steps_of, steps, eps)) != ALOCO_OK) return rc;
+    if (batch == 0 || rows == 0 || cols == 0) return done();
+    if (rows == 1) row_stride = cols;
+    if (row_stride < cols || row_stride > (int64_t)1 << 40)
+        return fail(ALOCO_ERR_ARG, "row_stride = %lld: rows of %lld overlap", (long long)row_stride,
+                    (long long)cols);
+    if (batch == 1) batch_stride = 0;
+    const int64_t extent = (rows - 1) * row_stride + cols;
+    if (batch > 1 && (batch_stride < extent || batch_stride > (int64_t)1 << 40))
+        return fail(ALOCO_ERR_ARG, "batch_stride = %lld: matrices overlap",
+                    (long long)batch_stride);
+    Plan plan;
+    plan_batch(batch, rows, cols, &plan);
+    if ((rc = check_scratch(scratch, scratch_bytes, plan.bytes)) != ALOCO_OK) return rc;
+    const size_t size = dtype == ALOCO_F32 ? 4 : 2;
+    Buffers s;
+    s.add("x", x, (size_t)((batch - 1) * batch_stride + extent) * size, size, false);
+    s.add("out", out, (size_t)(batch * rows * cols) * 2, 2, true);
+    s.add("scratch", scratch, plan.bytes, kAlign, true);
+    int sms;
+    if ((rc = check_buffers(s, false, &sms)) != ALOCO_OK) return rc;
+
+    OrthoArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.source = kSourceMatrix;
+    a.in_bf16 = dtype == ALOCO_BF16;
+    a.out_bf16 = 1;
+    a.in[0] = x;
+    a.out[0] = out;
+    a.batch_stride = batch_stride;
+    a.row_stride = row_stride;
+    a.eps = eps;
+    a.test_stall1 = take_stall();
+    for (const Pass &pass : plan.passes) {
+        rc = run_pass(plan, pass, a, steps_of, steps, nullptr, (char *)scratch, sms,
+                      stream_of(opts));
+        if (rc != ALOCO_OK) return rc;
+        a.test_stall1 = 0;
+    }
+    return done();
+}
+
+int no_memory() { return fail(ALOCO_ERR_NOMEM, "orthogonal factor: out of host memory"); }
+
+}  // namespace
+
+extern "C" {
+
+void aloco_muon_default_cfg(aloco_muon_cfg_t *cfg) {
+    if (!cfg) return;
+    std::memset(cfg, 0, sizeof *cfg);
+    cfg->lr = 4e-4;
+    cfg->momentum = 0.95;
+    cfg->weight_decay = 0.1;
+    cfg->eps = 1e-7;
+    cfg->nesterov = 1;
+    cfg->scale = ALOCO_MUON_ADAMW;
+    cfg->steps = 5;
+    for (int s = 0; s < 5; ++s) {
+        cfg->coefficients[s][0] = 3.4445;
+        cfg->coefficients[s][1] = -4.7750;
+        cfg->coefficients[s][2] = 2.0315;
+    }
+}
+
+size_t aloco_muon_scratch_bytes(const aloco_matrix_t *matrices, int64_t n, int M) {
+    try {
+        if (M < 1 || M > ALOCO_MAX_WORKERS || check_matrices(matrices, n, -1) != ALOCO_OK)
+            return 0;
+        Plan plan;
+        plan_matrices(matrices, n, M, &plan);
+        return plan.bytes;
+    } catch (const std::bad_alloc &) {
+        no_memory();
+        return 0;
+    }
+}
+
+int aloco_muon_step(void *const *params, const void *const *grads, float *const *momentum,
+                    size_t N, int M, aloco_dtype param_dtype, aloco_dtype grad_dtype,
+                    const aloco_matrix_t *matrices, int64_t n, const aloco_muon_cfg_t *cfg,
+                    void *scratch, size_t scratch_bytes, const aloco_opts_t *opts) {
+    try {
+        return muon_step(params, grads, momentum, N, M, param_dtype, grad_dtype, matrices, n, cfg,
+                         scratch, scratch_bytes, opts);
+    } catch (const std::bad_alloc &) {
+        return no_memory();
+    }
+}
+
+size_t aloco_orthogonalize_scratch_bytes(int64_t batch, int64_t rows, int64_t cols) {
+    try {
+        if (batch < 1 || batch > (1 << 20) || rows < 1 || cols < 1 ||
+            check_side(rows, cols, "x", 0) != ALOCO_OK)
+            return 0;
+        Plan plan;
+        plan_batch(batch, rows, cols, &plan);
+        return plan.bytes;
+    } catch (const std::bad_alloc &) {
+        no_memory();
+        return 0;
+    }
+}
+
+int aloco_orthogonalize(const void *x, int64_t batch, int64_t rows, int64_t cols,
+                        int64_t batch_stride, int64_t row_stride, aloco_dtype dtype, void *out,
+                        const double *coefficients, int32_t steps, double eps, void *scratch,
+                        size_t scratch_bytes, const aloco_opts_t *opts) {
+    try {
+        return orthogonalize(x, batch, rows, cols, batch_stride, row_stride, dtype, out,
+                             coefficients, steps, eps, scratch, scratch_bytes, opts);
+    } catch (const std::bad_alloc &) {
+        return no_memory();
+    }
+}
+
+}  // extern "C"

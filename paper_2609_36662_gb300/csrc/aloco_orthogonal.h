@@ -1,0 +1,76 @@
+// Internal interface of the orthogonalised updates: what aloco_muon.cpp plans
+// and what the kernels of aloco_orthogonal.cu take by value.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_fp16.h>
+
+#include "aloco_internal.h"
+
+namespace aloco {
+
+// Matrices of one shape in a pass.  X is the matrix with its smaller side as
+// rows (m <= n), in a pair of fp16 values hi + lo; A = X X^T and P = b A + c A A
+// are m x m in fp16 with zeros on the diagonal, which is kept in fp32 beside
+// them.  Rows lie ldx and lda elements apart (multiples of 8).
+struct OrthoGroup {
+    int m, n, ldx, lda;
+    int rows, cols;                  // as the caller has it
+    int tall;                        // rows > cols: X is its transpose
+    int count;                       // matrices of this pass
+    int first, period, skip;         // the i-th: number first + (skip + i) % period
+                                     // of worker (skip + i) / period
+    int sym_tiles, up_tiles;         // tiles of a matrix: symmetric products, update
+    int sym0, up0;                   // the group's first tile
+    int chunks, chunk;               // norm blocks of a matrix, elements of each
+    int norm0, prep0;                // the group's first block
+    __half *x[2], *lo, *a, *p;
+    float *diag;                     // A's diagonal
+    float *lead;                     // a + P's diagonal: what multiplies X itself
+    double *partial;                 // [count][chunks] sums of squares
+};
+
+constexpr int kOrthoGroups = 16;     // groups of a pass
+constexpr int kOrthoMatrices = 1024; // places of a pass (a worker's)
+
+// X is held times 2^8, so that fp16 keeps its values of any realistic size in
+// its normal range (its largest value is at most about 1.2).
+constexpr float kOrthoScale = 256.f;
+
+enum OrthoSource { kSourceMatrix, kSourceMuon };
+
+struct OrthoArgs {
+    CUtensorMap map_a[kOrthoGroups], map_b[kOrthoGroups];  // the operands of this product
+    OrthoGroup g[kOrthoGroups];
+    int64_t place[kOrthoMatrices];   // offset in a replica; kSourceMatrix: index in the batch
+    int n_groups;
+    int sym_tiles, up_tiles, norm_blocks, prep_blocks;      // all groups'
+    int next;                        // which of x[2] the update writes
+    int last;                        // 1: the update writes the result
+    float ca, cb, cc;                // this step's coefficients
+    double eps;
+    // where the matrices come from and go to
+    int source;
+    int in_bf16, out_bf16;
+    int64_t batch_stride, row_stride;      // kSourceMatrix
+    const void *in[ALOCO_MAX_WORKERS];     // gradients (kSourceMatrix: one)
+    float *momentum[ALOCO_MAX_WORKERS];
+    void *out[ALOCO_MAX_WORKERS];          // parameters (kSourceMatrix: one, bf16)
+    float mu;
+    int nesterov;
+    float decay;                     // 1 - lr weight_decay
+    float step[kOrthoGroups];        // -lr * scale of the group's shape
+    int64_t test_stall1;             // testing only: 1 + the slot whose copies a
+                                     // first block leaves out
+};
+
+enum OrthoProduct { kGram, kPoly, kUpdate };
+
+int ortho_pair_tile();               // rows of a tile by two CTAs; half by one
+cudaError_t launch_ortho_norm(const OrthoArgs &a, cudaStream_t stream);
+cudaError_t launch_ortho_prepare(const OrthoArgs &a, cudaStream_t stream);
+// ctas: 1 or 2 CTAs share a tile (of 128 or 256 rows and columns)
+cudaError_t launch_ortho_product(OrthoProduct what, const OrthoArgs &a, int ctas, int sm_count,
+                                 cudaStream_t stream);
+
+}  // namespace aloco
