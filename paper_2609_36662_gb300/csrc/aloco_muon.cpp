@@ -33,7 +33,7 @@ struct Shape {
     int64_t lda() const { return (int64_t)up((size_t)m(), 8); }
     // norm blocks of a matrix and the elements of each
     int64_t chunk() const {
-        return std::max<int64_t>(16384, (int64_t)up((size_t)(rows * cols / 512), 4096));
+        return std::max<int64_t>(4096, (int64_t)up((size_t)(rows * cols / 256), 4096));
     }
     int64_t chunks() const { return (rows * cols + chunk() - 1) / chunk(); }
     // scratch of `count` matrices
@@ -280,7 +280,6 @@ int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base,
         a.ca = (float)coefficients[s][0];
         a.cb = (float)coefficients[s][1];
         a.cc = (float)coefficients[s][2];
-        a.last = s + 1 == steps;
         a.next = (s & 1) ^ 1;
         const CUtensorMap *x = maps.x[s & 1];
         std::memcpy(a.map_a, x, map_bytes);
@@ -294,7 +293,10 @@ int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base,
         if (e != cudaSuccess) break;
         std::memcpy(a.map_a, maps.p, map_bytes);
         std::memcpy(a.map_b, x, map_bytes);
-        e = launch_ortho_product(kUpdate, a, up_ctas, sm_count, stream);
+        e = launch_ortho_product(s + 1 < steps  ? kUpdate
+                                 : a.out_bf16   ? kFinalBf16
+                                                : kFinal,
+                                 a, up_ctas, sm_count, stream);
     }
     return e == cudaSuccess ? ALOCO_OK : cuda_fail(e, "orthogonal factor");
 }

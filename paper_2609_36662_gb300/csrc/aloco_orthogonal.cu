@@ -8,15 +8,19 @@
 namespace aloco {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;        // of the norm and prepare kernels
+constexpr int kEpilogueWarps = 8;
+constexpr int kEpilogueWarp = 4;     // the first of them
+constexpr int kProductThreads = 32 * (kEpilogueWarp + kEpilogueWarps);
 constexpr int kHalfTile = 128;       // a CTA's rows of a tile
 constexpr int kK = 64;               // k-elements of a slot: 128 bytes a row
 constexpr int kBox = 64;             // rows of a copied box
 constexpr int kBoxBytes = kBox * kK * 2;
 constexpr int kSlotBytes = 4 * kBoxBytes;  // two boxes of either operand
 constexpr int kSlots = 6;
-constexpr int kSharedBytes = kSlots * kSlotBytes + 1024 + 256;
-constexpr int kEpilogueWarp = 4;     // the first of four
+constexpr int kStageBytes = 4096;    // an epilogue warp's: a pair of 32 x 32 fp16 blocks
+constexpr int kSharedBytes =
+    kSlots * kSlotBytes + kEpilogueWarps * kStageBytes + 1024 + 256;
 
 struct Tile {
     int group, matrix, row, col;     // row, col: in tiles
@@ -33,7 +37,7 @@ __device__ __forceinline__ int find_group(const OrthoArgs &a, int t, F first) {
 template <int kWhat>
 __device__ __forceinline__ Tile find_tile(const OrthoArgs &a, int t, int tile) {
     Tile f;
-    if constexpr (kWhat == kUpdate) {
+    if constexpr (kWhat >= kUpdate) {
         f.group = find_group(a, t, [](const OrthoGroup &g) { return g.up0; });
         const OrthoGroup &g = a.g[f.group];
         t -= g.up0;
@@ -75,43 +79,68 @@ __device__ __forceinline__ float2 unpack(uint32_t u) {
     return __half22float2(*reinterpret_cast<const __half2 *>(&u));
 }
 
-// 32 columns of row r of a symmetric matrix: those at or left of the diagonal as
-// they lie, and mirrored.
-//   v: the values; on the diagonal what goes beside the matrix has been taken
-//   out (they are 0 there).
-__device__ __forceinline__ void store_symmetric(__half *o, int m, int ld, int r, int c0,
-                                                bool crossing, int lane, const float (&v)[32]) {
-    if (!crossing) {                 // all c < r
-        if (r < m) {
-            __half *row = o + (int64_t)r * ld + c0;
+// A 32 x 32 block of fp16 values in a warp's shared memory: 64 bytes a row, whose
+// 16-byte pieces are turned so that neither a row to a lane nor four lanes to a
+// row meet in a bank.
+__device__ __forceinline__ uint4 *piece(char *block, int row, int q) {
+    return reinterpret_cast<uint4 *>(block) + row * 4 + (q ^ ((row >> 1) & 3));
+}
+
+// The block's pieces in global memory, four lanes to a row: 16-byte accesses of
+// whole 64-byte stretches.  Rows and columns beyond the limits are not touched
+// (columns up to the next multiple of 8 are padding).
+struct Pieces {
+    uint4 q[4];
+    __device__ __forceinline__ void load(const __half *p, int64_t ld, int rows, int cols) {
+        const int lane = threadIdx.x % 32;
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                reinterpret_cast<uint4 *>(row)[q] =
-                    make_uint4(pack(v[8 * q], v[8 * q + 1]), pack(v[8 * q + 2], v[8 * q + 3]),
-                               pack(v[8 * q + 4], v[8 * q + 5]), pack(v[8 * q + 6], v[8 * q + 7]));
+        for (int i = 0; i < 4; ++i) {
+            const int r = 8 * i + lane / 4, c = lane % 4 * 8;
+            q[i] = r < rows && c < cols ? *reinterpret_cast<const uint4 *>(p + r * ld + c)
+                                        : make_uint4(0, 0, 0, 0);
         }
-        // two lanes join their values of two columns: rows behind the last are
-        // padding up to a multiple of 8 and hold whatever comes
-        const bool even = !(lane & 1);
-        __half *col = o + (int64_t)(c0 + (lane & 1)) * ld + (r & ~1);
+    }
+    __device__ __forceinline__ void to_shared(char *block) const {
+        const int lane = threadIdx.x % 32;
 #pragma unroll
-        for (int q = 0; q < 16; ++q) {
-            const uint32_t own = pack(v[2 * q], v[2 * q + 1]);
-            const uint32_t other = __shfl_xor_sync(~0u, own, 1);
-            const uint32_t both = __byte_perm(own, other, even ? 0x5410 : 0x3276);
-            if (r < ld) *reinterpret_cast<uint32_t *>(col + (int64_t)2 * q * ld) = both;
+        for (int i = 0; i < 4; ++i) *piece(block, 8 * i + lane / 4, lane % 4) = q[i];
+    }
+};
+__device__ __forceinline__ void store_block(char *block, __half *p, int64_t ld, int rows,
+                                            int cols) {
+    const int lane = threadIdx.x % 32;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + lane / 4, c = lane % 4 * 8;
+        const uint4 q = *piece(block, r, lane % 4);
+        if (r < rows && c < cols) *reinterpret_cast<uint4 *>(p + r * ld + c) = q;
+    }
+}
+
+// A 32 x 32 block at (r0, c0) of a symmetric matrix, row `lane` in v: as it lies,
+// and mirrored where it is below the diagonal.  (A block on the diagonal holds
+// both halves.)
+__device__ __forceinline__ void store_symmetric(__half *o, int m, int ld, int r0, int c0, char *st,
+                                                const float (&v)[32]) {
+    const int lane = threadIdx.x % 32;
+    __half *mirror = reinterpret_cast<__half *>(st + 2048);
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        *piece(st, lane, q) =
+            make_uint4(pack(v[8 * q], v[8 * q + 1]), pack(v[8 * q + 2], v[8 * q + 3]),
+                       pack(v[8 * q + 4], v[8 * q + 5]), pack(v[8 * q + 6], v[8 * q + 7]));
+    if (c0 != r0) {
+        // element (lane, c) to row c of the mirrored block
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+            const int q = (lane >> 3) ^ ((c >> 1) & 3);
+            mirror[c * 32 + q * 8 + (lane & 7)] = __float2half_rn(v[c]);
         }
-        return;
     }
-    if (r >= m) return;
-#pragma unroll
-    for (int q = 0; q < 32; ++q) {
-        const int c = c0 + q;
-        if (c > r) continue;
-        const __half h = __float2half_rn(v[q]);
-        o[(int64_t)r * ld + c] = h;
-        if (c < r) o[(int64_t)c * ld + r] = h;
-    }
+    __syncwarp();
+    store_block(st, o + (int64_t)r0 * ld + c0, ld, m - r0, ld - c0);
+    if (c0 != r0) store_block(st + 2048, o + (int64_t)c0 * ld + r0, ld, m - c0, ld - r0);
 }
 
 __device__ __forceinline__ float param_load(const void *p, int64_t i, int bf16) {
@@ -125,22 +154,159 @@ __device__ __forceinline__ void param_store(void *p, int64_t i, int bf16, float 
         static_cast<float *>(p)[i] = v;
 }
 
+// Where a matrix's result goes: parameters p <- p decay + step o, or o itself.
+struct Result {
+    void *p;
+    int64_t at, stride;              // element (0, 0); to the next row in memory
+    int bf16, update, tall;          // tall: a row in memory is a column of X
+    bool whole;                      // 16-byte pieces of rows are aligned
+    float decay, step;
+
+    __device__ __forceinline__ Result(const OrthoArgs &a, const OrthoGroup &g, int group,
+                                      int matrix) {
+        const Place place = find_place(a, g, matrix);
+        update = a.source == kSourceMuon;
+        p = a.out[update ? place.worker : 0];
+        at = update ? place.at : place.at * g.rows * g.cols;
+        stride = g.cols;
+        bf16 = a.out_bf16;
+        tall = g.tall;
+        decay = a.decay;
+        step = a.step[group];
+        whole = !((uintptr_t)address(0) & 15) && !(stride & (bf16 ? 7 : 3));
+    }
+    __device__ __forceinline__ char *address(int64_t e) const {
+        return static_cast<char *>(p) + (at + e) * (bf16 ? 2 : 4);
+    }
+    __device__ __forceinline__ float value(float x, float o) const {
+        return update ? fmaf(x, decay, step * o) : o;
+    }
+};
+
+// A 32 x 32 block of parameters, row by row as memory has it, in 16-byte pieces:
+// fetched while the products run, joined with the factor in a warp's shared
+// memory, and stored.
+template <bool kBf16>
+struct Param {
+    static constexpr int kPieces = kBf16 ? 4 : 8, kEach = kBf16 ? 8 : 4;
+    uint4 q[kPieces];
+    static __device__ __forceinline__ int row(int i) {
+        return i * (32 / kPieces) + (int)(threadIdx.x % 32) / kPieces;
+    }
+    static __device__ __forceinline__ int col() { return threadIdx.x % kPieces * kEach; }
+    static __device__ __forceinline__ uint4 *place(char *st, int r, int c) {
+        return kBf16 ? piece(st, r, c / kEach)
+                     : reinterpret_cast<uint4 *>(st) + r * 8 + ((c / kEach) ^ (r & 7));
+    }
+    // (y, x): the block's place in memory's rows and columns
+    __device__ __forceinline__ void load(const Result &to, int y, int x, int rows, int cols) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int r = y + row(i), c = x + col();
+            q[i] = r < rows && c < cols
+                       ? *reinterpret_cast<const uint4 *>(to.address(r * to.stride + c))
+                       : make_uint4(0, 0, 0, 0);
+        }
+    }
+    // v: row `lane` of X's block
+    __device__ __forceinline__ void join(const Result &to, char *st, const float (&v)[32]) const {
+        const int lane = threadIdx.x % 32;
+        __syncwarp();
+        if (to.update) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) *place(st, row(i), col()) = q[i];
+            __syncwarp();
+        }
+        if (to.tall) {               // memory's rows are X's columns
+#pragma unroll
+            for (int c = 0; c < 32; ++c) {
+                char *at = reinterpret_cast<char *>(place(st, c, lane)) + lane % kEach * (16 / kEach);
+                param_store(at, 0, kBf16,
+                            to.value(to.update ? param_load(at, 0, kBf16) : 0.f, v[c]));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; i += kEach) {
+                uint4 *at = place(st, lane, i), w = to.update ? *at : make_uint4(0, 0, 0, 0);
+                uint32_t *p = &w.x;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if constexpr (kBf16) {
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(
+                            to.value(__uint_as_float(p[j] << 16), v[i + 2 * j]),
+                            to.value(__uint_as_float(p[j] & 0xffff0000u), v[i + 2 * j + 1]));
+                        p[j] = *reinterpret_cast<const uint32_t *>(&h);
+                    } else {
+                        p[j] = __float_as_uint(to.value(__uint_as_float(p[j]), v[i + j]));
+                    }
+                }
+                *at = w;
+            }
+        }
+        __syncwarp();
+    }
+    static __device__ __forceinline__ void store(const Result &to, char *st, int y, int x,
+                                                 int rows, int cols) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int r = y + row(i), c = x + col();
+            const uint4 w = *place(st, row(i), col());
+            if (r < rows && c < cols)
+                *reinterpret_cast<uint4 *>(to.address(r * to.stride + c)) = w;
+        }
+    }
+};
+
+// The same value by value, where pieces are not aligned.
+template <bool kBf16>
+__device__ __forceinline__ void store_values(const Result &to, int y, int x, int rows, int cols,
+                                             char *st, const float (&v)[32]) {
+    const int lane = threadIdx.x % 32;
+    float *f = reinterpret_cast<float *>(st);
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 32; ++c) {
+        const int r = to.tall ? c : lane, e = to.tall ? lane : c;
+        f[r * 32 + (e ^ r)] = v[c];
+    }
+    __syncwarp();
+    const bool in = x + lane < cols;
+#pragma unroll
+    for (int r = 0; r < 32; r += 8) {
+        float w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool is = in && y + r + j < rows;
+            const float o = f[(r + j) * 32 + (lane ^ (r + j))];
+            w[j] = to.value(is && to.update
+                                ? param_load(to.address((y + r + j) * to.stride + x + lane), 0, kBf16)
+                                : 0.f,
+                            o);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (in && y + r + j < rows)
+                param_store(to.address((y + r + j) * to.stride + x + lane), 0, kBf16, w[j]);
+    }
+}
+
 // One product of all matrices.  Persistent CTAs (pairs) take tiles in turn: one
 // thread copies operands into a ring of slots, one issues the products into one
-// of two accumulators, four warps write the other one's tile.  A wait that runs
+// of two accumulators, eight warps write the other one's tile.  A wait that runs
 // out leaves NaN in the tile, and with it in the matrix.
 //   kGram    A = X X^T, lower tiles, mirrored; the diagonal in fp32
 //   kPoly    P = b A + c A A, the same
-//   kUpdate  X <- a X + P X, or the result
+//   kUpdate  X <- a X + P X
+//   kFinal, kFinalBf16  the same, to the result in fp32 or bf16
 // A and P are symmetric: half their tiles are computed.
 template <int kWhat, int kCtas>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kProductThreads, 1)
     ortho_product_kernel(const __grid_constant__ OrthoArgs args) {
     constexpr int kTile = kHalfTile * kCtas;
-    constexpr uint32_t kDesc = product_desc(kTile, kTile, kWhat == kUpdate);
+    constexpr uint32_t kDesc = product_desc(kTile, kTile, kWhat >= kUpdate);
     extern __shared__ char raw[];
     const uint32_t smem = (smem_addr(raw) + 1023) & ~1023u;
-    const uint32_t bars = smem + kSlots * kSlotBytes;
+    const uint32_t bars = smem + kSlots * kSlotBytes + kEpilogueWarps * kStageBytes;
     const auto full = [&](int s) { return bars + 8 * s; };
     const auto empty = [&](int s) { return bars + 8 * (kSlots + s); };
     const auto acc_full = [&](int s) { return bars + 8 * (2 * kSlots + s); };
@@ -152,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = kCtas == 1 ? 0 : cluster_rank();
     const int first = blockIdx.x / kCtas, stride = gridDim.x / kCtas;
-    const int tiles = kWhat == kUpdate ? args.up_tiles : args.sym_tiles;
+    const int tiles = kWhat >= kUpdate ? args.up_tiles : args.sym_tiles;
 
     if (threadIdx.x == 0) {
         s_abort = 0;
@@ -162,7 +328,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(acc_full(s), 1);
-            mbar_init(acc_empty(s), 4 * kCtas);
+            mbar_init(acc_empty(s), kEpilogueWarps * kCtas);
         }
         mbar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -200,7 +366,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!skip) {
                     tensor_load<kCtas>(at, ma, k * kK, ra, f.matrix, bar);
                     tensor_load<kCtas>(at + kBoxBytes, ma, k * kK, ra + kBox, f.matrix, bar);
-                    if constexpr (kWhat == kUpdate) {
+                    if constexpr (kWhat >= kUpdate) {
                         tensor_load<kCtas>(at + 2 * kBoxBytes, mb, rb, k * kK, f.matrix, bar);
                         tensor_load<kCtas>(at + 3 * kBoxBytes, mb, rb + kBox, k * kK, f.matrix,
                                            bar);
@@ -238,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int steps = min(kK, K - k + 15) / 16;
                 for (int i = 0; i < steps; ++i) {
                     const uint64_t da = operand_desc(a0 + 32 * i, 16);
-                    const uint64_t db = kWhat == kUpdate ? operand_desc(b0 + 2048 * i, kBoxBytes)
+                    const uint64_t db = kWhat >= kUpdate ? operand_desc(b0 + 2048 * i, kBoxBytes)
                                                          : operand_desc(b0 + 32 * i, 16);
                     product<kCtas>(tmem + acc * kTile, da, db, kDesc, (k | i) != 0);
                 }
@@ -257,121 +423,147 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_wait(drained, 0, nullptr);
         }
     } else if (warp >= kEpilogueWarp) {
-        const int quad = warp - kEpilogueWarp;
+        // a warp reads its quarter of the lanes, and half of the columns
+        const int quad = warp % 4, half = (warp - kEpilogueWarp) / 4;
+        char *st = raw + (smem - smem_addr(raw)) + kSlots * kSlotBytes +
+                   (warp - kEpilogueWarp) * kStageBytes;
         int acc = 0;
         uint32_t acc_phase = 0;
         for (int t = first; t < tiles; t += stride) {
             const Tile f = find_tile<kWhat>(args, t, kTile);
             const OrthoGroup &g = args.g[f.group];
+            const int m = g.m, r0 = f.row * kTile + (int)rank * kHalfTile + quad * 32;
+            const int r = r0 + lane, limit = kWhat >= kUpdate ? g.n : min(m, r0 + 32);
+            const int c_end = min(limit, f.col * kTile + (half + 1) * (kTile / 2));
+            int c0 = f.col * kTile + half * (kTile / 2);
+            const bool some = r0 < m && c0 < c_end;
+            const int64_t row0 = (int64_t)f.matrix * m;  // of the matrix, in its group
+
+            const Result to(args, g, f.group, f.matrix);
+            if (kWhat > kUpdate && some && to.update) {
+                // parameters come from far: to L2 while the products run
+                const int along = to.tall ? 32 : c_end - c0, down = to.tall ? c_end - c0 : 32;
+                for (int i = lane; i < down; i += 32) {
+                    const int y = (to.tall ? c0 : r0) + i, x = to.tall ? r0 : c0;
+                    if (y >= g.rows) break;
+                    for (int j = 0; j < along && x + j < g.cols; j += 32)
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(to.address(y * to.stride + x + j)));
+                }
+            }
+
+            // what the tile is joined with is fetched a block ahead
+            Pieces hi, lo;
+            float by_row = 0.f, by_col = 0.f;
+            const auto fetch = [&](int c) {
+                if constexpr (kWhat >= kUpdate) {
+                    const int64_t at = (row0 + r0) * g.ldx + c;
+                    hi.load(g.x[args.next ^ 1] + at, g.ldx, m - r0, g.n - c);
+                    lo.load(g.lo + at, g.ldx, m - r0, g.n - c);
+                } else if constexpr (kWhat == kPoly) {
+                    hi.load(g.a + (row0 + r0) * g.lda + c, g.lda, m - r0, m - c);
+                    by_col = c + lane < m ? g.diag[row0 + c + lane] : 0.f;
+                }
+            };
+            if (some) {
+                if (kWhat != kGram && r < m) by_row = (kWhat == kPoly ? g.diag : g.lead)[row0 + r];
+                fetch(c0);
+            }
             const bool ok = mbar_wait(acc_full(acc), acc_phase, &s_abort);
             if (!ok) s_abort = 1;
             tc_fence_after();
-            const int m = g.m, r0 = f.row * kTile + (int)rank * kHalfTile + quad * 32;
-            const int r = r0 + lane, limit = kWhat == kUpdate ? g.n : m;
-            const Place place = kWhat == kUpdate && args.last ? find_place(args, g, f.matrix)
-                                                              : Place{0, 0};
 #pragma unroll 1
-            for (int q = 0; q < kTile / 32; ++q) {
-                const int c0 = f.col * kTile + q * 32;
-                if (r0 >= m || c0 >= limit) break;
-                if (kWhat != kUpdate && c0 > r0 + 31) break;
+            for (; some && c0 < c_end; c0 += 32) {
                 uint32_t u[32];
-                tmem_read32(tmem + acc * kTile + q * 32 + (quad << 21), u);
+                tmem_read32(tmem + acc * kTile + (c0 - f.col * kTile) + (quad << 21), u);
                 tmem_ready();
                 float v[32];
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
                     v[i] = ok ? __uint_as_float(u[i]) : __int_as_float(0x7fffffff);
                 if constexpr (kWhat == kGram) {
-                    const bool crossing = c0 + 31 >= r0;
-                    float *diag = g.diag + (int64_t)f.matrix * m;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        v[i] *= 1.f / (kOrthoScale * kOrthoScale);
-                        if (c0 + i == r) {
-                            if (r < m) diag[r] = v[i];
-                            v[i] = 0.f;
-                        }
+                    for (int i = 0; i < 32; ++i) v[i] *= 1.f / (kOrthoScale * kOrthoScale);
+                    if (c0 == r0) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (i == lane) {
+                                if (r < m) g.diag[row0 + r] = v[i];
+                                v[i] = 0.f;
+                            }
                     }
-                    store_symmetric(g.a + (int64_t)f.matrix * m * g.lda, m, g.lda, r, c0, crossing,
-                                    lane, v);
+                    store_symmetric(g.a + row0 * g.lda, m, g.lda, r0, c0, st, v);
                 } else if constexpr (kWhat == kPoly) {
-                    const bool crossing = c0 + 31 >= r0;
-                    const float *diag = g.diag + (int64_t)f.matrix * m;
-                    const float dr = r < m ? diag[r] : 0.f;
-                    const uint4 *row = reinterpret_cast<const uint4 *>(
-                        g.a + ((int64_t)f.matrix * m + min(r, m - 1)) * g.lda + c0);
+                    __syncwarp();
+                    hi.to_shared(st);
+                    const float dc = by_col;
+                    if (c0 + 32 < c_end) fetch(c0 + 32);
+                    __syncwarp();
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const uint4 w = c0 + 8 * i < m ? row[i] : make_uint4(0, 0, 0, 0);
+                        const uint4 w = *piece(st, lane, i);
                         const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
-                            const int c = c0 + 8 * i + j;
+                            const int e = 8 * i + j;
                             const float2 h = unpack(ws[j / 2]);
                             const float a = j & 1 ? h.y : h.x;
-                            const float dc = c < m ? diag[c] : 0.f;
-                            float &x = v[8 * i + j];
-                            if (c == r) {
+                            const float d = by_row + __shfl_sync(~0u, dc, e);
+                            if (c0 == r0 && e == lane) {
                                 if (r < m)
-                                    g.lead[(int64_t)f.matrix * m + r] =
-                                        args.ca + args.cb * dr + args.cc * (dr * dr + x);
-                                x = 0.f;
+                                    g.lead[row0 + r] = args.ca + args.cb * by_row +
+                                                       args.cc * (by_row * by_row + v[e]);
+                                v[e] = 0.f;
                             } else {
-                                x = args.cb * a + args.cc * ((dr + dc) * a + x);
+                                v[e] = args.cb * a + args.cc * (d * a + v[e]);
                             }
                         }
                     }
-                    store_symmetric(g.p + (int64_t)f.matrix * m * g.lda, m, g.lda, r, c0, crossing,
-                                    lane, v);
+                    store_symmetric(g.p + row0 * g.lda, m, g.lda, r0, c0, st, v);
                 } else {
-                    if (r >= m) continue;
-                    const int64_t base = args.source == kSourceMatrix
-                                             ? place.at * g.rows * g.cols
-                                             : place.at;
-                    const float lead = g.lead[(int64_t)f.matrix * m + r];
-                    const int64_t at = ((int64_t)f.matrix * m + r) * g.ldx + c0;
-                    const uint4 *hi = reinterpret_cast<const uint4 *>(g.x[args.next ^ 1] + at);
-                    uint4 *lo = reinterpret_cast<uint4 *>(g.lo + at);
-                    uint4 *to = reinterpret_cast<uint4 *>(g.x[args.next] + at);
+                    Param<kWhat == kFinalBf16> param;
+                    const int y = to.tall ? c0 : r0, x = to.tall ? r0 : c0;
+                    if (kWhat > kUpdate && to.update && to.whole)
+                        param.load(to, y, x, g.rows, g.cols);
+                    __syncwarp();
+                    hi.to_shared(st);
+                    lo.to_shared(st + 2048);
+                    if (c0 + 32 < c_end) fetch(c0 + 32);
+                    __syncwarp();
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        if (c0 + 8 * i >= g.n) continue;
-                        const uint4 h4 = hi[i], l4 = lo[i];
+                        const uint4 h4 = *piece(st, lane, i), l4 = *piece(st + 2048, lane, i);
                         const uint32_t hs[4] = {h4.x, h4.y, h4.z, h4.w};
                         const uint32_t ls[4] = {l4.x, l4.y, l4.z, l4.w};
                         uint32_t nh[4], nl[4];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const float2 h = unpack(hs[j]), l = unpack(ls[j]);
-                            float &x = v[8 * i + 2 * j], &y = v[8 * i + 2 * j + 1];
-                            x = fmaf(lead, h.x + l.x, x);
-                            y = fmaf(lead, h.y + l.y, y);
-                            nh[j] = pack(x, y);
+                            float &v0 = v[8 * i + 2 * j], &v1 = v[8 * i + 2 * j + 1];
+                            v0 = fmaf(by_row, h.x + l.x, v0);
+                            v1 = fmaf(by_row, h.y + l.y, v1);
+                            nh[j] = pack(v0, v1);
                             const float2 b = unpack(nh[j]);
-                            nl[j] = pack(x - b.x, y - b.y);
+                            nl[j] = pack(v0 - b.x, v1 - b.y);
                         }
-                        if (!args.last) {
-                            to[i] = make_uint4(nh[0], nh[1], nh[2], nh[3]);
-                            lo[i] = make_uint4(nl[0], nl[1], nl[2], nl[3]);
-                            continue;
+                        if (kWhat == kUpdate) {
+                            *piece(st, lane, i) = make_uint4(nh[0], nh[1], nh[2], nh[3]);
+                            *piece(st + 2048, lane, i) = make_uint4(nl[0], nl[1], nl[2], nl[3]);
                         }
+                    }
+                    if constexpr (kWhat > kUpdate) {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const int c = c0 + 8 * i + j;
-                            if (c >= g.n) break;
-                            const int64_t e = base + (g.tall ? (int64_t)c * g.cols + r
-                                                                 : (int64_t)r * g.cols + c);
-                            const float o = v[8 * i + j] * (1.f / kOrthoScale);
-                            if (args.source == kSourceMatrix) {
-                                param_store(args.out[0], e, 1, o);
-                            } else {
-                                void *p = args.out[place.worker];
-                                const float x = param_load(p, e, args.out_bf16);
-                                param_store(p, e, args.out_bf16,
-                                            fmaf(x, args.decay, args.step[f.group] * o));
-                            }
+                        for (int i = 0; i < 32; ++i) v[i] *= 1.f / kOrthoScale;
+                        if (to.whole) {
+                            param.join(to, st, v);
+                            param.store(to, st, y, x, g.rows, g.cols);
+                        } else {
+                            store_values<kWhat == kFinalBf16>(to, y, x, g.rows, g.cols, st, v);
                         }
+                    } else {
+                        __syncwarp();
+                        const int64_t at = (row0 + r0) * g.ldx + c0;
+                        store_block(st, g.x[args.next] + at, g.ldx, m - r0, g.n - c0);
+                        store_block(st + 2048, g.lo + at, g.ldx, m - r0, g.n - c0);
                     }
                 }
             }
@@ -396,11 +588,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // ------------------------------------------------- from the caller's matrices
 
-__device__ __forceinline__ float in_load(const void *p, int64_t i, int bf16) {
-    return param_load(p, i, bf16);
-}
-
-// u = g + mu b' (or b') with b' = mu b + g.
+// U = g + mu b' (or b') with b' = mu b + g.
 struct Momentum {
     float mu;
     int nesterov;
@@ -410,31 +598,81 @@ struct Momentum {
     }
 };
 
-__device__ __forceinline__ float load_u(const OrthoArgs &a, const OrthoGroup &g, const Place &p,
-                                        int64_t i) {
-    if (a.source == kSourceMatrix) {
-        const int64_t r = i / g.cols;
-        return in_load(a.in[0], p.at * a.batch_stride + r * a.row_stride + (i - r * g.cols),
-                       a.in_bf16);
-    }
-    const Momentum mo{a.mu, a.nesterov};
-    const float gr = in_load(a.in[p.worker], p.at + i, a.in_bf16);
-    return mo.u(mo.next(a.momentum[p.worker][p.at + i], gr), gr);
+// Four values from element i on, in one access (i and p suit it).
+__device__ __forceinline__ float4 load4(const void *p, int64_t i, int bf16) {
+    if (!bf16) return *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + i);
+    const uint2 w = *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(p) + i);
+    return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u),
+                       __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
 }
 
+// A matrix as the caller has it.
+struct Source {
+    const void *in;
+    float *momentum;                 // null: U is what lies there
+    int64_t at, stride;              // element (0, 0); to the next row
+    int bf16;
+    bool by4;                        // four values of a row at once
+    Momentum mo;
+
+    __device__ __forceinline__ Source(const OrthoArgs &a, const OrthoGroup &g, int matrix) {
+        const Place p = find_place(a, g, matrix);
+        const bool muon = a.source == kSourceMuon;
+        in = a.in[muon ? p.worker : 0];
+        momentum = muon ? a.momentum[p.worker] : nullptr;
+        at = muon ? p.at : p.at * a.batch_stride;
+        stride = muon ? g.cols : a.row_stride;
+        bf16 = a.in_bf16;
+        mo = {a.mu, a.nesterov};
+        const uintptr_t first = (uintptr_t)in + at * (bf16 ? 2 : 4);
+        by4 = !((g.cols | stride) & 3) && !(first & (bf16 ? 7 : 15)) &&
+              !(momentum && ((uintptr_t)(momentum + at) & 15));
+    }
+    __device__ __forceinline__ float u(int64_t e) const {
+        const float g = param_load(in, at + e, bf16);
+        return momentum ? mo.u(mo.next(momentum[at + e], g), g) : g;
+    }
+    __device__ __forceinline__ float4 u4(int64_t e) const {
+        float4 g = load4(in, at + e, bf16);
+        if (momentum) {
+            const float4 b = load4(momentum, at + e, 0);
+            g.x = mo.u(mo.next(b.x, g.x), g.x);
+            g.y = mo.u(mo.next(b.y, g.y), g.y);
+            g.z = mo.u(mo.next(b.z, g.z), g.z);
+            g.w = mo.u(mo.next(b.w, g.w), g.w);
+        }
+        return g;
+    }
+};
+
+// The block's sum, in thread 0.
 __device__ __forceinline__ double block_sum(double s, double *shared) {
 #pragma unroll
     for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
     if (threadIdx.x % 32 == 0) shared[threadIdx.x / 32] = s;
     __syncthreads();
     s = 0.0;
-    for (int i = 0; i < (int)blockDim.x / 32; ++i) s += shared[i];
-    __syncthreads();
+    if (threadIdx.x == 0)
+        for (int i = 0; i < (int)blockDim.x / 32; ++i) s += shared[i];
     return s;
 }
 
-// Sums of squares of the matrices' stretches: fp32 over 16 values, fp64 beyond;
-// what leaves fp32's range is squared in fp64.
+// The sum of 16 squares in fp32; of values whose squares leave its range in fp64.
+__device__ __forceinline__ double squares(const float (&v)[16]) {
+    float s = 0.f, top = 0.f;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        s = fmaf(v[j], v[j], s);
+        top = fmaxf(top, fabsf(v[j]));
+    }
+    if (top < 1e18f && (top > 1e-12f || top == 0.f) && s == s) return (double)s;
+    double d = 0.0;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) d += (double)v[j] * (double)v[j];
+    return d;
+}
+
+// Sums of squares of the matrices' stretches.
 __global__ void __launch_bounds__(kThreads) ortho_norm_kernel(const __grid_constant__ OrthoArgs args) {
     __shared__ double shared[kThreads / 32];
     grid_go();
@@ -442,27 +680,42 @@ __global__ void __launch_bounds__(kThreads) ortho_norm_kernel(const __grid_const
     const int gi = find_group(args, blockIdx.x, [](const OrthoGroup &g) { return g.norm0; });
     const OrthoGroup &g = args.g[gi];
     const int b = blockIdx.x - g.norm0, matrix = b / g.chunks, chunk = b - matrix * g.chunks;
-    const Place place = find_place(args, g, matrix);
+    const Source s(args, g, matrix);
     const int64_t total = (int64_t)g.rows * g.cols;
-    const int64_t begin = (int64_t)chunk * g.chunk, end = min(total, begin + g.chunk);
+    const int64_t begin = (int64_t)chunk * g.chunk;
+    const int n = (int)min((int64_t)g.chunk, total - begin);   // begin: a multiple of 4
+    // (a chunk of a matrix with padded rows starts in row r0, column c0)
+    const int64_t r0 = begin / g.cols;
+    const int c0 = (int)(begin - r0 * g.cols);
+    const bool solid = s.stride == g.cols;
+    const auto place = [&](int i) -> int64_t {
+        if (solid) return begin + i;
+        const unsigned c = (unsigned)c0 + (unsigned)i, r = c / (unsigned)g.cols;
+        return (r0 + r) * s.stride + (c - r * (unsigned)g.cols);
+    };
     double sum = 0.0;
-    for (int64_t i = begin + threadIdx.x; i < end; i += 16 * kThreads) {
-        float v[16], s = 0.f, top = 0.f;
+    float v[16];
+    if (s.by4) {
+        for (int i = 4 * threadIdx.x; i < n; i += 16 * kThreads) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const int64_t e = i + j * kThreads;
-            v[j] = e < end ? load_u(args, g, place, e) : 0.f;
+            for (int j = 0; j < 4; ++j) {
+                const int e = i + j * 4 * kThreads;
+                const float4 x = e < n ? s.u4(place(e)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                v[4 * j] = x.x;
+                v[4 * j + 1] = x.y;
+                v[4 * j + 2] = x.z;
+                v[4 * j + 3] = x.w;
+            }
+            sum += squares(v);
         }
+    } else {
+        for (int i = threadIdx.x; i < n; i += 16 * kThreads) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            s = fmaf(v[j], v[j], s);
-            top = fmaxf(top, fabsf(v[j]));
-        }
-        if (top < 1e18f && (top > 1e-12f || top == 0.f) && s == s) {
-            sum += (double)s;
-        } else {
-#pragma unroll 1
-            for (int j = 0; j < 16; ++j) sum += (double)v[j] * (double)v[j];
+            for (int j = 0; j < 16; ++j) {
+                const int e = i + j * kThreads;
+                v[j] = e < n ? s.u(place(e)) : 0.f;
+            }
+            sum += squares(v);
         }
     }
     sum = block_sum(sum, shared);
@@ -471,10 +724,11 @@ __global__ void __launch_bounds__(kThreads) ortho_norm_kernel(const __grid_const
 
 constexpr int kPrep = 64;            // rows and columns of a prepared tile
 
-// X = u 2^8 / (|u| + eps) as a pair of fp16, transposed where the matrix is
+// X = U 2^8 / (|U| + eps) as a pair of fp16, transposed where the matrix is
 // tall, and the new momentum.
 __global__ void __launch_bounds__(kThreads) ortho_prepare_kernel(const __grid_constant__ OrthoArgs args) {
-    __shared__ double shared[kThreads / 32];
+    __shared__ float s_f;            // the factor, where fp32 does for it
+    __shared__ double s_factor;
     __shared__ float tile[kPrep][kPrep + 1];
     grid_go();
     grid_wait();
@@ -485,56 +739,110 @@ __global__ void __launch_bounds__(kThreads) ortho_prepare_kernel(const __grid_co
     const int matrix = b / (across * down);
     b -= matrix * across * down;
     const int r0 = b / across * kPrep, c0 = b % across * kPrep;
-    const Place place = find_place(args, g, matrix);
+    const Source s(args, g, matrix);
+    const int tx = threadIdx.x % 16 * 4, ty = threadIdx.x / 16;
 
-    double s = 0.0;
-    for (int i = threadIdx.x; i < g.chunks; i += kThreads)
-        s += g.partial[(int64_t)matrix * g.chunks + i];
-    s = block_sum(s, shared);
-    const double factor = (double)kOrthoScale / (sqrt(s) + args.eps);
-    const bool plain = factor > 1e-30 && factor < 1e30;
-    const float f = (float)factor;
-
-    const Momentum mo{args.mu, args.nesterov};
-    for (int i = threadIdx.x; i < kPrep * kPrep; i += kThreads) {
-        const int y = i / kPrep, x = i % kPrep, r = r0 + y, c = c0 + x;
-        float u = 0.f;
-        if (r < g.rows && c < g.cols) {
-            if (args.source == kSourceMatrix) {
-                u = in_load(args.in[0],
-                            place.at * args.batch_stride + r * args.row_stride + c,
-                            args.in_bf16);
-            } else {
-                const int64_t e = place.at + (int64_t)r * g.cols + c;
-                const float gr = in_load(args.in[place.worker], e, args.in_bf16);
-                float *buf = args.momentum[place.worker] + e;
-                const float b1 = mo.next(*buf, gr);
-                *buf = b1;
-                u = mo.u(b1, gr);
-            }
+    // (the values first: they do not wait for the norm)
+    float4 in[4], old[4];
+    if (s.by4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = r0 + ty + 16 * i, c = c0 + tx;
+            const bool is = r < g.rows && c < g.cols;
+            const int64_t e = s.at + r * s.stride + c;
+            in[i] = is ? load4(s.in, e, s.bf16) : make_float4(0.f, 0.f, 0.f, 0.f);
+            old[i] = is && s.momentum ? load4(s.momentum, e, 0) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        tile[y][x] = plain ? u * f : (float)((double)u * factor);
+    }
+    // (one warp sums: the SM adds two doubles a clock)
+    if (threadIdx.x < 32) {
+        double sum = 0.0;
+        for (int i = threadIdx.x; i < g.chunks; i += 32)
+            sum += g.partial[(int64_t)matrix * g.chunks + i];
+#pragma unroll
+        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+        if (threadIdx.x == 0) {
+            const bool usual = sum > 1e-30 && sum < 1e30;
+            s_f = usual ? kOrthoScale / (sqrtf((float)sum) + (float)args.eps) : 0.f;
+            if (!usual) s_factor = (double)kOrthoScale / (sqrt(sum) + args.eps);
+        }
     }
     __syncthreads();
+    const float f = s_f;
+    const auto scaled = [&](float u) { return f > 0.f ? u * f : (float)((double)u * s_factor); };
+
     const int64_t base = (int64_t)matrix * g.m * g.ldx;
-    for (int i = threadIdx.x; i < kPrep * kPrep; i += kThreads) {
-        const int y = i / kPrep, x = i % kPrep;
-        const int r = (g.tall ? c0 : r0) + y, c = (g.tall ? r0 : c0) + x;
-        if (r >= g.m || c >= g.n) continue;
-        const float v = g.tall ? tile[x][y] : tile[y][x];
-        const __half h = __float2half_rn(v);
-        g.x[0][base + (int64_t)r * g.ldx + c] = h;
-        g.lo[base + (int64_t)r * g.ldx + c] = __float2half_rn(v - __half2float(h));
+    const auto store = [&](int r, int c, const float (&v)[4]) {  // columns c .. c + 3 of X
+        if (r >= g.m || c >= g.n) return;
+        const uint32_t h0 = pack(v[0], v[1]), h1 = pack(v[2], v[3]);
+        const float2 a = unpack(h0), z = unpack(h1);
+        const int64_t at = base + (int64_t)r * g.ldx + c;
+        *reinterpret_cast<uint2 *>(g.x[0] + at) = make_uint2(h0, h1);
+        *reinterpret_cast<uint2 *>(g.lo + at) =
+            make_uint2(pack(v[0] - a.x, v[1] - a.y), pack(v[2] - z.x, v[3] - z.y));
+    };
+    if (s.by4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int y = ty + 16 * i, r = r0 + y, c = c0 + tx;
+            float v[4] = {in[i].x, in[i].y, in[i].z, in[i].w};
+            if (s.momentum) {
+                const float o[4] = {old[i].x, old[i].y, old[i].z, old[i].w};
+                float n[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    n[j] = s.mo.next(o[j], v[j]);
+                    v[j] = s.mo.u(n[j], v[j]);
+                }
+                if (r < g.rows && c < g.cols)
+                    *reinterpret_cast<float4 *>(s.momentum + s.at + r * s.stride + c) =
+                        make_float4(n[0], n[1], n[2], n[3]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = scaled(v[j]);
+            if (!g.tall) {
+                store(r, c, v);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) tile[y][tx + j] = v[j];
+            }
+        }
+        if (!g.tall) return;
+    } else {
+#pragma unroll 4
+        for (int i = threadIdx.x; i < kPrep * kPrep; i += kThreads) {
+            const int y = i / kPrep, x = i % kPrep, r = r0 + y, c = c0 + x;
+            float u = 0.f;
+            if (r < g.rows && c < g.cols) {
+                const int64_t e = s.at + r * s.stride + c;
+                u = param_load(s.in, e, s.bf16);
+                if (s.momentum) {
+                    const float b1 = s.mo.next(s.momentum[e], u);
+                    s.momentum[e] = b1;
+                    u = s.mo.u(b1, u);
+                }
+            }
+            tile[y][x] = scaled(u);
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int y = ty + 16 * i;
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = g.tall ? tile[tx + j][y] : tile[y][tx + j];
+        store((g.tall ? c0 : r0) + y, (g.tall ? r0 : c0) + tx, v);
     }
 }
 
 template <typename K>
-cudaError_t launch(K kernel, const OrthoArgs &a, int grid, int ctas, int smem,
+cudaError_t launch(K kernel, const OrthoArgs &a, int grid, int threads, int ctas, int smem,
                    cudaStream_t stream) {
     if (grid == 0) return cudaSuccess;
     cudaLaunchConfig_t c{};
     c.gridDim = dim3(grid);
-    c.blockDim = dim3(kThreads);
+    c.blockDim = dim3(threads);
     c.dynamicSmemBytes = smem;
     c.stream = stream;
     cudaLaunchAttribute at[2];
@@ -558,9 +866,10 @@ cudaError_t launch_product(const OrthoArgs &a, int sm_count, cudaStream_t stream
         if (e != cudaSuccess) return e;
         ready.set(d, 1);
     }
-    const int tiles = kWhat == kUpdate ? a.up_tiles : a.sym_tiles;
+    const int tiles = kWhat >= kUpdate ? a.up_tiles : a.sym_tiles;
     const int most = sm_count / kCtas;
-    return launch(kernel, a, (tiles < most ? tiles : most) * kCtas, kCtas, kSharedBytes, stream);
+    return launch(kernel, a, (tiles < most ? tiles : most) * kCtas, kProductThreads, kCtas,
+                  kSharedBytes, stream);
 }
 
 }  // namespace
@@ -568,22 +877,26 @@ cudaError_t launch_product(const OrthoArgs &a, int sm_count, cudaStream_t stream
 int ortho_pair_tile() { return 2 * kHalfTile; }
 
 cudaError_t launch_ortho_norm(const OrthoArgs &a, cudaStream_t stream) {
-    return launch(ortho_norm_kernel, a, a.norm_blocks, 1, 0, stream);
+    return launch(ortho_norm_kernel, a, a.norm_blocks, kThreads, 1, 0, stream);
 }
 
 cudaError_t launch_ortho_prepare(const OrthoArgs &a, cudaStream_t stream) {
-    return launch(ortho_prepare_kernel, a, a.prep_blocks, 1, 0, stream);
+    return launch(ortho_prepare_kernel, a, a.prep_blocks, kThreads, 1, 0, stream);
 }
 
 cudaError_t launch_ortho_product(OrthoProduct what, const OrthoArgs &a, int ctas, int sm_count,
                                  cudaStream_t stream) {
     if (ctas == 1)
-        return what == kGram   ? launch_product<kGram, 1>(a, sm_count, stream)
-               : what == kPoly ? launch_product<kPoly, 1>(a, sm_count, stream)
-                               : launch_product<kUpdate, 1>(a, sm_count, stream);
-    return what == kGram   ? launch_product<kGram, 2>(a, sm_count, stream)
-           : what == kPoly ? launch_product<kPoly, 2>(a, sm_count, stream)
-                           : launch_product<kUpdate, 2>(a, sm_count, stream);
+        return what == kGram     ? launch_product<kGram, 1>(a, sm_count, stream)
+               : what == kPoly   ? launch_product<kPoly, 1>(a, sm_count, stream)
+               : what == kUpdate ? launch_product<kUpdate, 1>(a, sm_count, stream)
+               : what == kFinal  ? launch_product<kFinal, 1>(a, sm_count, stream)
+                                 : launch_product<kFinalBf16, 1>(a, sm_count, stream);
+    return what == kGram     ? launch_product<kGram, 2>(a, sm_count, stream)
+           : what == kPoly   ? launch_product<kPoly, 2>(a, sm_count, stream)
+           : what == kUpdate ? launch_product<kUpdate, 2>(a, sm_count, stream)
+           : what == kFinal  ? launch_product<kFinal, 2>(a, sm_count, stream)
+                             : launch_product<kFinalBf16, 2>(a, sm_count, stream);
 }
 
 }  // namespace aloco

@@ -46,7 +46,6 @@ struct OrthoArgs {
     int n_groups;
     int sym_tiles, up_tiles, norm_blocks, prep_blocks;      // all groups'
     int next;                        // which of x[2] the update writes
-    int last;                        // 1: the update writes the result
     float ca, cb, cc;                // this step's coefficients
     double eps;
     // where the matrices come from and go to
@@ -64,7 +63,7 @@ struct OrthoArgs {
                                      // first block leaves out
 };
 
-enum OrthoProduct { kGram, kPoly, kUpdate };
+enum OrthoProduct { kGram, kPoly, kUpdate, kFinal, kFinalBf16 };
 
 int ortho_pair_tile();               // rows of a tile by two CTAs; half by one
 cudaError_t launch_ortho_norm(const OrthoArgs &a, cudaStream_t stream);

@@ -8,6 +8,13 @@ from paper_2609_36662_gb300 import aloco as A
 from paper_2609_36662_gb300 import build as B
 
 BASE = 1 << 40
+
+
+def _name(kw):
+    return "-".join(f"{k}={v}" if isinstance(v, (int, float, tuple, type(None))) else k
+                    for k, v in kw.items())
+
+
 GAP = 1 << 28
 
 
@@ -48,7 +55,7 @@ def _grad(lib, tok=None, top=4, grad=True, **kw):
                                 dict(entropy=_at(3) + 2),
                                 dict(tok=_tokens(vocab=3, row_stride=3, batch_stride=9)),
                                 dict(tok=_tokens(temperature=0.0)), dict(tok=_tokens(dtype=3)),
-                                dict(tok=_tokens(row_stride=99))], ids=str)
+                                dict(tok=_tokens(row_stride=99))], ids=_name)
 def test_scores_refuse(lib, kw):
     assert _scores(lib, **kw) == A.ERR_ARG and A.last_error()
 
@@ -56,7 +63,7 @@ def test_scores_refuse(lib, kw):
 @pytest.mark.parametrize("kw", [dict(top=-1), dict(top=33), dict(grad=False), dict(stats=None),
                                 dict(entropy=None), dict(ids=None), dict(data=None),
                                 dict(rs=99), dict(stats=_at(2) + 4), dict(d_logp=_at(4) + 1)],
-                         ids=str)
+                         ids=_name)
 def test_scores_gradients_refuse(lib, kw):
     assert _grad(lib, **kw) == A.ERR_ARG and A.last_error()
 
@@ -96,7 +103,7 @@ BAD_MUON = [dict(M=0), dict(M=33), dict(pdt=5), dict(gdt=-1), dict(N=449),
             dict(scratch=None), dict(scratch=_at(20) + 16), dict(bytes_=100), dict(N=1 << 62)]
 
 
-@pytest.mark.parametrize("kw", BAD_MUON, ids=str)
+@pytest.mark.parametrize("kw", BAD_MUON, ids=_name)
 def test_steps_refuse(lib, kw):
     assert _muon(lib, **kw) == A.ERR_ARG and A.last_error()
 
@@ -106,7 +113,7 @@ def test_steps_refuse(lib, kw):
                                 dict(eps=float("inf")), dict(nesterov=2), dict(scale=3),
                                 dict(steps=0), dict(steps=17),
                                 dict(coefficients=[(101.0, 0, 0)]),
-                                dict(coefficients=[(float("nan"), 0, 0)])], ids=str)
+                                dict(coefficients=[(float("nan"), 0, 0)])], ids=_name)
 def test_steps_refuse_settings(lib, kw):
     assert _muon(lib, cfg=A.muon_cfg(**kw)) == A.ERR_ARG and A.last_error()
 
@@ -162,7 +169,7 @@ def _ortho(lib, **kw):
                                 dict(coefficients=False), dict(scratch=None), dict(bytes=1),
                                 dict(x=None), dict(out=None), dict(out=_at(2) + 1),
                                 dict(rows=A.MAX_SIDE + 1, cols=A.MAX_SIDE + 1, rs=1 << 20)],
-                         ids=str)
+                         ids=_name)
 def test_factors_refuse(lib, kw):
     assert _ortho(lib, **kw) == A.ERR_ARG and A.last_error()
 
