@@ -13,6 +13,7 @@ constexpr int kEpilogueWarps = 8;
 constexpr int kEpilogueWarp = 4;     // the first of them
 constexpr int kProductThreads = 32 * (kEpilogueWarp + kEpilogueWarps);
 constexpr int kHalfTile = 128;       // a CTA's rows of a tile
+constexpr int kFull = 256;           // blocks of A and P on the diagonal that are whole
 constexpr int kK = 64;               // k-elements of a slot: 128 bytes a row
 constexpr int kBox = 64;             // rows of a copied box
 constexpr int kBoxBytes = kBox * kK * 2;
@@ -117,20 +118,24 @@ __device__ __forceinline__ void store_block(char *block, __half *p, int64_t ld, 
     }
 }
 
+// Row `lane` in v.
+__device__ __forceinline__ void rows_to_shared(char *block, const float (&v)[32]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        *piece(block, threadIdx.x % 32, q) =
+            make_uint4(pack(v[8 * q], v[8 * q + 1]), pack(v[8 * q + 2], v[8 * q + 3]),
+                       pack(v[8 * q + 4], v[8 * q + 5]), pack(v[8 * q + 6], v[8 * q + 7]));
+}
+
 // A 32 x 32 block at (r0, c0) of a symmetric matrix, row `lane` in v: as it lies,
-// and mirrored where it is below the diagonal.  (A block on the diagonal holds
-// both halves.)
-__device__ __forceinline__ void store_symmetric(__half *o, int m, int ld, int r0, int c0, char *st,
-                                                const float (&v)[32]) {
+// and mirrored if asked.
+__device__ __forceinline__ void store_symmetric(__half *o, int m, int ld, int r0, int c0,
+                                                bool mirrored, char *st, const float (&v)[32]) {
     const int lane = threadIdx.x % 32;
     __half *mirror = reinterpret_cast<__half *>(st + 2048);
     __syncwarp();
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-        *piece(st, lane, q) =
-            make_uint4(pack(v[8 * q], v[8 * q + 1]), pack(v[8 * q + 2], v[8 * q + 3]),
-                       pack(v[8 * q + 4], v[8 * q + 5]), pack(v[8 * q + 6], v[8 * q + 7]));
-    if (c0 != r0) {
+    rows_to_shared(st, v);
+    if (mirrored) {
         // element (lane, c) to row c of the mirrored block
 #pragma unroll
         for (int c = 0; c < 32; ++c) {
@@ -140,7 +145,7 @@ __device__ __forceinline__ void store_symmetric(__half *o, int m, int ld, int r0
     }
     __syncwarp();
     store_block(st, o + (int64_t)r0 * ld + c0, ld, m - r0, ld - c0);
-    if (c0 != r0) store_block(st + 2048, o + (int64_t)c0 * ld + r0, ld, m - c0, ld - r0);
+    if (mirrored) store_block(st + 2048, o + (int64_t)c0 * ld + r0, ld, m - c0, ld - r0);
 }
 
 __device__ __forceinline__ float param_load(const void *p, int64_t i, int bf16) {
@@ -298,12 +303,14 @@ __device__ __forceinline__ void store_values(const Result &to, int y, int x, int
 //   kPoly    P = b A + c A A, the same
 //   kUpdate  X <- a X + P X
 //   kFinal, kFinalBf16  the same, to the result in fp32 or bf16
-// A and P are symmetric: half their tiles are computed.
+// A and P are symmetric: the lower tiles are computed and kept, with whole blocks
+// of kFull on the diagonal.  Where a product needs what would lie above them it
+// takes the tile below, MN-major instead of K-major: nothing is written twice.
 template <int kWhat, int kCtas>
 __global__ void __launch_bounds__(kProductThreads, 1)
     ortho_product_kernel(const __grid_constant__ OrthoArgs args) {
     constexpr int kTile = kHalfTile * kCtas;
-    constexpr uint32_t kDesc = product_desc(kTile, kTile, kWhat >= kUpdate);
+    constexpr uint32_t kDesc = product_desc(kTile, kTile);
     extern __shared__ char raw[];
     const uint32_t smem = (smem_addr(raw) + 1023) & ~1023u;
     const uint32_t bars = smem + kSlots * kSlotBytes + kEpilogueWarps * kStageBytes;
@@ -334,6 +341,10 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) tmem_alloc<kCtas>(smem_addr(&s_tmem), 2 * kTile);
+    if (warp == 3 && lane < args.n_groups) {
+        fetch_map(&args.map_a[lane]);
+        if (kWhat >= kUpdate) fetch_map(&args.map_b[lane]);
+    }
     tc_fence_before();
     __syncthreads();
     if constexpr (kCtas == 2) cluster_sync();
@@ -343,6 +354,8 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     grid_wait();
 
     const auto depth = [&](const OrthoGroup &g) { return kWhat == kGram ? g.n : g.m; };
+    // whether rows `row` of A or P have their columns `k` above the blocks kept
+    const auto above = [](int row, int k) { return kWhat != kGram && k / kFull > row / kFull; };
 
     if (warp == 0 && lane == 0) {
         // operands were written by ordinary stores of the kernel before
@@ -364,17 +377,14 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 const bool skip = args.test_stall1 && blockIdx.x == 0 &&
                                   issued == args.test_stall1 - 1;
                 if (!skip) {
-                    tensor_load<kCtas>(at, ma, k * kK, ra, f.matrix, bar);
-                    tensor_load<kCtas>(at + kBoxBytes, ma, k * kK, ra + kBox, f.matrix, bar);
-                    if constexpr (kWhat >= kUpdate) {
-                        tensor_load<kCtas>(at + 2 * kBoxBytes, mb, rb, k * kK, f.matrix, bar);
-                        tensor_load<kCtas>(at + 3 * kBoxBytes, mb, rb + kBox, k * kK, f.matrix,
-                                           bar);
-                    } else {
-                        tensor_load<kCtas>(at + 2 * kBoxBytes, mb, k * kK, rb, f.matrix, bar);
-                        tensor_load<kCtas>(at + 3 * kBoxBytes, mb, k * kK, rb + kBox, f.matrix,
-                                           bar);
-                    }
+                    const auto rows = [&](uint32_t dst, const CUtensorMap *map, int row, bool turned) {
+                        const int x = turned ? row : k * kK, y = turned ? k * kK : row;
+                        tensor_load<kCtas>(dst, map, x, y, f.matrix, bar);
+                        tensor_load<kCtas>(dst + kBoxBytes, map, x + (turned ? kBox : 0),
+                                           y + (turned ? 0 : kBox), f.matrix, bar);
+                    };
+                    rows(at, ma, ra, above(ra, k * kK));
+                    rows(at + 2 * kBoxBytes, mb, rb, kWhat >= kUpdate || above(rb, k * kK));
                 }
                 ++issued;
                 if (++slot == kSlots) slot = 0, phase ^= 1;
@@ -400,13 +410,17 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 if (!(ok = mbar_wait(full(slot), phase, &s_abort))) break;
                 tc_fence_after();
                 const uint32_t a0 = smem + slot * kSlotBytes, b0 = a0 + 2 * kBoxBytes;
+                const bool ta = above(f.row * kTile, k);
+                const bool tb = kWhat >= kUpdate || above(f.col * kTile, k);
+                const uint32_t desc = kDesc | (ta ? kAMnMajor : 0) | (tb ? kBMnMajor : 0);
+                const uint64_t da = operand_desc(a0, ta ? kBoxBytes : 16);
+                const uint64_t db = operand_desc(b0, tb ? kBoxBytes : 16);
+                // 16 k-elements on, in 16 bytes: 32 bytes of a row, or 16 rows
+                const int na = ta ? 2048 / 16 : 2, nb = tb ? 2048 / 16 : 2;
                 // (what lies behind K is zeros)
                 const int steps = min(kK, K - k + 15) / 16;
                 for (int i = 0; i < steps; ++i) {
-                    const uint64_t da = operand_desc(a0 + 32 * i, 16);
-                    const uint64_t db = kWhat >= kUpdate ? operand_desc(b0 + 2048 * i, kBoxBytes)
-                                                         : operand_desc(b0 + 32 * i, 16);
-                    product<kCtas>(tmem + acc * kTile, da, db, kDesc, (k | i) != 0);
+                    product<kCtas>(tmem + acc * kTile, da + i * na, db + i * nb, desc, (k | i) != 0);
                 }
                 product_commit<kCtas>(empty(slot));
                 if (++slot == kSlots) slot = 0, phase ^= 1;
@@ -433,123 +447,134 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             const Tile f = find_tile<kWhat>(args, t, kTile);
             const OrthoGroup &g = args.g[f.group];
             const int m = g.m, r0 = f.row * kTile + (int)rank * kHalfTile + quad * 32;
-            const int r = r0 + lane, limit = kWhat >= kUpdate ? g.n : min(m, r0 + 32);
+            const int r = r0 + lane, limit = kWhat >= kUpdate ? g.n : m;
             const int c_end = min(limit, f.col * kTile + (half + 1) * (kTile / 2));
             int c0 = f.col * kTile + half * (kTile / 2);
             const bool some = r0 < m && c0 < c_end;
             const int64_t row0 = (int64_t)f.matrix * m;  // of the matrix, in its group
-
+            // (single CTAs have two tiles of a block on the diagonal to fill)
+            const bool mirrored = kCtas == 1 && f.row != f.col &&
+                                  f.row * kTile / kFull == f.col * kTile / kFull;
+            // what a product is joined with: of A or P whole rows, of X blocks that
+            // lie as this warp holds them; fetched a block ahead
+            float4 *wide = nullptr;
+            if (kWhat >= kUpdate)
+                wide = g.wide + ((int64_t)(f.matrix * g.blocks_down + r0 / 32) * g.blocks_across +
+                                 c0 / 32) * kBlockQuads + lane;
             const Result to(args, g, f.group, f.matrix);
-            if (kWhat > kUpdate && some && to.update) {
-                // parameters come from far: to L2 while the products run
-                const int along = to.tall ? 32 : c_end - c0, down = to.tall ? c_end - c0 : 32;
-                for (int i = lane; i < down; i += 32) {
-                    const int y = (to.tall ? c0 : r0) + i, x = to.tall ? r0 : c0;
-                    if (y >= g.rows) break;
-                    for (int j = 0; j < along && x + j < g.cols; j += 32)
-                        asm volatile("prefetch.global.L2 [%0];" ::"l"(to.address(y * to.stride + x + j)));
-                }
-            }
-
-            // what the tile is joined with is fetched a block ahead
-            Pieces hi, lo;
+            Pieces part;
+            float4 quad4[8];
             float by_row = 0.f, by_col = 0.f;
+            const int begin = c0;
             const auto fetch = [&](int c) {
                 if constexpr (kWhat >= kUpdate) {
-                    const int64_t at = (row0 + r0) * g.ldx + c;
-                    hi.load(g.x[args.next ^ 1] + at, g.ldx, m - r0, g.n - c);
-                    lo.load(g.lo + at, g.ldx, m - r0, g.n - c);
+                    const float4 *p = wide + (c - begin) / 32 * kBlockQuads;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) quad4[i] = p[32 * i];
                 } else if constexpr (kWhat == kPoly) {
-                    hi.load(g.a + (row0 + r0) * g.lda + c, g.lda, m - r0, m - c);
-                    by_col = c + lane < m ? g.diag[row0 + c + lane] : 0.f;
+                    part.load(g.a + (row0 + r0) * g.lda + c, g.lda, m - r0, m - c);
+                    by_col = c + lane < m ? args.cc * g.diag[row0 + c + lane] : 0.f;
                 }
             };
-            if (some) {
-                if (kWhat != kGram && r < m) by_row = (kWhat == kPoly ? g.diag : g.lead)[row0 + r];
+            if (kWhat != kGram && some) {
+                if (kWhat >= kUpdate) {
+                    // the rest of the tile's comes to L2 while the products run
+                    for (int c = c0 + 32; c < c_end; c += 32)
+                        fetch_l2(wide - lane + (c - c0) / 32 * kBlockQuads + 8 * lane);
+                }
+                if (kWhat > kUpdate && to.update) {
+                    const int along = to.tall ? 32 : c_end - c0, down = to.tall ? c_end - c0 : 32;
+                    for (int i = lane; i < down; i += 32) {
+                        const int y = (to.tall ? c0 : r0) + i, x = to.tall ? r0 : c0;
+                        if (y >= g.rows) break;
+                        for (int j = 0; j < along && x + j < g.cols; j += 32)
+                            fetch_l2(to.address(y * to.stride + x + j));
+                    }
+                }
+                if (r < m) by_row = (kWhat == kPoly ? g.diag : g.lead)[row0 + r];
                 fetch(c0);
             }
             const bool ok = mbar_wait(acc_full(acc), acc_phase, &s_abort);
             if (!ok) s_abort = 1;
             tc_fence_after();
+            // the accumulator goes back when the last block has been read
+            const auto release = [&] {
+                tc_fence_before();
+                __syncwarp();
+                if (lane) return;
+                if (kCtas == 1)
+                    mbar_arrive(acc_empty(acc));
+                else
+                    mbar_arrive_cluster(cluster_addr(acc_empty(acc), 0));
+            };
 #pragma unroll 1
             for (; some && c0 < c_end; c0 += 32) {
+                Param<kWhat == kFinalBf16> param;
+                const int y = to.tall ? c0 : r0, x = to.tall ? r0 : c0;
+                if (kWhat > kUpdate && to.update && to.whole)
+                    param.load(to, y, x, g.rows, g.cols);
                 uint32_t u[32];
                 tmem_read32(tmem + acc * kTile + (c0 - f.col * kTile) + (quad << 21), u);
-                tmem_ready();
+                if (c0 + 32 >= c_end) release();
                 float v[32];
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    v[i] = ok ? __uint_as_float(u[i]) : __int_as_float(0x7fffffff);
+                for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(u[i]);
+                if (!ok) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = __int_as_float(0x7fffffff);
+                }
                 if constexpr (kWhat == kGram) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] *= 1.f / (kOrthoScale * kOrthoScale);
                     if (c0 == r0) {
+                        float own = 0.f;
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (i == lane) {
-                                if (r < m) g.diag[row0 + r] = v[i];
-                                v[i] = 0.f;
-                            }
+                            if (i == lane) own = v[i], v[i] = 0.f;
+                        if (r < m) g.diag[row0 + r] = own;
                     }
-                    store_symmetric(g.a + row0 * g.lda, m, g.lda, r0, c0, st, v);
+                    store_symmetric(g.a + row0 * g.lda, m, g.lda, r0, c0, mirrored, st, v);
                 } else if constexpr (kWhat == kPoly) {
                     __syncwarp();
-                    hi.to_shared(st);
-                    const float dc = by_col;
+                    part.to_shared(st);
+                    float *cols = reinterpret_cast<float *>(st + 2048);
+                    cols[lane] = by_col;
                     if (c0 + 32 < c_end) fetch(c0 + 32);
                     __syncwarp();
+                    float own = 0.f;
+                    if (c0 == r0) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (i == lane) own = v[i], v[i] = 0.f;
+                        if (r < m)
+                            g.lead[row0 + r] = args.ca + args.cb * by_row +
+                                               args.cc * (by_row * by_row + own);
+                    }
+                    // b a + c ((d_r + d_c) a + x); where A's diagonal is taken out a is 0
+                    const float dr = fmaf(args.cc, by_row, args.cb);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const uint4 w = *piece(st, lane, i);
                         const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+                        const float4 d0 = reinterpret_cast<const float4 *>(cols)[2 * i];
+                        const float4 d1 = reinterpret_cast<const float4 *>(cols)[2 * i + 1];
+                        const float dc[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w};
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
-                            const int e = 8 * i + j;
                             const float2 h = unpack(ws[j / 2]);
-                            const float a = j & 1 ? h.y : h.x;
-                            const float d = by_row + __shfl_sync(~0u, dc, e);
-                            if (c0 == r0 && e == lane) {
-                                if (r < m)
-                                    g.lead[row0 + r] = args.ca + args.cb * by_row +
-                                                       args.cc * (by_row * by_row + v[e]);
-                                v[e] = 0.f;
-                            } else {
-                                v[e] = args.cb * a + args.cc * (d * a + v[e]);
-                            }
+                            v[8 * i + j] = fmaf(j & 1 ? h.y : h.x, dr + dc[j], args.cc * v[8 * i + j]);
                         }
                     }
-                    store_symmetric(g.p + row0 * g.lda, m, g.lda, r0, c0, st, v);
+                    store_symmetric(g.p + row0 * g.lda, m, g.lda, r0, c0, mirrored, st, v);
                 } else {
-                    Param<kWhat == kFinalBf16> param;
-                    const int y = to.tall ? c0 : r0, x = to.tall ? r0 : c0;
-                    if (kWhat > kUpdate && to.update && to.whole)
-                        param.load(to, y, x, g.rows, g.cols);
-                    __syncwarp();
-                    hi.to_shared(st);
-                    lo.to_shared(st + 2048);
-                    if (c0 + 32 < c_end) fetch(c0 + 32);
-                    __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint4 h4 = *piece(st, lane, i), l4 = *piece(st + 2048, lane, i);
-                        const uint32_t hs[4] = {h4.x, h4.y, h4.z, h4.w};
-                        const uint32_t ls[4] = {l4.x, l4.y, l4.z, l4.w};
-                        uint32_t nh[4], nl[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float2 h = unpack(hs[j]), l = unpack(ls[j]);
-                            float &v0 = v[8 * i + 2 * j], &v1 = v[8 * i + 2 * j + 1];
-                            v0 = fmaf(by_row, h.x + l.x, v0);
-                            v1 = fmaf(by_row, h.y + l.y, v1);
-                            nh[j] = pack(v0, v1);
-                            const float2 b = unpack(nh[j]);
-                            nl[j] = pack(v0 - b.x, v1 - b.y);
-                        }
-                        if (kWhat == kUpdate) {
-                            *piece(st, lane, i) = make_uint4(nh[0], nh[1], nh[2], nh[3]);
-                            *piece(st + 2048, lane, i) = make_uint4(nl[0], nl[1], nl[2], nl[3]);
-                        }
+                    for (int i = 0; i < 8; ++i) {
+                        v[4 * i] = fmaf(by_row, quad4[i].x, v[4 * i]);
+                        v[4 * i + 1] = fmaf(by_row, quad4[i].y, v[4 * i + 1]);
+                        v[4 * i + 2] = fmaf(by_row, quad4[i].z, v[4 * i + 2]);
+                        v[4 * i + 3] = fmaf(by_row, quad4[i].w, v[4 * i + 3]);
                     }
+                    if (c0 + 32 < c_end) fetch(c0 + 32);
                     if constexpr (kWhat > kUpdate) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] *= 1.f / kOrthoScale;
@@ -560,21 +585,19 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                             store_values<kWhat == kFinalBf16>(to, y, x, g.rows, g.cols, st, v);
                         }
                     } else {
+                        float4 *p = wide + (c0 - begin) / 32 * kBlockQuads;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            p[32 * i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
                         __syncwarp();
-                        const int64_t at = (row0 + r0) * g.ldx + c0;
-                        store_block(st, g.x[args.next] + at, g.ldx, m - r0, g.n - c0);
-                        store_block(st + 2048, g.lo + at, g.ldx, m - r0, g.n - c0);
+                        rows_to_shared(st, v);
+                        __syncwarp();
+                        store_block(st, g.x[args.next] + (row0 + r0) * g.ldx + c0, g.ldx, m - r0,
+                                    g.n - c0);
                     }
                 }
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                if (kCtas == 1)
-                    mbar_arrive(acc_empty(acc));
-                else
-                    mbar_arrive_cluster(cluster_addr(acc_empty(acc), 0));
-            }
+            if (!some) release();
             if (acc) acc_phase ^= 1;
             acc ^= 1;
         }
@@ -724,8 +747,8 @@ __global__ void __launch_bounds__(kThreads) ortho_norm_kernel(const __grid_const
 
 constexpr int kPrep = 64;            // rows and columns of a prepared tile
 
-// X = U 2^8 / (|U| + eps) as a pair of fp16, transposed where the matrix is
-// tall, and the new momentum.
+// X = U 2^8 / (|U| + eps) in fp16 and fp32, transposed where the matrix is tall,
+// and the new momentum.
 __global__ void __launch_bounds__(kThreads) ortho_prepare_kernel(const __grid_constant__ OrthoArgs args) {
     __shared__ float s_f;            // the factor, where fp32 does for it
     __shared__ double s_factor;
@@ -774,12 +797,10 @@ __global__ void __launch_bounds__(kThreads) ortho_prepare_kernel(const __grid_co
     const int64_t base = (int64_t)matrix * g.m * g.ldx;
     const auto store = [&](int r, int c, const float (&v)[4]) {  // columns c .. c + 3 of X
         if (r >= g.m || c >= g.n) return;
-        const uint32_t h0 = pack(v[0], v[1]), h1 = pack(v[2], v[3]);
-        const float2 a = unpack(h0), z = unpack(h1);
-        const int64_t at = base + (int64_t)r * g.ldx + c;
-        *reinterpret_cast<uint2 *>(g.x[0] + at) = make_uint2(h0, h1);
-        *reinterpret_cast<uint2 *>(g.lo + at) =
-            make_uint2(pack(v[0] - a.x, v[1] - a.y), pack(v[2] - z.x, v[3] - z.y));
+        *reinterpret_cast<uint2 *>(g.x[0] + base + (int64_t)r * g.ldx + c) =
+            make_uint2(pack(v[0], v[1]), pack(v[2], v[3]));
+        g.wide[((int64_t)(matrix * g.blocks_down + r / 32) * g.blocks_across + c / 32) * kBlockQuads +
+               c % 32 / 4 * 32 + r % 32] = make_float4(v[0], v[1], v[2], v[3]);
     };
     if (s.by4) {
 #pragma unroll

@@ -23,12 +23,12 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, uint32_t leading
            (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
 
-// Instruction descriptor: fp16 operands, fp32 accumulators, an M x N tile; A is
-// K-major, B K-major or MN-major.
-constexpr uint32_t product_desc(int m, int n, bool b_mn_major) {
-    return 1u << 4 | (uint32_t)b_mn_major << 16 | (uint32_t)(n >> 3) << 17 |
-           (uint32_t)(m >> 4) << 24;
+// Instruction descriptor: fp16 operands, fp32 accumulators, an M x N tile of
+// K-major operands; what makes one of them MN-major.
+constexpr uint32_t product_desc(int m, int n) {
+    return 1u << 4 | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
 }
+constexpr uint32_t kAMnMajor = 1u << 15, kBMnMajor = 1u << 16;
 
 template <int kCtas>
 __device__ __forceinline__ void tmem_alloc(uint32_t slot, uint32_t columns) {
@@ -95,21 +95,20 @@ __device__ __forceinline__ void tc_fence_after() {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 }
 
-// 32 accumulator columns of this warp's 32 lanes; tmem_ready() before their use.
+// 32 accumulator columns of this warp's 32 lanes (25 cycles beside running products).
 __device__ __forceinline__ void tmem_read32(uint32_t tmem, uint32_t (&v)[32]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
         "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
         : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]),
           "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]),
           "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]),
           "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]),
           "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
-        : "r"(tmem));
-}
-__device__ __forceinline__ void tmem_ready() {
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        : "r"(tmem)
+        : "memory");
 }
 
 // A box of a 3-d tensor to shared memory of this CTA, its bytes counted on `bar`
@@ -137,9 +136,18 @@ __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
+// (relaxed: what it orders are reads of TMEM, by tc_fence_before(); a release
+// would wait for this thread's stores to global memory)
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar)
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar)
                  : "memory");
+}
+// A tensor map, which is a kernel's parameter, ahead of its first use.
+__device__ __forceinline__ void fetch_map(const CUtensorMap *map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+__device__ __forceinline__ void fetch_l2(const void *p) {
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
 }
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
