@@ -2,6 +2,8 @@
 // b A + c A A) X with A = X X^T, some steps of it, for many matrices at once.
 #include <cuda_bf16.h>
 
+#include <climits>
+
 #include "aloco_orthogonal.h"
 #include "aloco_tc.cuh"
 
@@ -295,8 +297,8 @@ __device__ __forceinline__ void store_values(const Result &to, int y, int x, int
     }
 }
 
-// One product of all matrices.  Persistent CTAs (pairs) take tiles in turn: one
-// thread copies operands into a ring of slots, one issues the products into one
+// One product of all matrices.  Persistent CTAs (pairs) take tiles in turn: two
+// threads copy operands into a ring of slots, one issues the products into one
 // of two accumulators, eight warps write the other one's tile.  A wait that runs
 // out leaves NaN in the tile, and with it in the matrix.
 //   kGram    A = X X^T, lower tiles, mirrored; the diagonal in fp32
@@ -341,7 +343,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) tmem_alloc<kCtas>(smem_addr(&s_tmem), 2 * kTile);
-    if (warp == 3 && lane < args.n_groups) {
+    if (warp == 4 && lane < args.n_groups) {
         fetch_map(&args.map_a[lane]);
         if (kWhat >= kUpdate) fetch_map(&args.map_b[lane]);
     }
@@ -354,37 +356,40 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     grid_wait();
 
     const auto depth = [&](const OrthoGroup &g) { return kWhat == kGram ? g.n : g.m; };
-    // whether rows `row` of A or P have their columns `k` above the blocks kept
-    const auto above = [](int row, int k) { return kWhat != kGram && k / kFull > row / kFull; };
 
-    if (warp == 0 && lane == 0) {
+    if ((warp == 0 || warp == 3) && lane == 0) {
+        // One thread for either operand: copying both, a thread takes as long as
+        // the products of a slot do.
+        const bool is_b = warp == 3;
         // operands were written by ordinary stores of the kernel before
         asm volatile("fence.proxy.async;" ::: "memory");
+        const uint32_t bar0 = kCtas == 1 ? full(0) : cluster_addr(full(0), 0);
         int slot = 0, issued = 0;
         uint32_t phase = 0;
         bool ok = true;
         for (int t = first; t < tiles && ok; t += stride) {
             const Tile f = find_tile<kWhat>(args, t, kTile);
             const int chunks = (depth(args.g[f.group]) + kK - 1) / kK;
-            const CUtensorMap *ma = &args.map_a[f.group], *mb = &args.map_b[f.group];
-            const int ra = f.row * kTile + (int)rank * kHalfTile;
-            const int rb = f.col * kTile + (int)rank * kHalfTile;
+            const CUtensorMap *map = is_b ? &args.map_b[f.group] : &args.map_a[f.group];
+            const int row = (is_b ? f.col : f.row) * kTile + (int)rank * kHalfTile;
+            // columns from here on lie below, MN-major (X does throughout)
+            const int turn = kWhat == kGram            ? INT_MAX
+                             : kWhat >= kUpdate && is_b ? 0
+                                                        : (row / kFull + 1) * kFull;
             for (int k = 0; k < chunks; ++k) {
                 if (!(ok = mbar_wait(empty(slot), phase ^ 1, &s_abort))) break;
-                const uint32_t bar = kCtas == 1 ? full(slot) : cluster_addr(full(slot), 0);
-                const uint32_t at = smem + slot * kSlotBytes;
-                if (rank == 0) mbar_arrive_expect_tx(full(slot), kCtas * kSlotBytes);
-                const bool skip = args.test_stall1 && blockIdx.x == 0 &&
-                                  issued == args.test_stall1 - 1;
-                if (!skip) {
-                    const auto rows = [&](uint32_t dst, const CUtensorMap *map, int row, bool turned) {
-                        const int x = turned ? row : k * kK, y = turned ? k * kK : row;
-                        tensor_load<kCtas>(dst, map, x, y, f.matrix, bar);
-                        tensor_load<kCtas>(dst + kBoxBytes, map, x + (turned ? kBox : 0),
-                                           y + (turned ? 0 : kBox), f.matrix, bar);
-                    };
-                    rows(at, ma, ra, above(ra, k * kK));
-                    rows(at + 2 * kBoxBytes, mb, rb, kWhat >= kUpdate || above(rb, k * kK));
+                const uint32_t at = smem + slot * kSlotBytes + (is_b ? 2 * kBoxBytes : 0);
+                const uint32_t bar = bar0 + 8 * slot;
+                if (rank == 0 && !is_b) mbar_arrive_expect_tx(full(slot), kCtas * kSlotBytes);
+                const int c = k * kK;
+                if (args.test_stall1 == 0 || blockIdx.x != 0 || issued != args.test_stall1 - 1) {
+                    if (c < turn) {
+                        tensor_load<kCtas>(at, map, c, row, f.matrix, bar);
+                        tensor_load<kCtas>(at + kBoxBytes, map, c, row + kBox, f.matrix, bar);
+                    } else {
+                        tensor_load<kCtas>(at, map, row, c, f.matrix, bar);
+                        tensor_load<kCtas>(at + kBoxBytes, map, row + kBox, c, f.matrix, bar);
+                    }
                 }
                 ++issued;
                 if (++slot == kSlots) slot = 0, phase ^= 1;
@@ -393,7 +398,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         if (!ok) {
             s_abort = 1;
             // copies in flight land before the block ends (each slot's last use)
-            if (rank == 0)
+            if (rank == 0 && !is_b)
                 for (int i = issued > kSlots ? issued - kSlots : 0; i < issued; ++i)
                     mbar_wait(full(i % kSlots), (i / kSlots) & 1, nullptr);
         }
@@ -406,22 +411,26 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             const int K = depth(args.g[f.group]);
             if (!(ok = mbar_wait(acc_empty(acc), acc_phase ^ 1, &s_abort))) break;
             tc_fence_after();
+            const int turn_a = kWhat == kGram ? INT_MAX : (f.row * kTile / kFull + 1) * kFull;
+            const int turn_b = kWhat == kGram      ? INT_MAX
+                               : kWhat >= kUpdate ? 0
+                                                  : (f.col * kTile / kFull + 1) * kFull;
+            const uint32_t d = tmem + acc * kTile;
             for (int k = 0; k < K; k += kK) {
                 if (!(ok = mbar_wait(full(slot), phase, &s_abort))) break;
                 tc_fence_after();
                 const uint32_t a0 = smem + slot * kSlotBytes, b0 = a0 + 2 * kBoxBytes;
-                const bool ta = above(f.row * kTile, k);
-                const bool tb = kWhat >= kUpdate || above(f.col * kTile, k);
+                const bool ta = k >= turn_a, tb = k >= turn_b;
                 const uint32_t desc = kDesc | (ta ? kAMnMajor : 0) | (tb ? kBMnMajor : 0);
                 const uint64_t da = operand_desc(a0, ta ? kBoxBytes : 16);
                 const uint64_t db = operand_desc(b0, tb ? kBoxBytes : 16);
                 // 16 k-elements on, in 16 bytes: 32 bytes of a row, or 16 rows
                 const int na = ta ? 2048 / 16 : 2, nb = tb ? 2048 / 16 : 2;
-                // (what lies behind K is zeros)
-                const int steps = min(kK, K - k + 15) / 16;
-                for (int i = 0; i < steps; ++i) {
-                    product<kCtas>(tmem + acc * kTile, da + i * na, db + i * nb, desc, (k | i) != 0);
-                }
+                // (straight on: between products this thread has 128 cycles)
+                product<kCtas>(d, da, db, desc, k != 0);
+                if (K - k > 16) product<kCtas>(d, da + na, db + nb, desc, true);
+                if (K - k > 32) product<kCtas>(d, da + 2 * na, db + 2 * nb, desc, true);
+                if (K - k > 48) product<kCtas>(d, da + 3 * na, db + 3 * nb, desc, true);
                 product_commit<kCtas>(empty(slot));
                 if (++slot == kSlots) slot = 0, phase ^= 1;
             }
