@@ -520,8 +520,8 @@ int aloco_adamw_step_normed(void *const *params, const void *const *grads,
  * singular values of U / (||U||_F + eps) towards 1 (Newton-Schulz products):
  *   X_0 = U / (||U||_F + eps),   A = X X^T,   X <- (a + b A + c A A) X
  * with X transposed where U has more rows than columns.  The products run on
- * the tensor cores: X is held in fp32 beside the fp16 values that the products
- * take, A and b A + c A A in fp16 with their diagonals in fp32, sums in fp32.  The factor's error
+ * the tensor cores: X is held as a sum of two fp16 values (22 bits), A and b A + c
+ * A A in fp16 with their diagonals in fp32, sums in fp32.  The factor's error
  * against exact steps is 2e-4 to 1.5e-3 of its norm.  A matrix that holds NaN or
  * inf gives NaN throughout, and no other matrix is affected; zeros give zeros.
  *

@@ -38,10 +38,10 @@ struct Shape {
     int64_t chunks() const { return (rows * cols + chunk() - 1) / chunk(); }
     int64_t down() const { return (m() + 31) / 32; }
     int64_t across() const { return (n() + 31) / 32; }
-    size_t wide_bytes() const { return (size_t)(down() * across()) * 4096; }
+    size_t rest_bytes() const { return (size_t)(down() * across()) * 2048; }
     // scratch of `count` matrices
     size_t bytes(int64_t count) const {
-        return 2 * up((size_t)(count * m() * ldx()) * 2, kAlign) + (size_t)count * wide_bytes() +
+        return 2 * up((size_t)(count * m() * ldx()) * 2, kAlign) + (size_t)count * rest_bytes() +
                2 * up((size_t)(count * m() * lda()) * 2, kAlign) +
                2 * up((size_t)(count * m()) * 4, kAlign) +
                up((size_t)(count * chunks()) * 8, kAlign);
@@ -253,7 +253,7 @@ int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base,
         const size_t x_bytes = (size_t)(count * m * s.ldx()) * 2;
         const size_t a_bytes = (size_t)(count * m * s.lda()) * 2;
         for (int k = 0; k < 2; ++k) g.x[k] = (__half *)take(x_bytes);
-        g.wide = (float4 *)take((size_t)count * s.wide_bytes());
+        g.rest = (uint4 *)take((size_t)count * s.rest_bytes());
         g.blocks_down = (int)s.down();
         g.blocks_across = (int)s.across();
         g.a = (__half *)take(a_bytes);

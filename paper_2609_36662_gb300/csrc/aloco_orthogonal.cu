@@ -466,20 +466,21 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                                   f.row * kTile / kFull == f.col * kTile / kFull;
             // what a product is joined with: of A or P whole rows, of X blocks that
             // lie as this warp holds them; fetched a block ahead
-            float4 *wide = nullptr;
+            uint4 *rest = nullptr;
             if (kWhat >= kUpdate)
-                wide = g.wide + ((int64_t)(f.matrix * g.blocks_down + r0 / 32) * g.blocks_across +
-                                 c0 / 32) * kBlockQuads + lane;
+                rest = g.rest + ((int64_t)(f.matrix * g.blocks_down + r0 / 32) * g.blocks_across +
+                                 c0 / 32) * kBlockPieces + lane;
             const Result to(args, g, f.group, f.matrix);
             Pieces part;
-            float4 quad4[8];
+            uint4 lo[4];
             float by_row = 0.f, by_col = 0.f;
             const int begin = c0;
             const auto fetch = [&](int c) {
                 if constexpr (kWhat >= kUpdate) {
-                    const float4 *p = wide + (c - begin) / 32 * kBlockQuads;
+                    const uint4 *p = rest + (c - begin) / 32 * kBlockPieces;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) quad4[i] = p[32 * i];
+                    for (int i = 0; i < 4; ++i) lo[i] = p[32 * i];
+                    part.load(g.x[args.next ^ 1] + (row0 + r0) * g.ldx + c, g.ldx, m - r0, g.n - c);
                 } else if constexpr (kWhat == kPoly) {
                     part.load(g.a + (row0 + r0) * g.lda + c, g.lda, m - r0, m - c);
                     by_col = c + lane < m ? args.cc * g.diag[row0 + c + lane] : 0.f;
@@ -487,9 +488,11 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             };
             if (kWhat != kGram && some) {
                 if (kWhat >= kUpdate) {
-                    // the rest of the tile's comes to L2 while the products run
-                    for (int c = c0 + 32; c < c_end; c += 32)
-                        fetch_l2(wide - lane + (c - c0) / 32 * kBlockQuads + 8 * lane);
+                    // what is kept of X beside the operands comes to L2 while the
+                    // products run
+                    // (64 of its 128-byte lines, of four blocks)
+                    const int lines = (c_end - c0 + 31) / 32 * 16;
+                    for (int i = lane; i < lines; i += 32) fetch_l2(rest - lane + 8 * i);
                 }
                 if (kWhat > kUpdate && to.update) {
                     const int along = to.tall ? 32 : c_end - c0, down = to.tall ? c_end - c0 : 32;
@@ -576,14 +579,31 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                     }
                     store_symmetric(g.p + row0 * g.lda, m, g.lda, r0, c0, mirrored, st, v);
                 } else {
+                    __syncwarp();
+                    part.to_shared(st);
+                    uint32_t ls[16];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        v[4 * i] = fmaf(by_row, quad4[i].x, v[4 * i]);
-                        v[4 * i + 1] = fmaf(by_row, quad4[i].y, v[4 * i + 1]);
-                        v[4 * i + 2] = fmaf(by_row, quad4[i].z, v[4 * i + 2]);
-                        v[4 * i + 3] = fmaf(by_row, quad4[i].w, v[4 * i + 3]);
+                    for (int i = 0; i < 4; ++i) {
+                        ls[4 * i] = lo[i].x;
+                        ls[4 * i + 1] = lo[i].y;
+                        ls[4 * i + 2] = lo[i].z;
+                        ls[4 * i + 3] = lo[i].w;
                     }
                     if (c0 + 32 < c_end) fetch(c0 + 32);
+                    __syncwarp();
+                    uint4 w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = *piece(st, lane, i);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const uint32_t hs = i % 4 == 0   ? w[i / 4].x
+                                            : i % 4 == 1 ? w[i / 4].y
+                                            : i % 4 == 2 ? w[i / 4].z
+                                                         : w[i / 4].w;
+                        const float2 h = unpack(hs), l = unpack(ls[i]);
+                        v[2 * i] = fmaf(by_row, h.x, fmaf(by_row, l.x, v[2 * i]));
+                        v[2 * i + 1] = fmaf(by_row, h.y, fmaf(by_row, l.y, v[2 * i + 1]));
+                    }
                     if constexpr (kWhat > kUpdate) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] *= 1.f / kOrthoScale;
@@ -594,12 +614,20 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                             store_values<kWhat == kFinalBf16>(to, y, x, g.rows, g.cols, st, v);
                         }
                     } else {
-                        float4 *p = wide + (c0 - begin) / 32 * kBlockQuads;
+                        uint4 *p = rest + (c0 - begin) / 32 * kBlockPieces;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            p[32 * i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-                        __syncwarp();
-                        rows_to_shared(st, v);
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t h[4], l[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const float x0 = v[8 * i + 2 * j], x1 = v[8 * i + 2 * j + 1];
+                                h[j] = pack(x0, x1);
+                                const float2 b = unpack(h[j]);
+                                l[j] = pack(x0 - b.x, x1 - b.y);
+                            }
+                            *piece(st, lane, i) = make_uint4(h[0], h[1], h[2], h[3]);
+                            p[32 * i] = make_uint4(l[0], l[1], l[2], l[3]);
+                        }
                         __syncwarp();
                         store_block(st, g.x[args.next] + (row0 + r0) * g.ldx + c0, g.ldx, m - r0,
                                     g.n - c0);
@@ -756,8 +784,8 @@ __global__ void __launch_bounds__(kThreads) ortho_norm_kernel(const __grid_const
 
 constexpr int kPrep = 64;            // rows and columns of a prepared tile
 
-// X = U 2^8 / (|U| + eps) in fp16 and fp32, transposed where the matrix is tall,
-// and the new momentum.
+// X = U 2^8 / (|U| + eps) as a sum of two fp16 values, transposed where the matrix
+// is tall, and the new momentum.
 __global__ void __launch_bounds__(kThreads) ortho_prepare_kernel(const __grid_constant__ OrthoArgs args) {
     __shared__ float s_f;            // the factor, where fp32 does for it
     __shared__ double s_factor;
@@ -806,10 +834,13 @@ __global__ void __launch_bounds__(kThreads) ortho_prepare_kernel(const __grid_co
     const int64_t base = (int64_t)matrix * g.m * g.ldx;
     const auto store = [&](int r, int c, const float (&v)[4]) {  // columns c .. c + 3 of X
         if (r >= g.m || c >= g.n) return;
-        *reinterpret_cast<uint2 *>(g.x[0] + base + (int64_t)r * g.ldx + c) =
-            make_uint2(pack(v[0], v[1]), pack(v[2], v[3]));
-        g.wide[((int64_t)(matrix * g.blocks_down + r / 32) * g.blocks_across + c / 32) * kBlockQuads +
-               c % 32 / 4 * 32 + r % 32] = make_float4(v[0], v[1], v[2], v[3]);
+        const uint32_t h0 = pack(v[0], v[1]), h1 = pack(v[2], v[3]);
+        const float2 a = unpack(h0), z = unpack(h1);
+        *reinterpret_cast<uint2 *>(g.x[0] + base + (int64_t)r * g.ldx + c) = make_uint2(h0, h1);
+        uint4 *rest = g.rest + ((int64_t)(matrix * g.blocks_down + r / 32) * g.blocks_across +
+                                c / 32) * kBlockPieces + c % 32 / 8 * 32 + r % 32;
+        reinterpret_cast<uint2 *>(rest)[c % 8 / 4] =
+            make_uint2(pack(v[0] - a.x, v[1] - a.y), pack(v[2] - z.x, v[3] - z.y));
     };
     if (s.by4) {
 #pragma unroll

@@ -10,9 +10,9 @@
 namespace aloco {
 
 // Matrices of one shape in a pass.  X is the matrix with its smaller side as
-// rows (m <= n), kept twice: in fp16 row by row for the products, and in fp32 for
-// what multiplies X itself, in blocks of 32 x 32 laid out as the epilogue's
-// threads hold them.  A = X X^T and P = b A + c A A are m x m in fp16 with zeros
+// rows (m <= n), as a sum of two fp16 values: the larger ones row by row, whose
+// products are taken, and what they leave, which only what multiplies X itself
+// sees, in blocks of 32 x 32 laid out as the epilogue's threads hold them.  A = X X^T and P = b A + c A A are m x m in fp16 with zeros
 // on the diagonal, which is kept in fp32 beside them.  Rows lie ldx and lda
 // elements apart (multiples of 8).
 struct OrthoGroup {
@@ -27,7 +27,7 @@ struct OrthoGroup {
     int chunks, chunk;               // norm blocks of a matrix, elements of each
     int norm0, prep0;                // the group's first block
     __half *x[2], *a, *p;
-    float4 *wide;                    // X in fp32, kBlockQuads a block
+    uint4 *rest;                     // X - x, kBlockPieces a block: 8 columns of a row each
     int blocks_down, blocks_across;  // of a matrix
     float *diag;                     // A's diagonal
     float *lead;                     // a + P's diagonal: what multiplies X itself
@@ -37,7 +37,7 @@ struct OrthoGroup {
 constexpr int kOrthoGroups = 16;     // groups of a pass
 constexpr int kOrthoMatrices = 1024; // places of a pass (a worker's)
 
-constexpr int kBlockQuads = 32 * 32 / 4;
+constexpr int kBlockPieces = 32 * 32 / 8;
 
 // X is held times 2^8, so that fp16 keeps its values of any realistic size in
 // its normal range (its largest value is at most about 1.2).

@@ -20,16 +20,16 @@ def exact(u, steps=5, eps=1e-7, coefficients=None):
 
 
 def rounded(u, steps=5, eps=1e-7, coefficients=None):
-    """The same with X (times 2^8) in fp32 beside its fp16 values, whose products are
-    taken, and A and b A + c A A in fp16 but for their diagonals."""
+    """The same with X (times 2^8) as a sum of two fp16 values, the products of the
+    larger, and A and b A + c A A in fp16 but for their diagonals."""
     coefficients = coefficients or [COEFFICIENTS] * steps
     u = u.double()
     if u.shape[0] > u.shape[1]:
         return rounded(u.T, steps, eps, coefficients).T
     x = 256 * u / (torch.linalg.matrix_norm(u) + eps)
     for a, b, c in coefficients:
-        x = x.float().double()
         hi = x.half().double()
+        x = hi + (x - hi).half().double()
         g = hi @ hi.T / 65536
         d = g.diagonal().float().double()
         g = (g - torch.diag(g.diagonal())).half().double()
