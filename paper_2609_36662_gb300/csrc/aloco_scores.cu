@@ -8,8 +8,10 @@
 namespace aloco {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
+constexpr int kThreads = 256;        // of a CTA
+#ifndef ALOCO_SC_MINB
+#define ALOCO_SC_MINB 4
+#endif
 constexpr int kBatch = 4;            // units of a thread in flight
 constexpr int kMaxSplit = 8;         // CTAs of a row
 constexpr int kMostFound = 512;      // values collected for the best ones
@@ -23,6 +25,24 @@ __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// Two at a time.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(r)
+        : "l"(*reinterpret_cast<unsigned long long *>(&a)),
+          "l"(*reinterpret_cast<unsigned long long *>(&b)),
+          "l"(*reinterpret_cast<unsigned long long *>(&c)));
+    return *reinterpret_cast<float2 *>(&r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;"
+        : "=l"(r)
+        : "l"(*reinterpret_cast<unsigned long long *>(&a)),
+          "l"(*reinterpret_cast<unsigned long long *>(&b)));
+    return *reinterpret_cast<float2 *>(&r);
 }
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;
@@ -67,7 +87,7 @@ struct Row {
     // the raw unit; what is not of the row is -inf
     __device__ __forceinline__ uint4 load(int u, int end) const {
         if (u >= full0 && u < full1 && u < end)
-            return __ldcs(reinterpret_cast<const uint4 *>(unit0) + u);
+            return reinterpret_cast<const uint4 *>(unit0)[u];
         uint32_t w[4];
         const uint32_t low = kBf16 ? 0xff80ff80u : 0xff800000u;
 #pragma unroll
@@ -101,6 +121,23 @@ struct Row {
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(w[i]);
         }
+    }
+    // values below -2^96 raised to it, -inf among them, so that products with 0 are
+    // 0 (a row of nothing else is a far one)
+    static __device__ __forceinline__ uint4 raised(const uint4 &q) {
+        uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (kBf16) {
+                const uint32_t low = 0xef80ef80u;
+                const __nv_bfloat162 x = __hmax2(*reinterpret_cast<const __nv_bfloat162 *>(&w[i]),
+                                                 *reinterpret_cast<const __nv_bfloat162 *>(&low));
+                w[i] = *reinterpret_cast<const uint32_t *>(&x);
+            } else {
+                w[i] = __float_as_uint(fmaxf(__uint_as_float(w[i]), -0x1p96f));
+            }
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
     }
     // the largest value (NaN if there is one)
     static __device__ __forceinline__ float largest(const uint4 (&q)[kBatch]) {
@@ -176,89 +213,148 @@ __device__ __forceinline__ T peer(const T &mine, int rank) {
     }
 }
 
-struct Found {
-    unsigned long long value[kMostFound];
-    int n;
-    int list[kThreads], listed;
-    unsigned long long warp_best[kWarps];
+// A group of threads that takes a row together: a CTA, or a warp of it.
+template <int kGroup>
+struct Group {
+    static constexpr int kWarps = kGroup / 32;
+    static __device__ __forceinline__ int thread() { return threadIdx.x % kGroup; }
+    static __device__ __forceinline__ int index() { return threadIdx.x / kGroup; }
+    static __device__ __forceinline__ void sync() {
+        if constexpr (kGroup == 32)
+            __syncwarp();
+        else
+            __syncthreads();
+    }
+    static __device__ __forceinline__ int count(bool is) {
+        if constexpr (kGroup == 32)
+            return __popc(__ballot_sync(~0u, is));
+        else
+            return __syncthreads_count(is);
+    }
 };
 
-// The values of the listed threads at or above `limit`, as (order, ~index).
-template <bool kBf16>
-__device__ __forceinline__ void collect(const Row<kBf16> &row, int u0, int u1, unsigned limit,
-                                        Found &f) {
-    constexpr int N = Row<kBf16>::N;
-    const int lane = threadIdx.x % 32;
-    for (int i = threadIdx.x / 32; i < f.listed; i += kWarps) {
-        for (int u = u0 + f.list[i] + lane * kThreads; u < u1; u += 32 * kThreads) {
-            float v[N];
-            Row<kBf16>::values(row.load(u, u1), v);
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const int j = u * N - row.phase + e;
-                const unsigned o = order(v[e]);
-                if (o < limit || j < 0 || j >= row.vocab) continue;
-                const int at = atomicAdd(&f.n, 1);
-                if (at < kMostFound) f.value[at] = (unsigned long long)o << 32 | (unsigned)~j;
-            }
+template <int kGroup>
+struct Found {
+    static constexpr int kList = 2 * kGroup;
+    unsigned long long value[kMostFound];
+    int n;
+    int list[kList], listed;
+    unsigned low[Group<kGroup>::kWarps];
+    unsigned long long best[Group<kGroup>::kWarps];
+
+    __device__ __forceinline__ void add(unsigned o, int j) {
+        const int at = atomicAdd(&n, 1);
+        if (at < kMostFound) value[at] = (unsigned long long)o << 32 | (unsigned)~j;
+    }
+};
+
+// The largest of a thread's batches, where two of them were, and the third.
+struct Largest {
+    float first = -INFINITY, second = -INFINITY, third = -INFINITY;
+    int at_first = 0, at_second = 0;
+    __device__ __forceinline__ void take(float m, int turn) {
+        if (m > first) {
+            third = second;
+            second = first;
+            at_second = at_first;
+            first = m;
+            at_first = turn;
+        } else if (m > second) {
+            third = second;
+            second = m;
+            at_second = turn;
+        } else {
+            third = fmaxf(third, m);
         }
+    }
+};
+
+// A lower limit that at least k of the row's values reach: the c-th largest of
+// the lanes' maxima in every warp that is full, the least of these.  `mine`: the
+// order of this thread's maximum.
+template <int kGroup>
+__device__ __forceinline__ unsigned lower_limit(unsigned mine, int units, int k,
+                                                Found<kGroup> &f) {
+    using G = Group<kGroup>;
+    const int full = min(units / 32, G::kWarps), lane = threadIdx.x % 32;
+    unsigned x = mine, c = 0;
+    if (full > 0)
+        for (int i = (k + full - 1) / full; i > 0; --i) {
+            c = __reduce_max_sync(~0u, x);
+            if (lane == __ffs(__ballot_sync(~0u, x == c)) - 1) x = 0;
+        }
+    if constexpr (kGroup == 32) return c;
+    if (lane == 0) f.low[G::thread() / 32] = c;
+    __syncthreads();
+    unsigned low = full > 0 ? f.low[0] : 0;
+    for (int i = 1; i < full; ++i) low = min(low, f.low[i]);
+    return low;
+}
+
+// The values of a unit at or above `limit`, as (order, ~index).
+template <bool kBf16, int kGroup>
+__device__ __forceinline__ void collect(const Row<kBf16> &row, int u, int u1, unsigned limit,
+                                        Found<kGroup> &f) {
+    constexpr int N = Row<kBf16>::N;
+    float v[N];
+    Row<kBf16>::values(row.load(u, u1), v);
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const int j = u * N - row.phase + e;
+        const unsigned o = order(v[e]);
+        if (o >= limit && u < u1 && j >= 0 && j < row.vocab) f.add(o, j);
     }
 }
 
-// The k best values of units [u0, u1), of which this thread's largest has order
-// `mine`.  A limit that at least k threads' largest values reach leaves few
-// values above it; only threads with one there are looked at again.
-template <bool kBf16>
-__device__ __forceinline__ void find_best(const Row<kBf16> &row, int u0, int u1, int k,
-                                          unsigned mine, unsigned largest, Found &f,
-                                          unsigned long long *best) {
-    const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
-    // bisection between an order that all reach and one that fewer than k do
-    __shared__ unsigned low_of[kWarps];
-    const unsigned low = __reduce_min_sync(~0u, mine);
-    if (lane == 0) low_of[warp] = low;
-    if (tid < k) best[tid] = 0;
-    __syncthreads();
-    unsigned lo = low_of[0], hi = largest;
-    for (int i = 1; i < kWarps; ++i) lo = min(lo, low_of[i]);
-    // (the largest value alone may be reached by k threads)
-    if (__syncthreads_count(mine >= hi) >= k) lo = hi;
-    int slack = 8;
-    for (;;) {
-        while (hi - lo > 1) {
-            const unsigned mid = lo + (hi - lo) / 2;
-            const int c = __syncthreads_count(mine >= mid);
-            if (c >= k) {
-                lo = mid;
-                if (c <= k + slack) break;
-            } else {
-                hi = mid;
-            }
-        }
-        const unsigned limit = slack ? lo : lo + 1;
-        if (tid == 0) f.n = f.listed = 0;
-        __syncthreads();
-        if (mine >= limit) f.list[atomicAdd(&f.listed, 1)] = tid;
-        __syncthreads();
-        collect(row, u0, u1, limit, f);
-        __syncthreads();
-        if (f.n <= kMostFound || !slack) break;
-        // too many: most of them are equal to the limit.  The exact one, and
-        // those above it first.
-        slack = 0;
-        hi = largest;
-        if (lo != hi && __syncthreads_count(mine >= hi) >= k) lo = hi;
-        __syncthreads();
+// Every collected value's place is the number of larger ones.
+template <int kGroup>
+__device__ __forceinline__ void place(const Found<kGroup> &f, int n, int k,
+                                      unsigned long long *best) {
+    for (int i = Group<kGroup>::thread(); i < n; i += kGroup) {
+        const unsigned long long v = f.value[i];
+        int above = 0;
+        for (int j = 0; j < n; ++j) above += f.value[j] > v;
+        if (above < k) best[above] = v;
     }
-    const int n = f.n;
-    if (n <= kMostFound) {
-        for (int i = tid; i < n; i += kThreads) {
-            const unsigned long long v = f.value[i];
-            int above = 0;
-            for (int j = 0; j < n; ++j) above += f.value[j] > v;
-            if (above < k) best[above] = v;
-        }
-        if (!slack && n < k && warp == 0) {  // the rest are the first of those equal to the limit
+}
+
+// The k best values of units [u0, u1) where a first limit leaves too many (equal
+// values throughout; everything worth having in few places): of the threads' maxima (`mine`) an exact limit that k of them reach is found by
+// bisection, and threads above it are read again.
+template <bool kBf16, int kGroup>
+__device__ __noinline__ void find_best(const Row<kBf16> &row, int u0, int u1, int k, unsigned mine,
+                                       unsigned largest, Found<kGroup> &f,
+                                       unsigned long long *best) {
+    using G = Group<kGroup>;
+    const int tid = G::thread(), lane = tid % 32, warp = tid / 32;
+    const unsigned low = __reduce_min_sync(~0u, mine);
+    if (lane == 0) f.low[warp] = low;
+    G::sync();
+    unsigned lo = f.low[0], hi = largest;
+    for (int i = 1; i < G::kWarps; ++i) lo = min(lo, f.low[i]);
+    // lo: an order that k threads reach, hi: one that fewer do
+    if (G::count(mine >= hi) >= k) lo = hi;
+    while (hi - lo > 1) {
+        const unsigned mid = lo + (hi - lo) / 2;
+        if (G::count(mine >= mid) >= k)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    for (int above = 0; above < 2; ++above) {   // all that reach it; those above it
+        G::sync();
+        if (tid == 0) f.n = f.listed = 0;
+        G::sync();
+        if (mine >= lo + above) f.list[atomicAdd(&f.listed, 1)] = tid;
+        G::sync();
+        for (int i = warp; i < f.listed; i += G::kWarps)
+            for (int u = u0 + f.list[i] + lane * kGroup; u < u1; u += 32 * kGroup)
+                collect<kBf16, kGroup>(row, u, u1, lo + above, f);
+        G::sync();
+        const int n = f.n;
+        if (n > kMostFound) continue;
+        place(f, n, k, best);
+        if (above && n < k && warp == 0) {  // the rest are the first of those equal to it
             int have = n;
             const int from = max(0, u0 * Row<kBf16>::N - row.phase);
             const int to = min(row.vocab, u1 * Row<kBf16>::N - row.phase);
@@ -270,14 +366,14 @@ __device__ __forceinline__ void find_best(const Row<kBf16> &row, int u0, int u1,
                 have += __popc(which);
             }
         }
-        __syncthreads();
+        G::sync();
         return;
     }
     // many different values in few threads: one after another
     unsigned long long below = ~0ull;
     for (int i = 0; i < k; ++i) {
         unsigned long long top = 0;
-        for (int u = u0 + tid; u < u1; u += kThreads) {
+        for (int u = u0 + tid; u < u1; u += kGroup) {
             float v[Row<kBf16>::N];
             Row<kBf16>::values(row.load(u, u1), v);
 #pragma unroll
@@ -293,28 +389,34 @@ __device__ __forceinline__ void find_best(const Row<kBf16> &row, int u0, int u1,
             const unsigned long long o = __shfl_xor_sync(~0u, top, d);
             top = o > top ? o : top;
         }
-        if (lane == 0) f.warp_best[warp] = top;
-        __syncthreads();
-        for (int w = 0; w < kWarps; ++w) top = f.warp_best[w] > top ? f.warp_best[w] : top;
+        if (lane == 0) f.best[warp] = top;
+        G::sync();
+        for (int w = 0; w < G::kWarps; ++w) top = f.best[w] > top ? f.best[w] : top;
         if (tid == 0) best[i] = top;
         below = top;
-        __syncthreads();
+        G::sync();
     }
 }
 
-// A row by a CTA or a cluster of them, read once: every thread keeps its
-// maximum and its sums to a whole reference.
-template <bool kBf16, bool kTop>
-__global__ void __launch_bounds__(kThreads)
+// A row by a warp, a CTA or a cluster of them, read once: every thread keeps its
+// maxima and its sums to a whole reference.  For the alternatives the maxima give
+// a limit that k values reach, and the few batches that reach it are read again.
+template <bool kBf16, bool kTop, int kGroup>
+__global__ void __launch_bounds__(kThreads, ALOCO_SC_MINB)
     token_scores_kernel(const __grid_constant__ ScoresArgs a, int split) {
-    constexpr int N = Row<kBf16>::N;
-    __shared__ Share share;
-    __shared__ Found found;
-    __shared__ float warp_ref[kWarps], warp_z[kWarps], warp_s[kWarps];
-    __shared__ unsigned warp_top[kWarps];
-    const int64_t r = blockIdx.x / split;
+    using G = Group<kGroup>;
+    constexpr int N = Row<kBf16>::N, kGroups = kThreads / kGroup, kWarps = G::kWarps;
+    __shared__ Share shares[kGroups];
+    __shared__ Found<kGroup> founds[kTop ? kGroups : 1];
+    __shared__ float warp_refs[kGroups][kWarps], warp_zs[kGroups][kWarps], warp_ss[kGroups][kWarps];
+    __shared__ unsigned warp_tops[kGroups][kWarps];
+    const int group = G::index();
+    Share &share = shares[group];
+    Found<kGroup> &found = founds[kTop ? group : 0];
+    const int64_t r = kGroup == 32 ? (int64_t)blockIdx.x * kGroups + group : blockIdx.x / split;
     const int rank = split > 1 ? (int)(blockIdx.x % split) : 0;
-    const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
+    const int tid = G::thread(), lane = tid % 32, warp = tid / 32;
+    if (r >= a.n) return;
     const int64_t target = load_index(a.target, a.target_bytes, r);
     if (target < 0) {
         if (rank) return;
@@ -334,42 +436,59 @@ __global__ void __launch_bounds__(kThreads)
     const int u0 = min(row.units, rank * each), u1 = min(row.units, u0 + each);
 
     Sums sums{-kFar, 0.f, 0.f};
-    float top = -INFINITY;
+    Largest large;
+    bool nan = false;
     const auto pass = [&](auto term) {
-        for (int u = u0 + tid; u < u1; u += kBatch * kThreads) {
+        int turn = 0;
+        for (int u = u0 + tid; u - tid < u1; u += kBatch * kGroup, ++turn) {
             uint4 q[kBatch];
 #pragma unroll
-            for (int b = 0; b < kBatch; ++b) q[b] = row.load(u + b * kThreads, u1);
-            term(q);
+            for (int b = 0; b < kBatch; ++b) q[b] = row.load(u + b * kGroup, u1);
+            term(q, u, turn);
         }
     };
-    pass([&](const uint4 (&q)[kBatch]) {
+    pass([&](const uint4 (&q)[kBatch], int, int turn) {
         const float m = Row<kBf16>::largest(q), need = ceilf(m * a.scale);
-        top = max_nan(top, m);
+        nan |= m != m;
+        large.take(m, turn);
         if (need > sums.ref) sums.refer(need);
-        float z = 0.f, s = 0.f;
+        float2 z = {0.f, 0.f}, s = {0.f, 0.f};
+        const float2 scale = {a.scale, a.scale}, ref = {-sums.ref, -sums.ref};
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
             float v[N];
-            Row<kBf16>::values(q[b], v);
+            Row<kBf16>::values(Row<kBf16>::raised(q[b]), v);
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float t = fmaxf(fmaf(v[i], a.scale, -sums.ref), kGone), e = ex2(t);
-                z += e;
-                s = fmaf(t, e, s);
+            for (int i = 0; i < N; i += 2) {
+                // (2^t is 0 where x was raised: t is below -2^60 there)
+                const float2 t = fma2({v[i], v[i + 1]}, scale, ref), e = {ex2(t.x), ex2(t.y)};
+                z = add2(z, e);
+                s = fma2(t, e, s);
             }
         }
-        sums.z += z;
-        sums.s += s;
+        sums.z += z.x + z.y;
+        sums.s += s.x + s.y;
     });
 
-    // the CTA's, then the cluster's
-    const unsigned mine = order(top);
+    // the group's, then the cluster's
+    const unsigned mine = nan ? ~0u : order(large.first);
     const auto combine = [&] {
         const unsigned high = __reduce_max_sync(~0u, mine);
         const int ref = __reduce_max_sync(~0u, (int)fminf(sums.ref, 2.f * kFar));
         sums.refer((float)ref);
         const float z = warp_sum(sums.z), s = warp_sum(sums.s);
+        if constexpr (kGroup == 32) {
+            if (lane == 0) {
+                share.largest = high;
+                share.ref = (float)ref;
+                share.z = z;
+                share.s = s;
+            }
+            __syncwarp();
+            return;
+        }
+        float *warp_ref = warp_refs[group], *warp_z = warp_zs[group], *warp_s = warp_ss[group];
+        unsigned *warp_top = warp_tops[group];
         if (lane == 0) {
             warp_top[warp] = high;
             warp_ref[warp] = (float)ref;
@@ -398,9 +517,39 @@ __global__ void __launch_bounds__(kThreads)
         }
         __syncthreads();
     };
+    if constexpr (kTop) {
+        if (tid < a.top) share.best[tid] = 0;
+        if (tid == 0) found.n = found.listed = 0;
+    }
     combine();
     if constexpr (kTop) {
-        if (a.top) find_best(row, u0, u1, a.top, mine, share.largest, found, share.best);
+        const unsigned limit = lower_limit<kGroup>(mine, u1 - u0, a.top, found);
+        constexpr int kList = Found<kGroup>::kList;
+        if (mine >= limit) {
+            const int turns = (u1 - u0 + kBatch * kGroup - 1) / (kBatch * kGroup);
+            const bool all = order(large.third) >= limit && turns > 2;
+            const int n = all ? turns : turns > 1 && order(large.second) >= limit ? 2 : 1;
+            const int at = atomicAdd(&found.listed, n);
+            for (int i = 0; i < n && at + i < kList; ++i)
+                found.list[at + i] =
+                    tid | (all ? i : i ? large.at_second : large.at_first) << 16;
+        }
+        G::sync();
+        const int listed = found.listed;
+        if (listed <= kList)
+            for (int i = tid; i < listed * kBatch; i += kGroup) {
+                const int entry = found.list[i / kBatch];
+                collect<kBf16, kGroup>(row, u0 + (entry & 0xffff) +
+                                                ((entry >> 16) * kBatch + i % kBatch) * kGroup,
+                                       u1, limit, found);
+            }
+        G::sync();
+        const int n = found.n;
+        if (listed > kList || n > kMostFound)
+            find_best<kBf16, kGroup>(row, u0, u1, a.top, mine, share.largest, found, share.best);
+        else
+            place(found, n, a.top, share.best);
+        G::sync();
     }
     unsigned high = share.largest;
     if (split > 1) {
@@ -413,7 +562,7 @@ __global__ void __launch_bounds__(kThreads)
         far = true;
         if (split > 1) cluster_sync();  // (all have read)
         sums = {0.f, 0.f, 0.f};
-        pass([&](const uint4 (&q)[kBatch]) {
+        pass([&](const uint4 (&q)[kBatch], int, int) {
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
                 float v[N];
@@ -501,12 +650,15 @@ __device__ __forceinline__ void store_one(char *p, float v) {
 
 // A row's units, read and written once; the token's and the alternatives'
 // elements are worked out before and written last.
-template <bool kBf16>
+template <bool kBf16, int kGroup>
 __global__ void __launch_bounds__(kThreads)
     token_scores_grad_kernel(const __grid_constant__ ScoresArgs a, int split) {
+    using G = Group<kGroup>;
     constexpr int N = Row<kBf16>::N, kSize = kBf16 ? 2 : 4;
-    const int64_t r = blockIdx.x / split;
-    const int rank = blockIdx.x % split, tid = threadIdx.x;
+    const int64_t r = kGroup == 32 ? (int64_t)blockIdx.x * (kThreads / kGroup) + G::index()
+                                   : blockIdx.x / split;
+    const int rank = split > 1 ? (int)(blockIdx.x % split) : 0, tid = G::thread();
+    if (r >= a.n) return;
     const int64_t target = load_index(a.target, a.target_bytes, r);
     const bool live = target >= 0;
     const Row<kBf16> row(a.x.data + row_offset(a.x, r) * kSize, a.vocab);
@@ -515,19 +667,53 @@ __global__ void __launch_bounds__(kThreads)
     const int each = (to.units + split - 1) / split;
     const int u0 = min(to.units, rank * each), u1 = min(to.units, u0 + each);
     const int j0 = max(0, u0 * N - to.phase), j1 = min(a.vocab, u1 * N - to.phase);
+    const bool same = row.phase == to.phase;
+
+    uint4 q[kBatch];                 // the first units come while the factors do
+    const auto load = [&](int u) {
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b)
+            q[b] = live ? row.load(u + b * kGroup, u1) : make_uint4(0, 0, 0, 0);
+    };
+    if (same) load(u0 + tid);
 
     Slope f{0.f, a.scale, 0.f, 0.f};
-    int special = -1;                // this thread's element, if it is the first for it
-    float value = 0.f;
+    int special = -1, spare = -1;    // this thread's elements, if it is the first for them
+    float value = 0.f, spare_value = 0.f;
     if (live) {
         const float2 st = a.stats_in[r];
-        const float by_logp = a.d_logp ? a.d_logp[r] : 0.f;
-        float sum = by_logp;
-        if (a.d_top)
-            for (int i = 0; i < a.top; ++i) {
-                const int id = a.ids_in[r * a.top + i];
-                if (id >= 0 && id < a.vocab) sum += a.d_top[r * a.top + i];
+        const int n = 1 + (a.d_top ? a.top : 0);
+        // lane i has the i-th element's index and gradient (lane 0 the 32nd
+        // alternative's too)
+        const int lane = threadIdx.x % 32;
+        int id = -1, id32 = -1;
+        float by = 0.f, by32 = 0.f;
+        if (lane == 0) {
+            id = (int)min(target, (int64_t)a.vocab);
+            by = a.d_logp ? a.d_logp[r] : 0.f;
+            if (n == 33) {
+                id32 = a.ids_in[r * 32 + 31];
+                by32 = a.d_top[r * 32 + 31];
             }
+        } else if (lane < n) {
+            id = a.ids_in[r * a.top + lane - 1];
+            by = a.d_top[r * a.top + lane - 1];
+        }
+        id32 = __shfl_sync(~0u, id32, 0);
+        by32 = __shfl_sync(~0u, by32, 0);
+        // sums in the order of the elements: of all, and of those with this
+        // thread's index
+        const int j = tid == 32 ? id32 : id;
+        bool mine = tid < n && j >= j0 && j < j1;
+        float sum = 0.f, add = 0.f;
+        for (int i = 0; i < n; ++i) {
+            const int jj = i < 32 ? __shfl_sync(~0u, id, i) : id32;
+            const float g = i < 32 ? __shfl_sync(~0u, by, i) : by32;
+            if (i == 0 || (jj >= 0 && jj < a.vocab)) sum += g;
+            if (jj != j) continue;
+            if (i < tid) mine = false;
+            add += g;
+        }
         f.m = st.x;
         float per = 0.f;             // d_entropy (H - log z)
         if (a.d_entropy) {
@@ -536,35 +722,30 @@ __global__ void __launch_bounds__(kThreads)
             f.c1 = -by_h * kLn2 * a.inv_temp / st.y;
         }
         f.c0 = target < a.vocab ? -(sum + per) * a.inv_temp / st.y : NAN;
-        const int n = 1 + (a.d_top ? a.top : 0);
-        if (tid < n) {
-            const auto id = [&](int i) -> int {
-                return i == 0 ? (int)min(target, (int64_t)a.vocab) : a.ids_in[r * a.top + i - 1];
-            };
-            const int j = id(tid);
-            bool mine = j >= j0 && j < j1;
-            float add = 0.f;
-            for (int i = 0; i < n; ++i) {
-                if (id(i) != j) continue;
-                if (i < tid) mine = false;
-                add += i == 0 ? by_logp : a.d_top[r * a.top + i - 1];
+        if (mine) {
+            special = j;
+            value = fmaf(add, a.inv_temp, f(row.at(j)));
+        }
+        // (a warp's 33rd element has no lane of its own)
+        if (kGroup == 32 && n == 33 && lane == 0) {
+            bool first = id32 >= j0 && id32 < j1;
+            for (int i = 0; i < 32; ++i) {
+                const int jj = i ? a.ids_in[r * 32 + i - 1] : id;
+                if (jj == id32) first = false;
             }
-            if (mine) {
-                special = j;
-                value = fmaf(add, a.inv_temp, f(row.at(j)));
+            if (first) {
+                spare = id32;
+                spare_value = fmaf(by32, a.inv_temp, f(row.at(id32)));
             }
         }
     }
-    __syncthreads();                 // before the gradient covers the logits
-    if (row.phase == to.phase) {
-        for (int u = u0 + tid; u < u1; u += kBatch * kThreads) {
-            uint4 q[kBatch];
-#pragma unroll
-            for (int b = 0; b < kBatch; ++b)
-                q[b] = live ? row.load(u + b * kThreads, u1) : make_uint4(0, 0, 0, 0);
+    G::sync();                       // before the gradient covers the logits
+    if (same) {
+        for (int u = u0 + tid; u < u1; u += kBatch * kGroup) {
+            if (u != u0 + tid) load(u);
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
-                const int w = u + b * kThreads;
+                const int w = u + b * kGroup;
                 if (w >= u1) break;
                 float v[N];
                 Row<kBf16>::values(q[b], v);
@@ -594,19 +775,22 @@ __global__ void __launch_bounds__(kThreads)
             }
         }
     } else {
-        for (int j = j0 + tid; j < j1; j += kThreads)
+        for (int j = j0 + tid; j < j1; j += kGroup)
             store_one<kBf16>(out + (int64_t)j * kSize, live ? f(row.at(j)) : 0.f);
     }
     if (live) {
-        __syncthreads();
+        G::sync();
         if (special >= 0) store_one<kBf16>(out + (int64_t)special * kSize, value);
+        if (spare >= 0) store_one<kBf16>(out + (int64_t)spare * kSize, spare_value);
     }
 }
 
 template <typename K>
-cudaError_t launch(K kernel, const ScoresArgs &a, int split, bool cluster, cudaStream_t stream) {
+cudaError_t launch(K kernel, const ScoresArgs &a, int group, int split, bool cluster,
+                   cudaStream_t stream) {
     cudaLaunchConfig_t c{};
-    c.gridDim = dim3((unsigned)(a.n * split));
+    const int rows = kThreads / group;
+    c.gridDim = dim3((unsigned)((a.n + rows - 1) / rows * split));
     c.blockDim = dim3(kThreads);
     c.stream = stream;
     cudaLaunchAttribute at[1];
@@ -617,30 +801,57 @@ cudaError_t launch(K kernel, const ScoresArgs &a, int split, bool cluster, cudaS
     return cudaLaunchKernelEx(&c, kernel, a, split);
 }
 
-// CTAs of a row: as many as give every SM four, of at least 512 units each.
-int split_of(const ScoresArgs &a, int sm_count) {
+// Who takes a row: a warp, a CTA, or a cluster of them.
+struct Shape {
+    int group, split;
+};
+#ifndef ALOCO_SC_WARP
+#define ALOCO_SC_WARP 1024
+#endif
+#ifndef ALOCO_SC_WAVES
+#define ALOCO_SC_WAVES 4
+#endif
+#ifndef ALOCO_SC_UNITS
+#define ALOCO_SC_UNITS 512
+#endif
+Shape shape_of(const ScoresArgs &a, int sm_count) {
     const int units = a.vocab / (a.bf16 ? 8 : 4);
+    if (units <= ALOCO_SC_WARP && (units <= 128 || a.n >= 8 * (int64_t)sm_count)) return {32, 1};
     int split = 1;
-    while (split < kMaxSplit && a.n * split < 4 * (int64_t)sm_count && units / (2 * split) >= 512)
+    while (split < kMaxSplit && a.n * split < ALOCO_SC_WAVES * (int64_t)sm_count &&
+           units / (2 * split) >= ALOCO_SC_UNITS)
         split *= 2;
-    return split;
+    return {kThreads, split};
+}
+
+template <bool kBf16, bool kTop>
+cudaError_t launch_scores(const ScoresArgs &a, const Shape &s, cudaStream_t stream) {
+    return s.group == 32
+               ? launch(token_scores_kernel<kBf16, kTop, 32>, a, 32, 1, false, stream)
+               : launch(token_scores_kernel<kBf16, kTop, kThreads>, a, kThreads, s.split, true,
+                        stream);
+}
+template <bool kBf16>
+cudaError_t launch_grad(const ScoresArgs &a, const Shape &s, cudaStream_t stream) {
+    return s.group == 32 ? launch(token_scores_grad_kernel<kBf16, 32>, a, 32, 1, false, stream)
+                         : launch(token_scores_grad_kernel<kBf16, kThreads>, a, kThreads, s.split,
+                                  false, stream);
 }
 
 }  // namespace
 
 cudaError_t launch_token_scores(const ScoresArgs &a, int sm_count, cudaStream_t stream) {
-    const int split = split_of(a, sm_count);
+    const Shape s = shape_of(a, sm_count);
     if (a.bf16)
-        return a.top ? launch(token_scores_kernel<true, true>, a, split, true, stream)
-                     : launch(token_scores_kernel<true, false>, a, split, true, stream);
-    return a.top ? launch(token_scores_kernel<false, true>, a, split, true, stream)
-                 : launch(token_scores_kernel<false, false>, a, split, true, stream);
+        return a.top ? launch_scores<true, true>(a, s, stream)
+                     : launch_scores<true, false>(a, s, stream);
+    return a.top ? launch_scores<false, true>(a, s, stream)
+                 : launch_scores<false, false>(a, s, stream);
 }
 
 cudaError_t launch_token_scores_grad(const ScoresArgs &a, int sm_count, cudaStream_t stream) {
-    const int split = split_of(a, sm_count);
-    return a.bf16 ? launch(token_scores_grad_kernel<true>, a, split, false, stream)
-                  : launch(token_scores_grad_kernel<false>, a, split, false, stream);
+    const Shape s = shape_of(a, sm_count);
+    return a.bf16 ? launch_grad<true>(a, s, stream) : launch_grad<false>(a, s, stream);
 }
 
 }  // namespace aloco
