@@ -9,9 +9,6 @@ namespace aloco {
 namespace {
 
 constexpr int kThreads = 256;        // of a CTA
-#ifndef ALOCO_SC_MINB
-#define ALOCO_SC_MINB 4
-#endif
 constexpr int kBatch = 4;            // units of a thread in flight
 constexpr int kMaxSplit = 8;         // CTAs of a row
 constexpr int kMostFound = 512;      // values collected for the best ones
@@ -270,18 +267,18 @@ struct Largest {
 };
 
 // A lower limit that at least k of the row's values reach: the c-th largest of
-// the lanes' maxima in every warp that is full, the least of these.  `mine`: the
-// order of this thread's maximum.
+// the lanes' batches (up to three of a lane) in every warp that is full, the least
+// of these.  `mine`: the order of this thread's maximum.
 template <int kGroup>
-__device__ __forceinline__ unsigned lower_limit(unsigned mine, int units, int k,
-                                                Found<kGroup> &f) {
+__device__ __forceinline__ unsigned lower_limit(unsigned mine, const Largest &large, int units,
+                                                int k, Found<kGroup> &f) {
     using G = Group<kGroup>;
     const int full = min(units / 32, G::kWarps), lane = threadIdx.x % 32;
-    unsigned x = mine, c = 0;
+    unsigned x = mine, x2 = order(large.second), x3 = order(large.third), c = 0;
     if (full > 0)
         for (int i = (k + full - 1) / full; i > 0; --i) {
             c = __reduce_max_sync(~0u, x);
-            if (lane == __ffs(__ballot_sync(~0u, x == c)) - 1) x = 0;
+            if (lane == __ffs(__ballot_sync(~0u, x == c)) - 1) x = x2, x2 = x3, x3 = 0;
         }
     if constexpr (kGroup == 32) return c;
     if (lane == 0) f.low[G::thread() / 32] = c;
@@ -402,7 +399,7 @@ __device__ __noinline__ void find_best(const Row<kBf16> &row, int u0, int u1, in
 // maxima and its sums to a whole reference.  For the alternatives the maxima give
 // a limit that k values reach, and the few batches that reach it are read again.
 template <bool kBf16, bool kTop, int kGroup>
-__global__ void __launch_bounds__(kThreads, ALOCO_SC_MINB)
+__global__ void __launch_bounds__(kThreads, kGroup == 32 ? 4 : kTop ? 6 : 5)
     token_scores_kernel(const __grid_constant__ ScoresArgs a, int split) {
     using G = Group<kGroup>;
     constexpr int N = Row<kBf16>::N, kGroups = kThreads / kGroup, kWarps = G::kWarps;
@@ -523,7 +520,7 @@ __global__ void __launch_bounds__(kThreads, ALOCO_SC_MINB)
     }
     combine();
     if constexpr (kTop) {
-        const unsigned limit = lower_limit<kGroup>(mine, u1 - u0, a.top, found);
+        const unsigned limit = lower_limit<kGroup>(mine, large, u1 - u0, a.top, found);
         constexpr int kList = Found<kGroup>::kList;
         if (mine >= limit) {
             const int turns = (u1 - u0 + kBatch * kGroup - 1) / (kBatch * kGroup);
@@ -801,25 +798,18 @@ cudaError_t launch(K kernel, const ScoresArgs &a, int group, int split, bool clu
     return cudaLaunchKernelEx(&c, kernel, a, split);
 }
 
-// Who takes a row: a warp, a CTA, or a cluster of them.
+// Who takes a row: a warp, a CTA, or `split` CTAs.
 struct Shape {
     int group, split;
 };
-#ifndef ALOCO_SC_WARP
-#define ALOCO_SC_WARP 1024
-#endif
-#ifndef ALOCO_SC_WAVES
-#define ALOCO_SC_WAVES 4
-#endif
-#ifndef ALOCO_SC_UNITS
-#define ALOCO_SC_UNITS 512
-#endif
-Shape shape_of(const ScoresArgs &a, int sm_count) {
+Shape shape_of(const ScoresArgs &a, int sm_count, int ctas_per_sm) {
     const int units = a.vocab / (a.bf16 ? 8 : 4);
-    if (units <= ALOCO_SC_WARP && (units <= 128 || a.n >= 8 * (int64_t)sm_count)) return {32, 1};
+    // 20000 x 4096 bf16 with 8 alternatives: 52 us by warps, 178 by CTAs; 4000 x 8192:
+    // 26 and 39 us.  Few rows do not fill the SMs with warps.
+    if (units <= 1024 && (units <= 128 || a.n >= 8 * (int64_t)sm_count)) return {32, 1};
     int split = 1;
-    while (split < kMaxSplit && a.n * split < ALOCO_SC_WAVES * (int64_t)sm_count &&
-           units / (2 * split) >= ALOCO_SC_UNITS)
+    while (split < kMaxSplit && a.n * split < ctas_per_sm * (int64_t)sm_count &&
+           units / (2 * split) >= 512)
         split *= 2;
     return {kThreads, split};
 }
@@ -841,7 +831,8 @@ cudaError_t launch_grad(const ScoresArgs &a, const Shape &s, cudaStream_t stream
 }  // namespace
 
 cudaError_t launch_token_scores(const ScoresArgs &a, int sm_count, cudaStream_t stream) {
-    const Shape s = shape_of(a, sm_count);
+    // (clusters wait for one another: only where rows are few)
+    const Shape s = shape_of(a, sm_count, 4);
     if (a.bf16)
         return a.top ? launch_scores<true, true>(a, s, stream)
                      : launch_scores<true, false>(a, s, stream);
@@ -850,7 +841,9 @@ cudaError_t launch_token_scores(const ScoresArgs &a, int sm_count, cudaStream_t 
 }
 
 cudaError_t launch_token_scores_grad(const ScoresArgs &a, int sm_count, cudaStream_t stream) {
-    const Shape s = shape_of(a, sm_count);
+    // parts of a row are their own here, and short CTAs end together: 1533 x 50257
+    // fp32 107 us with 4 an SM, 100 with 32; 111 with 64
+    const Shape s = shape_of(a, sm_count, 32);
     return a.bf16 ? launch_grad<true>(a, s, stream) : launch_grad<false>(a, s, stream);
 }
 
