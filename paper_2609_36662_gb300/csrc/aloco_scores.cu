@@ -8,10 +8,12 @@
 namespace aloco {
 namespace {
 
-constexpr int kThreads = 256;        // of a CTA
+// Threads of a CTA whose groups are a warp, or the CTA itself.
+constexpr int cta_of(int group) { return group == 32 ? 256 : group; }
 constexpr int kBatch = 4;            // units of a thread in flight
 constexpr int kMaxSplit = 8;         // CTAs of a row
 constexpr int kMostFound = 512;      // values collected for the best ones
+static_assert(kMostFound >= kMaxSplit * ALOCO_MAX_TOP, "a cluster's best are joined there");
 constexpr float kLn2 = 0.693147180559945f;
 // The reference of the powers of two: a whole number, so that factors between
 // references are powers of two and no rounding is common to a row's terms.
@@ -398,11 +400,18 @@ __device__ __noinline__ void find_best(const Row<kBf16> &row, int u0, int u1, in
 // A row by a warp, a CTA or a cluster of them, read once: every thread keeps its
 // maxima and its sums to a whole reference.  For the alternatives the maxima give
 // a limit that k values reach, and the few batches that reach it are read again.
+//
+// Bound by HBM; the steps behind a row's last unit (a limit, a few values read
+// again, their order: about 2 us) are hidden by the other CTAs of the SM, so CTAs
+// are small.  8184 x 32000 bf16 with 8 alternatives: 104 us with 11 CTAs of 128
+// threads an SM, 120 with 6 of 256 (77 at the copy rate); 4000 x 128256: 179 and
+// 182 us (152), 170 with 9 CTAs, which take 72 us where 11 take 59 for 1533 x 50257
+// fp32.  Without alternatives 10 are best: 88 and 159 us.
 template <bool kBf16, bool kTop, int kGroup>
-__global__ void __launch_bounds__(kThreads, kGroup == 32 ? 4 : kTop ? 6 : 5)
+__global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kTop ? 11 : 10)
     token_scores_kernel(const __grid_constant__ ScoresArgs a, int split) {
     using G = Group<kGroup>;
-    constexpr int N = Row<kBf16>::N, kGroups = kThreads / kGroup, kWarps = G::kWarps;
+    constexpr int N = Row<kBf16>::N, kGroups = cta_of(kGroup) / kGroup, kWarps = G::kWarps;
     __shared__ Share shares[kGroups];
     __shared__ Found<kGroup> founds[kTop ? kGroups : 1];
     __shared__ float warp_refs[kGroups][kWarps], warp_zs[kGroups][kWarps], warp_ss[kGroups][kWarps];
@@ -603,19 +612,25 @@ __global__ void __launch_bounds__(kThreads, kGroup == 32 ? 4 : kTop ? 6 : 5)
         if constexpr (kTop) {
             // an entry's place among all CTAs' is the number of larger ones
             const int n = split * a.top;
-            unsigned long long v = 0;
-            int place = tid;
-            if (tid < n) v = split == 1 ? share.best[tid] : peer(share.best[tid % a.top], tid / a.top);
             if (split > 1) {
-                if (tid < n) found.value[tid] = v;
+                for (int i = tid; i < n; i += kGroup)
+                    found.value[i] = peer(share.best[i % a.top], i / a.top);
                 __syncthreads();
-                place = 0;
-                for (int i = 0; i < n; ++i) place += found.value[i] > v;
             }
-            if (v && place < a.top) {
-                a.top_ids[r * a.top + place] = bad ? -1 : (int)~(unsigned)v;
-                a.top_logp[r * a.top + place] = bad ? NAN : log_p(unorder((unsigned)(v >> 32)));
+            for (int i = tid; i < n; i += kGroup) {
+                const unsigned long long v = split == 1 ? share.best[i] : found.value[i];
+                int place = i;
+                if (split > 1) {
+                    place = 0;
+                    for (int o = 0; o < n; ++o) place += found.value[o] > v;
+                }
+                if (v && place < a.top) {
+                    a.top_ids[r * a.top + place] = bad ? -1 : (int)~(unsigned)v;
+                    a.top_logp[r * a.top + place] =
+                        bad ? NAN : log_p(unorder((unsigned)(v >> 32)));
+                }
             }
+            if (bad) G::sync();
             // (a row with NaN may have filled fewer)
             if (bad && tid < a.top) {
                 a.top_ids[r * a.top + tid] = -1;
@@ -648,11 +663,11 @@ __device__ __forceinline__ void store_one(char *p, float v) {
 // A row's units, read and written once; the token's and the alternatives'
 // elements are worked out before and written last.
 template <bool kBf16, int kGroup>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(cta_of(kGroup))
     token_scores_grad_kernel(const __grid_constant__ ScoresArgs a, int split) {
     using G = Group<kGroup>;
     constexpr int N = Row<kBf16>::N, kSize = kBf16 ? 2 : 4;
-    const int64_t r = kGroup == 32 ? (int64_t)blockIdx.x * (kThreads / kGroup) + G::index()
+    const int64_t r = kGroup == 32 ? (int64_t)blockIdx.x * (cta_of(kGroup) / kGroup) + G::index()
                                    : blockIdx.x / split;
     const int rank = split > 1 ? (int)(blockIdx.x % split) : 0, tid = G::thread();
     if (r >= a.n) return;
@@ -786,9 +801,9 @@ template <typename K>
 cudaError_t launch(K kernel, const ScoresArgs &a, int group, int split, bool cluster,
                    cudaStream_t stream) {
     cudaLaunchConfig_t c{};
-    const int rows = kThreads / group;
+    const int rows = cta_of(group) / group;
     c.gridDim = dim3((unsigned)((a.n + rows - 1) / rows * split));
-    c.blockDim = dim3(kThreads);
+    c.blockDim = dim3(cta_of(group));
     c.stream = stream;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -802,7 +817,7 @@ cudaError_t launch(K kernel, const ScoresArgs &a, int group, int split, bool clu
 struct Shape {
     int group, split;
 };
-Shape shape_of(const ScoresArgs &a, int sm_count, int ctas_per_sm) {
+Shape shape_of(const ScoresArgs &a, int sm_count, int cta, int ctas_per_sm) {
     const int units = a.vocab / (a.bf16 ? 8 : 4);
     // 20000 x 4096 bf16 with 8 alternatives: 52 us by warps, 178 by CTAs; 4000 x 8192:
     // 26 and 39 us.  Few rows do not fill the SMs with warps.
@@ -811,28 +826,27 @@ Shape shape_of(const ScoresArgs &a, int sm_count, int ctas_per_sm) {
     while (split < kMaxSplit && a.n * split < ctas_per_sm * (int64_t)sm_count &&
            units / (2 * split) >= 512)
         split *= 2;
-    return {kThreads, split};
+    return {cta, split};
 }
 
 template <bool kBf16, bool kTop>
 cudaError_t launch_scores(const ScoresArgs &a, const Shape &s, cudaStream_t stream) {
     return s.group == 32
                ? launch(token_scores_kernel<kBf16, kTop, 32>, a, 32, 1, false, stream)
-               : launch(token_scores_kernel<kBf16, kTop, kThreads>, a, kThreads, s.split, true,
-                        stream);
+               : launch(token_scores_kernel<kBf16, kTop, 128>, a, 128, s.split, true, stream);
 }
 template <bool kBf16>
 cudaError_t launch_grad(const ScoresArgs &a, const Shape &s, cudaStream_t stream) {
     return s.group == 32 ? launch(token_scores_grad_kernel<kBf16, 32>, a, 32, 1, false, stream)
-                         : launch(token_scores_grad_kernel<kBf16, kThreads>, a, kThreads, s.split,
-                                  false, stream);
+                         : launch(token_scores_grad_kernel<kBf16, 256>, a, 256, s.split, false,
+                                  stream);
 }
 
 }  // namespace
 
 cudaError_t launch_token_scores(const ScoresArgs &a, int sm_count, cudaStream_t stream) {
     // (clusters wait for one another: only where rows are few)
-    const Shape s = shape_of(a, sm_count, 4);
+    const Shape s = shape_of(a, sm_count, 128, 8);
     if (a.bf16)
         return a.top ? launch_scores<true, true>(a, s, stream)
                      : launch_scores<true, false>(a, s, stream);
@@ -843,7 +857,7 @@ cudaError_t launch_token_scores(const ScoresArgs &a, int sm_count, cudaStream_t 
 cudaError_t launch_token_scores_grad(const ScoresArgs &a, int sm_count, cudaStream_t stream) {
     // parts of a row are their own here, and short CTAs end together: 1533 x 50257
     // fp32 107 us with 4 an SM, 100 with 32; 111 with 64
-    const Shape s = shape_of(a, sm_count, 32);
+    const Shape s = shape_of(a, sm_count, 256, 32);
     return a.bf16 ? launch_grad<true>(a, s, stream) : launch_grad<false>(a, s, stream);
 }
 
