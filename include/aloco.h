@@ -568,7 +568,8 @@ typedef struct aloco_muon_cfg {
 void aloco_muon_default_cfg(aloco_muon_cfg_t *cfg);
 
 /* Bytes of scratch of a step over these matrices on M replicas (0 where an
- * argument is out of range). */
+ * argument is out of range, and where all matrices are small ones, which need
+ * none: scratch may be NULL then). */
 size_t aloco_muon_scratch_bytes(const aloco_matrix_t *matrices, int64_t n, int M);
 
 /* One step of n matrices on M <= ALOCO_MAX_WORKERS replicas, in place:

@@ -59,19 +59,61 @@ struct Pass {
     size_t bytes = 0;
 };
 
+// Matrices that one kernel takes through all steps, `ctas` to a matrix.
+struct SmallPass {
+    int ctas;
+    std::vector<Part> parts;
+    int places = 0;
+};
+
 struct Plan {
     std::vector<int64_t> place;
     std::vector<Shape> shapes;
     std::vector<Pass> passes;
+    std::vector<SmallPass> small;
     size_t bytes = 0;
 };
 
+// CTAs of a small matrix, a power of two; 0: it is none.
+int small_ctas(const Shape &s, int most) {
+    if (s.m() > kOrthoSmallSide) return 0;
+    for (int c = 1; c <= most; c *= 2)
+        if (s.n() <= (int64_t)c * kOrthoSmallCols) return c;
+    return 0;
+}
+
+// The largest cluster that every device takes, which scratch is reckoned with.
+constexpr int kPortableCtas = 8;
+
 // Shapes in `p` (places set) into passes that keep within kPassBytes, kOrthoGroups
 // and kOrthoMatrices: deep products first, so that the last tiles are short.
-void split(Plan *p, int workers) {
+// Matrices for the small kernel, in clusters of up to `most_ctas`, go by themselves.
+void split(Plan *p, int workers, int most_ctas) {
     std::stable_sort(p->shapes.begin(), p->shapes.end(), [](const Shape &x, const Shape &y) {
         return x.m() != y.m() ? x.m() > y.m() : x.n() > y.n();
     });
+    std::vector<SmallPass> open;     // by cluster size
+    for (int i = 0; i < (int)p->shapes.size(); ++i) {
+        const Shape &s = p->shapes[i];
+        const int ctas = small_ctas(s, most_ctas);
+        if (!ctas) continue;
+        auto at = std::find_if(open.begin(), open.end(),
+                               [&](const SmallPass &x) { return x.ctas == ctas; });
+        if (at != open.end() &&
+            (at->parts.size() == kOrthoGroups || at->places + s.period > kOrthoMatrices)) {
+            p->small.push_back(std::move(*at));
+            open.erase(at);
+            at = open.end();
+        }
+        if (at == open.end()) {
+            open.push_back({ctas, {}, 0});
+            at = open.end() - 1;
+        }
+        at->parts.push_back({i, 0, (int64_t)s.period * workers});
+        at->places += s.period;
+    }
+    for (SmallPass &x : open) p->small.push_back(std::move(x));
+
     Pass pass;
     const auto flush = [&] {
         if (pass.parts.empty()) return;
@@ -81,6 +123,7 @@ void split(Plan *p, int workers) {
     };
     for (int i = 0; i < (int)p->shapes.size(); ++i) {
         const Shape &s = p->shapes[i];
+        if (small_ctas(s, most_ctas)) continue;
         const int64_t total = (int64_t)s.period * workers;
         for (int64_t at = 0; at < total;) {
             if (pass.parts.size() == kOrthoGroups || pass.places + s.period > kOrthoMatrices)
@@ -106,7 +149,7 @@ void split(Plan *p, int workers) {
 }
 
 // Matrices by shape, in the order of their places.
-int plan_matrices(const aloco_matrix_t *mats, int64_t n, int workers, Plan *p) {
+void plan_matrices(const aloco_matrix_t *mats, int64_t n, int workers, int most_ctas, Plan *p) {
     std::vector<int64_t> order;
     for (int64_t i = 0; i < n; ++i)
         if (mats[i].rows > 0 && mats[i].cols > 0) order.push_back(i);
@@ -122,18 +165,17 @@ int plan_matrices(const aloco_matrix_t *mats, int64_t n, int workers, Plan *p) {
         ++p->shapes.back().period;
         p->place.push_back(x.offset);
     }
-    split(p, workers);
-    return ALOCO_OK;
+    split(p, workers, most_ctas);
 }
 
-void plan_batch(int64_t batch, int64_t rows, int64_t cols, Plan *p) {
+void plan_batch(int64_t batch, int64_t rows, int64_t cols, int most_ctas, Plan *p) {
     for (int64_t i = 0; i < batch; ++i) {
         if (p->shapes.empty() || p->shapes.back().period == 256)
             p->shapes.push_back({rows, cols, (int)i, 0});
         ++p->shapes.back().period;
         p->place.push_back(i);
     }
-    split(p, 1);
+    split(p, 1, most_ctas);
 }
 
 int check_side(int64_t rows, int64_t cols, const char *what, int64_t i) {
@@ -212,6 +254,43 @@ void count_tiles(OrthoArgs *a, int sym_ctas, int up_ctas) {
     }
 }
 
+// What both kinds of passes fill in of a group.
+void fill_group(const Plan &plan, const Part &part, int64_t *places, int *n_places,
+                OrthoGroup *g) {
+    const Shape &s = plan.shapes[part.shape];
+    *g = OrthoGroup();
+    g->m = (int)s.m();
+    g->n = (int)s.n();
+    g->rows = (int)s.rows;
+    g->cols = (int)s.cols;
+    g->tall = s.rows > s.cols;
+    g->count = (int)part.count;
+    g->first = *n_places;
+    g->period = s.period;
+    g->skip = (int)part.skip;
+    for (int k = 0; k < s.period; ++k) places[(*n_places)++] = plan.place[s.first + k];
+}
+
+int run_small(const Plan &plan, const SmallPass &pass, const OrthoArgs &base,
+              const double (*coefficients)[3], int steps, const double *shape_step,
+              cudaStream_t stream) {
+    OrthoArgs a = base;
+    a.n_groups = (int)pass.parts.size();
+    a.small_ctas = pass.ctas;
+    a.steps = steps;
+    for (int s = 0; s < steps; ++s)
+        for (int i = 0; i < 3; ++i) a.coef[s][i] = (float)coefficients[s][i];
+    int places = 0, matrices = 0;
+    for (int i = 0; i < a.n_groups; ++i) {
+        fill_group(plan, pass.parts[i], a.place, &places, &a.g[i]);
+        a.g[i].small0 = matrices;
+        matrices += a.g[i].count;
+        a.step[i] = shape_step ? (float)shape_step[pass.parts[i].shape] : 0.f;
+    }
+    const cudaError_t e = launch_ortho_small(a, matrices, stream);
+    return e == cudaSuccess ? ALOCO_OK : cuda_fail(e, "orthogonal factor");
+}
+
 // `base`: the caller's buffers and settings filled in.
 int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base,
              const double (*coefficients)[3], int steps, const double *shape_step,
@@ -231,19 +310,9 @@ int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base,
         const Shape &s = plan.shapes[part.shape];
         OrthoGroup &g = a.g[i];
         const int64_t m = s.m(), n = s.n(), count = part.count;
-        g = OrthoGroup();
-        g.m = (int)m;
-        g.n = (int)n;
+        fill_group(plan, part, a.place, &places, &g);
         g.ldx = (int)s.ldx();
         g.lda = (int)s.lda();
-        g.rows = (int)s.rows;
-        g.cols = (int)s.cols;
-        g.tall = s.rows > s.cols;
-        g.count = (int)count;
-        g.first = places;
-        g.period = s.period;
-        g.skip = (int)part.skip;
-        for (int k = 0; k < s.period; ++k) a.place[places++] = plan.place[s.first + k];
         g.chunk = (int)s.chunk();
         g.chunks = (int)s.chunks();
         g.norm0 = norm;
@@ -306,7 +375,52 @@ int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base,
     return e == cudaSuccess ? ALOCO_OK : cuda_fail(e, "orthogonal factor");
 }
 
+// All of a call's passes.
+int run(const Plan &plan, const OrthoArgs &base, const double (*coefficients)[3], int steps,
+        const double *shape_step, char *scratch, int sm_count, cudaStream_t stream) {
+    OrthoArgs a = base;
+    for (const SmallPass &pass : plan.small) {
+        const int rc = run_small(plan, pass, a, coefficients, steps, shape_step, stream);
+        if (rc != ALOCO_OK) return rc;
+        a.test_stall1 = 0;
+    }
+    for (const Pass &pass : plan.passes) {
+        const int rc = run_pass(plan, pass, a, coefficients, steps, shape_step, scratch, sm_count,
+                                stream);
+        if (rc != ALOCO_OK) return rc;
+        a.test_stall1 = 0;
+    }
+    return done();
+}
+
+// The plan that the device takes: with its largest clusters, unless that would
+// want more scratch than callers were told of.
+template <typename F>
+int device_plan(const F &make, Plan *plan) {
+    bool fits = false, larger = false;
+    cudaError_t e = cudaSuccess;
+    for (const SmallPass &s : plan->small) {
+        if ((e = ortho_small_setup(s.ctas, &fits)) != cudaSuccess) break;
+        if (!fits)
+            return fail(ALOCO_ERR_CUDA, "the device has no room for a cluster of %d", s.ctas);
+    }
+    for (const Shape &s : plan->shapes)
+        larger = larger || small_ctas(s, kOrthoSmallCtas) > kPortableCtas;
+    if (e == cudaSuccess && larger) e = ortho_small_setup(kOrthoSmallCtas, &fits);
+    if (e != cudaSuccess) return cuda_fail(e, "orthogonal factor");
+    if (larger && fits) {
+        Plan other;
+        make(kOrthoSmallCtas, &other);
+        for (const SmallPass &s : other.small)
+            if ((e = ortho_small_setup(s.ctas, &fits)) != cudaSuccess)
+                return cuda_fail(e, "orthogonal factor");
+        if (other.bytes <= plan->bytes) *plan = std::move(other);
+    }
+    return ALOCO_OK;
+}
+
 int check_scratch(const void *scratch, size_t bytes, size_t need) {
+    if (need == 0) return ALOCO_OK;
     if (bytes < need)
         return fail(ALOCO_ERR_ARG, "scratch of %zu bytes, need %zu", bytes, need);
     if (!scratch) return fail(ALOCO_ERR_ARG, "NULL scratch");
@@ -381,8 +495,9 @@ int muon_step(void *const *params, const void *const *grads, float *const *momen
     if ((rc = check_steps(cfg->coefficients, cfg->steps, cfg->eps)) != ALOCO_OK) return rc;
     if ((rc = check_matrices(mats, n, (int64_t)N)) != ALOCO_OK) return rc;
     Plan plan;
-    plan_matrices(mats, n, M, &plan);
-    if (plan.passes.empty()) return done();
+    const auto make = [&](int ctas, Plan *p) { plan_matrices(mats, n, M, ctas, p); };
+    make(kPortableCtas, &plan);
+    if (plan.passes.empty() && plan.small.empty()) return done();
     if ((rc = check_scratch(scratch, scratch_bytes, plan.bytes)) != ALOCO_OK) return rc;
 
     const size_t px = param_dtype == ALOCO_F32 ? 4 : 2, pg = grad_dtype == ALOCO_F32 ? 4 : 2;
@@ -400,7 +515,7 @@ int muon_step(void *const *params, const void *const *grads, float *const *momen
             return fail(ALOCO_ERR_ARG, "%s[%d]: not aligned to its element", bufs[i].name,
                         bufs[i].i);
     }
-    bufs[nb++] = {scratch, plan.bytes, 1, true, "scratch", 0};
+    if (plan.bytes) bufs[nb++] = {scratch, plan.bytes, 1, true, "scratch", 0};
     for (int i = 0; i < nb; ++i)
         for (int j = 0; j < i; ++j)
             if ((bufs[i].written || bufs[j].written) &&
@@ -413,6 +528,8 @@ int muon_step(void *const *params, const void *const *grads, float *const *momen
     for (int i = 0; i < nb; ++i)
         if ((rc = check(bufs[i].p, bufs[i].bytes, device, bufs[i].name, bufs[i].i)) != ALOCO_OK)
             return rc;
+
+    if ((rc = device_plan(make, &plan)) != ALOCO_OK) return rc;
 
     OrthoArgs a;
     std::memset(&a, 0, sizeof a);
@@ -437,13 +554,8 @@ int muon_step(void *const *params, const void *const *grads, float *const *momen
                               : 1.0;
         step.push_back(-cfg->lr * by);
     }
-    for (const Pass &pass : plan.passes) {
-        rc = run_pass(plan, pass, a, cfg->coefficients, cfg->steps, step.data(), (char *)scratch,
-                      sms, stream_of(opts));
-        if (rc != ALOCO_OK) return rc;
-        a.test_stall1 = 0;
-    }
-    return done();
+    return run(plan, a, cfg->coefficients, cfg->steps, step.data(), (char *)scratch, sms,
+               stream_of(opts));
 }
 
 int orthogonalize(const void *x, int64_t batch, int64_t rows, int64_t cols, int64_t batch_stride,
@@ -472,7 +584,8 @@ int orthogonalize(const void *x, int64_t batch, int64_t rows, int64_t cols, int6
         return fail(ALOCO_ERR_ARG, "batch_stride = %lld: matrices overlap",
                     (long long)batch_stride);
     Plan plan;
-    plan_batch(batch, rows, cols, &plan);
+    const auto make = [&](int ctas, Plan *p) { plan_batch(batch, rows, cols, ctas, p); };
+    make(kPortableCtas, &plan);
     if ((rc = check_scratch(scratch, scratch_bytes, plan.bytes)) != ALOCO_OK) return rc;
     const size_t size = dtype == ALOCO_F32 ? 4 : 2;
     Buffers s;
@@ -481,6 +594,8 @@ int orthogonalize(const void *x, int64_t batch, int64_t rows, int64_t cols, int6
     s.add("scratch", scratch, plan.bytes, kAlign, true);
     int sms;
     if ((rc = check_buffers(s, false, &sms)) != ALOCO_OK) return rc;
+
+    if ((rc = device_plan(make, &plan)) != ALOCO_OK) return rc;
 
     OrthoArgs a;
     std::memset(&a, 0, sizeof a);
@@ -493,13 +608,7 @@ int orthogonalize(const void *x, int64_t batch, int64_t rows, int64_t cols, int6
     a.row_stride = row_stride;
     a.eps = eps;
     a.test_stall1 = take_stall();
-    for (const Pass &pass : plan.passes) {
-        rc = run_pass(plan, pass, a, steps_of, steps, nullptr, (char *)scratch, sms,
-                      stream_of(opts));
-        if (rc != ALOCO_OK) return rc;
-        a.test_stall1 = 0;
-    }
-    return done();
+    return run(plan, a, steps_of, steps, nullptr, (char *)scratch, sms, stream_of(opts));
 }
 
 int no_memory() { return fail(ALOCO_ERR_NOMEM, "orthogonal factor: out of host memory"); }
@@ -530,7 +639,7 @@ size_t aloco_muon_scratch_bytes(const aloco_matrix_t *matrices, int64_t n, int M
         if (M < 1 || M > ALOCO_MAX_WORKERS || check_matrices(matrices, n, -1) != ALOCO_OK)
             return 0;
         Plan plan;
-        plan_matrices(matrices, n, M, &plan);
+        plan_matrices(matrices, n, M, kPortableCtas, &plan);
         return plan.bytes;
     } catch (const std::bad_alloc &) {
         no_memory();
@@ -556,7 +665,7 @@ size_t aloco_orthogonalize_scratch_bytes(int64_t batch, int64_t rows, int64_t co
             check_side(rows, cols, "x", 0) != ALOCO_OK)
             return 0;
         Plan plan;
-        plan_batch(batch, rows, cols, &plan);
+        plan_batch(batch, rows, cols, kPortableCtas, &plan);
         return plan.bytes;
     } catch (const std::bad_alloc &) {
         no_memory();

@@ -26,6 +26,7 @@ struct OrthoGroup {
     int sym0, up0;                   // the group's first tile
     int chunks, chunk;               // norm blocks of a matrix, elements of each
     int norm0, prep0;                // the group's first block
+    int small0;                      // its first cluster (launch_ortho_small)
     __half *x[2], *a, *p;
     uint4 *rest;                     // X - x, kBlockPieces a block: 8 columns of a row each
     int blocks_down, blocks_across;  // of a matrix
@@ -33,6 +34,9 @@ struct OrthoGroup {
     float *lead;                     // a + P's diagonal: what multiplies X itself
     double *partial;                 // [count][chunks] sums of squares
 };
+
+// What fits a CTA of launch_ortho_small: rows of X, and columns of it.
+constexpr int kOrthoSmallSide = 128, kOrthoSmallCols = 256, kOrthoSmallCtas = 16;
 
 constexpr int kOrthoGroups = 16;     // groups of a pass
 constexpr int kOrthoMatrices = 1024; // places of a pass (a worker's)
@@ -53,6 +57,8 @@ struct OrthoArgs {
     int sym_tiles, up_tiles, norm_blocks, prep_blocks;      // all groups'
     int next;                        // which of x[2] the update writes
     float ca, cb, cc;                // this step's coefficients
+    float coef[ALOCO_MAX_NS_STEPS][3];     // launch_ortho_small: every step's
+    int steps, small_ctas;           // and the CTAs of a matrix
     double eps;
     // where the matrices come from and go to
     int source;
@@ -77,5 +83,10 @@ cudaError_t launch_ortho_prepare(const OrthoArgs &a, cudaStream_t stream);
 // ctas: 1 or 2 CTAs share a tile (of 128 or 256 rows and columns)
 cudaError_t launch_ortho_product(OrthoProduct what, const OrthoArgs &a, int ctas, int sm_count,
                                  cudaStream_t stream);
+
+// All steps of matrices with m <= kOrthoSmallSide and n <= kOrthoSmallCols *
+// a.small_ctas (1, 2, 4, 8 or 16, if the device has room for such a cluster).
+cudaError_t ortho_small_setup(int ctas, bool *fits);
+cudaError_t launch_ortho_small(const OrthoArgs &a, int matrices, cudaStream_t stream);
 
 }  // namespace aloco

@@ -12,7 +12,7 @@ BASE = 1 << 40
 
 def _name(kw):
     return "-".join(f"{k}={v}" if isinstance(v, (int, float, tuple, type(None))) else k
-                    for k, v in kw.items())
+                    for k, v in kw.items())  # (no addresses: names are the same in every process)
 
 
 GAP = 1 << 28
@@ -84,7 +84,7 @@ def _matrices(parts):
     return (A.Matrix * len(parts))(*parts)
 
 
-def _muon(lib, parts=((0, 10, 20), (300, 30, 5)), N=1000, M=2, cfg=None, pdt=A.F32, gdt=A.BF16,
+def _muon(lib, parts=((0, 10, 20), (300, 30, 5), (500, 130, 140)), N=20000, M=2, cfg=None, pdt=A.F32, gdt=A.BF16,
           scratch=_at(20), bytes_=None, x=None, g=None, b=None):
     mats = _matrices(parts)
     vec = ctypes.c_void_p * 64
@@ -96,7 +96,7 @@ def _muon(lib, parts=((0, 10, 20), (300, 30, 5)), N=1000, M=2, cfg=None, pdt=A.F
                                ctypes.byref(cfg or A.muon_cfg()), scratch, need, None)
 
 
-BAD_MUON = [dict(M=0), dict(M=33), dict(pdt=5), dict(gdt=-1), dict(N=449),
+BAD_MUON = [dict(M=0), dict(M=33), dict(pdt=5), dict(gdt=-1), dict(N=18699),
             dict(parts=((-1, 2, 2),)), dict(parts=((0, -2, 2),)),
             dict(parts=((0, 2, A.MAX_LONG_SIDE + 1),), N=1 << 40),
             dict(parts=((0, A.MAX_SIDE + 1, A.MAX_SIDE + 1),), N=1 << 40),
@@ -129,7 +129,7 @@ def test_steps_refuse_what_overlaps(lib):
 
 def test_no_matrices_is_no_work(lib):
     assert _muon(lib, parts=()) == A.OK
-    assert _muon(lib, parts=((5, 0, 7), (1000, 3, 0))) == A.OK
+    assert _muon(lib, parts=((5, 0, 7), (20000, 3, 0))) == A.OK
 
 
 def test_settings_by_name():
@@ -146,8 +146,8 @@ def test_settings_by_name():
 def test_scratch_is_bounded(lib):
     """Scratch grows with the matrices up to a pass's, never beyond what its
     largest matrix needs."""
-    few = lib.aloco_muon_scratch_bytes(_matrices([(0, 64, 64)]), 1, 1)
-    assert 0 < few < 1 << 17
+    assert lib.aloco_muon_scratch_bytes(_matrices([(0, 64, 64)]), 1, 1) == 0
+    assert 0 < lib.aloco_muon_scratch_bytes(_matrices([(0, 129, 129)]), 1, 1) < 1 << 20
     many = [(i * 2048 * 5632, 2048, 5632) for i in range(60)]
     assert lib.aloco_muon_scratch_bytes(_matrices(many), 60, 8) <= 3 << 30
     assert lib.aloco_muon_scratch_bytes(_matrices(many), 60, 0) == 0
@@ -156,7 +156,7 @@ def test_scratch_is_bounded(lib):
 
 
 def _ortho(lib, **kw):
-    p = dict(x=_at(1), batch=2, rows=10, cols=20, bs=200, rs=20, dtype=A.F32, out=_at(2), steps=5,
+    p = dict(x=_at(1), batch=2, rows=130, cols=140, bs=18200, rs=140, dtype=A.F32, out=_at(2), steps=5,
              eps=1e-7, scratch=_at(3), bytes=1 << 24, coefficients=True) | kw
     co = (ctypes.c_double * 48)(*([1.5, -0.5, 0.0] * 16)) if p["coefficients"] else None
     return lib.aloco_orthogonalize(p["x"], p["batch"], p["rows"], p["cols"], p["bs"], p["rs"],
@@ -164,8 +164,8 @@ def _ortho(lib, **kw):
                                    p["bytes"], None)
 
 
-@pytest.mark.parametrize("kw", [dict(dtype=2), dict(batch=-1), dict(rows=-1), dict(rs=19),
-                                dict(bs=199), dict(steps=0), dict(steps=17), dict(eps=0.0),
+@pytest.mark.parametrize("kw", [dict(dtype=2), dict(batch=-1), dict(rows=-1), dict(rs=139),
+                                dict(bs=18199), dict(steps=0), dict(steps=17), dict(eps=0.0),
                                 dict(coefficients=False), dict(scratch=None), dict(bytes=1),
                                 dict(x=None), dict(out=None), dict(out=_at(2) + 1),
                                 dict(rows=A.MAX_SIDE + 1, cols=A.MAX_SIDE + 1, rs=1 << 20)],
