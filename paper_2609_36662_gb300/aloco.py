@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import array
 import ctypes
+import functools
 import os
 import struct
 from dataclasses import dataclass
@@ -879,15 +880,23 @@ def muon_step(params, grads, momentum, matrices, cfg: MuonCfg, stream=None):
     lib = load()
     with ctx:
         need = matrices.scratch_bytes(M)
-        scratch = _scratch_of(need, device)
+        scratch = _scratch_of(need, device) if need else None
         rc = lib.aloco_muon_step(
             _pointers(params), _pointers(grads), _pointers(momentum), N, M,
             F32 if params[0].dtype is torch.float32 else BF16,
             F32 if grads[0].dtype is torch.float32 else BF16, matrices.array,
-            len(matrices.parts), ctypes.byref(cfg), scratch.data_ptr(), need,
+            len(matrices.parts), ctypes.byref(cfg), scratch.data_ptr() if need else None, need,
             ctypes.byref(Opts(stream=handle)))
     _finish(rc, ctx)
     _written([*params, *momentum])
+
+
+@functools.lru_cache(maxsize=32)
+def _steps(coefficients):
+    """The C array of a tuple of (a, b, c)."""
+    if any(len(s) != 3 for s in coefficients):
+        raise ValueError("coefficients must be triples")
+    return (ctypes.c_double * (3 * len(coefficients)))(*[float(v) for s in coefficients for v in s])
 
 
 def orthogonalize(x, *, coefficients=(NEWTON_SCHULZ,) * 5, eps: float = 1e-7, out=None,
@@ -904,9 +913,8 @@ def orthogonalize(x, *, coefficients=(NEWTON_SCHULZ,) * 5, eps: float = 1e-7, ou
         raise ValueError("need [rows, columns] or [batch, rows, columns]")
     if not x.is_cuda or (x.stride(-1) != 1 and x.shape[-1] > 1):
         raise ValueError("need a CUDA tensor with contiguous rows")
-    steps = [float(v) for s in coefficients for v in s]
-    if len(steps) != 3 * len(coefficients):
-        raise ValueError("coefficients must be triples")
+    steps = _steps(coefficients if coefficients.__class__ is tuple else
+                   tuple(tuple(s) for s in coefficients))
     if out is not None and (out.dtype is not torch.bfloat16 or out.shape != x.shape or
                             out.device != x.device or not out.is_contiguous()):
         raise ValueError("out must be a contiguous bfloat16 tensor of x's shape and device")
@@ -918,12 +926,12 @@ def orthogonalize(x, *, coefficients=(NEWTON_SCHULZ,) * 5, eps: float = 1e-7, ou
     with ctx:
         result = torch.empty(x.shape, dtype=torch.bfloat16, device=device) if out is None else out
         need = lib.aloco_orthogonalize_scratch_bytes(batch, rows, cols)
-        scratch = _scratch_of(need, device)
+        scratch = _scratch_of(need, device) if need else None
         rc = lib.aloco_orthogonalize(
             x.data_ptr(), batch, rows, cols, x.stride(0) if x.dim() == 3 else 0, x.stride(-2),
             F32 if x.dtype is torch.float32 else BF16, result.data_ptr(),
-            (ctypes.c_double * len(steps))(*steps), len(coefficients), eps, scratch.data_ptr(),
-            need, ctypes.byref(Opts(stream=handle)))
+            steps, len(coefficients), eps, scratch.data_ptr() if need else None, need,
+            ctypes.byref(Opts(stream=handle)))
     _finish(rc, ctx, result)
     if out is not None:
         _written(out)

@@ -87,16 +87,19 @@ constexpr int kPortableCtas = 8;
 
 // Shapes in `p` (places set) into passes that keep within kPassBytes, kOrthoGroups
 // and kOrthoMatrices: deep products first, so that the last tiles are short.
-// Matrices for the small kernel, in clusters of up to `most_ctas`, go by themselves.
+// Where all are small they go through the small kernel, in clusters of up to
+// `most_ctas`.
 void split(Plan *p, int workers, int most_ctas) {
     std::stable_sort(p->shapes.begin(), p->shapes.end(), [](const Shape &x, const Shape &y) {
         return x.m() != y.m() ? x.m() > y.m() : x.n() > y.n();
     });
+    // (beside larger ones the small fill tiles of the kernels that run anyway)
+    bool all = true;
+    for (const Shape &s : p->shapes) all = all && small_ctas(s, most_ctas);
     std::vector<SmallPass> open;     // by cluster size
-    for (int i = 0; i < (int)p->shapes.size(); ++i) {
+    for (int i = 0; all && i < (int)p->shapes.size(); ++i) {
         const Shape &s = p->shapes[i];
         const int ctas = small_ctas(s, most_ctas);
-        if (!ctas) continue;
         auto at = std::find_if(open.begin(), open.end(),
                                [&](const SmallPass &x) { return x.ctas == ctas; });
         if (at != open.end() &&
@@ -121,9 +124,8 @@ void split(Plan *p, int workers, int most_ctas) {
         p->passes.push_back(std::move(pass));
         pass = Pass();
     };
-    for (int i = 0; i < (int)p->shapes.size(); ++i) {
+    for (int i = 0; !all && i < (int)p->shapes.size(); ++i) {
         const Shape &s = p->shapes[i];
-        if (small_ctas(s, most_ctas)) continue;
         const int64_t total = (int64_t)s.period * workers;
         for (int64_t at = 0; at < total;) {
             if (pass.parts.size() == kOrthoGroups || pass.places + s.period > kOrthoMatrices)
@@ -406,6 +408,7 @@ int device_plan(const F &make, Plan *plan) {
     }
     for (const Shape &s : plan->shapes)
         larger = larger || small_ctas(s, kOrthoSmallCtas) > kPortableCtas;
+    for (const Shape &s : plan->shapes) larger = larger && small_ctas(s, kOrthoSmallCtas);
     if (e == cudaSuccess && larger) e = ortho_small_setup(kOrthoSmallCtas, &fits);
     if (e != cudaSuccess) return cuda_fail(e, "orthogonal factor");
     if (larger && fits) {

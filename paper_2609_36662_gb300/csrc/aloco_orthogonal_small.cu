@@ -53,6 +53,24 @@ __device__ __forceinline__ void store_peer(uint32_t at, const uint4 &q) {
 __device__ __forceinline__ uint32_t share_at(int r, int c) {
     return (uint32_t)(r * kRows * 4 + ((c / 4) ^ (r & 7)) * 16);
 }
+// The same of this CTA's X, which lies where A, P and the parts come to lie.
+__device__ __forceinline__ uint32_t stage_at(int r, int c) {
+    return (uint32_t)(r * kCols * 4 + ((c / 4) ^ (r & 7)) * 16 + c % 4 * 4);
+}
+static_assert(2 * kABytes + kShareBytes >= kRows * kCols * 4, "X's stage");
+
+// This CTA's part of a matrix in the order of memory: `runs` stretches of `length`
+// elements, taken `each` (1 or 4) at a time.
+struct Walk {
+    int per, units;
+    float inverse;
+    __device__ __forceinline__ Walk(int runs, int length, int each)
+        : per(length / each), units(runs * per), inverse(1.f / (float)max(1, per)) {}
+    // (units < 2^15: the quotient is at least 1 / 512 away from a whole number)
+    __device__ __forceinline__ int run(int unit) const {
+        return (int)(((float)unit + 0.5f) * inverse);
+    }
+};
 
 // Matrices of the groups whose clusters have this launch's size.  Thread (row,
 // half): columns half * 128 .. + 127 of its CTA's 256, of X in fp32 in registers;
@@ -91,81 +109,100 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) tmem_alloc<1>(smem_addr(&s_tmem), kTmemColumns);
-    for (uint32_t i = tid * 16; i < kXBytes + 2 * kABytes; i += kThreads * 16)
+    for (uint32_t i = tid * 16; i < kXBytes; i += kThreads * 16)
         store_shared(smem + i, make_uint4(0, 0, 0, 0));
     grid_go();
     grid_wait();
 
-    // U, its norm, and the new momentum
+    // U, its norm, and the new momentum, as they lie in memory; through shared
+    // memory to the threads' rows
     const Source s(args, g, matrix);
-    const int j0 = half * kEach;
-    const int count = r < m ? max(0, min(kEach, cols - j0)) : 0;  // of this thread
-    float x[kEach];
+    const Result to(args, g, gi, matrix);
+    const int runs = g.tall ? cols : m, length = g.tall ? m : cols;
+    const int64_t origin = g.tall ? (int64_t)first * s.stride : first;
     // (squares in fp32, where they fit: the SM adds two doubles a clock)
     float near = 0.f;
     double far = 0.0;
-#pragma unroll
-    for (int j = 0; j < kEach; j += 16) {
-        float v[16];
-        if (s.by4 && !g.tall && j + 16 <= count) {
-            float4 q[4], o[4];
-            const int64_t e = s.at + (int64_t)r * s.stride + first + j0 + j;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) q[i] = load4(s.in, e + 4 * i, s.bf16);
-            if (s.momentum) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = load4(s.momentum, e + 4 * i, 0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float *qi = &q[i].x, *oi = &o[i].x;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        oi[k] = s.mo.next(oi[k], qi[k]);
-                        qi[k] = s.mo.u(oi[k], qi[k]);
-                    }
-                    *reinterpret_cast<float4 *>(s.momentum + e + 4 * i) = o[i];
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[4 * i] = q[i].x;
-                v[4 * i + 1] = q[i].y;
-                v[4 * i + 2] = q[i].z;
-                v[4 * i + 3] = q[i].w;
-            }
-        } else {
-            // (element (r, c) of X is (c, r) of a tall matrix: lanes lie side by side)
-            const int64_t step = g.tall ? s.stride : 1;
-            const int64_t e = s.at + (g.tall ? (int64_t)(first + j0 + j) * s.stride + r
-                                             : (int64_t)r * s.stride + first + j0 + j);
-            float old[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const bool is = j + i < count;
-                v[i] = is ? param_load(s.in, e + i * step, s.bf16) : 0.f;
-                old[i] = is && s.momentum ? s.momentum[e + i * step] : 0.f;
-            }
-            if (s.momentum) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float next = s.mo.next(old[i], v[i]);
-                    if (j + i < count) s.momentum[e + i * step] = next;
-                    v[i] = s.mo.u(next, v[i]);
-                }
-            }
-        }
+    const auto take = [&](const float *v, int n) {
         float sq = 0.f, top = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            sq = fmaf(v[i], v[i], sq);
-            top = fmaxf(top, fabsf(v[i]));
-            x[j + i] = v[i];
+        for (int j = 0; j < n; ++j) {
+            sq = fmaf(v[j], v[j], sq);
+            top = fmaxf(top, fabsf(v[j]));
         }
-        if (top < 1e18f && (top > 1e-12f || top == 0.f) && sq == sq) {
+        if (top < 1e16f && (top > 1e-14f || top == 0.f) && sq == sq) {
             near += sq;
         } else {
+            for (int j = 0; j < n; ++j) far += (double)v[j] * (double)v[j];
+        }
+    };
+    const auto stage = [&](int run, int l) {   // element l of a run
+        return as + (g.tall ? stage_at(l, run) : stage_at(run, l));
+    };
+    if (s.by4) {
+        const Walk w(runs, length, 4);
+        for (int i = tid; i < w.units; i += 8 * kThreads) {
+            float4 q[8], o[8];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) far += (double)v[i] * (double)v[i];
+            for (int k = 0; k < 8; ++k) {
+                const int u = i + k * kThreads, run = w.run(u);
+                if (u >= w.units) continue;
+                const int64_t e = s.at + origin + run * s.stride + (u - run * w.per) * 4;
+                q[k] = load4(s.in, e, s.bf16);
+                if (s.momentum) o[k] = load4(s.momentum, e, 0);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int u = i + k * kThreads, run = w.run(u), l = (u - run * w.per) * 4;
+                if (u >= w.units) continue;
+                float *v = &q[k].x, *b = &o[k].x;
+                if (s.momentum) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        b[j] = s.mo.next(b[j], v[j]);
+                        v[j] = s.mo.u(b[j], v[j]);
+                    }
+                    *reinterpret_cast<float4 *>(s.momentum + s.at + origin + run * s.stride + l) =
+                        o[k];
+                    if (u % 8 == 0) fetch_l2(to.address(origin + run * s.stride + l));
+                }
+                take(v, 4);
+                if (!g.tall) {
+                    store_shared(as + stage_at(run, l),
+                                 make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]),
+                                            __float_as_uint(v[2]), __float_as_uint(v[3])));
+                    continue;
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(stage(run, l + j)), "f"(v[j])
+                                 : "memory");
+            }
+        }
+    } else {
+        const Walk w(runs, length, 1);
+        for (int i = tid; i < w.units; i += 16 * kThreads) {
+            float v[16], b[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const int u = i + k * kThreads, run = w.run(u);
+                if (u >= w.units) continue;
+                const int64_t e = s.at + origin + run * s.stride + (u - run * w.per);
+                v[k] = param_load(s.in, e, s.bf16);
+                if (s.momentum) b[k] = s.momentum[e];
+            }
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const int u = i + k * kThreads, run = w.run(u), l = u - run * w.per;
+                if (u >= w.units) continue;
+                if (s.momentum) {
+                    const float next = s.mo.next(b[k], v[k]);
+                    s.momentum[s.at + origin + run * s.stride + l] = next;
+                    v[k] = s.mo.u(next, v[k]);
+                    if (lane == 0) fetch_l2(to.address(origin + run * s.stride + l));
+                }
+                take(&v[k], 1);
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(stage(run, l)), "f"(v[k]) : "memory");
+            }
         }
     }
     double sum = (double)near + far;
@@ -203,6 +240,18 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!usual) s_sum[0] = (double)kOrthoScale / (sqrt(total) + args.eps);
     }
     __syncthreads();
+    const int j0 = half * kEach;
+    const int count = r < m ? max(0, min(kEach, cols - j0)) : 0;  // of this thread
+    float x[kEach];
+#pragma unroll
+    for (int j = 0; j < kEach; j += 4) {
+        uint4 q = make_uint4(0, 0, 0, 0);
+        if (j < count) q = load_shared(as + stage_at(r, j0 + j));
+        x[j] = __uint_as_float(q.x);
+        x[j + 1] = j + 1 < count ? __uint_as_float(q.y) : 0.f;
+        x[j + 2] = j + 2 < count ? __uint_as_float(q.z) : 0.f;
+        x[j + 3] = j + 3 < count ? __uint_as_float(q.w) : 0.f;
+    }
     if (s_factor > 0.f) {
 #pragma unroll
         for (int j = 0; j < kEach; ++j) x[j] *= s_factor;
@@ -211,6 +260,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int j = 0; j < kEach; ++j) x[j] = (float)((double)x[j] * factor);
     }
+    // (rows and columns of A and P that there are not)
+    __syncthreads();
+    for (uint32_t i = tid * 16; i < 2 * kABytes; i += kThreads * 16)
+        store_shared(as + i, make_uint4(0, 0, 0, 0));
 
     // X's fp16 values: rows and columns that there are
     const auto show = [&] {
@@ -389,54 +442,82 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int j = 0; j < kEach; ++j) x[j] = __int_as_float(0x7fffffff);
     }
 
-    const Result to(args, g, gi, matrix);
-    const int64_t step = g.tall ? to.stride : 1;
-    const int64_t e = g.tall ? (int64_t)(first + j0) * to.stride + r
-                             : (int64_t)r * to.stride + first + j0;
+    // the result, back the same way (peers have read their parts of A)
 #pragma unroll
-    for (int j = 0; j < kEach; j += 8) {
-        if (!g.tall && to.whole && j + 8 <= count) {
-            uint4 w[2];
-            char *p = to.address(e + j);
-            const int n = to.bf16 ? 1 : 2;
-            for (int i = 0; i < n; ++i)
-                w[i] = to.update ? reinterpret_cast<uint4 *>(p)[i] : make_uint4(0, 0, 0, 0);
-            float o[8];
+    for (int j = 0; j < kEach; j += 4)
+        if (j < count)
+            store_shared(as + stage_at(r, j0 + j),
+                         make_uint4(__float_as_uint(x[j] * (1.f / kOrthoScale)),
+                                    __float_as_uint(x[j + 1] * (1.f / kOrthoScale)),
+                                    __float_as_uint(x[j + 2] * (1.f / kOrthoScale)),
+                                    __float_as_uint(x[j + 3] * (1.f / kOrthoScale))));
+    __syncthreads();
+    const int64_t base = g.tall ? (int64_t)first * to.stride : first;
+    const auto staged = [&](int run, int l) {
+        float v;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(stage(run, l)) : "memory");
+        return v;
+    };
+    if (to.whole) {
+        const Walk w(runs, length, 4);
+        for (int i = tid; i < w.units; i += 8 * kThreads) {
+            float4 old[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] = x[j + i] * (1.f / kOrthoScale);
-            if (to.bf16) {
-                uint32_t *q = &w[0].x;
+            for (int k = 0; k < 8; ++k) {
+                const int u = i + k * kThreads, run = w.run(u);
+                if (u < w.units && to.update)
+                    old[k] = load4(to.p, to.at + base + run * to.stride + (u - run * w.per) * 4,
+                                   to.bf16);
+            }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const __nv_bfloat162 h =
-                        __floats2bfloat162_rn(to.value(__uint_as_float(q[i] << 16), o[2 * i]),
-                                              to.value(__uint_as_float(q[i] & 0xffff0000u),
-                                                       o[2 * i + 1]));
-                    q[i] = *reinterpret_cast<const uint32_t *>(&h);
+            for (int k = 0; k < 8; ++k) {
+                const int u = i + k * kThreads, run = w.run(u), l = (u - run * w.per) * 4;
+                if (u >= w.units) continue;
+                const float *o = &old[k].x;
+                float v[4];
+                if (!g.tall) {
+                    const uint4 q = load_shared(as + stage_at(run, l));
+                    v[0] = __uint_as_float(q.x);
+                    v[1] = __uint_as_float(q.y);
+                    v[2] = __uint_as_float(q.z);
+                    v[3] = __uint_as_float(q.w);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = staged(run, l + j);
                 }
-                *reinterpret_cast<uint4 *>(p) = w[0];
-            } else {
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    float *q = reinterpret_cast<float *>(&w[k]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) q[i] = to.value(q[i], o[4 * k + i]);
-                    reinterpret_cast<uint4 *>(p)[k] = w[k];
+                for (int j = 0; j < 4; ++j) v[j] = to.value(o[j], v[j]);
+                char *p = to.address(base + run * to.stride + l);
+                if (to.bf16) {
+                    const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]),
+                                         c = __floats2bfloat162_rn(v[2], v[3]);
+                    *reinterpret_cast<uint2 *>(p) =
+                        make_uint2(*reinterpret_cast<const uint32_t *>(&a),
+                                   *reinterpret_cast<const uint32_t *>(&c));
+                } else {
+                    *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
                 }
             }
-            continue;
         }
-        float old[8];
+    } else {
+        const Walk w(runs, length, 1);
+        for (int i = tid; i < w.units; i += 16 * kThreads) {
+            float old[16];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            old[i] = to.update && j + i < count
-                         ? param_load(to.address(e + (j + i) * step), 0, to.bf16)
-                         : 0.f;
+            for (int k = 0; k < 16; ++k) {
+                const int u = i + k * kThreads, run = w.run(u);
+                if (u < w.units && to.update)
+                    old[k] = param_load(to.address(base + run * to.stride + (u - run * w.per)), 0,
+                                        to.bf16);
+            }
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (j + i < count)
-                param_store(to.address(e + (j + i) * step), 0, to.bf16,
-                            to.value(old[i], x[j + i] * (1.f / kOrthoScale)));
+            for (int k = 0; k < 16; ++k) {
+                const int u = i + k * kThreads, run = w.run(u), l = u - run * w.per;
+                if (u < w.units)
+                    param_store(to.address(base + run * to.stride + l), 0, to.bf16,
+                                to.value(old[k], staged(run, l)));
+            }
+        }
     }
     tc_fence_before();
     if (ctas > 1)
