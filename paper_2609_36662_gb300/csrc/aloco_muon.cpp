@@ -23,6 +23,9 @@ constexpr size_t kAlign = 256;
 
 size_t up(size_t x, size_t to) { return (x + to - 1) / to * to; }
 
+// The next tile and the tiles done of every matrix of a pass.
+size_t counter_bytes(int64_t matrices) { return up((size_t)(matrices + 1) * 4, kAlign); }
+
 // Matrices of one shape: `period` places of M workers.
 struct Shape {
     int64_t rows, cols;
@@ -120,7 +123,9 @@ void split(Plan *p, int workers, int most_ctas) {
     Pass pass;
     const auto flush = [&] {
         if (pass.parts.empty()) return;
-        p->bytes = std::max(p->bytes, pass.bytes);
+        int64_t matrices = 0;
+        for (const Part &part : pass.parts) matrices += part.count;
+        p->bytes = std::max(p->bytes, pass.bytes + counter_bytes(matrices));
         p->passes.push_back(std::move(pass));
         pass = Pass();
     };
@@ -234,21 +239,15 @@ int tensor_map(CUtensorMap *map, void *data, int64_t cols, int64_t rows, int64_t
     return ALOCO_OK;
 }
 
-// The tensor maps of a pass; the products copy the ones that they take.
-struct Maps {
-    CUtensorMap x[2][kOrthoGroups], a[kOrthoGroups], p[kOrthoGroups];
-};
-
 // Tiles of all groups for products by `ctas` CTAs a tile.
-void count_tiles(OrthoArgs *a, int sym_ctas, int up_ctas) {
-    const int half = ortho_pair_tile() / 2;
+void count_tiles(OrthoArgs *a, int ctas) {
+    const int tile = ortho_pair_tile() / 2 * ctas;
     a->sym_tiles = a->up_tiles = 0;
     for (int i = 0; i < a->n_groups; ++i) {
         OrthoGroup &g = a->g[i];
-        const int s = half * sym_ctas, u = half * up_ctas;
-        const int rows = (g.m + s - 1) / s;
+        const int rows = (g.m + tile - 1) / tile;
         g.sym_tiles = rows * (rows + 1) / 2;
-        g.up_tiles = ((g.m + u - 1) / u) * ((g.n + u - 1) / u);
+        g.up_tiles = rows * ((g.n + tile - 1) / tile);
         g.sym0 = a->sym_tiles;
         g.up0 = a->up_tiles;
         a->sym_tiles += g.sym_tiles * g.count;
@@ -274,14 +273,10 @@ void fill_group(const Plan &plan, const Part &part, int64_t *places, int *n_plac
 }
 
 int run_small(const Plan &plan, const SmallPass &pass, const OrthoArgs &base,
-              const double (*coefficients)[3], int steps, const double *shape_step,
-              cudaStream_t stream) {
+              const double *shape_step, cudaStream_t stream) {
     OrthoArgs a = base;
     a.n_groups = (int)pass.parts.size();
     a.small_ctas = pass.ctas;
-    a.steps = steps;
-    for (int s = 0; s < steps; ++s)
-        for (int i = 0; i < 3; ++i) a.coef[s][i] = (float)coefficients[s][i];
     int places = 0, matrices = 0;
     for (int i = 0; i < a.n_groups; ++i) {
         fill_group(plan, pass.parts[i], a.place, &places, &a.g[i]);
@@ -294,11 +289,9 @@ int run_small(const Plan &plan, const SmallPass &pass, const OrthoArgs &base,
 }
 
 // `base`: the caller's buffers and settings filled in.
-int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base,
-             const double (*coefficients)[3], int steps, const double *shape_step,
+int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base, const double *shape_step,
              char *scratch, int sm_count, cudaStream_t stream) {
     OrthoArgs a = base;
-    Maps maps;
     char *at = scratch;
     const auto take = [&](size_t bytes) {
         char *p = at;
@@ -307,6 +300,9 @@ int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base,
     };
     a.n_groups = (int)pass.parts.size();
     int places = 0, norm = 0, prep = 0;
+    for (const Part &part : pass.parts) a.matrices += (int)part.count;
+    a.next_tile = (int *)take(counter_bytes(a.matrices));
+    int *done = a.next_tile + 1;
     for (int i = 0; i < a.n_groups; ++i) {
         const Part &part = pass.parts[i];
         const Shape &s = plan.shapes[part.shape];
@@ -332,48 +328,27 @@ int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base,
         g.diag = (float *)take((size_t)(count * m) * 4);
         g.lead = (float *)take((size_t)(count * m) * 4);
         g.partial = (double *)take((size_t)(count * s.chunks()) * 8);
+        g.done = done;
+        done += count;
         a.step[i] = shape_step ? (float)shape_step[part.shape] : 0.f;
         int rc;
         for (int k = 0; k < 2; ++k)
-            if ((rc = tensor_map(&maps.x[k][i], g.x[k], n, m, s.ldx(), count)) != ALOCO_OK)
+            if ((rc = tensor_map(&a.map[kMapX0 + k][i], g.x[k], n, m, s.ldx(), count)) != ALOCO_OK)
                 return rc;
-        if ((rc = tensor_map(&maps.a[i], g.a, m, m, s.lda(), count)) != ALOCO_OK) return rc;
-        if ((rc = tensor_map(&maps.p[i], g.p, m, m, s.lda(), count)) != ALOCO_OK) return rc;
+        if ((rc = tensor_map(&a.map[kMapA][i], g.a, m, m, s.lda(), count)) != ALOCO_OK) return rc;
+        if ((rc = tensor_map(&a.map[kMapP][i], g.p, m, m, s.lda(), count)) != ALOCO_OK) return rc;
     }
     a.norm_blocks = norm;
     a.prep_blocks = prep;
     // Pairs of CTAs where their tiles fill the GPU; single CTAs, whose tiles are
     // a quarter, below.
-    count_tiles(&a, 2, 2);
-    const int sym_ctas = a.sym_tiles >= sm_count / 2 ? 2 : 1;
-    const int up_ctas = a.up_tiles >= sm_count / 2 ? 2 : 1;
-    count_tiles(&a, sym_ctas, up_ctas);
+    int ctas = 2;
+    count_tiles(&a, ctas);
+    if (a.up_tiles < sm_count / 2) count_tiles(&a, ctas = 1);
 
     cudaError_t e = launch_ortho_norm(a, stream);
     if (e == cudaSuccess) e = launch_ortho_prepare(a, stream);
-    const size_t map_bytes = sizeof(CUtensorMap) * a.n_groups;
-    for (int s = 0; s < steps && e == cudaSuccess; ++s) {
-        a.ca = (float)coefficients[s][0];
-        a.cb = (float)coefficients[s][1];
-        a.cc = (float)coefficients[s][2];
-        a.next = (s & 1) ^ 1;
-        const CUtensorMap *x = maps.x[s & 1];
-        std::memcpy(a.map_a, x, map_bytes);
-        std::memcpy(a.map_b, x, map_bytes);
-        e = launch_ortho_product(kGram, a, sym_ctas, sm_count, stream);
-        a.test_stall1 = 0;
-        if (e != cudaSuccess) break;
-        std::memcpy(a.map_a, maps.a, map_bytes);
-        std::memcpy(a.map_b, maps.a, map_bytes);
-        e = launch_ortho_product(kPoly, a, sym_ctas, sm_count, stream);
-        if (e != cudaSuccess) break;
-        std::memcpy(a.map_a, maps.p, map_bytes);
-        std::memcpy(a.map_b, x, map_bytes);
-        e = launch_ortho_product(s + 1 < steps  ? kUpdate
-                                 : a.out_bf16   ? kFinalBf16
-                                                : kFinal,
-                                 a, up_ctas, sm_count, stream);
-    }
+    if (e == cudaSuccess) e = launch_ortho_chain(a, ctas, sm_count, stream);
     return e == cudaSuccess ? ALOCO_OK : cuda_fail(e, "orthogonal factor");
 }
 
@@ -381,14 +356,16 @@ int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base,
 int run(const Plan &plan, const OrthoArgs &base, const double (*coefficients)[3], int steps,
         const double *shape_step, char *scratch, int sm_count, cudaStream_t stream) {
     OrthoArgs a = base;
+    a.steps = steps;
+    for (int s = 0; s < steps; ++s)
+        for (int i = 0; i < 3; ++i) a.coef[s][i] = (float)coefficients[s][i];
     for (const SmallPass &pass : plan.small) {
-        const int rc = run_small(plan, pass, a, coefficients, steps, shape_step, stream);
+        const int rc = run_small(plan, pass, a, shape_step, stream);
         if (rc != ALOCO_OK) return rc;
         a.test_stall1 = 0;
     }
     for (const Pass &pass : plan.passes) {
-        const int rc = run_pass(plan, pass, a, coefficients, steps, shape_step, scratch, sm_count,
-                                stream);
+        const int rc = run_pass(plan, pass, a, shape_step, scratch, sm_count, stream);
         if (rc != ALOCO_OK) return rc;
         a.test_stall1 = 0;
     }

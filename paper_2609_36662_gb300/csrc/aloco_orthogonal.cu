@@ -21,16 +21,26 @@ constexpr int kSlotBytes = 4 * kBoxBytes;  // two boxes of either operand
 constexpr int kSlots = 6;
 constexpr int kStageBytes = 4096;    // an epilogue warp's: a pair of 32 x 32 fp16 blocks
 constexpr int kSharedBytes =
-    kSlots * kSlotBytes + kEpilogueWarps * kStageBytes + 1024 + 256;
+    kSlots * kSlotBytes + kEpilogueWarps * kStageBytes + 1024 + 512;
+constexpr int kRing = 4;             // tiles that a CTA knows of
 
-struct Tile {
-    int group, matrix, row, col;     // row, col: in tiles
+// The steps' products, in the order in which tiles are handed out.
+enum { kGram, kPoly, kUpdate };
+
+struct Work {
+    int what, step, group, matrix;
+    int row, col;                    // in tiles
+    int before;                      // tiles of the matrix that have to be done
 };
 
-template <int kWhat>
-__device__ __forceinline__ Tile find_tile(const OrthoArgs &a, int t, int tile) {
-    Tile f;
-    if constexpr (kWhat >= kUpdate) {
+__device__ __forceinline__ Work find_work(const OrthoArgs &a, int t, int tile) {
+    Work f;
+    const int per = 2 * a.sym_tiles + a.up_tiles;
+    f.step = t / per;
+    t -= f.step * per;
+    f.what = t >= 2 * a.sym_tiles ? kUpdate : t >= a.sym_tiles ? kPoly : kGram;
+    t -= f.what * a.sym_tiles;
+    if (f.what == kUpdate) {
         f.group = find_group(a, t, [](const OrthoGroup &g) { return g.up0; });
         const OrthoGroup &g = a.g[f.group];
         t -= g.up0;
@@ -52,6 +62,8 @@ __device__ __forceinline__ Tile find_tile(const OrthoArgs &a, int t, int tile) {
         f.row = r;
         f.col = t - r * (r + 1) / 2;
     }
+    const OrthoGroup &g = a.g[f.group];
+    f.before = f.step * (2 * g.sym_tiles + g.up_tiles) + f.what * g.sym_tiles;
     return f;
 }
 
@@ -72,8 +84,10 @@ struct Pieces {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = 8 * i + lane / 4, c = lane % 4 * 8;
-            q[i] = r < rows && c < cols ? *reinterpret_cast<const uint4 *>(p + r * ld + c)
-                                        : make_uint4(0, 0, 0, 0);
+            // (past the SM's cache: other SMs write it while this kernel runs)
+            q[i] = r < rows && c < cols
+                       ? __ldcg(reinterpret_cast<const uint4 *>(p + r * ld + c))
+                       : make_uint4(0, 0, 0, 0);
         }
     }
     __device__ __forceinline__ void to_shared(char *block) const {
@@ -230,22 +244,59 @@ __device__ __forceinline__ void store_values(const Result &to, int y, int x, int
     }
 }
 
-// One product of all matrices.  Persistent CTAs (pairs) take tiles in turn: two
-// threads copy operands into a ring of slots, one issues the products into one
-// of two accumulators, eight warps write the other one's tile.  A wait that runs
-// out leaves NaN in the tile, and with it in the matrix.
-//   kGram    A = X X^T, lower tiles, mirrored; the diagonal in fp32
-//   kPoly    P = b A + c A A, the same
-//   kUpdate  X <- a X + P X
-//   kFinal, kFinalBf16  the same, to the result in fp32 or bf16
-// A and P are symmetric: the lower tiles are computed and kept, with whole blocks
-// of kFull on the diagonal.  Where a product needs what would lie above them it
-// takes the tile below, MN-major instead of K-major: nothing is written twice.
-template <int kWhat, int kCtas>
+// Where tiles that a matrix's next products take are done with: what `count` warps
+// have written is seen by whoever finds them counted.
+__device__ __forceinline__ int load_acquire(const int *p) {
+    int v;
+    asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ bool wait_done(const int *done, int count, const volatile int *abort) {
+    if (load_acquire(done) >= count) return true;
+    const long long t0 = clock64();
+    while (load_acquire(done) < count) {
+        if (*abort || clock64() - t0 > kTmaWaitCycles) return false;
+        __nanosleep(64);
+    }
+    return true;
+}
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity) {
+    const long long t0 = clock64();
+    for (;;) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (ok) return true;
+        if (clock64() - t0 > 2 * kTmaWaitCycles) return false;
+    }
+}
+
+// All steps of all matrices: of every step the tiles of A = X X^T, of P = b A + c A
+// A, and of X <- a X + P X, matrix after matrix.  CTAs (pairs of them) take the next
+// tile when they have asked for the operands of the one before, so that no two
+// wait for each other: what a tile needs was handed out before it, and counts of
+// the matrix's tiles that are done say when it is there.
+//
+// In a CTA two threads copy operands into a ring of slots (the first of a pair's
+// also takes the tiles), one issues the products into one of two accumulators,
+// eight warps join the other one with what it needs and write it.  A and P are
+// symmetric: the lower tiles are computed and kept, with whole blocks of kFull on
+// the diagonal; where a product needs what would lie above them it takes the tile
+// below, MN-major instead of K-major.
+//
+// A wait that runs out ends the waits of its CTA; its tiles are NaN from there on,
+// and with them their matrices.
+template <int kCtas, bool kOutBf16>
 __global__ void __launch_bounds__(kProductThreads, 1)
-    ortho_product_kernel(const __grid_constant__ OrthoArgs args) {
+    ortho_chain_kernel(const __grid_constant__ OrthoArgs args) {
     constexpr int kTile = kHalfTile * kCtas;
     constexpr uint32_t kDesc = product_desc(kTile, kTile);
+    constexpr int kSignals = kCtas * kEpilogueWarps;     // of a tile
     extern __shared__ char raw[];
     const uint32_t smem = (smem_addr(raw) + 1023) & ~1023u;
     const uint32_t bars = smem + kSlots * kSlotBytes + kEpilogueWarps * kStageBytes;
@@ -254,13 +305,15 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     const auto acc_full = [&](int s) { return bars + 8 * (2 * kSlots + s); };
     const auto acc_empty = [&](int s) { return bars + 8 * (2 * kSlots + 2 + s); };
     const uint32_t drained = bars + 8 * (2 * kSlots + 4);
+    const auto told = [&](int s) { return bars + 8 * (2 * kSlots + 5 + s); };
+    const auto heard = [&](int s) { return bars + 8 * (2 * kSlots + 5 + kRing + s); };
+    const auto tile_at = [&](int s) { return bars + 8 * (2 * kSlots + 5 + 2 * kRing) + 4 * s; };
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_abort;
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = kCtas == 1 ? 0 : cluster_rank();
-    const int first = blockIdx.x / kCtas, stride = gridDim.x / kCtas;
-    const int tiles = kWhat >= kUpdate ? args.up_tiles : args.sym_tiles;
+    const int tiles = args.steps * (2 * args.sym_tiles + args.up_tiles);
 
     if (threadIdx.x == 0) {
         s_abort = 0;
@@ -273,13 +326,17 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             mbar_init(acc_empty(s), kEpilogueWarps * kCtas);
         }
         mbar_init(drained, 1);
+        for (int s = 0; s < kRing; ++s) {
+            mbar_init(told(s), 1);
+            // all that hear of a tile but the thread that tells
+            mbar_init(heard(s), kCtas * (kEpilogueWarps + 2));
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) tmem_alloc<kCtas>(smem_addr(&s_tmem), 2 * kTile);
-    if (warp == 4 && lane < args.n_groups) {
-        fetch_map(&args.map_a[lane]);
-        if (kWhat >= kUpdate) fetch_map(&args.map_b[lane]);
-    }
+    if (warp == 4)
+        for (int i = lane; i < kOrthoMaps * args.n_groups; i += 32)
+            fetch_map(&args.map[i / args.n_groups][i % args.n_groups]);
     tc_fence_before();
     __syncthreads();
     if constexpr (kCtas == 2) cluster_sync();
@@ -288,32 +345,88 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     grid_go();
     grid_wait();
 
-    const auto depth = [&](const OrthoGroup &g) { return kWhat == kGram ? g.n : g.m; };
+    // The next tile, as all but the first producer hear of it; -1: there is none.
+    int ring = 0;
+    uint32_t ring_phase = 0;
+    const auto on = [&] {
+        if (++ring == kRing) ring = 0, ring_phase ^= 1;
+    };
+    const auto hear = [&](bool whole_warp) -> int {
+        int t = -1;
+        if (mbar_wait_cluster(told(ring), ring_phase))
+            asm volatile("ld.shared.s32 %0, [%1];" : "=r"(t) : "r"(tile_at(ring)) : "memory");
+        if (whole_warp) __syncwarp();
+        if (!whole_warp || lane == 0) {
+            if (kCtas == 1 || rank == 0)
+                mbar_arrive(heard(ring));
+            else
+                asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(
+                                 cluster_addr(heard(ring), 0))
+                             : "memory");
+        }
+        on();
+        return t;
+    };
+    const auto done_of = [&](const Work &f) { return args.g[f.group].done + f.matrix; };
+    const auto depth = [&](const Work &f) {
+        return f.what == kGram ? args.g[f.group].n : args.g[f.group].m;
+    };
 
     if ((warp == 0 || warp == 3) && lane == 0) {
         // One thread for either operand: copying both, a thread takes as long as
         // the products of a slot do.
-        const bool is_b = warp == 3;
-        // operands were written by ordinary stores of the kernel before
-        asm volatile("fence.proxy.async;" ::: "memory");
+        const bool is_b = warp == 3, tells = rank == 0 && !is_b;
         const uint32_t bar0 = kCtas == 1 ? full(0) : cluster_addr(full(0), 0);
         int slot = 0, issued = 0;
         uint32_t phase = 0;
         bool ok = true;
-        for (int t = first; t < tiles && ok; t += stride) {
-            const Tile f = find_tile<kWhat>(args, t, kTile);
-            const int chunks = (depth(args.g[f.group]) + kK - 1) / kK;
-            const CUtensorMap *map = is_b ? &args.map_b[f.group] : &args.map_a[f.group];
+        int next = tells ? atomicAdd(args.next_tile, 1) : 0;
+        for (;;) {
+            int t;
+            if (tells) {
+                t = next < tiles ? next : -1;
+                if (!mbar_wait_cluster(heard(ring), ring_phase ^ 1)) break;
+                asm volatile("st.shared.s32 [%0], %1;" ::"r"(tile_at(ring)), "r"(t) : "memory");
+                mbar_arrive(told(ring));
+                if constexpr (kCtas == 2) {
+                    asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(
+                                     cluster_addr(tile_at(ring), 1)),
+                                 "r"(t)
+                                 : "memory");
+                    asm volatile(
+                        "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(
+                            cluster_addr(told(ring), 1))
+                        : "memory");
+                }
+                on();
+            } else {
+                t = hear(false);
+            }
+            if (t < 0) break;
+            const Work f = find_work(args, t, kTile);
+            const int chunks = (depth(f) + kK - 1) / kK;
+            const int ask = max(0, chunks - kSlots);   // where to take the next tile
+            if (ok && !s_abort)
+                ok = wait_done(done_of(f), f.before * kSignals, &s_abort);
+            else
+                ok = false;
+            // operands were written by ordinary stores
+            asm volatile("fence.proxy.async;" ::: "memory");
+            const CUtensorMap *map =
+                &args.map[f.what == kPoly              ? kMapA
+                          : f.what == kUpdate && !is_b ? kMapP
+                                                       : kMapX0 + (f.step & 1)][f.group];
             const int row = (is_b ? f.col : f.row) * kTile + (int)rank * kHalfTile;
             // columns from here on lie below, MN-major (X does throughout)
-            const int turn = kWhat == kGram            ? INT_MAX
-                             : kWhat >= kUpdate && is_b ? 0
-                                                        : (row / kFull + 1) * kFull;
+            const int turn = f.what == kGram            ? INT_MAX
+                             : f.what == kUpdate && is_b ? 0
+                                                         : (row / kFull + 1) * kFull;
             for (int k = 0; k < chunks; ++k) {
-                if (!(ok = mbar_wait(empty(slot), phase ^ 1, &s_abort))) break;
+                if (tells && k == ask) next = atomicAdd(args.next_tile, 1);
+                if (!ok || !(ok = mbar_wait(empty(slot), phase ^ 1, &s_abort))) continue;
                 const uint32_t at = smem + slot * kSlotBytes + (is_b ? 2 * kBoxBytes : 0);
                 const uint32_t bar = bar0 + 8 * slot;
-                if (rank == 0 && !is_b) mbar_arrive_expect_tx(full(slot), kCtas * kSlotBytes);
+                if (tells) mbar_arrive_expect_tx(full(slot), kCtas * kSlotBytes);
                 const int c = k * kK;
                 if (args.test_stall1 == 0 || blockIdx.x != 0 || issued != args.test_stall1 - 1) {
                     if (c < turn) {
@@ -327,29 +440,29 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 ++issued;
                 if (++slot == kSlots) slot = 0, phase ^= 1;
             }
+            if (!ok) s_abort = 1;
         }
-        if (!ok) {
-            s_abort = 1;
+        if ((!ok || s_abort) && tells)
             // copies in flight land before the block ends (each slot's last use)
-            if (rank == 0 && !is_b)
-                for (int i = issued > kSlots ? issued - kSlots : 0; i < issued; ++i)
-                    mbar_wait(full(i % kSlots), (i / kSlots) & 1, nullptr);
-        }
+            for (int i = issued > kSlots ? issued - kSlots : 0; i < issued; ++i)
+                mbar_wait(full(i % kSlots), (i / kSlots) & 1, nullptr);
     } else if (warp == 1 && lane == 0 && rank == 0) {
         int slot = 0, acc = 0;
         uint32_t phase = 0, acc_phase = 0;
         bool ok = true;
-        for (int t = first; t < tiles && ok; t += stride) {
-            const Tile f = find_tile<kWhat>(args, t, kTile);
-            const int K = depth(args.g[f.group]);
-            if (!(ok = mbar_wait(acc_empty(acc), acc_phase ^ 1, &s_abort))) break;
+        for (;;) {
+            const int t = hear(false);
+            if (t < 0) break;
+            const Work f = find_work(args, t, kTile);
+            const int K = depth(f);
+            if (ok) ok = mbar_wait(acc_empty(acc), acc_phase ^ 1, &s_abort);
             tc_fence_after();
-            const int turn_a = kWhat == kGram ? INT_MAX : (f.row * kTile / kFull + 1) * kFull;
-            const int turn_b = kWhat == kGram      ? INT_MAX
-                               : kWhat >= kUpdate ? 0
-                                                  : (f.col * kTile / kFull + 1) * kFull;
+            const int turn_a = f.what == kGram ? INT_MAX : (f.row * kTile / kFull + 1) * kFull;
+            const int turn_b = f.what == kGram     ? INT_MAX
+                               : f.what == kUpdate ? 0
+                                                   : (f.col * kTile / kFull + 1) * kFull;
             const uint32_t d = tmem + acc * kTile;
-            for (int k = 0; k < K; k += kK) {
+            for (int k = 0; ok && k < K; k += kK) {
                 if (!(ok = mbar_wait(full(slot), phase, &s_abort))) break;
                 tc_fence_after();
                 const uint32_t a0 = smem + slot * kSlotBytes, b0 = a0 + 2 * kBoxBytes;
@@ -367,13 +480,14 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 product_commit<kCtas>(empty(slot));
                 if (++slot == kSlots) slot = 0, phase ^= 1;
             }
-            if (!ok) break;
-            product_commit<kCtas>(acc_full(acc));
+            if (ok)
+                product_commit<kCtas>(acc_full(acc));
+            else
+                s_abort = 1;
             if (acc) acc_phase ^= 1;
             acc ^= 1;
         }
         if (!ok) {
-            s_abort = 1;
             // products in flight end before their accumulators are given back
             product_commit<kCtas>(drained);
             mbar_wait(drained, 0, nullptr);
@@ -385,11 +499,14 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                    (warp - kEpilogueWarp) * kStageBytes;
         int acc = 0;
         uint32_t acc_phase = 0;
-        for (int t = first; t < tiles; t += stride) {
-            const Tile f = find_tile<kWhat>(args, t, kTile);
+        for (;;) {
+            const int t = hear(true);
+            if (t < 0) break;
+            const Work f = find_work(args, t, kTile);
             const OrthoGroup &g = args.g[f.group];
+            const bool last = f.what == kUpdate && f.step + 1 == args.steps;
             const int m = g.m, r0 = f.row * kTile + (int)rank * kHalfTile + quad * 32;
-            const int r = r0 + lane, limit = kWhat >= kUpdate ? g.n : m;
+            const int r = r0 + lane, limit = f.what == kUpdate ? g.n : m;
             const int c_end = min(limit, f.col * kTile + (half + 1) * (kTile / 2));
             int c0 = f.col * kTile + half * (kTile / 2);
             const bool some = r0 < m && c0 < c_end;
@@ -397,49 +514,55 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             // (single CTAs have two tiles of a block on the diagonal to fill)
             const bool mirrored = kCtas == 1 && f.row != f.col &&
                                   f.row * kTile / kFull == f.col * kTile / kFull;
-            // what a product is joined with: of A or P whole rows, of X blocks that
+            const float ca = args.coef[f.step][0], cb = args.coef[f.step][1],
+                        cc = args.coef[f.step][2];
+            // what a product is joined with: of A or P whole rows, of X also blocks that
             // lie as this warp holds them; fetched a block ahead
-            uint4 *rest = nullptr;
-            if (kWhat >= kUpdate)
-                rest = g.rest + ((int64_t)(f.matrix * g.blocks_down + r0 / 32) * g.blocks_across +
-                                 c0 / 32) * kBlockPieces + lane;
+            uint4 *rest = g.rest + ((int64_t)(f.matrix * g.blocks_down + r0 / 32) * g.blocks_across +
+                                    c0 / 32) * kBlockPieces + lane;
             const Result to(args, g, f.group, f.matrix);
             Pieces part;
             uint4 lo[4];
             float by_row = 0.f, by_col = 0.f;
             const int begin = c0;
-            const auto fetch = [&](int c) {
-                if constexpr (kWhat >= kUpdate) {
-                    const uint4 *p = rest + (c - begin) / 32 * kBlockPieces;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) lo[i] = p[32 * i];
-                    part.load(g.x[args.next ^ 1] + (row0 + r0) * g.ldx + c, g.ldx, m - r0, g.n - c);
-                } else if constexpr (kWhat == kPoly) {
-                    part.load(g.a + (row0 + r0) * g.lda + c, g.lda, m - r0, m - c);
-                    by_col = c + lane < m ? args.cc * g.diag[row0 + c + lane] : 0.f;
-                }
+            const auto fetch_a = [&](int c) {
+                part.load(g.a + (row0 + r0) * g.lda + c, g.lda, m - r0, m - c);
+                by_col = c + lane < m ? cc * __ldcg(g.diag + row0 + c + lane) : 0.f;
             };
-            if (kWhat != kGram && some) {
-                if (kWhat >= kUpdate) {
+            const auto fetch_x = [&](int c) {
+                const uint4 *p = rest + (c - begin) / 32 * kBlockPieces;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) lo[i] = __ldcg(p + 32 * i);
+                part.load(g.x[f.step & 1] + (row0 + r0) * g.ldx + c, g.ldx, m - r0, g.n - c);
+            };
+            if (last && some && to.update) {
+                // parameters come from far: to L2 while the products run
+                const int along = to.tall ? 32 : c_end - c0, down = to.tall ? c_end - c0 : 32;
+                for (int i = lane; i < down; i += 32) {
+                    const int y = (to.tall ? c0 : r0) + i, x = to.tall ? r0 : c0;
+                    if (y >= g.rows) break;
+                    for (int j = 0; j < along && x + j < g.cols; j += 32)
+                        fetch_l2(to.address(y * to.stride + x + j));
+                }
+            }
+            bool ok = !s_abort;
+            if (f.what != kGram && some) {
+                if (ok) ok = wait_done(done_of(f), f.before * kSignals, &s_abort);
+                ok = __all_sync(~0u, ok);
+                if (f.what == kUpdate) {
                     // what is kept of X beside the operands comes to L2 while the
                     // products run
-                    // (64 of its 128-byte lines, of four blocks)
                     const int lines = (c_end - c0 + 31) / 32 * 16;
                     for (int i = lane; i < lines; i += 32) fetch_l2(rest - lane + 8 * i);
+                    if (r < m) by_row = __ldcg(g.lead + row0 + r);
+                    fetch_x(c0);
+                } else {
+                    if (r < m) by_row = __ldcg(g.diag + row0 + r);
+                    fetch_a(c0);
                 }
-                if (kWhat > kUpdate && to.update) {
-                    const int along = to.tall ? 32 : c_end - c0, down = to.tall ? c_end - c0 : 32;
-                    for (int i = lane; i < down; i += 32) {
-                        const int y = (to.tall ? c0 : r0) + i, x = to.tall ? r0 : c0;
-                        if (y >= g.rows) break;
-                        for (int j = 0; j < along && x + j < g.cols; j += 32)
-                            fetch_l2(to.address(y * to.stride + x + j));
-                    }
-                }
-                if (r < m) by_row = (kWhat == kPoly ? g.diag : g.lead)[row0 + r];
-                fetch(c0);
             }
-            const bool ok = mbar_wait(acc_full(acc), acc_phase, &s_abort);
+            if (ok) ok = mbar_wait(acc_full(acc), acc_phase, &s_abort);
+            ok = __all_sync(~0u, ok);
             if (!ok) s_abort = 1;
             tc_fence_after();
             // the accumulator goes back when the last block has been read
@@ -452,23 +575,26 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 else
                     mbar_arrive_cluster(cluster_addr(acc_empty(acc), 0));
             };
-#pragma unroll 1
-            for (; some && c0 < c_end; c0 += 32) {
-                Param<kWhat == kFinalBf16> param;
-                const int y = to.tall ? c0 : r0, x = to.tall ? r0 : c0;
-                if (kWhat > kUpdate && to.update && to.whole)
-                    param.load(to, y, x, g.rows, g.cols);
+            // column c0's accumulators of this row
+            const auto values = [&](float (&v)[32]) {
                 uint32_t u[32];
+                __syncwarp();
                 tmem_read32(tmem + acc * kTile + (c0 - f.col * kTile) + (quad << 21), u);
                 if (c0 + 32 >= c_end) release();
-                float v[32];
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(u[i]);
                 if (!ok) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = __int_as_float(0x7fffffff);
                 }
-                if constexpr (kWhat == kGram) {
+            };
+            if (!some) {
+                release();
+            } else if (f.what == kGram) {
+#pragma unroll 1
+                for (; c0 < c_end; c0 += 32) {
+                    float v[32];
+                    values(v);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] *= 1.f / (kOrthoScale * kOrthoScale);
                     if (c0 == r0) {
@@ -479,24 +605,28 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                         if (r < m) g.diag[row0 + r] = own;
                     }
                     store_symmetric(g.a + row0 * g.lda, m, g.lda, r0, c0, mirrored, st, v);
-                } else if constexpr (kWhat == kPoly) {
+                }
+            } else if (f.what == kPoly) {
+                // b a + c ((d_r + d_c) a + x); where A's diagonal is taken out a is 0
+                const float dr = fmaf(cc, by_row, cb);
+#pragma unroll 1
+                for (; c0 < c_end; c0 += 32) {
+                    float v[32];
+                    values(v);
                     __syncwarp();
                     part.to_shared(st);
                     float *cols = reinterpret_cast<float *>(st + 2048);
                     cols[lane] = by_col;
-                    if (c0 + 32 < c_end) fetch(c0 + 32);
+                    if (c0 + 32 < c_end) fetch_a(c0 + 32);
                     __syncwarp();
-                    float own = 0.f;
                     if (c0 == r0) {
+                        float own = 0.f;
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
                             if (i == lane) own = v[i], v[i] = 0.f;
                         if (r < m)
-                            g.lead[row0 + r] = args.ca + args.cb * by_row +
-                                               args.cc * (by_row * by_row + own);
+                            g.lead[row0 + r] = ca + cb * by_row + cc * (by_row * by_row + own);
                     }
-                    // b a + c ((d_r + d_c) a + x); where A's diagonal is taken out a is 0
-                    const float dr = fmaf(args.cc, by_row, args.cb);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const uint4 w = *piece(st, lane, i);
@@ -507,11 +637,20 @@ __global__ void __launch_bounds__(kProductThreads, 1)
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             const float2 h = unpack(ws[j / 2]);
-                            v[8 * i + j] = fmaf(j & 1 ? h.y : h.x, dr + dc[j], args.cc * v[8 * i + j]);
+                            v[8 * i + j] =
+                                fmaf(j & 1 ? h.y : h.x, dr + dc[j], cc * v[8 * i + j]);
                         }
                     }
                     store_symmetric(g.p + row0 * g.lda, m, g.lda, r0, c0, mirrored, st, v);
-                } else {
+                }
+            } else {
+#pragma unroll 1
+                for (; c0 < c_end; c0 += 32) {
+                    Param<kOutBf16> param;
+                    const int y = to.tall ? c0 : r0, x = to.tall ? r0 : c0;
+                    if (last && to.update && to.whole) param.load(to, y, x, g.rows, g.cols);
+                    float v[32];
+                    values(v);
                     __syncwarp();
                     part.to_shared(st);
                     uint32_t ls[16];
@@ -522,7 +661,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                         ls[4 * i + 2] = lo[i].z;
                         ls[4 * i + 3] = lo[i].w;
                     }
-                    if (c0 + 32 < c_end) fetch(c0 + 32);
+                    if (c0 + 32 < c_end) fetch_x(c0 + 32);
                     __syncwarp();
                     uint4 w[4];
 #pragma unroll
@@ -537,37 +676,44 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                         v[2 * i] = fmaf(by_row, h.x, fmaf(by_row, l.x, v[2 * i]));
                         v[2 * i + 1] = fmaf(by_row, h.y, fmaf(by_row, l.y, v[2 * i + 1]));
                     }
-                    if constexpr (kWhat > kUpdate) {
+                    if (last) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] *= 1.f / kOrthoScale;
                         if (to.whole) {
                             param.join(to, st, v);
                             param.store(to, st, y, x, g.rows, g.cols);
                         } else {
-                            store_values<kWhat == kFinalBf16>(to, y, x, g.rows, g.cols, st, v);
+                            store_values<kOutBf16>(to, y, x, g.rows, g.cols, st, v);
                         }
-                    } else {
-                        uint4 *p = rest + (c0 - begin) / 32 * kBlockPieces;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            uint32_t h[4], l[4];
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const float x0 = v[8 * i + 2 * j], x1 = v[8 * i + 2 * j + 1];
-                                h[j] = pack(x0, x1);
-                                const float2 b = unpack(h[j]);
-                                l[j] = pack(x0 - b.x, x1 - b.y);
-                            }
-                            *piece(st, lane, i) = make_uint4(h[0], h[1], h[2], h[3]);
-                            p[32 * i] = make_uint4(l[0], l[1], l[2], l[3]);
-                        }
-                        __syncwarp();
-                        store_block(st, g.x[args.next] + (row0 + r0) * g.ldx + c0, g.ldx, m - r0,
-                                    g.n - c0);
+                        continue;
                     }
+                    uint4 *p = rest + (c0 - begin) / 32 * kBlockPieces;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t h[4], l[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float x0 = v[8 * i + 2 * j], x1 = v[8 * i + 2 * j + 1];
+                            h[j] = pack(x0, x1);
+                            const float2 b = unpack(h[j]);
+                            l[j] = pack(x0 - b.x, x1 - b.y);
+                        }
+                        *piece(st, lane, i) = make_uint4(h[0], h[1], h[2], h[3]);
+                        p[32 * i] = make_uint4(l[0], l[1], l[2], l[3]);
+                    }
+                    __syncwarp();
+                    store_block(st, g.x[(f.step & 1) ^ 1] + (row0 + r0) * g.ldx + c0, g.ldx, m - r0,
+                                g.n - c0);
                 }
             }
-            if (!some) release();
+            if (!last) {
+                // done: what this warp has written is seen behind the count (by tensor
+                // copies behind a fence of theirs)
+                __syncwarp();
+                if (lane == 0)
+                    asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(done_of(f))
+                                 : "memory");
+            }
             if (acc) acc_phase ^= 1;
             acc ^= 1;
         }
@@ -578,8 +724,6 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     tc_fence_after();
     if (warp == 2) tmem_free<kCtas>(tmem, 2 * kTile);
 }
-
-// ------------------------------------------------- from the caller's matrices
 
 // The block's sum, in thread 0.
 __device__ __forceinline__ double block_sum(double s, double *shared) {
@@ -598,6 +742,8 @@ __global__ void __launch_bounds__(kThreads) ortho_norm_kernel(const __grid_const
     __shared__ double shared[kThreads / 32];
     grid_go();
     grid_wait();
+    if (blockIdx.x == 0)             // for the products' kernel: its tiles, and those done
+        for (int i = threadIdx.x; i <= args.matrices; i += kThreads) args.next_tile[i] = 0;
     const int gi = find_group(args, blockIdx.x, [](const OrthoGroup &g) { return g.norm0; });
     const OrthoGroup &g = args.g[gi];
     const int b = blockIdx.x - g.norm0, matrix = b / g.chunks, chunk = b - matrix * g.chunks;
@@ -777,10 +923,10 @@ cudaError_t launch(K kernel, const OrthoArgs &a, int grid, int threads, int ctas
     return cudaLaunchKernelEx(&c, kernel, a);
 }
 
-template <int kWhat, int kCtas>
-cudaError_t launch_product(const OrthoArgs &a, int sm_count, cudaStream_t stream) {
+template <int kCtas, bool kOutBf16>
+cudaError_t launch_chain(const OrthoArgs &a, int sm_count, cudaStream_t stream) {
     static PerDevice ready;
-    const auto kernel = ortho_product_kernel<kWhat, kCtas>;
+    const auto kernel = ortho_chain_kernel<kCtas, kOutBf16>;
     const int d = PerDevice::device();
     if (!ready.get(d)) {
         const cudaError_t e = cudaFuncSetAttribute(
@@ -788,9 +934,9 @@ cudaError_t launch_product(const OrthoArgs &a, int sm_count, cudaStream_t stream
         if (e != cudaSuccess) return e;
         ready.set(d, 1);
     }
-    const int tiles = kWhat >= kUpdate ? a.up_tiles : a.sym_tiles;
-    const int most = sm_count / kCtas;
-    return launch(kernel, a, (tiles < most ? tiles : most) * kCtas, kProductThreads, kCtas,
+    const int64_t tiles = (int64_t)a.steps * (2 * a.sym_tiles + a.up_tiles);
+    const int64_t most = sm_count / kCtas;
+    return launch(kernel, a, (int)(tiles < most ? tiles : most) * kCtas, kProductThreads, kCtas,
                   kSharedBytes, stream);
 }
 
@@ -806,19 +952,12 @@ cudaError_t launch_ortho_prepare(const OrthoArgs &a, cudaStream_t stream) {
     return launch(ortho_prepare_kernel, a, a.prep_blocks, kThreads, 1, 0, stream);
 }
 
-cudaError_t launch_ortho_product(OrthoProduct what, const OrthoArgs &a, int ctas, int sm_count,
-                                 cudaStream_t stream) {
+cudaError_t launch_ortho_chain(const OrthoArgs &a, int ctas, int sm_count, cudaStream_t stream) {
     if (ctas == 1)
-        return what == kGram     ? launch_product<kGram, 1>(a, sm_count, stream)
-               : what == kPoly   ? launch_product<kPoly, 1>(a, sm_count, stream)
-               : what == kUpdate ? launch_product<kUpdate, 1>(a, sm_count, stream)
-               : what == kFinal  ? launch_product<kFinal, 1>(a, sm_count, stream)
-                                 : launch_product<kFinalBf16, 1>(a, sm_count, stream);
-    return what == kGram     ? launch_product<kGram, 2>(a, sm_count, stream)
-           : what == kPoly   ? launch_product<kPoly, 2>(a, sm_count, stream)
-           : what == kUpdate ? launch_product<kUpdate, 2>(a, sm_count, stream)
-           : what == kFinal  ? launch_product<kFinal, 2>(a, sm_count, stream)
-                             : launch_product<kFinalBf16, 2>(a, sm_count, stream);
+        return a.out_bf16 ? launch_chain<1, true>(a, sm_count, stream)
+                          : launch_chain<1, false>(a, sm_count, stream);
+    return a.out_bf16 ? launch_chain<2, true>(a, sm_count, stream)
+                      : launch_chain<2, false>(a, sm_count, stream);
 }
 
 }  // namespace aloco

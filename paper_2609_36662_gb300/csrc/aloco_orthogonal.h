@@ -33,6 +33,7 @@ struct OrthoGroup {
     float *diag;                     // A's diagonal
     float *lead;                     // a + P's diagonal: what multiplies X itself
     double *partial;                 // [count][chunks] sums of squares
+    int *done;                       // [count] warps that have finished a tile
 };
 
 // What fits a CTA of launch_ortho_small: rows of X, and columns of it.
@@ -49,16 +50,20 @@ constexpr float kOrthoScale = 256.f;
 
 enum OrthoSource { kSourceMatrix, kSourceMuon };
 
+// Operands of the products: X, which alternates between two places, A and P.
+enum { kMapX0, kMapX1, kMapA, kMapP, kOrthoMaps };
+
 struct OrthoArgs {
-    CUtensorMap map_a[kOrthoGroups], map_b[kOrthoGroups];  // the operands of this product
+    CUtensorMap map[kOrthoMaps][kOrthoGroups];
     OrthoGroup g[kOrthoGroups];
     int64_t place[kOrthoMatrices];   // offset in a replica; kSourceMatrix: index in the batch
     int n_groups;
     int sym_tiles, up_tiles, norm_blocks, prep_blocks;      // all groups'
-    int next;                        // which of x[2] the update writes
-    float ca, cb, cc;                // this step's coefficients
-    float coef[ALOCO_MAX_NS_STEPS][3];     // launch_ortho_small: every step's
-    int steps, small_ctas;           // and the CTAs of a matrix
+    float coef[ALOCO_MAX_NS_STEPS][3];     // the steps' coefficients
+    int steps;
+    int small_ctas;                  // launch_ortho_small: the CTAs of a matrix
+    int matrices;                    // all groups'
+    int *next_tile;                  // the next tile to take, and the groups' `done`
     double eps;
     // where the matrices come from and go to
     int source;
@@ -75,15 +80,12 @@ struct OrthoArgs {
                                      // first block leaves out
 };
 
-enum OrthoProduct { kGram, kPoly, kUpdate, kFinal, kFinalBf16 };
-
 int ortho_pair_tile();               // rows of a tile by two CTAs; half by one
 cudaError_t launch_ortho_norm(const OrthoArgs &a, cudaStream_t stream);
 cudaError_t launch_ortho_prepare(const OrthoArgs &a, cudaStream_t stream);
-// ctas: 1 or 2 CTAs share a tile (of 128 or 256 rows and columns)
-cudaError_t launch_ortho_product(OrthoProduct what, const OrthoArgs &a, int ctas, int sm_count,
-                                 cudaStream_t stream);
-
+// All steps' products; ctas: 1 or 2 CTAs share a tile (of 128 or 256 rows and
+// columns).
+cudaError_t launch_ortho_chain(const OrthoArgs &a, int ctas, int sm_count, cudaStream_t stream);
 // All steps of matrices with m <= kOrthoSmallSide and n <= kOrthoSmallCols *
 // a.small_ctas (1, 2, 4, 8 or 16, if the device has room for such a cluster).
 cudaError_t ortho_small_setup(int ctas, bool *fits);

@@ -155,7 +155,7 @@ def test_a_copy_or_product_that_never_comes_ends_in_nan(shape):
     A.test_stall_tile(1)
     out = A.orthogonalize(x)
     torch.cuda.synchronize()
-    assert out[0].isnan().any()
+    assert out.isnan().any()
     assert torch.equal(A.orthogonalize(x), want)
 
 
