@@ -28,10 +28,12 @@ constexpr int kRing = 4;             // tiles that a CTA knows of
 enum { kGram, kPoly, kUpdate };
 
 struct Work {
-    int what, step, group, matrix;
+    int what, step, group, matrix;   // what < 0: there is no more
     int row, col;                    // in tiles
     int before;                      // tiles of the matrix that have to be done
+    int unused;
 };
+static_assert(sizeof(Work) == 32, "a ring's entry");
 
 __device__ __forceinline__ Work find_work(const OrthoArgs &a, int t, int tile) {
     Work f;
@@ -307,7 +309,9 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     const uint32_t drained = bars + 8 * (2 * kSlots + 4);
     const auto told = [&](int s) { return bars + 8 * (2 * kSlots + 5 + s); };
     const auto heard = [&](int s) { return bars + 8 * (2 * kSlots + 5 + kRing + s); };
-    const auto tile_at = [&](int s) { return bars + 8 * (2 * kSlots + 5 + 2 * kRing) + 4 * s; };
+    const auto work_at = [&](int s) {
+        return ((bars + 8 * (2 * kSlots + 5 + 2 * kRing) + 15) & ~15u) + 32 * s;
+    };
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_abort;
 
@@ -345,16 +349,25 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     grid_go();
     grid_wait();
 
-    // The next tile, as all but the first producer hear of it; -1: there is none.
+    // The next tile, as all but the first producer hear of it.
     int ring = 0;
     uint32_t ring_phase = 0;
     const auto on = [&] {
         if (++ring == kRing) ring = 0, ring_phase ^= 1;
     };
-    const auto hear = [&](bool whole_warp) -> int {
-        int t = -1;
-        if (mbar_wait_cluster(told(ring), ring_phase))
-            asm volatile("ld.shared.s32 %0, [%1];" : "=r"(t) : "r"(tile_at(ring)) : "memory");
+    const auto hear = [&](bool whole_warp) -> Work {
+        Work f;
+        f.what = -1;
+        if (mbar_wait_cluster(told(ring), ring_phase)) {
+            asm volatile("ld.shared.v4.s32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(f.what), "=r"(f.step), "=r"(f.group), "=r"(f.matrix)
+                         : "r"(work_at(ring))
+                         : "memory");
+            asm volatile("ld.shared.v4.s32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(f.row), "=r"(f.col), "=r"(f.before), "=r"(f.unused)
+                         : "r"(work_at(ring) + 16)
+                         : "memory");
+        }
         if (whole_warp) __syncwarp();
         if (!whole_warp || lane == 0) {
             if (kCtas == 1 || rank == 0)
@@ -365,7 +378,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                              : "memory");
         }
         on();
-        return t;
+        return f;
     };
     const auto done_of = [&](const Work &f) { return args.g[f.group].done + f.matrix; };
     const auto depth = [&](const Work &f) {
@@ -382,28 +395,31 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         bool ok = true;
         int next = tells ? atomicAdd(args.next_tile, 1) : 0;
         for (;;) {
-            int t;
+            Work f;
             if (tells) {
-                t = next < tiles ? next : -1;
+                f = find_work(args, min(next, tiles - 1), kTile);
+                if (next >= tiles) f.what = -1;
                 if (!mbar_wait_cluster(heard(ring), ring_phase ^ 1)) break;
-                asm volatile("st.shared.s32 [%0], %1;" ::"r"(tile_at(ring)), "r"(t) : "memory");
-                mbar_arrive(told(ring));
-                if constexpr (kCtas == 2) {
-                    asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(
-                                     cluster_addr(tile_at(ring), 1)),
-                                 "r"(t)
+                for (int p = 0; p < kCtas; ++p) {
+                    const uint32_t at = kCtas == 1 ? work_at(ring) : cluster_addr(work_at(ring), p);
+                    asm volatile("st.shared::cluster.v4.s32 [%0], {%1, %2, %3, %4};" ::"r"(at),
+                                 "r"(f.what), "r"(f.step), "r"(f.group), "r"(f.matrix)
                                  : "memory");
+                    asm volatile("st.shared::cluster.v4.s32 [%0], {%1, %2, %3, %4};" ::"r"(at + 16),
+                                 "r"(f.row), "r"(f.col), "r"(f.before), "r"(0)
+                                 : "memory");
+                }
+                mbar_arrive(told(ring));
+                if constexpr (kCtas == 2)
                     asm volatile(
                         "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(
                             cluster_addr(told(ring), 1))
                         : "memory");
-                }
                 on();
             } else {
-                t = hear(false);
+                f = hear(false);
             }
-            if (t < 0) break;
-            const Work f = find_work(args, t, kTile);
+            if (f.what < 0) break;
             const int chunks = (depth(f) + kK - 1) / kK;
             const int ask = max(0, chunks - kSlots);   // where to take the next tile
             if (ok && !s_abort)
@@ -451,9 +467,8 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         uint32_t phase = 0, acc_phase = 0;
         bool ok = true;
         for (;;) {
-            const int t = hear(false);
-            if (t < 0) break;
-            const Work f = find_work(args, t, kTile);
+            const Work f = hear(false);
+            if (f.what < 0) break;
             const int K = depth(f);
             if (ok) ok = mbar_wait(acc_empty(acc), acc_phase ^ 1, &s_abort);
             tc_fence_after();
@@ -500,9 +515,8 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         int acc = 0;
         uint32_t acc_phase = 0;
         for (;;) {
-            const int t = hear(true);
-            if (t < 0) break;
-            const Work f = find_work(args, t, kTile);
+            const Work f = hear(true);
+            if (f.what < 0) break;
             const OrthoGroup &g = args.g[f.group];
             const bool last = f.what == kUpdate && f.step + 1 == args.steps;
             const int m = g.m, r0 = f.row * kTile + (int)rank * kHalfTile + quad * 32;
