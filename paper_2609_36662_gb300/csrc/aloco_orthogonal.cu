@@ -530,6 +530,11 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                                   f.row * kTile / kFull == f.col * kTile / kFull;
             const float ca = args.coef[f.step][0], cb = args.coef[f.step][1],
                         cc = args.coef[f.step][2];
+            // P = c (A + e)^2 - c e^2 with e = b / 2c, which is added to A's diagonal: its
+            // tiles need nothing but their product.  (Where e is large against A, P
+            // is put together from A's values.)
+            const bool square = fabsf(cb) <= 4.f * fabsf(cc);
+            const float shift = square ? cb / (2.f * cc) : 0.f;
             // what a product is joined with: of A or P whole rows, of X also blocks that
             // lie as this warp holds them; fetched a block ahead
             uint4 *rest = g.rest + ((int64_t)(f.matrix * g.blocks_down + r0 / 32) * g.blocks_across +
@@ -561,7 +566,9 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             }
             bool ok = !s_abort;
             if (f.what != kGram && some) {
-                if (ok) ok = wait_done(done_of(f), f.before * kSignals, &s_abort);
+                // (products that are done had what they needed)
+                if (ok && !__all_sync(~0u, mbar_test(acc_full(acc), acc_phase)))
+                    ok = wait_done(done_of(f), f.before * kSignals, &s_abort);
                 ok = __all_sync(~0u, ok);
                 if (f.what == kUpdate) {
                     // what is kept of X beside the operands comes to L2 while the
@@ -572,7 +579,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                     fetch_x(c0);
                 } else {
                     if (r < m) by_row = __ldcg(g.diag + row0 + r);
-                    fetch_a(c0);
+                    if (!square) fetch_a(c0);
                 }
             }
             if (ok) ok = mbar_wait(acc_full(acc), acc_phase, &s_abort);
@@ -615,10 +622,31 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                         float own = 0.f;
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (i == lane) own = v[i], v[i] = 0.f;
+                            if (i == lane) own = v[i], v[i] = square ? own + shift : 0.f;
                         if (r < m) g.diag[row0 + r] = own;
                     }
                     store_symmetric(g.a + row0 * g.lda, m, g.lda, r0, c0, mirrored, st, v);
+                }
+            } else if (f.what == kPoly && square) {
+#pragma unroll 1
+                for (; c0 < c_end; c0 += 32) {
+                    float v[32];
+                    values(v);
+                    if (c0 == r0) {
+                        float own = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (i == lane) own = v[i], v[i] = 0.f;
+                        // the diagonal's own square as the product has it is taken out,
+                        // and put back from what was not rounded
+                        const float rounded = __half2float(__float2half_rn(by_row + shift));
+                        if (r < m)
+                            g.lead[row0 + r] =
+                                ca + cb * by_row + cc * (by_row * by_row + (own - rounded * rounded));
+                    }
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] *= cc;
+                    store_symmetric(g.p + row0 * g.lda, m, g.lda, r0, c0, mirrored, st, v);
                 }
             } else if (f.what == kPoly) {
                 // b a + c ((d_r + d_c) a + x); where A's diagonal is taken out a is 0

@@ -13,7 +13,8 @@ namespace aloco {
 // rows (m <= n), as a sum of two fp16 values: the larger ones row by row, whose
 // products are taken, and what they leave, which only what multiplies X itself
 // sees, in blocks of 32 x 32 laid out as the epilogue's threads hold them.  A = X X^T and P = b A + c A A are m x m in fp16 with zeros
-// on the diagonal, which is kept in fp32 beside them.  Rows lie ldx and lda
+// on the diagonal (A: or b / 2c more than its values), which is kept in fp32
+// beside them.  Rows lie ldx and lda
 // elements apart (multiples of 8).
 struct OrthoGroup {
     int m, n, ldx, lda;
