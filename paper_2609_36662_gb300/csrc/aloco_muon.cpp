@@ -1,6 +1,7 @@
 // Entry points of the orthogonalised updates: argument checks, the split of
 // the matrices into passes, and the passes' launches (aloco_orthogonal.cu).
 #include <algorithm>
+#include <array>
 #include <cmath>
 #include <limits>
 #include <new>
@@ -23,8 +24,8 @@ constexpr size_t kAlign = 256;
 
 size_t up(size_t x, size_t to) { return (x + to - 1) / to * to; }
 
-// The next tile and the tiles done of every matrix of a pass.
-size_t counter_bytes(int64_t matrices) { return up((size_t)(matrices + 1) * 4, kAlign); }
+// SMs that passes are planned for: scratch is reckoned without a device.
+constexpr int kPlannedSms = 152;
 
 // Matrices of one shape: `period` places of M workers.
 struct Shape {
@@ -56,10 +57,15 @@ struct Part {
     int shape;
     int64_t skip, count;
 };
+// Matrices that go through the products' kernel together.
 struct Pass {
     std::vector<Part> parts;
     int places = 0;
-    size_t bytes = 0;
+    size_t bytes = 0;                // but for what follows from the tiles:
+    int ctas = 2;                    // that share one
+    std::vector<std::array<int, 2>> split;  // by part: of A's and P's tiles
+    size_t counters = 0;             // ints that begin as zero
+    size_t all_bytes = 0;
 };
 
 // Matrices that one kernel takes through all steps, `ctas` to a matrix.
@@ -87,6 +93,68 @@ int small_ctas(const Shape &s, int most) {
 
 // The largest cluster that every device takes, which scratch is reckoned with.
 constexpr int kPortableCtas = 8;
+
+int64_t tiles_of(int64_t x, int tile) { return (x + tile - 1) / tile; }
+int64_t sym_tiles(const Shape &s, int tile) {
+    const int64_t rows = tiles_of(s.m(), tile);
+    return rows * (rows + 1) / 2;
+}
+// Bytes of the sums that the parts of a group's tiles leave.
+size_t sums_bytes(const Shape &s, int64_t count, const std::array<int, 2> &split, int tile) {
+    const int parts = std::max(split[0], split[1]);
+    return parts > 1 ? (size_t)(count * sym_tiles(s, tile) * parts) * tile * tile * 4 : 0;
+}
+
+// Tiles by pairs of CTAs where they fill the GPU; by single CTAs, whose tiles are a
+// quarter, below.  Where A's or P's tiles are fewer than the CTAs, parts of their
+// depth are tiles of their own: as many as there are CTAs for, of at least 12
+// slots.  (5632 x 2048 alone: 88 slots a tile of A, 36 tiles for 76 pairs.)
+void lay_out(const Plan &plan, Pass *pass) {
+    int64_t up_tiles = 0;
+    for (const Part &part : pass->parts) {
+        const Shape &s = plan.shapes[part.shape];
+        up_tiles += part.count * tiles_of(s.m(), ortho_pair_tile()) *
+                    tiles_of(s.n(), ortho_pair_tile());
+    }
+    pass->ctas = up_tiles >= kPlannedSms / 2 ? 2 : 1;
+    const int tile = ortho_pair_tile() / 2 * pass->ctas, slots = kPlannedSms / pass->ctas;
+    pass->split.assign(pass->parts.size(), {1, 1});
+    for (int what = 0; what < 2; ++what) {
+        const auto chunks = [&](const Part &part) {
+            const Shape &s = plan.shapes[part.shape];
+            return tiles_of(what == 0 ? s.n() : s.m(), ortho_slot_depth());
+        };
+        int64_t most = 0, tiles = 0;
+        for (const Part &part : pass->parts) {
+            most = std::max(most, chunks(part));
+            tiles += part.count * sym_tiles(plan.shapes[part.shape], tile);
+        }
+        if (tiles >= slots) continue;
+        for (int64_t depth = 12; depth < most; depth = depth * 5 / 4) {
+            int64_t parts = 0;
+            for (const Part &part : pass->parts)
+                parts += part.count * sym_tiles(plan.shapes[part.shape], tile) *
+                         tiles_of(chunks(part), (int)depth);
+            if (parts > slots) continue;
+            for (size_t i = 0; i < pass->parts.size(); ++i)
+                pass->split[i][what] = (int)tiles_of(chunks(pass->parts[i]), (int)depth);
+            break;
+        }
+    }
+    pass->counters = 1;
+    pass->all_bytes = pass->bytes;
+    for (size_t i = 0; i < pass->parts.size(); ++i) {
+        const Part &part = pass->parts[i];
+        const Shape &s = plan.shapes[part.shape];
+        pass->counters += (size_t)part.count;
+        const size_t sums = sums_bytes(s, part.count, pass->split[i], tile);
+        if (!sums) continue;
+        pass->counters += (size_t)(part.count * sym_tiles(s, tile)) * pass->ctas *
+                          ortho_epilogue_warps();
+        pass->all_bytes += up(sums, kAlign);
+    }
+    pass->all_bytes += up(pass->counters * 4, kAlign);
+}
 
 // Shapes in `p` (places set) into passes that keep within kPassBytes, kOrthoGroups
 // and kOrthoMatrices: deep products first, so that the last tiles are short.
@@ -123,9 +191,8 @@ void split(Plan *p, int workers, int most_ctas) {
     Pass pass;
     const auto flush = [&] {
         if (pass.parts.empty()) return;
-        int64_t matrices = 0;
-        for (const Part &part : pass.parts) matrices += part.count;
-        p->bytes = std::max(p->bytes, pass.bytes + counter_bytes(matrices));
+        lay_out(*p, &pass);
+        p->bytes = std::max(p->bytes, pass.all_bytes);
         p->passes.push_back(std::move(pass));
         pass = Pass();
     };
@@ -239,22 +306,6 @@ int tensor_map(CUtensorMap *map, void *data, int64_t cols, int64_t rows, int64_t
     return ALOCO_OK;
 }
 
-// Tiles of all groups for products by `ctas` CTAs a tile.
-void count_tiles(OrthoArgs *a, int ctas) {
-    const int tile = ortho_pair_tile() / 2 * ctas;
-    a->sym_tiles = a->up_tiles = 0;
-    for (int i = 0; i < a->n_groups; ++i) {
-        OrthoGroup &g = a->g[i];
-        const int rows = (g.m + tile - 1) / tile;
-        g.sym_tiles = rows * (rows + 1) / 2;
-        g.up_tiles = rows * ((g.n + tile - 1) / tile);
-        g.sym0 = a->sym_tiles;
-        g.up0 = a->up_tiles;
-        a->sym_tiles += g.sym_tiles * g.count;
-        a->up_tiles += g.up_tiles * g.count;
-    }
-}
-
 // What both kinds of passes fill in of a group.
 void fill_group(const Plan &plan, const Part &part, int64_t *places, int *n_places,
                 OrthoGroup *g) {
@@ -300,9 +351,10 @@ int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base, const do
     };
     a.n_groups = (int)pass.parts.size();
     int places = 0, norm = 0, prep = 0;
-    for (const Part &part : pass.parts) a.matrices += (int)part.count;
-    a.next_tile = (int *)take(counter_bytes(a.matrices));
-    int *done = a.next_tile + 1;
+    a.counters = (int)pass.counters;
+    a.next_tile = (int *)take(pass.counters * 4);
+    int *counter = a.next_tile + 1;
+    const int tile = ortho_pair_tile() / 2 * pass.ctas;
     for (int i = 0; i < a.n_groups; ++i) {
         const Part &part = pass.parts[i];
         const Shape &s = plan.shapes[part.shape];
@@ -328,8 +380,22 @@ int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base, const do
         g.diag = (float *)take((size_t)(count * m) * 4);
         g.lead = (float *)take((size_t)(count * m) * 4);
         g.partial = (double *)take((size_t)(count * s.chunks()) * 8);
-        g.done = done;
-        done += count;
+        g.done = counter;
+        counter += count;
+        g.sym_tiles = (int)sym_tiles(s, tile);
+        g.up_tiles = (int)(tiles_of(m, tile) * tiles_of(n, tile));
+        for (int k = 0; k < 2; ++k) g.split[k] = pass.split[i][k];
+        g.gram0 = a.gram_tiles;
+        g.poly0 = a.poly_tiles;
+        g.up0 = a.up_tiles;
+        a.gram_tiles += g.sym_tiles * g.split[0] * g.count;
+        a.poly_tiles += g.sym_tiles * g.split[1] * g.count;
+        a.up_tiles += g.up_tiles * g.count;
+        if (const size_t sums = sums_bytes(s, count, pass.split[i], tile)) {
+            g.sums = (float4 *)take(sums);
+            g.came = counter;
+            counter += count * g.sym_tiles * pass.ctas * ortho_epilogue_warps();
+        }
         a.step[i] = shape_step ? (float)shape_step[part.shape] : 0.f;
         int rc;
         for (int k = 0; k < 2; ++k)
@@ -340,15 +406,9 @@ int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base, const do
     }
     a.norm_blocks = norm;
     a.prep_blocks = prep;
-    // Pairs of CTAs where their tiles fill the GPU; single CTAs, whose tiles are
-    // a quarter, below.
-    int ctas = 2;
-    count_tiles(&a, ctas);
-    if (a.up_tiles < sm_count / 2) count_tiles(&a, ctas = 1);
-
     cudaError_t e = launch_ortho_norm(a, stream);
     if (e == cudaSuccess) e = launch_ortho_prepare(a, stream);
-    if (e == cudaSuccess) e = launch_ortho_chain(a, ctas, sm_count, stream);
+    if (e == cudaSuccess) e = launch_ortho_chain(a, pass.ctas, sm_count, stream);
     return e == cudaSuccess ? ALOCO_OK : cuda_fail(e, "orthogonal factor");
 }
 

@@ -1,6 +1,7 @@
 // Orthogonal factors by Newton-Schulz products on the tensor cores: X <- (a +
 // b A + c A A) X with A = X X^T, some steps of it, for many matrices at once.
 #include <climits>
+#include <type_traits>
 
 #include "aloco_orthogonal.cuh"
 #include "aloco_tc.cuh"
@@ -31,18 +32,19 @@ struct Work {
     int what, step, group, matrix;   // what < 0: there is no more
     int row, col;                    // in tiles
     int before;                      // tiles of the matrix that have to be done
-    int unused;
+    int part;                        // of the depth
 };
 static_assert(sizeof(Work) == 32, "a ring's entry");
 
 __device__ __forceinline__ Work find_work(const OrthoArgs &a, int t, int tile) {
     Work f;
-    const int per = 2 * a.sym_tiles + a.up_tiles;
+    const int per = a.gram_tiles + a.poly_tiles + a.up_tiles;
     f.step = t / per;
     t -= f.step * per;
-    f.what = t >= 2 * a.sym_tiles ? kUpdate : t >= a.sym_tiles ? kPoly : kGram;
-    t -= f.what * a.sym_tiles;
-    if (f.what == kUpdate) {
+    f.part = 0;
+    if (t >= a.gram_tiles + a.poly_tiles) {
+        f.what = kUpdate;
+        t -= a.gram_tiles + a.poly_tiles;
         f.group = find_group(a, t, [](const OrthoGroup &g) { return g.up0; });
         const OrthoGroup &g = a.g[f.group];
         t -= g.up0;
@@ -52,11 +54,21 @@ __device__ __forceinline__ Work find_work(const OrthoArgs &a, int t, int tile) {
         f.col = t / rows;            // the rows of P first: X's columns stay in L2
         f.row = t - f.col * rows;
     } else {
-        f.group = find_group(a, t, [](const OrthoGroup &g) { return g.sym0; });
+        f.what = t >= a.gram_tiles ? kPoly : kGram;
+        if (f.what == kPoly) {
+            t -= a.gram_tiles;
+            f.group = find_group(a, t, [](const OrthoGroup &g) { return g.poly0; });
+            t -= a.g[f.group].poly0;
+        } else {
+            f.group = find_group(a, t, [](const OrthoGroup &g) { return g.gram0; });
+            t -= a.g[f.group].gram0;
+        }
         const OrthoGroup &g = a.g[f.group];
-        t -= g.sym0;
-        f.matrix = t / g.sym_tiles;
-        t -= f.matrix * g.sym_tiles;
+        const int parts = g.split[f.what];
+        f.matrix = t / (g.sym_tiles * parts);
+        t -= f.matrix * g.sym_tiles * parts;
+        f.part = t % parts;
+        t /= parts;
         // row r of the lower triangle holds tiles r (r + 1) / 2 ..
         int r = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
         while (r * (r + 1) / 2 > t) --r;
@@ -293,7 +305,7 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity)
 //
 // A wait that runs out ends the waits of its CTA; its tiles are NaN from there on,
 // and with them their matrices.
-template <int kCtas, bool kOutBf16>
+template <int kCtas, bool kOutBf16, bool kParts>
 __global__ void __launch_bounds__(kProductThreads, 1)
     ortho_chain_kernel(const __grid_constant__ OrthoArgs args) {
     constexpr int kTile = kHalfTile * kCtas;
@@ -317,7 +329,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = kCtas == 1 ? 0 : cluster_rank();
-    const int tiles = args.steps * (2 * args.sym_tiles + args.up_tiles);
+    const int tiles = args.steps * (args.gram_tiles + args.poly_tiles + args.up_tiles);
 
     if (threadIdx.x == 0) {
         s_abort = 0;
@@ -364,7 +376,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                          : "r"(work_at(ring))
                          : "memory");
             asm volatile("ld.shared.v4.s32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(f.row), "=r"(f.col), "=r"(f.before), "=r"(f.unused)
+                         : "=r"(f.row), "=r"(f.col), "=r"(f.before), "=r"(f.part)
                          : "r"(work_at(ring) + 16)
                          : "memory");
         }
@@ -383,6 +395,14 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     const auto done_of = [&](const Work &f) { return args.g[f.group].done + f.matrix; };
     const auto depth = [&](const Work &f) {
         return f.what == kGram ? args.g[f.group].n : args.g[f.group].m;
+    };
+    // the slots that a tile, or its part, takes
+    const auto slots_of = [&](const Work &f, int *begin) {
+        const int chunks = (depth(f) + kK - 1) / kK;
+        const int parts =
+            !kParts || f.what == kUpdate ? 1 : args.g[f.group].split[f.what];
+        *begin = chunks * f.part / parts;
+        return chunks * (f.part + 1) / parts;
     };
 
     if ((warp == 0 || warp == 3) && lane == 0) {
@@ -406,7 +426,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                                  "r"(f.what), "r"(f.step), "r"(f.group), "r"(f.matrix)
                                  : "memory");
                     asm volatile("st.shared::cluster.v4.s32 [%0], {%1, %2, %3, %4};" ::"r"(at + 16),
-                                 "r"(f.row), "r"(f.col), "r"(f.before), "r"(0)
+                                 "r"(f.row), "r"(f.col), "r"(f.before), "r"(f.part)
                                  : "memory");
                 }
                 mbar_arrive(told(ring));
@@ -420,8 +440,9 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 f = hear(false);
             }
             if (f.what < 0) break;
-            const int chunks = (depth(f) + kK - 1) / kK;
-            const int ask = max(0, chunks - kSlots);   // where to take the next tile
+            int k0;
+            const int chunks = slots_of(f, &k0);
+            const int ask = max(k0, chunks - kSlots);  // where to take the next tile
             if (ok && !s_abort)
                 ok = wait_done(done_of(f), f.before * kSignals, &s_abort);
             else
@@ -437,7 +458,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             const int turn = f.what == kGram            ? INT_MAX
                              : f.what == kUpdate && is_b ? 0
                                                          : (row / kFull + 1) * kFull;
-            for (int k = 0; k < chunks; ++k) {
+            for (int k = k0; k < chunks; ++k) {
                 if (tells && k == ask) next = atomicAdd(args.next_tile, 1);
                 if (!ok || !(ok = mbar_wait(empty(slot), phase ^ 1, &s_abort))) continue;
                 const uint32_t at = smem + slot * kSlotBytes + (is_b ? 2 * kBoxBytes : 0);
@@ -469,7 +490,9 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         for (;;) {
             const Work f = hear(false);
             if (f.what < 0) break;
-            const int K = depth(f);
+            int k0;
+            const int k_end = slots_of(f, &k0) * kK, K = min(depth(f), k_end);
+            k0 *= kK;
             if (ok) ok = mbar_wait(acc_empty(acc), acc_phase ^ 1, &s_abort);
             tc_fence_after();
             const int turn_a = f.what == kGram ? INT_MAX : (f.row * kTile / kFull + 1) * kFull;
@@ -477,7 +500,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                                : f.what == kUpdate ? 0
                                                    : (f.col * kTile / kFull + 1) * kFull;
             const uint32_t d = tmem + acc * kTile;
-            for (int k = 0; ok && k < K; k += kK) {
+            for (int k = k0; ok && k < K; k += kK) {
                 if (!(ok = mbar_wait(full(slot), phase, &s_abort))) break;
                 tc_fence_after();
                 const uint32_t a0 = smem + slot * kSlotBytes, b0 = a0 + 2 * kBoxBytes;
@@ -488,7 +511,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 // 16 k-elements on, in 16 bytes: 32 bytes of a row, or 16 rows
                 const int na = ta ? 2048 / 16 : 2, nb = tb ? 2048 / 16 : 2;
                 // (straight on: between products this thread has 128 cycles)
-                product<kCtas>(d, da, db, desc, k != 0);
+                product<kCtas>(d, da, db, desc, k != k0);
                 if (K - k > 16) product<kCtas>(d, da + na, db + nb, desc, true);
                 if (K - k > 32) product<kCtas>(d, da + 2 * na, db + 2 * nb, desc, true);
                 if (K - k > 48) product<kCtas>(d, da + 3 * na, db + 3 * nb, desc, true);
@@ -596,8 +619,62 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 else
                     mbar_arrive_cluster(cluster_addr(acc_empty(acc), 0));
             };
-            // column c0's accumulators of this row
+            // A part of a tile leaves its sums; the warp that finds all others' there
+            // goes on with the tile.
+            const int parts = !kParts || f.what == kUpdate ? 1 : g.split[f.what];
+            bool finishes = true;
+            const float4 *sums = nullptr;
+            const int64_t next_part = kCtas * kEpilogueWarps * (kTile / 64) * kBlockQuads;
+            if (kParts && parts > 1 && some) {
+                const int64_t tile =
+                    (int64_t)f.matrix * g.sym_tiles + f.row * (f.row + 1) / 2 + f.col;
+                const int place = (int)rank * kEpilogueWarps + warp - kEpilogueWarp;
+                float4 *at = g.sums + tile * max(g.split[0], g.split[1]) * next_part +
+                             place * (kTile / 64) * kBlockQuads + lane;
+                sums = at;
+                at += f.part * next_part;
+#pragma unroll 1
+                for (int c = c0; c < c_end; c += 32, at += kBlockQuads) {
+                    uint32_t u[32];
+                    tmem_read32(tmem + acc * kTile + (c - f.col * kTile) + (quad << 21), u);
+                    const float bad = ok ? 0.f : __int_as_float(0x7fffffff);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        at[32 * i] = make_float4(
+                            __uint_as_float(u[4 * i]) + bad, __uint_as_float(u[4 * i + 1]) + bad,
+                            __uint_as_float(u[4 * i + 2]) + bad, __uint_as_float(u[4 * i + 3]) + bad);
+                }
+                release();
+                int came = 0;
+                if (lane == 0) {
+                    int *count = g.came + tile * kSignals + place;
+                    asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;"
+                                 : "=r"(came)
+                                 : "l"(count)
+                                 : "memory");
+                    if (came == parts - 1) *count = 0;   // for the next product
+                }
+                finishes = __shfl_sync(~0u, came, 0) == parts - 1;
+                __syncwarp();
+            }
+            // column c0's sums of this row
             const auto values = [&](float (&v)[32]) {
+                if (kParts && sums) {
+                    const float4 *p = sums + (c0 - begin) / 32 * kBlockQuads;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = 0.f;
+                    for (int k = 0; k < parts; ++k, p += next_part) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float4 q = __ldcg(p + 32 * i);
+                            v[4 * i] += q.x;
+                            v[4 * i + 1] += q.y;
+                            v[4 * i + 2] += q.z;
+                            v[4 * i + 3] += q.w;
+                        }
+                    }
+                    return;
+                }
                 uint32_t u[32];
                 __syncwarp();
                 tmem_read32(tmem + acc * kTile + (c0 - f.col * kTile) + (quad << 21), u);
@@ -611,6 +688,8 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             };
             if (!some) {
                 release();
+                finishes = parts == 1 || f.part == 0;
+            } else if (!finishes) {
             } else if (f.what == kGram) {
 #pragma unroll 1
                 for (; c0 < c_end; c0 += 32) {
@@ -748,7 +827,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                                 g.n - c0);
                 }
             }
-            if (!last) {
+            if (!last && finishes) {
                 // done: what this warp has written is seen behind the count (by tensor
                 // copies behind a fence of theirs)
                 __syncwarp();
@@ -784,8 +863,9 @@ __global__ void __launch_bounds__(kThreads) ortho_norm_kernel(const __grid_const
     __shared__ double shared[kThreads / 32];
     grid_go();
     grid_wait();
-    if (blockIdx.x == 0)             // for the products' kernel: its tiles, and those done
-        for (int i = threadIdx.x; i <= args.matrices; i += kThreads) args.next_tile[i] = 0;
+    for (int i = blockIdx.x * kThreads + threadIdx.x; i < args.counters;
+         i += gridDim.x * kThreads)
+        args.next_tile[i] = 0;       // for the products' kernel
     const int gi = find_group(args, blockIdx.x, [](const OrthoGroup &g) { return g.norm0; });
     const OrthoGroup &g = args.g[gi];
     const int b = blockIdx.x - g.norm0, matrix = b / g.chunks, chunk = b - matrix * g.chunks;
@@ -965,10 +1045,10 @@ cudaError_t launch(K kernel, const OrthoArgs &a, int grid, int threads, int ctas
     return cudaLaunchKernelEx(&c, kernel, a);
 }
 
-template <int kCtas, bool kOutBf16>
+template <int kCtas, bool kOutBf16, bool kParts>
 cudaError_t launch_chain(const OrthoArgs &a, int sm_count, cudaStream_t stream) {
     static PerDevice ready;
-    const auto kernel = ortho_chain_kernel<kCtas, kOutBf16>;
+    const auto kernel = ortho_chain_kernel<kCtas, kOutBf16, kParts>;
     const int d = PerDevice::device();
     if (!ready.get(d)) {
         const cudaError_t e = cudaFuncSetAttribute(
@@ -976,7 +1056,7 @@ cudaError_t launch_chain(const OrthoArgs &a, int sm_count, cudaStream_t stream) 
         if (e != cudaSuccess) return e;
         ready.set(d, 1);
     }
-    const int64_t tiles = (int64_t)a.steps * (2 * a.sym_tiles + a.up_tiles);
+    const int64_t tiles = (int64_t)a.steps * (a.gram_tiles + a.poly_tiles + a.up_tiles);
     const int64_t most = sm_count / kCtas;
     return launch(kernel, a, (int)(tiles < most ? tiles : most) * kCtas, kProductThreads, kCtas,
                   kSharedBytes, stream);
@@ -985,6 +1065,8 @@ cudaError_t launch_chain(const OrthoArgs &a, int sm_count, cudaStream_t stream) 
 }  // namespace
 
 int ortho_pair_tile() { return 2 * kHalfTile; }
+int ortho_slot_depth() { return kK; }
+int ortho_epilogue_warps() { return kEpilogueWarps; }
 
 cudaError_t launch_ortho_norm(const OrthoArgs &a, cudaStream_t stream) {
     return launch(ortho_norm_kernel, a, a.norm_blocks, kThreads, 1, 0, stream);
@@ -995,11 +1077,17 @@ cudaError_t launch_ortho_prepare(const OrthoArgs &a, cudaStream_t stream) {
 }
 
 cudaError_t launch_ortho_chain(const OrthoArgs &a, int ctas, int sm_count, cudaStream_t stream) {
-    if (ctas == 1)
-        return a.out_bf16 ? launch_chain<1, true>(a, sm_count, stream)
-                          : launch_chain<1, false>(a, sm_count, stream);
-    return a.out_bf16 ? launch_chain<2, true>(a, sm_count, stream)
-                      : launch_chain<2, false>(a, sm_count, stream);
+    bool parts = false;
+    for (int i = 0; i < a.n_groups; ++i)
+        parts = parts || a.g[i].split[0] > 1 || a.g[i].split[1] > 1;
+    const auto by = [&](auto n, auto p) {
+        return a.out_bf16 ? launch_chain<n.value, true, p.value>(a, sm_count, stream)
+                          : launch_chain<n.value, false, p.value>(a, sm_count, stream);
+    };
+    const std::integral_constant<int, 1> one;
+    const std::integral_constant<int, 2> two;
+    if (ctas == 1) return parts ? by(one, std::true_type()) : by(one, std::false_type());
+    return parts ? by(two, std::true_type()) : by(two, std::false_type());
 }
 
 }  // namespace aloco

@@ -12,9 +12,9 @@ namespace aloco {
 // Matrices of one shape in a pass.  X is the matrix with its smaller side as
 // rows (m <= n), as a sum of two fp16 values: the larger ones row by row, whose
 // products are taken, and what they leave, which only what multiplies X itself
-// sees, in blocks of 32 x 32 laid out as the epilogue's threads hold them.  A = X X^T and P = b A + c A A are m x m in fp16 with zeros
-// on the diagonal (A: or b / 2c more than its values), which is kept in fp32
-// beside them.  Rows lie ldx and lda
+// sees, in blocks of 32 x 32 laid out as the epilogue's threads hold them.  A = X X^T
+// and P = b A + c A A are m x m in fp16 with zeros on the diagonal (A: or b / 2c more
+// than its values), which is kept in fp32 beside them.  Rows lie ldx and lda
 // elements apart (multiples of 8).
 struct OrthoGroup {
     int m, n, ldx, lda;
@@ -24,7 +24,8 @@ struct OrthoGroup {
     int first, period, skip;         // the i-th: number first + (skip + i) % period
                                      // of worker (skip + i) / period
     int sym_tiles, up_tiles;         // tiles of a matrix: symmetric products, update
-    int sym0, up0;                   // the group's first tile
+    int split[2];                    // parts of the depth of A's and P's tiles
+    int gram0, poly0, up0;           // the group's first tile (part of one)
     int chunks, chunk;               // norm blocks of a matrix, elements of each
     int norm0, prep0;                // the group's first block
     int small0;                      // its first cluster (launch_ortho_small)
@@ -35,6 +36,10 @@ struct OrthoGroup {
     float *lead;                     // a + P's diagonal: what multiplies X itself
     double *partial;                 // [count][chunks] sums of squares
     int *done;                       // [count] warps that have finished a tile
+    // where tiles have parts: their sums, a block as a warp holds it after the other,
+    // and how many of a tile's parts a warp's place has
+    float4 *sums;                    // [count][sym_tiles][parts]
+    int *came;                       // [count][sym_tiles][warps]
 };
 
 // What fits a CTA of launch_ortho_small: rows of X, and columns of it.
@@ -43,7 +48,7 @@ constexpr int kOrthoSmallSide = 128, kOrthoSmallCols = 256, kOrthoSmallCtas = 16
 constexpr int kOrthoGroups = 16;     // groups of a pass
 constexpr int kOrthoMatrices = 1024; // places of a pass (a worker's)
 
-constexpr int kBlockPieces = 32 * 32 / 8;
+constexpr int kBlockPieces = 32 * 32 / 8, kBlockQuads = 32 * 32 / 4;
 
 // X is held times 2^8, so that fp16 keeps its values of any realistic size in
 // its normal range (its largest value is at most about 1.2).
@@ -59,12 +64,12 @@ struct OrthoArgs {
     OrthoGroup g[kOrthoGroups];
     int64_t place[kOrthoMatrices];   // offset in a replica; kSourceMatrix: index in the batch
     int n_groups;
-    int sym_tiles, up_tiles, norm_blocks, prep_blocks;      // all groups'
+    int gram_tiles, poly_tiles, up_tiles, norm_blocks, prep_blocks;  // all groups'
     float coef[ALOCO_MAX_NS_STEPS][3];     // the steps' coefficients
     int steps;
     int small_ctas;                  // launch_ortho_small: the CTAs of a matrix
-    int matrices;                    // all groups'
-    int *next_tile;                  // the next tile to take, and the groups' `done`
+    int *next_tile;                  // the next tile to take, `done` and `came`: zero
+    int counters;                    // when the products begin, so many
     double eps;
     // where the matrices come from and go to
     int source;
@@ -82,6 +87,8 @@ struct OrthoArgs {
 };
 
 int ortho_pair_tile();               // rows of a tile by two CTAs; half by one
+int ortho_slot_depth();              // k-elements of a slot
+int ortho_epilogue_warps();          // of a CTA
 cudaError_t launch_ortho_norm(const OrthoArgs &a, cudaStream_t stream);
 cudaError_t launch_ortho_prepare(const OrthoArgs &a, cudaStream_t stream);
 // All steps' products; ctas: 1 or 2 CTAs share a tile (of 128 or 256 rows and
