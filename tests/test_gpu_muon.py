@@ -127,6 +127,23 @@ def _check_some(before, after, parts):
                tuple([t[cut] for t in ts] for ts in after), [(0, r, c)])
 
 
+def test_bands_beside_other_shapes():
+    """Many matrices of two shapes, which go through L2 in bands, and a few others."""
+    parts, at = [], 0
+    for r, c in [(300, 520)] * 30 + [(520, 256)] * 30 + [(140, 150), (9, 700), (700, 131)]:
+        parts.append((at, r, c))
+        at += r * c
+    s = _state(parts, at, 8, BF16, BF16, seed=9)
+    before = _clone(s)
+    A.muon_step(*s, parts, A.muon_cfg(lr=2e-3))
+    some = [parts[i] for i in (0, 17, 29, 30, 44, 59, 60, 61, 62)]
+    for m in (0, 3, 7):
+        for p in some:
+            cut = slice(p[0], p[0] + p[1] * p[2])
+            _check(tuple([ts[m][cut]] for ts in before), tuple([ts[m][cut]] for ts in s),
+                   [(0, p[1], p[2])])
+
+
 def test_order_of_the_matrices_does_not_matter():
     s = _state(ODD, ODD_SIZE, 2, F32, F32)
     other = _clone(s)

@@ -36,7 +36,8 @@ def test_matrices_of_many_shapes(shape, dtype):
 
 
 @pytest.mark.parametrize("shape", [(40, 768, 768), (300, 64, 130), (5, 300, 200), (3, 1, 1),
-                                   (7, 200, 1024), (700, 8, 8)],
+                                   (7, 200, 1024), (700, 8, 8), (700, 200, 256), (260, 129, 500),
+                                   (2, 400, 6000)],
                          ids=lambda s: "x".join(map(str, s)))
 def test_batches(shape):
     """The first, some and the last matrix of a batch."""
