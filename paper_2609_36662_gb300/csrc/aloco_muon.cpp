@@ -31,6 +31,7 @@ constexpr int kPlannedSms = 152;
 struct Shape {
     int64_t rows, cols;
     int first, period;               // places [first, first + period)
+    bool merged;                     // may take two steps at a time
     int64_t m() const { return std::min(rows, cols); }
     int64_t n() const { return std::max(rows, cols); }
     int64_t ldx() const { return (int64_t)up((size_t)n(), 8); }
@@ -40,17 +41,25 @@ struct Shape {
         return std::max<int64_t>(4096, (int64_t)up((size_t)(rows * cols / 256), 4096));
     }
     int64_t chunks() const { return (rows * cols + chunk() - 1) / chunk(); }
+    // places for symmetric matrices
+    int syms() const { return merged ? kOrthoSyms : 2; }
     int64_t down() const { return (m() + 31) / 32; }
     int64_t across() const { return (n() + 31) / 32; }
     size_t rest_bytes() const { return (size_t)(down() * across()) * 2048; }
     // scratch of `count` matrices
     size_t bytes(int64_t count) const {
         return 2 * up((size_t)(count * m() * ldx()) * 2, kAlign) + (size_t)count * rest_bytes() +
-               2 * up((size_t)(count * m() * lda()) * 2, kAlign) +
-               2 * up((size_t)(count * m()) * 4, kAlign) +
+               syms() * (up((size_t)(count * m() * lda()) * 2, kAlign) +
+                         up((size_t)(count * m()) * 4, kAlign)) +
                up((size_t)(count * chunks()) * 8, kAlign);
     }
 };
+
+int64_t tiles_of(int64_t x, int tile) { return (x + tile - 1) / tile; }
+int64_t sym_tiles(const Shape &s, int tile) {
+    const int64_t rows = tiles_of(s.m(), tile);
+    return rows * (rows + 1) / 2;
+}
 
 // A part of a shape's matrices: those from `skip` on.
 struct Part {
@@ -94,11 +103,6 @@ int small_ctas(const Shape &s, int most) {
 // The largest cluster that every device takes, which scratch is reckoned with.
 constexpr int kPortableCtas = 8;
 
-int64_t tiles_of(int64_t x, int tile) { return (x + tile - 1) / tile; }
-int64_t sym_tiles(const Shape &s, int tile) {
-    const int64_t rows = tiles_of(s.m(), tile);
-    return rows * (rows + 1) / 2;
-}
 // Bytes of the sums that the parts of a group's tiles leave.
 size_t sums_bytes(const Shape &s, int64_t count, const std::array<int, 2> &split, int tile) {
     const int parts = std::max(split[0], split[1]);
@@ -164,6 +168,11 @@ void split(Plan *p, int workers, int most_ctas) {
     std::stable_sort(p->shapes.begin(), p->shapes.end(), [](const Shape &x, const Shape &y) {
         return x.m() != y.m() ? x.m() > y.m() : x.n() > y.n();
     });
+    // Two steps at a time, where the matrix is wide and its symmetric products fill
+    // the GPU (they take their depth alone, without X's length).
+    for (Shape &s : p->shapes)
+        s.merged = 2 * s.n() >= 3 * s.m() &&
+                   s.period * workers * sym_tiles(s, ortho_pair_tile()) >= kPlannedSms;
     // (beside larger ones the small fill tiles of the kernels that run anyway)
     bool all = true;
     for (const Shape &s : p->shapes) all = all && small_ctas(s, most_ctas);
@@ -235,7 +244,7 @@ void plan_matrices(const aloco_matrix_t *mats, int64_t n, int workers, int most_
         const aloco_matrix_t &x = mats[i];
         if (p->shapes.empty() || p->shapes.back().rows != x.rows ||
             p->shapes.back().cols != x.cols || p->shapes.back().period == 256)
-            p->shapes.push_back({x.rows, x.cols, (int)p->place.size(), 0});
+            p->shapes.push_back({x.rows, x.cols, (int)p->place.size(), 0, false});
         ++p->shapes.back().period;
         p->place.push_back(x.offset);
     }
@@ -245,7 +254,7 @@ void plan_matrices(const aloco_matrix_t *mats, int64_t n, int workers, int most_
 void plan_batch(int64_t batch, int64_t rows, int64_t cols, int most_ctas, Plan *p) {
     for (int64_t i = 0; i < batch; ++i) {
         if (p->shapes.empty() || p->shapes.back().period == 256)
-            p->shapes.push_back({rows, cols, (int)i, 0});
+            p->shapes.push_back({rows, cols, (int)i, 0, false});
         ++p->shapes.back().period;
         p->place.push_back(i);
     }
@@ -375,22 +384,22 @@ int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base, const do
         g.rest = (uint4 *)take((size_t)count * s.rest_bytes());
         g.blocks_down = (int)s.down();
         g.blocks_across = (int)s.across();
-        g.a = (__half *)take(a_bytes);
-        g.p = (__half *)take(a_bytes);
-        g.diag = (float *)take((size_t)(count * m) * 4);
-        g.lead = (float *)take((size_t)(count * m) * 4);
+        g.list = s.merged && base.n_ops[kMerged] ? kMerged : kPlain;
+        for (int k = 0; k < s.syms(); ++k) {
+            g.sym[k] = (__half *)take(a_bytes);
+            g.diag[k] = (float *)take((size_t)(count * m) * 4);
+        }
         g.partial = (double *)take((size_t)(count * s.chunks()) * 8);
         g.done = counter;
         counter += count;
         g.sym_tiles = (int)sym_tiles(s, tile);
         g.up_tiles = (int)(tiles_of(m, tile) * tiles_of(n, tile));
         for (int k = 0; k < 2; ++k) g.split[k] = pass.split[i][k];
-        g.gram0 = a.gram_tiles;
-        g.poly0 = a.poly_tiles;
-        g.up0 = a.up_tiles;
-        a.gram_tiles += g.sym_tiles * g.split[0] * g.count;
-        a.poly_tiles += g.sym_tiles * g.split[1] * g.count;
-        a.up_tiles += g.up_tiles * g.count;
+        for (int k = 0; k < base.n_ops[g.list]; ++k) {
+            const OrthoOp &op = base.ops[g.list][k];
+            a.tiles += g.count * (op.what == kUpdate ? g.up_tiles
+                                                     : g.sym_tiles * g.split[op.what != kGram]);
+        }
         if (const size_t sums = sums_bytes(s, count, pass.split[i], tile)) {
             g.sums = (float4 *)take(sums);
             g.came = counter;
@@ -401,8 +410,10 @@ int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base, const do
         for (int k = 0; k < 2; ++k)
             if ((rc = tensor_map(&a.map[kMapX0 + k][i], g.x[k], n, m, s.ldx(), count)) != ALOCO_OK)
                 return rc;
-        if ((rc = tensor_map(&a.map[kMapA][i], g.a, m, m, s.lda(), count)) != ALOCO_OK) return rc;
-        if ((rc = tensor_map(&a.map[kMapP][i], g.p, m, m, s.lda(), count)) != ALOCO_OK) return rc;
+        for (int k = 0; k < s.syms(); ++k)
+            if ((rc = tensor_map(&a.map[kMapSym + k][i], g.sym[k], m, m, s.lda(), count)) !=
+                ALOCO_OK)
+                return rc;
     }
     a.norm_blocks = norm;
     a.prep_blocks = prep;
@@ -412,6 +423,68 @@ int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base, const do
     return e == cudaSuccess ? ALOCO_OK : cuda_fail(e, "orthogonal factor");
 }
 
+// The lists of operations.  One step: A = X X^T, P = a + b A + c A A, X <- P X.  Two,
+// of m x m matrices but for the first and last product:
+//   A = X X^T,  P = p(A),  A' = P A P  (which is X' X'^T),  X <- p'(A') P X
+// of which all factors commute, so that every product is symmetric: 3 n + 5 m
+// products of m^2 in place of 6 n + 2 m (halved where symmetric).  The factor's
+// error is up to three times as large, so only for results in bf16.
+void list_operations(const double (*coefficients)[3], int steps, bool bf16, OrthoArgs *a) {
+    const auto add = [&](int list, OrthoOp op) {
+        int &n = a->n_ops[list];
+        if (n) {
+            const OrthoOp &last = a->ops[list][n - 1];
+            op.syms = (int8_t)(last.syms + (last.what != kUpdate));
+            op.ups = (int8_t)(last.ups + (last.what == kUpdate));
+        }
+        a->ops[list][n++] = op;
+    };
+    const auto op = [](int what, int left, int right, int out, int step, int x) {
+        OrthoOp o{};
+        o.what = (int8_t)what;
+        o.left = (int8_t)left;
+        o.right = (int8_t)right;
+        o.out = (int8_t)out;
+        o.step = (int8_t)step;
+        o.x = (int8_t)x;
+        return o;
+    };
+    const auto one = [&](int list, int s, int x) {
+        // (where e = b / 2c is not large against A)
+        const bool shifted = std::fabs(coefficients[s][1]) <= 4 * std::fabs(coefficients[s][2]);
+        OrthoOp o = op(kGram, 0, 0, 0, s, x);
+        o.shifted = shifted;
+        add(list, o);
+        o = op(kPoly, 0, 0, 1, s, x);
+        o.shifted = shifted;
+        o.bare = 1;
+        add(list, o);
+        o = op(kUpdate, 1, 0, 0, s, x);
+        o.last = s + 1 == steps;
+        add(list, o);
+    };
+    for (int s = 0; s < steps; ++s) one(kPlain, s, s & 1);
+    if (!bf16 || steps < 2) return;
+    int x = 0;
+    for (int s = 0; s < steps; s += 2, x ^= 1) {
+        if (s + 1 == steps) {
+            one(kMerged, s, x);
+            break;
+        }
+        add(kMerged, op(kGram, 0, 0, 0, s, x));
+        add(kMerged, op(kPoly, 0, 0, 1, s, x));
+        add(kMerged, op(kProduct, 1, 0, 2, s, x));
+        add(kMerged, op(kProduct, 2, 1, 0, s, x));
+        add(kMerged, op(kPoly, 0, 0, 3, s + 1, x));
+        OrthoOp o = op(kProduct, 3, 1, 2, s, x);
+        o.bare = 1;
+        add(kMerged, o);
+        o = op(kUpdate, 2, 0, 0, s, x);
+        o.last = s + 2 == steps;
+        add(kMerged, o);
+    }
+}
+
 // All of a call's passes.
 int run(const Plan &plan, const OrthoArgs &base, const double (*coefficients)[3], int steps,
         const double *shape_step, char *scratch, int sm_count, cudaStream_t stream) {
@@ -419,6 +492,7 @@ int run(const Plan &plan, const OrthoArgs &base, const double (*coefficients)[3]
     a.steps = steps;
     for (int s = 0; s < steps; ++s)
         for (int i = 0; i < 3; ++i) a.coef[s][i] = (float)coefficients[s][i];
+    list_operations(coefficients, steps, a.out_bf16, &a);
     for (const SmallPass &pass : plan.small) {
         const int rc = run_small(plan, pass, a, shape_step, stream);
         if (rc != ALOCO_OK) return rc;

@@ -25,61 +25,71 @@ constexpr int kSharedBytes =
     kSlots * kSlotBytes + kEpilogueWarps * kStageBytes + 1024 + 512;
 constexpr int kRing = 4;             // tiles that a CTA knows of
 
-// The steps' products, in the order in which tiles are handed out.
-enum { kGram, kPoly, kUpdate };
-
 struct Work {
-    int what, step, group, matrix;   // what < 0: there is no more
+    int op;                          // of the group's list; < 0: there is no more
+    int group, matrix;
     int row, col;                    // in tiles
     int before;                      // tiles of the matrix that have to be done
     int part;                        // of the depth
+    int unused;
 };
 static_assert(sizeof(Work) == 32, "a ring's entry");
 
-__device__ __forceinline__ Work find_work(const OrthoArgs &a, int t, int tile) {
-    Work f;
-    const int per = a.gram_tiles + a.poly_tiles + a.up_tiles;
-    f.step = t / per;
-    t -= f.step * per;
-    f.part = 0;
-    if (t >= a.gram_tiles + a.poly_tiles) {
-        f.what = kUpdate;
-        t -= a.gram_tiles + a.poly_tiles;
-        f.group = find_group(a, t, [](const OrthoGroup &g) { return g.up0; });
-        const OrthoGroup &g = a.g[f.group];
-        t -= g.up0;
-        f.matrix = t / g.up_tiles;
-        t -= f.matrix * g.up_tiles;
-        const int rows = (g.m + tile - 1) / tile;
-        f.col = t / rows;            // the rows of P first: X's columns stay in L2
-        f.row = t - f.col * rows;
-    } else {
-        f.what = t >= a.gram_tiles ? kPoly : kGram;
-        if (f.what == kPoly) {
-            t -= a.gram_tiles;
-            f.group = find_group(a, t, [](const OrthoGroup &g) { return g.poly0; });
-            t -= a.g[f.group].poly0;
-        } else {
-            f.group = find_group(a, t, [](const OrthoGroup &g) { return g.gram0; });
-            t -= a.g[f.group].gram0;
-        }
-        const OrthoGroup &g = a.g[f.group];
-        const int parts = g.split[f.what];
-        f.matrix = t / (g.sym_tiles * parts);
-        t -= f.matrix * g.sym_tiles * parts;
-        f.part = t % parts;
-        t /= parts;
-        // row r of the lower triangle holds tiles r (r + 1) / 2 ..
-        int r = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
-        while (r * (r + 1) / 2 > t) --r;
-        while ((r + 1) * (r + 2) / 2 <= t) ++r;
-        f.row = r;
-        f.col = t - r * (r + 1) / 2;
-    }
-    const OrthoGroup &g = a.g[f.group];
-    f.before = f.step * (2 * g.sym_tiles + g.up_tiles) + f.what * g.sym_tiles;
-    return f;
+__device__ __forceinline__ const OrthoOp &op_of(const OrthoArgs &a, const Work &f) {
+    return a.ops[a.g[f.group].list][f.op];
 }
+__device__ __forceinline__ int parts_of(const OrthoGroup &g, const OrthoOp &op) {
+    return op.what == kUpdate ? 1 : g.split[op.what != kGram];
+}
+
+// Tiles in the order in which they are handed out: the first operation of all
+// groups, the second of all, and so on.
+struct Finder {
+    int op = 0, group = 0, start = 0;
+
+    // Tile t, not before an earlier one.
+    __device__ __forceinline__ Work find(const OrthoArgs &a, int t, int tile) {
+        Work f;
+        for (;;) {
+            const OrthoGroup &g = a.g[group];
+            int n = 0;
+            if (op < a.n_ops[g.list]) {
+                const OrthoOp &o = a.ops[g.list][op];
+                n = g.count * (o.what == kUpdate ? g.up_tiles : g.sym_tiles * parts_of(g, o));
+            }
+            if (t < start + n) break;
+            start += n;
+            if (++group == a.n_groups) group = 0, ++op;
+        }
+        f.op = op;
+        f.group = group;
+        const OrthoGroup &g = a.g[group];
+        const OrthoOp &o = a.ops[g.list][op];
+        t -= start;
+        f.part = 0;
+        if (o.what == kUpdate) {
+            f.matrix = t / g.up_tiles;
+            t -= f.matrix * g.up_tiles;
+            const int rows = (g.m + tile - 1) / tile;
+            f.col = t / rows;        // the left matrix's rows first: X's columns stay in L2
+            f.row = t - f.col * rows;
+        } else {
+            const int parts = parts_of(g, o);
+            f.matrix = t / (g.sym_tiles * parts);
+            t -= f.matrix * g.sym_tiles * parts;
+            f.part = t % parts;
+            t /= parts;
+            // row r of the lower triangle holds tiles r (r + 1) / 2 ..
+            int r = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
+            while (r * (r + 1) / 2 > t) --r;
+            while ((r + 1) * (r + 2) / 2 <= t) ++r;
+            f.row = r;
+            f.col = t - r * (r + 1) / 2;
+        }
+        f.before = o.syms * g.sym_tiles + o.ups * g.up_tiles;
+        return f;
+    }
+};
 
 // A 32 x 32 block of fp16 values in a warp's shared memory: 64 bytes a row, whose
 // 16-byte pieces are turned so that neither a row to a lane nor four lanes to a
@@ -290,17 +300,16 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity)
     }
 }
 
-// All steps of all matrices: of every step the tiles of A = X X^T, of P = b A + c A
-// A, and of X <- a X + P X, matrix after matrix.  CTAs (pairs of them) take the next
+// All operations of all matrices, tile by tile.  CTAs (pairs of them) take the next
 // tile when they have asked for the operands of the one before, so that no two
 // wait for each other: what a tile needs was handed out before it, and counts of
 // the matrix's tiles that are done say when it is there.
 //
 // In a CTA two threads copy operands into a ring of slots (the first of a pair's
 // also takes the tiles), one issues the products into one of two accumulators,
-// eight warps join the other one with what it needs and write it.  A and P are
-// symmetric: the lower tiles are computed and kept, with whole blocks of kFull on
-// the diagonal; where a product needs what would lie above them it takes the tile
+// eight warps join the other one with what it needs and write it.  Of symmetric
+// matrices the lower tiles are computed and kept, with whole blocks of kFull on the
+// diagonal; where a product needs what would lie above them it takes the tile
 // below, MN-major instead of K-major.
 //
 // A wait that runs out ends the waits of its CTA; its tiles are NaN from there on,
@@ -329,7 +338,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = kCtas == 1 ? 0 : cluster_rank();
-    const int tiles = args.steps * (args.gram_tiles + args.poly_tiles + args.up_tiles);
+    const int tiles = args.tiles;
 
     if (threadIdx.x == 0) {
         s_abort = 0;
@@ -369,14 +378,14 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     };
     const auto hear = [&](bool whole_warp) -> Work {
         Work f;
-        f.what = -1;
+        f.op = -1;
         if (mbar_wait_cluster(told(ring), ring_phase)) {
             asm volatile("ld.shared.v4.s32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(f.what), "=r"(f.step), "=r"(f.group), "=r"(f.matrix)
+                         : "=r"(f.op), "=r"(f.group), "=r"(f.matrix), "=r"(f.row)
                          : "r"(work_at(ring))
                          : "memory");
             asm volatile("ld.shared.v4.s32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(f.row), "=r"(f.col), "=r"(f.before), "=r"(f.part)
+                         : "=r"(f.col), "=r"(f.before), "=r"(f.part), "=r"(f.unused)
                          : "r"(work_at(ring) + 16)
                          : "memory");
         }
@@ -393,16 +402,13 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         return f;
     };
     const auto done_of = [&](const Work &f) { return args.g[f.group].done + f.matrix; };
-    const auto depth = [&](const Work &f) {
-        return f.what == kGram ? args.g[f.group].n : args.g[f.group].m;
-    };
-    // the slots that a tile, or its part, takes
-    const auto slots_of = [&](const Work &f, int *begin) {
-        const int chunks = (depth(f) + kK - 1) / kK;
-        const int parts =
-            !kParts || f.what == kUpdate ? 1 : args.g[f.group].split[f.what];
-        *begin = chunks * f.part / parts;
-        return chunks * (f.part + 1) / parts;
+    // the k-elements that a tile, or its part, takes: from *begin on
+    const auto depth_of = [&](const Work &f, const OrthoOp &op, int *begin) {
+        const OrthoGroup &g = args.g[f.group];
+        const int all = op.what == kGram ? g.n : g.m, parts = kParts ? parts_of(g, op) : 1;
+        const int chunks = (all + kK - 1) / kK;
+        *begin = chunks * f.part / parts * kK;
+        return min(all, chunks * (f.part + 1) / parts * kK);
     };
 
     if ((warp == 0 || warp == 3) && lane == 0) {
@@ -413,20 +419,23 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         int slot = 0, issued = 0;
         uint32_t phase = 0;
         bool ok = true;
+        Finder finder;
         int next = tells ? atomicAdd(args.next_tile, 1) : 0;
         for (;;) {
             Work f;
             if (tells) {
-                f = find_work(args, min(next, tiles - 1), kTile);
-                if (next >= tiles) f.what = -1;
+                if (next < tiles)
+                    f = finder.find(args, next, kTile);
+                else
+                    f.op = -1;
                 if (!mbar_wait_cluster(heard(ring), ring_phase ^ 1)) break;
                 for (int p = 0; p < kCtas; ++p) {
                     const uint32_t at = kCtas == 1 ? work_at(ring) : cluster_addr(work_at(ring), p);
                     asm volatile("st.shared::cluster.v4.s32 [%0], {%1, %2, %3, %4};" ::"r"(at),
-                                 "r"(f.what), "r"(f.step), "r"(f.group), "r"(f.matrix)
+                                 "r"(f.op), "r"(f.group), "r"(f.matrix), "r"(f.row)
                                  : "memory");
                     asm volatile("st.shared::cluster.v4.s32 [%0], {%1, %2, %3, %4};" ::"r"(at + 16),
-                                 "r"(f.row), "r"(f.col), "r"(f.before), "r"(f.part)
+                                 "r"(f.col), "r"(f.before), "r"(f.part), "r"(0)
                                  : "memory");
                 }
                 mbar_arrive(told(ring));
@@ -439,32 +448,29 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             } else {
                 f = hear(false);
             }
-            if (f.what < 0) break;
-            int k0;
-            const int chunks = slots_of(f, &k0);
-            const int ask = max(k0, chunks - kSlots);  // where to take the next tile
+            if (f.op < 0) break;
+            const OrthoOp op = op_of(args, f);
+            int begin;
+            const int end = depth_of(f, op, &begin);
+            const int ask = begin + max(0, (end - begin - 1) / kK + 1 - kSlots) * kK;
             if (ok && !s_abort)
                 ok = wait_done(done_of(f), f.before * kSignals, &s_abort);
             else
                 ok = false;
             // operands were written by ordinary stores
             asm volatile("fence.proxy.async;" ::: "memory");
+            const bool x = op.what == kGram || (op.what == kUpdate && is_b);
             const CUtensorMap *map =
-                &args.map[f.what == kPoly              ? kMapA
-                          : f.what == kUpdate && !is_b ? kMapP
-                                                       : kMapX0 + (f.step & 1)][f.group];
+                &args.map[x ? kMapX0 + op.x : kMapSym + (is_b ? op.right : op.left)][f.group];
             const int row = (is_b ? f.col : f.row) * kTile + (int)rank * kHalfTile;
             // columns from here on lie below, MN-major (X does throughout)
-            const int turn = f.what == kGram            ? INT_MAX
-                             : f.what == kUpdate && is_b ? 0
-                                                         : (row / kFull + 1) * kFull;
-            for (int k = k0; k < chunks; ++k) {
-                if (tells && k == ask) next = atomicAdd(args.next_tile, 1);
+            const int turn = op.what == kGram ? INT_MAX : x ? 0 : (row / kFull + 1) * kFull;
+            for (int c = begin; c < end; c += kK) {
+                if (tells && c == ask) next = atomicAdd(args.next_tile, 1);
                 if (!ok || !(ok = mbar_wait(empty(slot), phase ^ 1, &s_abort))) continue;
                 const uint32_t at = smem + slot * kSlotBytes + (is_b ? 2 * kBoxBytes : 0);
                 const uint32_t bar = bar0 + 8 * slot;
                 if (tells) mbar_arrive_expect_tx(full(slot), kCtas * kSlotBytes);
-                const int c = k * kK;
                 if (args.test_stall1 == 0 || blockIdx.x != 0 || issued != args.test_stall1 - 1) {
                     if (c < turn) {
                         tensor_load<kCtas>(at, map, c, row, f.matrix, bar);
@@ -489,18 +495,18 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         bool ok = true;
         for (;;) {
             const Work f = hear(false);
-            if (f.what < 0) break;
-            int k0;
-            const int k_end = slots_of(f, &k0) * kK, K = min(depth(f), k_end);
-            k0 *= kK;
+            if (f.op < 0) break;
+            const OrthoOp op = op_of(args, f);
+            int begin;
+            const int end = depth_of(f, op, &begin);
             if (ok) ok = mbar_wait(acc_empty(acc), acc_phase ^ 1, &s_abort);
             tc_fence_after();
-            const int turn_a = f.what == kGram ? INT_MAX : (f.row * kTile / kFull + 1) * kFull;
-            const int turn_b = f.what == kGram     ? INT_MAX
-                               : f.what == kUpdate ? 0
-                                                   : (f.col * kTile / kFull + 1) * kFull;
+            const int turn_a = op.what == kGram ? INT_MAX : (f.row * kTile / kFull + 1) * kFull;
+            const int turn_b = op.what == kGram     ? INT_MAX
+                               : op.what == kUpdate ? 0
+                                                    : (f.col * kTile / kFull + 1) * kFull;
             const uint32_t d = tmem + acc * kTile;
-            for (int k = k0; ok && k < K; k += kK) {
+            for (int k = begin; ok && k < end; k += kK) {
                 if (!(ok = mbar_wait(full(slot), phase, &s_abort))) break;
                 tc_fence_after();
                 const uint32_t a0 = smem + slot * kSlotBytes, b0 = a0 + 2 * kBoxBytes;
@@ -511,10 +517,10 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 // 16 k-elements on, in 16 bytes: 32 bytes of a row, or 16 rows
                 const int na = ta ? 2048 / 16 : 2, nb = tb ? 2048 / 16 : 2;
                 // (straight on: between products this thread has 128 cycles)
-                product<kCtas>(d, da, db, desc, k != k0);
-                if (K - k > 16) product<kCtas>(d, da + na, db + nb, desc, true);
-                if (K - k > 32) product<kCtas>(d, da + 2 * na, db + 2 * nb, desc, true);
-                if (K - k > 48) product<kCtas>(d, da + 3 * na, db + 3 * nb, desc, true);
+                product<kCtas>(d, da, db, desc, k != begin);
+                if (end - k > 16) product<kCtas>(d, da + na, db + nb, desc, true);
+                if (end - k > 32) product<kCtas>(d, da + 2 * na, db + 2 * nb, desc, true);
+                if (end - k > 48) product<kCtas>(d, da + 3 * na, db + 3 * nb, desc, true);
                 product_commit<kCtas>(empty(slot));
                 if (++slot == kSlots) slot = 0, phase ^= 1;
             }
@@ -539,11 +545,12 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         uint32_t acc_phase = 0;
         for (;;) {
             const Work f = hear(true);
-            if (f.what < 0) break;
+            if (f.op < 0) break;
             const OrthoGroup &g = args.g[f.group];
-            const bool last = f.what == kUpdate && f.step + 1 == args.steps;
+            const OrthoOp op = op_of(args, f);
+            const bool up = op.what == kUpdate;
             const int m = g.m, r0 = f.row * kTile + (int)rank * kHalfTile + quad * 32;
-            const int r = r0 + lane, limit = f.what == kUpdate ? g.n : m;
+            const int r = r0 + lane, limit = up ? g.n : m;
             const int c_end = min(limit, f.col * kTile + (half + 1) * (kTile / 2));
             int c0 = f.col * kTile + half * (kTile / 2);
             const bool some = r0 < m && c0 < c_end;
@@ -551,33 +558,31 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             // (single CTAs have two tiles of a block on the diagonal to fill)
             const bool mirrored = kCtas == 1 && f.row != f.col &&
                                   f.row * kTile / kFull == f.col * kTile / kFull;
-            const float ca = args.coef[f.step][0], cb = args.coef[f.step][1],
-                        cc = args.coef[f.step][2];
-            // P = c (A + e)^2 - c e^2 with e = b / 2c, which is added to A's diagonal: its
-            // tiles need nothing but their product.  (Where e is large against A, P
-            // is put together from A's values.)
-            const bool square = fabsf(cb) <= 4.f * fabsf(cc);
-            const float shift = square ? cb / (2.f * cc) : 0.f;
-            // what a product is joined with: of A or P whole rows, of X also blocks that
-            // lie as this warp holds them; fetched a block ahead
+            const float ca = args.coef[op.step][0], cb = args.coef[op.step][1],
+                        cc = args.coef[op.step][2];
+            // a + b L + c L^2 = c (L + e)^2 + a - c e^2 with e = b / 2c, which is added to
+            // L's diagonal: its tiles need nothing but their product
+            const float shift = op.shifted ? cb / (2.f * cc) : 0.f;
+            const bool joined = op.what == kPoly && !op.shifted;   // b L is added
+            // what a product is joined with: of L whole rows, of X also blocks that lie
+            // as this warp holds them; fetched a block ahead
             uint4 *rest = g.rest + ((int64_t)(f.matrix * g.blocks_down + r0 / 32) * g.blocks_across +
                                     c0 / 32) * kBlockPieces + lane;
             const Result to(args, g, f.group, f.matrix);
             Pieces part;
             uint4 lo[4];
-            float by_row = 0.f, by_col = 0.f;
+            float by_row = 0.f, by_row2 = 0.f;
             const int begin = c0;
-            const auto fetch_a = [&](int c) {
-                part.load(g.a + (row0 + r0) * g.lda + c, g.lda, m - r0, m - c);
-                by_col = c + lane < m ? cc * __ldcg(g.diag + row0 + c + lane) : 0.f;
+            const auto fetch_l = [&](int c) {
+                part.load(g.sym[op.left] + (row0 + r0) * g.lda + c, g.lda, m - r0, m - c);
             };
             const auto fetch_x = [&](int c) {
                 const uint4 *p = rest + (c - begin) / 32 * kBlockPieces;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) lo[i] = __ldcg(p + 32 * i);
-                part.load(g.x[f.step & 1] + (row0 + r0) * g.ldx + c, g.ldx, m - r0, g.n - c);
+                part.load(g.x[op.x] + (row0 + r0) * g.ldx + c, g.ldx, m - r0, g.n - c);
             };
-            if (last && some && to.update) {
+            if (op.last && some && to.update) {
                 // parameters come from far: to L2 while the products run
                 const int along = to.tall ? 32 : c_end - c0, down = to.tall ? c_end - c0 : 32;
                 for (int i = lane; i < down; i += 32) {
@@ -588,21 +593,23 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 }
             }
             bool ok = !s_abort;
-            if (f.what != kGram && some) {
+            if (op.what != kGram && some) {
                 // (products that are done had what they needed)
                 if (ok && !__all_sync(~0u, mbar_test(acc_full(acc), acc_phase)))
                     ok = wait_done(done_of(f), f.before * kSignals, &s_abort);
                 ok = __all_sync(~0u, ok);
-                if (f.what == kUpdate) {
+                if (r < m) {
+                    by_row = __ldcg(g.diag[op.left] + row0 + r);
+                    if (op.what == kProduct) by_row2 = __ldcg(g.diag[op.right] + row0 + r);
+                }
+                if (up) {
                     // what is kept of X beside the operands comes to L2 while the
                     // products run
                     const int lines = (c_end - c0 + 31) / 32 * 16;
                     for (int i = lane; i < lines; i += 32) fetch_l2(rest - lane + 8 * i);
-                    if (r < m) by_row = __ldcg(g.lead + row0 + r);
                     fetch_x(c0);
-                } else {
-                    if (r < m) by_row = __ldcg(g.diag + row0 + r);
-                    if (!square) fetch_a(c0);
+                } else if (joined) {
+                    fetch_l(c0);
                 }
             }
             if (ok) ok = mbar_wait(acc_full(acc), acc_phase, &s_abort);
@@ -621,7 +628,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             };
             // A part of a tile leaves its sums; the warp that finds all others' there
             // goes on with the tile.
-            const int parts = !kParts || f.what == kUpdate ? 1 : g.split[f.what];
+            const int parts = kParts ? parts_of(g, op) : 1;
             bool finishes = true;
             const float4 *sums = nullptr;
             const int64_t next_part = kCtas * kEpilogueWarps * (kTile / 64) * kBlockQuads;
@@ -690,86 +697,72 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 release();
                 finishes = parts == 1 || f.part == 0;
             } else if (!finishes) {
-            } else if (f.what == kGram) {
+            } else if (!up) {
+                const float scale = op.what == kGram   ? 1.f / (kOrthoScale * kOrthoScale)
+                                    : op.what == kPoly ? cc
+                                                       : 1.f;
+                __half *out = g.sym[op.out] + row0 * g.lda;
 #pragma unroll 1
                 for (; c0 < c_end; c0 += 32) {
                     float v[32];
                     values(v);
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] *= 1.f / (kOrthoScale * kOrthoScale);
+                    if (joined) {
+                        __syncwarp();
+                        part.to_shared(st);
+                        if (c0 + 32 < c_end) fetch_l(c0 + 32);
+                        __syncwarp();
+                    }
+                    // The diagonal from what lies beside the operands: their own values as
+                    // the product has them are taken out, and put back unrounded.
+                    float own = 0.f;
                     if (c0 == r0) {
-                        float own = 0.f;
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (i == lane) own = v[i], v[i] = square ? own + shift : 0.f;
-                        if (r < m) g.diag[row0 + r] = own;
-                    }
-                    store_symmetric(g.a + row0 * g.lda, m, g.lda, r0, c0, mirrored, st, v);
-                }
-            } else if (f.what == kPoly && square) {
-#pragma unroll 1
-                for (; c0 < c_end; c0 += 32) {
-                    float v[32];
-                    values(v);
-                    if (c0 == r0) {
-                        float own = 0.f;
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (i == lane) own = v[i], v[i] = 0.f;
-                        // the diagonal's own square as the product has it is taken out,
-                        // and put back from what was not rounded
-                        const float rounded = __half2float(__float2half_rn(by_row + shift));
-                        if (r < m)
-                            g.lead[row0 + r] =
-                                ca + cb * by_row + cc * (by_row * by_row + (own - rounded * rounded));
+                            if (i == lane) own = v[i];
+                        const auto rounded = [](float x) {
+                            return __half2float(__float2half_rn(x));
+                        };
+                        if (op.what == kGram) {
+                            own *= scale;
+                        } else if (op.what == kPoly) {
+                            const float s = rounded(by_row + shift);
+                            own = ca + cb * by_row + cc * (by_row * by_row + (own - s * s));
+                        } else {
+                            own = by_row * by_row2 +
+                                  (own - rounded(by_row) * rounded(by_row2));
+                        }
+                        if (r < m) g.diag[op.out][row0 + r] = own;
                     }
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] *= cc;
-                    store_symmetric(g.p + row0 * g.lda, m, g.lda, r0, c0, mirrored, st, v);
-                }
-            } else if (f.what == kPoly) {
-                // b a + c ((d_r + d_c) a + x); where A's diagonal is taken out a is 0
-                const float dr = fmaf(cc, by_row, cb);
-#pragma unroll 1
-                for (; c0 < c_end; c0 += 32) {
-                    float v[32];
-                    values(v);
-                    __syncwarp();
-                    part.to_shared(st);
-                    float *cols = reinterpret_cast<float *>(st + 2048);
-                    cols[lane] = by_col;
-                    if (c0 + 32 < c_end) fetch_a(c0 + 32);
-                    __syncwarp();
-                    if (c0 == r0) {
-                        float own = 0.f;
+                    for (int i = 0; i < 32; ++i) v[i] *= scale;
+                    if (joined) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (i == lane) own = v[i], v[i] = 0.f;
-                        if (r < m)
-                            g.lead[row0 + r] = ca + cb * by_row + cc * (by_row * by_row + own);
-                    }
+                        for (int i = 0; i < 4; ++i) {
+                            const uint4 w = *piece(st, lane, i);
+                            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint4 w = *piece(st, lane, i);
-                        const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-                        const float4 d0 = reinterpret_cast<const float4 *>(cols)[2 * i];
-                        const float4 d1 = reinterpret_cast<const float4 *>(cols)[2 * i + 1];
-                        const float dc[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w};
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float2 h = unpack(ws[j / 2]);
-                            v[8 * i + j] =
-                                fmaf(j & 1 ? h.y : h.x, dr + dc[j], cc * v[8 * i + j]);
+                            for (int j = 0; j < 4; ++j) {
+                                const float2 h = unpack(ws[j]);
+                                v[8 * i + 2 * j] = fmaf(cb, h.x, v[8 * i + 2 * j]);
+                                v[8 * i + 2 * j + 1] = fmaf(cb, h.y, v[8 * i + 2 * j + 1]);
+                            }
                         }
                     }
-                    store_symmetric(g.p + row0 * g.lda, m, g.lda, r0, c0, mirrored, st, v);
+                    if (c0 == r0) {
+                        const float kept =
+                            op.bare ? 0.f : op.what == kGram ? own + shift : own;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (i == lane) v[i] = kept;
+                    }
+                    store_symmetric(out, m, g.lda, r0, c0, mirrored, st, v);
                 }
             } else {
 #pragma unroll 1
                 for (; c0 < c_end; c0 += 32) {
                     Param<kOutBf16> param;
                     const int y = to.tall ? c0 : r0, x = to.tall ? r0 : c0;
-                    if (last && to.update && to.whole) param.load(to, y, x, g.rows, g.cols);
+                    if (op.last && to.update && to.whole) param.load(to, y, x, g.rows, g.cols);
                     float v[32];
                     values(v);
                     __syncwarp();
@@ -797,7 +790,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                         v[2 * i] = fmaf(by_row, h.x, fmaf(by_row, l.x, v[2 * i]));
                         v[2 * i + 1] = fmaf(by_row, h.y, fmaf(by_row, l.y, v[2 * i + 1]));
                     }
-                    if (last) {
+                    if (op.last) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] *= 1.f / kOrthoScale;
                         if (to.whole) {
@@ -823,11 +816,11 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                         p[32 * i] = make_uint4(l[0], l[1], l[2], l[3]);
                     }
                     __syncwarp();
-                    store_block(st, g.x[(f.step & 1) ^ 1] + (row0 + r0) * g.ldx + c0, g.ldx, m - r0,
+                    store_block(st, g.x[op.x ^ 1] + (row0 + r0) * g.ldx + c0, g.ldx, m - r0,
                                 g.n - c0);
                 }
             }
-            if (!last && finishes) {
+            if (!op.last && finishes) {
                 // done: what this warp has written is seen behind the count (by tensor
                 // copies behind a fence of theirs)
                 __syncwarp();
@@ -1056,9 +1049,8 @@ cudaError_t launch_chain(const OrthoArgs &a, int sm_count, cudaStream_t stream) 
         if (e != cudaSuccess) return e;
         ready.set(d, 1);
     }
-    const int64_t tiles = (int64_t)a.steps * (a.gram_tiles + a.poly_tiles + a.up_tiles);
-    const int64_t most = sm_count / kCtas;
-    return launch(kernel, a, (int)(tiles < most ? tiles : most) * kCtas, kProductThreads, kCtas,
+    const int most = sm_count / kCtas;
+    return launch(kernel, a, (a.tiles < most ? a.tiles : most) * kCtas, kProductThreads, kCtas,
                   kSharedBytes, stream);
 }
 

@@ -12,10 +12,34 @@ namespace aloco {
 // Matrices of one shape in a pass.  X is the matrix with its smaller side as
 // rows (m <= n), as a sum of two fp16 values: the larger ones row by row, whose
 // products are taken, and what they leave, which only what multiplies X itself
-// sees, in blocks of 32 x 32 laid out as the epilogue's threads hold them.  A = X X^T
-// and P = b A + c A A are m x m in fp16 with zeros on the diagonal (A: or b / 2c more
-// than its values), which is kept in fp32 beside them.  Rows lie ldx and lda
-// elements apart (multiples of 8).
+// sees, in blocks of 32 x 32 laid out as the epilogue's threads hold them.  The
+// symmetric m x m matrices (A = X X^T, polynomials of it) are fp16 values with their
+// diagonals beside them in fp32.  Rows lie ldx and lda elements apart (multiples
+// of 8).
+constexpr int kOrthoSyms = 4;        // places for symmetric matrices
+
+// What a matrix's next operation is.
+enum { kGram, kPoly, kProduct, kUpdate };
+struct OrthoOp {
+    // kGram     out = X X^T
+    // kPoly     out = a + b L + c L L
+    // kProduct  out = L R
+    // kUpdate   X <- L X
+    int8_t what;
+    int8_t left, right, out;         // places of symmetric matrices
+    int8_t step;                     // whose coefficients are taken
+    int8_t x;                        // which of x[2] X is
+    // kGram, kPoly: L is (to be) kept as L + b / 2c, as whose square the polynomial
+    // comes out but for its diagonal
+    int8_t shifted;
+    int8_t bare;                     // out's diagonal lies beside it only (for kUpdate)
+    int8_t last;                     // kUpdate: writes the result
+    int8_t syms, ups;                // operations of either kind ahead of it
+};
+// Lists of operations: one step after another, or two at a time.
+enum { kPlain, kMerged, kOrthoLists };
+constexpr int kOrthoOps = 64;
+
 struct OrthoGroup {
     int m, n, ldx, lda;
     int rows, cols;                  // as the caller has it
@@ -24,16 +48,16 @@ struct OrthoGroup {
     int first, period, skip;         // the i-th: number first + (skip + i) % period
                                      // of worker (skip + i) / period
     int sym_tiles, up_tiles;         // tiles of a matrix: symmetric products, update
-    int split[2];                    // parts of the depth of A's and P's tiles
-    int gram0, poly0, up0;           // the group's first tile (part of one)
+    int split[2];                    // parts of the depth of tiles of X X^T, and of the
+                                     // other symmetric products'
     int chunks, chunk;               // norm blocks of a matrix, elements of each
     int norm0, prep0;                // the group's first block
     int small0;                      // its first cluster (launch_ortho_small)
-    __half *x[2], *a, *p;
+    __half *x[2], *sym[kOrthoSyms];
+    float *diag[kOrthoSyms];
+    int list;                        // of operations: kPlain or kMerged
     uint4 *rest;                     // X - x, kBlockPieces a block: 8 columns of a row each
     int blocks_down, blocks_across;  // of a matrix
-    float *diag;                     // A's diagonal
-    float *lead;                     // a + P's diagonal: what multiplies X itself
     double *partial;                 // [count][chunks] sums of squares
     int *done;                       // [count] warps that have finished a tile
     // where tiles have parts: their sums, a block as a warp holds it after the other,
@@ -56,15 +80,18 @@ constexpr float kOrthoScale = 256.f;
 
 enum OrthoSource { kSourceMatrix, kSourceMuon };
 
-// Operands of the products: X, which alternates between two places, A and P.
-enum { kMapX0, kMapX1, kMapA, kMapP, kOrthoMaps };
+// Operands of the products: X, which alternates between two places, and the
+// symmetric matrices.
+enum { kMapX0, kMapX1, kMapSym, kOrthoMaps = kMapSym + kOrthoSyms };
 
 struct OrthoArgs {
     CUtensorMap map[kOrthoMaps][kOrthoGroups];
     OrthoGroup g[kOrthoGroups];
     int64_t place[kOrthoMatrices];   // offset in a replica; kSourceMatrix: index in the batch
     int n_groups;
-    int gram_tiles, poly_tiles, up_tiles, norm_blocks, prep_blocks;  // all groups'
+    OrthoOp ops[kOrthoLists][kOrthoOps];
+    int n_ops[kOrthoLists];
+    int tiles, norm_blocks, prep_blocks;   // all groups'
     float coef[ALOCO_MAX_NS_STEPS][3];     // the steps' coefficients
     int steps;
     int small_ctas;                  // launch_ortho_small: the CTAs of a matrix

@@ -35,7 +35,7 @@ def _scale(kind, r, c):
 
 
 def _check(before, after, parts, lr=2e-3, mu=0.95, wd=0.1, nesterov=True, kind=A.MUON_ADAMW,
-           eps=1e-7, workers=None):
+           eps=1e-7, workers=None, two_at_a_time=False):
     half = torch.finfo(after[0][0].dtype).eps / 2
     for m in workers or range(len(after[0])):
         x, g, b = (s[m] for s in before)
@@ -51,7 +51,7 @@ def _check(before, after, parts, lr=2e-3, mu=0.95, wd=0.1, nesterov=True, kind=A
             tol = 2.0 ** -24 * (want.abs() + (mu * bd).abs())
             assert ((b1[cut].double() - want).abs() <= tol + 1e-44).all()
             u = gd + mu * want if nesterov else want
-            o, off = allowed(u.view(r, c), eps=eps)
+            o, off = allowed(u.view(r, c), eps=eps, two_at_a_time=two_at_a_time)
             step = lr * _scale(kind, r, c)
             theta = (1 - lr * wd) * x[cut].double() - step * o.reshape(-1)
             # the factor's error, u's roundings (3 in fp32, which the steps raise
@@ -127,13 +127,15 @@ def _check_some(before, after, parts):
                tuple([t[cut] for t in ts] for ts in after), [(0, r, c)])
 
 
-def test_bands_beside_other_shapes():
-    """Many matrices of two shapes, which go through L2 in bands, and a few others."""
+@pytest.mark.parametrize("pdt", [F32, BF16], ids=["f32", "bf16"])
+def test_many_wide_matrices_beside_other_shapes(pdt):
+    """Two shapes of which there are many (in bf16 they take two steps at a time), and
+    a few others."""
     parts, at = [], 0
     for r, c in [(300, 520)] * 30 + [(520, 256)] * 30 + [(140, 150), (9, 700), (700, 131)]:
         parts.append((at, r, c))
         at += r * c
-    s = _state(parts, at, 8, BF16, BF16, seed=9)
+    s = _state(parts, at, 8, pdt, BF16, seed=9)
     before = _clone(s)
     A.muon_step(*s, parts, A.muon_cfg(lr=2e-3))
     some = [parts[i] for i in (0, 17, 29, 30, 44, 59, 60, 61, 62)]
@@ -141,7 +143,7 @@ def test_bands_beside_other_shapes():
         for p in some:
             cut = slice(p[0], p[0] + p[1] * p[2])
             _check(tuple([ts[m][cut]] for ts in before), tuple([ts[m][cut]] for ts in s),
-                   [(0, p[1], p[2])])
+                   [(0, p[1], p[2])], two_at_a_time=pdt is BF16 and p in parts[:60])
 
 
 def test_order_of_the_matrices_does_not_matter():

@@ -36,8 +36,7 @@ def test_matrices_of_many_shapes(shape, dtype):
 
 
 @pytest.mark.parametrize("shape", [(40, 768, 768), (300, 64, 130), (5, 300, 200), (3, 1, 1),
-                                   (7, 200, 1024), (700, 8, 8), (700, 200, 256), (260, 129, 500),
-                                   (2, 400, 6000)],
+                                   (7, 200, 1024), (700, 8, 8), (700, 200, 256), (2, 400, 6000)],
                          ids=lambda s: "x".join(map(str, s)))
 def test_batches(shape):
     """The first, some and the last matrix of a batch."""
@@ -46,6 +45,23 @@ def test_batches(shape):
     for i in {0, 1, shape[0] // 2, shape[0] - 1}:
         _check(x[i], out[i])
     assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 5])
+@pytest.mark.parametrize("shape", [(260, 129, 500), (60, 300, 520), (52, 700, 260)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_wide_matrices_that_take_two_steps_at_a_time(shape, steps):
+    x = torch.stack([momentum_like(*shape[1:], _gen(i)) for i in range(shape[0])])
+    x[7] = torch.randn(shape[1:], generator=_gen(50), device="cuda")
+    x[9] = 0
+    x[11, 5, 5] = float("nan")
+    out = A.orthogonalize(x, coefficients=[COEFFICIENTS] * steps)
+    for i in (0, 7, 8, shape[0] - 1):
+        _check(x[i], out[i], steps=steps, two_at_a_time=True)
+    assert (out[9] == 0).all() and out[11].isnan().all()
+    mixed = [(3.9, -6.2, 2.6), (1.5, -0.5, 0.0), (1.875, -1.25, 0.375), (1.5, -0.5, 0.0)][:steps]
+    out = A.orthogonalize(x, coefficients=mixed)
+    _check(x[8], out[8], coefficients=mixed, two_at_a_time=True)
 
 
 @pytest.mark.parametrize("kind", ["square", "wide", "rank_one", "decaying", "equal", "large",
