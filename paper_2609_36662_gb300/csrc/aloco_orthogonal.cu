@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 f = hear(false);
             }
             if (f.op < 0) break;
-            const OrthoOp op = op_of(args, f);
+            const OrthoOp &op = op_of(args, f);
             int begin;
             const int end = depth_of(f, op, &begin);
             const int ask = begin + max(0, (end - begin - 1) / kK + 1 - kSlots) * kK;
@@ -496,7 +496,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         for (;;) {
             const Work f = hear(false);
             if (f.op < 0) break;
-            const OrthoOp op = op_of(args, f);
+            const OrthoOp &op = op_of(args, f);
             int begin;
             const int end = depth_of(f, op, &begin);
             if (ok) ok = mbar_wait(acc_empty(acc), acc_phase ^ 1, &s_abort);
@@ -547,7 +547,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             const Work f = hear(true);
             if (f.op < 0) break;
             const OrthoGroup &g = args.g[f.group];
-            const OrthoOp op = op_of(args, f);
+            const OrthoOp &op = op_of(args, f);
             const bool up = op.what == kUpdate;
             const int m = g.m, r0 = f.row * kTile + (int)rank * kHalfTile + quad * 32;
             const int r = r0 + lane, limit = up ? g.n : m;
@@ -670,6 +670,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                     const float4 *p = sums + (c0 - begin) / 32 * kBlockQuads;
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = 0.f;
+#pragma unroll 1
                     for (int k = 0; k < parts; ++k, p += next_part) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
