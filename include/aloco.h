@@ -522,8 +522,13 @@ int aloco_adamw_step_normed(void *const *params, const void *const *grads,
  * with X transposed where U has more rows than columns.  The products run on
  * the tensor cores: X is held as a sum of two fp16 values (22 bits), A and b A + c
  * A A in fp16 with their diagonals in fp32, sums in fp32.  The factor's error
- * against exact steps is 2e-4 to 1.5e-3 of its norm.  A matrix that holds NaN or
- * inf gives NaN throughout, and no other matrix is affected; zeros give zeros.
+ * against exact steps is 2e-4 to 1e-3 of its norm, 2e-3 for a matrix of rank one.
+ * Where the result is bf16 and many matrices are one and a half times as wide as
+ * high (or the other way), two steps are taken at a time, in products of the
+ * symmetric matrices alone: 5e-4 to 2.5e-3, 3e-3 for rank one, beside a rounding of
+ * 1.7e-3.  A matrix that holds NaN or inf gives NaN throughout, and no other matrix
+ * is affected; zeros give zeros.  Polynomials that let singular values grow beyond
+ * 200 leave fp16's range (inf or NaN).
  *
  * The calls only enqueue on opts->stream (the other options do not apply) and
  * allocate nothing on the device; results are bit-identical from call to call.
@@ -554,7 +559,7 @@ typedef struct aloco_muon_cfg {
     double lr;              /* finite, >= 0                                  */
     double momentum;        /* mu, in [0, 1)                                 */
     double weight_decay;    /* decoupled, finite, >= 0                       */
-    double eps;             /* beside the norm, finite, > 0                  */
+    double eps;             /* beside the norm, finite, >= 1e-30             */
     int32_t nesterov;       /* 1: U = g + mu b', 0: U = b'                   */
     int32_t scale;          /* ALOCO_MUON_*                                  */
     int32_t steps;          /* of the factor, in [1, ALOCO_MAX_NS_STEPS]     */
@@ -588,10 +593,9 @@ int aloco_muon_step(void *const *params, const void *const *grads,
                     size_t scratch_bytes, const aloco_opts_t *opts);
 
 /* Orthogonal factors of `batch` matrices of rows x cols elements (dtype fp32 or
- * bf16; rows lie row_stride >= cols elements apart, matrices batch_stride >=
- * rows * row_stride, or any whole number of elements for a batch of 1), in bf16
- * and contiguous in `out`, which may not overlap x.  coefficients: [steps][3]
- * host values. */
+ * bf16), in bf16 and contiguous in `out`, which may not overlap x.  Rows lie
+ * row_stride and matrices batch_stride elements apart, any numbers >= 0 (x is only
+ * read).  coefficients: [steps][3] host values. */
 size_t aloco_orthogonalize_scratch_bytes(int64_t batch, int64_t rows, int64_t cols);
 int aloco_orthogonalize(const void *x, int64_t batch, int64_t rows, int64_t cols,
                         int64_t batch_stride, int64_t row_stride, aloco_dtype dtype,

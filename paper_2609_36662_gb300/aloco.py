@@ -902,8 +902,8 @@ def _steps(coefficients):
 def orthogonalize(x, *, coefficients=(NEWTON_SCHULZ,) * 5, eps: float = 1e-7, out=None,
                   stream=None):
     """Orthogonal factors of matrices [rows, columns] or [batch, rows, columns]
-    (float32 or bfloat16 CUDA tensor with contiguous rows, any strides between
-    them) by Newton-Schulz steps, one for every (a, b, c) of `coefficients`
+    (float32 or bfloat16 CUDA tensor with contiguous rows, any strides of the other
+    dimensions) by Newton-Schulz steps, one for every (a, b, c) of `coefficients`
     (aloco_orthogonalize).  Returns bfloat16 of x's shape, or fills `out`, a
     contiguous one.  Enqueues only."""
     torch = _torch_module()

@@ -688,15 +688,15 @@ int orthogonalize(const void *x, int64_t batch, int64_t rows, int64_t cols, int6
         std::memcpy(steps_of, coefficients, sizeof(double) * 3 * (size_t)steps);
     if ((rc = check_steps(steps_of, steps, eps)) != ALOCO_OK) return rc;
     if (batch == 0 || rows == 0 || cols == 0) return done();
-    if (rows == 1) row_stride = cols;
-    if (row_stride < cols || row_stride > (int64_t)1 << 40)
-        return fail(ALOCO_ERR_ARG, "row_stride = %lld: rows of %lld overlap", (long long)row_stride,
-                    (long long)cols);
+    if (rows == 1) row_stride = 0;
     if (batch == 1) batch_stride = 0;
+    // (x is only read: rows and matrices may overlap)
+    const int64_t limit = std::numeric_limits<int64_t>::max() / 64;
+    if (row_stride < 0 || row_stride > limit / rows || batch_stride < 0 ||
+        batch_stride > limit / batch)
+        return fail(ALOCO_ERR_ARG, "strides (%lld, %lld) out of range", (long long)batch_stride,
+                    (long long)row_stride);
     const int64_t extent = (rows - 1) * row_stride + cols;
-    if (batch > 1 && (batch_stride < extent || batch_stride > (int64_t)1 << 40))
-        return fail(ALOCO_ERR_ARG, "batch_stride = %lld: matrices overlap",
-                    (long long)batch_stride);
     Plan plan;
     const auto make = [&](int ctas, Plan *p) { plan_batch(batch, rows, cols, ctas, p); };
     make(kPortableCtas, &plan);

@@ -89,7 +89,8 @@ def test_kinds_of_spectra(kind):
 def test_views():
     """Padded rows, every other matrix of a batch, starts off any boundary."""
     base = momentum_like(6 * 150, 260, _gen(4)).view(6, 150, 260)
-    for x in (base[:, :133, 1:202], base[::2, 5:, 3:], base[1, :, 7:100], base[:, 40:41, :]):
+    for x in (base[:, :133, 1:202], base[::2, 5:, 3:], base[1, :, 7:100], base[:, 40:41, :],
+              base.transpose(0, 1)[:7, :, 8:], base[2].expand(3, -1, -1)):
         out = A.orthogonalize(x)
         assert out.shape == x.shape and out.is_contiguous()
         for i in ([0, x.shape[0] - 1] if x.dim() == 3 else [None]):

@@ -164,8 +164,8 @@ def _ortho(lib, **kw):
                                    p["bytes"], None)
 
 
-@pytest.mark.parametrize("kw", [dict(dtype=2), dict(batch=-1), dict(rows=-1), dict(rs=139),
-                                dict(bs=18199), dict(steps=0), dict(steps=17), dict(eps=0.0),
+@pytest.mark.parametrize("kw", [dict(dtype=2), dict(batch=-1), dict(rows=-1), dict(rs=-1),
+                                dict(bs=-140), dict(bs=1 << 62), dict(steps=0), dict(steps=17), dict(eps=0.0),
                                 dict(coefficients=False), dict(scratch=None), dict(bytes=1),
                                 dict(x=None), dict(out=None), dict(out=_at(2) + 1),
                                 dict(rows=A.MAX_SIDE + 1, cols=A.MAX_SIDE + 1, rs=1 << 20)],
