@@ -569,7 +569,7 @@ typedef struct aloco_muon_cfg {
 } aloco_muon_cfg_t;
 
 /* lr 4e-4, momentum 0.95 with nesterov, weight decay 0.1, eps 1e-7, the ADAMW
- * scale, five steps of (3.4445, -4.7750, 2.0315). */
+ * scale, five steps; (3.4445, -4.7750, 2.0315) for these and all further ones. */
 void aloco_muon_default_cfg(aloco_muon_cfg_t *cfg);
 
 /* Bytes of scratch of a step over these matrices on M replicas (0 where an

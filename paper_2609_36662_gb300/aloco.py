@@ -9,6 +9,7 @@ from __future__ import annotations
 import array
 import ctypes
 import functools
+import operator
 import os
 import struct
 from dataclasses import dataclass
@@ -836,7 +837,7 @@ class Matrices:
     for muon_step step after step."""
 
     def __init__(self, parts):
-        self.parts = [tuple(int(x) for x in p) for p in parts]
+        self.parts = [tuple(operator.index(x) for x in p) for p in parts]
         self.array = (Matrix * len(self.parts))(*self.parts)
         self._need = {}
 
@@ -893,7 +894,7 @@ def muon_step(params, grads, momentum, matrices, cfg: MuonCfg, stream=None):
 
 @functools.lru_cache(maxsize=32)
 def _steps(coefficients):
-    """The C array of a tuple of (a, b, c)."""
+    """The C array of a tuple of tuples (a, b, c)."""
     if any(len(s) != 3 for s in coefficients):
         raise ValueError("coefficients must be triples")
     return (ctypes.c_double * (3 * len(coefficients)))(*[float(v) for s in coefficients for v in s])
@@ -913,8 +914,7 @@ def orthogonalize(x, *, coefficients=(NEWTON_SCHULZ,) * 5, eps: float = 1e-7, ou
         raise ValueError("need [rows, columns] or [batch, rows, columns]")
     if not x.is_cuda or (x.stride(-1) != 1 and x.shape[-1] > 1):
         raise ValueError("need a CUDA tensor with contiguous rows")
-    steps = _steps(coefficients if coefficients.__class__ is tuple else
-                   tuple(tuple(s) for s in coefficients))
+    steps = _steps(tuple(map(tuple, coefficients)))
     if out is not None and (out.dtype is not torch.bfloat16 or out.shape != x.shape or
                             out.device != x.device or not out.is_contiguous()):
         raise ValueError("out must be a contiguous bfloat16 tensor of x's shape and device")
@@ -930,7 +930,7 @@ def orthogonalize(x, *, coefficients=(NEWTON_SCHULZ,) * 5, eps: float = 1e-7, ou
         rc = lib.aloco_orthogonalize(
             x.data_ptr(), batch, rows, cols, x.stride(0) if x.dim() == 3 else 0, x.stride(-2),
             F32 if x.dtype is torch.float32 else BF16, result.data_ptr(),
-            steps, len(coefficients), eps, scratch.data_ptr() if need else None, need,
+            steps, len(steps) // 3, eps, scratch.data_ptr() if need else None, need,
             ctypes.byref(Opts(stream=handle)))
     _finish(rc, ctx, result)
     if out is not None:

@@ -154,7 +154,7 @@ void lay_out(const Plan &plan, Pass *pass) {
         const size_t sums = sums_bytes(s, part.count, pass->split[i], tile);
         if (!sums) continue;
         pass->counters += (size_t)(part.count * sym_tiles(s, tile)) * pass->ctas *
-                          ortho_epilogue_warps();
+                          ortho_epilogue_warps() * 2;
         pass->all_bytes += up(sums, kAlign);
     }
     pass->all_bytes += up(pass->counters * 4, kAlign);
@@ -403,7 +403,7 @@ int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base, const do
         if (const size_t sums = sums_bytes(s, count, pass.split[i], tile)) {
             g.sums = (float4 *)take(sums);
             g.came = counter;
-            counter += count * g.sym_tiles * pass.ctas * ortho_epilogue_warps();
+            counter += count * g.sym_tiles * pass.ctas * ortho_epilogue_warps() * 2;
         }
         a.step[i] = shape_step ? (float)shape_step[part.shape] : 0.f;
         int rc;
@@ -451,7 +451,8 @@ void list_operations(const double (*coefficients)[3], int steps, bool bf16, Orth
     };
     const auto one = [&](int list, int s, int x) {
         // (where e = b / 2c is not large against A)
-        const bool shifted = std::fabs(coefficients[s][1]) <= 4 * std::fabs(coefficients[s][2]);
+        const float b = (float)coefficients[s][1], c = (float)coefficients[s][2];
+        const bool shifted = c != 0.f && std::fabs(b) <= 4 * std::fabs(c);
         OrthoOp o = op(kGram, 0, 0, 0, s, x);
         o.shifted = shifted;
         add(list, o);
@@ -741,7 +742,7 @@ void aloco_muon_default_cfg(aloco_muon_cfg_t *cfg) {
     cfg->nesterov = 1;
     cfg->scale = ALOCO_MUON_ADAMW;
     cfg->steps = 5;
-    for (int s = 0; s < 5; ++s) {
+    for (int s = 0; s < ALOCO_MAX_NS_STEPS; ++s) {
         cfg->coefficients[s][0] = 3.4445;
         cfg->coefficients[s][1] = -4.7750;
         cfg->coefficients[s][2] = 2.0315;

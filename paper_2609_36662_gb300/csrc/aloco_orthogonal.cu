@@ -319,7 +319,9 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     ortho_chain_kernel(const __grid_constant__ OrthoArgs args) {
     constexpr int kTile = kHalfTile * kCtas;
     constexpr uint32_t kDesc = product_desc(kTile, kTile);
-    constexpr int kSignals = kCtas * kEpilogueWarps;     // of a tile
+    constexpr int kPlaces = kCtas * kEpilogueWarps;      // warps that share a tile
+    constexpr int kBlocks = kTile / 64;                  // of a warp: 32 x 32 of its tile
+    constexpr int kSignals = kPlaces * kBlocks;
     extern __shared__ char raw[];
     const uint32_t smem = (smem_addr(raw) + 1023) & ~1023u;
     const uint32_t bars = smem + kSlots * kSlotBytes + kEpilogueWarps * kStageBytes;
@@ -564,6 +566,8 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             // L's diagonal: its tiles need nothing but their product
             const float shift = op.shifted ? cb / (2.f * cc) : 0.f;
             const bool joined = op.what == kPoly && !op.shifted;   // b L is added
+            const int parts = kParts ? parts_of(g, op) : 1;
+            const bool in_parts = kParts && parts > 1;
             // what a product is joined with: of L whole rows, of X also blocks that lie
             // as this warp holds them; fetched a block ahead
             uint4 *rest = g.rest + ((int64_t)(f.matrix * g.blocks_down + r0 / 32) * g.blocks_across +
@@ -608,7 +612,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                     const int lines = (c_end - c0 + 31) / 32 * 16;
                     for (int i = lane; i < lines; i += 32) fetch_l2(rest - lane + 8 * i);
                     fetch_x(c0);
-                } else if (joined) {
+                } else if (joined && !in_parts) {
                     fetch_l(c0);
                 }
             }
@@ -626,138 +630,166 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 else
                     mbar_arrive_cluster(cluster_addr(acc_empty(acc), 0));
             };
-            // A part of a tile leaves its sums; the warp that finds all others' there
-            // goes on with the tile.
-            const int parts = kParts ? parts_of(g, op) : 1;
-            bool finishes = true;
-            const float4 *sums = nullptr;
-            const int64_t next_part = kCtas * kEpilogueWarps * (kTile / 64) * kBlockQuads;
-            if (kParts && parts > 1 && some) {
-                const int64_t tile =
-                    (int64_t)f.matrix * g.sym_tiles + f.row * (f.row + 1) / 2 + f.col;
-                const int place = (int)rank * kEpilogueWarps + warp - kEpilogueWarp;
-                float4 *at = g.sums + tile * max(g.split[0], g.split[1]) * next_part +
-                             place * (kTile / 64) * kBlockQuads + lane;
-                sums = at;
-                at += f.part * next_part;
-#pragma unroll 1
-                for (int c = c0; c < c_end; c += 32, at += kBlockQuads) {
-                    uint32_t u[32];
-                    tmem_read32(tmem + acc * kTile + (c - f.col * kTile) + (quad << 21), u);
-                    const float bad = ok ? 0.f : __int_as_float(0x7fffffff);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        at[32 * i] = make_float4(
-                            __uint_as_float(u[4 * i]) + bad, __uint_as_float(u[4 * i + 1]) + bad,
-                            __uint_as_float(u[4 * i + 2]) + bad, __uint_as_float(u[4 * i + 3]) + bad);
-                }
-                release();
-                int came = 0;
-                if (lane == 0) {
-                    int *count = g.came + tile * kSignals + place;
-                    asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;"
-                                 : "=r"(came)
-                                 : "l"(count)
-                                 : "memory");
-                    if (came == parts - 1) *count = 0;   // for the next product
-                }
-                finishes = __shfl_sync(~0u, came, 0) == parts - 1;
+            // Of a tile in parts the warps that share a place go through its halves in turn,
+            // every other one from the second half on: where another part is missing a
+            // warp leaves its sums, where all others are there it finishes the half.  So
+            // two parts that end together finish a half each, and nobody waits.  (One warp
+            // that finishes all: 11 us after the last product of 2048 rows.)
+            const int64_t tile =
+                (int64_t)f.matrix * g.sym_tiles + f.row * (f.row + 1) / 2 + f.col;
+            const int place = (int)rank * kEpilogueWarps + warp - kEpilogueWarp;
+            const int64_t next_part = kPlaces * kBlocks * kBlockQuads;
+            float4 *const sums = in_parts
+                                     ? g.sums + tile * max(g.split[0], g.split[1]) * next_part +
+                                           place * kBlocks * kBlockQuads + lane
+                                     : nullptr;
+            const auto read = [&](int c, uint32_t (&u)[32]) {
                 __syncwarp();
-            }
+                tmem_read32(tmem + acc * kTile + (c - f.col * kTile) + (quad << 21), u);
+                if (!ok) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) u[i] = 0x7fffffff;
+                }
+            };
+            // Columns [c, to): true if all other parts' sums are there.
+            const auto meets = [&](bool late, int half, int c, int to) {
+                int *count = g.came + (tile * kPlaces + place) * 2 + half;
+                int came = late && lane == 0 ? load_acquire(count) : 0;
+                if (__shfl_sync(~0u, came, 0) != parts - 1) {
+                    float4 *at = sums + f.part * next_part + (c - begin) / 32 * kBlockQuads;
+#pragma unroll 1
+                    for (; c < to; c += 32, at += kBlockQuads) {
+                        uint32_t u[32];
+                        read(c, u);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            at[32 * i] = make_float4(
+                                __uint_as_float(u[4 * i]), __uint_as_float(u[4 * i + 1]),
+                                __uint_as_float(u[4 * i + 2]), __uint_as_float(u[4 * i + 3]));
+                    }
+                    __syncwarp();
+                    if (lane == 0)
+                        asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;"
+                                     : "=r"(came)
+                                     : "l"(count)
+                                     : "memory");
+                    if (__shfl_sync(~0u, came, 0) != parts - 1) return false;
+                }
+                if (lane == 0) *count = 0;   // for the next product
+                __syncwarp();
+                return true;
+            };
             // column c0's sums of this row
             const auto values = [&](float (&v)[32]) {
-                if (kParts && sums) {
-                    const float4 *p = sums + (c0 - begin) / 32 * kBlockQuads;
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = 0.f;
-#pragma unroll 1
-                    for (int k = 0; k < parts; ++k, p += next_part) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float4 q = __ldcg(p + 32 * i);
-                            v[4 * i] += q.x;
-                            v[4 * i + 1] += q.y;
-                            v[4 * i + 2] += q.z;
-                            v[4 * i + 3] += q.w;
-                        }
-                    }
-                    return;
-                }
                 uint32_t u[32];
-                __syncwarp();
-                tmem_read32(tmem + acc * kTile + (c0 - f.col * kTile) + (quad << 21), u);
+                read(c0, u);
                 if (c0 + 32 >= c_end) release();
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(u[i]);
-                if (!ok) {
+            };
+            // The same of all parts: of two this warp's and the other's, of more all as
+            // they lie there, in their order.
+            const auto total = [&](float (&v)[32]) {
+                uint32_t u[32];
+                read(c0, u);
+                const float4 *p = sums + (c0 - begin) / 32 * kBlockQuads;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = __int_as_float(0x7fffffff);
+                for (int i = 0; i < 32; ++i) v[i] = parts == 2 ? __uint_as_float(u[i]) : 0.f;
+#pragma unroll 1
+                for (int k = 0; k < parts; ++k, p += next_part) {
+                    if (parts == 2 && k == f.part) continue;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float4 q = __ldcg(p + 32 * i);
+                        v[4 * i] += q.x;
+                        v[4 * i + 1] += q.y;
+                        v[4 * i + 2] += q.z;
+                        v[4 * i + 3] += q.w;
+                    }
                 }
             };
+            int finished = kBlocks;          // blocks
             if (!some) {
                 release();
-                finishes = parts == 1 || f.part == 0;
-            } else if (!finishes) {
+                if (f.part) finished = 0;
             } else if (!up) {
                 const float scale = op.what == kGram   ? 1.f / (kOrthoScale * kOrthoScale)
                                     : op.what == kPoly ? cc
                                                        : 1.f;
                 __half *out = g.sym[op.out] + row0 * g.lda;
+                int stop = c_end;
+                // (of blocks that there are not the first part tells)
+                if (in_parts) finished = f.part ? 0 : kBlocks - (c_end - begin + 31) / 32;
 #pragma unroll 1
-                for (; c0 < c_end; c0 += 32) {
-                    float v[32];
-                    values(v);
-                    if (joined) {
-                        __syncwarp();
-                        part.to_shared(st);
-                        if (c0 + 32 < c_end) fetch_l(c0 + 32);
-                        __syncwarp();
+                for (int turn = 0; turn < (in_parts ? 2 : 1); ++turn) {
+                    if (in_parts) {
+                        const int half = turn ^ (f.part & 1);
+                        c0 = begin + half * (kTile / 4);
+                        stop = min(c_end, c0 + kTile / 4);
+                        if (c0 >= stop || !meets(turn && parts == 2, half, c0, stop)) continue;
+                        finished += (stop - c0 + 31) / 32;
+                        if (joined) fetch_l(c0);
                     }
-                    // The diagonal from what lies beside the operands: their own values as
-                    // the product has them are taken out, and put back unrounded.
-                    float own = 0.f;
-                    if (c0 == r0) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (i == lane) own = v[i];
-                        const auto rounded = [](float x) {
-                            return __half2float(__float2half_rn(x));
-                        };
-                        if (op.what == kGram) {
-                            own *= scale;
-                        } else if (op.what == kPoly) {
-                            const float s = rounded(by_row + shift);
-                            own = ca + cb * by_row + cc * (by_row * by_row + (own - s * s));
-                        } else {
-                            own = by_row * by_row2 +
-                                  (own - rounded(by_row) * rounded(by_row2));
+#pragma unroll 1
+                    for (; c0 < stop; c0 += 32) {
+                        float v[32];
+                        if (in_parts)
+                            total(v);
+                        else
+                            values(v);
+                        if (joined) {
+                            __syncwarp();
+                            part.to_shared(st);
+                            if (c0 + 32 < stop) fetch_l(c0 + 32);
+                            __syncwarp();
                         }
-                        if (r < m) g.diag[op.out][row0 + r] = own;
-                    }
+                        // The diagonal from what lies beside the operands: their own values as
+                        // the product has them are taken out, and put back unrounded.
+                        float own = 0.f;
+                        if (c0 == r0) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] *= scale;
-                    if (joined) {
+                            for (int i = 0; i < 32; ++i)
+                                if (i == lane) own = v[i];
+                            const auto rounded = [](float x) {
+                                return __half2float(__float2half_rn(x));
+                            };
+                            if (op.what == kGram) {
+                                own *= scale;
+                            } else if (op.what == kPoly) {
+                                const float s = rounded(by_row + shift);
+                                own = ca + cb * by_row + cc * (by_row * by_row + (own - s * s));
+                            } else {
+                                own = by_row * by_row2 +
+                                      (own - rounded(by_row) * rounded(by_row2));
+                            }
+                            if (r < m) g.diag[op.out][row0 + r] = own;
+                        }
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint4 w = *piece(st, lane, i);
-                            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+                        for (int i = 0; i < 32; ++i) v[i] *= scale;
+                        if (joined) {
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const float2 h = unpack(ws[j]);
-                                v[8 * i + 2 * j] = fmaf(cb, h.x, v[8 * i + 2 * j]);
-                                v[8 * i + 2 * j + 1] = fmaf(cb, h.y, v[8 * i + 2 * j + 1]);
+                            for (int i = 0; i < 4; ++i) {
+                                const uint4 w = *piece(st, lane, i);
+                                const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    const float2 h = unpack(ws[j]);
+                                    v[8 * i + 2 * j] = fmaf(cb, h.x, v[8 * i + 2 * j]);
+                                    v[8 * i + 2 * j + 1] = fmaf(cb, h.y, v[8 * i + 2 * j + 1]);
+                                }
                             }
                         }
-                    }
-                    if (c0 == r0) {
-                        const float kept =
-                            op.bare ? 0.f : op.what == kGram ? own + shift : own;
+                        if (c0 == r0) {
+                            const float kept =
+                                op.bare ? 0.f : op.what == kGram ? own + shift : own;
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (i == lane) v[i] = kept;
+                            for (int i = 0; i < 32; ++i)
+                                if (i == lane) v[i] = kept;
+                        }
+                        store_symmetric(out, m, g.lda, r0, c0, mirrored, st, v);
                     }
-                    store_symmetric(out, m, g.lda, r0, c0, mirrored, st, v);
                 }
+                if (in_parts) release();
             } else {
 #pragma unroll 1
                 for (; c0 < c_end; c0 += 32) {
@@ -821,12 +853,13 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                                 g.n - c0);
                 }
             }
-            if (!op.last && finishes) {
+            if (!op.last && finished) {
                 // done: what this warp has written is seen behind the count (by tensor
                 // copies behind a fence of theirs)
                 __syncwarp();
                 if (lane == 0)
-                    asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(done_of(f))
+                    asm volatile("red.release.gpu.global.add.s32 [%0], %1;" ::"l"(done_of(f)),
+                                 "r"(finished)
                                  : "memory");
             }
             if (acc) acc_phase ^= 1;
@@ -945,7 +978,7 @@ __global__ void __launch_bounds__(kThreads) ortho_prepare_kernel(const __grid_co
 #pragma unroll
         for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
         if (threadIdx.x == 0) {
-            const bool usual = sum > 1e-30 && sum < 1e30;
+            const bool usual = sum > 1e-30 && sum < 1e30 && args.eps < 1e30;
             s_f = usual ? kOrthoScale / (sqrtf((float)sum) + (float)args.eps) : 0.f;
             if (!usual) s_factor = (double)kOrthoScale / (sqrt(sum) + args.eps);
         }

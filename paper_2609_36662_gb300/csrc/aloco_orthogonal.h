@@ -59,11 +59,11 @@ struct OrthoGroup {
     uint4 *rest;                     // X - x, kBlockPieces a block: 8 columns of a row each
     int blocks_down, blocks_across;  // of a matrix
     double *partial;                 // [count][chunks] sums of squares
-    int *done;                       // [count] warps that have finished a tile
+    int *done;                       // [count] blocks of 32 x 32 that are finished
     // where tiles have parts: their sums, a block as a warp holds it after the other,
-    // and how many of a tile's parts a warp's place has
+    // and how many parts have left theirs for either half of a warp's blocks
     float4 *sums;                    // [count][sym_tiles][parts]
-    int *came;                       // [count][sym_tiles][warps]
+    int *came;                       // [count][sym_tiles][warps][2]
 };
 
 // What fits a CTA of launch_ortho_small: rows of X, and columns of it.

@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 total += t;
             }
         }
-        const bool usual = total > 1e-30 && total < 1e30;
+        const bool usual = total > 1e-30 && total < 1e30 && args.eps < 1e30;
         s_factor = usual ? kOrthoScale / (sqrtf((float)total) + (float)args.eps) : 0.f;
         if (!usual) s_sum[0] = (double)kOrthoScale / (sqrt(total) + args.eps);
     }

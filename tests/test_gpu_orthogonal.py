@@ -107,6 +107,36 @@ def test_coefficients_of_every_step():
     _check(x, A.orthogonalize(x, coefficients=many), coefficients=many)
 
 
+@pytest.mark.parametrize("shape", [(3, 40, 200), (2, 140, 300), (60, 300, 520)],
+                         ids=["small", "tiles", "two_steps"])
+def test_polynomials_without_products(shape):
+    """b = c = 0: X times the steps' a.  Rounded to bf16 once; X before that to 22
+    bits, or 2^-33 where fp16's least value counts."""
+    x = torch.randn(shape, generator=_gen(6), device="cuda")
+    out = A.orthogonalize(x, coefficients=[[1.7, 0, 0], [0.6, 0.0, 0.0]])
+    want = 1.7 * 0.6 * x.double() / (x.double().square().sum((1, 2), keepdim=True).sqrt() + 1e-7)
+    assert ((out.double() - want).abs() <= (2.0**-8 + 2.0**-19) * want.abs() + 2.0**-31).all()
+
+
+@pytest.mark.parametrize("eps", [3.0, 1e20, 1e39, 1e300])
+@pytest.mark.parametrize("shape", [(40, 200), (140, 300)], ids=["small", "tiles"])
+def test_eps_of_any_size(shape, eps):
+    x = torch.randn(shape, generator=_gen(7), device="cuda")
+    out = A.orthogonalize(x, eps=eps)
+    if eps == 3.0:
+        _check(x, out, eps=eps)
+    else:
+        # 3.4445^5 |x| / eps < 485 * 6 / 1e20, or nothing where X is fp16 values
+        assert (out.abs() < 1e-16).all()
+
+
+def test_coefficients_in_any_sequence():
+    x = momentum_like(40, 60, _gen(8))
+    first = A.orthogonalize(x)
+    for c in ([list(COEFFICIENTS)] * 5, (list(COEFFICIENTS),) * 5, iter([COEFFICIENTS] * 5)):
+        assert torch.equal(A.orthogonalize(x, coefficients=c), first)
+
+
 def test_zeros_and_what_is_not_finite():
     x = torch.stack([momentum_like(130, 150, _gen(i)) for i in range(5)])
     alone = A.orthogonalize(x)

@@ -139,6 +139,9 @@ def test_settings_by_name():
         A.muon_cfg(coefficients=[])
     with pytest.raises(ValueError):
         A.muon_cfg(coefficients=[(1.0, 2.0)])
+    with pytest.raises(TypeError):
+        A.Matrices([(0, 2.5, 4)])
+    assert list(A.muon_cfg(steps=16).coefficients[15]) == list(A.NEWTON_SCHULZ)
     c = A.muon_cfg(coefficients=[(1.5, -0.5, 0.0)] * 3, lr=0.1)
     assert c.steps == 3 and list(c.coefficients[2]) == [1.5, -0.5, 0.0] and c.lr == 0.1
 
