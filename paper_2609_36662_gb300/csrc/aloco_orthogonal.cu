@@ -24,12 +24,16 @@ constexpr int kStageBytes = 4096;    // an epilogue warp's: a pair of 32 x 32 fp
 constexpr int kSharedBytes =
     kSlots * kSlotBytes + kEpilogueWarps * kStageBytes + 1024 + 512;
 constexpr int kRing = 4;             // tiles that a CTA knows of
+constexpr int kAsk = 6;              // the next is taken so many slots before a tile's last
 
 struct Work {
     int op;                          // of the group's list; < 0: there is no more
     int group, matrix;
     int row, col;                    // in tiles
-    int before;                      // tiles of the matrix that have to be done
+    union {
+        int before;                  // tiles of the matrix that have to be done
+        int given_up;                // as it is told: they were not
+    };
     int part;                        // of the depth
     int unused;
 };
@@ -332,9 +336,8 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     const uint32_t drained = bars + 8 * (2 * kSlots + 4);
     const auto told = [&](int s) { return bars + 8 * (2 * kSlots + 5 + s); };
     const auto heard = [&](int s) { return bars + 8 * (2 * kSlots + 5 + kRing + s); };
-    const auto work_at = [&](int s) {
-        return ((bars + 8 * (2 * kSlots + 5 + 2 * kRing) + 15) & ~15u) + 32 * s;
-    };
+    const uint32_t asked = bars + 8 * (2 * kSlots + 5 + 2 * kRing);
+    const auto work_at = [&](int s) { return ((asked + 8 + 15) & ~15u) + 32 * s; };
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_abort;
 
@@ -355,9 +358,11 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         mbar_init(drained, 1);
         for (int s = 0; s < kRing; ++s) {
             mbar_init(told(s), 1);
-            // all that hear of a tile but the thread that tells
-            mbar_init(heard(s), kCtas * (kEpilogueWarps + 2));
+            // all that hear of a tile: a CTA's copying threads and warps, and whoever
+            // issues the products
+            mbar_init(heard(s), kCtas * (kEpilogueWarps + 2) + 1);
         }
+        mbar_init(asked, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) tmem_alloc<kCtas>(smem_addr(&s_tmem), 2 * kTile);
@@ -372,7 +377,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     grid_go();
     grid_wait();
 
-    // The next tile, as all but the first producer hear of it.
+    // The next tile, as all but the thread that takes it hear of it.
     int ring = 0;
     uint32_t ring_phase = 0;
     const auto on = [&] {
@@ -387,7 +392,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                          : "r"(work_at(ring))
                          : "memory");
             asm volatile("ld.shared.v4.s32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(f.col), "=r"(f.before), "=r"(f.part), "=r"(f.unused)
+                         : "=r"(f.col), "=r"(f.given_up), "=r"(f.part), "=r"(f.unused)
                          : "r"(work_at(ring) + 16)
                          : "memory");
         }
@@ -413,52 +418,54 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         return min(all, chunks * (f.part + 1) / parts * kK);
     };
 
-    if ((warp == 0 || warp == 3) && lane == 0) {
+    if (warp == 2 && lane == 0 && rank == 0) {
+        // Takes tiles, and tells of one when all that it needs is there.
+        Finder finder;
+        uint32_t asked_phase = 0;
+        for (;;) {
+            const int next = atomicAdd(args.next_tile, 1);
+            Work f;
+            f.op = -1;
+            if (next < tiles) {
+                f = finder.find(args, next, kTile);
+                if (s_abort || !wait_done(done_of(f), f.before * kSignals, &s_abort)) s_abort = 1;
+            }
+            if (!mbar_wait_cluster(heard(ring), ring_phase ^ 1)) break;
+            for (int p = 0; p < kCtas; ++p) {
+                const uint32_t at = kCtas == 1 ? work_at(ring) : cluster_addr(work_at(ring), p);
+                asm volatile("st.shared::cluster.v4.s32 [%0], {%1, %2, %3, %4};" ::"r"(at),
+                             "r"(f.op), "r"(f.group), "r"(f.matrix), "r"(f.row)
+                             : "memory");
+                asm volatile("st.shared::cluster.v4.s32 [%0], {%1, %2, %3, %4};" ::"r"(at + 16),
+                             "r"(f.col), "r"(s_abort), "r"(f.part), "r"(0)
+                             : "memory");
+            }
+            mbar_arrive(told(ring));
+            if constexpr (kCtas == 2)
+                asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(
+                                 cluster_addr(told(ring), 1))
+                             : "memory");
+            on();
+            if (f.op < 0) break;
+            if (!mbar_wait_cluster(asked, asked_phase)) break;
+            asked_phase ^= 1;
+        }
+    } else if ((warp == 0 || warp == 3) && lane == 0) {
         // One thread for either operand: copying both, a thread takes as long as
         // the products of a slot do.
-        const bool is_b = warp == 3, tells = rank == 0 && !is_b;
+        const bool is_b = warp == 3, leads = rank == 0 && !is_b;
         const uint32_t bar0 = kCtas == 1 ? full(0) : cluster_addr(full(0), 0);
         int slot = 0, issued = 0;
         uint32_t phase = 0;
         bool ok = true;
-        Finder finder;
-        int next = tells ? atomicAdd(args.next_tile, 1) : 0;
         for (;;) {
-            Work f;
-            if (tells) {
-                if (next < tiles)
-                    f = finder.find(args, next, kTile);
-                else
-                    f.op = -1;
-                if (!mbar_wait_cluster(heard(ring), ring_phase ^ 1)) break;
-                for (int p = 0; p < kCtas; ++p) {
-                    const uint32_t at = kCtas == 1 ? work_at(ring) : cluster_addr(work_at(ring), p);
-                    asm volatile("st.shared::cluster.v4.s32 [%0], {%1, %2, %3, %4};" ::"r"(at),
-                                 "r"(f.op), "r"(f.group), "r"(f.matrix), "r"(f.row)
-                                 : "memory");
-                    asm volatile("st.shared::cluster.v4.s32 [%0], {%1, %2, %3, %4};" ::"r"(at + 16),
-                                 "r"(f.col), "r"(f.before), "r"(f.part), "r"(0)
-                                 : "memory");
-                }
-                mbar_arrive(told(ring));
-                if constexpr (kCtas == 2)
-                    asm volatile(
-                        "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(
-                            cluster_addr(told(ring), 1))
-                        : "memory");
-                on();
-            } else {
-                f = hear(false);
-            }
+            const Work f = hear(false);
             if (f.op < 0) break;
             const OrthoOp &op = op_of(args, f);
             int begin;
             const int end = depth_of(f, op, &begin);
-            const int ask = begin + max(0, (end - begin - 1) / kK + 1 - kSlots) * kK;
-            if (ok && !s_abort)
-                ok = wait_done(done_of(f), f.before * kSignals, &s_abort);
-            else
-                ok = false;
+            const int ask = begin + max(0, (end - begin - 1) / kK + 1 - kAsk) * kK;
+            ok = ok && !f.given_up && !s_abort;
             // operands were written by ordinary stores
             asm volatile("fence.proxy.async;" ::: "memory");
             const bool x = op.what == kGram || (op.what == kUpdate && is_b);
@@ -468,11 +475,11 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             // columns from here on lie below, MN-major (X does throughout)
             const int turn = op.what == kGram ? INT_MAX : x ? 0 : (row / kFull + 1) * kFull;
             for (int c = begin; c < end; c += kK) {
-                if (tells && c == ask) next = atomicAdd(args.next_tile, 1);
+                if (leads && c == ask) mbar_arrive(asked);
                 if (!ok || !(ok = mbar_wait(empty(slot), phase ^ 1, &s_abort))) continue;
                 const uint32_t at = smem + slot * kSlotBytes + (is_b ? 2 * kBoxBytes : 0);
                 const uint32_t bar = bar0 + 8 * slot;
-                if (tells) mbar_arrive_expect_tx(full(slot), kCtas * kSlotBytes);
+                if (leads) mbar_arrive_expect_tx(full(slot), kCtas * kSlotBytes);
                 if (args.test_stall1 == 0 || blockIdx.x != 0 || issued != args.test_stall1 - 1) {
                     if (c < turn) {
                         tensor_load<kCtas>(at, map, c, row, f.matrix, bar);
@@ -487,7 +494,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             }
             if (!ok) s_abort = 1;
         }
-        if ((!ok || s_abort) && tells)
+        if ((!ok || s_abort) && leads)
             // copies in flight land before the block ends (each slot's last use)
             for (int i = issued > kSlots ? issued - kSlots : 0; i < issued; ++i)
                 mbar_wait(full(i % kSlots), (i / kSlots) & 1, nullptr);
@@ -598,10 +605,6 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             }
             bool ok = !s_abort;
             if (op.what != kGram && some) {
-                // (products that are done had what they needed)
-                if (ok && !__all_sync(~0u, mbar_test(acc_full(acc), acc_phase)))
-                    ok = wait_done(done_of(f), f.before * kSignals, &s_abort);
-                ok = __all_sync(~0u, ok);
                 if (r < m) {
                     by_row = __ldcg(g.diag[op.left] + row0 + r);
                     if (op.what == kProduct) by_row2 = __ldcg(g.diag[op.right] + row0 + r);
