@@ -32,15 +32,12 @@ struct Shape {
     int64_t rows, cols;
     int first, period;               // places [first, first + period)
     bool merged;                     // may take two steps at a time
+    int64_t chunk;                   // elements of a norm block
     int64_t m() const { return std::min(rows, cols); }
     int64_t n() const { return std::max(rows, cols); }
     int64_t ldx() const { return (int64_t)up((size_t)n(), 8); }
     int64_t lda() const { return (int64_t)up((size_t)m(), 8); }
-    // norm blocks of a matrix and the elements of each
-    int64_t chunk() const {
-        return std::max<int64_t>(4096, (int64_t)up((size_t)(rows * cols / 256), 4096));
-    }
-    int64_t chunks() const { return (rows * cols + chunk() - 1) / chunk(); }
+    int64_t chunks() const { return (rows * cols + chunk - 1) / chunk; }
     // places for symmetric matrices
     int syms() const { return merged ? kOrthoSyms : 2; }
     int64_t down() const { return (m() + 31) / 32; }
@@ -170,9 +167,15 @@ void split(Plan *p, int workers, int most_ctas) {
     });
     // Two steps at a time, where the matrix is wide and its symmetric products fill
     // the GPU (they take their depth alone, without X's length).
-    for (Shape &s : p->shapes)
+    // Norm blocks: two rounds of eight an SM, of 4096 to 65536 elements; at most 1024 of
+    // a matrix.
+    for (Shape &s : p->shapes) {
+        const int64_t all = s.period * (int64_t)workers, size = s.rows * s.cols;
         s.merged = 2 * s.n() >= 3 * s.m() &&
-                   s.period * workers * sym_tiles(s, ortho_pair_tile()) >= kPlannedSms;
+                   all * sym_tiles(s, ortho_pair_tile()) >= kPlannedSms;
+        const int64_t each = std::min<int64_t>(65536, all * size / (kPlannedSms * 16));
+        s.chunk = std::max<int64_t>(4096, (int64_t)up((size_t)std::max(each, size / 1024), 4096));
+    }
     // (beside larger ones the small fill tiles of the kernels that run anyway)
     bool all = true;
     for (const Shape &s : p->shapes) all = all && small_ctas(s, most_ctas);
@@ -244,7 +247,7 @@ void plan_matrices(const aloco_matrix_t *mats, int64_t n, int workers, int most_
         const aloco_matrix_t &x = mats[i];
         if (p->shapes.empty() || p->shapes.back().rows != x.rows ||
             p->shapes.back().cols != x.cols || p->shapes.back().period == 256)
-            p->shapes.push_back({x.rows, x.cols, (int)p->place.size(), 0, false});
+            p->shapes.push_back({x.rows, x.cols, (int)p->place.size(), 0, false, 0});
         ++p->shapes.back().period;
         p->place.push_back(x.offset);
     }
@@ -254,7 +257,7 @@ void plan_matrices(const aloco_matrix_t *mats, int64_t n, int workers, int most_
 void plan_batch(int64_t batch, int64_t rows, int64_t cols, int most_ctas, Plan *p) {
     for (int64_t i = 0; i < batch; ++i) {
         if (p->shapes.empty() || p->shapes.back().period == 256)
-            p->shapes.push_back({rows, cols, (int)i, 0, false});
+            p->shapes.push_back({rows, cols, (int)i, 0, false, 0});
         ++p->shapes.back().period;
         p->place.push_back(i);
     }
@@ -372,7 +375,7 @@ int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base, const do
         fill_group(plan, part, a.place, &places, &g);
         g.ldx = (int)s.ldx();
         g.lda = (int)s.lda();
-        g.chunk = (int)s.chunk();
+        g.chunk = (int)s.chunk;
         g.chunks = (int)s.chunks();
         g.norm0 = norm;
         norm += g.chunks * g.count;

@@ -944,8 +944,9 @@ __global__ void __launch_bounds__(kThreads) ortho_norm_kernel(const __grid_const
 constexpr int kPrep = 64;            // rows and columns of a prepared tile
 
 // X = U 2^8 / (|U| + eps) as a sum of two fp16 values, transposed where the matrix
-// is tall, and the new momentum.
-__global__ void __launch_bounds__(kThreads) ortho_prepare_kernel(const __grid_constant__ OrthoArgs args) {
+// is tall, and the new momentum.  Bound by HBM: 48 x 768 x 768 fp32 (227 MB) 51 us
+// with cold caches.  Five blocks an SM: 4 us less than four or six in a call.
+__global__ void __launch_bounds__(kThreads, 5) ortho_prepare_kernel(const __grid_constant__ OrthoArgs args) {
     __shared__ float s_f;            // the factor, where fp32 does for it
     __shared__ double s_factor;
     __shared__ float tile[kPrep][kPrep + 1];
@@ -973,14 +974,20 @@ __global__ void __launch_bounds__(kThreads) ortho_prepare_kernel(const __grid_co
             old[i] = is && s.momentum ? load4(s.momentum, e, 0) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
     }
-    // (one warp sums: the SM adds two doubles a clock)
-    if (threadIdx.x < 32) {
+    // (few warps where there is little to add: the SM adds two doubles a clock)
+    const int warps = min(kThreads / 32, (g.chunks + 63) / 64);
+    __shared__ double sums[kThreads / 32];
+    if ((int)threadIdx.x < 32 * warps) {
         double sum = 0.0;
-        for (int i = threadIdx.x; i < g.chunks; i += 32)
+        for (int i = threadIdx.x; i < g.chunks; i += 32 * warps)
             sum += g.partial[(int64_t)matrix * g.chunks + i];
 #pragma unroll
         for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+        if (threadIdx.x % 32 == 0) sums[threadIdx.x / 32] = sum;
+        if (warps > 1)
+            asm volatile("bar.sync 1, %0;" ::"r"(32 * warps) : "memory");
         if (threadIdx.x == 0) {
+            for (int w = 1; w < warps; ++w) sum += sums[w];
             const bool usual = sum > 1e-30 && sum < 1e30 && args.eps < 1e30;
             s_f = usual ? kOrthoScale / (sqrtf((float)sum) + (float)args.eps) : 0.f;
             if (!usual) s_factor = (double)kOrthoScale / (sqrt(sum) + args.eps);
