@@ -1,5 +1,11 @@
 // Orthogonal factors by Newton-Schulz products on the tensor cores: X <- (a +
 // b A + c A A) X with A = X X^T, some steps of it, for many matrices at once.
+//
+// X in bf16 loses 1 to 4e-2 of the factor, in fp16 up to 0.15 at rank one: what
+// multiplies X itself grows by a^steps where singular values are small.  So X is a sum
+// of two fp16 values, of which products take the larger; the diagonal of the
+// polynomial, which multiplies X itself, comes in fp32 from diagonals kept beside the
+// matrices and takes both.
 #include <climits>
 #include <type_traits>
 
@@ -14,7 +20,7 @@ constexpr int kEpilogueWarps = 8;
 constexpr int kEpilogueWarp = 4;     // the first of them
 constexpr int kProductThreads = 32 * (kEpilogueWarp + kEpilogueWarps);
 constexpr int kHalfTile = 128;       // a CTA's rows of a tile
-constexpr int kFull = 256;           // blocks of A and P on the diagonal that are whole
+constexpr int kFull = 256;           // symmetric matrices' diagonal blocks that are whole
 constexpr int kK = 64;               // k-elements of a slot: 128 bytes a row
 constexpr int kBox = 64;             // rows of a copied box
 constexpr int kBoxBytes = kBox * kK * 2;
@@ -307,14 +313,25 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity)
 // All operations of all matrices, tile by tile.  CTAs (pairs of them) take the next
 // tile when they have asked for the operands of the one before, so that no two
 // wait for each other: what a tile needs was handed out before it, and counts of
-// the matrix's tiles that are done say when it is there.
+// the matrix's blocks that are done say when it is there.
 //
-// In a CTA two threads copy operands into a ring of slots (the first of a pair's
-// also takes the tiles), one issues the products into one of two accumulators,
-// eight warps join the other one with what it needs and write it.  Of symmetric
-// matrices the lower tiles are computed and kept, with whole blocks of kFull on the
-// diagonal; where a product needs what would lie above them it takes the tile
-// below, MN-major instead of K-major.
+// In a CTA two threads copy operands into a ring of slots, one issues the products
+// into one of two accumulators, eight warps join the other one with what it needs
+// and write it, and one (of a pair's first CTA) takes the tiles, waits for what they
+// need, and tells the others.  Of symmetric matrices the lower tiles are computed
+// and kept, with whole blocks of kFull on the diagonal; where a product needs what
+// would lie above them it takes the tile below, MN-major instead of K-major.
+//
+// Bound by the tensor cores where matrices are large (16 x 2048 x 2048: 512 of 540
+// cycles a slot, at the clock that 1360 W leave); at 768 by the epilogue too, which
+// moves 8 bytes an element of X in and out of L2 for 12 slots of products (48 x 768
+// x 768: tensor cores 42 % busy, HBM 44 % of its peak, 7.8 GB through L2; 566 us the
+// whole call); for a few small matrices by 15 dependent products, of which each
+// takes about 10 us: 1 until it is known that its operands are there, 2 until the
+// first of them have come, 3 of products, 4 until the last tile is written.
+// A kernel for every product took 315 us in place of 254 for 7 odd matrices of 3
+// workers, 663 of 641 for 48 x 768 x 768 and 2.48 of 2.25 ms for 16 x 2048 x 2048: a
+// matrix waits for itself alone.
 //
 // A wait that runs out ends the waits of its CTA; its tiles are NaN from there on,
 // and with them their matrices.

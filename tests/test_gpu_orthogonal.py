@@ -162,6 +162,24 @@ def test_reruns_streams_and_out():
     assert torch.equal(first, out) and torch.equal(first, other)
 
 
+@pytest.mark.parametrize("shape", [(300, 6000), (140, 4100), (1500, 2100), (1030, 1030)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_parts_of_tiles_give_the_same_bits(shape):
+    """Whichever part comes last: alone, and beside a call that takes SMs away."""
+    x = momentum_like(*shape, _gen(9))
+    first = A.orthogonalize(x)
+    _check(x, first)
+    other = torch.stack([momentum_like(300, 400, _gen(i)) for i in range(20)])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    outs = []
+    for _ in range(6):
+        A.orthogonalize(other, stream=side)
+        outs.append(A.orthogonalize(x))
+    torch.cuda.synchronize()
+    assert all(torch.equal(first, o) for o in outs)
+
+
 def test_captured_calls_have_scratch_of_their_own():
     xs = [momentum_like(300, 200, _gen(i)) for i in range(2)]
     want = [A.orthogonalize(x) for x in xs]
