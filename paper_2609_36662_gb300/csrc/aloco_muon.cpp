@@ -106,18 +106,20 @@ size_t sums_bytes(const Shape &s, int64_t count, const std::array<int, 2> &split
     return parts > 1 ? (size_t)(count * sym_tiles(s, tile) * parts) * tile * tile * 4 : 0;
 }
 
-// Tiles by pairs of CTAs where they fill the GPU; by single CTAs, whose tiles are a
-// quarter, below.  Where A's or P's tiles are fewer than the CTAs, parts of their
+// Tiles by pairs of CTAs where the matrices' elements fill them; by single CTAs, whose
+// tiles are a quarter, below: 8 matrices of 300 x 2000 192 us by single ones and 225 by
+// pairs, 7 odd ones of 3 workers 217 and 254, where a matrix's edges count as whole
+// tiles too; 3 of 1500 x 1500 (103 tiles' elements) 333 and 302.  Where A's or P's tiles are fewer than the CTAs, parts of their
 // depth are tiles of their own: as many as there are CTAs for, of at least 12
 // slots.  (5632 x 2048 alone: 88 slots a tile of A, 36 tiles for 76 pairs.)
 void lay_out(const Plan &plan, Pass *pass) {
-    int64_t up_tiles = 0;
+    int64_t elements = 0;
     for (const Part &part : pass->parts) {
         const Shape &s = plan.shapes[part.shape];
-        up_tiles += part.count * tiles_of(s.m(), ortho_pair_tile()) *
-                    tiles_of(s.n(), ortho_pair_tile());
+        elements += part.count * s.m() * s.n();
     }
-    pass->ctas = up_tiles >= kPlannedSms / 2 ? 2 : 1;
+    const int64_t tile_elements = (int64_t)ortho_pair_tile() * ortho_pair_tile();
+    pass->ctas = elements >= kPlannedSms / 2 * tile_elements ? 2 : 1;
     const int tile = ortho_pair_tile() / 2 * pass->ctas, slots = kPlannedSms / pass->ctas;
     pass->split.assign(pass->parts.size(), {1, 1});
     for (int what = 0; what < 2; ++what) {
