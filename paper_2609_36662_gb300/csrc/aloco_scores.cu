@@ -192,7 +192,7 @@ __device__ __forceinline__ float warp_sum(float x) {
 // One CTA's share of a row, as the others of its cluster read it.
 struct Share {
     unsigned largest;
-    float ref, z, s;
+    float ref, z, s;                 // z: without the largest's term, where rows are split
     unsigned long long best[ALOCO_MAX_TOP];  // (order, ~index), largest first; 0: none
 };
 
@@ -401,14 +401,17 @@ __device__ __noinline__ void find_best(const Row<kBf16> &row, int u0, int u1, in
 // maxima and its sums to a whole reference.  For the alternatives the maxima give
 // a limit that k values reach, and the few batches that reach it are read again.
 //
+// kSplit: rows of more than one CTA (where there are none a split that the compiler
+// knows spills: 84 us in place of 80).
+//
 // Bound by HBM; the steps behind a row's last unit (a limit, a few values read
 // again, their order: about 2 us) are hidden by the other CTAs of the SM, so CTAs
 // are small.  8184 x 32000 bf16 with 8 alternatives: 104 us with 11 CTAs of 128
 // threads an SM, 120 with 6 of 256 (77 at the copy rate); 4000 x 128256: 179 and
 // 182 us (152), 170 with 9 CTAs, which take 72 us where 11 take 59 for 1533 x 50257
 // fp32.  Without alternatives 10 are best: 88 and 159 us.
-template <bool kBf16, bool kTop, int kGroup>
-__global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kTop ? 11 : 10)
+template <bool kBf16, bool kTop, int kGroup, bool kSplit>
+__global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kSplit ? 8 : kTop ? 11 : 10)
     token_scores_kernel(const __grid_constant__ ScoresArgs a, int split) {
     using G = Group<kGroup>;
     constexpr int N = Row<kBf16>::N, kGroups = cta_of(kGroup) / kGroup, kWarps = G::kWarps;
@@ -476,13 +479,42 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kTop ? 11 :
         sums.s += s.x + s.y;
     });
 
-    // the group's, then the cluster's
+    // The group's, then the cluster's.  The largest value's term stays beside the sum:
+    // the log-probability of a token that is nearly certain is what the other terms are
+    // to it, which a sum with it would round away.  Where it is a quarter of a warp's sum
+    // the warp takes the units of the thread that had it again, without it.  (Where rows
+    // are few.  Where they are many the sum is of all terms: what follows a row is not
+    // hidden then, and 8184 x 32000 bf16, a quarter left out, took 88 us in place of 80.)
     const unsigned mine = nan ? ~0u : order(large.first);
-    const auto combine = [&] {
+    const auto combine = [&](auto term) {        // term: of a value, to a reference
         const unsigned high = __reduce_max_sync(~0u, mine);
         const int ref = __reduce_max_sync(~0u, (int)fminf(sums.ref, 2.f * kFar));
         sums.refer((float)ref);
-        const float z = warp_sum(sums.z), s = warp_sum(sums.s);
+        const float s = warp_sum(sums.s);
+        float z = warp_sum(sums.z);
+        if constexpr (kSplit) {
+            const float top = unorder(high), e = term(top, (float)ref);
+            if (4.f * e > z) {
+                const int owner = __ffs(__ballot_sync(~0u, mine == high)) - 1;
+                float rest = lane == owner ? 0.f : sums.z;
+                int equal = 0;
+                for (int u = u0 + tid - lane + owner + lane * kGroup; u < u1; u += 32 * kGroup) {
+                    float v[N];
+                    Row<kBf16>::values(row.load(u, u1), v);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        if (v[i] == top)
+                            ++equal;
+                        else
+                            rest += term(v[i], (float)ref);
+                    }
+                }
+                equal = __reduce_add_sync(~0u, equal);
+                z = warp_sum(rest) + (float)(equal - 1) * e;
+            } else {
+                z -= e;
+            }
+        }
         if constexpr (kGroup == 32) {
             if (lane == 0) {
                 share.largest = high;
@@ -510,11 +542,15 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kTop ? 11 :
                 to = fmaxf(to, warp_ref[w]);
             }
             Sums all{to, 0.f, 0.f};
+            bool missing = true;     // the largest has not come yet
             for (int w = 0; w < kWarps; ++w) {
-                Sums x{warp_ref[w], warp_z[w], warp_s[w]};
+                const float e = kSplit ? term(unorder(warp_top[w]), warp_ref[w]) : 0.f;
+                Sums x{warp_ref[w], warp_z[w] + e, warp_s[w]};
                 x.refer(to);
-                all.z += x.z;
                 all.s += x.s;
+                const bool is = kSplit && missing && warp_top[w] == h;
+                all.z += is ? warp_z[w] * pow2(warp_ref[w] - to) : x.z;
+                missing = missing && !is;
             }
             share.largest = h;
             share.ref = all.ref;
@@ -527,7 +563,7 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kTop ? 11 :
         if (tid < a.top) share.best[tid] = 0;
         if (tid == 0) found.n = found.listed = 0;
     }
-    combine();
+    combine([&](float x, float ref) { return ex2(fmaf(x, a.scale, -ref)); });
     if constexpr (kTop) {
         const unsigned limit = lower_limit<kGroup>(mine, large, u1 - u0, a.top, found);
         constexpr int kList = Found<kGroup>::kList;
@@ -563,6 +599,7 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kTop ? 11 :
         for (int p = 0; p < split; ++p) high = max(high, peer(share.largest, p));
     }
     const float m = high == ~0u ? NAN : unorder(high);
+    const auto far_term = [&](float x) { return ex2(fmaxf((x - m) * a.scale, kGone)); };
     bool far = false;                // logits so large that a whole reference does not do
     if (fabsf(m * a.scale) > kFar && fabsf(m) < INFINITY) {
         far = true;
@@ -581,31 +618,52 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kTop ? 11 :
                 }
             }
         });
-        combine();
+        combine([&](float x, float) { return far_term(x); });
         if (split > 1) cluster_sync();
     }
     if (rank == 0) {
         Sums all{share.ref, share.z, share.s};
-        for (int p = 1; p < split; ++p) {
-            Sums x{peer(share.ref, p), peer(share.z, p), peer(share.s, p)};
-            const float to = fmaxf(all.ref, x.ref);
-            all.refer(to);
-            x.refer(to);
-            all.z += x.z;
-            all.s += x.s;
-        }
         const bool bad = !(fabsf(m) < INFINITY);
-        const float log2z = log2f(all.z);
+        const auto term = [&](float x, float ref) {
+            return far ? far_term(x) : ex2(fmaf(x, a.scale, -ref));
+        };
+        float others = 0.f, log_z;   // the other terms, to the largest's
+        if constexpr (kSplit) {
+            bool missing = share.largest != high;
+            all.z += term(unorder(share.largest), all.ref);
+            others = missing ? all.z : share.z;
+            for (int p = 1; p < split; ++p) {
+                const unsigned top = peer(share.largest, p);
+                const float ref = peer(share.ref, p), z = peer(share.z, p);
+                Sums x{ref, z + term(unorder(top), ref), peer(share.s, p)};
+                const float to = fmaxf(all.ref, ref);
+                others *= pow2(all.ref - to);
+                all.refer(to);
+                x.refer(to);
+                const bool is = missing && top == high;
+                others += is ? z * pow2(ref - to) : x.z;
+                missing = missing && !is;
+                all.z += x.z;
+                all.s += x.s;
+            }
+            others /= term(m, all.ref);
+            log_z = log1pf(others);
+        } else {
+            log_z = log2f(all.z);
+        }
         const auto log_p = [&](float x) {
+            if constexpr (kSplit) return (x - m) * a.inv_temp - log_z;
             const float t = far ? (x - m) * a.scale : fmaf(x, a.scale, -all.ref);
             // (the lowest values leave fp32 in powers of two alone)
-            return t < -1e30f ? (x - m) * a.inv_temp : kLn2 * (t - log2z);
+            return t < -1e30f ? (x - m) * a.inv_temp : kLn2 * (t - log_z);
         };
         if (tid == 0) {
             a.logp[r] = bad || target >= a.vocab ? NAN : log_p(row.at((int)target));
-            if (a.entropy) a.entropy[r] = bad ? NAN : kLn2 * (log2z - all.s / all.z);
+            if (a.entropy) a.entropy[r] = bad ? NAN : kLn2 * (log2f(all.z) - all.s / all.z);
             if (a.stats) {
-                const float z = far ? all.z : all.z * exp2f(-fmaf(m, a.scale, -all.ref));
+                const float z = kSplit ? 1.f + others
+                                : far  ? all.z
+                                       : all.z * exp2f(-fmaf(m, a.scale, -all.ref));
                 a.stats[r] = bad ? make_float2(NAN, NAN) : make_float2(m, z);
             }
         }
@@ -831,9 +889,11 @@ Shape shape_of(const ScoresArgs &a, int sm_count, int cta, int ctas_per_sm) {
 
 template <bool kBf16, bool kTop>
 cudaError_t launch_scores(const ScoresArgs &a, const Shape &s, cudaStream_t stream) {
-    return s.group == 32
-               ? launch(token_scores_kernel<kBf16, kTop, 32>, a, 32, 1, false, stream)
-               : launch(token_scores_kernel<kBf16, kTop, 128>, a, 128, s.split, true, stream);
+    if (s.group == 32)
+        return launch(token_scores_kernel<kBf16, kTop, 32, false>, a, 32, 1, false, stream);
+    return s.split > 1
+               ? launch(token_scores_kernel<kBf16, kTop, 128, true>, a, 128, s.split, true, stream)
+               : launch(token_scores_kernel<kBf16, kTop, 128, false>, a, 128, 1, true, stream);
 }
 template <bool kBf16>
 cudaError_t launch_grad(const ScoresArgs &a, const Shape &s, cudaStream_t stream) {

@@ -111,6 +111,29 @@ def test_vocabularies(v, dtype):
     _check_grad(x, t, min(5, v), seed=v + 1)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,v", [(1, 32000), (3, 9000), (40, 30011), (300, 128256), (2000, 513), (1300, 50257)])
+def test_tokens_that_are_nearly_certain(rows, v, dtype):
+    """log p = -log(1 + r) of the largest has r's own relative error, that of the other
+    terms' sum, and the logarithm's; where rows are many also that of at most 60 additions
+    behind the largest term and four roundings more, 2^-25 of it each."""
+    x = 2 * torch.randn(rows, v, generator=_gen(rows), device="cuda")
+    t = torch.randint(0, v, (rows,), generator=_gen(1), device="cuda")
+    x.scatter_(1, t[:, None], -INF)
+    by = torch.tensor([0.5, 3.0, 8.0, 14.0], device="cuda")[torch.arange(rows, device="cuda") % 4]
+    x = x.scatter(1, t[:, None], (torch.logsumexp(x.double(), 1) + by).float()[:, None]).to(dtype)
+    r = A.token_scores(x, t, top=2)
+    y = x.double()
+    d = y - y.gather(1, t[:, None])
+    d.scatter_(1, t[:, None], -INF)
+    want = -torch.log1p(d.exp().sum(1))
+    more = 64 * 2.0**-25 if rows > 1200 else 0.0
+    assert ((r.logp - want).abs() <= 1e-5 * want.abs() + more).all()
+    assert torch.equal(r.top_logp[:, 0], r.logp) or (r.top_ids[:, 0] != t).any()
+    # stats: the same sum, times the largest's term
+    assert ((r.stats[:, 1] - want.neg().exp()).abs() <= 1e-5 * want.neg().exp()).all()
+
+
 @pytest.mark.parametrize("rows", [1, 2, 37, 300, 1300])
 @pytest.mark.parametrize("v,dtype", [(9001, BF16), (20011, F32), (129, BF16)])
 def test_row_counts(rows, v, dtype):
