@@ -356,7 +356,8 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     const uint32_t asked = bars + 8 * (2 * kSlots + 5 + 2 * kRing);
     const auto work_at = [&](int s) { return ((asked + 8 + 15) & ~15u) + 32 * s; };
     __shared__ uint32_t s_tmem;
-    __shared__ volatile int s_abort;
+    __shared__ volatile int s_abort;             // a wait of this CTA's, or its pair's, ran out
+    __shared__ volatile int s_issued[2 * kCtas]; // slots that the copying threads have filled
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = kCtas == 1 ? 0 : cluster_rank();
@@ -394,6 +395,17 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     grid_go();
     grid_wait();
 
+    // (to both CTAs of a pair)
+    const auto tell_pair = [&](volatile int *at, int v) {
+        *at = v;
+        if constexpr (kCtas == 2)
+            asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(
+                             cluster_addr(smem_addr(const_cast<int *>(at)), rank ^ 1)),
+                         "r"(v)
+                         : "memory");
+    };
+    const auto give_up = [&] { tell_pair(&s_abort, 1); };
+
     // The next tile, as all but the thread that takes it hear of it.
     int ring = 0;
     uint32_t ring_phase = 0;
@@ -412,6 +424,8 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                          : "=r"(f.col), "=r"(f.given_up), "=r"(f.part), "=r"(f.unused)
                          : "r"(work_at(ring) + 16)
                          : "memory");
+        } else {
+            give_up();
         }
         if (whole_warp) __syncwarp();
         if (!whole_warp || lane == 0) {
@@ -445,9 +459,12 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             f.op = -1;
             if (next < tiles) {
                 f = finder.find(args, next, kTile);
-                if (s_abort || !wait_done(done_of(f), f.before * kSignals, &s_abort)) s_abort = 1;
+                if (s_abort || !wait_done(done_of(f), f.before * kSignals, &s_abort)) give_up();
             }
-            if (!mbar_wait_cluster(heard(ring), ring_phase ^ 1)) break;
+            if (!mbar_wait_cluster(heard(ring), ring_phase ^ 1)) {
+                give_up();
+                break;
+            }
             for (int p = 0; p < kCtas; ++p) {
                 const uint32_t at = kCtas == 1 ? work_at(ring) : cluster_addr(work_at(ring), p);
                 asm volatile("st.shared::cluster.v4.s32 [%0], {%1, %2, %3, %4};" ::"r"(at),
@@ -464,7 +481,10 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                              : "memory");
             on();
             if (f.op < 0) break;
-            if (!mbar_wait_cluster(asked, asked_phase)) break;
+            if (!mbar_wait_cluster(asked, asked_phase)) {
+                give_up();
+                break;
+            }
             asked_phase ^= 1;
         }
     } else if ((warp == 0 || warp == 3) && lane == 0) {
@@ -509,12 +529,9 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                 ++issued;
                 if (++slot == kSlots) slot = 0, phase ^= 1;
             }
-            if (!ok) s_abort = 1;
+            if (!ok) give_up();
         }
-        if ((!ok || s_abort) && leads)
-            // copies in flight land before the block ends (each slot's last use)
-            for (int i = issued > kSlots ? issued - kSlots : 0; i < issued; ++i)
-                mbar_wait(full(i % kSlots), (i / kSlots) & 1, nullptr);
+        tell_pair(&s_issued[2 * rank + is_b], issued);
     } else if (warp == 1 && lane == 0 && rank == 0) {
         int slot = 0, acc = 0;
         uint32_t phase = 0, acc_phase = 0;
@@ -553,14 +570,9 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             if (ok)
                 product_commit<kCtas>(acc_full(acc));
             else
-                s_abort = 1;
+                give_up();
             if (acc) acc_phase ^= 1;
             acc ^= 1;
-        }
-        if (!ok) {
-            // products in flight end before their accumulators are given back
-            product_commit<kCtas>(drained);
-            mbar_wait(drained, 0, nullptr);
         }
     } else if (warp >= kEpilogueWarp) {
         // a warp reads its quarter of the lanes, and half of the columns
@@ -638,7 +650,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             }
             if (ok) ok = mbar_wait(acc_full(acc), acc_phase, &s_abort);
             ok = __all_sync(~0u, ok);
-            if (!ok) s_abort = 1;
+            if (!ok) give_up();
             tc_fence_after();
             // the accumulator goes back when the last block has been read
             const auto release = [&] {
@@ -890,6 +902,40 @@ __global__ void __launch_bounds__(kProductThreads, 1)
     __syncthreads();
     if constexpr (kCtas == 2) cluster_sync();
     tc_fence_after();
+    if (s_abort) {
+        // All threads of the pair are behind their loops here, wherever each of them gave
+        // up: what is in flight lands before shared memory and accumulators go back.
+        if ((warp == 0 || warp == 3) && lane == 0) {
+            const bool is_b = warp == 3, leads = rank == 0 && !is_b;
+            const uint32_t bar0 = kCtas == 1 ? full(0) : cluster_addr(full(0), 0);
+            const int issued = s_issued[2 * rank + is_b];
+            // A slot that not all copying threads have filled is free in both CTAs (one of
+            // them has seen that): the others fill it too, so that it completes.
+            const auto fill = [&](int i) {
+                const uint32_t at = smem + i % kSlots * kSlotBytes + (is_b ? 2 * kBoxBytes : 0);
+                for (int k = 0; k < 2; ++k)
+                    tensor_load<kCtas>(at + k * kBoxBytes, &args.map[kMapX0][0], 0, 0, 0,
+                                       bar0 + 8 * (i % kSlots));
+            };
+            // (what the testing hook left out)
+            if (blockIdx.x == 0 && args.test_stall1 > 0 && args.test_stall1 <= issued)
+                fill((int)args.test_stall1 - 1);
+            int last = 0;
+            for (int k = 0; k < 2 * kCtas; ++k) last = max(last, s_issued[k]);
+            for (int i = issued; i < last; ++i) {
+                if (leads) mbar_arrive_expect_tx(full(i % kSlots), kCtas * kSlotBytes);
+                fill(i);
+            }
+            if (leads)               // each slot's last use
+                for (int i = max(0, last - kSlots); i < last; ++i)
+                    mbar_wait(full(i % kSlots), (i / kSlots) & 1, nullptr);
+        } else if (warp == 1 && lane == 0 && rank == 0) {
+            product_commit<kCtas>(drained);
+            mbar_wait(drained, 0, nullptr);
+        }
+        __syncthreads();
+        if constexpr (kCtas == 2) cluster_sync();
+    }
     if (warp == 2) tmem_free<kCtas>(tmem, 2 * kTile);
 }
 
