@@ -534,7 +534,8 @@ int aloco_adamw_step_normed(void *const *params, const void *const *grads,
  * allocate nothing on the device; results are bit-identical from call to call.
  * Scratch is the caller's device memory, 256-byte aligned and not set up in any
  * way: calls that may overlap on the GPU need their own.  Every wait inside the
- * kernels is bounded (about 2 s); one that runs out leaves NaN in the matrix.
+ * kernels is bounded (2 s, of what waits for such a wait 4 s); one that runs out
+ * leaves NaN in the matrices that its block was at.  What is not NaN is right.
  * ---------------------------------------------------------------------- */
 
 #define ALOCO_MAX_NS_STEPS 16

@@ -144,7 +144,7 @@ void lay_out(const Plan &plan, Pass *pass) {
             break;
         }
     }
-    pass->counters = 1;
+    pass->counters = kOrthoCounters;
     pass->all_bytes = pass->bytes;
     for (size_t i = 0; i < pass->parts.size(); ++i) {
         const Part &part = pass->parts[i];
@@ -367,7 +367,7 @@ int run_pass(const Plan &plan, const Pass &pass, const OrthoArgs &base, const do
     int places = 0, norm = 0, prep = 0;
     a.counters = (int)pass.counters;
     a.next_tile = (int *)take(pass.counters * 4);
-    int *counter = a.next_tile + 1;
+    int *counter = a.next_tile + kOrthoCounters;
     const int tile = ortho_pair_tile() / 2 * pass.ctas;
     for (int i = 0; i < a.n_groups; ++i) {
         const Part &part = pass.parts[i];

@@ -38,7 +38,7 @@ struct Work {
     int row, col;                    // in tiles
     union {
         int before;                  // tiles of the matrix that have to be done
-        int given_up;                // as it is told: they were not
+        int given_up;                // as it is told: they never were
     };
     int part;                        // of the depth
     int unused;
@@ -279,20 +279,25 @@ __device__ __forceinline__ void store_values(const Result &to, int y, int x, int
 }
 
 // Where tiles that a matrix's next products take are done with: what `count` warps
-// have written is seen by whoever finds them counted.
+// have written is seen by whoever finds them counted.  A matrix of which a tile was
+// given up has kLost there, which no count reaches: a count says how much is done, not
+// what, so that tiles without their operands must not make up for others.
+constexpr int kLost = 1 << 30;
 __device__ __forceinline__ int load_acquire(const int *p) {
     int v;
     asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
     return v;
 }
 __device__ __forceinline__ bool wait_done(const int *done, int count, const volatile int *abort) {
-    if (load_acquire(done) >= count) return true;
-    const long long t0 = clock64();
-    while (load_acquire(done) < count) {
-        if (*abort || clock64() - t0 > kTmaWaitCycles) return false;
-        __nanosleep(64);
+    int is = load_acquire(done);
+    if (is < count) {
+        const long long t0 = clock64();
+        while ((is = load_acquire(done)) < count) {
+            if (*abort || clock64() - t0 > kTmaWaitCycles) return false;
+            __nanosleep(64);
+        }
     }
-    return true;
+    return is < kLost;
 }
 __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity) {
     const long long t0 = clock64();
@@ -333,8 +338,10 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity)
 // workers, 663 of 641 for 48 x 768 x 768 and 2.48 of 2.25 ms for 16 x 2048 x 2048: a
 // matrix waits for itself alone.
 //
-// A wait that runs out ends the waits of its CTA; its tiles are NaN from there on,
-// and with them their matrices.
+// A wait that runs out ends the waits of its pair.  The tiles that the pair knows of
+// become NaN, and their matrices are marked: whoever takes another tile of one does
+// the same, without a wait.  The pair takes no more tiles, unless all pairs have given
+// up: then the last of them makes NaN of what is left, so that nothing stays unwritten.
 template <int kCtas, bool kOutBf16, bool kParts>
 __global__ void __launch_bounds__(kProductThreads, 1)
     ortho_chain_kernel(const __grid_constant__ OrthoArgs args) {
@@ -453,13 +460,18 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         // Takes tiles, and tells of one when all that it needs is there.
         Finder finder;
         uint32_t asked_phase = 0;
+        bool counted = false, last = false;
         for (;;) {
-            const int next = atomicAdd(args.next_tile, 1);
+            if (s_abort && !counted) {
+                counted = true;
+                last = atomicAdd(args.next_tile + 1, 1) + 1 == (int)gridDim.x / kCtas;
+            }
+            const int next = counted && !last ? tiles : atomicAdd(args.next_tile, 1);
             Work f;
             f.op = -1;
             if (next < tiles) {
                 f = finder.find(args, next, kTile);
-                if (s_abort || !wait_done(done_of(f), f.before * kSignals, &s_abort)) give_up();
+                f.given_up = s_abort || !wait_done(done_of(f), f.before * kSignals, &s_abort);
             }
             if (!mbar_wait_cluster(heard(ring), ring_phase ^ 1)) {
                 give_up();
@@ -471,7 +483,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                              "r"(f.op), "r"(f.group), "r"(f.matrix), "r"(f.row)
                              : "memory");
                 asm volatile("st.shared::cluster.v4.s32 [%0], {%1, %2, %3, %4};" ::"r"(at + 16),
-                             "r"(f.col), "r"(s_abort), "r"(f.part), "r"(0)
+                             "r"(f.col), "r"(f.given_up), "r"(f.part), "r"(0)
                              : "memory");
             }
             mbar_arrive(told(ring));
@@ -498,11 +510,15 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         for (;;) {
             const Work f = hear(false);
             if (f.op < 0) break;
+            if (f.given_up) {
+                if (leads) mbar_arrive(asked);
+                continue;
+            }
             const OrthoOp &op = op_of(args, f);
             int begin;
             const int end = depth_of(f, op, &begin);
             const int ask = begin + max(0, (end - begin - 1) / kK + 1 - kAsk) * kK;
-            ok = ok && !f.given_up && !s_abort;
+            ok = ok && !s_abort;
             // operands were written by ordinary stores
             asm volatile("fence.proxy.async;" ::: "memory");
             const bool x = op.what == kGram || (op.what == kUpdate && is_b);
@@ -539,6 +555,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         for (;;) {
             const Work f = hear(false);
             if (f.op < 0) break;
+            if (f.given_up) continue;
             const OrthoOp &op = op_of(args, f);
             int begin;
             const int end = depth_of(f, op, &begin);
@@ -632,7 +649,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                         fetch_l2(to.address(y * to.stride + x + j));
                 }
             }
-            bool ok = !s_abort;
+            bool ok = !s_abort && !f.given_up;
             if (op.what != kGram && some) {
                 if (r < m) {
                     by_row = __ldcg(g.diag[op.left] + row0 + r);
@@ -650,10 +667,12 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             }
             if (ok) ok = mbar_wait(acc_full(acc), acc_phase, &s_abort);
             ok = __all_sync(~0u, ok);
-            if (!ok) give_up();
+            if (!ok && !f.given_up) give_up();
             tc_fence_after();
-            // the accumulator goes back when the last block has been read
+            // the accumulator goes back when the last block has been read (a tile that was
+            // given up has none)
             const auto release = [&] {
+                if (f.given_up) return;
                 tc_fence_before();
                 __syncwarp();
                 if (lane) return;
@@ -885,6 +904,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                                 g.n - c0);
                 }
             }
+            if (!ok && lane == 0) atomicMax(done_of(f), kLost);
             if (!op.last && finished) {
                 // done: what this warp has written is seen behind the count (by tensor
                 // copies behind a fence of theirs)
@@ -894,6 +914,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
                                  "r"(finished)
                                  : "memory");
             }
+            if (f.given_up) continue;
             if (acc) acc_phase ^= 1;
             acc ^= 1;
         }

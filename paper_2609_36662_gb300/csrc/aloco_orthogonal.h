@@ -69,6 +69,7 @@ struct OrthoGroup {
 // What fits a CTA of launch_ortho_small: rows of X, and columns of it.
 constexpr int kOrthoSmallSide = 128, kOrthoSmallCols = 256, kOrthoSmallCtas = 16;
 
+constexpr int kOrthoCounters = 2;    // of a pass, ahead of its matrices' (OrthoArgs::next_tile)
 constexpr int kOrthoGroups = 16;     // groups of a pass
 constexpr int kOrthoMatrices = 1024; // places of a pass (a worker's)
 
@@ -95,8 +96,9 @@ struct OrthoArgs {
     float coef[ALOCO_MAX_NS_STEPS][3];     // the steps' coefficients
     int steps;
     int small_ctas;                  // launch_ortho_small: the CTAs of a matrix
-    int *next_tile;                  // the next tile to take, `done` and `came`: zero
-    int counters;                    // when the products begin, so many
+    int *next_tile;                  // the next tile to take, how many pairs have given
+    int counters;                    // up, `done` and `came`: zero when the products
+                                     // begin, so many
     double eps;
     // where the matrices come from and go to
     int source;

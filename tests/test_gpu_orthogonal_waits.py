@@ -33,3 +33,22 @@ def test_copies_in_flight_land_before_their_block_ends(shape, slot):
     torch.cuda.synchronize()
     assert out.isnan().any()
     assert all(torch.equal(a, want) for a in after)
+
+
+@pytest.mark.parametrize("shape,slot,lost", [((3, 140, 500), 1, 3), ((20, 200, 300), 0, 8),
+                                             ((40, 400, 520), 2, 8), ((1, 300, 6000), 2, 1),
+                                             ((3, 40, 200), 0, 1), ((3, 40, 900), 0, 1)],
+                         ids=["few", "single", "pairs", "parts", "small", "small_cluster"])
+def test_what_is_not_nan_is_right(shape, slot, lost):
+    """The matrices of the tiles that the block knew of are lost, in part or as a whole;
+    no other is, and no element is a number that comes of operands that were not there.
+    (A block knows of at most eight tiles: four in its ring, two whose products are not
+    done, and two that its threads have in hand.)"""
+    x = _batch(shape)
+    want = A.orthogonalize(x)
+    A.test_stall_tile(slot)
+    out = A.orthogonalize(x)
+    torch.cuda.synchronize()
+    nan = out.isnan()
+    assert torch.equal(torch.where(nan, 0, out), torch.where(nan, 0, want))
+    assert 1 <= int(nan.flatten(1).any(1).sum()) <= lost
