@@ -719,6 +719,7 @@ int aloco_preference_loss(const aloco_tokens_t *tokens, const float *ref_logp,
  * no part and are not read: 0, and -1 as ids):
  *   logp       log p[a]
  *   entropy    H = -sum_j p_j log p_j  (terms with p_j = 0 are 0)
+ *              (no log-probability is above 0 and no entropy below)
  *   top_ids    the `top` largest logits' indices, largest first, equal ones by
  *              their index; [batch * rows, top] int32
  *   top_logp   their log-probabilities (-inf where the logit is)

@@ -19,6 +19,7 @@ constexpr float kLn2 = 0.693147180559945f;
 // references are powers of two and no rounding is common to a row's terms.
 constexpr float kFar = 1048576.f;    // 2^20
 constexpr float kGone = -200.f;      // 2^-200 is 0 in fp32
+constexpr float kCertain = 0.0625f;  // the other terms' share beside a nearly certain token
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -192,7 +193,8 @@ __device__ __forceinline__ float warp_sum(float x) {
 // One CTA's share of a row, as the others of its cluster read it.
 struct Share {
     unsigned largest;
-    float ref, z, s;                 // z: without the largest's term, where rows are split
+    float ref, z, s;
+    int owner;                       // the thread that read the row's largest value
     unsigned long long best[ALOCO_MAX_TOP];  // (order, ~index), largest first; 0: none
 };
 
@@ -422,11 +424,13 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kSplit ? 8 
     const int group = G::index();
     Share &share = shares[group];
     Found<kGroup> &found = founds[kTop ? group : 0];
-    const int64_t r = kGroup == 32 ? (int64_t)blockIdx.x * kGroups + group : blockIdx.x / split;
+    const int r = kGroup == 32 ? (int)blockIdx.x * kGroups + group : (int)blockIdx.x / split;
     const int rank = split > 1 ? (int)(blockIdx.x % split) : 0;
     const int tid = G::thread(), lane = tid % 32, warp = tid / 32;
     if (r >= a.n) return;
-    const int64_t target = load_index(a.target, a.target_bytes, r);
+    // (in 32 bits, as r is: with either in 64 the loop's values spill)
+    const int target = (int)max((int64_t)-1, min(load_index(a.target, a.target_bytes, r),
+                                                 (int64_t)a.vocab));
     if (target < 0) {
         if (rank) return;
         if (tid == 0) {
@@ -435,8 +439,8 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kSplit ? 8 
             if (a.stats) a.stats[r] = make_float2(0.f, 0.f);
         }
         if (kTop && tid < a.top) {
-            a.top_ids[r * a.top + tid] = -1;
-            a.top_logp[r * a.top + tid] = 0.f;
+            a.top_ids[(int64_t)r * a.top + tid] = -1;
+            a.top_logp[(int64_t)r * a.top + tid] = 0.f;
         }
         return;
     }
@@ -479,42 +483,13 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kSplit ? 8 
         sums.s += s.x + s.y;
     });
 
-    // The group's, then the cluster's.  The largest value's term stays beside the sum:
-    // the log-probability of a token that is nearly certain is what the other terms are
-    // to it, which a sum with it would round away.  Where it is a quarter of a warp's sum
-    // the warp takes the units of the thread that had it again, without it.  (Where rows
-    // are few.  Where they are many the sum is of all terms: what follows a row is not
-    // hidden then, and 8184 x 32000 bf16, a quarter left out, took 88 us in place of 80.)
+    // The group's.
     const unsigned mine = nan ? ~0u : order(large.first);
-    const auto combine = [&](auto term) {        // term: of a value, to a reference
+    const auto combine = [&] {
         const unsigned high = __reduce_max_sync(~0u, mine);
         const int ref = __reduce_max_sync(~0u, (int)fminf(sums.ref, 2.f * kFar));
         sums.refer((float)ref);
-        const float s = warp_sum(sums.s);
-        float z = warp_sum(sums.z);
-        if constexpr (kSplit) {
-            const float top = unorder(high), e = term(top, (float)ref);
-            if (4.f * e > z) {
-                const int owner = __ffs(__ballot_sync(~0u, mine == high)) - 1;
-                float rest = lane == owner ? 0.f : sums.z;
-                int equal = 0;
-                for (int u = u0 + tid - lane + owner + lane * kGroup; u < u1; u += 32 * kGroup) {
-                    float v[N];
-                    Row<kBf16>::values(row.load(u, u1), v);
-#pragma unroll
-                    for (int i = 0; i < N; ++i) {
-                        if (v[i] == top)
-                            ++equal;
-                        else
-                            rest += term(v[i], (float)ref);
-                    }
-                }
-                equal = __reduce_add_sync(~0u, equal);
-                z = warp_sum(rest) + (float)(equal - 1) * e;
-            } else {
-                z -= e;
-            }
-        }
+        const float z = warp_sum(sums.z), s = warp_sum(sums.s);
         if constexpr (kGroup == 32) {
             if (lane == 0) {
                 share.largest = high;
@@ -542,15 +517,11 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kSplit ? 8 
                 to = fmaxf(to, warp_ref[w]);
             }
             Sums all{to, 0.f, 0.f};
-            bool missing = true;     // the largest has not come yet
             for (int w = 0; w < kWarps; ++w) {
-                const float e = kSplit ? term(unorder(warp_top[w]), warp_ref[w]) : 0.f;
-                Sums x{warp_ref[w], warp_z[w] + e, warp_s[w]};
+                Sums x{warp_ref[w], warp_z[w], warp_s[w]};
                 x.refer(to);
+                all.z += x.z;
                 all.s += x.s;
-                const bool is = kSplit && missing && warp_top[w] == h;
-                all.z += is ? warp_z[w] * pow2(warp_ref[w] - to) : x.z;
-                missing = missing && !is;
             }
             share.largest = h;
             share.ref = all.ref;
@@ -563,7 +534,7 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kSplit ? 8 
         if (tid < a.top) share.best[tid] = 0;
         if (tid == 0) found.n = found.listed = 0;
     }
-    combine([&](float x, float ref) { return ex2(fmaf(x, a.scale, -ref)); });
+    combine();
     if constexpr (kTop) {
         const unsigned limit = lower_limit<kGroup>(mine, large, u1 - u0, a.top, found);
         constexpr int kList = Found<kGroup>::kList;
@@ -594,16 +565,25 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kSplit ? 8 
         G::sync();
     }
     unsigned high = share.largest;
-    if (split > 1) {
+    if constexpr (kSplit) {
         cluster_sync();
         for (int p = 0; p < split; ++p) high = max(high, peer(share.largest, p));
     }
     const float m = high == ~0u ? NAN : unorder(high);
-    const auto far_term = [&](float x) { return ex2(fmaxf((x - m) * a.scale, kGone)); };
-    bool far = false;                // logits so large that a whole reference does not do
-    if (fabsf(m * a.scale) > kFar && fabsf(m) < INFINITY) {
-        far = true;
-        if (split > 1) cluster_sync();  // (all have read)
+    const bool bad = !(fabsf(m) < INFINITY);
+    // logits so large that a whole reference does not do
+    const bool far = !bad && fabsf(m * a.scale) > kFar;
+    // a power and its term; (values that are -inf at 2^-200, which is 0)
+    const auto power = [&](float x, float ref) {
+        return far ? fmaxf((x - m) * a.scale, kGone) : fmaf(fmaxf(x, -0x1p96f), a.scale, -ref);
+    };
+    const auto share_again = [&] {
+        __syncwarp();
+        if constexpr (kSplit) cluster_sync();  // (all have read)
+        combine();
+        if constexpr (kSplit) cluster_sync();
+    };
+    if (far) {
         sums = {0.f, 0.f, 0.f};
         pass([&](const uint4 (&q)[kBatch], int, int) {
 #pragma unroll
@@ -618,85 +598,93 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kSplit ? 8 
                 }
             }
         });
-        combine([&](float x, float) { return far_term(x); });
-        if (split > 1) cluster_sync();
+        share_again();
     }
-    if (rank == 0) {
-        Sums all{share.ref, share.z, share.s};
-        const bool bad = !(fabsf(m) < INFINITY);
-        const auto term = [&](float x, float ref) {
-            return far ? far_term(x) : ex2(fmaf(x, a.scale, -ref));
-        };
-        float others = 0.f, log_z;   // the other terms, to the largest's
-        if constexpr (kSplit) {
-            bool missing = share.largest != high;
-            all.z += term(unorder(share.largest), all.ref);
-            others = missing ? all.z : share.z;
-            for (int p = 1; p < split; ++p) {
-                const unsigned top = peer(share.largest, p);
-                const float ref = peer(share.ref, p), z = peer(share.z, p);
-                Sums x{ref, z + term(unorder(top), ref), peer(share.s, p)};
-                const float to = fmaxf(all.ref, ref);
-                others *= pow2(all.ref - to);
-                all.refer(to);
-                x.refer(to);
-                const bool is = missing && top == high;
-                others += is ? z * pow2(ref - to) : x.z;
-                missing = missing && !is;
-                all.z += x.z;
-                all.s += x.s;
-            }
-            others /= term(m, all.ref);
-            log_z = log1pf(others);
-        } else {
-            log_z = log2f(all.z);
+    // All CTAs' sums, the same in every thread of them.
+    const auto total = [&] {
+        if constexpr (!kSplit) return Sums{share.ref, share.z, share.s};
+        Sums all{peer(share.ref, 0), peer(share.z, 0), peer(share.s, 0)};
+        for (int p = 1; p < split; ++p) {
+            Sums x{peer(share.ref, p), peer(share.z, p), peer(share.s, p)};
+            const float to = fmaxf(all.ref, x.ref);
+            all.refer(to);
+            x.refer(to);
+            all.z += x.z;
+            all.s += x.s;
         }
-        const auto log_p = [&](float x) {
-            if constexpr (kSplit) return (x - m) * a.inv_temp - log_z;
-            const float t = far ? (x - m) * a.scale : fmaf(x, a.scale, -all.ref);
-            // (the lowest values leave fp32 in powers of two alone)
-            return t < -1e30f ? (x - m) * a.inv_temp : kLn2 * (t - log_z);
-        };
-        if (tid == 0) {
-            a.logp[r] = bad || target >= a.vocab ? NAN : log_p(row.at((int)target));
-            if (a.entropy) a.entropy[r] = bad ? NAN : kLn2 * (log2f(all.z) - all.s / all.z);
-            if (a.stats) {
-                const float z = kSplit ? 1.f + others
-                                : far  ? all.z
-                                       : all.z * exp2f(-fmaf(m, a.scale, -all.ref));
-                a.stats[r] = bad ? make_float2(NAN, NAN) : make_float2(m, z);
+        return all;
+    };
+    // The log-probability of the largest is -log(1 + r), r the other terms to it, and the
+    // entropy log(1 + r) and what the others' powers lie below its own: of parts that
+    // are not below 0, so that neither has the wrong sign where one token has all.
+    Sums others = total();           // but for the largest's term, presently
+    const float t_m = power(m, others.ref), e_m = ex2(t_m);
+    if (kSplit && !bad && others.z - e_m < kCertain * others.z) {
+        // Of a token that is nearly certain r is what a sum with its term has rounded away:
+        // the units of the thread that had it are taken again without it.
+        sums.refer(others.ref);
+        if (mine == high) {
+            share.owner = tid;
+            sums.z = sums.s = 0.f;
+        }
+        G::sync();
+        if (share.largest == high) {
+            for (int u = u0 + share.owner + tid * kGroup; u < u1; u += kGroup * kGroup) {
+                float v[N];
+                Row<kBf16>::values(row.load(u, u1), v);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float t = power(v[i], others.ref), e = v[i] == m ? 0.f : ex2(t);
+                    sums.z += e;
+                    sums.s = fmaf(t, e, sums.s);
+                }
             }
+        }
+        share_again();
+        others = total();
+    } else {
+        others.z -= e_m;
+        others.s -= __fmul_rn(t_m, e_m);  // (as it was added: one value alone leaves 0)
+    }
+    // (of a row of one CTA the first warp does the rest)
+    if (!kSplit && warp) return;
+    if (rank == 0) {
+        if constexpr (kTop && kSplit) {
+            for (int i = tid; i < split * a.top; i += kGroup)
+                found.value[i] = peer(share.best[i % a.top], i / a.top);
+            __syncthreads();
+        }
+        // sum (t_j - t_m) 2^t_j over the others, which is not above 0
+        const float below = fminf(fmaf(-t_m, others.z, others.s), 0.f);
+        const float to_m = others.z / e_m, log_z = log1pf(to_m);
+        const auto log_p = [&](float x) { return fmaf(x - m, a.inv_temp, -log_z); };
+        if (tid == 0) {
+            a.logp[r] = bad || target >= a.vocab ? NAN : log_p(row.at(target));
+            if (a.entropy)
+                a.entropy[r] = bad ? NAN : fmaf(-kLn2, below / (others.z + e_m), log_z);
+            if (a.stats) a.stats[r] = bad ? make_float2(NAN, NAN) : make_float2(m, 1.f + to_m);
         }
         if constexpr (kTop) {
-            // an entry's place among all CTAs' is the number of larger ones
-            const int n = split * a.top;
-            if (split > 1) {
-                for (int i = tid; i < n; i += kGroup)
-                    found.value[i] = peer(share.best[i % a.top], i / a.top);
-                __syncthreads();
-            }
+            const int n = bad ? a.top : split * a.top;
             for (int i = tid; i < n; i += kGroup) {
-                const unsigned long long v = split == 1 ? share.best[i] : found.value[i];
+                // an entry's place among all CTAs' is the number of larger ones (a row with
+                // NaN may have fewer)
+                unsigned long long v = 0;
                 int place = i;
-                if (split > 1) {
-                    place = 0;
-                    for (int o = 0; o < n; ++o) place += found.value[o] > v;
+                if (!bad) {
+                    v = kSplit ? found.value[i] : share.best[i];
+                    if constexpr (kSplit) {
+                        place = 0;
+                        for (int o = 0; o < n; ++o) place += found.value[o] > v;
+                    }
+                    if (!v || place >= a.top) continue;
                 }
-                if (v && place < a.top) {
-                    a.top_ids[r * a.top + place] = bad ? -1 : (int)~(unsigned)v;
-                    a.top_logp[r * a.top + place] =
-                        bad ? NAN : log_p(unorder((unsigned)(v >> 32)));
-                }
-            }
-            if (bad) G::sync();
-            // (a row with NaN may have filled fewer)
-            if (bad && tid < a.top) {
-                a.top_ids[r * a.top + tid] = -1;
-                a.top_logp[r * a.top + tid] = NAN;
+                a.top_ids[(int64_t)r * a.top + place] = bad ? -1 : (int)~(unsigned)v;
+                a.top_logp[(int64_t)r * a.top + place] = bad ? NAN : log_p(unorder((unsigned)(v >> 32)));
             }
         }
     }
-    if (split > 1) cluster_sync();   // nobody leaves while it is read
+    if constexpr (kSplit) cluster_sync();  // nobody leaves while it is read
 }
 
 // ------------------------------------------------------------------ gradient
