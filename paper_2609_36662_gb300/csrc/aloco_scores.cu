@@ -619,9 +619,11 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kSplit ? 8 
     // are not below 0, so that neither has the wrong sign where one token has all.
     Sums others = total();           // but for the largest's term, presently
     const float t_m = power(m, others.ref), e_m = ex2(t_m);
-    if (kSplit && !bad && others.z - e_m < kCertain * others.z) {
+    if (!bad && others.z - e_m < kCertain * others.z) {
         // Of a token that is nearly certain r is what a sum with its term has rounded away:
-        // the units of the thread that had it are taken again without it.
+        // the units of the thread that had it are taken again without it.  (8 x 1023 x 32000
+        // bf16, of which 12 % are such rows: 80.0 us, 78.1 with the sum of all; 81.1 where
+        // the limit is an eighth.)
         sums.refer(others.ref);
         if (mine == high) {
             share.owner = tid;

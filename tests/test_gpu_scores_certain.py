@@ -65,7 +65,8 @@ def _small(x, t):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
-@pytest.mark.parametrize("rows,v", [(1, 32000), (300, 32000), (300, 128256)])
+@pytest.mark.parametrize("rows,v", [(1, 32000), (300, 32000), (300, 128256), (300, 700),
+                                    (2000, 900), (1300, 32000), (1300, 20011)])
 def test_small_values_keep_their_digits(rows, v, dtype):
     """Where the others are a sixteenth of the sum at most they are summed without the
     largest: 9e-6 of them (see test_gpu_scores), and in the entropy 2^-22 more for the
@@ -76,4 +77,20 @@ def test_small_values_keep_their_digits(rows, v, dtype):
     small = (logp < 0.06) & (logp > 1e-30)
     assert ((-r.logp - logp).abs() <= 1e-5 * logp)[small].all()
     assert ((r.entropy - h).abs() <= 1e-5 * h)[small].all()
-    assert ((r.stats[:, 1] - logp.exp()).abs() <= 1e-5 * logp.exp()).all()
+    # (to the largest logit, which is another where the token is behind it)
+    z = (x.double() - x.double().amax(1, keepdim=True)).exp().sum(1)
+    assert ((r.stats[:, 1] - z).abs() <= 1e-5 * z).all()
+
+
+def test_digits_do_not_depend_on_the_rows_beside():
+    """A row alone, and among a thousand others: both within 1e-5 of its definition."""
+    x, t = _certain(1300, 32000, BF16)
+    among = A.token_scores(x, t)
+    for i in range(0, 1300, 100):
+        one = A.token_scores(x[i:i + 1], t[i:i + 1])
+        logp, h = _small(x[i:i + 1], t[i:i + 1])
+        if not 1e-30 < float(logp) < 0.06:
+            continue
+        for r, k in ((one, 0), (among, i)):
+            assert abs(float(r.logp[k]) + float(logp)) <= 1e-5 * float(logp)
+            assert abs(float(r.entropy[k]) - float(h)) <= 1e-5 * float(h)
