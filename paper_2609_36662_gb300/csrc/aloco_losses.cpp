@@ -98,7 +98,9 @@ void take_scores(const aloco_tokens_t *t, const LogitsArgs &a, int top, ScoresAr
     s->bf16 = t->dtype == ALOCO_BF16;
     s->target = a.target;
     s->target_bytes = a.target_bytes;
-    s->scale = (float)(1.4426950408889634 / t->temperature);
+    const double scale = 1.4426950408889634 / t->temperature;
+    s->scale = (float)scale;
+    s->tilt = (float)(0.6931471805599453 * (scale / (double)s->scale - 1.0));
     s->inv_temp = a.inv_temp;
     s->top = top;
 }

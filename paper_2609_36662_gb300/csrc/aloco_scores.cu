@@ -658,7 +658,11 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kSplit ? 8 
         }
         // sum (t_j - t_m) 2^t_j over the others, which is not above 0
         const float below = fminf(fmaf(-t_m, others.z, others.s), 0.f);
-        const float to_m = others.z / e_m, log_z = log1pf(to_m);
+        // One float for log2(e) / tau puts the same relative error on all powers of a call,
+        // which sums over many rows' logp would keep: sum 2^(t (1 + d)) is sum 2^t + d ln 2
+        // sum t 2^t to first order (d < 2^-24, t < 126).  (What ex2 loses on average,
+        // 5e-8, is in both of z and e_m.)
+        const float to_m = fmaf(a.tilt, below, others.z) / e_m, log_z = log1pf(to_m);
         const auto log_p = [&](float x) { return fmaf(x - m, a.inv_temp, -log_z); };
         if (tid == 0) {
             a.logp[r] = bad || target >= a.vocab ? NAN : log_p(row.at(target));

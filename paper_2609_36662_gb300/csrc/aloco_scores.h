@@ -13,6 +13,8 @@ struct ScoresArgs {
     const void *target;
     int target_bytes;
     float scale;                     // log2(e) / tau
+    float tilt;                      // what scale's rounding does to a sum of terms, to
+                                     // its powers times their terms: ln 2 (exact / scale - 1)
     float inv_temp;                  // 1 / tau
     int top;
     float *logp, *entropy, *top_logp;
