@@ -523,15 +523,18 @@ int aloco_adamw_step_normed(void *const *params, const void *const *grads,
  * the tensor cores: X is held as a sum of two fp16 values (22 bits), A and b A + c
  * A A in fp16 with their diagonals in fp32, sums in fp32.  The factor's error
  * against exact steps is 2e-4 to 1e-3 of its norm, 2e-3 for a matrix of rank one.
- * Where the result is bf16 and many matrices are one and a half times as wide as
- * high (or the other way), two steps are taken at a time, in products of the
- * symmetric matrices alone: 5e-4 to 2.5e-3, 3e-3 for rank one, beside a rounding of
- * 1.7e-3.  A matrix that holds NaN or inf gives NaN throughout, and no other matrix
+ * Where the result is bf16 and the matrix is large, its larger side n at least one and
+ * a half times the smaller m (and m m (n - m) >= 2^28), two steps are taken at a time,
+ * in products of the symmetric matrices alone: 5e-4 to 2.5e-3, 3e-3 for rank one,
+ * beside a rounding of 1.7e-3.  A matrix that holds NaN or inf gives NaN throughout, and no other matrix
  * is affected; zeros give zeros.  Polynomials that let singular values grow beyond
  * 200 leave fp16's range (inf or NaN).
  *
  * The calls only enqueue on opts->stream (the other options do not apply) and
- * allocate nothing on the device; results are bit-identical from call to call.
+ * allocate nothing on the device.  Results are bit-identical from call to call with
+ * the same matrices, M and types.  Beside other matrices, or on another number of
+ * replicas, a matrix goes through the same operations, whose sums may be added in
+ * another order.
  * Scratch is the caller's device memory, 256-byte aligned and not set up in any
  * way: calls that may overlap on the GPU need their own.  Every wait inside the
  * kernels is bounded (2 s, of what waits for such a wait 4 s); one that runs out

@@ -159,6 +159,17 @@ void lay_out(const Plan &plan, Pass *pass) {
     pass->all_bytes += up(pass->counters * 4, kAlign);
 }
 
+// Two steps at a time (list_operations), by the matrix's shape alone: its rounding must
+// not depend on what else a call holds.  They save 3 m m (n - m) products of the
+// two steps' and add two dependent products of m x m.  One matrix of 512 x 2048 takes
+// 188 us with them and 176 without, 1024 x 2048 244 and 232, 1500 x 2250 307 and 326,
+// 2048 x 8192 543 and 656; 64 of 512 x 2048 757 and 933, of 768 x 1536 1064 and 1235,
+// of 1024 x 1536 1711 and 1885.  Below the limit they are left out, although many of 512
+// x 1024 (64: 497 and 543) would gain: one alone loses (179 and 163).
+bool two_at_a_time(int64_t m, int64_t n) {
+    return 2 * n >= 3 * m && m * m * (n - m) >= (int64_t)1 << 28;
+}
+
 // Shapes in `p` (places set) into passes that keep within kPassBytes, kOrthoGroups
 // and kOrthoMatrices: deep products first, so that the last tiles are short.
 // Where all are small they go through the small kernel, in clusters of up to
@@ -167,14 +178,11 @@ void split(Plan *p, int workers, int most_ctas) {
     std::stable_sort(p->shapes.begin(), p->shapes.end(), [](const Shape &x, const Shape &y) {
         return x.m() != y.m() ? x.m() > y.m() : x.n() > y.n();
     });
-    // Two steps at a time, where the matrix is wide and its symmetric products fill
-    // the GPU (they take their depth alone, without X's length).
     // Norm blocks: two rounds of eight an SM, of 4096 to 65536 elements; at most 1024 of
     // a matrix.
     for (Shape &s : p->shapes) {
         const int64_t all = s.period * (int64_t)workers, size = s.rows * s.cols;
-        s.merged = 2 * s.n() >= 3 * s.m() &&
-                   all * sym_tiles(s, ortho_pair_tile()) >= kPlannedSms;
+        s.merged = two_at_a_time(s.m(), s.n());
         const int64_t each = std::min<int64_t>(65536, all * size / (kPlannedSms * 16));
         s.chunk = std::max<int64_t>(4096, (int64_t)up((size_t)std::max(each, size / 1024), 4096));
     }
