@@ -1038,7 +1038,12 @@ int aloco_sync_noalloc(float *global, float *momentum, void *const *locals,
  * what waits for it leaves NaN in the log-probabilities of that row and of the
  * block's later ones, and so in the loss; with a tile below -1 it issues its
  * first copy -tile cycles late instead (at most 8e9; no other round heeds such a
- * tile).  The hook is consumed by that round or call; no other reads it. */
+ * tile).  aloco_orthogonalize and aloco_muon_step read tiles >= 0: block 0 of the
+ * first kernel that takes products leaves out the copies of its slot `tile` (of
+ * small matrices, with any tile, the first products of the first one), and what
+ * waits for them makes NaN of the matrices that the block was at; a tile below -1
+ * they leave for the call that heeds it.  The hook is consumed by that round or
+ * call; no other reads it. */
 void aloco_test_stall_tile(int64_t tile);
 
 /* Message of the last failure on the calling thread ("" if none).  The

@@ -939,10 +939,10 @@ def orthogonalize(x, *, coefficients=(NEWTON_SCHULZ,) * 5, eps: float = 1e-7, ou
 
 
 def test_stall_tile(tile: int):
-    """Testing only: the next bulk-copy round (or post-training loss) on this
-    thread skips the copies of one tile, so that its bounded wait runs out; a
-    tile below -1 makes a loss's first copy so many cycles late
-    (aloco_test_stall_tile)."""
+    """Testing only: the next bulk-copy round (post-training loss, orthogonal
+    factor or muon step) on this thread skips the copies of one tile, so that its
+    bounded wait runs out; a tile below -1 makes a loss's first copy so many cycles
+    late (aloco_test_stall_tile)."""
     load().aloco_test_stall_tile(int(tile))
 
 

@@ -2,6 +2,8 @@
 out, and the call ends with the device usable.  The stall is requested through
 aloco_test_stall_tile: the first block leaves out the copies of one slot (of a
 small matrix: its first products)."""
+import time
+
 import pytest
 import torch
 
@@ -52,3 +54,19 @@ def test_what_is_not_nan_is_right(shape, slot, lost):
     nan = out.isnan()
     assert torch.equal(torch.where(nan, 0, out), torch.where(nan, 0, want))
     assert 1 <= int(nan.flatten(1).any(1).sum()) <= lost
+
+
+def test_a_late_copy_stays_for_the_call_that_heeds_it():
+    """2e8 cycles, 0.1 s at the highest clock."""
+    x = _batch((3, 40, 200))
+    logits = torch.randn(4, 900, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    t = torch.arange(4, device="cuda")
+    want = A.orthogonalize(x), A.token_logprobs(logits, t)
+    A.test_stall_tile(-200_000_000)
+    first = A.orthogonalize(x)
+    torch.cuda.synchronize()
+    t0 = time.perf_counter()
+    logp = A.token_logprobs(logits, t)
+    torch.cuda.synchronize()
+    assert time.perf_counter() - t0 > 0.09
+    assert torch.equal(first, want[0]) and torch.equal(logp, want[1])
