@@ -567,7 +567,7 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kSplit ? 8 
     unsigned high = share.largest;
     if constexpr (kSplit) {
         cluster_sync();
-        for (int p = 0; p < split; ++p) high = max(high, peer(share.largest, p));
+        high = __reduce_max_sync(~0u, lane < split ? peer(share.largest, lane) : 0);
     }
     const float m = high == ~0u ? NAN : unorder(high);
     const bool bad = !(fabsf(m) < INFINITY);
@@ -600,19 +600,13 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kSplit ? 8 
         });
         share_again();
     }
-    // All CTAs' sums, the same in every thread of them.
+    // All CTAs' sums, the same in every thread of them: a lane reads a CTA's.
     const auto total = [&] {
         if constexpr (!kSplit) return Sums{share.ref, share.z, share.s};
-        Sums all{peer(share.ref, 0), peer(share.z, 0), peer(share.s, 0)};
-        for (int p = 1; p < split; ++p) {
-            Sums x{peer(share.ref, p), peer(share.z, p), peer(share.s, p)};
-            const float to = fmaxf(all.ref, x.ref);
-            all.refer(to);
-            x.refer(to);
-            all.z += x.z;
-            all.s += x.s;
-        }
-        return all;
+        Sums x{-kFar, 0.f, 0.f};
+        if (lane < split) x = {peer(share.ref, lane), peer(share.z, lane), peer(share.s, lane)};
+        x.refer((float)__reduce_max_sync(~0u, (int)x.ref));
+        return Sums{x.ref, warp_sum(x.z), warp_sum(x.s)};
     };
     // The log-probability of the largest is -log(1 + r), r the other terms to it, and the
     // entropy log(1 + r) and what the others' powers lie below its own: of parts that
