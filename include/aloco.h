@@ -526,9 +526,10 @@ int aloco_adamw_step_normed(void *const *params, const void *const *grads,
  * Where the result is bf16 and the matrix is large, its larger side n at least one and
  * a half times the smaller m (and m m (n - m) >= 2^28), two steps are taken at a time,
  * in products of the symmetric matrices alone: 5e-4 to 2.5e-3, 3e-3 for rank one,
- * beside a rounding of 1.7e-3.  A matrix that holds NaN or inf gives NaN throughout, and no other matrix
- * is affected; zeros give zeros.  Polynomials that let singular values grow beyond
- * 200 leave fp16's range (inf or NaN).
+ * beside a rounding of 1.7e-3.  A matrix that holds NaN or inf gives NaN throughout,
+ * and no other matrix is affected; zeros give zeros.  Polynomials that let singular
+ * values grow beyond 200 leave fp16's range (inf or NaN).  X is kept to 2^-33: a large
+ * matrix whose norm is 1e-4 of eps or less keeps fewer digits.
  *
  * The calls only enqueue on opts->stream (the other options do not apply) and
  * allocate nothing on the device.  Results are bit-identical from call to call with

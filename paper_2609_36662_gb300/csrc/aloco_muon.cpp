@@ -109,9 +109,10 @@ size_t sums_bytes(const Shape &s, int64_t count, const std::array<int, 2> &split
 // Tiles by pairs of CTAs where the matrices' elements fill them; by single CTAs, whose
 // tiles are a quarter, below: 8 matrices of 300 x 2000 192 us by single ones and 225 by
 // pairs, 7 odd ones of 3 workers 217 and 254, where a matrix's edges count as whole
-// tiles too; 3 of 1500 x 1500 (103 tiles' elements) 333 and 302.  Where A's or P's tiles are fewer than the CTAs, parts of their
-// depth are tiles of their own: as many as there are CTAs for, of at least 12
-// slots.  (5632 x 2048 alone: 88 slots a tile of A, 36 tiles for 76 pairs.)
+// tiles too; 3 of 1500 x 1500 (103 tiles' elements) 333 and 302.  Where A's or P's tiles
+// are fewer than the CTAs, parts of their depth are tiles of their own: as many as there
+// are CTAs for, of at least 12 slots.  (5632 x 2048 alone: 88 slots a tile of A, 36 tiles
+// for 76 pairs.)
 void lay_out(const Plan &plan, Pass *pass) {
     int64_t elements = 0;
     for (const Part &part : pass->parts) {

@@ -330,12 +330,13 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity)
 // Bound by the tensor cores where matrices are large (16 x 2048 x 2048: 512 of 540
 // cycles a slot, at the clock that 1360 W leave); at 768 by the epilogue too, which
 // moves 8 bytes an element of X in and out of L2 for 12 slots of products (48 x 768
-// x 768: tensor cores 42 % busy, HBM 44 % of its peak, 7.8 GB through L2; 566 us the
-// whole call); for a few small matrices by 15 dependent products, of which each
-// takes about 10 us: 1 until it is known that its operands are there, 2 until the
-// first of them have come, 3 of products, 4 until the last tile is written.
-// A kernel for every product took 315 us in place of 254 for 7 odd matrices of 3
-// workers, 663 of 641 for 48 x 768 x 768 and 2.48 of 2.25 ms for 16 x 2048 x 2048: a
+// x 768: tensor cores 43 % busy, HBM 44 % of its peak, 7.8 GB through L2; 593 us the
+// whole call on matrices that are not in L2, 567 where they are the last call's); for a
+// few small matrices by 15 dependent products, of which each takes about 10 us: 1 until
+// it is known that its operands are there, 2 until the first of them have come, 3 of
+// products, 4 until the last tile is written.
+// When it came a kernel for every product took 315 us in place of 254 for 7 odd matrices
+// of 3 workers, 663 of 641 for 48 x 768 x 768 and 2.48 of 2.25 ms for 16 x 2048 x 2048: a
 // matrix waits for itself alone.
 //
 // A wait that runs out ends the waits of its pair.  The tiles that the pair knows of
@@ -973,7 +974,8 @@ __device__ __forceinline__ double block_sum(double s, double *shared) {
 }
 
 // Sums of squares of the matrices' stretches.
-__global__ void __launch_bounds__(kThreads) ortho_norm_kernel(const __grid_constant__ OrthoArgs args) {
+__global__ void __launch_bounds__(kThreads)
+    ortho_norm_kernel(const __grid_constant__ OrthoArgs args) {
     __shared__ double shared[kThreads / 32];
     grid_go();
     grid_wait();
@@ -1029,8 +1031,10 @@ constexpr int kPrep = 64;            // rows and columns of a prepared tile
 
 // X = U 2^8 / (|U| + eps) as a sum of two fp16 values, transposed where the matrix
 // is tall, and the new momentum.  Bound by HBM: 48 x 768 x 768 fp32 (227 MB) 51 us
-// with cold caches.  Five blocks an SM: 4 us less than four or six in a call.
-__global__ void __launch_bounds__(kThreads, 5) ortho_prepare_kernel(const __grid_constant__ OrthoArgs args) {
+// with cold caches.  Five blocks an SM (48 registers, of which it spills 24 bytes): 4 us
+// less than four or six in a call.
+__global__ void __launch_bounds__(kThreads, 5)
+    ortho_prepare_kernel(const __grid_constant__ OrthoArgs args) {
     __shared__ float s_f;            // the factor, where fp32 does for it
     __shared__ double s_factor;
     __shared__ float tile[kPrep][kPrep + 1];

@@ -81,7 +81,7 @@ struct Walk {
 // A step is a chain of latencies (three products, their fences and reads, and the
 // cluster's exchange: about 4 us, 6 with it), where the products' kernel takes 20: one
 // 2048 x 16 matrix takes 33 us in all and 4 workers' two of 512 x 64 take 47, 122 and
-// 101 there.  64 of 16 x 2048, by clusters of 8, take 174 us in four rounds.
+// 101 there.  64 of 16 x 2048, by clusters of 8, take 157 us in four rounds.
 __global__ void __launch_bounds__(kThreads, 1)
     ortho_small_kernel(const __grid_constant__ OrthoArgs args) {
     extern __shared__ char raw[];

@@ -320,8 +320,9 @@ __device__ __forceinline__ void place(const Found<kGroup> &f, int n, int k,
 }
 
 // The k best values of units [u0, u1) where a first limit leaves too many (equal
-// values throughout; everything worth having in few places): of the threads' maxima (`mine`) an exact limit that k of them reach is found by
-// bisection, and threads above it are read again.
+// values throughout; everything worth having in few places): of the threads' maxima
+// (`mine`) an exact limit that k of them reach is found by bisection, and threads above
+// it are read again.
 template <bool kBf16, int kGroup>
 __device__ __noinline__ void find_best(const Row<kBf16> &row, int u0, int u1, int k, unsigned mine,
                                        unsigned largest, Found<kGroup> &f,
@@ -403,8 +404,9 @@ __device__ __noinline__ void find_best(const Row<kBf16> &row, int u0, int u1, in
 // maxima and its sums to a whole reference.  For the alternatives the maxima give
 // a limit that k values reach, and the few batches that reach it are read again.
 //
-// kSplit: rows of more than one CTA (where there are none a split that the compiler
-// knows spills: 84 us in place of 80).
+// kSplit: rows of more than one CTA.  (Where there are none `split` stays a value that the
+// compiler does not know: one that it knows makes the loop's values spill, in fp32 still
+// and at first in bf16 too, 84 us in place of 80.)
 //
 // Bound by HBM; the steps behind a row's last unit (a limit, a few values read
 // again, their order: about 2 us) are hidden by the other CTAs of the SM, so CTAs
