@@ -176,6 +176,16 @@ __device__ __forceinline__ int64_t load_index(const void *p, int bytes, int64_t 
 // z = sum 2^t, s = sum t 2^t with t = x scale - ref.
 struct Sums {
     float ref, z, s;
+    __device__ __forceinline__ void add(float t) {
+        const float e = ex2(t);
+        z += e;
+        s = fmaf(t, e, s);
+    }
+    __device__ __forceinline__ void take_away(float t) {  // (one value alone leaves 0)
+        const float e = ex2(t);
+        z -= e;
+        s -= __fmul_rn(t, e);
+    }
     __device__ __forceinline__ void refer(float to) {   // to >= ref, both whole
         const float d = ref - to, f = pow2(d);
         s = f == 0.f ? 0.f : fmaf(d, z, s) * f;
@@ -193,7 +203,7 @@ __device__ __forceinline__ float warp_sum(float x) {
 // One CTA's share of a row, as the others of its cluster read it.
 struct Share {
     unsigned largest;
-    float ref, z, s;
+    float ref, z, s;                 // without the largest's term, where rows are split
     int owner;                       // the thread that read the row's largest value
     unsigned long long best[ALOCO_MAX_TOP];  // (order, ~index), largest first; 0: none
 };
@@ -485,13 +495,51 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kSplit ? 8 
         sums.s += s.x + s.y;
     });
 
-    // The group's.
+    // A value's power (of -inf one whose term is 0).  Logits so large that a whole
+    // reference does not do, far ones, have the largest as theirs.
+    bool far = false;
+    float m = 0.f;
+    const auto power = [&](float x, float ref) {
+        return far ? fmaxf((x - m) * a.scale, kGone) : fmaf(fmaxf(x, -0x1p96f), a.scale, -ref);
+    };
+    // The log-probability of a token that is nearly certain is what the other terms are to
+    // it, which a sum with its term has rounded away: where they are a sixteenth at most
+    // the units of the thread that had it are taken again without it.
+    const auto certain = [](float z, float e) { return z - e < kCertain * z; };
+    const auto take_again = [&](int u, int step, float without, float ref) {
+        for (; u < u1; u += step) {
+            float v[N];
+            Row<kBf16>::values(row.load(u, u1), v);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float t = power(v[i], ref), e = v[i] == without ? 0.f : ex2(t);
+                sums.z += e;
+                sums.s = fmaf(t, e, sums.s);
+            }
+        }
+    };
+    // The group's sums.  Where rows are split every warp sees to its own largest value,
+    // which costs no barrier more; else the row's is seen to below (by warps: 189 us in
+    // place of 184 for 4000 x 128256 bf16, 60 in place of 55 for 1533 x 50257 fp32; by the
+    // row where it is split: 300 x 50257 bf16, all nearly certain, 26 us in place of 20).
     const unsigned mine = nan ? ~0u : order(large.first);
     const auto combine = [&] {
         const unsigned high = __reduce_max_sync(~0u, mine);
         const int ref = __reduce_max_sync(~0u, (int)fminf(sums.ref, 2.f * kFar));
         sums.refer((float)ref);
-        const float z = warp_sum(sums.z), s = warp_sum(sums.s);
+        Sums all{(float)ref, warp_sum(sums.z), warp_sum(sums.s)};
+        if constexpr (kSplit) {
+            const float top = unorder(high), t = power(top, all.ref);
+            if (certain(all.z, ex2(t))) {
+                const int owner = __ffs(__ballot_sync(~0u, mine == high)) - 1;
+                if (lane == owner) sums.z = sums.s = 0.f;
+                take_again(u0 + tid - lane + owner + lane * kGroup, 32 * kGroup, top, all.ref);
+                all = {all.ref, warp_sum(sums.z), warp_sum(sums.s)};
+            } else {
+                all.take_away(t);
+            }
+        }
+        const float z = all.z, s = all.s;
         if constexpr (kGroup == 32) {
             if (lane == 0) {
                 share.largest = high;
@@ -519,8 +567,13 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kSplit ? 8 
                 to = fmaxf(to, warp_ref[w]);
             }
             Sums all{to, 0.f, 0.f};
+            bool missing = kSplit;   // the largest has not come yet
             for (int w = 0; w < kWarps; ++w) {
                 Sums x{warp_ref[w], warp_z[w], warp_s[w]};
+                if (missing && warp_top[w] == h)
+                    missing = false;
+                else if (kSplit)
+                    x.add(power(unorder(warp_top[w]), x.ref));
                 x.refer(to);
                 all.z += x.z;
                 all.s += x.s;
@@ -571,20 +624,9 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kSplit ? 8 
         cluster_sync();
         high = __reduce_max_sync(~0u, lane < split ? peer(share.largest, lane) : 0);
     }
-    const float m = high == ~0u ? NAN : unorder(high);
+    m = high == ~0u ? NAN : unorder(high);
     const bool bad = !(fabsf(m) < INFINITY);
-    // logits so large that a whole reference does not do
-    const bool far = !bad && fabsf(m * a.scale) > kFar;
-    // a power and its term; (values that are -inf at 2^-200, which is 0)
-    const auto power = [&](float x, float ref) {
-        return far ? fmaxf((x - m) * a.scale, kGone) : fmaf(fmaxf(x, -0x1p96f), a.scale, -ref);
-    };
-    const auto share_again = [&] {
-        __syncwarp();
-        if constexpr (kSplit) cluster_sync();  // (all have read)
-        combine();
-        if constexpr (kSplit) cluster_sync();
-    };
+    far = !bad && fabsf(m * a.scale) > kFar;
     if (far) {
         sums = {0.f, 0.f, 0.f};
         pass([&](const uint4 (&q)[kBatch], int, int) {
@@ -600,59 +642,55 @@ __global__ void __launch_bounds__(cta_of(kGroup), kGroup == 32 ? 4 : kSplit ? 8 
                 }
             }
         });
-        share_again();
+        if constexpr (kSplit) cluster_sync();  // (all have read)
+        combine();
+        if constexpr (kSplit) cluster_sync();
     }
-    // All CTAs' sums, the same in every thread of them: a lane reads a CTA's.
-    const auto total = [&] {
-        if constexpr (!kSplit) return Sums{share.ref, share.z, share.s};
-        Sums x{-kFar, 0.f, 0.f};
-        if (lane < split) x = {peer(share.ref, lane), peer(share.z, lane), peer(share.s, lane)};
-        x.refer((float)__reduce_max_sync(~0u, (int)x.ref));
-        return Sums{x.ref, warp_sum(x.z), warp_sum(x.s)};
-    };
-    // The log-probability of the largest is -log(1 + r), r the other terms to it, and the
-    // entropy log(1 + r) and what the others' powers lie below its own: of parts that
-    // are not below 0, so that neither has the wrong sign where one token has all.
-    Sums others = total();           // but for the largest's term, presently
-    const float t_m = power(m, others.ref), e_m = ex2(t_m);
-    if (!bad && others.z - e_m < kCertain * others.z) {
-        // Of a token that is nearly certain r is what a sum with its term has rounded away:
-        // the units of the thread that had it are taken again without it.  (8 x 1023 x 32000
-        // bf16, of which 12 % are such rows: 80.0 us, 78.1 with the sum of all; 81.1 where
-        // the limit is an eighth.)
-        sums.refer(others.ref);
-        if (mine == high) {
-            share.owner = tid;
-            sums.z = sums.s = 0.f;
+    // The other terms' sums.
+    Sums others{-kFar, 0.f, 0.f};
+    if constexpr (kSplit) {          // a lane reads a CTA's
+        const unsigned top = lane < split ? peer(share.largest, lane) : 0;
+        const int first = __ffs(__ballot_sync(~0u, top == high)) - 1;
+        if (lane < split) {
+            others = {peer(share.ref, lane), peer(share.z, lane), peer(share.s, lane)};
+            if (lane != first) others.add(power(unorder(top), others.ref));
         }
-        G::sync();
-        if (share.largest == high) {
-            for (int u = u0 + share.owner + tid * kGroup; u < u1; u += kGroup * kGroup) {
-                float v[N];
-                Row<kBf16>::values(row.load(u, u1), v);
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const float t = power(v[i], others.ref), e = v[i] == m ? 0.f : ex2(t);
-                    sums.z += e;
-                    sums.s = fmaf(t, e, sums.s);
-                }
-            }
-        }
-        share_again();
-        others = total();
+        others.refer((float)__reduce_max_sync(~0u, (int)others.ref));
+        others.z = warp_sum(others.z);
+        others.s = warp_sum(others.s);
     } else {
-        others.z -= e_m;
-        others.s -= __fmul_rn(t_m, e_m);  // (as it was added: one value alone leaves 0)
+        others = {share.ref, share.z, share.s};
     }
-    // (of a row of one CTA the first warp does the rest)
-    if (!kSplit && warp) return;
+    const float t_m = power(m, others.ref), e_m = ex2(t_m);
+    if constexpr (!kSplit) {
+        // (8 x 1023 x 32000 bf16, of which 12 % are nearly certain: 80.0 us, 78.1 with the
+        // sum of all; 81.1 where the limit is an eighth)
+        if (!bad && certain(others.z, e_m)) {
+            sums.refer(others.ref);
+            if (mine == high) {
+                share.owner = tid;
+                sums.z = sums.s = 0.f;
+            }
+            G::sync();
+            take_again(u0 + share.owner + tid * kGroup, kGroup * kGroup, m, others.ref);
+            __syncwarp();
+            combine();
+            others = {share.ref, share.z, share.s};
+        } else {
+            others.take_away(t_m);
+        }
+        if (warp) return;            // the first warp does the rest
+    }
     if (rank == 0) {
         if constexpr (kTop && kSplit) {
             for (int i = tid; i < split * a.top; i += kGroup)
                 found.value[i] = peer(share.best[i % a.top], i / a.top);
             __syncthreads();
         }
-        // sum (t_j - t_m) 2^t_j over the others, which is not above 0
+        // The log-probability of the largest is -log(1 + r), r the other terms to it, and the
+        // entropy log(1 + r) and what the others' powers lie below its own: of parts that
+        // are not below 0, so that neither has the wrong sign where one token has all.
+        // (sum (t_j - t_m) 2^t_j over the others, which is not above 0)
         const float below = fminf(fmaf(-t_m, others.z, others.s), 0.f);
         // One float for log2(e) / tau puts the same relative error on all powers of a call,
         // which sums over many rows' logp would keep: sum 2^(t (1 + d)) is sum 2^t + d ln 2
