@@ -535,7 +535,8 @@ int aloco_adamw_step_normed(void *const *params, const void *const *grads,
  * allocate nothing on the device.  Results are bit-identical from call to call with
  * the same matrices, M and types.  Beside other matrices, or on another number of
  * replicas, a matrix goes through the same operations, whose sums may be added in
- * another order.
+ * another order; small ones (m <= 128, n <= 2048 or 4096) go through a kernel of their
+ * own where the call has no larger ones, with the same bounds.
  * Scratch is the caller's device memory, 256-byte aligned and not set up in any
  * way: calls that may overlap on the GPU need their own.  Every wait inside the
  * kernels is bounded (2 s, of what waits for such a wait 4 s); one that runs out

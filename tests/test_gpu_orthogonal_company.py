@@ -1,5 +1,5 @@
-"""A matrix's factor does not depend on what else a call holds: the same operations in
-the same precision, whatever matrices, replicas or passes are beside it."""
+"""Whether a matrix takes two steps at a time, and so its factor's precision, does not
+depend on what else a call holds: whatever matrices, replicas or passes are beside it."""
 import pytest
 import torch
 
